@@ -329,6 +329,143 @@ hla_status ahla_step(const void *q, const void *k, const void *v, void *out, hla
                      float *state, hla_stream_t stream);
 
 /*
+ * Around the mixers: a short convolution, a selective scan, norms with rotation
+ * ------------------------------------------------------------------------------
+ * The operators below stand before and beside the HLA mixers in one layer (no
+ * counterpart in the paper).  They read and write rows of projections, so a
+ * token tensor is given by a base pointer and a row stride in elements: token t
+ * of sequence b is row b*n + t (the step functions: row b), and a row holds its
+ * heads or channels contiguously.  A row stride is at least the row's width, so
+ * a tensor may be a slice of a wider projection.  No alignment beyond the
+ * element's is asked of these rows (16-byte aligned rows take the wide path);
+ * [B, H, n, d] tensors, fp32 states and tables are 16-byte aligned.
+ * lengths: device int32 [B] or NULL (= n everywhere), clamped to 0..n: tokens at
+ * and after a sequence's length are not read, give zeros in the outputs, and
+ * leave the state as it is.
+ * A buffer that is written may not overlap one that is read, except where said.
+ */
+
+/*
+ * hla_conv_forward -- causal depthwise convolution of a few taps:
+ *   pre_t = bias + sum_{j<width} w[c][j] x_{t-(width-1)+j},
+ *   out_t = pre_t * sigmoid(pre_t) if silu, else pre_t,
+ * rows before the first being state_in's.
+ * x      : device [B, n, C], row stride x_stride, of type dt
+ * w      : device [C, width] of type dt; bias: device [C] of type dt, or NULL (= 0)
+ * out    : device [B, n, C], row stride out_stride (written)
+ * state_in  : device [B, width-1, C] of type dt, the rows before the call, or NULL (= 0)
+ * state_out : device [B, width-1, C] of type dt or NULL; receives the last
+ *             width-1 rows (after lengths[b] tokens).  May equal state_in.
+ * width in {2, 3, 4}.  Errors: HLA_ERR_INVALID_ARGUMENT, HLA_ERR_UNSUPPORTED
+ * before anything is launched, HLA_ERR_CUDA.
+ */
+hla_status hla_conv_forward(const void *x, const void *w, const void *bias, void *out, hla_dtype dt, int B, int n,
+                            int C, int width, long long x_stride, long long out_stride, int silu, const int *lengths,
+                            const void *state_in, void *state_out, hla_stream_t stream);
+
+/*
+ * hla_conv_step -- hla_conv_forward of one token a sequence, the state updated
+ * in place.  x, out: device [B, C], row strides x_stride, out_stride (out may
+ * equal x); state: device [B, width-1, C] of type dt.
+ */
+hla_status hla_conv_step(const void *x, const void *w, const void *bias, void *out, hla_dtype dt, int B, int C,
+                         int width, long long x_stride, long long out_stride, int silu, void *state,
+                         hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_conv_backward needs (0 if unsupported). */
+size_t hla_conv_backward_workspace_bytes(int B, int n, int C, int width, hla_dtype dt);
+
+/*
+ * hla_conv_backward -- gradients of hla_conv_forward (from a zero state) for
+ * L = sum dout . out:  dx, dw and, if not NULL, dbias.
+ * dout: device [B, n, C], row stride dout_stride; dx: device [B, n, C], row stride
+ * dx_stride (written); dw: device fp32 [C, width] (written); dbias: device fp32
+ * [C] or NULL.  Weight gradients are summed in a fixed order: equal inputs give
+ * equal bits.  workspace: 256-byte aligned.
+ */
+hla_status hla_conv_backward(const void *x, const void *w, const void *bias, const void *dout, void *dx, float *dw,
+                             float *dbias, hla_dtype dt, int B, int n, int C, int width, long long x_stride,
+                             long long dout_stride, long long dx_stride, int silu, const int *lengths,
+                             void *workspace, size_t workspace_bytes, hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_ssm_forward needs (0 if unsupported). */
+size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dtype dt);
+
+/*
+ * hla_ssm_forward -- selective state space scan over a prompt.  Per head h of
+ * group g = h / (H / G), with the N x P state s:
+ *   delta_t = softplus(raw_t + delta_bias_h)   (raw_t + delta_bias_h if softplus == 0)
+ *   s_t = exp(a_h delta_t) s_{t-1} + delta_t b_t x_t^T,   y_t = s_t^T c_t + skip_h x_t
+ * x, y  : device [B, n, H, P], row strides x_stride, y_stride, of type dt
+ * delta : device [B, n, H], row stride delta_stride, of type dt (the raw step sizes)
+ * b, c  : device [B, n, G, N], row strides b_stride, c_stride, of type dt
+ * a     : device fp32 [H], not above 0 (with delta not below 0: the state does not grow)
+ * skip, delta_bias : device fp32 [H] or NULL (= 0)
+ * state_in  : device fp32 [B, H, N, P] or NULL (= 0)
+ * state_out : device fp32 [B, H, N, P] or NULL; the state after lengths[b] tokens.
+ *             May equal state_in.
+ * P, N in {16, 32, 64, 128}; H a multiple of G.
+ * workspace : at least hla_ssm_workspace_bytes(...) bytes, 256-byte aligned; calls
+ *             that share one are ordered on one stream; hla_poll_error reads its flag.
+ * Finite inputs are assumed: a NaN or infinity in a token may also reach the
+ * outputs of earlier tokens of its 128-token tile.
+ */
+hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, const void *b, const void *c,
+                           const float *skip, const float *delta_bias, void *y, hla_dtype dt, int B, int n, int H,
+                           int P, int G, int N, long long x_stride, long long delta_stride, long long b_stride,
+                           long long c_stride, long long y_stride, int softplus, const int *lengths,
+                           const float *state_in, float *state_out, void *workspace, size_t workspace_bytes,
+                           hla_stream_t stream);
+
+/*
+ * hla_ssm_step -- hla_ssm_forward of one token a sequence: x, y [B, H, P], delta
+ * [B, H], b, c [B, G, N] with their row strides; state fp32 [B, H, N, P], updated
+ * in place.  y may equal x.  No workspace.
+ */
+hla_status hla_ssm_step(const void *x, const void *delta, const float *a, const void *b, const void *c,
+                        const float *skip, const float *delta_bias, void *y, hla_dtype dt, int B, int H, int P, int G,
+                        int N, long long x_stride, long long delta_stride, long long b_stride, long long c_stride,
+                        long long y_stride, int softplus, float *state, hla_stream_t stream);
+
+/*
+ * hla_qk_norm_forward -- RMS norm of every query and key head, the rotation of
+ * its first rot components by the token's position, and the change of layout to
+ * the one the mixers read:
+ *   y = x / sqrt(mean(x^2) + eps) * w                          (over the d components)
+ *   out_i = y_i cos - y_j sin,  out_j = y_j cos + y_i sin      for each pair (i, j)
+ * pairs (i, i + rot/2), or (2i, 2i+1) if interleaved; pair i takes column i of the
+ * tables.  q has H heads, k has Hk; key head h is written for the H/Hk query
+ * heads h*H/Hk .. that share it.
+ * q, k  : device [B, n, H, d], [B, n, Hk, d], row strides q_stride, k_stride
+ * wq, wk: device [d] of type dt, or NULL (= 1)
+ * cos, sin : device fp32 [table_rows, rot/2] (NULL if rot == 0), 16-byte aligned
+ * positions: device int32 [B, n], the tables' rows; NULL: token t has row pos0 + t.
+ *            A position outside the tables gives NaN in the rotated components.
+ * q_out, k_out : device [B, H, n, d] of type dt, 16-byte aligned (written)
+ * d in {16, 32, 64, 128}; rot a multiple of 8, 0..d; H a multiple of Hk; eps >= 0.
+ */
+hla_status hla_qk_norm_forward(const void *q, const void *k, const void *wq, const void *wk, const float *cos,
+                               const float *sin, const int *positions, void *q_out, void *k_out, hla_dtype dt, int B,
+                               int n, int H, int Hk, int d, int rot, int interleaved, long long q_stride,
+                               long long k_stride, int pos0, int table_rows, float eps, hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_qk_norm_backward needs (0 if unsupported). */
+size_t hla_qk_norm_backward_workspace_bytes(int B, int n, int H, int Hk, int d, hla_dtype dt);
+
+/*
+ * hla_qk_norm_backward -- gradients of hla_qk_norm_forward: dq, dk (rows like q,
+ * k, strides dq_stride, dk_stride) and the weights' dwq, dwk (device fp32 [d] or
+ * NULL) from dq_out, dk_out [B, H, n, d].  A key head's gradient is the sum over
+ * the query heads that share it.  Sums in a fixed order: equal inputs give equal bits.
+ */
+hla_status hla_qk_norm_backward(const void *q, const void *k, const void *wq, const void *wk, const float *cos,
+                                const float *sin, const int *positions, const void *dq_out, const void *dk_out,
+                                void *dq, void *dk, float *dwq, float *dwk, hla_dtype dt, int B, int n, int H, int Hk,
+                                int d, int rot, int interleaved, long long q_stride, long long k_stride,
+                                long long dq_stride, long long dk_stride, int pos0, int table_rows, float eps,
+                                void *workspace, size_t workspace_bytes, hla_stream_t stream);
+
+/*
  * hla_poll_error_noalloc -- hla_poll_error for hla2_forward_noalloc (no
  * counterpart in the paper): waits for `stream`, then reports and clears the
  * device-side error word of the library's scratch array on the current device:

@@ -120,4 +120,72 @@ bool hla3_tc_applicable(const Fwd2 &p);
 int hla3_tc_launches(int BH, int n);
 cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 
+// short causal convolution (hla_conv.cu); strides are row strides in elements
+struct Conv {
+    const void *x, *w, *bias;
+    void *out;
+    hla_dtype dt;
+    int B, n, C, width, silu;
+    long long x_stride, out_stride;
+    const int *lengths;
+    const void *state_in;
+    void *state_out;  // the step's state, updated in place
+};
+struct ConvBwd {
+    const void *x, *w, *bias, *dout;
+    void *dx;
+    float *dw, *dbias;
+    hla_dtype dt;
+    int B, n, C, width, silu;
+    long long x_stride, dout_stride, dx_stride;
+    const int *lengths;
+    float *partial;
+    WsHeader *header;
+};
+cudaError_t conv_forward_launch(const Conv &p, cudaStream_t stream);
+cudaError_t conv_step_launch(const Conv &p, cudaStream_t stream);
+size_t conv_backward_partial_floats(int B, int n, int C, int width);
+cudaError_t conv_backward_launch(const ConvBwd &p, cudaStream_t stream);
+
+// selective state space scan
+struct Ssm {
+    const void *x, *delta, *b, *c;
+    const float *a, *skip, *delta_bias;
+    void *y;
+    hla_dtype dt;
+    int B, n, H, P, G, N, softplus;
+    long long x_stride, delta_stride, b_stride, c_stride, y_stride;
+    const int *lengths;
+    const float *state_in;
+    float *state_out;  // the step's state, updated in place
+    char *ws;          // workspace base (header included)
+};
+size_t ssm_scan_workspace_floats(const Ssm &p);
+cudaError_t ssm_scan_launch(const Ssm &p, cudaStream_t stream);
+cudaError_t ssm_step_launch(const Ssm &p, cudaStream_t stream);
+
+// norm of queries and keys for each head with the position rotation
+struct QkNorm {
+    const void *q, *k, *wq, *wk;
+    const float *cos, *sin;
+    const int *positions;
+    void *q_out, *k_out;
+    hla_dtype dt;
+    int B, n, H, Hk, d, rot, interleaved;
+    long long q_stride, k_stride;
+    int pos0, table_rows;
+    float eps;
+};
+struct QkNormBwd {
+    QkNorm f;  // q_out, k_out unused
+    const void *dq_out, *dk_out;
+    void *dq, *dk;
+    long long dq_stride, dk_stride;
+    float *dwq, *dwk, *partial;
+    WsHeader *header;
+};
+cudaError_t qk_norm_forward_launch(const QkNorm &p, cudaStream_t stream);
+size_t qk_norm_partial_floats(int B, int n, int H, int Hk, int d);
+cudaError_t qk_norm_backward_launch(const QkNormBwd &p, cudaStream_t stream);
+
 }  // namespace hla

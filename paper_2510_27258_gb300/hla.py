@@ -25,7 +25,10 @@ EXPORTS = ("hla_status_string", "hla_last_error", "hla2_state_floats", "hla2_wor
            "hla3_forward_path", "hla2_backward_path",
            "hla2_forward_noalloc", "hla_poll_error_noalloc", "hla_poll_error", "hla2_sde_state_floats",
            "hla2_state_to_sde", "hla2_step_sde", "ahla_state_floats", "ahla_workspace_bytes", "ahla_forward",
-           "ahla_step", "hla2_backward_workspace_bytes", "hla2_backward", "ahla_forward_path")
+           "ahla_step", "hla2_backward_workspace_bytes", "hla2_backward", "ahla_forward_path",
+           "hla_conv_forward", "hla_conv_step", "hla_conv_backward_workspace_bytes", "hla_conv_backward",
+           "hla_ssm_workspace_bytes", "hla_ssm_forward", "hla_ssm_step", "hla_qk_norm_forward",
+           "hla_qk_norm_backward_workspace_bytes", "hla_qk_norm_backward")
 
 _lib = None
 
@@ -89,6 +92,23 @@ def lib():
         L.hla2_state_to_sde.restype = i
         L.hla2_step_sde.argtypes = [vp, vp, vp, vp, i, i, i, i, i, i, f, vp, vp]
         L.hla2_step_sde.restype = i
+        ll = ctypes.c_longlong
+        L.hla_conv_forward.argtypes = [vp] * 4 + [i] * 5 + [ll, ll, i] + [vp] * 4
+        L.hla_conv_step.argtypes = [vp] * 4 + [i] * 4 + [ll, ll, i] + [vp] * 2
+        L.hla_conv_backward_workspace_bytes.argtypes = [i] * 5
+        L.hla_conv_backward.argtypes = [vp] * 7 + [i] * 5 + [ll] * 3 + [i, vp, vp, sz, vp]
+        L.hla_ssm_workspace_bytes.argtypes = [i] * 7
+        L.hla_ssm_forward.argtypes = [vp] * 8 + [i] * 7 + [ll] * 5 + [i] + [vp] * 4 + [sz, vp]
+        L.hla_ssm_step.argtypes = [vp] * 8 + [i] * 6 + [ll] * 5 + [i, vp, vp]
+        L.hla_qk_norm_forward.argtypes = [vp] * 9 + [i] * 8 + [ll, ll, i, i, f, vp]
+        L.hla_qk_norm_backward_workspace_bytes.argtypes = [i] * 6
+        L.hla_qk_norm_backward.argtypes = [vp] * 13 + [i] * 8 + [ll] * 4 + [i, i, f, vp, sz, vp]
+        for name in ("hla_conv_backward_workspace_bytes", "hla_ssm_workspace_bytes",
+                     "hla_qk_norm_backward_workspace_bytes"):
+            getattr(L, name).restype = sz
+        for name in ("hla_conv_forward", "hla_conv_step", "hla_conv_backward", "hla_ssm_forward", "hla_ssm_step",
+                     "hla_qk_norm_forward", "hla_qk_norm_backward"):
+            getattr(L, name).restype = i
         _lib = L
     return _lib
 
@@ -354,3 +374,277 @@ def hla_poll_error_noalloc(stream=None) -> int:
 def hla_poll_error(workspace, stream=None) -> int:
     """Synchronise and read the device-side error flag of a workspace (include/hla.h: hla_poll_error)."""
     return int(lib().hla_poll_error(_ptr(workspace), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# the operators around the mixers: short convolution, selective scan, q/k norm with rotation
+# ------------------------------------------------------------------------------------------------
+
+def _type_code(dtype) -> int:
+    if isinstance(dtype, int):
+        return dtype
+    if dtype == torch.bfloat16:
+        return HLA_BF16
+    if dtype == torch.float32:
+        return HLA_F32
+    raise TypeError("tokens must be bfloat16 or float32, got %s" % dtype)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _like(name, t, shape, dtype, device):
+    """Checks a contiguous tensor's (or None's) shape, type and device."""
+    if t is None:
+        return
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on %s, got %s %s on %s"
+                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+
+
+def _row_stride(name, t, lead, shape, dtype, device):
+    """Row stride (elements) of a token tensor of `lead` leading dimensions whose rows are contiguous and
+    equally spaced; raises where they are not."""
+    if t.shape != shape or t.dtype != dtype or t.device != device:
+        raise ValueError("%s must be a %s tensor %s on %s, got %s %s on %s"
+                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    st, width = t.stride(), 1
+    for j in range(len(shape) - 1, lead - 1, -1):
+        if st[j] != width and shape[j] > 1:
+            raise ValueError("%s: the elements of a row must be contiguous, got strides %s" % (name, st))
+        width *= shape[j]
+    if lead == 1:
+        return st[0] if shape[0] > 1 else width
+    if shape[1] > 1:
+        row = st[1]
+        if shape[0] > 1 and st[0] != shape[1] * row:
+            raise ValueError("%s: rows must be equally spaced over batch and tokens, got strides %s" % (name, st))
+        return row
+    return st[0] if shape[0] > 1 else width
+
+
+def _need_cuda(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be CUDA tensors, got one on %s" % t.device)
+    return t.device
+
+
+def _on(stream, device):
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _scratch(workspace, nbytes, device):
+    if workspace is None:
+        workspace = alloc_workspace(nbytes, device)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on %s" % device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None, state_in=None, state_out=None,
+                     stream=None):
+    """Short causal depthwise convolution over a prompt (include/hla.h: hla_conv_forward).  Returns ``out``.
+
+    x: [B, n, C], rows may be slices of wider rows; weight: [C, width]; bias: [C]; lengths: int32 [B];
+    states: [B, width - 1, C] (state_out may be state_in).
+    """
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be [B, n, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
+    dev, T = _need_cuda(x), x.dtype
+    B, n, C = x.shape
+    W = weight.shape[1]
+    dt = _type_code(T)
+    if out is None:
+        out = torch.empty((B, n, C), dtype=T, device=dev)
+    xs, os_ = _row_stride("x", x, 2, (B, n, C), T, dev), _row_stride("out", out, 2, (B, n, C), T, dev)
+    _like("weight", weight, (C, W), T, dev)
+    _like("bias", bias, (C,), T, dev)
+    _like("lengths", lengths, (B,), torch.int32, dev)
+    _like("state_in", state_in, (B, W - 1, C), T, dev)
+    _like("state_out", state_out, (B, W - 1, C), T, dev)
+    _check(lib().hla_conv_forward(x.data_ptr(), weight.data_ptr(), _at(bias), out.data_ptr(), dt, B, n, C, W, xs, os_,
+                                  int(silu), _at(lengths), _at(state_in), _at(state_out), _on(stream, dev)),
+           "hla_conv_forward")
+    return out
+
+
+def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=None):
+    """One token a sequence of hla_conv_forward (include/hla.h: hla_conv_step); ``state`` [B, width - 1, C] is
+    updated in place.  x: [B, C]; ``out`` may be ``x``."""
+    if x.dim() != 2 or weight.dim() != 2:
+        raise ValueError("x must be [B, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
+    dev, T = _need_cuda(x), x.dtype
+    B, C = x.shape
+    W = weight.shape[1]
+    dt = _type_code(T)
+    if out is None:
+        out = torch.empty((B, C), dtype=T, device=dev)
+    xs, os_ = _row_stride("x", x, 1, (B, C), T, dev), _row_stride("out", out, 1, (B, C), T, dev)
+    _like("weight", weight, (C, W), T, dev)
+    _like("bias", bias, (C,), T, dev)
+    _like("state", state, (B, W - 1, C), T, dev)
+    _check(lib().hla_conv_step(x.data_ptr(), weight.data_ptr(), _at(bias), out.data_ptr(), dt, B, C, W, xs, os_,
+                               int(silu), state.data_ptr(), _on(stream, dev)), "hla_conv_step")
+    return out
+
+
+def hla_conv_backward_workspace_bytes(B, n, C, width, dtype) -> int:
+    return int(lib().hla_conv_backward_workspace_bytes(B, n, C, width, _type_code(dtype)))
+
+
+def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths=None, workspace=None, stream=None):
+    """Gradients (dx, dweight, dbias) of sum(dout * out) for hla_conv_forward from a zero state
+    (include/hla.h: hla_conv_backward); the weights' are fp32, dbias is None where bias is."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x must be [B, n, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
+    dev, T = _need_cuda(x), x.dtype
+    B, n, C = x.shape
+    W = weight.shape[1]
+    dt = _type_code(T)
+    if dx is None:
+        dx = torch.empty((B, n, C), dtype=T, device=dev)
+    xs, gs, ds = (_row_stride(name, t, 2, (B, n, C), T, dev) for name, t in (("x", x), ("dout", dout), ("dx", dx)))
+    _like("weight", weight, (C, W), T, dev)
+    _like("bias", bias, (C,), T, dev)
+    _like("lengths", lengths, (B,), torch.int32, dev)
+    dw = torch.empty((C, W), dtype=torch.float32, device=dev)
+    db = None if bias is None else torch.empty((C,), dtype=torch.float32, device=dev)
+    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
+                            hla_conv_backward_workspace_bytes(B, n, C, W, dt), dev)
+    _check(lib().hla_conv_backward(x.data_ptr(), weight.data_ptr(), _at(bias), dout.data_ptr(), dx.data_ptr(),
+                                   dw.data_ptr(), _at(db), dt, B, n, C, W, xs, gs, ds, int(silu), _at(lengths),
+                                   ws.data_ptr(), ws_bytes, _on(stream, dev)), "hla_conv_backward")
+    return dx, dw, db
+
+
+def hla_ssm_workspace_bytes(B, n, H, P, G, N, dtype) -> int:
+    return int(lib().hla_ssm_workspace_bytes(B, n, H, P, G, N, _type_code(dtype)))
+
+
+def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, softplus=True, lengths=None,
+                    state_in=None, state_out=None, workspace=None, stream=None):
+    """Selective state space scan over a prompt (include/hla.h: hla_ssm_forward).  Returns ``out``.
+
+    x: [B, n, H, P]; delta: [B, n, H]; b, c: [B, n, G, N] (rows of all four may be slices of wider rows);
+    a, skip, delta_bias: fp32 [H]; lengths: int32 [B]; states: fp32 [B, H, N, P] (state_out may be state_in).
+    """
+    if x.dim() != 4 or b.dim() != 4:
+        raise ValueError("x must be [B, n, H, P] and b [B, n, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
+    dev, T = _need_cuda(x), x.dtype
+    B, n, H, P = x.shape
+    G, N = b.shape[2:]
+    dt, f32 = _type_code(T), torch.float32
+    if out is None:
+        out = torch.empty((B, n, H, P), dtype=T, device=dev)
+    xs, ys = _row_stride("x", x, 2, (B, n, H, P), T, dev), _row_stride("out", out, 2, (B, n, H, P), T, dev)
+    ds = _row_stride("delta", delta, 2, (B, n, H), T, dev)
+    bs, cs = _row_stride("b", b, 2, (B, n, G, N), T, dev), _row_stride("c", c, 2, (B, n, G, N), T, dev)
+    for name, t in (("a", a), ("skip", skip), ("delta_bias", delta_bias)):
+        _like(name, t, (H,), f32, dev)
+    _like("lengths", lengths, (B,), torch.int32, dev)
+    _like("state_in", state_in, (B, H, N, P), f32, dev)
+    _like("state_out", state_out, (B, H, N, P), f32, dev)
+    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
+                            hla_ssm_workspace_bytes(B, n, H, P, G, N, dt), dev)
+    _check(lib().hla_ssm_forward(x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(), _at(skip),
+                                 _at(delta_bias), out.data_ptr(), dt, B, n, H, P, G, N, xs, ds, bs, cs, ys,
+                                 int(softplus), _at(lengths), _at(state_in), _at(state_out), ws.data_ptr(), ws_bytes,
+                                 _on(stream, dev)), "hla_ssm_forward")
+    return out
+
+
+def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=None, softplus=True, stream=None):
+    """One token a sequence of hla_ssm_forward (include/hla.h: hla_ssm_step); ``state`` fp32 [B, H, N, P] is
+    updated in place.  x: [B, H, P]; delta: [B, H]; b, c: [B, G, N]; ``out`` may be ``x``."""
+    if x.dim() != 3 or b.dim() != 3:
+        raise ValueError("x must be [B, H, P] and b [B, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
+    dev, T = _need_cuda(x), x.dtype
+    B, H, P = x.shape
+    G, N = b.shape[1:]
+    dt, f32 = _type_code(T), torch.float32
+    if out is None:
+        out = torch.empty((B, H, P), dtype=T, device=dev)
+    xs, ys = _row_stride("x", x, 1, (B, H, P), T, dev), _row_stride("out", out, 1, (B, H, P), T, dev)
+    ds = _row_stride("delta", delta, 1, (B, H), T, dev)
+    bs, cs = _row_stride("b", b, 1, (B, G, N), T, dev), _row_stride("c", c, 1, (B, G, N), T, dev)
+    for name, t in (("a", a), ("skip", skip), ("delta_bias", delta_bias)):
+        _like(name, t, (H,), f32, dev)
+    _like("state", state, (B, H, N, P), f32, dev)
+    _check(lib().hla_ssm_step(x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(), _at(skip),
+                              _at(delta_bias), out.data_ptr(), dt, B, H, P, G, N, xs, ds, bs, cs, ys, int(softplus),
+                              state.data_ptr(), _on(stream, dev)), "hla_ssm_step")
+    return out
+
+
+def _qk_sizes(q, k, wq, wk, cos, sin, positions):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q must be [B, n, H, d] and k [B, n, Hk, d], got %s and %s" % (tuple(q.shape), tuple(k.shape)))
+    dev, T = _need_cuda(q), q.dtype
+    B, n, H, d = q.shape
+    Hk = k.shape[2]
+    qs, ks = _row_stride("q", q, 2, (B, n, H, d), T, dev), _row_stride("k", k, 2, (B, n, Hk, d), T, dev)
+    _like("wq", wq, (d,), T, dev)
+    _like("wk", wk, (d,), T, dev)
+    rot, top = 0, 0
+    if cos is not None:
+        if cos.dim() != 2 or sin is None:
+            raise ValueError("cos and sin must both be [rows, rot / 2]")
+        top, rot = cos.shape[0], 2 * cos.shape[1]
+        _like("cos", cos, cos.shape, torch.float32, dev)
+        _like("sin", sin, cos.shape, torch.float32, dev)
+    _like("positions", positions, (B, n), torch.int32, dev)
+    return dev, T, B, n, H, Hk, d, rot, top, qs, ks
+
+
+def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, k_out=None, *, positions=None, pos0=0,
+                        eps=1e-6, interleaved=False, stream=None):
+    """Norm of every query and key head and rotation by position, into the mixers' layout
+    (include/hla.h: hla_qk_norm_forward).  Returns (q_out, k_out), both [B, H, n, d].
+
+    q: [B, n, H, d]; k: [B, n, Hk, d] (rows may be slices of wider rows); wq, wk: [d]; cos, sin: fp32
+    [rows, rot / 2]; positions: int32 [B, n], or None for pos0, pos0 + 1, ...
+    """
+    dev, T, B, n, H, Hk, d, rot, top, qs, ks = _qk_sizes(q, k, wq, wk, cos, sin, positions)
+    if q_out is None:
+        q_out = torch.empty((B, H, n, d), dtype=T, device=dev)
+    if k_out is None:
+        k_out = torch.empty((B, H, n, d), dtype=T, device=dev)
+    _like("q_out", q_out, (B, H, n, d), T, dev)
+    _like("k_out", k_out, (B, H, n, d), T, dev)
+    _check(lib().hla_qk_norm_forward(q.data_ptr(), k.data_ptr(), _at(wq), _at(wk), _at(cos), _at(sin), _at(positions),
+                                     q_out.data_ptr(), k_out.data_ptr(), _type_code(T), B, n, H, Hk, d, rot,
+                                     int(interleaved), qs, ks, int(pos0), top, float(eps), _on(stream, dev)),
+           "hla_qk_norm_forward")
+    return q_out, k_out
+
+
+def hla_qk_norm_backward_workspace_bytes(B, n, H, Hk, d, dtype) -> int:
+    return int(lib().hla_qk_norm_backward_workspace_bytes(B, n, H, Hk, d, _type_code(dtype)))
+
+
+def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=None, *, positions=None, pos0=0, eps=1e-6,
+                         interleaved=False, workspace=None, stream=None):
+    """Gradients (dq, dk, dwq, dwk) of sum(dq_out * q_out) + sum(dk_out * k_out) for hla_qk_norm_forward
+    (include/hla.h: hla_qk_norm_backward); dwq, dwk are fp32 [d], None where the weight is."""
+    dev, T, B, n, H, Hk, d, rot, top, qs, ks = _qk_sizes(q, k, wq, wk, cos, sin, positions)
+    _like("dq_out", dq_out, (B, H, n, d), T, dev)
+    _like("dk_out", dk_out, (B, H, n, d), T, dev)
+    if dq is None:
+        dq = torch.empty((B, n, H, d), dtype=T, device=dev)
+    if dk is None:
+        dk = torch.empty((B, n, Hk, d), dtype=T, device=dev)
+    dqs, dks = _row_stride("dq", dq, 2, (B, n, H, d), T, dev), _row_stride("dk", dk, 2, (B, n, Hk, d), T, dev)
+    dwq = None if wq is None else torch.empty((d,), dtype=torch.float32, device=dev)
+    dwk = None if wk is None else torch.empty((d,), dtype=torch.float32, device=dev)
+    dt = _type_code(T)
+    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
+                            hla_qk_norm_backward_workspace_bytes(B, n, H, Hk, d, dt), dev)
+    _check(lib().hla_qk_norm_backward(q.data_ptr(), k.data_ptr(), _at(wq), _at(wk), _at(cos), _at(sin),
+                                      _at(positions), dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(),
+                                      dk.data_ptr(), _at(dwq), _at(dwk), dt, B, n, H, Hk, d, rot, int(interleaved), qs,
+                                      ks, dqs, dks, int(pos0), top, float(eps), ws.data_ptr(), ws_bytes,
+                                      _on(stream, dev)), "hla_qk_norm_backward")
+    return dq, dk, dwq, dwk
