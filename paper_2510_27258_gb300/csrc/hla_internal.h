@@ -163,6 +163,13 @@ struct Ssm {
 size_t ssm_scan_workspace_floats(const Ssm &p);
 cudaError_t ssm_scan_launch(const Ssm &p, cudaStream_t stream);
 cudaError_t ssm_step_launch(const Ssm &p, cudaStream_t stream);
+// replaces each segment's own state by the state before it (`heads` x `segments` x NP floats)
+cudaError_t ssm_chain_launch(const float *state_in, float *seg_state, const float *seg_decay, long long heads, int NP,
+                             int segments, cudaStream_t stream);
+// the scan on the tensor cores (hla_ssm_sm103.cu): bf16, 16-byte aligned rows
+size_t ssm_tc_workspace_floats(const Ssm &p);
+bool ssm_tc_applicable(const Ssm &p);
+cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream);
 
 // norm of queries and keys for each head with the position rotation
 struct QkNorm {

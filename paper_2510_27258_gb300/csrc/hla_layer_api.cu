@@ -197,7 +197,8 @@ size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dty
     if ((dt != HLA_F32 && dt != HLA_BF16) || (long long)B * n > kMaxRows || (long long)B * H > (1LL << 27)) return 0;
     Ssm p{};
     p.dt = dt; p.B = B; p.n = n; p.H = H; p.P = P; p.G = G; p.N = N;
-    return scratch_bytes(ssm_scan_workspace_floats(p));
+    const size_t scan = ssm_scan_workspace_floats(p), tc = dt == HLA_BF16 ? ssm_tc_workspace_floats(p) : 0;
+    return scratch_bytes(scan > tc ? scan : tc);
 }
 
 hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, const void *b, const void *c,
@@ -220,6 +221,7 @@ hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, con
         return cuda_status(state_in ? cudaMemcpyAsync(state_out, state_in, bytes, cudaMemcpyDeviceToDevice, s)
                                     : cudaMemsetAsync(state_out, 0, bytes, s), "copying the state");
     }
+    if (ssm_tc_applicable(p)) return cuda_status(ssm_tc_launch(p, s), "selective scan (tensor cores)");
     return cuda_status(ssm_scan_launch(p, s), "selective scan");
 }
 

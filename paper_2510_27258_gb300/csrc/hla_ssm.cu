@@ -253,9 +253,7 @@ cudaError_t scan_as(const Ssm &p, cudaStream_t s) {
         scan_kernel<T, N, true><<<per * (segments - 1), kScanThreads, 0, s>>>(p, segments, seg_len, state, decay);
         cudaError_t e = cudaGetLastError();
         if (e) return e;
-        const long long units = BH * NP;
-        chain_kernel<<<(unsigned)((units + 255) / 256), 256, 0, s>>>(p.state_in, state, decay, units, (int)NP, segments);
-        e = cudaGetLastError();
+        e = ssm_chain_launch(p.state_in, state, decay, BH, (int)NP, segments, s);
         if (e) return e;
     }
     scan_kernel<T, N, false><<<per * segments, kScanThreads, 0, s>>>(p, segments, seg_len, state, decay);
@@ -284,6 +282,13 @@ cudaError_t step_of(const Ssm &p, cudaStream_t s) {
 }
 
 }  // namespace
+
+cudaError_t ssm_chain_launch(const float *state_in, float *seg_state, const float *seg_decay, long long heads, int NP,
+                             int segments, cudaStream_t s) {
+    const long long units = heads * NP;
+    chain_kernel<<<(unsigned)((units + 255) / 256), 256, 0, s>>>(state_in, seg_state, seg_decay, units, NP, segments);
+    return cudaGetLastError();
+}
 
 size_t ssm_scan_workspace_floats(const Ssm &p) {
     const long long s = segments_of(p), BH = (long long)p.B * p.H;

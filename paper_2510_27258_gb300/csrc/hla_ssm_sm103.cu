@@ -1,0 +1,705 @@
+// Selective state space scan over prompts on the tensor cores (sm_103a): tcgen05 MMAs with TMEM
+// accumulators, TMA tile loads and stores.
+//
+// With L_t = sum_{u <= t} a delta_u inside a 128-token tile and H the state before it, a tile is
+//   S = C B^T,   W_ts = S_ts exp(L_t - L_s) delta_s  (s <= t, else 0)
+//   Y = W X + diag(exp(L_t)) C H + skip X
+//   H' = exp(L_end) H + B^T (w X),   w_s = exp(L_end - L_s) delta_s
+// S depends on the group alone and B^T (.), C (.) take any number of columns, so a CTA works on 128
+// columns at once: two heads of a group (P <= 64, padded to 64) or one head of 128.
+//
+// Decays: the exponent of every pair further apart than a 32-token block factors into a row part and
+// a column part that are both <= 0 (for a <= 0), so only the diagonal blocks take an exponential a
+// pair; all sums of exponents run inside a block or towards the nearer end, so that weights of
+// neighbouring tokens do not come from differences of large numbers.
+//
+// Precision: products accumulate in fp32 and the state is fp32 (registers).  W and the copy of H that
+// C H reads are rounded to bf16 once, they only reach the bf16 output.  w X, which reaches the fp32
+// state, is an exact-to-2^-16 pair hi + lo of bf16, two products.
+//
+// TMEM (512 columns): two S regions (S, then W of both heads as packed bf16 in its place, then
+// B^T w X), Y's two parts.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
+// then hi), and lo, which takes C's place once S and C H are done (its own slot for N <= 64).  The
+// output is staged in X's place.
+//
+// Roles: warp 16 issues copies and MMAs (one thread); warps 0-15 are the epilogue, warp w on TMEM lanes
+// 32 (w % 4) .. (one row each: a token, or a state row) and columns 32 (w / 4) .. .  While the epilogue
+// turns S into W and X into hi, lo and writes a tile's output, the tensor cores run the products handed
+// over before and the next tile's S.
+//
+// Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
+// each segment's own state, chain_kernel the state before each segment.
+#include <cstdlib>
+#include <utility>
+
+#include "hla_vec.cuh"
+#include "sm103_prims.cuh"
+
+namespace hla {
+namespace {
+
+using namespace sm103;
+
+constexpr int kTile = 128;
+constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
+constexpr int kThreads = kEpiThreads + 32;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+enum Bar {
+    bLd0 = 0, bLd1 = 1,                      // C, B, X of a buffer have landed
+    bEvS = 2, bEvY2 = 3, bEvY1 = 4, bEvU = 5,  // MMA commits
+    bEpE = 6, bEpW = 7, bEpX = 8,            // epilogue hand-offs (16 warp arrivals)
+    bTear = 9,
+    kNumBars = 10
+};
+
+struct Misc {
+    // of both halves' tokens: step, decay up to the token in its block, factor of its column in later
+    // blocks; decay of each 32-token block
+    float dl[2][kTile], cum[2][kTile], cf[2][kTile - 32], tot[2][4];
+    uint64_t bar[kNumBars];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// shared-memory map for N <= 64 (kN = 64) and N = 128
+template <int kN>
+struct Map {
+    static constexpr uint32_t kOperand = kN / 64 * kBlockBytes;  // a C or B tile
+    static constexpr uint32_t C(int buf) { return buf * kOperand; }
+    static constexpr uint32_t B(int buf) { return (2 + buf) * kOperand; }
+    static constexpr uint32_t X(int buf) { return 4 * kOperand + buf * kTileBytes; }
+    static constexpr uint32_t kEH = 4 * kOperand + 2 * kTileBytes;
+    static constexpr uint32_t kEnd = kEH + kTileBytes + (kN == 64 ? kTileBytes : 0);
+    static constexpr uint32_t lo(int buf) { return kN == 64 ? kEH + kTileBytes : C(buf); }
+    static constexpr uint32_t kBytes = kEnd + sizeof(Misc);
+};
+static_assert(Map<128>::kBytes <= 232448, "shared memory");
+
+constexpr uint32_t kTS = 0, kTY1 = 256, kTY2 = 384;  // TMEM columns: S regions 0 and 128, Y's parts
+
+struct Params {
+    int n, H, P, G, N, softplus;
+    int per_group;         // units of 128 columns in a group
+    int units, segments, seg_tiles;
+    long long delta_stride;
+    const __nv_bfloat16 *delta;
+    __nv_bfloat16 *y;
+    long long y_stride;
+    const float *a, *skip, *delta_bias;
+    const int *lengths;
+    const float *state_in;
+    float *state_out, *seg_state, *seg_decay;
+    WsHeader *err;
+    int clear;             // this launch clears the error word
+};
+
+constexpr unsigned long long kBarWaitNs = 2000000000ull;
+
+__device__ __forceinline__ void set_error(WsHeader *err, unsigned where, unsigned detail) {
+    if (atomicCAS(&err->error, 0u, (unsigned)kDevTimeout) == 0u) {
+        err->where = where;
+        err->detail = detail;
+    }
+}
+
+__device__ __forceinline__ bool bar_wait(Misc *ms, int b, uint32_t parity, const Params &p) {
+    if (mbar_try_wait(&ms->bar[b], parity)) return true;
+    if (*(volatile int *)&ms->abort_flag) return false;
+    if (mbar_wait(&ms->bar[b], parity, kBarWaitNs)) return true;
+    set_error(p.err, 400 + b, parity);
+    *(volatile int *)&ms->abort_flag = 1;
+    return false;
+}
+
+__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory"); }
+
+__device__ __forceinline__ void epi_arrive(Misc *ms, int b) {
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&ms->bar[b]);
+}
+
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// two fp32 values in a 64-bit register, and the paired operations on them
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
+    float lo, hi;
+    unpair(v, lo, hi);
+    return pack_bf16x2(lo, hi);
+}
+__device__ __forceinline__ uint64_t of_bf16(uint32_t u) { return pair(bf16_lo(u), bf16_hi(u)); }
+
+__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(expf(-fabsf(v))); }
+
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+constexpr uint32_t kLboK = 1u << 16, kLboMN = (kBlockBytes >> 4) << 16;
+
+// D (+)= A B, KS steps of 16 over K, N columns, both operands in shared memory (low descriptor words)
+template <bool A_MN, bool B_MN, int KS>
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t accumulate) {
+    constexpr uint32_t id = idesc_bf16(128, 128, A_MN, B_MN);
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+        const uint32_t ka = A_MN ? kk * 128u : (kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2u;
+        const uint32_t kb = B_MN ? kk * 128u : (kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2u;
+        umma_bf16(d_tmem, (static_cast<uint64_t>(kDescHi) << 32) | (a_lo + ka),
+                  (static_cast<uint64_t>(kDescHi) << 32) | (b_lo + kb), id, kk > 0 ? 1u : accumulate);
+    }
+}
+
+// D = A B with A (128 x 128 bf16) in TMEM: K elements 16 kk .. of a row packed in columns a_tmem + 16 kk .. +7
+template <int N>
+__device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo) {
+    constexpr uint32_t id = idesc_bf16(128, N, 0, 1);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+        umma_bf16_ts(d_tmem, a_tmem + 16u * kk,
+                     (static_cast<uint64_t>(kDescHi) << 32) | (b_lo + kk * 128u), id, kk > 0 ? 1u : 0u);
+}
+
+template <int kN, bool kStateOnly>
+__global__ void __launch_bounds__(kThreads, 1)
+ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_b,
+              const __grid_constant__ CUtensorMap tm_c, const __grid_constant__ CUtensorMap tm_y, Params p) {
+    using Sm = Map<kN>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Misc *ms = reinterpret_cast<Misc *>(smem + Sm::kEnd);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool issuer = warp == kEpiWarps;
+
+    if (p.clear && blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
+    if (smem_u32(smem) & 1023u) {  // the tile layout needs 1 KiB alignment
+        if (tid == 0) set_error(p.err, 399, smem_u32(smem));
+        return;
+    }
+    if (tid == 0) {
+        for (int b = 0; b < kNumBars; ++b) mbar_init(&ms->bar[b], (b >= bEpE && b <= bEpX) ? kEpiWarps : 1);
+        ms->abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (issuer) {
+        tmem_alloc(&ms->tmem_base, 512);
+        tmem_relinquish();
+        if (lane == 0) {
+            prefetch_tmap(&tm_x); prefetch_tmap(&tm_b);
+            if (!kStateOnly) { prefetch_tmap(&tm_c); prefetch_tmap(&tm_y); }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tb = ms->tmem_base;
+
+    // this CTA's unit of 128 columns and its tiles
+    const int unit = blockIdx.x % p.units, seg = blockIdx.x / p.units;
+    const bool one = p.P == 128;  // one head of 128 columns, else two heads of up to 64
+    const int group_heads = p.H / p.G;
+    const int k = unit % p.per_group, g = unit / p.per_group % p.G, b = unit / p.per_group / p.G;
+    const int h0 = g * group_heads + (one ? k : 2 * k);
+    const bool both = one || 2 * k + 1 < group_heads;  // the second 64 columns are a head of this group
+    const int t_lo = seg * p.seg_tiles * kTile, t_hi = min(t_lo + p.seg_tiles * kTile, p.n);
+    int len = p.n;
+    if (p.lengths) len = min(max(p.lengths[b], 0), p.n);
+    const int live = min(t_hi, len);
+    const int tiles = live > t_lo ? (live - t_lo + kTile - 1) / kTile : 0;
+
+    if (issuer) {
+        if (lane == 0) {
+            const uint32_t sb4 = smem_u32(smem) >> 4;
+            auto lk = [&](uint32_t off) { return sb4 + (off >> 4) + kLboK; };
+            auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
+            auto load = [&](int j) {
+                const int buf = j & 1, t = t_lo + j * kTile;
+                uint64_t *bar = &ms->bar[bLd0 + buf];
+                mbar_arrive_expect_tx(bar, kTileBytes + (kStateOnly ? 1 : 2) * Sm::kOperand);
+                for (int i = 0; i < kN / 64; ++i) {
+                    tma_load_4d(smem + Sm::B(buf) + i * kBlockBytes, &tm_b, bar, 64 * i, g, t, b);
+                    if (!kStateOnly) tma_load_4d(smem + Sm::C(buf) + i * kBlockBytes, &tm_c, bar, 64 * i, g, t, b);
+                }
+                // a second head that the group does not have: the first one again, its result unused
+                tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, h0, t, b);
+                tma_load_4d(smem + Sm::X(buf) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
+            };
+            auto score = [&](int j) {  // S_j = C B^T
+                const int buf = j & 1;
+                mma_ss<false, false, kN / 16>(tb + kTS + 128 * buf, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);
+                umma_commit(&ms->bar[bEvS]);
+            };
+            int loaded = 0, landed = 0;  // tiles whose copies were issued / have been waited for
+            auto wait_ld = [&](int j) {
+                if (!bar_wait(ms, bLd0 + (j & 1), (j >> 1) & 1, p)) return false;
+                landed = j + 1;
+                tc_fence_after();
+                return true;
+            };
+            while (loaded < 2 && loaded < tiles) load(loaded++);
+            bool ok = true;
+            if (!kStateOnly && tiles > 0 && (ok = wait_ld(0))) score(0);
+            for (int j = 0; ok && j < tiles; ++j) {
+                const int buf = j & 1, par = j & 1;
+                // H before the tile is in EH; the previous tile is read out, its buffers are free
+                if (!(ok = bar_wait(ms, bEpE, par, p))) break;
+                tc_fence_after();
+                if (!kStateOnly) {
+                    mma_ss<false, true, kN / 16>(tb + kTY2, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
+                    umma_commit(&ms->bar[bEvY2]);
+                }
+                if (j > 0 && loaded < tiles) load(loaded++);
+                if (kStateOnly) {
+                    if (!(ok = wait_ld(j))) break;
+                } else {
+                    if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+                    tc_fence_after();
+                    const uint32_t w = tb + kTS + 128 * buf;
+                    if (one) {
+                        mma_ts<128>(tb + kTY1, w, lm(Sm::X(buf)));
+                    } else {
+                        mma_ts<64>(tb + kTY1, w, lm(Sm::X(buf)));
+                        mma_ts<64>(tb + kTY1 + 64, w + 8, lm(Sm::X(buf) + kBlockBytes));
+                    }
+                    umma_commit(&ms->bar[bEvY1]);
+                }
+                if (!(ok = bar_wait(ms, bEpX, par, p))) break;
+                tc_fence_after();
+                mma_ss<true, true, 8>(tb + kTS + 128 * buf, lm(Sm::B(buf)), lm(Sm::kEH), 0u);  // B^T (w X)
+                mma_ss<true, true, 8>(tb + kTS + 128 * buf, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
+                umma_commit(&ms->bar[bEvU]);
+                if (!kStateOnly && j + 1 < tiles) {
+                    if (!(ok = wait_ld(j + 1))) break;
+                    score(j + 1);
+                }
+            }
+            if (!ok) {
+                // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
+                // TMEM are released
+                for (int j = landed; j < loaded; ++j) mbar_wait(&ms->bar[bLd0 + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                umma_commit(&ms->bar[bTear]);
+                mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ============================ epilogue ============================
+        const int qd = warp & 3, cq = warp >> 2;
+        const int r = 32 * qd + lane, c0 = 32 * cq;
+        const uint32_t lane_base = (uint32_t)(32 * qd) << 16;
+        const int hs = cq >> 1;                     // which half of the columns
+        const int hcol = one ? c0 : (cq & 1) * 32;  // first column within the head
+        const int head = one || !hs ? h0 : h0 + 1;
+        const bool mine = hs == 0 || both;
+        const bool srow = kN == 128 || qd < 2;      // this thread's row is a state row
+        const float skip = p.skip && mine ? p.skip[head] : 0.f;
+        const long long bh = (long long)b * p.H + head;
+        const long long NP = (long long)p.N * p.P;
+
+        // the step size of token r for this thread's half
+        const int dhead = mine ? head : h0;
+        const float da = p.a[dhead] * kLog2e, dbias = p.delta_bias ? p.delta_bias[dhead] : 0.f;
+        const __nv_bfloat16 *raw = p.delta + (long long)b * p.n * p.delta_stride + dhead;
+        auto fetch = [&](int j) {
+            const int t = t_lo + j * kTile + r;
+            return t < live ? raw[(long long)t * p.delta_stride] : __nv_bfloat16();
+        };
+
+        float st[32];
+        {
+            const float *from = kStateOnly ? nullptr
+                                : p.segments > 1 ? p.seg_state + (bh * p.segments + seg) * NP
+                                : p.state_in     ? p.state_in + bh * NP
+                                                 : nullptr;
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (from && mine && r < p.N && hcol + i < p.P)
+                    v = *reinterpret_cast<const float4 *>(from + (long long)r * p.P + hcol + i);
+                st[i] = v.x; st[i + 1] = v.y; st[i + 2] = v.z; st[i + 3] = v.w;
+            }
+        }
+        auto put_state = [&]() {  // the state as bf16, rows = state rows, into EH
+            if (!kStateOnly && srow) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + i)) =
+                        make_uint4(pack_bf16x2(st[i], st[i + 1]), pack_bf16x2(st[i + 2], st[i + 3]),
+                                   pack_bf16x2(st[i + 4], st[i + 5]), pack_bf16x2(st[i + 6], st[i + 7]));
+            }
+            fence_async_smem();
+            epi_arrive(ms, bEpE);
+        };
+        float la_sum = 0.f;
+        __nv_bfloat16 next_raw = fetch(0);
+
+        // steps and decays of tile j's tokens: this thread's row for its half (and the columns' arrays)
+        float up = 0.f, row_cf = 0.f;  // decay of the block up to this token; its weight at the block's end
+        auto steps = [&](int j) {
+            const bool in = t_lo + j * kTile + r < live;
+            const float v = to_f32(next_raw) + dbias;
+            const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
+            next_raw = fetch(j + 1);
+            float down = up = in ? da * d : 0.f;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
+                if (lane >= o) up += x;
+                if (lane + o < 32) down += z;
+            }
+            const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
+            row_cf = ex2(lane < 31 ? after : 0.f) * d;
+            if ((cq & 1) == 0) {
+                ms->dl[hs][r] = d;
+                ms->cum[hs][r] = up;
+                if (qd < 3) ms->cf[hs][r] = row_cf;
+                if (lane == 31) ms->tot[hs][qd] = up;
+            }
+        };
+        if (tiles > 0) {
+            put_state();
+            steps(0);
+        }
+
+        for (int j = 0; j < tiles; ++j) {
+            const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
+            uint8_t *xs = smem + Sm::X(buf);
+            const bool in = t0 + r < live;
+            epi_sync();  // the tile's steps are in shared memory
+            bar_wait(ms, bLd0 + buf, (j >> 1) & 1, p);
+            if (t0 + kTile > live) {  // tokens that do not count: zero rows of X and B, whatever was read
+                if (!in) {
+                    const uint4 z = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        *reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + i)) = z;
+                        if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(buf) + tile_off(r, c0 + i)) = z;
+                    }
+                }
+                fence_async_smem();
+            }
+            // (a) W = S . decay, packed bf16 in S's place: this thread's 32 columns of both halves.  A
+            // step of 16 columns turns into 8 words of the first half's W and 8 of the second's.
+            if (!kStateOnly) {
+                const uint32_t sw = tb + lane_base + kTS + 128 * buf + c0;
+                bar_wait(ms, bEvS, par, p);
+                tc_fence_after();
+                if (cq > qd) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = 0u;
+                    tmem_st16(sw, w);
+                    tmem_st16(sw + 16, w);
+                } else {
+                    float lr[2], rf[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        lr[e] = ms->cum[e][r];
+                        float between = lr[e];  // decay from the end of the columns' block to this token
+                        for (int q = cq + 1; q < qd; ++q) between += ms->tot[e][q];
+                        rf[e] = ex2(between);
+                    }
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        uint32_t sv[16], w[8];
+                        tmem_ld16(sw + 16 * o, sv);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            if (e == 1 && one) break;
+                            if (cq < qd) {
+                                const ulonglong2 *cf = reinterpret_cast<const ulonglong2 *>(&ms->cf[e][c0 + 16 * o]);
+                                const uint64_t rf2 = pair(rf[e], rf[e]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const ulonglong2 f = cf[i];
+                                    w[2 * i] = bf16_of(mul2(pair(sv[4 * i], sv[4 * i + 1]), mul2(rf2, f.x)));
+                                    w[2 * i + 1] = bf16_of(mul2(pair(sv[4 * i + 2], sv[4 * i + 3]), mul2(rf2, f.y)));
+                                }
+                            } else {
+                                const float4 *cu = reinterpret_cast<const float4 *>(&ms->cum[e][c0 + 16 * o]);
+                                const ulonglong2 *dl = reinterpret_cast<const ulonglong2 *>(&ms->dl[e][c0 + 16 * o]);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const float4 u = cu[i];
+                                    const ulonglong2 d = dl[i];
+                                    const int c = 16 * o + 4 * i;
+                                    // above the diagonal the exponential may overflow: the select drops it
+                                    const uint64_t v0 = mul2(pair(sv[4 * i], sv[4 * i + 1]),
+                                                             mul2(pair(ex2(lr[e] - u.x), ex2(lr[e] - u.y)), d.x));
+                                    const uint64_t v1 = mul2(pair(sv[4 * i + 2], sv[4 * i + 3]),
+                                                             mul2(pair(ex2(lr[e] - u.z), ex2(lr[e] - u.w)), d.y));
+                                    float a0, a1, a2, a3;
+                                    unpair(v0, a0, a1);
+                                    unpair(v1, a2, a3);
+                                    w[2 * i] = pack_bf16x2(c <= lane ? a0 : 0.f, c + 1 <= lane ? a1 : 0.f);
+                                    w[2 * i + 1] = pack_bf16x2(c + 2 <= lane ? a2 : 0.f, c + 3 <= lane ? a3 : 0.f);
+                                }
+                            }
+                            tmem_st8(sw + 16 * o + 8 * e, w);
+                        }
+                    }
+                }
+                tmem_st_wait();
+                epi_arrive(ms, bEpW);
+            }
+            // (b) w X -> hi (EH), lo
+            float before = 0.f, later = 0.f;  // decay of the blocks before / after this token's
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (q < qd) before += ms->tot[hs][q];
+                if (q > qd) later += ms->tot[hs][q];
+            }
+            const float total = before + ms->tot[hs][qd] + later;
+            const float yf = ex2(before + up);
+            if (!kStateOnly) {  // C H has read EH (and C)
+                bar_wait(ms, bEvY2, par, p);
+                tc_fence_after();
+            }
+            {
+                const float wr = row_cf * ex2(later);
+                const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    const uint32_t off = tile_off(r, c0 + i);
+                    const uint4 u = *reinterpret_cast<const uint4 *>(xs + off);
+                    uint32_t hi[4], lo[4];
+                    const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint64_t v = mul2(wr2, of_bf16(x[e]));
+                        hi[e] = bf16_of(v);
+                        lo[e] = bf16_of(fma2(of_bf16(hi[e]), minus, v));
+                    }
+                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                    *reinterpret_cast<uint4 *>(smem + Sm::lo(buf) + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                }
+            }
+            fence_async_smem();
+            epi_arrive(ms, bEpX);
+            // (c) Y -> bf16 in X's place -> TMA store
+            if (!kStateOnly) {
+                bar_wait(ms, bEvY1, par, p);
+                tc_fence_after();
+                const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t y1[16], y2[16];
+                    tmem_ld16(tb + lane_base + kTY1 + c0 + 16 * half, y1);
+                    tmem_ld16(tb + lane_base + kTY2 + c0 + 16 * half, y2);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; i += 8) {
+                        uint4 *at = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + 16 * half + i));
+                        const uint4 u = *at;
+                        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+                        uint32_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint64_t v = fma2(yf2, pair(y2[i + 2 * e], y2[i + 2 * e + 1]),
+                                                    pair(y1[i + 2 * e], y1[i + 2 * e + 1]));
+                            const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
+                            o[e] = in ? y : 0u;
+                        }
+                        *at = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
+                }
+                fence_async_smem();
+            }
+            tc_fence_before();
+            epi_sync();  // the output is staged; every warp has done with the tile's steps
+            if (!kStateOnly && tid == 0) {
+                tma_store_4d(&tm_y, xs, 0, h0, t0, b);
+                if (both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
+                tma_store_commit();
+            }
+            la_sum += total;
+            if (j + 1 < tiles) steps(j + 1);  // under B^T (w X)
+            // (d) the state after the tile
+            bar_wait(ms, bEvU, par, p);
+            tc_fence_after();
+            if (srow) {
+                const float keep = ex2(total);
+#pragma unroll
+                for (int o = 0; o < 32; o += 16) {
+                    uint32_t u[16];
+                    tmem_ld16(tb + lane_base + kTS + 128 * buf + c0 + o, u);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) st[o + i] = fmaf(keep, st[o + i], __uint_as_float(u[i]));
+                }
+            }
+            if (!kStateOnly && tid == 0) tma_store_wait_read();  // X's slot may be loaded again
+            if (j + 1 < tiles) put_state();
+        }
+
+        // the rest of the segment does not count: zeros
+        if (!kStateOnly && mine) {
+            for (int t = max(t_lo, live) + r; t < t_hi; t += kTile) {
+                __nv_bfloat16 *row = p.y + ((long long)b * p.n + t) * p.y_stride + (long long)head * p.P + hcol;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+                    if (hcol + i < p.P) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0, 0, 0, 0);
+            }
+        }
+        float *to = nullptr;
+        if (kStateOnly) {
+            to = p.seg_state + (bh * p.segments + seg) * NP;
+            if (mine && hcol == 0 && r == 0) p.seg_decay[bh * p.segments + seg] = la_sum * kLn2;
+        } else if (p.state_out && seg == p.segments - 1) {
+            to = p.state_out + bh * NP;
+        }
+        if (to && mine && r < p.N) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+                if (hcol + i < p.P)
+                    *reinterpret_cast<float4 *>(to + (long long)r * p.P + hcol + i) =
+                        make_float4(st[i], st[i + 1], st[i + 2], st[i + 3]);
+        }
+        if (!kStateOnly && tid == 0) tma_store_wait_all();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (issuer) {
+        tc_fence_after();
+        tmem_dealloc(tb, 512);
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        cudaDriverEntryPointQueryResult qr;
+        void *f = nullptr;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &qr) ==
+                cudaSuccess &&
+            qr == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(f);
+    }
+    return fn;
+}
+
+// rows [B, n] at a row stride, `heads` blocks of `inner` bf16 in each; boxes of 64 columns of one head x
+// 128 tokens, 128-byte swizzle, zero fill past a head's columns and past a sequence's n tokens
+bool make_map(CUtensorMap *m, const void *base, int B, int n, int heads, int inner, long long stride) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)heads, (cuuint64_t)n, (cuuint64_t)B};
+    cuuint64_t strides[3] = {(cuuint64_t)inner * 2, (cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * (cuuint64_t)n};
+    cuuint32_t box[4] = {64, 1, (cuuint32_t)kTile, 1};
+    cuuint32_t es[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Cut {
+    int per_group, units, segments, seg_tiles;
+};
+
+// Units of 128 columns, and segments: the number that gives the shortest chain of tiles over 152 SMs,
+// where a segmented scan pays a state-only pass (about half a tile's work) on top
+Cut cut(const Ssm &p) {
+    Cut c{};
+    const int group_heads = p.H / p.G;
+    c.per_group = p.P == 128 ? group_heads : (group_heads + 1) / 2;
+    c.units = p.B * p.G * c.per_group;
+    const int tiles = (p.n + kTile - 1) / kTile;
+    double best = 0;
+    for (int s = 1; s <= tiles && s <= 152; ++s) {
+        const int len = (tiles + s - 1) / s, segs = (tiles + len - 1) / len;
+        const long long waves = ((long long)c.units * segs + 151) / 152;
+        const double cost = waves * (len * (segs > 1 ? 1.5 : 1.0) + (segs > 1 ? 6.0 : 0.0));
+        if (s == 1 || cost < best) {
+            best = cost;
+            c.segments = segs;
+            c.seg_tiles = len;
+        }
+    }
+    return c;
+}
+
+}  // namespace
+
+size_t ssm_tc_workspace_floats(const Ssm &p) {
+    if (p.n <= 0 || p.B <= 0) return 0;
+    const Cut c = cut(p);
+    return c.segments > 1 ? (size_t)p.B * p.H * c.segments * ((size_t)p.N * p.P + 1) : 0;
+}
+
+bool ssm_tc_applicable(const Ssm &p) {
+    if (getenv("HLA_DISABLE_FUSED")) return false;
+    if (p.dt != HLA_BF16 || p.n <= 0 || p.B <= 0) return false;
+    for (auto [ptr, stride] : {std::pair<const void *, long long>{p.x, p.x_stride}, {p.b, p.b_stride}, {p.c, p.c_stride},
+                               {p.y, p.y_stride}})
+        if (!rows_aligned(ptr, stride, 2, 16)) return false;
+    int dev = 0, major = 0, minor = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+    cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev);
+    return major == 10 && minor == 3 && encode_fn() != nullptr;
+}
+
+cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
+    CUtensorMap mx, mb, mc, my;
+    if (!make_map(&mx, p.x, p.B, p.n, p.H, p.P, p.x_stride) || !make_map(&mb, p.b, p.B, p.n, p.G, p.N, p.b_stride) ||
+        !make_map(&mc, p.c, p.B, p.n, p.G, p.N, p.c_stride) || !make_map(&my, p.y, p.B, p.n, p.H, p.P, p.y_stride))
+        return cudaErrorInvalidValue;
+    const Cut c = cut(p);
+    Params q{};
+    q.n = p.n; q.H = p.H; q.P = p.P; q.G = p.G; q.N = p.N; q.softplus = p.softplus;
+    q.per_group = c.per_group; q.units = c.units; q.segments = c.segments; q.seg_tiles = c.seg_tiles;
+    q.delta_stride = p.delta_stride; q.delta = static_cast<const __nv_bfloat16 *>(p.delta);
+    q.y = static_cast<__nv_bfloat16 *>(p.y); q.y_stride = p.y_stride;
+    q.a = p.a; q.skip = p.skip; q.delta_bias = p.delta_bias; q.lengths = p.lengths;
+    q.state_in = p.state_in; q.state_out = p.state_out;
+    q.seg_state = reinterpret_cast<float *>(p.ws + kWsHeaderBytes);
+    q.seg_decay = q.seg_state + (size_t)p.B * p.H * c.segments * p.N * p.P;
+    q.err = reinterpret_cast<WsHeader *>(p.ws);
+    q.clear = 1;
+    auto launch = [&](auto kern, int blocks, uint32_t smem) -> cudaError_t {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e) return e;
+        kern<<<blocks, kThreads, smem, stream>>>(mx, mb, mc, my, q);
+        return cudaGetLastError();
+    };
+    const bool wide = p.N == 128;
+    if (c.segments > 1) {
+        const int blocks = c.units * (c.segments - 1);
+        cudaError_t e = wide ? launch(ssm_tc_kernel<128, true>, blocks, Map<128>::kBytes)
+                             : launch(ssm_tc_kernel<64, true>, blocks, Map<64>::kBytes);
+        if (e) return e;
+        e = ssm_chain_launch(p.state_in, q.seg_state, q.seg_decay, (long long)p.B * p.H, p.N * p.P, c.segments, stream);
+        if (e) return e;
+        q.clear = 0;
+    }
+    const int blocks = c.units * c.segments;
+    return wide ? launch(ssm_tc_kernel<128, false>, blocks, Map<128>::kBytes)
+                : launch(ssm_tc_kernel<64, false>, blocks, Map<64>::kBytes);
+}
+
+}  // namespace hla
