@@ -13,12 +13,12 @@
 // pair; all sums of exponents run inside a block or towards the nearer end, so that weights of
 // neighbouring tokens do not come from differences of large numbers.
 //
-// Precision: products accumulate in fp32 and the state is fp32 (registers).  W and the copy of H that
+// Precision: products accumulate in fp32 and the state is fp32.  W and the copy of H that
 // C H reads are rounded to bf16 once, they only reach the bf16 output.  w X, which reaches the fp32
 // state, is an exact-to-2^-16 pair hi + lo of bf16, two products.
 //
-// TMEM (512 columns): two S regions (S, then W of both heads as packed bf16 in its place, then
-// B^T w X), Y's two parts.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
+// TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H, Y's two parts.  H is
+// kept multiplied by the coming tile's decay, so that B^T w X accumulates onto it.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
 // then hi), and lo, which takes C's place once S and C H are done (its own slot for N <= 64).  The
 // output is staged in X's place.
 //
@@ -43,6 +43,9 @@ using namespace sm103;
 constexpr int kTile = 128;
 constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
 constexpr int kThreads = kEpiThreads + 32;
+constexpr int kStorer = 12 * 32;  // the thread that stores the output (its warp has no part of W)
+// decay of a block (a power of two) down to which its diagonal part is factored, too
+constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum Bar {
@@ -54,12 +57,15 @@ enum Bar {
 };
 
 struct Misc {
-    // of both halves' tokens: step, decay up to the token in its block, factor of its column in later
-    // blocks; decay of each 32-token block
-    float dl[2][kTile], cum[2][kTile], cf[2][kTile - 32], tot[2][4];
+    // of both halves' tokens: decay up to the token in its 32-token block, step times the decay from the
+    // token to its block's end; decay of each block
+    float cum[2][kTile], cf[2][kTile], tot[2][4];
     uint64_t bar[kNumBars];
     uint32_t tmem_base;
     int abort_flag;
+    // what the epilogue needs now and then of its place in the problem (kept out of its registers):
+    // sequence, first head, segment, whether the second 64 columns are a head of this group
+    int b, h0, seg, both;
 };
 
 // shared-memory map for N <= 64 (kN = 64) and N = 128
@@ -76,7 +82,7 @@ struct Map {
 };
 static_assert(Map<128>::kBytes <= 232448, "shared memory");
 
-constexpr uint32_t kTS = 0, kTY1 = 256, kTY2 = 384;  // TMEM columns: S regions 0 and 128, Y's parts
+constexpr uint32_t kTS = 0, kTH = 128, kTY1 = 256, kTY2 = 384;  // TMEM columns
 
 struct Params {
     int n, H, P, G, N, softplus;
@@ -153,7 +159,18 @@ __device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
 }
 __device__ __forceinline__ uint64_t of_bf16(uint32_t u) { return pair(bf16_lo(u), bf16_hi(u)); }
 
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.f) + log1pf(expf(-fabsf(v))); }
+// max(v, 0) + log(1 + e), e = exp(-|v|), by log(1 + e) = 2 atanh(s) with s = e / (2 + e) <= 1/3 and the
+// series of atanh up to s^13 (what follows is below 2^-23 of the sum)
+__device__ __forceinline__ float softplus(float v) {
+    const float e = ex2(-kLog2e * fabsf(v)), s = __fdividef(e, 2.f + e), q = s * s;
+    float y = fmaf(q, 1.f / 13.f, 1.f / 11.f);
+    y = fmaf(q, y, 1.f / 9.f);
+    y = fmaf(q, y, 1.f / 7.f);
+    y = fmaf(q, y, 1.f / 5.f);
+    y = fmaf(q, y, 1.f / 3.f);
+    y = fmaf(q, y, 1.f);
+    return fmaf(2.f * s, y, fmaxf(v, 0.f));
+}
 
 constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 constexpr uint32_t kLboK = 1u << 16, kLboMN = (kBlockBytes >> 4) << 16;
@@ -191,14 +208,28 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kEpiWarps;
 
+    // this CTA's unit of 128 columns and its tiles
+    const int unit = blockIdx.x % p.units, seg = blockIdx.x / p.units;
+    const bool one = p.P == 128;  // one head of 128 columns, else two heads of up to 64
+    const int group_heads = p.H / p.G;
+    const int k = unit % p.per_group, g = unit / p.per_group % p.G, b = unit / p.per_group / p.G;
+    const int h0 = g * group_heads + (one ? k : 2 * k);
+    const bool both = one || 2 * k + 1 < group_heads;  // the second 64 columns are a head of this group
+    const int t_lo = seg * p.seg_tiles * kTile, t_hi = min(t_lo + p.seg_tiles * kTile, p.n);
+    int len = p.n;
+    if (p.lengths) len = min(max(p.lengths[b], 0), p.n);
+    const int live = min(t_hi, len);
+    const int tiles = live > t_lo ? (live - t_lo + kTile - 1) / kTile : 0;
+
     if (p.clear && blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
     if (smem_u32(smem) & 1023u) {  // the tile layout needs 1 KiB alignment
         if (tid == 0) set_error(p.err, 399, smem_u32(smem));
         return;
     }
     if (tid == 0) {
-        for (int b = 0; b < kNumBars; ++b) mbar_init(&ms->bar[b], (b >= bEpE && b <= bEpX) ? kEpiWarps : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpX) ? kEpiWarps : 1);
         ms->abort_flag = 0;
+        ms->b = b; ms->h0 = h0; ms->seg = seg; ms->both = both;
         fence_mbar_init();
     }
     if (issuer) {
@@ -213,19 +244,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     __syncthreads();
     tc_fence_after();
     const uint32_t tb = ms->tmem_base;
-
-    // this CTA's unit of 128 columns and its tiles
-    const int unit = blockIdx.x % p.units, seg = blockIdx.x / p.units;
-    const bool one = p.P == 128;  // one head of 128 columns, else two heads of up to 64
-    const int group_heads = p.H / p.G;
-    const int k = unit % p.per_group, g = unit / p.per_group % p.G, b = unit / p.per_group / p.G;
-    const int h0 = g * group_heads + (one ? k : 2 * k);
-    const bool both = one || 2 * k + 1 < group_heads;  // the second 64 columns are a head of this group
-    const int t_lo = seg * p.seg_tiles * kTile, t_hi = min(t_lo + p.seg_tiles * kTile, p.n);
-    int len = p.n;
-    if (p.lengths) len = min(max(p.lengths[b], 0), p.n);
-    const int live = min(t_hi, len);
-    const int tiles = live > t_lo ? (live - t_lo + kTile - 1) / kTile : 0;
 
     if (issuer) {
         if (lane == 0) {
@@ -246,7 +264,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             };
             auto score = [&](int j) {  // S_j = C B^T
                 const int buf = j & 1;
-                mma_ss<false, false, kN / 16>(tb + kTS + 128 * buf, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);
+                mma_ss<false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);
                 umma_commit(&ms->bar[bEvS]);
             };
             int loaded = 0, landed = 0;  // tiles whose copies were issued / have been waited for
@@ -274,7 +292,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 } else {
                     if (!(ok = bar_wait(ms, bEpW, par, p))) break;
                     tc_fence_after();
-                    const uint32_t w = tb + kTS + 128 * buf;
+                    const uint32_t w = tb + kTS;
                     if (one) {
                         mma_ts<128>(tb + kTY1, w, lm(Sm::X(buf)));
                     } else {
@@ -285,8 +303,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 }
                 if (!(ok = bar_wait(ms, bEpX, par, p))) break;
                 tc_fence_after();
-                mma_ss<true, true, 8>(tb + kTS + 128 * buf, lm(Sm::B(buf)), lm(Sm::kEH), 0u);  // B^T (w X)
-                mma_ss<true, true, 8>(tb + kTS + 128 * buf, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
+                mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::kEH), 1u);  // H += B^T (w X)
+                mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
                 umma_commit(&ms->bar[bEvU]);
                 if (!kStateOnly && j + 1 < tiles) {
                     if (!(ok = wait_ld(j + 1))) break;
@@ -308,59 +326,70 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const int r = 32 * qd + lane, c0 = 32 * cq;
         const uint32_t lane_base = (uint32_t)(32 * qd) << 16;
         const int hs = cq >> 1;                     // which half of the columns
-        const int hcol = one ? c0 : (cq & 1) * 32;  // first column within the head
-        const int head = one || !hs ? h0 : h0 + 1;
-        const bool mine = hs == 0 || both;
         const bool srow = kN == 128 || qd < 2;      // this thread's row is a state row
-        const float skip = p.skip && mine ? p.skip[head] : 0.f;
-        const long long bh = (long long)b * p.H + head;
-        const long long NP = (long long)p.N * p.P;
-
-        // the step size of token r for this thread's half
-        const int dhead = mine ? head : h0;
+        const int dhead = one || !hs || !both ? h0 : h0 + 1;  // a second head that is not there: the first
+        const float skip = p.skip ? p.skip[dhead] : 0.f;
         const float da = p.a[dhead] * kLog2e, dbias = p.delta_bias ? p.delta_bias[dhead] : 0.f;
-        const __nv_bfloat16 *raw = p.delta + (long long)b * p.n * p.delta_stride + dhead;
-        auto fetch = [&](int j) {
-            const int t = t_lo + j * kTile + r;
-            return t < live ? raw[(long long)t * p.delta_stride] : __nv_bfloat16();
+        // the warps of even column quarters compute the tokens' steps (a thread its row's, for its half)
+        const bool stepper = (cq & 1) == 0;
+        const __nv_bfloat16 *raw = p.delta + ((long long)b * p.n + t_lo + r) * p.delta_stride + dhead;
+        int left = stepper ? live - t_lo - r : 0;  // tokens that count, from the next one to fetch on
+        auto fetch = [&]() {
+            __nv_bfloat16 v = left > 0 ? *raw : __nv_bfloat16();
+            raw += kTile * p.delta_stride;
+            left -= kTile;
+            return v;
         };
 
-        float st[32];
-        {
-            const float *from = kStateOnly ? nullptr
-                                : p.segments > 1 ? p.seg_state + (bh * p.segments + seg) * NP
-                                : p.state_in     ? p.state_in + bh * NP
-                                                 : nullptr;
+        // the state rows and columns of this thread within [B, H, segs, N, P]; null where it has none
+        auto state_at = [&](float *base, int segs, int seg_i) -> float * {
+            const volatile Misc *m = ms;
+            const int col = p.P == 128 ? c0 : (cq & 1) * 32;
+            if (!base || r >= p.N || (hs && !m->both)) return nullptr;
+            const long long bh = (long long)m->b * p.H + m->h0 + (p.P != 128 && hs ? 1 : 0);
+            return base + ((bh * segs + seg_i) * p.N + r) * p.P + col;
+        };
+        const uint32_t h_at = tb + lane_base + kTH + c0;
+        // 16 columns of the state: their bf16 copy to EH, and times the coming tile's decay to TMEM
+        auto put_state = [&](const float (&v)[16], int o, float keep) {
+            if (!kStateOnly) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (from && mine && r < p.N && hcol + i < p.P)
-                    v = *reinterpret_cast<const float4 *>(from + (long long)r * p.P + hcol + i);
-                st[i] = v.x; st[i + 1] = v.y; st[i + 2] = v.z; st[i + 3] = v.w;
+                for (int i = 0; i < 16; i += 8)
+                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + o + i)) =
+                        make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                                   pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
             }
-        }
-        auto put_state = [&]() {  // the state as bf16, rows = state rows, into EH
-            if (!kStateOnly && srow) {
+            uint32_t u[16];
 #pragma unroll
-                for (int i = 0; i < 32; i += 8)
-                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + i)) =
-                        make_uint4(pack_bf16x2(st[i], st[i + 1]), pack_bf16x2(st[i + 2], st[i + 3]),
-                                   pack_bf16x2(st[i + 4], st[i + 5]), pack_bf16x2(st[i + 6], st[i + 7]));
-            }
+            for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i] * keep);
+            tmem_st16(h_at + o, u);
+        };
+        auto state_is_put = [&]() {
+            tmem_st_wait();
             fence_async_smem();
             epi_arrive(ms, bEpE);
         };
+        // decay of the tile's blocks before / after this token's, and of the whole tile
+        float before = 0.f, later = 0.f, total = 0.f;
+        auto decays = [&]() {
+            before = later = 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (q < qd) before += ms->tot[hs][q];
+                if (q > qd) later += ms->tot[hs][q];
+            }
+            total = before + ms->tot[hs][qd] + later;
+        };
         float la_sum = 0.f;
-        __nv_bfloat16 next_raw = fetch(0);
 
-        // steps and decays of tile j's tokens: this thread's row for its half (and the columns' arrays)
-        float up = 0.f, row_cf = 0.f;  // decay of the block up to this token; its weight at the block's end
-        auto steps = [&](int j) {
+        // decays of tile j's tokens from their raw steps
+        auto steps = [&](int j, __nv_bfloat16 next_raw) {
+            if (!stepper) return;
             const bool in = t_lo + j * kTile + r < live;
             const float v = to_f32(next_raw) + dbias;
             const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
-            next_raw = fetch(j + 1);
-            float down = up = in ? da * d : 0.f;
+            const float la = in ? da * d : 0.f;
+            float up = la, down = la;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
@@ -368,24 +397,41 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 if (lane + o < 32) down += z;
             }
             const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
-            row_cf = ex2(lane < 31 ? after : 0.f) * d;
-            if ((cq & 1) == 0) {
-                ms->dl[hs][r] = d;
-                ms->cum[hs][r] = up;
-                if (qd < 3) ms->cf[hs][r] = row_cf;
-                if (lane == 31) ms->tot[hs][qd] = up;
-            }
+            ms->cum[hs][r] = up;
+            ms->cf[hs][r] = ex2(lane < 31 ? after : 0.f) * d;
+            if (lane == 31) ms->tot[hs][qd] = up;
         };
+        // state 0: from state_in or the segment's chained state
+        const float *from = kStateOnly ? nullptr
+                            : p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
+                                             : state_at(const_cast<float *>(p.state_in), 1, 0);
+        const int cols = p.P - (one ? c0 : (cq & 1) * 32);  // columns of the head from this thread's first one on
         if (tiles > 0) {
-            put_state();
-            steps(0);
+            steps(0, fetch());
+            epi_sync();  // the tile's decays are in shared memory
+            decays();
+            if (srow) {
+                const float keep = ex2(total);
+#pragma unroll
+                for (int o = 0; o < 32; o += 16) {
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (from && o + i < cols) f = *reinterpret_cast<const float4 *>(from + o + i);
+                        v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+                    }
+                    put_state(v, o, keep);
+                }
+            }
+            state_is_put();
         }
 
         for (int j = 0; j < tiles; ++j) {
             const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
             uint8_t *xs = smem + Sm::X(buf);
             const bool in = t0 + r < live;
-            epi_sync();  // the tile's steps are in shared memory
+            const __nv_bfloat16 next_raw = fetch();  // of the next tile, used at the end of this one
             bar_wait(ms, bLd0 + buf, (j >> 1) & 1, p);
             if (t0 + kTile > live) {  // tokens that do not count: zero rows of X and B, whatever was read
                 if (!in) {
@@ -401,7 +447,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             // (a) W = S . decay, packed bf16 in S's place: this thread's 32 columns of both halves.  A
             // step of 16 columns turns into 8 words of the first half's W and 8 of the second's.
             if (!kStateOnly) {
-                const uint32_t sw = tb + lane_base + kTS + 128 * buf + c0;
+                const uint32_t sw = tb + lane_base + kTS + c0;
                 bar_wait(ms, bEvS, par, p);
                 tc_fence_after();
                 if (cq > qd) {
@@ -411,13 +457,19 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     tmem_st16(sw, w);
                     tmem_st16(sw + 16, w);
                 } else {
-                    float lr[2], rf[2];
+                    // a row's factor: the decay from the end of the columns' block to the token.  In the
+                    // diagonal block that is the inverse of the decay still to come, finite unless the
+                    // block decays by more than 2^-kFactored; then every pair takes its own exponential.
+                    float rf[2];
+                    bool factored = true;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        lr[e] = ms->cum[e][r];
-                        float between = lr[e];  // decay from the end of the columns' block to this token
-                        for (int q = cq + 1; q < qd; ++q) between += ms->tot[e][q];
-                        rf[e] = ex2(between);
+                        const float own = ms->tot[e][qd];
+                        float x = ms->cum[e][r] - (cq == qd ? own : 0.f);
+                        if (cq < 1 && qd > 1) x += ms->tot[e][1];
+                        if (cq < 2 && qd > 2) x += ms->tot[e][2];
+                        rf[e] = ex2(x);
+                        if (cq == qd && !(fabsf(own) <= kFactored)) factored = false;
                     }
 #pragma unroll
                     for (int o = 0; o < 2; ++o) {
@@ -427,7 +479,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
                             if (e == 1 && one) break;
-                            if (cq < qd) {
+                            if (factored) {
                                 const ulonglong2 *cf = reinterpret_cast<const ulonglong2 *>(&ms->cf[e][c0 + 16 * o]);
                                 const uint64_t rf2 = pair(rf[e], rf[e]);
 #pragma unroll
@@ -437,23 +489,29 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                                     w[2 * i + 1] = bf16_of(mul2(pair(sv[4 * i + 2], sv[4 * i + 3]), mul2(rf2, f.y)));
                                 }
                             } else {
-                                const float4 *cu = reinterpret_cast<const float4 *>(&ms->cum[e][c0 + 16 * o]);
-                                const ulonglong2 *dl = reinterpret_cast<const ulonglong2 *>(&ms->dl[e][c0 + 16 * o]);
+                                const volatile Misc *m = ms;
+                                const int tc = t0 + c0 + lane, he = m->h0 + (e && m->both ? 1 : 0);
+                                float dc = 0.f;  // the step of this lane's column
+                                if (tc < live) {
+                                    dc = to_f32(p.delta[((long long)m->b * p.n + tc) * p.delta_stride + he]) +
+                                         (p.delta_bias ? p.delta_bias[he] : 0.f);
+                                    dc = p.softplus ? softplus(dc) : dc;
+                                }
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const float4 u = cu[i];
-                                    const ulonglong2 d = dl[i];
-                                    const int c = 16 * o + 4 * i;
-                                    // above the diagonal the exponential may overflow: the select drops it
-                                    const uint64_t v0 = mul2(pair(sv[4 * i], sv[4 * i + 1]),
-                                                             mul2(pair(ex2(lr[e] - u.x), ex2(lr[e] - u.y)), d.x));
-                                    const uint64_t v1 = mul2(pair(sv[4 * i + 2], sv[4 * i + 3]),
-                                                             mul2(pair(ex2(lr[e] - u.z), ex2(lr[e] - u.w)), d.y));
-                                    float a0, a1, a2, a3;
-                                    unpair(v0, a0, a1);
-                                    unpair(v1, a2, a3);
-                                    w[2 * i] = pack_bf16x2(c <= lane ? a0 : 0.f, c + 1 <= lane ? a1 : 0.f);
-                                    w[2 * i + 1] = pack_bf16x2(c + 2 <= lane ? a2 : 0.f, c + 3 <= lane ? a3 : 0.f);
+                                for (int i = 0; i < 8; ++i) {
+                                    const int c = 16 * o + 2 * i;
+                                    const float e0 = ex2(m->cum[e][r] - m->cum[e][c0 + c]);
+                                    const float e1 = ex2(m->cum[e][r] - m->cum[e][c0 + c + 1]);
+                                    const float d0 = __shfl_sync(0xffffffffu, dc, c), d1 = __shfl_sync(0xffffffffu, dc, c + 1);
+                                    w[i] = pack_bf16x2(__uint_as_float(sv[2 * i]) * (c <= lane ? e0 * d0 : 0.f),
+                                                       __uint_as_float(sv[2 * i + 1]) * (c + 1 <= lane ? e1 * d1 : 0.f));
+                                }
+                            }
+                            if (cq == qd) {  // above the diagonal: zero
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) {
+                                    const int c = 16 * o + 2 * i;
+                                    w[i] = c < lane ? w[i] : c == lane ? w[i] & 0xffffu : 0u;
                                 }
                             }
                             tmem_st8(sw + 16 * o + 8 * e, w);
@@ -464,20 +522,13 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 epi_arrive(ms, bEpW);
             }
             // (b) w X -> hi (EH), lo
-            float before = 0.f, later = 0.f;  // decay of the blocks before / after this token's
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (q < qd) before += ms->tot[hs][q];
-                if (q > qd) later += ms->tot[hs][q];
-            }
-            const float total = before + ms->tot[hs][qd] + later;
-            const float yf = ex2(before + up);
+            const float yf = ex2(before + ms->cum[hs][r]);
             if (!kStateOnly) {  // C H has read EH (and C)
                 bar_wait(ms, bEvY2, par, p);
                 tc_fence_after();
             }
             {
-                const float wr = row_cf * ex2(later);
+                const float wr = ms->cf[hs][r] * ex2(later);
                 const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
@@ -503,80 +554,100 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 tc_fence_after();
                 const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
+                for (int c = 0; c < 32; c += 16) {
                     uint32_t y1[16], y2[16];
-                    tmem_ld16(tb + lane_base + kTY1 + c0 + 16 * half, y1);
-                    tmem_ld16(tb + lane_base + kTY2 + c0 + 16 * half, y2);
+                    tmem_ld16(tb + lane_base + kTY1 + c0 + c, y1);
+                    tmem_ld16(tb + lane_base + kTY2 + c0 + c, y2);
+                    uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
+                    uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
+                    const uint4 u0 = *at0, u1 = *at1;
+                    const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+                    uint32_t o[8];
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8) {
-                        uint4 *at = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + 16 * half + i));
-                        const uint4 u = *at;
-                        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-                        uint32_t o[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint64_t v = fma2(yf2, pair(y2[i + 2 * e], y2[i + 2 * e + 1]),
-                                                    pair(y1[i + 2 * e], y1[i + 2 * e + 1]));
-                            const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
-                            o[e] = in ? y : 0u;
-                        }
-                        *at = make_uint4(o[0], o[1], o[2], o[3]);
+                    for (int e = 0; e < 8; ++e) {
+                        const uint64_t v = fma2(yf2, pair(y2[2 * e], y2[2 * e + 1]), pair(y1[2 * e], y1[2 * e + 1]));
+                        const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
+                        o[e] = in ? y : 0u;
                     }
+                    *at0 = make_uint4(o[0], o[1], o[2], o[3]);
+                    *at1 = make_uint4(o[4], o[5], o[6], o[7]);
                 }
                 fence_async_smem();
             }
             tc_fence_before();
             epi_sync();  // the output is staged; every warp has done with the tile's steps
-            if (!kStateOnly && tid == 0) {
-                tma_store_4d(&tm_y, xs, 0, h0, t0, b);
-                if (both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
+            if (!kStateOnly && tid == kStorer) {
+                const volatile Misc *m = ms;
+                const int h = m->h0, bb = m->b;
+                tma_store_4d(&tm_y, xs, 0, h, t0, bb);
+                if (m->both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h : h + 1, t0, bb);
                 tma_store_commit();
             }
-            la_sum += total;
-            if (j + 1 < tiles) steps(j + 1);  // under B^T (w X)
+            if (kStateOnly) la_sum += total;
+            if (j + 1 < tiles) steps(j + 1, next_raw);  // under B^T (w X)
+            epi_sync();  // the next tile's decays are in shared memory
             // (d) the state after the tile
             bar_wait(ms, bEvU, par, p);
             tc_fence_after();
-            if (srow) {
-                const float keep = ex2(total);
-#pragma unroll
-                for (int o = 0; o < 32; o += 16) {
-                    uint32_t u[16];
-                    tmem_ld16(tb + lane_base + kTS + 128 * buf + c0 + o, u);
+            if (!kStateOnly && tid == kStorer) tma_store_wait_read();  // X's slot may be loaded again
+            if (j + 1 < tiles) {
+                decays();
+                if (srow) {
+                    const float keep = ex2(total);
+                    uint32_t u[2][16];
+                    tmem_ld16(h_at, u[0]);
+                    tmem_ld16(h_at + 16, u[1]);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) st[o + i] = fmaf(keep, st[o + i], __uint_as_float(u[i]));
+                    for (int o = 0; o < 2; ++o) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[o][i]);
+                        put_state(v, 16 * o, keep);
+                    }
                 }
+                state_is_put();
             }
-            if (!kStateOnly && tid == 0) tma_store_wait_read();  // X's slot may be loaded again
-            if (j + 1 < tiles) put_state();
         }
 
-        // the rest of the segment does not count: zeros
-        if (!kStateOnly && mine) {
-            for (int t = max(t_lo, live) + r; t < t_hi; t += kTile) {
-                __nv_bfloat16 *row = p.y + ((long long)b * p.n + t) * p.y_stride + (long long)head * p.P + hcol;
+        const volatile Misc *m = ms;
+        const int hcol = one ? c0 : (cq & 1) * 32;
+        const int head = m->h0 + (one ? 0 : hs);
+        const bool mine = !hs || m->both;
+        if (!kStateOnly && mine) {  // the rest of the segment does not count: zeros
+            const int end = min((m->seg + 1) * p.seg_tiles * kTile, p.n);
+            for (int t = max(m->seg * p.seg_tiles * kTile, live) + r; t < end; t += kTile) {
+                __nv_bfloat16 *row = p.y + ((long long)m->b * p.n + t) * p.y_stride + (long long)head * p.P + hcol;
 #pragma unroll
                 for (int i = 0; i < 32; i += 8)
-                    if (hcol + i < p.P) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0, 0, 0, 0);
+                    if (i < cols) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0, 0, 0, 0);
             }
         }
         float *to = nullptr;
         if (kStateOnly) {
-            to = p.seg_state + (bh * p.segments + seg) * NP;
-            if (mine && hcol == 0 && r == 0) p.seg_decay[bh * p.segments + seg] = la_sum * kLn2;
-        } else if (p.state_out && seg == p.segments - 1) {
-            to = p.state_out + bh * NP;
+            to = state_at(p.seg_state, p.segments, m->seg);
+            if (mine && hcol == 0 && r == 0)
+                p.seg_decay[((long long)m->b * p.H + head) * p.segments + m->seg] = la_sum * kLn2;
+        } else if (m->seg == p.segments - 1) {
+            to = state_at(p.state_out, 1, 0);
         }
-        if (to && mine && r < p.N) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4)
-                if (hcol + i < p.P)
-                    *reinterpret_cast<float4 *>(to + (long long)r * p.P + hcol + i) =
-                        make_float4(st[i], st[i + 1], st[i + 2], st[i + 3]);
+        for (int o = 0; o < 32; o += 16) {
+            uint32_t u[16];
+            tmem_ld16(h_at + o, u);  // by whole warps, wherever the values go
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                if (!to || o + i >= cols) continue;
+                float4 f = make_float4(__uint_as_float(u[i]), __uint_as_float(u[i + 1]), __uint_as_float(u[i + 2]),
+                                       __uint_as_float(u[i + 3]));
+                if (tiles == 0)  // nothing counts: the state as it was
+                    f = from ? *reinterpret_cast<const float4 *>(from + o + i) : make_float4(0.f, 0.f, 0.f, 0.f);
+                *reinterpret_cast<float4 *>(to + o + i) = f;
+            }
         }
-        if (!kStateOnly && tid == 0) tma_store_wait_all();
+        if (!kStateOnly && tid == kStorer) tma_store_wait_all();
     }
     tc_fence_before();
     __syncthreads();
