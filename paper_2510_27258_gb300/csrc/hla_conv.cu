@@ -10,7 +10,7 @@
 // About 2 W flops a value: bound by memory traffic.  A thread owns V neighbouring channels (one
 // 16-byte access a row, neighbouring lanes on neighbouring channels) and walks a strip of
 // consecutive tokens with the W - 1 previous rows in registers, so each x row is loaded once a strip
-// and W - 1 rows a strip are read twice (from L2).  Four rows are loaded ahead of their use.
+// and W - 1 rows a strip are read twice (from L2).  A ring of kAhead rows is in flight.
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -19,7 +19,7 @@ namespace hla {
 namespace {
 
 constexpr int kThreads = 256, kStrips = kThreads / 32;
-constexpr int kAhead = 4;  // rows a thread loads at once; strip lengths are multiples of it
+constexpr int kAhead = 4;  // rows a thread has in flight; strip lengths are multiples of it
 
 struct Geom {
     int B, n, C, L;          // L: tokens a strip
@@ -45,7 +45,25 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, int n) {
     return m < 0 ? 0 : m > n ? n : m;
 }
 
-__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// sigmoid(v[i]) for V values: exp(-v) is kept below 2^63 (v above -43.6, where v sigmoid(v) has come
+// down to 5e-18), so that two values can share one reciprocal (the multi-function unit is what they
+// wait for).  v itself is replaced by the kept value; NaN stays NaN.
+template <int V>
+__device__ __forceinline__ void sigmoids(float (&v)[V], float (&s)[V]) {
+    float a[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(v[i]) : "f"(v[i]), "f"(-43.6f));
+        a[i] = 1.f + __expf(-v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i + 1 < V; i += 2) {
+        const float r = __fdividef(1.f, a[i] * a[i + 1]);
+        s[i] = r * a[i + 1];
+        s[i + 1] = r * a[i];
+    }
+    if (V % 2) s[V - 1] = __fdividef(1.f, a[V - 1]);
+}
 
 // w[c0 .. c0 + V - 1][W] and bias[c0 ..] as fp32
 template <typename T, int W, int V>
@@ -88,32 +106,42 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
     const T *st = state_in ? state_in + (size_t)at.b * (W - 1) * g.C : nullptr;
     const int end = min(at.t0 + g.L, g.n), live = min(end, len);
     if (at.t0 < live) {
-        float wr[V][W], br[V], win[W - 1 + kAhead][V];
+        float wr[V][W], br[V], win[W][V];  // row t of x in win[t % W] (counted from the strip's start)
+        const T *src = x + (size_t)at.t0 * xs + at.c0;
+        Raw<T, V> ring[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            ring[u] = at.t0 + u < live ? raw_load<T, V>(src + (size_t)u * xs) : raw_zero<T, V>();
         load_taps<T, W, V>(w, bias, at.c0, wr, br);
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) load_row<T, W, V>(x, xs, st, g.C, at.c0, at.t0 - (W - 1) + i, win[i]);
-        for (int t = at.t0; t < live; t += kAhead) {
+        for (int i = 1; i < W; ++i) load_row<T, W, V>(x, xs, st, g.C, at.c0, at.t0 - W + i, win[i]);
+        // unrolled over a common multiple of the window's and the ring's turns
+        constexpr int kTurn = W == 3 ? 3 * kAhead : kAhead;
+        T *dst = out + (size_t)at.t0 * os;
+        for (int t = at.t0; t < live; t += kTurn) {
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
-                if (t + u < live) VecIo<T, V>::load(x + (size_t)(t + u) * xs + at.c0, win[W - 1 + u]);
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
+            for (int u = 0; u < kTurn; ++u) {
                 if (t + u < live) {
-                    float y[V];
+                    raw_floats(ring[u % kAhead], win[u % W]);
+                    if (t + u + kAhead < live) ring[u % kAhead] = raw_load<T, V>(src + (size_t)kAhead * xs);
+                    src += xs;
+                    float y[V], s[V];
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
                         float a = br[v];
 #pragma unroll
-                        for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], win[u + j][v], a);
-                        y[v] = kSilu ? a * sigmoid(a) : a;
+                        for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], win[(u + 1 + j) % W][v], a);
+                        y[v] = a;
                     }
-                    VecIo<T, V>::store(out + (size_t)(t + u) * os, y);
+                    if (kSilu) {
+                        sigmoids<V>(y, s);
+#pragma unroll
+                        for (int v = 0; v < V; ++v) y[v] *= s[v];
+                    }
+                    VecIo<T, V>::store(dst, y);
+                    dst += os;
                 }
             }
-#pragma unroll
-            for (int i = 0; i < W - 1; ++i)
-#pragma unroll
-                for (int v = 0; v < V; ++v) win[i][v] = win[kAhead + i][v];
         }
     }
     const float zero[V] = {};
@@ -150,7 +178,13 @@ conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, co
         float a = br[v];
 #pragma unroll
         for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], win[j][v], a);
-        y[v] = kSilu ? a * sigmoid(a) : a;
+        y[v] = a;
+    }
+    if (kSilu) {
+        float s[V];
+        sigmoids<V>(y, s);
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[v] *= s[v];
     }
     VecIo<T, V>::store(out + b * os + c0, y);
 #pragma unroll
@@ -177,7 +211,16 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
         dx += (size_t)at.b * g.n * ds + at.c0;
         const int end = min(at.t0 + g.L, g.n), live = min(end, len);
         if (at.t0 < live) {
+            // rows t of x and g in xw[t % W], gw[t % W] (counted from the strip's start)
             float wr[V][W], br[V], xw[W][V], gw[W][V];
+            const int last = min(live + W - 1, len);  // tokens from here on have g = 0
+            Raw<T, V> xr[kAhead], gr[kAhead];
+            const T *xp = x + (size_t)at.t0 * xs, *gp = dout + (size_t)at.t0 * gs;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                xr[u] = at.t0 + u < last ? raw_load<T, V>(xp + (size_t)u * xs) : raw_zero<T, V>();
+                gr[u] = at.t0 + u < last ? raw_load<T, V>(gp + (size_t)u * gs) : raw_zero<T, V>();
+            }
             load_taps<T, W, V>(w, bias, at.c0, wr, br);
 #pragma unroll
             for (int i = 0; i < W; ++i) {
@@ -185,57 +228,61 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
                 for (int v = 0; v < V; ++v) xw[i][v] = gw[i][v] = 0.f;
                 if (i > 0 && at.t0 - W + i >= 0) VecIo<T, V>::load(x + (ptrdiff_t)(at.t0 - W + i) * (ptrdiff_t)xs, xw[i]);
             }
-            for (int t = at.t0; t < live + W - 1; t += kAhead) {
-                float xn[kAhead][V], gn[kAhead][V];
+            constexpr int kTurn = W == 3 ? 3 * kAhead : kAhead;
+            T *to = dx + (size_t)at.t0 * ds;  // of token t + u - (W - 1), once its g and the next W - 1 are there
+            for (int t = at.t0; t < live + W - 1; t += kTurn) {
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) xn[u][v] = gn[u][v] = 0.f;
-                    if (t + u < live + W - 1 && t + u < len) {
-                        VecIo<T, V>::load(x + (size_t)(t + u) * xs, xn[u]);
-                        VecIo<T, V>::load(dout + (size_t)(t + u) * gs, gn[u]);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
+                for (int u = 0; u < kTurn; ++u) {
                     const int tt = t + u;
-                    // windows of the last W rows: xw[W-1] = x_tt, gw[W-1] = g_tt
-#pragma unroll
-                    for (int i = 0; i < W - 1; ++i)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            xw[i][v] = xw[i + 1][v];
-                            gw[i][v] = gw[i + 1][v];
+                    if (tt < live + W - 1) {
+                        float(&xc)[V] = xw[u % W];
+                        float(&gc)[V] = gw[u % W];
+                        raw_floats(xr[u % kAhead], xc);
+                        raw_floats(gr[u % kAhead], gc);
+                        if (tt + kAhead < last) {
+                            xr[u % kAhead] = raw_load<T, V>(xp + (size_t)kAhead * xs);
+                            gr[u % kAhead] = raw_load<T, V>(gp + (size_t)kAhead * gs);
+                        } else {
+                            xr[u % kAhead] = gr[u % kAhead] = raw_zero<T, V>();
                         }
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        xw[W - 1][v] = xn[u][v];
-                        float gt = gn[u][v];
+                        xp += xs;
+                        gp += gs;
                         if (kSilu) {
-                            float a = br[v];
+                            float a[V], s[V];
 #pragma unroll
-                            for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], xw[j][v], a);
-                            const float s = sigmoid(a);
-                            gt *= s * (1.f + a * (1.f - s));
+                            for (int v = 0; v < V; ++v) {
+                                a[v] = br[v];
+#pragma unroll
+                                for (int j = 0; j < W; ++j) a[v] = fmaf(wr[v][j], xw[(u + 1 + j) % W][v], a[v]);
+                            }
+                            sigmoids<V>(a, s);
+#pragma unroll
+                            for (int v = 0; v < V; ++v) gc[v] *= s[v] * fmaf(a[v], 1.f - s[v], 1.f);
                         }
-                        gw[W - 1][v] = tt < len ? gt : 0.f;
+                        if (tt >= len) {  // (silu' of a row that was not read may be anything)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) gc[v] = 0.f;
+                        }
                         if (tt < live) {
 #pragma unroll
-                            for (int j = 0; j < W; ++j) dw[j][v] = fmaf(gt, xw[j][v], dw[j][v]);
-                            dw[W][v] += gt;
-                        }
-                    }
-                    // dx of token tt - (W-1): its g and the next W - 1 are in gw[0 .. W-1]
-                    if (tt - (W - 1) >= at.t0 && tt - (W - 1) < live) {
-                        float d[V];
+                            for (int v = 0; v < V; ++v) {
 #pragma unroll
-                        for (int v = 0; v < V; ++v) {
-                            float a = 0.f;
-#pragma unroll
-                            for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], gw[W - 1 - j][v], a);
-                            d[v] = a;
+                                for (int j = 0; j < W; ++j) dw[j][v] = fmaf(gc[v], xw[(u + 1 + j) % W][v], dw[j][v]);
+                                dw[W][v] += gc[v];
+                            }
                         }
-                        VecIo<T, V>::store(dx + (size_t)(tt - (W - 1)) * ds, d);
+                        if (tt - (W - 1) >= at.t0) {
+                            float d[V];
+#pragma unroll
+                            for (int v = 0; v < V; ++v) {
+                                float a = 0.f;
+#pragma unroll
+                                for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], gw[(u + W - j) % W][v], a);
+                                d[v] = a;
+                            }
+                            VecIo<T, V>::store(to, d);
+                            to += ds;
+                        }
                     }
                 }
             }

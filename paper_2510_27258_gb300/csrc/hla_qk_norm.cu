@@ -21,6 +21,7 @@ namespace hla {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 4, kAheadBwd = 2;  // heads whose rows a thread has in flight
 
 // V elements at p: one access, or element by element where rows are not aligned to it
 template <typename T, int V, bool kVec>
@@ -31,6 +32,27 @@ __device__ __forceinline__ void load_row(const T *p, float (&v)[V]) {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = to_f32(p[i]);
     }
+}
+
+template <typename T, int V, bool kVec>
+__device__ __forceinline__ Raw<T, V> load_raw(const T *p) {
+    if (kVec) return raw_load<T, V>(p);
+    Raw<T, V> r;
+    T *e = reinterpret_cast<T *>(&r);
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = p[i];
+    return r;
+}
+
+// the row another lane holds
+template <typename R>
+__device__ __forceinline__ R raw_from(const R &r, int lane) {
+    R got;
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(&r);
+    uint32_t *to = reinterpret_cast<uint32_t *>(&got);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(R) / 4); ++i) to[i] = __shfl_sync(0xffffffffu, from[i], lane);
+    return got;
 }
 
 template <typename T, int V, bool kVec>
@@ -112,32 +134,59 @@ __global__ void __launch_bounds__(kThreads) qk_norm_forward_kernel(QkNorm p, Spl
     const int half = p.rot / 2;
     const bool turned = i0 < p.rot, paired = turned && !p.interleaved;
     const int partner = paired ? (i0 < half ? half : -half) : 0;
+    const int mate_lane = (int)(threadIdx.x & 31) + partner / V;
     const int h_lo = blockIdx.y * sp.hpb, h_hi = min(h_lo + sp.hpb, p.H + p.Hk);
 
     auto walk = [&](const T *x, T *out, const void *weight, int lo, int hi, int per) {
         if (lo >= hi) return;
-        float w[V], wp[V];
-        load_weight<T, V>(weight, i0, w);
-        load_weight<T, V>(weight, i0 + partner, wp);
-#pragma unroll 4
-        for (int h = lo; h < hi; ++h) {
-            const T *src = x + (size_t)h * D + i0;
-            float v[V], vp[V];
-            load_row<T, V, kVec>(src, v);
-            if (paired) load_row<T, V, kVec>(src + partner, vp);
-            float ss = 0.f;
+        // the rotation with the weights in it: out_i = r (v_i wc_i + v_p(i) ws_i)
+        float wc[V], ws[V];
+        load_weight<T, V>(weight, i0, wc);
+        load_weight<T, V>(weight, i0 + partner, ws);
+        if (turned && p.interleaved) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) ss = fmaf(v[e], v[e], ss);
-            const float r = rsqrtf(row_sum<kLanes>(ss) * (1.f / D) + p.eps);
-            float y[V];
+            for (int e = 0; e < V; ++e) ws[e] = wc[e ^ 1] * s[e];
+#pragma unroll
+            for (int e = 0; e < V; ++e) wc[e] *= c[e];
+        } else {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float mate = paired ? vp[e] * r * wp[e] : turned ? v[e ^ 1] * r * w[e ^ 1] : 0.f;
-                y[e] = fmaf(v[e] * r * w[e], c[e], mate * s[e]);
+                wc[e] *= c[e];
+                ws[e] *= s[e];
             }
-            if (row < rows)
-                for (int m = 0; m < per; ++m)
-                    VecIo<T, V>::store(out + (((size_t)b * p.H + (size_t)h * per + m) * p.n + t) * D + i0, y);
+        }
+        T *to = out + (((size_t)b * p.H + (size_t)lo * per) * p.n + t) * D + i0;
+        const size_t step = (size_t)p.n * D;
+        Raw<T, V> ring[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            ring[u] = lo + u < hi ? load_raw<T, V, kVec>(x + (size_t)(lo + u) * D + i0) : raw_zero<T, V>();
+        for (int h = lo; h < hi; h += kAhead) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (h + u >= hi) break;
+                const Raw<T, V> raw = ring[u];
+                if (h + u + kAhead < hi) ring[u] = load_raw<T, V, kVec>(x + (size_t)(h + u + kAhead) * D + i0);
+                float v[V], m[V];
+                raw_floats(raw, v);
+                if (p.interleaved) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) m[e] = v[e ^ 1];
+                } else {
+                    raw_floats(raw_from(raw, mate_lane), m);
+                }
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) ss = fmaf(v[e], v[e], ss);
+                const float r = rsqrtf(row_sum<kLanes>(ss) * (1.f / D) + p.eps);
+                float y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = r * fmaf(v[e], wc[e], turned ? m[e] * ws[e] : 0.f);
+                for (int k = 0; k < per; ++k) {
+                    if (row < rows) VecIo<T, V>::store(to, y);
+                    to += step;
+                }
+            }
         }
     };
     walk(static_cast<const T *>(p.q) + (size_t)r0 * p.q_stride, static_cast<T *>(p.q_out), p.wq, h_lo,
@@ -168,39 +217,57 @@ __global__ void __launch_bounds__(kThreads) qk_norm_backward_kernel(QkNormBwd p,
     auto walk = [&](const T *x, const T *dout, T *dx, const void *weight, int lo, int hi, int per, float (&dw)[V]) {
         float w[V];
         load_weight<T, V>(weight, i0, w);
-#pragma unroll 2
-        for (int h = lo; h < hi; ++h) {
-            float v[V], g[V];
-            load_row<T, V, kVec>(x + (size_t)h * D + i0, v);
-            const T *src = dout + (((size_t)b * f.H + (size_t)h * per) * f.n + t) * D + i0;
-            VecIo<T, V>::load(src, g);
-            for (int m = 1; m < per; ++m) {
-                float more[V];
-                VecIo<T, V>::load(src + (size_t)m * f.n * D, more);
+        const size_t step = (size_t)f.n * D;
+        const T *src = dout + (((size_t)b * f.H + (size_t)lo * per) * f.n + t) * D + i0;
+        Raw<T, V> xr[kAheadBwd], gr[kAheadBwd];
 #pragma unroll
-                for (int e = 0; e < V; ++e) g[e] += more[e];
+        for (int u = 0; u < kAheadBwd; ++u) {
+            const bool on = lo + u < hi;
+            xr[u] = on ? load_raw<T, V, kVec>(x + (size_t)(lo + u) * D + i0) : raw_zero<T, V>();
+            gr[u] = on ? raw_load<T, V>(src + (size_t)u * per * step) : raw_zero<T, V>();
+        }
+        for (int h0 = lo; h0 < hi; h0 += kAheadBwd) {
+#pragma unroll
+            for (int u = 0; u < kAheadBwd; ++u) {
+                const int h = h0 + u;
+                if (h >= hi) break;
+                float v[V], g[V];
+                raw_floats(xr[u], v);
+                raw_floats(gr[u], g);
+                for (int m = 1; m < per; ++m) {
+                    float more[V];
+                    VecIo<T, V>::load(src + (size_t)m * step, more);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) g[e] += more[e];
+                }
+                if (h + kAheadBwd < hi) {
+                    xr[u] = load_raw<T, V, kVec>(x + (size_t)(h + kAheadBwd) * D + i0);
+                    gr[u] = raw_load<T, V>(src + (size_t)kAheadBwd * per * step);
+                }
+                src += (size_t)per * step;
+                float dy[V], ss = 0.f, dot = 0.f;
+                float gp[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) gp[e] = f.interleaved ? g[e ^ 1] : __shfl_sync(0xffffffffu, g[e], mate_lane);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    dy[e] = fmaf(g[e], c[e], turned ? -gp[e] * s[e] : 0.f);
+                    ss = fmaf(v[e], v[e], ss);
+                    dot = fmaf(dy[e] * w[e], v[e], dot);
+                }
+                ss = row_sum<kLanes>(ss);
+                dot = row_sum<kLanes>(dot);
+                const float r = rsqrtf(ss * (1.f / D) + f.eps);
+                const float m = dot * r * (1.f / D);
+                float d[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float unit = v[e] * r;
+                    d[e] = r * fmaf(dy[e], w[e], -unit * m);
+                    if (real) dw[e] = fmaf(dy[e], unit, dw[e]);
+                }
+                if (real) store_row<T, V, kVec>(dx + (size_t)h * D + i0, d);
             }
-            float dy[V], ss = 0.f, dot = 0.f;
-            float gp[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) gp[e] = __shfl_sync(0xffffffffu, g[e], mate_lane);
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float mate = paired ? gp[e] : turned ? g[e ^ 1] : 0.f;
-                dy[e] = fmaf(g[e], c[e], -mate * s[e]);
-                ss = fmaf(v[e], v[e], ss);
-                dot = fmaf(dy[e] * w[e], v[e], dot);
-            }
-            const float r = rsqrtf(row_sum<kLanes>(ss) * (1.f / D) + f.eps);
-            const float m = row_sum<kLanes>(dot) * r * (1.f / D);
-            float d[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float u = v[e] * r;
-                d[e] = r * (dy[e] * w[e] - u * m);
-                if (real) dw[e] = fmaf(dy[e], u, dw[e]);
-            }
-            if (real) store_row<T, V, kVec>(dx + (size_t)h * D + i0, d);
         }
     };
     float dwq[V] = {}, dwk[V] = {};

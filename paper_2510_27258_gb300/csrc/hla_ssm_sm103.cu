@@ -279,7 +279,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if (!kStateOnly && tiles > 0 && (ok = wait_ld(0))) score(0);
             for (int j = 0; ok && j < tiles; ++j) {
                 const int buf = j & 1, par = j & 1;
-                // H before the tile is in EH; the previous tile is read out, its buffers are free
+                // H before the tile is in EH and TMEM; the previous tile is read out, its buffers are free
                 if (!(ok = bar_wait(ms, bEpE, par, p))) break;
                 tc_fence_after();
                 if (!kStateOnly) {
@@ -292,12 +292,11 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 } else {
                     if (!(ok = bar_wait(ms, bEpW, par, p))) break;
                     tc_fence_after();
-                    const uint32_t w = tb + kTS;
                     if (one) {
-                        mma_ts<128>(tb + kTY1, w, lm(Sm::X(buf)));
+                        mma_ts<128>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
                     } else {
-                        mma_ts<64>(tb + kTY1, w, lm(Sm::X(buf)));
-                        mma_ts<64>(tb + kTY1 + 64, w + 8, lm(Sm::X(buf) + kBlockBytes));
+                        mma_ts<64>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
+                        mma_ts<64>(tb + kTY1 + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
                     }
                     umma_commit(&ms->bar[bEvY1]);
                 }
@@ -427,115 +426,137 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             state_is_put();
         }
 
-        for (int j = 0; j < tiles; ++j) {
-            const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
-            uint8_t *xs = smem + Sm::X(buf);
-            const bool in = t0 + r < live;
-            const __nv_bfloat16 next_raw = fetch();  // of the next tile, used at the end of this one
+        // waits for tile j's copies; tokens that do not count: zero rows of X and B, whatever was read
+        auto landed = [&](int j) {
+            const int buf = j & 1, t0 = t_lo + j * kTile;
             bar_wait(ms, bLd0 + buf, (j >> 1) & 1, p);
-            if (t0 + kTile > live) {  // tokens that do not count: zero rows of X and B, whatever was read
-                if (!in) {
+            if (t0 + kTile > live) {
+                if (t0 + r >= live) {
                     const uint4 z = make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
-                        *reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + i)) = z;
+                        *reinterpret_cast<uint4 *>(smem + Sm::X(buf) + tile_off(r, c0 + i)) = z;
                         if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(buf) + tile_off(r, c0 + i)) = z;
                     }
                 }
                 fence_async_smem();
             }
-            // (a) W = S . decay, packed bf16 in S's place: this thread's 32 columns of both halves.  A
-            // step of 16 columns turns into 8 words of the first half's W and 8 of the second's.
-            if (!kStateOnly) {
-                const uint32_t sw = tb + lane_base + kTS + c0;
-                bar_wait(ms, bEvS, par, p);
-                tc_fence_after();
-                if (cq > qd) {
-                    uint32_t w[16];
+        };
+
+        // W = S . decay of tile j, packed bf16 in S's place: this thread's 32 columns of both halves.  A
+        // step of 16 columns turns into 8 words of the first half's W and 8 of the second's.
+        auto weights = [&](int j) {
+            const uint32_t sw = tb + lane_base + kTS + c0;
+            // a row's factor: the decay from the end of the columns' block to the token.  In the diagonal
+            // block that is the inverse of the decay still to come, finite unless the block decays by
+            // more than 2^-kFactored; then every pair takes its own exponential.
+            float rf[2];
+            bool factored = true;
+            if (cq <= qd) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = 0u;
-                    tmem_st16(sw, w);
-                    tmem_st16(sw + 16, w);
-                } else {
-                    // a row's factor: the decay from the end of the columns' block to the token.  In the
-                    // diagonal block that is the inverse of the decay still to come, finite unless the
-                    // block decays by more than 2^-kFactored; then every pair takes its own exponential.
-                    float rf[2];
-                    bool factored = true;
+                for (int e = 0; e < 2; ++e) {
+                    const float own = ms->tot[e][qd];
+                    float x = ms->cum[e][r] - (cq == qd ? own : 0.f);
+                    if (cq < 1 && qd > 1) x += ms->tot[e][1];
+                    if (cq < 2 && qd > 2) x += ms->tot[e][2];
+                    rf[e] = ex2(x);
+                    if (cq == qd && !(fabsf(own) <= kFactored)) factored = false;
+                }
+            }
+            landed(j);
+            bar_wait(ms, bEvS, j & 1, p);
+            tc_fence_after();
+            if (cq > qd) {
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = 0u;
+                tmem_st16(sw, w);
+                tmem_st16(sw + 16, w);
+            } else if (factored) {
+                const uint64_t rf0 = pair(rf[0], rf[0]), rf1 = pair(rf[1], rf[1]);
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    uint32_t sv[16], w[8];
+                    tmem_ld16(sw + 16 * o, sv);
+                    tmem_ld_wait();
+                    if (cq == qd) {  // above the diagonal: zero
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (16 * o + i > lane) sv[i] = 0u;
+                    }
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float own = ms->tot[e][qd];
-                        float x = ms->cum[e][r] - (cq == qd ? own : 0.f);
-                        if (cq < 1 && qd > 1) x += ms->tot[e][1];
-                        if (cq < 2 && qd > 2) x += ms->tot[e][2];
-                        rf[e] = ex2(x);
-                        if (cq == qd && !(fabsf(own) <= kFactored)) factored = false;
-                    }
+                        if (e == 1 && one) break;
+                        const ulonglong2 *cf = reinterpret_cast<const ulonglong2 *>(&ms->cf[e][c0 + 16 * o]);
 #pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        uint32_t sv[16], w[8];
-                        tmem_ld16(sw + 16 * o, sv);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            if (e == 1 && one) break;
-                            if (factored) {
-                                const ulonglong2 *cf = reinterpret_cast<const ulonglong2 *>(&ms->cf[e][c0 + 16 * o]);
-                                const uint64_t rf2 = pair(rf[e], rf[e]);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const ulonglong2 f = cf[i];
-                                    w[2 * i] = bf16_of(mul2(pair(sv[4 * i], sv[4 * i + 1]), mul2(rf2, f.x)));
-                                    w[2 * i + 1] = bf16_of(mul2(pair(sv[4 * i + 2], sv[4 * i + 3]), mul2(rf2, f.y)));
-                                }
-                            } else {
-                                const volatile Misc *m = ms;
-                                const int tc = t0 + c0 + lane, he = m->h0 + (e && m->both ? 1 : 0);
-                                float dc = 0.f;  // the step of this lane's column
-                                if (tc < live) {
-                                    dc = to_f32(p.delta[((long long)m->b * p.n + tc) * p.delta_stride + he]) +
-                                         (p.delta_bias ? p.delta_bias[he] : 0.f);
-                                    dc = p.softplus ? softplus(dc) : dc;
-                                }
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    const int c = 16 * o + 2 * i;
-                                    const float e0 = ex2(m->cum[e][r] - m->cum[e][c0 + c]);
-                                    const float e1 = ex2(m->cum[e][r] - m->cum[e][c0 + c + 1]);
-                                    const float d0 = __shfl_sync(0xffffffffu, dc, c), d1 = __shfl_sync(0xffffffffu, dc, c + 1);
-                                    w[i] = pack_bf16x2(__uint_as_float(sv[2 * i]) * (c <= lane ? e0 * d0 : 0.f),
-                                                       __uint_as_float(sv[2 * i + 1]) * (c + 1 <= lane ? e1 * d1 : 0.f));
-                                }
-                            }
-                            if (cq == qd) {  // above the diagonal: zero
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) {
-                                    const int c = 16 * o + 2 * i;
-                                    w[i] = c < lane ? w[i] : c == lane ? w[i] & 0xffffu : 0u;
-                                }
-                            }
-                            tmem_st8(sw + 16 * o + 8 * e, w);
+                        for (int i = 0; i < 4; ++i) {
+                            const ulonglong2 f = cf[i];
+                            w[2 * i] = bf16_of(mul2(pair(sv[4 * i], sv[4 * i + 1]), mul2(e ? rf1 : rf0, f.x)));
+                            w[2 * i + 1] = bf16_of(mul2(pair(sv[4 * i + 2], sv[4 * i + 3]), mul2(e ? rf1 : rf0, f.y)));
                         }
+                        tmem_st8(sw + 16 * o + 8 * e, w);
                     }
                 }
-                tmem_st_wait();
-                epi_arrive(ms, bEpW);
+            } else {
+                const volatile Misc *m = ms;
+                const int tc = t_lo + j * kTile + c0 + lane;  // this lane's column
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    uint32_t sv[16], w[8];
+                    tmem_ld16(sw + 16 * o, sv);
+                    tmem_ld_wait();
+#pragma unroll 1
+                    for (int e = 0; e < 2; ++e) {
+                        const int he = m->h0 + (e && m->both && !one ? 1 : 0);
+                        float dc = 0.f;  // its step
+                        if (tc < live) {
+                            dc = to_f32(p.delta[((long long)m->b * p.n + tc) * p.delta_stride + he]) +
+                                 (p.delta_bias ? p.delta_bias[he] : 0.f);
+                            dc = p.softplus ? softplus(dc) : dc;
+                        }
+                        const float lr = m->cum[e][r];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int c = 16 * o + 2 * i;
+                            const float d0 = __shfl_sync(0xffffffffu, dc, c), d1 = __shfl_sync(0xffffffffu, dc, c + 1);
+                            const float w0 = c <= lane ? ex2(lr - m->cum[e][c0 + c]) * d0 : 0.f;
+                            const float w1 = c + 1 <= lane ? ex2(lr - m->cum[e][c0 + c + 1]) * d1 : 0.f;
+                            w[i] = pack_bf16x2(c <= lane ? __uint_as_float(sv[2 * i]) * w0 : 0.f,
+                                               c + 1 <= lane ? __uint_as_float(sv[2 * i + 1]) * w1 : 0.f);
+                        }
+                        tmem_st8(sw + 16 * o + 8 * e, w);
+                    }
+                }
             }
+            tmem_st_wait();
+            epi_arrive(ms, bEpW);
+        };
+        for (int j = 0; j < tiles; ++j) {
+            const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
+            uint8_t *xs = smem + Sm::X(buf);
+            const bool in = t0 + r < live;
+            const __nv_bfloat16 next_raw = fetch();  // of the next tile
+            // (a) W
+            if (kStateOnly) {
+                la_sum += total;
+                landed(j);
+            } else {
+                weights(j);
+            }
+            const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
             // (b) w X -> hi (EH), lo
-            const float yf = ex2(before + ms->cum[hs][r]);
             if (!kStateOnly) {  // C H has read EH (and C)
                 bar_wait(ms, bEvY2, par, p);
                 tc_fence_after();
             }
             {
-                const float wr = ms->cf[hs][r] * ex2(later);
                 const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
 #pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    const uint32_t off = tile_off(r, c0 + i);
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t off = tile_off(r, c0 + 8 * i);
                     const uint4 u = *reinterpret_cast<const uint4 *>(xs + off);
-                    uint32_t hi[4], lo[4];
                     const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+                    uint32_t hi[4], lo[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const uint64_t v = mul2(wr2, of_bf16(x[e]));
@@ -555,14 +576,13 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
 #pragma unroll
                 for (int c = 0; c < 32; c += 16) {
-                    uint32_t y1[16], y2[16];
+                    uint32_t y1[16], y2[16], o[8];
                     tmem_ld16(tb + lane_base + kTY1 + c0 + c, y1);
                     tmem_ld16(tb + lane_base + kTY2 + c0 + c, y2);
                     uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
                     uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
                     const uint4 u0 = *at0, u1 = *at1;
                     const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
-                    uint32_t o[8];
                     tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -576,7 +596,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 fence_async_smem();
             }
             tc_fence_before();
-            epi_sync();  // the output is staged; every warp has done with the tile's steps
+            epi_sync();  // the output is staged; every warp has done with the tile's decays
             if (!kStateOnly && tid == kStorer) {
                 const volatile Misc *m = ms;
                 const int h = m->h0, bb = m->b;
@@ -584,7 +604,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 if (m->both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h : h + 1, t0, bb);
                 tma_store_commit();
             }
-            if (kStateOnly) la_sum += total;
             if (j + 1 < tiles) steps(j + 1, next_raw);  // under B^T (w X)
             epi_sync();  // the next tile's decays are in shared memory
             // (d) the state after the tile

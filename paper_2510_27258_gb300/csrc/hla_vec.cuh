@@ -2,6 +2,8 @@
 // access where V > 1 (the caller guarantees V-element alignment), else scalar.
 #pragma once
 
+#include <string.h>
+
 #include "hla_internal.h"
 
 namespace hla {
@@ -57,6 +59,47 @@ struct VecIo<__nv_bfloat16, 8> {
             make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
     }
 };
+
+// V elements as they are stored (for loads issued well before their use), and as fp32 pairs
+template <typename T, int V>
+struct Raw {
+    T v[V];
+};
+template <>
+struct Raw<float, 4> {
+    float4 v;
+};
+template <>
+struct Raw<__nv_bfloat16, 4> {
+    uint2 v;
+};
+template <>
+struct Raw<__nv_bfloat16, 8> {
+    uint4 v;
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> raw_load(const T *p) {
+    return *reinterpret_cast<const Raw<T, V> *>(p);
+}
+template <typename T, int V>
+__device__ __forceinline__ Raw<T, V> raw_zero() {
+    Raw<T, V> r;
+    memset(&r, 0, sizeof(r));
+    return r;
+}
+__device__ __forceinline__ void raw_floats(const Raw<float, 1> &r, float (&f)[1]) { f[0] = r.v[0]; }
+__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 1> &r, float (&f)[1]) { f[0] = to_f32(r.v[0]); }
+__device__ __forceinline__ void raw_floats(const Raw<float, 4> &r, float (&f)[4]) {
+    f[0] = r.v.x; f[1] = r.v.y; f[2] = r.v.z; f[3] = r.v.w;
+}
+__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 4> &r, float (&f)[4]) {
+    f[0] = bf16_lo(r.v.x); f[1] = bf16_hi(r.v.x); f[2] = bf16_lo(r.v.y); f[3] = bf16_hi(r.v.y);
+}
+__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 8> &r, float (&f)[8]) {
+    f[0] = bf16_lo(r.v.x); f[1] = bf16_hi(r.v.x); f[2] = bf16_lo(r.v.y); f[3] = bf16_hi(r.v.y);
+    f[4] = bf16_lo(r.v.z); f[5] = bf16_hi(r.v.z); f[6] = bf16_lo(r.v.w); f[7] = bf16_hi(r.v.w);
+}
 
 // whether a base pointer and a row stride (elements of `eb` bytes) keep every row aligned to `bytes`
 inline bool rows_aligned(const void *p, long long stride, size_t eb, size_t bytes) {
