@@ -19,7 +19,9 @@ namespace hla {
 namespace {
 
 constexpr int kThreads = 256, kStrips = kThreads / 32;
-constexpr int kAhead = 4;  // rows a thread has in flight; strip lengths are multiples of it
+constexpr int kAhead = 8;  // rows a thread has in flight
+constexpr int kAheadBwd = 4;
+constexpr int kStrip = 4;  // strip lengths are multiples of this
 
 struct Geom {
     int B, n, C, L;          // L: tokens a strip
@@ -45,52 +47,53 @@ __device__ __forceinline__ int length_of(const int *lengths, int b, int n) {
     return m < 0 ? 0 : m > n ? n : m;
 }
 
-// sigmoid(v[i]) for V values: exp(-v) is kept below 2^63 (v above -43.6, where v sigmoid(v) has come
-// down to 5e-18), so that two values can share one reciprocal (the multi-function unit is what they
-// wait for).  v itself is replaced by the kept value; NaN stays NaN.
-template <int V>
-__device__ __forceinline__ void sigmoids(float (&v)[V], float (&s)[V]) {
-    float a[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(v[i]) : "f"(v[i]), "f"(-43.6f));
-        a[i] = 1.f + __expf(-v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i + 1 < V; i += 2) {
-        const float r = __fdividef(1.f, a[i] * a[i + 1]);
-        s[i] = r * a[i + 1];
-        s[i + 1] = r * a[i];
-    }
-    if (V % 2) s[V - 1] = __fdividef(1.f, a[V - 1]);
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
 
-// w[c0 .. c0 + V - 1][W] and bias[c0 ..] as fp32
+// sigmoids of a pair.  exp(-v) is kept below 2^63 (v above -43.6, where v sigmoid(v) has come down to
+// 5e-18), so that two values can share one reciprocal: the multi-function unit takes 1.5 operations
+// a value instead of 2.  v itself is replaced by the kept value; NaN stays NaN.
+__device__ __forceinline__ void sigmoids(uint64_t &v, float &s0, float &s1) {
+    float v0, v1, e0, e1, r;
+    unpair(v, v0, v1);
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v0) : "f"(v0), "f"(-43.6f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v1) : "f"(v1), "f"(-43.6f));
+    v = pair(v0, v1);
+    unpair(mul2(v, pair(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
+    unpair(add2(pair(fast_exp2(e0), fast_exp2(e1)), pair(1.f, 1.f)), e0, e1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e0 * e1));
+    s0 = r * e1;
+    s1 = r * e0;
+}
+
+// w[c0 .. c0 + V - 1][W] and bias[c0 ..] as pairs of channels
 template <typename T, int W, int V>
-__device__ __forceinline__ void load_taps(const T *w, const T *bias, int c0, float (&wr)[V][W], float (&br)[V]) {
+__device__ __forceinline__ void load_taps(const T *w, const T *bias, int c0, uint64_t (&wr)[W][(V + 1) / 2],
+                                          uint64_t (&br)[(V + 1) / 2]) {
     float flat[W][V];  // V W consecutive elements
 #pragma unroll
     for (int i = 0; i < W; ++i) VecIo<T, V>::load(w + (size_t)c0 * W + i * V, flat[i]);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; v += 2)
 #pragma unroll
-        for (int j = 0; j < W; ++j) wr[v][j] = flat[(v * W + j) / V][(v * W + j) % V];
+        for (int j = 0; j < W; ++j) {
+            const int a = v * W + j, b = a + W;
+            wr[j][v / 2] = pair(flat[a / V][a % V], v + 1 < V ? flat[(b / V) % W][b % V] : 0.f);
+        }
 #pragma unroll
-    for (int v = 0; v < V; ++v) br[v] = 0.f;
-    if (bias) VecIo<T, V>::load(bias + c0, br);
+    for (int v = 0; v < (V + 1) / 2; ++v) br[v] = pair(0.f, 0.f);
+    if (bias) to_pairs(raw_load<T, V>(bias + c0), br);
 }
 
 // row t of x (t >= 0), of the state (-(W-1) <= t < 0), or zero
 template <typename T, int W, int V>
-__device__ __forceinline__ void load_row(const T *x, size_t stride, const T *state, int C, int c0, int t, float (&r)[V]) {
-    if (t >= 0) {
-        VecIo<T, V>::load(x + (size_t)t * stride + c0, r);
-    } else if (state) {
-        VecIo<T, V>::load(state + (size_t)(t + W - 1) * C + c0, r);
-    } else {
-#pragma unroll
-        for (int v = 0; v < V; ++v) r[v] = 0.f;
-    }
+__device__ __forceinline__ Raw<T, V> load_row(const T *x, size_t stride, const T *state, int C, int c0, int t) {
+    if (t >= 0) return raw_load<T, V>(x + (size_t)t * stride + c0);
+    if (state) return raw_load<T, V>(state + (size_t)(t + W - 1) * C + c0);
+    return raw_zero<T, V>();
 }
 
 template <typename T, int W, int V, bool kSilu>
@@ -98,6 +101,7 @@ __global__ void __launch_bounds__(kThreads)
 conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ bias,
                     T *__restrict__ out, size_t xs, size_t os, const int *__restrict__ lengths, const T *state_in,
                     T *state_out) {
+    __shared__ Raw<T, V> ring[kAhead][kThreads];
     const Place at = place<V>(g);
     if (at.c0 >= g.C) return;
     const int len = length_of(lengths, at.b, g.n);
@@ -106,39 +110,45 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
     const T *st = state_in ? state_in + (size_t)at.b * (W - 1) * g.C : nullptr;
     const int end = min(at.t0 + g.L, g.n), live = min(end, len);
     if (at.t0 < live) {
-        float wr[V][W], br[V], win[W][V];  // row t of x in win[t % W] (counted from the strip's start)
+        constexpr int kP = (V + 1) / 2;
+        uint64_t wr[W][kP], br[kP], win[W][kP];  // row t of x in win[t % W] (counted from the strip's start)
         const T *src = x + (size_t)at.t0 * xs + at.c0;
-        Raw<T, V> ring[kAhead];
+        const int count = live - at.t0;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            ring[u] = at.t0 + u < live ? raw_load<T, V>(src + (size_t)u * xs) : raw_zero<T, V>();
+        for (int u = 0; u < kAhead; ++u) {
+            ring_copy<T, V>(&ring[u][threadIdx.x], src + (size_t)u * xs, u < count);
+            ring_commit();
+        }
         load_taps<T, W, V>(w, bias, at.c0, wr, br);
 #pragma unroll
-        for (int i = 1; i < W; ++i) load_row<T, W, V>(x, xs, st, g.C, at.c0, at.t0 - W + i, win[i]);
+        for (int i = 1; i < W; ++i) to_pairs(load_row<T, W, V>(x, xs, st, g.C, at.c0, at.t0 - W + i), win[i]);
         // unrolled over a common multiple of the window's and the ring's turns
         constexpr int kTurn = W == 3 ? 3 * kAhead : kAhead;
         T *dst = out + (size_t)at.t0 * os;
-        for (int t = at.t0; t < live; t += kTurn) {
+        src += (size_t)kAhead * xs;
+        for (int t = 0; t < count; t += kTurn) {
 #pragma unroll
             for (int u = 0; u < kTurn; ++u) {
-                if (t + u < live) {
-                    raw_floats(ring[u % kAhead], win[u % W]);
-                    if (t + u + kAhead < live) ring[u % kAhead] = raw_load<T, V>(src + (size_t)kAhead * xs);
+                if (t + u < count) {
+                    ring_wait<kAhead - 1>();
+                    Raw<T, V> &slot = ring[u % kAhead][threadIdx.x];
+                    to_pairs(slot, win[u % W]);
+                    ring_copy<T, V>(&slot, src, t + u + kAhead < count);
+                    ring_commit();
                     src += xs;
-                    float y[V], s[V];
+                    uint64_t y[kP];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        float a = br[v];
+                    for (int v = 0; v < kP; ++v) {
+                        y[v] = br[v];
 #pragma unroll
-                        for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], win[(u + 1 + j) % W][v], a);
-                        y[v] = a;
+                        for (int j = 0; j < W; ++j) y[v] = fma2(wr[j][v], win[(u + 1 + j) % W][v], y[v]);
+                        if (kSilu) {
+                            float s0, s1;
+                            sigmoids(y[v], s0, s1);
+                            y[v] = mul2(y[v], pair(s0, s1));
+                        }
                     }
-                    if (kSilu) {
-                        sigmoids<V>(y, s);
-#pragma unroll
-                        for (int v = 0; v < V; ++v) y[v] *= s[v];
-                    }
-                    VecIo<T, V>::store(dst, y);
+                    store_pairs(dst, y);
                     dst += os;
                 }
             }
@@ -149,12 +159,12 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
     // the state after the sequence's last token; the thread that read these channels' state_in
     // writes it, so the two may be the same buffer
     if (state_out && at.lead) {
-        float r[W - 1][V];
+        Raw<T, V> r[W - 1];
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i) load_row<T, W, V>(x, xs, st, g.C, at.c0, len - (W - 1) + i, r[i]);
+        for (int i = 0; i < W - 1; ++i) r[i] = load_row<T, W, V>(x, xs, st, g.C, at.c0, len - (W - 1) + i);
 #pragma unroll
         for (int i = 0; i < W - 1; ++i)
-            VecIo<T, V>::store(state_out + ((size_t)at.b * (W - 1) + i) * g.C + at.c0, r[i]);
+            *reinterpret_cast<Raw<T, V> *>(state_out + ((size_t)at.b * (W - 1) + i) * g.C + at.c0) = r[i];
     }
 }
 
@@ -167,28 +177,32 @@ conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, co
     if (i >= units) return;
     const int per = C / V, c0 = (int)(i % per) * V;
     const size_t b = i / per;
-    float wr[V][W], br[V], win[W][V], y[V];
+    constexpr int kP = (V + 1) / 2;
+    Raw<T, V> row[W];
     T *st = state + b * (W - 1) * C + c0;
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) VecIo<T, V>::load(st + (size_t)j * C, win[j]);
-    VecIo<T, V>::load(x + b * xs + c0, win[W - 1]);
-    load_taps<T, W, V>(w, bias, c0, wr, br);
+    for (int j = 0; j < W - 1; ++j) row[j] = raw_load<T, V>(st + (size_t)j * C);
+    row[W - 1] = raw_load<T, V>(x + b * xs + c0);
+    uint64_t wr[W][kP], y[kP];
+    load_taps<T, W, V>(w, bias, c0, wr, y);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        float a = br[v];
+    for (int j = 0; j < W; ++j) {
+        uint64_t f[kP];
+        to_pairs(row[j], f);
 #pragma unroll
-        for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], win[j][v], a);
-        y[v] = a;
+        for (int v = 0; v < kP; ++v) y[v] = fma2(wr[j][v], f[v], y[v]);
     }
     if (kSilu) {
-        float s[V];
-        sigmoids<V>(y, s);
 #pragma unroll
-        for (int v = 0; v < V; ++v) y[v] *= s[v];
+        for (int v = 0; v < kP; ++v) {
+            float s0, s1;
+            sigmoids(y[v], s0, s1);
+            y[v] = mul2(y[v], pair(s0, s1));
+        }
     }
-    VecIo<T, V>::store(out + b * os + c0, y);
+    store_pairs(out + b * os + c0, y);
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) VecIo<T, V>::store(st + (size_t)j * C, win[j + 1]);
+    for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Raw<T, V> *>(st + (size_t)j * C) = row[j + 1];
 }
 
 // Gradients.  A strip computes g for its tokens and the W - 1 that follow (which its dx needs), sums
@@ -200,10 +214,16 @@ __global__ void __launch_bounds__(kThreads)
 conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ bias,
                      const T *__restrict__ dout, T *__restrict__ dx, size_t xs, size_t gs, size_t ds,
                      const int *__restrict__ lengths, float *__restrict__ partial) {
-    __shared__ float red[kStrips][W + 1][V][32];
+    union Scratch {
+        Raw<T, V> ring[2][kAheadBwd][kThreads];
+        float red[kStrips][W + 1][V][32];
+    };
+    __shared__ Scratch sm;
+    auto &red = sm.red;
     const Place at = place<V>(g);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float dw[W + 1][V] = {};  // row W: dbias
+    constexpr int kP = (V + 1) / 2;
+    uint64_t dw[W + 1][kP] = {};  // row W: dbias
     if (at.c0 < g.C) {
         const int len = length_of(lengths, at.b, g.n);
         x += (size_t)at.b * g.n * xs + at.c0;
@@ -212,75 +232,74 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
         const int end = min(at.t0 + g.L, g.n), live = min(end, len);
         if (at.t0 < live) {
             // rows t of x and g in xw[t % W], gw[t % W] (counted from the strip's start)
-            float wr[V][W], br[V], xw[W][V], gw[W][V];
+            uint64_t wr[W][kP], br[kP], xw[W][kP], gw[W][kP];
             const int last = min(live + W - 1, len);  // tokens from here on have g = 0
-            Raw<T, V> xr[kAhead], gr[kAhead];
             const T *xp = x + (size_t)at.t0 * xs, *gp = dout + (size_t)at.t0 * gs;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                xr[u] = at.t0 + u < last ? raw_load<T, V>(xp + (size_t)u * xs) : raw_zero<T, V>();
-                gr[u] = at.t0 + u < last ? raw_load<T, V>(gp + (size_t)u * gs) : raw_zero<T, V>();
+            for (int u = 0; u < kAheadBwd; ++u) {
+                ring_copy<T, V>(&sm.ring[0][u][threadIdx.x], xp, at.t0 + u < last);
+                ring_copy<T, V>(&sm.ring[1][u][threadIdx.x], gp, at.t0 + u < last);
+                ring_commit();
+                xp += xs;
+                gp += gs;
             }
             load_taps<T, W, V>(w, bias, at.c0, wr, br);
 #pragma unroll
             for (int i = 0; i < W; ++i) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) xw[i][v] = gw[i][v] = 0.f;
-                if (i > 0 && at.t0 - W + i >= 0) VecIo<T, V>::load(x + (ptrdiff_t)(at.t0 - W + i) * (ptrdiff_t)xs, xw[i]);
+                for (int v = 0; v < kP; ++v) xw[i][v] = gw[i][v] = pair(0.f, 0.f);
+                if (i > 0 && at.t0 - W + i >= 0) to_pairs(raw_load<T, V>(x + (size_t)(at.t0 - W + i) * xs), xw[i]);
             }
-            constexpr int kTurn = W == 3 ? 3 * kAhead : kAhead;
+            constexpr int kTurn = W == 3 ? 3 * kAheadBwd : kAheadBwd;
             T *to = dx + (size_t)at.t0 * ds;  // of token t + u - (W - 1), once its g and the next W - 1 are there
             for (int t = at.t0; t < live + W - 1; t += kTurn) {
 #pragma unroll
                 for (int u = 0; u < kTurn; ++u) {
                     const int tt = t + u;
                     if (tt < live + W - 1) {
-                        float(&xc)[V] = xw[u % W];
-                        float(&gc)[V] = gw[u % W];
-                        raw_floats(xr[u % kAhead], xc);
-                        raw_floats(gr[u % kAhead], gc);
-                        if (tt + kAhead < last) {
-                            xr[u % kAhead] = raw_load<T, V>(xp + (size_t)kAhead * xs);
-                            gr[u % kAhead] = raw_load<T, V>(gp + (size_t)kAhead * gs);
-                        } else {
-                            xr[u % kAhead] = gr[u % kAhead] = raw_zero<T, V>();
-                        }
+                        uint64_t(&gc)[kP] = gw[u % W];
+                        ring_wait<kAheadBwd - 1>();
+                        Raw<T, V> &xr = sm.ring[0][u % kAheadBwd][threadIdx.x], &gr = sm.ring[1][u % kAheadBwd][threadIdx.x];
+                        to_pairs(tt < last ? xr : raw_zero<T, V>(), xw[u % W]);
+                        to_pairs(tt < last ? gr : raw_zero<T, V>(), gc);
+                        ring_copy<T, V>(&xr, xp, tt + kAheadBwd < last);
+                        ring_copy<T, V>(&gr, gp, tt + kAheadBwd < last);
+                        ring_commit();
                         xp += xs;
                         gp += gs;
                         if (kSilu) {
-                            float a[V], s[V];
 #pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                a[v] = br[v];
+                            for (int v = 0; v < kP; ++v) {
+                                uint64_t a = br[v];
 #pragma unroll
-                                for (int j = 0; j < W; ++j) a[v] = fmaf(wr[v][j], xw[(u + 1 + j) % W][v], a[v]);
+                                for (int j = 0; j < W; ++j) a = fma2(wr[j][v], xw[(u + 1 + j) % W][v], a);
+                                float s0, s1;
+                                sigmoids(a, s0, s1);
+                                const uint64_t s = pair(s0, s1), one = pair(1.f, 1.f);
+                                gc[v] = mul2(mul2(gc[v], s), fma2(a, fma2(s, pair(-1.f, -1.f), one), one));
                             }
-                            sigmoids<V>(a, s);
-#pragma unroll
-                            for (int v = 0; v < V; ++v) gc[v] *= s[v] * fmaf(a[v], 1.f - s[v], 1.f);
                         }
-                        if (tt >= len) {  // (silu' of a row that was not read may be anything)
+                        if (tt >= last) {  // (silu' of a row that was not read may be anything)
 #pragma unroll
-                            for (int v = 0; v < V; ++v) gc[v] = 0.f;
+                            for (int v = 0; v < kP; ++v) gc[v] = pair(0.f, 0.f);
                         }
                         if (tt < live) {
 #pragma unroll
-                            for (int v = 0; v < V; ++v) {
+                            for (int v = 0; v < kP; ++v) {
 #pragma unroll
-                                for (int j = 0; j < W; ++j) dw[j][v] = fmaf(gc[v], xw[(u + 1 + j) % W][v], dw[j][v]);
-                                dw[W][v] += gc[v];
+                                for (int j = 0; j < W; ++j) dw[j][v] = fma2(gc[v], xw[(u + 1 + j) % W][v], dw[j][v]);
+                                dw[W][v] = add2(dw[W][v], gc[v]);
                             }
                         }
                         if (tt - (W - 1) >= at.t0) {
-                            float d[V];
+                            uint64_t d[kP];
 #pragma unroll
-                            for (int v = 0; v < V; ++v) {
-                                float a = 0.f;
+                            for (int v = 0; v < kP; ++v) {
+                                d[v] = mul2(wr[0][v], gw[u % W][v]);
 #pragma unroll
-                                for (int j = 0; j < W; ++j) a = fmaf(wr[v][j], gw[(u + W - j) % W][v], a);
-                                d[v] = a;
+                                for (int j = 1; j < W; ++j) d[v] = fma2(wr[j][v], gw[(u + W - j) % W][v], d[v]);
                             }
-                            VecIo<T, V>::store(to, d);
+                            store_pairs(to, d);
                             to += ds;
                         }
                     }
@@ -290,10 +309,16 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
         const float zero[V] = {};
         for (int t = max(at.t0, live); t < end; ++t) VecIo<T, V>::store(dx + (size_t)t * ds, zero);
     }
+    __syncthreads();  // every thread has done with its ring
 #pragma unroll
     for (int j = 0; j <= W; ++j)
 #pragma unroll
-        for (int v = 0; v < V; ++v) red[warp][j][v][lane] = dw[j][v];
+        for (int v = 0; v < kP; ++v) {
+            float d0, d1;
+            unpair(dw[j][v], d0, d1);
+            red[warp][j][2 * v][lane] = d0;
+            if (2 * v + 1 < V) red[warp][j][2 * v + 1][lane] = d1;
+        }
     __syncthreads();
     const int cb = blockIdx.x % g.cblocks;
     float *to = partial + (size_t)(blockIdx.x / g.cblocks) * (W + 1) * g.C;
@@ -334,12 +359,21 @@ conv_sum_kernel(const float *__restrict__ partial, int rows, int C, float *__res
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Strip length: 32 tokens where that still gives every SM eight blocks, else shorter (a strip
-// re-reads W - 1 rows, 9 % of a 32-token strip, and shorter strips give more threads).
+// Strip length: the one that ends first when kResident blocks an SM run at a time, each costing its
+// strip and about eight tokens more (the rows read twice, the taps, the first loads)
+constexpr int kResident = 2;
 Geom geometry(int B, int n, int C, int V) {
-    Geom g{B, n, C, 32, ceil_div(C, 32 * V), 1};
-    while (g.L > kAhead && (long long)B * g.cblocks * ceil_div(n, g.L * kStrips) < 152 * 8) g.L /= 2;
-    g.tblocks = n > 0 ? ceil_div(n, g.L * kStrips) : 1;
+    Geom g{B, n, C, kStrip, ceil_div(C, 32 * V), 1};
+    long long best = 0;
+    for (int L = kStrip; L <= 128; L += kStrip) {
+        const long long tb = n > 0 ? ceil_div(n, (long long)L * kStrips) : 1;
+        const long long waves = ((long long)B * g.cblocks * tb + 152 * kResident - 1) / (152 * kResident);
+        if (L == kStrip || waves * (L + 8) < best) {
+            best = waves * (L + 8);
+            g.L = L;
+            g.tblocks = (int)tb;
+        }
+    }
     return g;
 }
 
@@ -407,8 +441,7 @@ bool wide(const ConvBwd &p, size_t eb, int V) {
 
 }  // namespace
 
-// fewer token blocks than this for any V: the scalar variant has the most channel blocks, hence
-// the longest strips; the shortest strips (kAhead tokens) bound the number of partial rows
+// the larger of what the scalar and the wide variant write
 size_t conv_backward_partial_floats(int B, int n, int C, int width) {
     size_t rows = 0;
     for (int V : {1, 4}) {

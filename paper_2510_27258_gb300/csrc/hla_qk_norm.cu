@@ -9,10 +9,12 @@
 // sharing heads):
 //   dy_i = g_i c_i - g_p(i) s_i,  dw = sum dy u,  dx = r (dy w - u mean(dy w u)).
 //
-// A few operations a value: bound by memory traffic.  A row of d components belongs to d / V
-// neighbouring lanes (one 16- or 8-byte access each), which hold the token's cosines and sines and
-// the weights in registers and walk through the heads, so tables and weights are read once a token
-// and block, not once a head.  Statistics and products are fp32; each output is rounded once.
+// A few operations a value: bound by memory traffic, and close behind it by issue slots.  A row of d
+// components belongs to d / 8 neighbouring lanes.  A lane holds both members of its four pairs (two
+// runs of four components, half a rotation apart; eight consecutive ones if interleaved), so the
+// rotation needs no other lane, keeps its products of cosines, sines and weights in registers, and
+// walks through the heads of its token with the next heads' rows in flight.  Statistics and products
+// are fp32; each output is rounded once.
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -22,46 +24,30 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kAhead = 4, kAheadBwd = 2;  // heads whose rows a thread has in flight
+constexpr int kBlocksFwd = 4, kBlocksBwd = 2;  // blocks of an SM at a time
 
-// V elements at p: one access, or element by element where rows are not aligned to it
-template <typename T, int V, bool kVec>
-__device__ __forceinline__ void load_row(const T *p, float (&v)[V]) {
-    if (kVec) {
-        VecIo<T, V>::load(p, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = to_f32(p[i]);
-    }
-}
-
-template <typename T, int V, bool kVec>
-__device__ __forceinline__ Raw<T, V> load_raw(const T *p) {
-    if (kVec) return raw_load<T, V>(p);
-    Raw<T, V> r;
+// four elements at p: one access, or element by element where rows are not aligned to it
+template <typename T, bool kVec>
+__device__ __forceinline__ Raw<T, 4> load4(const T *p) {
+    if (kVec) return raw_load<T, 4>(p);
+    Raw<T, 4> r;
     T *e = reinterpret_cast<T *>(&r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = p[i];
+    for (int i = 0; i < 4; ++i) e[i] = p[i];
     return r;
 }
 
-// the row another lane holds
-template <typename R>
-__device__ __forceinline__ R raw_from(const R &r, int lane) {
-    R got;
-    const uint32_t *from = reinterpret_cast<const uint32_t *>(&r);
-    uint32_t *to = reinterpret_cast<uint32_t *>(&got);
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(R) / 4); ++i) to[i] = __shfl_sync(0xffffffffu, from[i], lane);
-    return got;
-}
-
-template <typename T, int V, bool kVec>
-__device__ __forceinline__ void store_row(T *p, const float (&v)[V]) {
+template <typename T, bool kVec>
+__device__ __forceinline__ void store4(T *p, uint64_t a, uint64_t b) {
     if (kVec) {
-        VecIo<T, V>::store(p, v);
+        const uint64_t f[2] = {a, b};
+        store_pairs(p, f);
     } else {
+        float v[4];
+        unpair(a, v[0], v[1]);
+        unpair(b, v[2], v[3]);
 #pragma unroll
-        for (int i = 0; i < V; ++i) from_f32(p + i, v[i]);
+        for (int i = 0; i < 4; ++i) from_f32(p + i, v[i]);
     }
 }
 
@@ -72,121 +58,165 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// this thread's cosines and signed sines: components i0 .. i0 + V - 1 at table row `pos`
-template <int V>
-__device__ __forceinline__ void load_turn(const QkNorm &p, int i0, long long pos, float (&c)[V], float (&s)[V]) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        c[v] = 1.f;
-        s[v] = 0.f;
+// a lane's eight components: runs of four from at[0] and at[1]
+struct Runs {
+    int at[2];
+};
+
+template <int D, bool kInter>
+__device__ __forceinline__ Runs runs_of(int sub, int rot) {
+    if (kInter) return {{8 * sub, 8 * sub + 4}};
+    // pairs i < rot / 2 turn with i + rot / 2; what is not rotated is paired alike
+    const int half = rot / 2, i = 4 * sub;
+    if (i < half) return {{i, i + half}};
+    return {{half + i, half + i + (D - rot) / 2}};
+}
+
+template <typename T, bool kVec>
+struct Row {
+    Raw<T, 4> r[2];
+    __device__ __forceinline__ void load(const T *p, const Runs &at) {
+        r[0] = load4<T, kVec>(p + at.at[0]);
+        r[1] = load4<T, kVec>(p + at.at[1]);
     }
-    if (i0 >= p.rot) return;
-    if (pos < 0 || pos >= p.table_rows) {  // no such row: the rotated part becomes NaN
-#pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = s[v] = __int_as_float(0x7fffffff);
-        return;
+    __device__ __forceinline__ void pairs(uint64_t (&v)[4]) const {
+        uint64_t f[2];
+        to_pairs(r[0], f);
+        v[0] = f[0]; v[1] = f[1];
+        to_pairs(r[1], f);
+        v[2] = f[0]; v[3] = f[1];
     }
-    const int half = p.rot / 2;
-    const float *ct = p.cos + pos * half, *st = p.sin + pos * half;
-    if (p.interleaved) {
+};
+
+// the other members of the pairs a lane holds
+template <bool kInter>
+__device__ __forceinline__ void mates(const uint64_t (&v)[4], uint64_t (&m)[4]) {
 #pragma unroll
-        for (int v = 0; v < V; v += 2) {
-            c[v] = c[v + 1] = ct[(i0 + v) / 2];
-            s[v + 1] = st[(i0 + v) / 2];
-            s[v] = -s[v + 1];
-        }
-    } else {
-        const bool first = i0 < half;
-        const int j = first ? i0 : i0 - half;
-#pragma unroll
-        for (int v = 0; v < V; v += 4) {
-            const float4 cu = *reinterpret_cast<const float4 *>(ct + j + v);
-            const float4 su = *reinterpret_cast<const float4 *>(st + j + v);
-            c[v] = cu.x; c[v + 1] = cu.y; c[v + 2] = cu.z; c[v + 3] = cu.w;
-            s[v] = first ? -su.x : su.x;
-            s[v + 1] = first ? -su.y : su.y;
-            s[v + 2] = first ? -su.z : su.z;
-            s[v + 3] = first ? -su.w : su.w;
+    for (int e = 0; e < 4; ++e) {
+        if (kInter) {
+            float a, b;
+            unpair(v[e], a, b);
+            m[e] = pair(b, a);
+        } else {
+            m[e] = v[e ^ 2];
         }
     }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void load_weight(const void *w, int i0, float (&r)[V]) {
+// this lane's cosines and signed sines at table row `pos`: minus the sine for a pair's first member
+template <bool kInter>
+__device__ __forceinline__ void load_turn(const QkNorm &p, const Runs &at, long long pos, float (&c)[8], float (&s)[8]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) r[v] = w ? to_f32(static_cast<const T *>(w)[i0 + v]) : 1.f;
+    for (int v = 0; v < 8; ++v) {
+        c[v] = 1.f;
+        s[v] = 0.f;
+    }
+    if (at.at[0] >= p.rot) return;
+    if (pos < 0 || pos >= p.table_rows) {  // no such row: the rotated part becomes NaN
+#pragma unroll
+        for (int v = 0; v < 8; ++v) c[v] = s[v] = __int_as_float(0x7fffffff);
+        return;
+    }
+    const size_t from = (size_t)pos * (p.rot / 2) + (kInter ? at.at[0] / 2 : at.at[0]);
+    const float4 cu = *reinterpret_cast<const float4 *>(p.cos + from);
+    const float4 su = *reinterpret_cast<const float4 *>(p.sin + from);
+    const float cv[4] = {cu.x, cu.y, cu.z, cu.w}, sv[4] = {su.x, su.y, su.z, su.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int first = kInter ? 2 * i : i, second = kInter ? 2 * i + 1 : i + 4;
+        c[first] = c[second] = cv[i];
+        s[first] = -sv[i];
+        s[second] = sv[i];
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void load_weight(const void *w, const Runs &at, float (&r)[8]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const T *p = static_cast<const T *>(w) + at.at[k];
+        float f[4] = {1.f, 1.f, 1.f, 1.f};
+        if (w && reinterpret_cast<uintptr_t>(w) % sizeof(Raw<T, 4>) == 0) {
+            VecIo<T, 4>::load(p, f);
+        } else if (w) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = to_f32(p[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[4 * k + i] = f[i];
+    }
 }
 
 struct Split {
     int hpb;  // input heads a block walks through (blockIdx.y picks them)
 };
 
-template <typename T, int D, int V, bool kVec>
-__global__ void __launch_bounds__(kThreads) qk_norm_forward_kernel(QkNorm p, Split sp) {
-    constexpr int kLanes = D / V, kRows = kThreads / kLanes;
-    const int sub = threadIdx.x % kLanes, i0 = sub * V;
-    const long long row = (long long)blockIdx.x * kRows + threadIdx.x / kLanes, rows = (long long)p.B * p.n;
+template <typename T, int D, bool kInter, bool kVec>
+__global__ void __launch_bounds__(kThreads, kBlocksFwd) qk_norm_forward_kernel(QkNorm p, Split sp) {
+    constexpr int kLanes = D / 8, kRows = kThreads / kLanes;
+    const Runs at = runs_of<D, kInter>(threadIdx.x % kLanes, p.rot);
+    const unsigned row = blockIdx.x * kRows + threadIdx.x / kLanes, rows = (unsigned)p.B * p.n;  // below 2^31
     // rows past the end repeat the last one without storing: every lane joins the shuffles
-    const long long r0 = row < rows ? row : rows - 1;
-    const int b = (int)(r0 / p.n), t = (int)(r0 % p.n);
-    float c[V], s[V];
-    load_turn<V>(p, i0, p.positions ? (long long)p.positions[r0] : (long long)p.pos0 + t, c, s);
-    const int half = p.rot / 2;
-    const bool turned = i0 < p.rot, paired = turned && !p.interleaved;
-    const int partner = paired ? (i0 < half ? half : -half) : 0;
-    const int mate_lane = (int)(threadIdx.x & 31) + partner / V;
+    const unsigned r0 = row < rows ? row : rows - 1;
+    const unsigned b = r0 / p.n, t = r0 - b * p.n;
     const int h_lo = blockIdx.y * sp.hpb, h_hi = min(h_lo + sp.hpb, p.H + p.Hk);
+    float c[8], s[8];
+    load_turn<kInter>(p, at, p.positions ? (long long)p.positions[r0] : (long long)p.pos0 + t, c, s);
 
     auto walk = [&](const T *x, T *out, const void *weight, int lo, int hi, int per) {
         if (lo >= hi) return;
+        x += (size_t)lo * D;
+        Row<T, kVec> ring[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ring[u].load(x + (lo + u < hi ? u : 0) * D, at);
         // the rotation with the weights in it: out_i = r (v_i wc_i + v_p(i) ws_i)
-        float wc[V], ws[V];
-        load_weight<T, V>(weight, i0, wc);
-        load_weight<T, V>(weight, i0 + partner, ws);
-        if (turned && p.interleaved) {
+        uint64_t wc[4], ws[4];
+        {
+            float w[8];
+            load_weight<T>(weight, at, w);
 #pragma unroll
-            for (int e = 0; e < V; ++e) ws[e] = wc[e ^ 1] * s[e];
-#pragma unroll
-            for (int e = 0; e < V; ++e) wc[e] *= c[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                wc[e] *= c[e];
-                ws[e] *= s[e];
+            for (int e = 0; e < 8; e += 2) {
+                const int m0 = kInter ? e + 1 : e ^ 4, m1 = kInter ? e : (e + 1) ^ 4;
+                wc[e / 2] = pair(w[e] * c[e], w[e + 1] * c[e + 1]);
+                ws[e / 2] = pair(w[m0] * s[e], w[m1] * s[e + 1]);
             }
         }
-        T *to = out + (((size_t)b * p.H + (size_t)lo * per) * p.n + t) * D + i0;
+        const bool turned = at.at[0] < p.rot;
         const size_t step = (size_t)p.n * D;
-        Raw<T, V> ring[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            ring[u] = lo + u < hi ? load_raw<T, V, kVec>(x + (size_t)(lo + u) * D + i0) : raw_zero<T, V>();
-        for (int h = lo; h < hi; h += kAhead) {
+        T *to = out + (((size_t)b * p.H + (size_t)lo * per) * p.n + t) * D;
+        int left = hi - lo;
+        while (left > 0) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (h + u >= hi) break;
-                const Raw<T, V> raw = ring[u];
-                if (h + u + kAhead < hi) ring[u] = load_raw<T, V, kVec>(x + (size_t)(h + u + kAhead) * D + i0);
-                float v[V], m[V];
-                raw_floats(raw, v);
-                if (p.interleaved) {
+                if (left <= 0) break;
+                uint64_t v[4], m[4];
+                ring[u].pairs(v);
+                if (left > kAhead) ring[u].load(x + (u + kAhead) * D, at);
+                mates<kInter>(v, m);
+                uint64_t sum = mul2(v[0], v[0]);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) m[e] = v[e ^ 1];
-                } else {
-                    raw_floats(raw_from(raw, mate_lane), m);
+                for (int e = 1; e < 4; ++e) sum = fma2(v[e], v[e], sum);
+                float s0, s1;
+                unpair(sum, s0, s1);
+                const float r = rsqrtf(row_sum<kLanes>(s0 + s1) * (1.f / D) + p.eps);
+                const uint64_t r2 = pair(r, r);
+                uint64_t y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = mul2(v[e], wc[e]);
+                    if (turned) y[e] = fma2(m[e], ws[e], y[e]);
+                    y[e] = mul2(y[e], r2);
                 }
-                float ss = 0.f;
-#pragma unroll
-                for (int e = 0; e < V; ++e) ss = fmaf(v[e], v[e], ss);
-                const float r = rsqrtf(row_sum<kLanes>(ss) * (1.f / D) + p.eps);
-                float y[V];
-#pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = r * fmaf(v[e], wc[e], turned ? m[e] * ws[e] : 0.f);
                 for (int k = 0; k < per; ++k) {
-                    if (row < rows) VecIo<T, V>::store(to, y);
+                    if (row < rows) {
+                        store4<T, true>(to + at.at[0], y[0], y[1]);
+                        store4<T, true>(to + at.at[1], y[2], y[3]);
+                    }
                     to += step;
                 }
+                --left;
             }
+            x += kAhead * D;
         }
     };
     walk(static_cast<const T *>(p.q) + (size_t)r0 * p.q_stride, static_cast<T *>(p.q_out), p.wq, h_lo,
@@ -197,80 +227,106 @@ __global__ void __launch_bounds__(kThreads) qk_norm_forward_kernel(QkNorm p, Spl
 
 // Gradients.  Weight gradients are summed over a thread's heads in registers, over the block's
 // rows in shared memory, and over blocks by qk_norm_sum_kernel in a fixed order.
-template <typename T, int D, int V, bool kVec>
-__global__ void __launch_bounds__(kThreads) qk_norm_backward_kernel(QkNormBwd p, Split sp) {
-    constexpr int kLanes = D / V, kRows = kThreads / kLanes;
+template <typename T, int D, bool kInter, bool kVec>
+__global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(QkNormBwd p, Split sp) {
+    constexpr int kLanes = D / 8, kRows = kThreads / kLanes;
     __shared__ float red[kRows][D];
     const QkNorm &f = p.f;
-    const int sub = threadIdx.x % kLanes, i0 = sub * V;
-    const long long row = (long long)blockIdx.x * kRows + threadIdx.x / kLanes, rows = (long long)f.B * f.n;
-    const long long r0 = row < rows ? row : rows - 1;
+    const Runs at = runs_of<D, kInter>(threadIdx.x % kLanes, f.rot);
+    const unsigned row = blockIdx.x * kRows + threadIdx.x / kLanes, rows = (unsigned)f.B * f.n;  // below 2^31
+    const unsigned r0 = row < rows ? row : rows - 1;
     const bool real = row < rows;
-    const int b = (int)(r0 / f.n), t = (int)(r0 % f.n);
-    float c[V], s[V];
-    load_turn<V>(f, i0, f.positions ? (long long)f.positions[r0] : (long long)f.pos0 + t, c, s);
-    const int half = f.rot / 2;
-    const bool turned = i0 < f.rot, paired = turned && !f.interleaved;
-    const int mate_lane = (threadIdx.x & 31) + (paired ? (i0 < half ? half : -half) / V : 0);
+    const unsigned b = r0 / f.n, t = r0 - b * f.n;
     const int h_lo = blockIdx.y * sp.hpb, h_hi = min(h_lo + sp.hpb, f.H + f.Hk);
+    uint64_t c2[4], s2[4];  // cosines, and the negated signed sines
+    {
+        float c[8], s[8];
+        load_turn<kInter>(f, at, f.positions ? (long long)f.positions[r0] : (long long)f.pos0 + t, c, s);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            c2[e] = pair(c[2 * e], c[2 * e + 1]);
+            s2[e] = pair(-s[2 * e], -s[2 * e + 1]);
+        }
+    }
+    const bool turned = at.at[0] < f.rot;
 
-    auto walk = [&](const T *x, const T *dout, T *dx, const void *weight, int lo, int hi, int per, float (&dw)[V]) {
-        float w[V];
-        load_weight<T, V>(weight, i0, w);
-        const size_t step = (size_t)f.n * D;
-        const T *src = dout + (((size_t)b * f.H + (size_t)lo * per) * f.n + t) * D + i0;
-        Raw<T, V> xr[kAheadBwd], gr[kAheadBwd];
+    auto walk = [&](const T *x, const T *dout, T *dx, const void *weight, int lo, int hi, int per, uint64_t (&dw)[4]) {
+        if (lo >= hi) return;
+        uint64_t w2[4];
+        {
+            float w[8];
+            load_weight<T>(weight, at, w);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w2[e] = pair(w[2 * e], w[2 * e + 1]);
+        }
+        const size_t step = (size_t)f.n * D, jump = step * per;
+        x += (size_t)lo * D;
+        dx += (size_t)lo * D;
+        const T *src = dout + (((size_t)b * f.H + (size_t)lo * per) * f.n + t) * D;
+        Row<T, kVec> xr[kAheadBwd];
+        Row<T, true> gr[kAheadBwd];
 #pragma unroll
         for (int u = 0; u < kAheadBwd; ++u) {
-            const bool on = lo + u < hi;
-            xr[u] = on ? load_raw<T, V, kVec>(x + (size_t)(lo + u) * D + i0) : raw_zero<T, V>();
-            gr[u] = on ? raw_load<T, V>(src + (size_t)u * per * step) : raw_zero<T, V>();
+            const int k = lo + u < hi ? u : 0;
+            xr[u].load(x + k * D, at);
+            gr[u].load(src + k * jump, at);
         }
-        for (int h0 = lo; h0 < hi; h0 += kAheadBwd) {
+        int left = hi - lo;
+        while (left > 0) {
 #pragma unroll
             for (int u = 0; u < kAheadBwd; ++u) {
-                const int h = h0 + u;
-                if (h >= hi) break;
-                float v[V], g[V];
-                raw_floats(xr[u], v);
-                raw_floats(gr[u], g);
-                for (int m = 1; m < per; ++m) {
-                    float more[V];
-                    VecIo<T, V>::load(src + (size_t)m * step, more);
+                if (left <= 0) break;
+                uint64_t v[4], g[4], m[4];
+                xr[u].pairs(v);
+                gr[u].pairs(g);
+                for (int k = 1; k < per; ++k) {
+                    Row<T, true> r;
+                    r.load(src + k * step, at);
+                    uint64_t more[4];
+                    r.pairs(more);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) g[e] += more[e];
+                    for (int e = 0; e < 4; ++e) g[e] = add2(g[e], more[e]);
                 }
-                if (h + kAheadBwd < hi) {
-                    xr[u] = load_raw<T, V, kVec>(x + (size_t)(h + kAheadBwd) * D + i0);
-                    gr[u] = raw_load<T, V>(src + (size_t)kAheadBwd * per * step);
+                if (left > kAheadBwd) {
+                    xr[u].load(x + (size_t)kAheadBwd * D, at);
+                    gr[u].load(src + kAheadBwd * jump, at);
                 }
-                src += (size_t)per * step;
-                float dy[V], ss = 0.f, dot = 0.f;
-                float gp[V];
+                mates<kInter>(g, m);
+                uint64_t ss2 = pair(0.f, 0.f), dot2 = ss2;
 #pragma unroll
-                for (int e = 0; e < V; ++e) gp[e] = f.interleaved ? g[e ^ 1] : __shfl_sync(0xffffffffu, g[e], mate_lane);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    dy[e] = fmaf(g[e], c[e], turned ? -gp[e] * s[e] : 0.f);
-                    ss = fmaf(v[e], v[e], ss);
-                    dot = fmaf(dy[e] * w[e], v[e], dot);
+                for (int e = 0; e < 4; ++e) {
+                    uint64_t dy = mul2(g[e], c2[e]);
+                    if (turned) dy = fma2(m[e], s2[e], dy);
+                    ss2 = fma2(v[e], v[e], ss2);
+                    dot2 = fma2(mul2(dy, w2[e]), v[e], dot2);
+                    g[e] = dy;
                 }
-                ss = row_sum<kLanes>(ss);
-                dot = row_sum<kLanes>(dot);
+                float ss, dot, more;
+                unpair(ss2, ss, more);
+                ss = row_sum<kLanes>(ss + more);
+                unpair(dot2, dot, more);
+                dot = row_sum<kLanes>(dot + more);
                 const float r = rsqrtf(ss * (1.f / D) + f.eps);
-                const float m = dot * r * (1.f / D);
-                float d[V];
+                const float q = -dot * r * r * (1.f / D);  // dx = r (dy w + v q)
+                const uint64_t r2 = pair(r, r), q2 = pair(q, q);
+                uint64_t d[4];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float unit = v[e] * r;
-                    d[e] = r * fmaf(dy[e], w[e], -unit * m);
-                    if (real) dw[e] = fmaf(dy[e], unit, dw[e]);
+                for (int e = 0; e < 4; ++e) {
+                    d[e] = mul2(r2, fma2(v[e], q2, mul2(g[e], w2[e])));
+                    if (real) dw[e] = fma2(g[e], mul2(v[e], r2), dw[e]);
                 }
-                if (real) store_row<T, V, kVec>(dx + (size_t)h * D + i0, d);
+                if (real) {
+                    store4<T, kVec>(dx + at.at[0], d[0], d[1]);
+                    store4<T, kVec>(dx + at.at[1], d[2], d[3]);
+                }
+                x += D;
+                dx += D;
+                src += jump;
+                --left;
             }
         }
     };
-    float dwq[V] = {}, dwk[V] = {};
+    uint64_t dwq[4] = {}, dwk[4] = {};
     walk(static_cast<const T *>(f.q) + (size_t)r0 * f.q_stride, static_cast<const T *>(p.dq_out),
          static_cast<T *>(p.dq) + (size_t)r0 * p.dq_stride, f.wq, h_lo, min(h_hi, f.H), 1, dwq);
     walk(static_cast<const T *>(f.k) + (size_t)r0 * f.k_stride, static_cast<const T *>(p.dk_out),
@@ -279,8 +335,12 @@ __global__ void __launch_bounds__(kThreads) qk_norm_backward_kernel(QkNormBwd p,
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
+        float *mine = red[threadIdx.x / kLanes];
 #pragma unroll
-        for (int e = 0; e < V; ++e) red[threadIdx.x / kLanes][i0 + e] = which ? dwk[e] : dwq[e];
+        for (int e = 0; e < 4; ++e) {
+            const int i = at.at[e / 2] + 2 * (e % 2);
+            unpair(which ? dwk[e] : dwq[e], mine[i], mine[i + 1]);
+        }
         __syncthreads();
         for (int i = threadIdx.x; i < D; i += kThreads) {
             float sum = 0.f;
@@ -310,16 +370,21 @@ struct Plan {
     Split sp;
 };
 
-// All heads in one block where the rows alone give every SM eight blocks (tables and weights are
-// then read once a token), else as many head groups as that takes
-Plan plan(long long rows, int heads, int per_block) {
-    Plan g;
-    g.gx = (unsigned)((rows + per_block - 1) / per_block);
-    long long groups = (152 * 8 + (long long)g.gx - 1) / g.gx;
-    if (groups > heads) groups = heads;
-    g.sp.hpb = (int)((heads + groups - 1) / groups);
-    g.gy = (unsigned)((heads + g.sp.hpb - 1) / g.sp.hpb);
-    return g;
+// The split of the heads over blocks that ends first when `resident` blocks an SM run at a time, each
+// costing its heads and about four heads' time more (tables, weights, first loads)
+Plan plan(long long rows, int heads, int per_block, int resident) {
+    Plan best{};
+    long long least = 0;
+    const unsigned gx = (unsigned)((rows + per_block - 1) / per_block);
+    for (int groups = 1; groups <= heads && groups <= 64; ++groups) {
+        const int hpb = (heads + groups - 1) / groups, gy = (heads + hpb - 1) / hpb;
+        const long long slots = 152LL * resident, waves = ((long long)gx * gy + slots - 1) / slots;
+        if (groups == 1 || waves * (hpb + 4) < least) {
+            least = waves * (hpb + 4);
+            best = {gx, (unsigned)gy, {hpb}};
+        }
+    }
+    return best;
 }
 
 template <typename F>
@@ -332,20 +397,20 @@ cudaError_t by_size(int d, F f) {
     }
 }
 
-template <typename T, int V, bool kVec>
+template <typename T, bool kInter, bool kVec>
 cudaError_t forward_as(const QkNorm &p, cudaStream_t s) {
     return by_size(p.d, [&](auto D) -> cudaError_t {
-        const Plan g = plan((long long)p.B * p.n, p.H + p.Hk, kThreads / (D() / V));
-        qk_norm_forward_kernel<T, D(), V, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
+        const Plan g = plan((long long)p.B * p.n, p.H + p.Hk, kThreads / (D() / 8), kBlocksFwd);
+        qk_norm_forward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
         return cudaGetLastError();
     });
 }
 
-template <typename T, int V, bool kVec>
+template <typename T, bool kInter, bool kVec>
 cudaError_t backward_as(const QkNormBwd &p, cudaStream_t s) {
     return by_size(p.f.d, [&](auto D) -> cudaError_t {
-        const Plan g = plan((long long)p.f.B * p.f.n, p.f.H + p.f.Hk, kThreads / (D() / V));
-        qk_norm_backward_kernel<T, D(), V, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
+        const Plan g = plan((long long)p.f.B * p.f.n, p.f.H + p.f.Hk, kThreads / (D() / 8), kBlocksBwd);
+        qk_norm_backward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
         cudaError_t e = cudaGetLastError();
         if (e) return e;
         qk_norm_sum_kernel<<<(2 * p.f.d * 32 + kThreads - 1) / kThreads, kThreads, 0, s>>>(
@@ -354,41 +419,32 @@ cudaError_t backward_as(const QkNormBwd &p, cudaStream_t s) {
     });
 }
 
-// components a lane holds: 8 bf16 or 4 fp32 (16 bytes); 4 bf16 where the pairs of a half-split
-// rotation would not lie whole in other lanes
-int lane_width(const QkNorm &p) { return p.dt == HLA_BF16 && (p.interleaved || p.rot % 16 == 0) ? 8 : 4; }
-
 }  // namespace
 
 size_t qk_norm_partial_floats(int B, int n, int H, int Hk, int d) {
-    size_t most = 0;
-    for (int V : {4, 8}) {
-        const Plan g = plan((long long)B * n, H + Hk, kThreads / (d / V));
-        const size_t f = (size_t)g.gx * g.gy * 2 * d;
-        if (f > most) most = f;
-    }
-    return most;
+    const Plan g = plan((long long)B * n, H + Hk, kThreads / (d / 8), kBlocksBwd);
+    return (size_t)g.gx * g.gy * 2 * d;
 }
 
+#define HLA_QK_DISPATCH(FN, VEC, INTER, DT)                                                              \
+    if ((DT) == HLA_BF16) {                                                                              \
+        if (INTER) return (VEC) ? FN<__nv_bfloat16, true, true>(p, s) : FN<__nv_bfloat16, true, false>(p, s); \
+        return (VEC) ? FN<__nv_bfloat16, false, true>(p, s) : FN<__nv_bfloat16, false, false>(p, s);     \
+    }                                                                                                    \
+    if (INTER) return (VEC) ? FN<float, true, true>(p, s) : FN<float, true, false>(p, s);                \
+    return (VEC) ? FN<float, false, true>(p, s) : FN<float, false, false>(p, s);
+
 cudaError_t qk_norm_forward_launch(const QkNorm &p, cudaStream_t s) {
-    const int V = lane_width(p);
-    const size_t eb = p.dt == HLA_BF16 ? 2 : 4, by = V * eb;
+    const size_t eb = p.dt == HLA_BF16 ? 2 : 4, by = 4 * eb;
     const bool vec = rows_aligned(p.q, p.q_stride, eb, by) && rows_aligned(p.k, p.k_stride, eb, by);
-    if (p.dt == HLA_F32) return vec ? forward_as<float, 4, true>(p, s) : forward_as<float, 4, false>(p, s);
-    if (V == 8)
-        return vec ? forward_as<__nv_bfloat16, 8, true>(p, s) : forward_as<__nv_bfloat16, 8, false>(p, s);
-    return vec ? forward_as<__nv_bfloat16, 4, true>(p, s) : forward_as<__nv_bfloat16, 4, false>(p, s);
+    HLA_QK_DISPATCH(forward_as, vec, p.interleaved, p.dt)
 }
 
 cudaError_t qk_norm_backward_launch(const QkNormBwd &p, cudaStream_t s) {
-    const int V = lane_width(p.f);
-    const size_t eb = p.f.dt == HLA_BF16 ? 2 : 4, by = V * eb;
+    const size_t eb = p.f.dt == HLA_BF16 ? 2 : 4, by = 4 * eb;
     const bool vec = rows_aligned(p.f.q, p.f.q_stride, eb, by) && rows_aligned(p.f.k, p.f.k_stride, eb, by) &&
                      rows_aligned(p.dq, p.dq_stride, eb, by) && rows_aligned(p.dk, p.dk_stride, eb, by);
-    if (p.f.dt == HLA_F32) return vec ? backward_as<float, 4, true>(p, s) : backward_as<float, 4, false>(p, s);
-    if (V == 8)
-        return vec ? backward_as<__nv_bfloat16, 8, true>(p, s) : backward_as<__nv_bfloat16, 8, false>(p, s);
-    return vec ? backward_as<__nv_bfloat16, 4, true>(p, s) : backward_as<__nv_bfloat16, 4, false>(p, s);
+    HLA_QK_DISPATCH(backward_as, vec, p.f.interleaved, p.f.dt)
 }
 
 }  // namespace hla

@@ -132,33 +132,6 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
-// two fp32 values in a 64-bit register, and the paired operations on them
-__device__ __forceinline__ uint64_t pair(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
-__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
-    float lo, hi;
-    unpair(v, lo, hi);
-    return pack_bf16x2(lo, hi);
-}
-__device__ __forceinline__ uint64_t of_bf16(uint32_t u) { return pair(bf16_lo(u), bf16_hi(u)); }
-
 // max(v, 0) + log(1 + e), e = exp(-|v|), by log(1 + e) = 2 atanh(s) with s = e / (2 + e) <= 1/3 and the
 // series of atanh up to s^13 (what follows is below 2^-23 of the sum)
 __device__ __forceinline__ float softplus(float v) {

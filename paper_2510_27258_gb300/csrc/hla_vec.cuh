@@ -88,17 +88,94 @@ __device__ __forceinline__ Raw<T, V> raw_zero() {
     memset(&r, 0, sizeof(r));
     return r;
 }
-__device__ __forceinline__ void raw_floats(const Raw<float, 1> &r, float (&f)[1]) { f[0] = r.v[0]; }
-__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 1> &r, float (&f)[1]) { f[0] = to_f32(r.v[0]); }
-__device__ __forceinline__ void raw_floats(const Raw<float, 4> &r, float (&f)[4]) {
-    f[0] = r.v.x; f[1] = r.v.y; f[2] = r.v.z; f[3] = r.v.w;
+
+// A ring of rows in flight per thread: slot s of thread t is the Raw at s * blockDim.x + t of a
+// shared array, written by the thread's own asynchronous copies (one group a row) and read by it
+// alone, so no barrier is needed.  One-element rows are copied through a register.
+template <typename T, int V>
+__device__ __forceinline__ void ring_copy(Raw<T, V> *slot, const T *src, bool on) {
+    if constexpr (sizeof(Raw<T, V>) >= 4) {
+        if (on)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(
+                             static_cast<uint32_t>(__cvta_generic_to_shared(slot))),
+                         "l"(src), "n"((int)sizeof(Raw<T, V>))
+                         : "memory");
+    } else {
+        if (on) *slot = raw_load<T, V>(src);
+    }
 }
-__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 4> &r, float (&f)[4]) {
-    f[0] = bf16_lo(r.v.x); f[1] = bf16_hi(r.v.x); f[2] = bf16_lo(r.v.y); f[3] = bf16_hi(r.v.y);
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void ring_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void raw_floats(const Raw<__nv_bfloat16, 8> &r, float (&f)[8]) {
-    f[0] = bf16_lo(r.v.x); f[1] = bf16_hi(r.v.x); f[2] = bf16_lo(r.v.y); f[3] = bf16_hi(r.v.y);
-    f[4] = bf16_lo(r.v.z); f[5] = bf16_hi(r.v.z); f[6] = bf16_lo(r.v.w); f[7] = bf16_hi(r.v.w);
+
+// two fp32 values in a 64-bit register, and the paired operations on them (one issue slot for two)
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(uint32_t lo, uint32_t hi) { return pair(__uint_as_float(lo), __uint_as_float(hi)); }
+__device__ __forceinline__ void unpair(uint64_t v, float &lo, float &hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
+    float lo, hi;
+    unpair(v, lo, hi);
+    return bf16_pair(lo, hi);
+}
+__device__ __forceinline__ uint64_t of_bf16(uint32_t u) { return pair(bf16_lo(u), bf16_hi(u)); }
+
+// a row's V elements as (V + 1) / 2 pairs (V = 1: the second half of the pair is zero), and back
+__device__ __forceinline__ void to_pairs(const Raw<float, 1> &r, uint64_t (&f)[1]) { f[0] = pair(r.v[0], 0.f); }
+__device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 1> &r, uint64_t (&f)[1]) { f[0] = pair(to_f32(r.v[0]), 0.f); }
+__device__ __forceinline__ void to_pairs(const Raw<float, 4> &r, uint64_t (&f)[2]) {
+    f[0] = pair(r.v.x, r.v.y);
+    f[1] = pair(r.v.z, r.v.w);
+}
+__device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 4> &r, uint64_t (&f)[2]) {
+    f[0] = of_bf16(r.v.x);
+    f[1] = of_bf16(r.v.y);
+}
+__device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 8> &r, uint64_t (&f)[4]) {
+    f[0] = of_bf16(r.v.x);
+    f[1] = of_bf16(r.v.y);
+    f[2] = of_bf16(r.v.z);
+    f[3] = of_bf16(r.v.w);
+}
+__device__ __forceinline__ void store_pairs(float *p, const uint64_t (&f)[1]) {
+    float none;
+    unpair(f[0], *p, none);
+}
+__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[1]) {
+    float v, none;
+    unpair(f[0], v, none);
+    from_f32(p, v);
+}
+__device__ __forceinline__ void store_pairs(float *p, const uint64_t (&f)[2]) {
+    *reinterpret_cast<ulonglong2 *>(p) = make_ulonglong2(f[0], f[1]);
+}
+__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[2]) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_of(f[0]), bf16_of(f[1]));
+}
+__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[4]) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_of(f[0]), bf16_of(f[1]), bf16_of(f[2]), bf16_of(f[3]));
 }
 
 // whether a base pointer and a row stride (elements of `eb` bytes) keep every row aligned to `bytes`
