@@ -361,8 +361,8 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // Strip length: the one that ends first when kResident blocks an SM run at a time, each costing its
 // strip and about eight tokens more (the rows read twice, the taps, the first loads)
-constexpr int kResident = 2;
 Geom geometry(int B, int n, int C, int V) {
+    const int kResident = V == 1 ? 4 : 2;  // by their registers
     Geom g{B, n, C, kStrip, ceil_div(C, 32 * V), 1};
     long long best = 0;
     for (int L = kStrip; L <= 128; L += kStrip) {

@@ -30,7 +30,7 @@ hla_status check_flag(int v, const char *name) {
 
 hla_status check_rows(int B, int n) {
     if (B < 0 || n < 0) return fail(HLA_ERR_INVALID_ARGUMENT, "negative size B=%d n=%d", B, n);
-    return (long long)B * n <= kMaxRows ? HLA_OK : fail(HLA_ERR_UNSUPPORTED, "problem too large");
+    return n <= (1 << 30) && (long long)B * n <= kMaxRows ? HLA_OK : fail(HLA_ERR_UNSUPPORTED, "problem too large");
 }
 
 // a strided token tensor: pointer (where there are rows), element alignment, row stride

@@ -135,19 +135,19 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
             }
         }
     }
-    if (kStateOnly) {
+    if constexpr (kStateOnly) {
         float *to = seg_state + ((size_t)head * segments + seg) * N * p.P;
 #pragma unroll
         for (int i = 0; i < NS; ++i) to[(size_t)state_index<NS>(lane8, i) * p.P + pc] = st[i];
         if (tid == 0 && slice == 0) seg_decay[(size_t)head * segments + seg] = la_sum;
-        return;
-    }
-    for (int i = tid; i < (t_hi - max(t_lo, live)) * kCols; i += kScanThreads)
-        from_f32(y + (size_t)(max(t_lo, live) + i / kCols) * p.y_stride + i % kCols, 0.f);
-    if (p.state_out && seg == segments - 1) {
-        float *to = p.state_out + (size_t)head * N * p.P;
+    } else {
+        for (int i = tid; i < (t_hi - max(t_lo, live)) * kCols; i += kScanThreads)
+            from_f32(y + (size_t)(max(t_lo, live) + i / kCols) * p.y_stride + i % kCols, 0.f);
+        if (p.state_out && seg == segments - 1) {
+            float *to = p.state_out + (size_t)head * N * p.P;
 #pragma unroll
-        for (int i = 0; i < NS; ++i) to[(size_t)state_index<NS>(lane8, i) * p.P + pc] = st[i];
+            for (int i = 0; i < NS; ++i) to[(size_t)state_index<NS>(lane8, i) * p.P + pc] = st[i];
+        }
     }
 }
 
@@ -160,10 +160,20 @@ chain_kernel(const float *state_in, float *seg_state, const float *seg_decay, lo
     float h = state_in ? state_in[head * NP + e] : 0.f;
     float *s = seg_state + head * segments * NP + e;
     const float *la = seg_decay + head * segments;
-    for (int k = 0; k < segments; ++k) {
-        const float own = k + 1 < segments ? s[(size_t)k * NP] : 0.f;
-        s[(size_t)k * NP] = h;
-        if (k + 1 < segments) h = fmaf(h, expf(la[k]), own);
+    constexpr int kBatch = 8;  // segments loaded at once
+    for (int k0 = 0; k0 < segments; k0 += kBatch) {
+        float own[kBatch], decay[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {  // (the last segment has no state of its own)
+            const bool on = k0 + u + 1 < segments;
+            own[u] = on ? s[(size_t)(k0 + u) * NP] : 0.f;
+            decay[u] = on ? la[k0 + u] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (k0 + u < segments) s[(size_t)(k0 + u) * NP] = h;
+            h = fmaf(h, expf(decay[u]), own[u]);
+        }
     }
 }
 
@@ -227,12 +237,12 @@ __global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(Ssm p) {
 }
 
 // Segments of a prompt: none where the heads alone give every SM two blocks; else as many as that
-// takes, of 128 tokens or more (a segment costs a second pass over its tokens)
+// takes, of 32 tokens or more (a segment costs a second pass over its tokens)
 int segments_of(const Ssm &p) {
     const long long blocks = (long long)p.B * p.H * (p.P / kCols);
     if (blocks >= 152 * 2 || blocks == 0) return 1;
     long long s = (152 * 4 + blocks - 1) / blocks;
-    const long long most = p.n / 128;
+    const long long most = p.n / 32;
     if (s > most) s = most;
     return s < 1 ? 1 : (int)s;
 }

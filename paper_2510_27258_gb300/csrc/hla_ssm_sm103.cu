@@ -80,7 +80,7 @@ struct Map {
     static constexpr uint32_t lo(int buf) { return kN == 64 ? kEH + kTileBytes : C(buf); }
     static constexpr uint32_t kBytes = kEnd + sizeof(Misc);
 };
-static_assert(Map<128>::kBytes <= 232448, "shared memory");
+static_assert(Map<128>::kBytes <= 232448 && Map<64>::kBytes <= 232448, "shared memory");
 
 constexpr uint32_t kTS = 0, kTH = 128, kTY1 = 256, kTY2 = 384;  // TMEM columns
 
@@ -109,22 +109,7 @@ __device__ __forceinline__ void set_error(WsHeader *err, unsigned where, unsigne
     }
 }
 
-__device__ __forceinline__ bool bar_wait(Misc *ms, int b, uint32_t parity, const Params &p) {
-    if (mbar_try_wait(&ms->bar[b], parity)) return true;
-    if (*(volatile int *)&ms->abort_flag) return false;
-    if (mbar_wait(&ms->bar[b], parity, kBarWaitNs)) return true;
-    set_error(p.err, 400 + b, parity);
-    *(volatile int *)&ms->abort_flag = 1;
-    return false;
-}
-
 __device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory"); }
-
-__device__ __forceinline__ void epi_arrive(Misc *ms, int b) {
-    tc_fence_before();
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) mbar_arrive(&ms->bar[b]);
-}
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -171,7 +156,263 @@ __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_
                      (static_cast<uint64_t>(kDescHi) << 32) | (b_lo + kk * 128u), id, kk > 0 ? 1u : 0u);
 }
 
-template <int kN, bool kStateOnly>
+// a CTA's 128 columns and its tiles
+struct Unit {
+    int b, g, h0, seg, t_lo, t_hi, live, tiles;  // sequence, group, first head; tokens, those that count
+    bool one, both;  // one head of 128 columns, else two heads of up to 64; the second one is in the group
+};
+
+__device__ __forceinline__ Unit unit_of(const Params &p) {
+    Unit u;
+    const int unit = blockIdx.x % p.units, group_heads = p.H / p.G, k = unit % p.per_group;
+    u.seg = blockIdx.x / p.units;
+    u.one = p.P == 128;
+    u.g = unit / p.per_group % p.G;
+    u.b = unit / p.per_group / p.G;
+    u.h0 = u.g * group_heads + (u.one ? k : 2 * k);
+    u.both = u.one || 2 * k + 1 < group_heads;
+    u.t_lo = u.seg * p.seg_tiles * kTile;
+    u.t_hi = min(u.t_lo + p.seg_tiles * kTile, p.n);
+    u.live = min(u.t_hi, p.lengths ? min(max(p.lengths[u.b], 0), p.n) : p.n);
+    u.tiles = u.live > u.t_lo ? (u.live - u.t_lo + kTile - 1) / kTile : 0;
+    return u;
+}
+
+// inclusive sums of a warp's values up to and down from each lane's
+__device__ __forceinline__ void sums_of(float &up, float &down) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
+        if (lane >= o) up += x;
+        if (lane + o < 32) down += z;
+    }
+}
+
+// 32 elements of a row of w X as the bf16 pairs hi + lo, rows and columns as in the X tile
+__device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
+    const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t off = tile_off(r, c0 + 8 * i);
+        const uint4 u = *reinterpret_cast<const uint4 *>(xs + off);
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t v = mul2(wr2, of_bf16(x[e]));
+            hi[e] = bf16_of(v);
+            lo[e] = bf16_of(fma2(of_bf16(hi[e]), minus, v));
+        }
+        *reinterpret_cast<uint4 *>(hi_tile + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4 *>(lo_tile + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+
+// The state that a segment's tokens leave, from a zero state (all segments but the last): H = B^T (w X)
+// with w_s the decay from token s to the segment's end times its step.  The tiles are taken from the
+// last to the first, so that the decay of what follows a tile is known and H only accumulates.
+template <int kN>
+struct StateMap {
+    static constexpr uint32_t kOperand = kN / 64 * kBlockBytes;
+    static constexpr int kSplits = kN == 64 ? 2 : 1;  // buffers of hi, lo
+    static constexpr uint32_t B(int buf) { return buf * kOperand; }
+    static constexpr uint32_t X(int buf) { return 2 * kOperand + buf * kTileBytes; }
+    static constexpr uint32_t Hi(int buf) { return 2 * kOperand + 2 * kTileBytes + buf * 2 * kTileBytes; }
+    static constexpr uint32_t Lo(int buf) { return Hi(buf) + kTileBytes; }
+    static constexpr uint32_t kEnd = Hi(kSplits);
+};
+
+struct StateMisc {
+    float cf[2][2][kTile], tot[2][2][4];  // of two tiles' tokens, as in Misc
+    uint64_t bar[kNumBars];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// (the products of even and odd tiles commit to barriers of their own: a wait may come after the next
+// tile's commit, which would turn a shared barrier's parity)
+static_assert(StateMap<64>::kEnd + sizeof(StateMisc) <= 232448, "shared memory");
+
+enum StateBar { sLd0 = 0, sLd1 = 1, sEvU0 = 2, sEvU1 = 3, sEpX = 4, sTear = 5 };
+
+template <typename M>
+__device__ __forceinline__ bool bar_wait(M *ms, int b, uint32_t parity, const Params &p) {
+    if (mbar_try_wait(&ms->bar[b], parity)) return true;
+    if (*(volatile int *)&ms->abort_flag) return false;
+    if (mbar_wait(&ms->bar[b], parity, kBarWaitNs)) return true;
+    set_error(p.err, 400 + b, parity);
+    *(volatile int *)&ms->abort_flag = 1;
+    return false;
+}
+
+template <typename M>
+__device__ __forceinline__ void epi_arrive(M *ms, int b) {
+    tc_fence_before();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(&ms->bar[b]);
+}
+
+template <int kN>
+__global__ void __launch_bounds__(kThreads, 1)
+ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_b, Params p) {
+    using Sm = StateMap<kN>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    StateMisc *ms = reinterpret_cast<StateMisc *>(smem + Sm::kEnd);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool issuer = warp == kEpiWarps;
+    const Unit u = unit_of(p);
+
+    if (blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
+    if (smem_u32(smem) & 1023u) {                          // the tile layout needs 1 KiB alignment
+        if (tid == 0) set_error(p.err, 398, smem_u32(smem));
+        return;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], i == sEpX ? kEpiWarps : 1);
+        ms->abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (issuer) {
+        tmem_alloc(&ms->tmem_base, 128);
+        tmem_relinquish();
+        if (lane == 0) {
+            prefetch_tmap(&tm_x);
+            prefetch_tmap(&tm_b);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tb = ms->tmem_base;
+
+    if (issuer) {
+        if (lane == 0) {
+            const uint32_t sb4 = smem_u32(smem) >> 4;
+            auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
+            auto load = [&](int j) {  // the j-th tile from the end
+                const int buf = j & 1, t = u.t_lo + (u.tiles - 1 - j) * kTile;
+                uint64_t *bar = &ms->bar[sLd0 + buf];
+                mbar_arrive_expect_tx(bar, kTileBytes + Sm::kOperand);
+                for (int i = 0; i < kN / 64; ++i)
+                    tma_load_4d(smem + Sm::B(buf) + i * kBlockBytes, &tm_b, bar, 64 * i, u.g, t, u.b);
+                tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, u.h0, t, u.b);
+                tma_load_4d(smem + Sm::X(buf) + kBlockBytes, &tm_x, bar, u.one ? 64 : 0,
+                            u.one || !u.both ? u.h0 : u.h0 + 1, t, u.b);
+            };
+            int loaded = 0, landed = 0;
+            while (loaded < 2 && loaded < u.tiles) load(loaded++);
+            bool ok = true;
+            for (int j = 0; j < u.tiles; ++j) {
+                if (!(ok = bar_wait(ms, sLd0 + (j & 1), (j >> 1) & 1, p))) break;
+                landed = j + 1;
+                if (!(ok = bar_wait(ms, sEpX, j & 1, p))) break;
+                tc_fence_after();
+                const int hl = j % Sm::kSplits;
+                mma_ss<true, true, 8>(tb, lm(Sm::B(j & 1)), lm(Sm::Hi(hl)), j > 0 ? 1u : 0u);
+                mma_ss<true, true, 8>(tb, lm(Sm::B(j & 1)), lm(Sm::Lo(hl)), 1u);
+                umma_commit(&ms->bar[sEvU0 + (j & 1)]);
+                if (j > 0 && loaded < u.tiles) {  // the previous tile's products are done: its buffers are free
+                    if (!(ok = bar_wait(ms, sEvU0 + ((j - 1) & 1), ((j - 1) >> 1) & 1, p))) break;
+                    load(loaded++);
+                }
+            }
+            if (!ok) {
+                // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
+                // TMEM are released
+                for (int j = landed; j < loaded; ++j) mbar_wait(&ms->bar[sLd0 + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                umma_commit(&ms->bar[sTear]);
+                mbar_wait(&ms->bar[sTear], 0, kBarWaitNs);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int qd = warp & 3, cq = warp >> 2, r = 32 * qd + lane, c0 = 32 * cq, hs = cq >> 1;
+        const int head = u.one || !hs || !u.both ? u.h0 : u.h0 + 1;  // a second head that is not there: the first
+        const float da = p.a[head] * kLog2e, dbias = p.delta_bias ? p.delta_bias[head] : 0.f;
+        const bool stepper = (cq & 1) == 0;
+        const __nv_bfloat16 *raw = p.delta + (long long)u.b * p.n * p.delta_stride + head;
+        auto fetch = [&](int j) {
+            const int t = u.t_lo + (u.tiles - 1 - j) * kTile + r;
+            return stepper && t >= u.t_lo && t < u.live ? raw[(long long)t * p.delta_stride] : __nv_bfloat16();
+        };
+        float run = 0.f;  // decay of the tiles taken so far (a power of two)
+        __nv_bfloat16 now = fetch(0);
+        for (int j = 0; j < u.tiles; ++j) {
+            const int buf = j & 1, t0 = u.t_lo + (u.tiles - 1 - j) * kTile;
+            const bool in = t0 + r < u.live;
+            const __nv_bfloat16 next = fetch(j + 1);
+            if (stepper) {
+                const float v = to_f32(now) + dbias;
+                const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
+                float up = in ? da * d : 0.f, down = up;
+                sums_of(up, down);
+                const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
+                ms->cf[buf][hs][r] = ex2(lane < 31 ? after : 0.f) * d;
+                if (lane == 31) ms->tot[buf][hs][qd] = up;
+            }
+            now = next;
+            epi_sync();
+            float later = run;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float x = ms->tot[buf][hs][q];
+                if (q > qd) later += x;
+                run += x;
+            }
+            const float wr = ms->cf[buf][hs][r] * ex2(later);
+            bar_wait(ms, sLd0 + buf, (j >> 1) & 1, p);
+            if (t0 + kTile > u.live && !in) {  // tokens that do not count: zero rows, whatever was read
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    const uint4 z = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(smem + Sm::X(buf) + tile_off(r, c0 + i)) = z;
+                    if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(buf) + tile_off(r, c0 + i)) = z;
+                }
+            }
+            if (j >= Sm::kSplits) {  // the products of kSplits tiles ago have read this buffer
+                const int i = j - Sm::kSplits;
+                bar_wait(ms, sEvU0 + (i & 1), (i >> 1) & 1, p);
+                tc_fence_after();
+            }
+            const int hl = j % Sm::kSplits;
+            split_row(smem + Sm::X(buf), smem + Sm::Hi(hl), smem + Sm::Lo(hl), r, c0, wr);
+            fence_async_smem();
+            epi_arrive(ms, sEpX);
+        }
+        if (u.tiles > 0) {
+            const int i = u.tiles - 1;
+            bar_wait(ms, sEvU0 + (i & 1), (i >> 1) & 1, p);
+            tc_fence_after();
+        }
+        const int col = u.one ? c0 : (cq & 1) * 32;  // of the head
+        const bool mine = (!hs || u.both) && r < p.N;
+        const long long at = ((long long)u.b * p.H + head) * p.segments + u.seg;
+        if (mine && col == 0 && r == 0) p.seg_decay[at] = run * kLn2;
+        float *to = p.seg_state + (at * p.N + r) * p.P + col;
+#pragma unroll
+        for (int o = 0; o < 32; o += 16) {
+            uint32_t v[16];
+            tmem_ld16(tb + ((uint32_t)(32 * qd) << 16) + c0 + o, v);  // by whole warps, wherever the values go
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                if (mine && col + o + i < p.P)
+                    *reinterpret_cast<float4 *>(to + o + i) =
+                        u.tiles > 0 ? make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]),
+                                                  __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]))
+                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (issuer) {
+        tc_fence_after();
+        tmem_dealloc(tb, 128);
+    }
+}
+
+template <int kN>
 __global__ void __launch_bounds__(kThreads, 1)
 ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_b,
               const __grid_constant__ CUtensorMap tm_c, const __grid_constant__ CUtensorMap tm_y, Params p) {
@@ -181,18 +422,9 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kEpiWarps;
 
-    // this CTA's unit of 128 columns and its tiles
-    const int unit = blockIdx.x % p.units, seg = blockIdx.x / p.units;
-    const bool one = p.P == 128;  // one head of 128 columns, else two heads of up to 64
-    const int group_heads = p.H / p.G;
-    const int k = unit % p.per_group, g = unit / p.per_group % p.G, b = unit / p.per_group / p.G;
-    const int h0 = g * group_heads + (one ? k : 2 * k);
-    const bool both = one || 2 * k + 1 < group_heads;  // the second 64 columns are a head of this group
-    const int t_lo = seg * p.seg_tiles * kTile, t_hi = min(t_lo + p.seg_tiles * kTile, p.n);
-    int len = p.n;
-    if (p.lengths) len = min(max(p.lengths[b], 0), p.n);
-    const int live = min(t_hi, len);
-    const int tiles = live > t_lo ? (live - t_lo + kTile - 1) / kTile : 0;
+    const Unit u = unit_of(p);
+    const int b = u.b, g = u.g, h0 = u.h0, seg = u.seg, t_lo = u.t_lo, live = u.live, tiles = u.tiles;
+    const bool one = u.one, both = u.both;
 
     if (p.clear && blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
     if (smem_u32(smem) & 1023u) {  // the tile layout needs 1 KiB alignment
@@ -210,7 +442,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         tmem_relinquish();
         if (lane == 0) {
             prefetch_tmap(&tm_x); prefetch_tmap(&tm_b);
-            if (!kStateOnly) { prefetch_tmap(&tm_c); prefetch_tmap(&tm_y); }
+            prefetch_tmap(&tm_c); prefetch_tmap(&tm_y);
         }
     }
     tc_fence_before();
@@ -226,10 +458,10 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             auto load = [&](int j) {
                 const int buf = j & 1, t = t_lo + j * kTile;
                 uint64_t *bar = &ms->bar[bLd0 + buf];
-                mbar_arrive_expect_tx(bar, kTileBytes + (kStateOnly ? 1 : 2) * Sm::kOperand);
+                mbar_arrive_expect_tx(bar, kTileBytes + 2 * Sm::kOperand);
                 for (int i = 0; i < kN / 64; ++i) {
                     tma_load_4d(smem + Sm::B(buf) + i * kBlockBytes, &tm_b, bar, 64 * i, g, t, b);
-                    if (!kStateOnly) tma_load_4d(smem + Sm::C(buf) + i * kBlockBytes, &tm_c, bar, 64 * i, g, t, b);
+                    tma_load_4d(smem + Sm::C(buf) + i * kBlockBytes, &tm_c, bar, 64 * i, g, t, b);
                 }
                 // a second head that the group does not have: the first one again, its result unused
                 tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, h0, t, b);
@@ -249,36 +481,30 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             };
             while (loaded < 2 && loaded < tiles) load(loaded++);
             bool ok = true;
-            if (!kStateOnly && tiles > 0 && (ok = wait_ld(0))) score(0);
+            if (tiles > 0 && (ok = wait_ld(0))) score(0);
             for (int j = 0; ok && j < tiles; ++j) {
                 const int buf = j & 1, par = j & 1;
                 // H before the tile is in EH and TMEM; the previous tile is read out, its buffers are free
                 if (!(ok = bar_wait(ms, bEpE, par, p))) break;
                 tc_fence_after();
-                if (!kStateOnly) {
-                    mma_ss<false, true, kN / 16>(tb + kTY2, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
-                    umma_commit(&ms->bar[bEvY2]);
-                }
+                mma_ss<false, true, kN / 16>(tb + kTY2, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
+                umma_commit(&ms->bar[bEvY2]);
                 if (j > 0 && loaded < tiles) load(loaded++);
-                if (kStateOnly) {
-                    if (!(ok = wait_ld(j))) break;
+                if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+                tc_fence_after();
+                if (one) {
+                    mma_ts<128>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
                 } else {
-                    if (!(ok = bar_wait(ms, bEpW, par, p))) break;
-                    tc_fence_after();
-                    if (one) {
-                        mma_ts<128>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
-                    } else {
-                        mma_ts<64>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
-                        mma_ts<64>(tb + kTY1 + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
-                    }
-                    umma_commit(&ms->bar[bEvY1]);
+                    mma_ts<64>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
+                    mma_ts<64>(tb + kTY1 + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
                 }
+                umma_commit(&ms->bar[bEvY1]);
                 if (!(ok = bar_wait(ms, bEpX, par, p))) break;
                 tc_fence_after();
                 mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::kEH), 1u);  // H += B^T (w X)
                 mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
                 umma_commit(&ms->bar[bEvU]);
-                if (!kStateOnly && j + 1 < tiles) {
+                if (j + 1 < tiles) {
                     if (!(ok = wait_ld(j + 1))) break;
                     score(j + 1);
                 }
@@ -324,13 +550,11 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const uint32_t h_at = tb + lane_base + kTH + c0;
         // 16 columns of the state: their bf16 copy to EH, and times the coming tile's decay to TMEM
         auto put_state = [&](const float (&v)[16], int o, float keep) {
-            if (!kStateOnly) {
 #pragma unroll
-                for (int i = 0; i < 16; i += 8)
-                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + o + i)) =
-                        make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
-                                   pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-            }
+            for (int i = 0; i < 16; i += 8)
+                *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + o + i)) =
+                    make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                               pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
             uint32_t u[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i] * keep);
@@ -352,8 +576,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             }
             total = before + ms->tot[hs][qd] + later;
         };
-        float la_sum = 0.f;
-
         // decays of tile j's tokens from their raw steps
         auto steps = [&](int j, __nv_bfloat16 next_raw) {
             if (!stepper) return;
@@ -362,21 +584,15 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
             const float la = in ? da * d : 0.f;
             float up = la, down = la;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
-                if (lane >= o) up += x;
-                if (lane + o < 32) down += z;
-            }
+            sums_of(up, down);
             const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
             ms->cum[hs][r] = up;
             ms->cf[hs][r] = ex2(lane < 31 ? after : 0.f) * d;
             if (lane == 31) ms->tot[hs][qd] = up;
         };
         // state 0: from state_in or the segment's chained state
-        const float *from = kStateOnly ? nullptr
-                            : p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
-                                             : state_at(const_cast<float *>(p.state_in), 1, 0);
+        const float *from = p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
+                                           : state_at(const_cast<float *>(p.state_in), 1, 0);
         const int cols = p.P - (one ? c0 : (cq & 1) * 32);  // columns of the head from this thread's first one on
         if (tiles > 0) {
             steps(0, fetch());
@@ -510,67 +726,41 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const bool in = t0 + r < live;
             const __nv_bfloat16 next_raw = fetch();  // of the next tile
             // (a) W
-            if (kStateOnly) {
-                la_sum += total;
-                landed(j);
-            } else {
-                weights(j);
-            }
+            weights(j);
             const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
             // (b) w X -> hi (EH), lo
-            if (!kStateOnly) {  // C H has read EH (and C)
-                bar_wait(ms, bEvY2, par, p);
-                tc_fence_after();
-            }
-            {
-                const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t off = tile_off(r, c0 + 8 * i);
-                    const uint4 u = *reinterpret_cast<const uint4 *>(xs + off);
-                    const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-                    uint32_t hi[4], lo[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint64_t v = mul2(wr2, of_bf16(x[e]));
-                        hi[e] = bf16_of(v);
-                        lo[e] = bf16_of(fma2(of_bf16(hi[e]), minus, v));
-                    }
-                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                    *reinterpret_cast<uint4 *>(smem + Sm::lo(buf) + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                }
-            }
+            bar_wait(ms, bEvY2, par, p);  // C H has read EH (and C)
+            tc_fence_after();
+            split_row(xs, smem + Sm::kEH, smem + Sm::lo(buf), r, c0, wr);
             fence_async_smem();
             epi_arrive(ms, bEpX);
             // (c) Y -> bf16 in X's place -> TMA store
-            if (!kStateOnly) {
-                bar_wait(ms, bEvY1, par, p);
-                tc_fence_after();
-                const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
+            bar_wait(ms, bEvY1, par, p);
+            tc_fence_after();
+            const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
 #pragma unroll
-                for (int c = 0; c < 32; c += 16) {
-                    uint32_t y1[16], y2[16], o[8];
-                    tmem_ld16(tb + lane_base + kTY1 + c0 + c, y1);
-                    tmem_ld16(tb + lane_base + kTY2 + c0 + c, y2);
-                    uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
-                    uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
-                    const uint4 u0 = *at0, u1 = *at1;
-                    const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
-                    tmem_ld_wait();
+            for (int c = 0; c < 32; c += 16) {
+                uint32_t y1[16], y2[16], o[8];
+                tmem_ld16(tb + lane_base + kTY1 + c0 + c, y1);
+                tmem_ld16(tb + lane_base + kTY2 + c0 + c, y2);
+                uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
+                uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
+                const uint4 u0 = *at0, u1 = *at1;
+                const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+                tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const uint64_t v = fma2(yf2, pair(y2[2 * e], y2[2 * e + 1]), pair(y1[2 * e], y1[2 * e + 1]));
-                        const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
-                        o[e] = in ? y : 0u;
-                    }
-                    *at0 = make_uint4(o[0], o[1], o[2], o[3]);
-                    *at1 = make_uint4(o[4], o[5], o[6], o[7]);
+                for (int e = 0; e < 8; ++e) {
+                    const uint64_t v = fma2(yf2, pair(y2[2 * e], y2[2 * e + 1]), pair(y1[2 * e], y1[2 * e + 1]));
+                    const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
+                    o[e] = in ? y : 0u;
                 }
-                fence_async_smem();
+                *at0 = make_uint4(o[0], o[1], o[2], o[3]);
+                *at1 = make_uint4(o[4], o[5], o[6], o[7]);
             }
+            fence_async_smem();
             tc_fence_before();
             epi_sync();  // the output is staged; every warp has done with the tile's decays
-            if (!kStateOnly && tid == kStorer) {
+            if (tid == kStorer) {
                 const volatile Misc *m = ms;
                 const int h = m->h0, bb = m->b;
                 tma_store_4d(&tm_y, xs, 0, h, t0, bb);
@@ -582,7 +772,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             // (d) the state after the tile
             bar_wait(ms, bEvU, par, p);
             tc_fence_after();
-            if (!kStateOnly && tid == kStorer) tma_store_wait_read();  // X's slot may be loaded again
+            if (tid == kStorer) tma_store_wait_read();  // X's slot may be loaded again
             if (j + 1 < tiles) {
                 decays();
                 if (srow) {
@@ -607,7 +797,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const int hcol = one ? c0 : (cq & 1) * 32;
         const int head = m->h0 + (one ? 0 : hs);
         const bool mine = !hs || m->both;
-        if (!kStateOnly && mine) {  // the rest of the segment does not count: zeros
+        if (mine) {  // the rest of the segment does not count: zeros
             const int end = min((m->seg + 1) * p.seg_tiles * kTile, p.n);
             for (int t = max(m->seg * p.seg_tiles * kTile, live) + r; t < end; t += kTile) {
                 __nv_bfloat16 *row = p.y + ((long long)m->b * p.n + t) * p.y_stride + (long long)head * p.P + hcol;
@@ -616,14 +806,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     if (i < cols) *reinterpret_cast<uint4 *>(row + i) = make_uint4(0, 0, 0, 0);
             }
         }
-        float *to = nullptr;
-        if (kStateOnly) {
-            to = state_at(p.seg_state, p.segments, m->seg);
-            if (mine && hcol == 0 && r == 0)
-                p.seg_decay[((long long)m->b * p.H + head) * p.segments + m->seg] = la_sum * kLn2;
-        } else if (m->seg == p.segments - 1) {
-            to = state_at(p.state_out, 1, 0);
-        }
+        float *to = m->seg == p.segments - 1 ? state_at(p.state_out, 1, 0) : nullptr;
 #pragma unroll
         for (int o = 0; o < 32; o += 16) {
             uint32_t u[16];
@@ -639,7 +822,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 *reinterpret_cast<float4 *>(to + o + i) = f;
             }
         }
-        if (!kStateOnly && tid == kStorer) tma_store_wait_all();
+        if (tid == kStorer) tma_store_wait_all();
     }
     tc_fence_before();
     __syncthreads();
@@ -753,16 +936,23 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     const bool wide = p.N == 128;
     if (c.segments > 1) {
         const int blocks = c.units * (c.segments - 1);
-        cudaError_t e = wide ? launch(ssm_tc_kernel<128, true>, blocks, Map<128>::kBytes)
-                             : launch(ssm_tc_kernel<64, true>, blocks, Map<64>::kBytes);
+        auto run = [&](auto kern, uint32_t smem) -> cudaError_t {
+            cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e) return e;
+            kern<<<blocks, kThreads, smem, stream>>>(mx, mb, q);
+            return cudaGetLastError();
+        };
+        constexpr uint32_t kMisc = sizeof(StateMisc);
+        cudaError_t e = wide ? run(ssm_state_kernel<128>, StateMap<128>::kEnd + kMisc)
+                             : run(ssm_state_kernel<64>, StateMap<64>::kEnd + kMisc);
         if (e) return e;
         e = ssm_chain_launch(p.state_in, q.seg_state, q.seg_decay, (long long)p.B * p.H, p.N * p.P, c.segments, stream);
         if (e) return e;
         q.clear = 0;
     }
     const int blocks = c.units * c.segments;
-    return wide ? launch(ssm_tc_kernel<128, false>, blocks, Map<128>::kBytes)
-                : launch(ssm_tc_kernel<64, false>, blocks, Map<64>::kBytes);
+    return wide ? launch(ssm_tc_kernel<128>, blocks, Map<128>::kBytes)
+                : launch(ssm_tc_kernel<64>, blocks, Map<64>::kBytes);
 }
 
 }  // namespace hla

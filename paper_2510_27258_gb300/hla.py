@@ -390,17 +390,32 @@ def _type_code(dtype) -> int:
     raise TypeError("tokens must be bfloat16 or float32, got %s" % dtype)
 
 
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _like(name, t, shape, dtype, device):
-    """Checks a contiguous tensor's (or None's) shape, type and device."""
+def _flat(name, t, count, dtype, index):
+    """Address of a contiguous tensor of `count` elements on GPU `index` (None stays None)."""
     if t is None:
-        return
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor %s on %s, got %s %s on %s"
-                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+        return None
+    if t.numel() != count or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on cuda:%d, got %s %s on %s"
+                         % (name, dtype, count, index, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _rows(name, t, shape, inner, dtype, index):
+    """Row stride (elements) of a token tensor on GPU `index`: `shape` with rows of strides `inner`."""
+    if t.dtype is dtype and t.get_device() == index and t.shape == shape:
+        st, lead = t.stride(), len(shape) - len(inner)
+        if st[lead:] == inner:
+            rows = shape[lead - 1]
+            if rows > 1:
+                if lead == 1 or shape[0] == 1 or st[0] == rows * st[1]:
+                    return st[lead - 1]
+            elif lead == 2 and rows == 1 and shape[0] > 1:
+                return st[0]
+            else:
+                return inner[0] * shape[lead]
+    else:
+        lead = len(shape) - len(inner)
+    return _row_stride(name, t, lead, shape, dtype, torch.device("cuda", index))
 
 
 def _row_stride(name, t, lead, shape, dtype, device):
@@ -424,24 +439,34 @@ def _row_stride(name, t, lead, shape, dtype, device):
     return st[0] if shape[0] > 1 else width
 
 
-def _need_cuda(t):
-    if not t.is_cuda:
+def _gpu(t):
+    """Index of a tensor's GPU."""
+    index = t.get_device()
+    if index < 0:
         raise ValueError("tensors must be CUDA tensors, got one on %s" % t.device)
-    return t.device
+    return index
 
 
-def _on(stream, device):
+def _on(stream, index):
     if stream is None:
-        return torch.cuda.current_stream(device).cuda_stream
+        return torch.cuda.current_stream(index).cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _scratch(workspace, nbytes, device):
+def _scratch(workspace, need, index, *sizes):
+    """(address, bytes, tensor) of the caller's workspace, or of a new one of need(*sizes) bytes."""
     if workspace is None:
-        workspace = alloc_workspace(nbytes, device)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on %s" % device)
-    return workspace, workspace.numel() * workspace.element_size()
+        workspace = alloc_workspace(need(*sizes), torch.device("cuda", index))
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on cuda:%d" % index)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+
+
+def _conv_sizes(x, weight, dims):
+    if x.dim() != dims or weight.dim() != 2:
+        raise ValueError("x must be %s and weight [C, width], got %s and %s"
+                         % ("[B, n, C]" if dims == 3 else "[B, C]", tuple(x.shape), tuple(weight.shape)))
+    return x.shape, weight.shape[1], _type_code(x.dtype), x.dtype, _gpu(x)
 
 
 def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None, state_in=None, state_out=None,
@@ -451,43 +476,30 @@ def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None,
     x: [B, n, C], rows may be slices of wider rows; weight: [C, width]; bias: [C]; lengths: int32 [B];
     states: [B, width - 1, C] (state_out may be state_in).
     """
-    if x.dim() != 3 or weight.dim() != 2:
-        raise ValueError("x must be [B, n, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
-    dev, T = _need_cuda(x), x.dtype
-    B, n, C = x.shape
-    W = weight.shape[1]
-    dt = _type_code(T)
+    shape, W, dt, T, i = _conv_sizes(x, weight, 3)
+    B, n, C = shape
     if out is None:
-        out = torch.empty((B, n, C), dtype=T, device=dev)
-    xs, os_ = _row_stride("x", x, 2, (B, n, C), T, dev), _row_stride("out", out, 2, (B, n, C), T, dev)
-    _like("weight", weight, (C, W), T, dev)
-    _like("bias", bias, (C,), T, dev)
-    _like("lengths", lengths, (B,), torch.int32, dev)
-    _like("state_in", state_in, (B, W - 1, C), T, dev)
-    _like("state_out", state_out, (B, W - 1, C), T, dev)
-    _check(lib().hla_conv_forward(x.data_ptr(), weight.data_ptr(), _at(bias), out.data_ptr(), dt, B, n, C, W, xs, os_,
-                                  int(silu), _at(lengths), _at(state_in), _at(state_out), _on(stream, dev)),
-           "hla_conv_forward")
+        out = torch.empty(shape, dtype=T, device=x.device)
+    kept = B * (W - 1) * C
+    _check(lib().hla_conv_forward(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, n, C, W,
+        _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
+        _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, T, i),
+        _flat("state_out", state_out, kept, T, i), _on(stream, i)), "hla_conv_forward")
     return out
 
 
 def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=None):
     """One token a sequence of hla_conv_forward (include/hla.h: hla_conv_step); ``state`` [B, width - 1, C] is
     updated in place.  x: [B, C]; ``out`` may be ``x``."""
-    if x.dim() != 2 or weight.dim() != 2:
-        raise ValueError("x must be [B, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
-    dev, T = _need_cuda(x), x.dtype
-    B, C = x.shape
-    W = weight.shape[1]
-    dt = _type_code(T)
+    shape, W, dt, T, i = _conv_sizes(x, weight, 2)
+    B, C = shape
     if out is None:
-        out = torch.empty((B, C), dtype=T, device=dev)
-    xs, os_ = _row_stride("x", x, 1, (B, C), T, dev), _row_stride("out", out, 1, (B, C), T, dev)
-    _like("weight", weight, (C, W), T, dev)
-    _like("bias", bias, (C,), T, dev)
-    _like("state", state, (B, W - 1, C), T, dev)
-    _check(lib().hla_conv_step(x.data_ptr(), weight.data_ptr(), _at(bias), out.data_ptr(), dt, B, C, W, xs, os_,
-                               int(silu), state.data_ptr(), _on(stream, dev)), "hla_conv_step")
+        out = torch.empty(shape, dtype=T, device=x.device)
+    _check(lib().hla_conv_step(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, C, W,
+        _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
+        _flat("state", state, B * (W - 1) * C, T, i), _on(stream, i)), "hla_conv_step")
     return out
 
 
@@ -498,25 +510,18 @@ def hla_conv_backward_workspace_bytes(B, n, C, width, dtype) -> int:
 def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths=None, workspace=None, stream=None):
     """Gradients (dx, dweight, dbias) of sum(dout * out) for hla_conv_forward from a zero state
     (include/hla.h: hla_conv_backward); the weights' are fp32, dbias is None where bias is."""
-    if x.dim() != 3 or weight.dim() != 2:
-        raise ValueError("x must be [B, n, C] and weight [C, width], got %s and %s" % (tuple(x.shape), tuple(weight.shape)))
-    dev, T = _need_cuda(x), x.dtype
-    B, n, C = x.shape
-    W = weight.shape[1]
-    dt = _type_code(T)
+    shape, W, dt, T, i = _conv_sizes(x, weight, 3)
+    B, n, C = shape
     if dx is None:
-        dx = torch.empty((B, n, C), dtype=T, device=dev)
-    xs, gs, ds = (_row_stride(name, t, 2, (B, n, C), T, dev) for name, t in (("x", x), ("dout", dout), ("dx", dx)))
-    _like("weight", weight, (C, W), T, dev)
-    _like("bias", bias, (C,), T, dev)
-    _like("lengths", lengths, (B,), torch.int32, dev)
-    dw = torch.empty((C, W), dtype=torch.float32, device=dev)
-    db = None if bias is None else torch.empty((C,), dtype=torch.float32, device=dev)
-    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
-                            hla_conv_backward_workspace_bytes(B, n, C, W, dt), dev)
-    _check(lib().hla_conv_backward(x.data_ptr(), weight.data_ptr(), _at(bias), dout.data_ptr(), dx.data_ptr(),
-                                   dw.data_ptr(), _at(db), dt, B, n, C, W, xs, gs, ds, int(silu), _at(lengths),
-                                   ws.data_ptr(), ws_bytes, _on(stream, dev)), "hla_conv_backward")
+        dx = torch.empty(shape, dtype=T, device=x.device)
+    dw = torch.empty((C, W), dtype=torch.float32, device=x.device)
+    db = None if bias is None else torch.empty((C,), dtype=torch.float32, device=x.device)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, B, n, C, W, dt)
+    _check(lib().hla_conv_backward(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), dout.data_ptr(), dx.data_ptr(),
+        dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i),
+        _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), 1 if silu else 0,
+        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, _on(stream, i)), "hla_conv_backward")
     return dx, dw, db
 
 
@@ -533,26 +538,21 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
     """
     if x.dim() != 4 or b.dim() != 4:
         raise ValueError("x must be [B, n, H, P] and b [B, n, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
-    dev, T = _need_cuda(x), x.dtype
-    B, n, H, P = x.shape
+    T, i, shape = x.dtype, _gpu(x), x.shape
+    B, n, H, P = shape
     G, N = b.shape[2:]
     dt, f32 = _type_code(T), torch.float32
     if out is None:
-        out = torch.empty((B, n, H, P), dtype=T, device=dev)
-    xs, ys = _row_stride("x", x, 2, (B, n, H, P), T, dev), _row_stride("out", out, 2, (B, n, H, P), T, dev)
-    ds = _row_stride("delta", delta, 2, (B, n, H), T, dev)
-    bs, cs = _row_stride("b", b, 2, (B, n, G, N), T, dev), _row_stride("c", c, 2, (B, n, G, N), T, dev)
-    for name, t in (("a", a), ("skip", skip), ("delta_bias", delta_bias)):
-        _like(name, t, (H,), f32, dev)
-    _like("lengths", lengths, (B,), torch.int32, dev)
-    _like("state_in", state_in, (B, H, N, P), f32, dev)
-    _like("state_out", state_out, (B, H, N, P), f32, dev)
-    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
-                            hla_ssm_workspace_bytes(B, n, H, P, G, N, dt), dev)
-    _check(lib().hla_ssm_forward(x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(), _at(skip),
-                                 _at(delta_bias), out.data_ptr(), dt, B, n, H, P, G, N, xs, ds, bs, cs, ys,
-                                 int(softplus), _at(lengths), _at(state_in), _at(state_out), ws.data_ptr(), ws_bytes,
-                                 _on(stream, dev)), "hla_ssm_forward")
+        out = torch.empty(shape, dtype=T, device=x.device)
+    bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), B * H * N * P
+    ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, B, n, H, P, G, N, dt)
+    _check(lib().hla_ssm_forward(
+        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, n, H, P, G, N,
+        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
+        _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
+        1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, f32, i),
+        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, _on(stream, i)), "hla_ssm_forward")
     return out
 
 
@@ -561,42 +561,32 @@ def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=No
     updated in place.  x: [B, H, P]; delta: [B, H]; b, c: [B, G, N]; ``out`` may be ``x``."""
     if x.dim() != 3 or b.dim() != 3:
         raise ValueError("x must be [B, H, P] and b [B, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
-    dev, T = _need_cuda(x), x.dtype
-    B, H, P = x.shape
-    G, N = b.shape[1:]
+    T, i, shape, bc = x.dtype, _gpu(x), x.shape, b.shape
+    B, H, P = shape
+    G, N = bc[1], bc[2]
     dt, f32 = _type_code(T), torch.float32
     if out is None:
-        out = torch.empty((B, H, P), dtype=T, device=dev)
-    xs, ys = _row_stride("x", x, 1, (B, H, P), T, dev), _row_stride("out", out, 1, (B, H, P), T, dev)
-    ds = _row_stride("delta", delta, 1, (B, H), T, dev)
-    bs, cs = _row_stride("b", b, 1, (B, G, N), T, dev), _row_stride("c", c, 1, (B, G, N), T, dev)
-    for name, t in (("a", a), ("skip", skip), ("delta_bias", delta_bias)):
-        _like(name, t, (H,), f32, dev)
-    _like("state", state, (B, H, N, P), f32, dev)
-    _check(lib().hla_ssm_step(x.data_ptr(), delta.data_ptr(), a.data_ptr(), b.data_ptr(), c.data_ptr(), _at(skip),
-                              _at(delta_bias), out.data_ptr(), dt, B, H, P, G, N, xs, ds, bs, cs, ys, int(softplus),
-                              state.data_ptr(), _on(stream, dev)), "hla_ssm_step")
+        out = torch.empty(shape, dtype=T, device=x.device)
+    bc, inner, bc_inner = (B, G, N), (P, 1), (N, 1)
+    _check(lib().hla_ssm_step(
+        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, H, P, G, N,
+        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i), _rows("b", b, bc, bc_inner, T, i),
+        _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i), 1 if softplus else 0,
+        _flat("state", state, B * H * N * P, f32, i), _on(stream, i)), "hla_ssm_step")
     return out
 
 
-def _qk_sizes(q, k, wq, wk, cos, sin, positions):
+def _qk_sizes(q, k, cos, sin):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q must be [B, n, H, d] and k [B, n, Hk, d], got %s and %s" % (tuple(q.shape), tuple(k.shape)))
-    dev, T = _need_cuda(q), q.dtype
-    B, n, H, d = q.shape
-    Hk = k.shape[2]
-    qs, ks = _row_stride("q", q, 2, (B, n, H, d), T, dev), _row_stride("k", k, 2, (B, n, Hk, d), T, dev)
-    _like("wq", wq, (d,), T, dev)
-    _like("wk", wk, (d,), T, dev)
     rot, top = 0, 0
     if cos is not None:
         if cos.dim() != 2 or sin is None:
             raise ValueError("cos and sin must both be [rows, rot / 2]")
-        top, rot = cos.shape[0], 2 * cos.shape[1]
-        _like("cos", cos, cos.shape, torch.float32, dev)
-        _like("sin", sin, cos.shape, torch.float32, dev)
-    _like("positions", positions, (B, n), torch.int32, dev)
-    return dev, T, B, n, H, Hk, d, rot, top, qs, ks
+        top, half = cos.shape
+        rot = 2 * half
+    return q.dtype, _gpu(q), q.shape, k.shape[2], rot, top
 
 
 def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, k_out=None, *, positions=None, pos0=0,
@@ -607,17 +597,20 @@ def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, 
     q: [B, n, H, d]; k: [B, n, Hk, d] (rows may be slices of wider rows); wq, wk: [d]; cos, sin: fp32
     [rows, rot / 2]; positions: int32 [B, n], or None for pos0, pos0 + 1, ...
     """
-    dev, T, B, n, H, Hk, d, rot, top, qs, ks = _qk_sizes(q, k, wq, wk, cos, sin, positions)
+    T, i, shape, Hk, rot, top = _qk_sizes(q, k, cos, sin)
+    B, n, H, d = shape
     if q_out is None:
-        q_out = torch.empty((B, H, n, d), dtype=T, device=dev)
+        q_out = torch.empty((B, H, n, d), dtype=T, device=q.device)
     if k_out is None:
-        k_out = torch.empty((B, H, n, d), dtype=T, device=dev)
-    _like("q_out", q_out, (B, H, n, d), T, dev)
-    _like("k_out", k_out, (B, H, n, d), T, dev)
-    _check(lib().hla_qk_norm_forward(q.data_ptr(), k.data_ptr(), _at(wq), _at(wk), _at(cos), _at(sin), _at(positions),
-                                     q_out.data_ptr(), k_out.data_ptr(), _type_code(T), B, n, H, Hk, d, rot,
-                                     int(interleaved), qs, ks, int(pos0), top, float(eps), _on(stream, dev)),
-           "hla_qk_norm_forward")
+        k_out = torch.empty((B, H, n, d), dtype=T, device=q.device)
+    inner, table, count = (d, 1), top * rot // 2, B * H * n * d
+    _check(lib().hla_qk_norm_forward(
+        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
+        _flat("positions", positions, B * n, torch.int32, i), _flat("q_out", q_out, count, T, i),
+        _flat("k_out", k_out, count, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
+        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, _on(stream, i)),
+        "hla_qk_norm_forward")
     return q_out, k_out
 
 
@@ -629,22 +622,23 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
                          interleaved=False, workspace=None, stream=None):
     """Gradients (dq, dk, dwq, dwk) of sum(dq_out * q_out) + sum(dk_out * k_out) for hla_qk_norm_forward
     (include/hla.h: hla_qk_norm_backward); dwq, dwk are fp32 [d], None where the weight is."""
-    dev, T, B, n, H, Hk, d, rot, top, qs, ks = _qk_sizes(q, k, wq, wk, cos, sin, positions)
-    _like("dq_out", dq_out, (B, H, n, d), T, dev)
-    _like("dk_out", dk_out, (B, H, n, d), T, dev)
+    T, i, shape, Hk, rot, top = _qk_sizes(q, k, cos, sin)
+    B, n, H, d = shape
+    k_shape = (B, n, Hk, d)
     if dq is None:
-        dq = torch.empty((B, n, H, d), dtype=T, device=dev)
+        dq = torch.empty(shape, dtype=T, device=q.device)
     if dk is None:
-        dk = torch.empty((B, n, Hk, d), dtype=T, device=dev)
-    dqs, dks = _row_stride("dq", dq, 2, (B, n, H, d), T, dev), _row_stride("dk", dk, 2, (B, n, Hk, d), T, dev)
-    dwq = None if wq is None else torch.empty((d,), dtype=torch.float32, device=dev)
-    dwk = None if wk is None else torch.empty((d,), dtype=torch.float32, device=dev)
-    dt = _type_code(T)
-    ws, ws_bytes = _scratch(workspace, 0 if workspace is not None else
-                            hla_qk_norm_backward_workspace_bytes(B, n, H, Hk, d, dt), dev)
-    _check(lib().hla_qk_norm_backward(q.data_ptr(), k.data_ptr(), _at(wq), _at(wk), _at(cos), _at(sin),
-                                      _at(positions), dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(),
-                                      dk.data_ptr(), _at(dwq), _at(dwk), dt, B, n, H, Hk, d, rot, int(interleaved), qs,
-                                      ks, dqs, dks, int(pos0), top, float(eps), ws.data_ptr(), ws_bytes,
-                                      _on(stream, dev)), "hla_qk_norm_backward")
+        dk = torch.empty(k_shape, dtype=T, device=q.device)
+    dwq = None if wq is None else torch.empty((d,), dtype=torch.float32, device=q.device)
+    dwk = None if wk is None else torch.empty((d,), dtype=torch.float32, device=q.device)
+    dt, inner, table, count = _type_code(T), (d, 1), top * rot // 2, B * H * n * d
+    ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, B, n, H, Hk, d, dt)
+    _check(lib().hla_qk_norm_backward(
+        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
+        _flat("positions", positions, B * n, torch.int32, i), _flat("dq_out", dq_out, count, T, i),
+        _flat("dk_out", dk_out, count, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
+        None if dwk is None else dwk.data_ptr(), dt, B, n, H, Hk, d, rot, 1 if interleaved else 0,
+        _rows("q", q, shape, inner, T, i), _rows("k", k, k_shape, inner, T, i), _rows("dq", dq, shape, inner, T, i),
+        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, _on(stream, i)), "hla_qk_norm_backward")
     return dq, dk, dwq, dwk
