@@ -368,7 +368,7 @@ Geom geometry(int B, int n, int C, int V) {
     for (int L = kStrip; L <= 128; L += kStrip) {
         const long long tb = n > 0 ? ceil_div(n, (long long)L * kStrips) : 1;
         const long long waves = ((long long)B * g.cblocks * tb + 152 * kResident - 1) / (152 * kResident);
-        if (L == kStrip || waves * (L + 8) < best) {
+        if (L == kStrip || waves * (L + 8) <= best) {
             best = waves * (L + 8);
             g.L = L;
             g.tblocks = (int)tb;

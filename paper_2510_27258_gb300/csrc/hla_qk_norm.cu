@@ -351,18 +351,23 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
     }
 }
 
-// dwq and dwk from `rows` partials [2][d]: one warp an entry
-__global__ void __launch_bounds__(kThreads)
+// dwq and dwk from `rows` partials [2][d]: 32 entries a block, a warp for every 32nd row
+constexpr int kSumThreads = 1024;
+
+__global__ void __launch_bounds__(kSumThreads)
 qk_norm_sum_kernel(const float *__restrict__ partial, int rows, int d, float *dwq, float *dwk, WsHeader *header) {
+    __shared__ float red[32][33];
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
-    const int i = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (i >= 2 * d) return;
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;  // 2 d is a multiple of 32
     float s = 0.f;
 #pragma unroll 8
-    for (int r = lane; r < rows; r += 32) s += partial[(size_t)r * 2 * d + i];
-    s = row_sum<32>(s);
-    float *to = i < d ? dwq : dwk;
-    if (lane == 0 && to) to[i < d ? i : i - d] = s;
+    for (int r = group; r < rows; r += 32) s += partial[(size_t)r * 2 * d + i];
+    red[group][lane] = s;
+    __syncthreads();
+    s = row_sum<32>(red[lane][group]);  // entry `group` of the block
+    const int e = blockIdx.x * 32 + group;
+    float *to = e < d ? dwq : dwk;
+    if (lane == 0 && to) to[e < d ? e : e - d] = s;
 }
 
 struct Plan {
@@ -413,7 +418,7 @@ cudaError_t backward_as(const QkNormBwd &p, cudaStream_t s) {
         qk_norm_backward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
         cudaError_t e = cudaGetLastError();
         if (e) return e;
-        qk_norm_sum_kernel<<<(2 * p.f.d * 32 + kThreads - 1) / kThreads, kThreads, 0, s>>>(
+        qk_norm_sum_kernel<<<2 * p.f.d / 32, kSumThreads, 0, s>>>(
             p.partial, (int)(g.gx * g.gy), p.f.d, p.dwq, p.dwk, p.header);
         return cudaGetLastError();
     });

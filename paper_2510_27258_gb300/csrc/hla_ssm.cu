@@ -70,23 +70,46 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
     if (!kStateOnly && blockIdx.x == 0 && tid == 0)  // no device-side waits here: never an error
         *reinterpret_cast<WsHeader *>(p.ws) = WsHeader{};
 
+    // a block of tokens is loaded into registers while the one before it is computed
+    constexpr int kPer = kTok * N / kScanThreads, kPerX = kTok * kCols / kScanThreads;
+    float br[kPer], cr[kPer], xr[kPerX], dr = 0.f;
+    auto fetch = [&](int t0) {
+        const int left = live - t0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = tid + i * kScanThreads, t = e / N, k = e % N;
+            br[i] = t < left ? to_f32(bm[(size_t)(t0 + t) * p.b_stride + k]) : 0.f;
+            if (!kStateOnly) cr[i] = t < left ? to_f32(cm[(size_t)(t0 + t) * p.c_stride + k]) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kPerX; ++i) {
+            const int e = tid + i * kScanThreads, t = e / kCols;
+            xr[i] = t < left ? to_f32(x[(size_t)(t0 + t) * p.x_stride + e % kCols]) : 0.f;
+        }
+        if (tid < kTok) dr = tid < left ? to_f32(raw[(size_t)(t0 + tid) * p.delta_stride]) : 0.f;
+    };
+    if (t_lo < live) fetch(t_lo);
     for (int t0 = t_lo; t0 < live; t0 += kTok) {
         const int count = min(kTok, live - t0);
         __syncthreads();
-        for (int i = tid; i < count * N; i += kScanThreads) {
-            const int t = i / N, k = i % N;
-            bs[t][k] = to_f32(bm[(size_t)(t0 + t) * p.b_stride + k]);
-            if (!kStateOnly) cs[t][k] = to_f32(cm[(size_t)(t0 + t) * p.c_stride + k]);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = tid + i * kScanThreads;
+            bs[e / N][e % N] = br[i];
+            if (!kStateOnly) cs[e / N][e % N] = cr[i];
         }
-        for (int i = tid; i < count * kCols; i += kScanThreads)
-            xs[i / kCols][i % kCols] = to_f32(x[(size_t)(t0 + i / kCols) * p.x_stride + i % kCols]);
+#pragma unroll
+        for (int i = 0; i < kPerX; ++i) {
+            const int e = tid + i * kScanThreads;
+            xs[e / kCols][e % kCols] = xr[i];
+        }
         if (tid < count) {
-            const float d = step_size(to_f32(raw[(size_t)(t0 + tid) * p.delta_stride]), bias, p.softplus);
+            const float d = step_size(dr, bias, p.softplus);
             dl[tid] = d;
             decay[tid] = expf(a * d);
             if (kStateOnly) {
                 float sum = a * d;
-                const unsigned mask = count == 32 ? 0xffffffffu : (1u << count) - 1u;
+                const unsigned mask = (1u << count) - 1u;
                 for (int o = 1; o < kTok; o <<= 1) {
                     const float other = __shfl_down_sync(mask, sum, o);
                     if (tid + o < count) sum += other;
@@ -94,6 +117,7 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
                 if (tid == 0) la_sum += sum;
             }
         }
+        if (t0 + kTok < live) fetch(t0 + kTok);
         __syncthreads();
         for (int t8 = 0; t8 < count; t8 += 8) {
             float part[8];
@@ -160,7 +184,7 @@ chain_kernel(const float *state_in, float *seg_state, const float *seg_decay, lo
     float h = state_in ? state_in[head * NP + e] : 0.f;
     float *s = seg_state + head * segments * NP + e;
     const float *la = seg_decay + head * segments;
-    constexpr int kBatch = 8;  // segments loaded at once
+    constexpr int kBatch = 16;  // segments loaded at once
     for (int k0 = 0; k0 < segments; k0 += kBatch) {
         float own[kBatch], decay[kBatch];
 #pragma unroll

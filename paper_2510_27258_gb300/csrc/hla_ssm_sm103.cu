@@ -189,7 +189,8 @@ __device__ __forceinline__ void sums_of(float &up, float &down) {
     }
 }
 
-// 32 elements of a row of w X as the bf16 pairs hi + lo, rows and columns as in the X tile
+// 32 elements of a row of w X as the bf16 pairs hi + lo, rows and columns as in the X tile (hi may take
+// its place)
 __device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
     const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
 #pragma unroll
@@ -212,15 +213,15 @@ __device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, u
 // The state that a segment's tokens leave, from a zero state (all segments but the last): H = B^T (w X)
 // with w_s the decay from token s to the segment's end times its step.  The tiles are taken from the
 // last to the first, so that the decay of what follows a tile is known and H only accumulates.
+// A stage holds a tile's B and X; hi takes X's place.
 template <int kN>
 struct StateMap {
     static constexpr uint32_t kOperand = kN / 64 * kBlockBytes;
-    static constexpr int kSplits = kN == 64 ? 2 : 1;  // buffers of hi, lo
-    static constexpr uint32_t B(int buf) { return buf * kOperand; }
-    static constexpr uint32_t X(int buf) { return 2 * kOperand + buf * kTileBytes; }
-    static constexpr uint32_t Hi(int buf) { return 2 * kOperand + 2 * kTileBytes + buf * 2 * kTileBytes; }
-    static constexpr uint32_t Lo(int buf) { return Hi(buf) + kTileBytes; }
-    static constexpr uint32_t kEnd = Hi(kSplits);
+    static constexpr int kStages = kN == 64 ? 3 : 2;
+    static constexpr uint32_t B(int s) { return s * kOperand; }
+    static constexpr uint32_t X(int s) { return kStages * kOperand + s * kTileBytes; }
+    static constexpr uint32_t Lo(int j) { return kStages * (kOperand + kTileBytes) + (j & 1) * kTileBytes; }
+    static constexpr uint32_t kEnd = Lo(1) + kTileBytes;
 };
 
 struct StateMisc {
@@ -230,11 +231,12 @@ struct StateMisc {
     int abort_flag;
 };
 
+static_assert(StateMap<64>::kEnd + sizeof(StateMisc) <= 232448 && StateMap<128>::kEnd + sizeof(StateMisc) <= 232448,
+              "shared memory");
+
 // (the products of even and odd tiles commit to barriers of their own: a wait may come after the next
 // tile's commit, which would turn a shared barrier's parity)
-static_assert(StateMap<64>::kEnd + sizeof(StateMisc) <= 232448, "shared memory");
-
-enum StateBar { sLd0 = 0, sLd1 = 1, sEvU0 = 2, sEvU1 = 3, sEpX = 4, sTear = 5 };
+enum StateBar { sLd0 = 0, sEvU0 = 3, sEvU1 = 4, sEpX = 5, sTear = 6 };  // sLd0 + stage
 
 template <typename M>
 __device__ __forceinline__ bool bar_wait(M *ms, int b, uint32_t parity, const Params &p) {
@@ -291,7 +293,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             const uint32_t sb4 = smem_u32(smem) >> 4;
             auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
             auto load = [&](int j) {  // the j-th tile from the end
-                const int buf = j & 1, t = u.t_lo + (u.tiles - 1 - j) * kTile;
+                const int buf = j % Sm::kStages, t = u.t_lo + (u.tiles - 1 - j) * kTile;
                 uint64_t *bar = &ms->bar[sLd0 + buf];
                 mbar_arrive_expect_tx(bar, kTileBytes + Sm::kOperand);
                 for (int i = 0; i < kN / 64; ++i)
@@ -301,18 +303,18 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                             u.one || !u.both ? u.h0 : u.h0 + 1, t, u.b);
             };
             int loaded = 0, landed = 0;
-            while (loaded < 2 && loaded < u.tiles) load(loaded++);
+            while (loaded < Sm::kStages && loaded < u.tiles) load(loaded++);
             bool ok = true;
             for (int j = 0; j < u.tiles; ++j) {
-                if (!(ok = bar_wait(ms, sLd0 + (j & 1), (j >> 1) & 1, p))) break;
+                const int st = j % Sm::kStages;
+                if (!(ok = bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p))) break;
                 landed = j + 1;
                 if (!(ok = bar_wait(ms, sEpX, j & 1, p))) break;
                 tc_fence_after();
-                const int hl = j % Sm::kSplits;
-                mma_ss<true, true, 8>(tb, lm(Sm::B(j & 1)), lm(Sm::Hi(hl)), j > 0 ? 1u : 0u);
-                mma_ss<true, true, 8>(tb, lm(Sm::B(j & 1)), lm(Sm::Lo(hl)), 1u);
+                mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::X(st)), j > 0 ? 1u : 0u);
+                mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::Lo(j)), 1u);
                 umma_commit(&ms->bar[sEvU0 + (j & 1)]);
-                if (j > 0 && loaded < u.tiles) {  // the previous tile's products are done: its buffers are free
+                if (j > 0 && loaded < u.tiles) {  // the previous tile's products are done: its stage is free
                     if (!(ok = bar_wait(ms, sEvU0 + ((j - 1) & 1), ((j - 1) >> 1) & 1, p))) break;
                     load(loaded++);
                 }
@@ -320,7 +322,8 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             if (!ok) {
                 // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
                 // TMEM are released
-                for (int j = landed; j < loaded; ++j) mbar_wait(&ms->bar[sLd0 + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                for (int j = landed; j < loaded; ++j)
+                    mbar_wait(&ms->bar[sLd0 + j % Sm::kStages], (j / Sm::kStages) & 1, kBarWaitNs);
                 umma_commit(&ms->bar[sTear]);
                 mbar_wait(&ms->bar[sTear], 0, kBarWaitNs);
             }
@@ -361,22 +364,22 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                 run += x;
             }
             const float wr = ms->cf[buf][hs][r] * ex2(later);
-            bar_wait(ms, sLd0 + buf, (j >> 1) & 1, p);
+            const int st = j % Sm::kStages;
+            uint8_t *xs = smem + Sm::X(st);
+            bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p);
             if (t0 + kTile > u.live && !in) {  // tokens that do not count: zero rows, whatever was read
 #pragma unroll
                 for (int i = 0; i < 32; i += 8) {
                     const uint4 z = make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(smem + Sm::X(buf) + tile_off(r, c0 + i)) = z;
-                    if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(buf) + tile_off(r, c0 + i)) = z;
+                    *reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + i)) = z;
+                    if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(st) + tile_off(r, c0 + i)) = z;
                 }
             }
-            if (j >= Sm::kSplits) {  // the products of kSplits tiles ago have read this buffer
-                const int i = j - Sm::kSplits;
-                bar_wait(ms, sEvU0 + (i & 1), (i >> 1) & 1, p);
+            if (j >= 2) {  // the products of two tiles ago have read this lo
+                bar_wait(ms, sEvU0 + (j & 1), ((j - 2) >> 1) & 1, p);
                 tc_fence_after();
             }
-            const int hl = j % Sm::kSplits;
-            split_row(smem + Sm::X(buf), smem + Sm::Hi(hl), smem + Sm::Lo(hl), r, c0, wr);
+            split_row(xs, xs, smem + Sm::Lo(j), r, c0, wr);
             fence_async_smem();
             epi_arrive(ms, sEpX);
         }
