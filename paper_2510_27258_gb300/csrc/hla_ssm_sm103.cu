@@ -17,15 +17,18 @@
 // C H reads are rounded to bf16 once, they only reach the bf16 output.  w X, which reaches the fp32
 // state, is an exact-to-2^-16 pair hi + lo of bf16, two products.
 //
-// TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H, Y's two parts.  H is
-// kept multiplied by the coming tile's decay, so that B^T w X accumulates onto it.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
+// TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H, and Y twice.  H is kept
+// multiplied by the coming tile's decay, so that B^T w X accumulates onto it; Y is C H, whose rows the
+// epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
 // then hi), and lo, which takes C's place once S and C H are done (its own slot for N <= 64).  The
 // output is staged in X's place.
 //
-// Roles: warp 16 issues copies and MMAs (one thread); warps 0-15 are the epilogue, warp w on TMEM lanes
-// 32 (w % 4) .. (one row each: a token, or a state row) and columns 32 (w / 4) .. .  While the epilogue
-// turns S into W and X into hi, lo and writes a tile's output, the tensor cores run the products handed
-// over before and the next tile's S.
+// Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
+// state row) and columns 32 (w / 4) .. ; warp 16 issues loads and MMAs, warp 17 stores the output (one
+// thread each), warps 18 and 19 compute the next tile's decays, one half's each.  They meet at mbarriers
+// only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
+// W while the tensor cores run B^T w X, puts the new H down while they run W X, and writes the output
+// while they run the next tile's C H.
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
 // each segment's own state, chain_kernel the state before each segment.
@@ -42,8 +45,8 @@ using namespace sm103;
 
 constexpr int kTile = 128;
 constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
-constexpr int kThreads = kEpiThreads + 32;
-constexpr int kStorer = 12 * 32;  // the thread that stores the output (its warp has no part of W)
+constexpr int kIssuerWarp = kEpiWarps, kStoreWarp = kEpiWarps + 1, kStepWarp = kEpiWarps + 2;  // (two of the last)
+constexpr int kStateThreads = kEpiThreads + 32, kThreads = kEpiThreads + 4 * 32;
 // decay of a block (a power of two) down to which its diagonal part is factored, too
 constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -52,8 +55,11 @@ enum Bar {
     bLd0 = 0, bLd1 = 1,                      // C, B, X of a buffer have landed
     bEvS = 2, bEvY2 = 3, bEvY1 = 4, bEvU = 5,  // MMA commits
     bEpE = 6, bEpW = 7, bEpX = 8,            // epilogue hand-offs (16 warp arrivals)
-    bTear = 9,
-    kNumBars = 10
+    bEpY0 = 9, bEpY1 = 10,                   // ... of the output, staged in X's slot of even, odd tiles
+    bXf = 11,                                // the output has left X's slot
+    bStep = 12,                              // a tile's decays are in shared memory (2 warp arrivals)
+    bTear = 13,
+    kNumBars = 14
 };
 
 struct Misc {
@@ -67,6 +73,7 @@ struct Misc {
     // sequence, first head, segment, whether the second 64 columns are a head of this group
     int b, h0, seg, both;
 };
+static_assert(sizeof(Misc) <= 3072, "fits beside the tiles");
 
 // shared-memory map for N <= 64 (kN = 64) and N = 128
 template <int kN>
@@ -82,7 +89,7 @@ struct Map {
 };
 static_assert(Map<128>::kBytes <= 232448 && Map<64>::kBytes <= 232448, "shared memory");
 
-constexpr uint32_t kTS = 0, kTH = 128, kTY1 = 256, kTY2 = 384;  // TMEM columns
+constexpr uint32_t kTS = 0, kTH = 128, kTY = 256;  // TMEM columns; Y of even tiles, then of odd ones
 
 struct Params {
     int n, H, P, G, N, softplus;
@@ -146,14 +153,14 @@ __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t 
     }
 }
 
-// D = A B with A (128 x 128 bf16) in TMEM: K elements 16 kk .. of a row packed in columns a_tmem + 16 kk .. +7
+// D += A B with A (128 x 128 bf16) in TMEM: K elements 16 kk .. of a row packed in columns a_tmem + 16 kk .. +7
 template <int N>
 __device__ __forceinline__ void mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo) {
     constexpr uint32_t id = idesc_bf16(128, N, 0, 1);
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk)
         umma_bf16_ts(d_tmem, a_tmem + 16u * kk,
-                     (static_cast<uint64_t>(kDescHi) << 32) | (b_lo + kk * 128u), id, kk > 0 ? 1u : 0u);
+                     (static_cast<uint64_t>(kDescHi) << 32) | (b_lo + kk * 128u), id, 1u);
 }
 
 // a CTA's 128 columns and its tiles
@@ -256,7 +263,7 @@ __device__ __forceinline__ void epi_arrive(M *ms, int b) {
 }
 
 template <int kN>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kStateThreads, 1)
 ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_b, Params p) {
     using Sm = StateMap<kN>;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -423,7 +430,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     extern __shared__ __align__(1024) uint8_t smem[];
     Misc *ms = reinterpret_cast<Misc *>(smem + Sm::kEnd);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const bool issuer = warp == kEpiWarps;
+    const bool issuer = warp == kIssuerWarp;
 
     const Unit u = unit_of(p);
     const int b = u.b, g = u.g, h0 = u.h0, seg = u.seg, t_lo = u.t_lo, live = u.live, tiles = u.tiles;
@@ -435,7 +442,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpX) ? kEpiWarps : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : i == bStep ? 2 : 1);
         ms->abort_flag = 0;
         ms->b = b; ms->h0 = h0; ms->seg = seg; ms->both = both;
         fence_mbar_init();
@@ -470,11 +477,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, h0, t, b);
                 tma_load_4d(smem + Sm::X(buf) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
             };
-            auto score = [&](int j) {  // S_j = C B^T
-                const int buf = j & 1;
-                mma_ss<false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);
-                umma_commit(&ms->bar[bEvS]);
-            };
             int loaded = 0, landed = 0;  // tiles whose copies were issued / have been waited for
             auto wait_ld = [&](int j) {
                 if (!bar_wait(ms, bLd0 + (j & 1), (j >> 1) & 1, p)) return false;
@@ -483,34 +485,36 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 return true;
             };
             while (loaded < 2 && loaded < tiles) load(loaded++);
-            bool ok = true;
-            if (tiles > 0 && (ok = wait_ld(0))) score(0);
+            bool ok = tiles == 0 || wait_ld(0);
             for (int j = 0; ok && j < tiles; ++j) {
                 const int buf = j & 1, par = j & 1;
-                // H before the tile is in EH and TMEM; the previous tile is read out, its buffers are free
+                // H before the tile is in EH and TMEM
                 if (!(ok = bar_wait(ms, bEpE, par, p))) break;
                 tc_fence_after();
-                mma_ss<false, true, kN / 16>(tb + kTY2, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
+                mma_ss<false, true, kN / 16>(tb + kTY + 128 * buf, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
                 umma_commit(&ms->bar[bEvY2]);
-                if (j > 0 && loaded < tiles) load(loaded++);
-                if (!(ok = bar_wait(ms, bEpW, par, p))) break;
-                tc_fence_after();
-                if (one) {
-                    mma_ts<128>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
-                } else {
-                    mma_ts<64>(tb + kTY1, tb + kTS, lm(Sm::X(buf)));
-                    mma_ts<64>(tb + kTY1 + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
+                mma_ss<false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);  // S = C B^T
+                umma_commit(&ms->bar[bEvS]);
+                if (loaded < tiles && j > 0) {  // the previous tile's products are done and its output has left
+                    if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
+                    load(loaded++);
                 }
-                umma_commit(&ms->bar[bEvY1]);
                 if (!(ok = bar_wait(ms, bEpX, par, p))) break;
                 tc_fence_after();
                 mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::kEH), 1u);  // H += B^T (w X)
                 mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
                 umma_commit(&ms->bar[bEvU]);
-                if (j + 1 < tiles) {
-                    if (!(ok = wait_ld(j + 1))) break;
-                    score(j + 1);
+                if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+                tc_fence_after();
+                const uint32_t y = tb + kTY + 128 * buf;  // Y += W X
+                if (one) {
+                    mma_ts<128>(y, tb + kTS, lm(Sm::X(buf)));
+                } else {
+                    mma_ts<64>(y, tb + kTS, lm(Sm::X(buf)));
+                    mma_ts<64>(y + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
                 }
+                umma_commit(&ms->bar[bEvY1]);
+                if (j + 1 < tiles && !(ok = wait_ld(j + 1))) break;
             }
             if (!ok) {
                 // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
@@ -521,6 +525,73 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             }
         }
         __syncwarp();
+    } else if (warp == kStoreWarp) {
+        if (lane == 0) {
+            for (int j = 0; j < tiles; ++j) {
+                const uint8_t *xs = smem + Sm::X(j & 1);
+                const int t0 = t_lo + j * kTile;
+                if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
+                tma_store_4d(&tm_y, xs, 0, h0, t0, b);
+                if (both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
+                tma_store_commit();
+                tma_store_wait_read();
+                mbar_arrive(&ms->bar[bXf]);
+            }
+            tma_store_wait_all();
+        }
+        __syncwarp();
+    } else if (warp >= kStepWarp) {
+        // steps and decays of a tile's tokens for half e, four consecutive tokens a lane
+        const int e = warp - kStepWarp, head = one || !e || !both ? h0 : h0 + 1;
+        const float da = p.a[head] * kLog2e, bias = p.delta_bias ? p.delta_bias[head] : 0.f;
+        const __nv_bfloat16 *raw = p.delta + ((long long)b * p.n + t_lo + 4 * lane) * p.delta_stride + head;
+        __nv_bfloat16 next[4];
+        auto fetch = [&](int j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                next[i] = t_lo + j * kTile + 4 * lane + i < live ? raw[((long long)j * kTile + i) * p.delta_stride]
+                                                                 : __nv_bfloat16();
+        };
+        fetch(0);
+        for (int j = 0; j < tiles; ++j) {
+            float d[4], up[4], down[4];  // step; decay of the block up to the token, and after it
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = to_f32(next[i]) + bias;
+                const bool in = t_lo + j * kTile + 4 * lane + i < live;
+                d[i] = in ? (p.softplus ? softplus(v) : v) : 0.f;
+                up[i] = in ? da * d[i] : 0.f;
+            }
+            fetch(j + 1);
+            down[3] = 0.f;
+#pragma unroll
+            for (int i = 2; i >= 0; --i) down[i] = down[i + 1] + up[i + 1];
+            float own = down[0] + up[0];  // of the lane's four tokens
+#pragma unroll
+            for (int i = 1; i < 4; ++i) up[i] += up[i - 1];
+            float below = own, above = own;  // inclusive sums over the block's eight lanes
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) {
+                const float x = __shfl_up_sync(0xffffffffu, below, o), z = __shfl_down_sync(0xffffffffu, above, o);
+                if ((lane & 7) >= o) below += x;
+                if ((lane & 7) + o < 8) above += z;
+            }
+            // what the lanes before and after it hold, without this lane's own
+            float first = __shfl_up_sync(0xffffffffu, below, 1), last = __shfl_down_sync(0xffffffffu, above, 1);
+            first = (lane & 7) > 0 ? first : 0.f;
+            last = (lane & 7) < 7 ? last : 0.f;
+            // every epilogue warp has done with the previous tile's decays
+            if (j > 0 && !bar_wait(ms, bEpW, (j - 1) & 1, p)) break;
+            float4 cu, cf;
+            cu = make_float4(first + up[0], first + up[1], first + up[2], first + up[3]);
+            cf = make_float4(ex2(last + down[0]) * d[0], ex2(last + down[1]) * d[1], ex2(last + down[2]) * d[2],
+                             ex2(last + down[3]) * d[3]);
+            *reinterpret_cast<float4 *>(&ms->cum[e][4 * lane]) = cu;
+            *reinterpret_cast<float4 *>(&ms->cf[e][4 * lane]) = cf;
+            if ((lane & 7) == 7) ms->tot[e][lane >> 3] = cu.w;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ms->bar[bStep]);
+        }
     } else {
         // ============================ epilogue ============================
         const int qd = warp & 3, cq = warp >> 2;
@@ -530,18 +601,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const bool srow = kN == 128 || qd < 2;      // this thread's row is a state row
         const int dhead = one || !hs || !both ? h0 : h0 + 1;  // a second head that is not there: the first
         const float skip = p.skip ? p.skip[dhead] : 0.f;
-        const float da = p.a[dhead] * kLog2e, dbias = p.delta_bias ? p.delta_bias[dhead] : 0.f;
-        // the warps of even column quarters compute the tokens' steps (a thread its row's, for its half)
-        const bool stepper = (cq & 1) == 0;
-        const __nv_bfloat16 *raw = p.delta + ((long long)b * p.n + t_lo + r) * p.delta_stride + dhead;
-        int left = stepper ? live - t_lo - r : 0;  // tokens that count, from the next one to fetch on
-        auto fetch = [&]() {
-            __nv_bfloat16 v = left > 0 ? *raw : __nv_bfloat16();
-            raw += kTile * p.delta_stride;
-            left -= kTile;
-            return v;
-        };
-
         // the state rows and columns of this thread within [B, H, segs, N, P]; null where it has none
         auto state_at = [&](float *base, int segs, int seg_i) -> float * {
             const volatile Misc *m = ms;
@@ -579,27 +638,12 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             }
             total = before + ms->tot[hs][qd] + later;
         };
-        // decays of tile j's tokens from their raw steps
-        auto steps = [&](int j, __nv_bfloat16 next_raw) {
-            if (!stepper) return;
-            const bool in = t_lo + j * kTile + r < live;
-            const float v = to_f32(next_raw) + dbias;
-            const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
-            const float la = in ? da * d : 0.f;
-            float up = la, down = la;
-            sums_of(up, down);
-            const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
-            ms->cum[hs][r] = up;
-            ms->cf[hs][r] = ex2(lane < 31 ? after : 0.f) * d;
-            if (lane == 31) ms->tot[hs][qd] = up;
-        };
         // state 0: from state_in or the segment's chained state
         const float *from = p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
                                            : state_at(const_cast<float *>(p.state_in), 1, 0);
         const int cols = p.P - (one ? c0 : (cq & 1) * 32);  // columns of the head from this thread's first one on
         if (tiles > 0) {
-            steps(0, fetch());
-            epi_sync();  // the tile's decays are in shared memory
+            bar_wait(ms, bStep, 0, p);
             decays();
             if (srow) {
                 const float keep = ex2(total);
@@ -655,7 +699,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     if (cq == qd && !(fabsf(own) <= kFactored)) factored = false;
                 }
             }
-            landed(j);
             bar_wait(ms, bEvS, j & 1, p);
             tc_fence_after();
             if (cq > qd) {
@@ -727,56 +770,40 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
             uint8_t *xs = smem + Sm::X(buf);
             const bool in = t0 + r < live;
-            const __nv_bfloat16 next_raw = fetch();  // of the next tile
-            // (a) W
-            weights(j);
+            // (a) w X -> hi (EH), lo
             const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
-            // (b) w X -> hi (EH), lo
-            bar_wait(ms, bEvY2, par, p);  // C H has read EH (and C)
+            landed(j);
+            bar_wait(ms, bEvY2, par, p);  // C H has read EH
+            if (kN == 128) bar_wait(ms, bEvS, par, p);  // (and C B^T has read C, where lo goes)
             tc_fence_after();
             split_row(xs, smem + Sm::kEH, smem + Sm::lo(buf), r, c0, wr);
             fence_async_smem();
             epi_arrive(ms, bEpX);
-            // (c) Y -> bf16 in X's place -> TMA store
-            bar_wait(ms, bEvY1, par, p);
-            tc_fence_after();
-            const uint64_t yf2 = pair(yf, yf), skip2 = pair(skip, skip);
+            // (b) C H times the decay up to each token, and W, while the tensor cores run B^T (w X)
+            const uint32_t y_at = tb + lane_base + kTY + 128 * buf + c0;
+            {
+                const uint64_t yf2 = pair(yf, yf);
 #pragma unroll
-            for (int c = 0; c < 32; c += 16) {
-                uint32_t y1[16], y2[16], o[8];
-                tmem_ld16(tb + lane_base + kTY1 + c0 + c, y1);
-                tmem_ld16(tb + lane_base + kTY2 + c0 + c, y2);
-                uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
-                uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
-                const uint4 u0 = *at0, u1 = *at1;
-                const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
-                tmem_ld_wait();
+                for (int c = 0; c < 32; c += 16) {
+                    uint32_t y[16];
+                    tmem_ld16(y_at + c, y);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint64_t v = fma2(yf2, pair(y2[2 * e], y2[2 * e + 1]), pair(y1[2 * e], y1[2 * e + 1]));
-                    const uint32_t y = bf16_of(fma2(skip2, of_bf16(x[e]), v));
-                    o[e] = in ? y : 0u;
+                    for (int e = 0; e < 16; e += 2) {
+                        float a, b2;
+                        unpair(mul2(yf2, pair(y[e], y[e + 1])), a, b2);
+                        y[e] = __float_as_uint(a);
+                        y[e + 1] = __float_as_uint(b2);
+                    }
+                    tmem_st16(y_at + c, y);
                 }
-                *at0 = make_uint4(o[0], o[1], o[2], o[3]);
-                *at1 = make_uint4(o[4], o[5], o[6], o[7]);
             }
-            fence_async_smem();
-            tc_fence_before();
-            epi_sync();  // the output is staged; every warp has done with the tile's decays
-            if (tid == kStorer) {
-                const volatile Misc *m = ms;
-                const int h = m->h0, bb = m->b;
-                tma_store_4d(&tm_y, xs, 0, h, t0, bb);
-                if (m->both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h : h + 1, t0, bb);
-                tma_store_commit();
-            }
-            if (j + 1 < tiles) steps(j + 1, next_raw);  // under B^T (w X)
-            epi_sync();  // the next tile's decays are in shared memory
-            // (d) the state after the tile
+            weights(j);
+            // (c) the state after the tile, while they run W X
             bar_wait(ms, bEvU, par, p);
             tc_fence_after();
-            if (tid == kStorer) tma_store_wait_read();  // X's slot may be loaded again
             if (j + 1 < tiles) {
+                bar_wait(ms, bStep, (j + 1) & 1, p);
                 decays();
                 if (srow) {
                     const float keep = ex2(total);
@@ -794,6 +821,29 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 }
                 state_is_put();
             }
+            // (d) Y -> bf16 in X's place -> TMA store
+            bar_wait(ms, bEvY1, par, p);
+            tc_fence_after();
+            const uint64_t skip2 = pair(skip, skip);
+#pragma unroll
+            for (int c = 0; c < 32; c += 16) {
+                uint32_t y[16], o[8];
+                tmem_ld16(y_at + c, y);
+                uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
+                uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
+                const uint4 u0 = *at0, u1 = *at1;
+                const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t v = bf16_of(fma2(skip2, of_bf16(x[e]), pair(y[2 * e], y[2 * e + 1])));
+                    o[e] = in ? v : 0u;
+                }
+                *at0 = make_uint4(o[0], o[1], o[2], o[3]);
+                *at1 = make_uint4(o[4], o[5], o[6], o[7]);
+            }
+            fence_async_smem();
+            epi_arrive(ms, bEpY0 + buf);
         }
 
         const volatile Misc *m = ms;
@@ -825,7 +875,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 *reinterpret_cast<float4 *>(to + o + i) = f;
             }
         }
-        if (tid == kStorer) tma_store_wait_all();
     }
     tc_fence_before();
     __syncthreads();
@@ -942,7 +991,7 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
         auto run = [&](auto kern, uint32_t smem) -> cudaError_t {
             cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e) return e;
-            kern<<<blocks, kThreads, smem, stream>>>(mx, mb, q);
+            kern<<<blocks, kStateThreads, smem, stream>>>(mx, mb, q);
             return cudaGetLastError();
         };
         constexpr uint32_t kMisc = sizeof(StateMisc);
