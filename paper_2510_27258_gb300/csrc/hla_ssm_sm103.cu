@@ -196,10 +196,19 @@ __device__ __forceinline__ void sums_of(float &up, float &down) {
     }
 }
 
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+
 // 32 elements of a row of w X as the bf16 pairs hi + lo, rows and columns as in the X tile (hi may take
-// its place)
+// its place).  With w = wh + wl in bf16 (to 2^-17): hi = x wh rounded, x wh - hi is a bf16 exactly, and
+// lo = x wl + (x wh - hi) rounded, all by fused multiply-adds on the packed elements.
 __device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
-    const uint64_t wr2 = pair(wr, wr), minus = pair(-1.f, -1.f);
+    const uint32_t wh = pack_bf16x2(wr, wr);
+    const float rest = wr - bf16_lo(wh);
+    const uint32_t wl = pack_bf16x2(rest, rest);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t off = tile_off(r, c0 + 8 * i);
@@ -208,9 +217,8 @@ __device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, u
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const uint64_t v = mul2(wr2, of_bf16(x[e]));
-            hi[e] = bf16_of(v);
-            lo[e] = bf16_of(fma2(of_bf16(hi[e]), minus, v));
+            hi[e] = fma_bf16x2(x[e], wh, 0x80008000u);                          // (plus minus zero)
+            lo[e] = fma_bf16x2(x[e], wl, fma_bf16x2(x[e], wh, hi[e] ^ 0x80008000u));
         }
         *reinterpret_cast<uint4 *>(hi_tile + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4 *>(lo_tile + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -610,23 +618,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             return base + ((bh * segs + seg_i) * p.N + r) * p.P + col;
         };
         const uint32_t h_at = tb + lane_base + kTH + c0;
-        // 16 columns of the state: their bf16 copy to EH, and times the coming tile's decay to TMEM
-        auto put_state = [&](const float (&v)[16], int o, float keep) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 8)
-                *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + o + i)) =
-                    make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
-                               pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-            uint32_t u[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i] * keep);
-            tmem_st16(h_at + o, u);
-        };
-        auto state_is_put = [&]() {
-            tmem_st_wait();
-            fence_async_smem();
-            epi_arrive(ms, bEpE);
-        };
         // decay of the tile's blocks before / after this token's, and of the whole tile
         float before = 0.f, later = 0.f, total = 0.f;
         auto decays = [&]() {
@@ -638,6 +629,26 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             }
             total = before + ms->tot[hs][qd] + later;
         };
+        // the state before a tile: its bf16 copy to EH, handed over at once, and times the tile's decay to
+        // TMEM, which is read only after the hand-over of w X
+        auto put_state = [&](float (&v)[32]) {
+            if (srow) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + i)) =
+                        make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                                   pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
+            }
+            fence_async_smem();
+            epi_arrive(ms, bEpE);
+            if (srow) {
+                const float keep = ex2(total);
+                uint32_t u[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i] * keep);
+                tmem_st32(h_at, u);
+            }
+        };
         // state 0: from state_in or the segment's chained state
         const float *from = p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
                                            : state_at(const_cast<float *>(p.state_in), 1, 0);
@@ -645,21 +656,14 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         if (tiles > 0) {
             bar_wait(ms, bStep, 0, p);
             decays();
-            if (srow) {
-                const float keep = ex2(total);
+            float v[32];
 #pragma unroll
-                for (int o = 0; o < 32; o += 16) {
-                    float v[16];
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (from && o + i < cols) f = *reinterpret_cast<const float4 *>(from + o + i);
-                        v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
-                    }
-                    put_state(v, o, keep);
-                }
+            for (int i = 0; i < 32; i += 4) {
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (from && i < cols) f = *reinterpret_cast<const float4 *>(from + i);
+                v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
             }
-            state_is_put();
+            put_state(v);
         }
 
         // waits for tile j's copies; tokens that do not count: zero rows of X and B, whatever was read
@@ -778,6 +782,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             tc_fence_after();
             split_row(xs, smem + Sm::kEH, smem + Sm::lo(buf), r, c0, wr);
             fence_async_smem();
+            tmem_st_wait();  // (H times the tile's decay)
             epi_arrive(ms, bEpX);
             // (b) C H times the decay up to each token, and W, while the tensor cores run B^T (w X)
             const uint32_t y_at = tb + lane_base + kTY + 128 * buf + c0;
@@ -805,21 +810,15 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if (j + 1 < tiles) {
                 bar_wait(ms, bStep, (j + 1) & 1, p);
                 decays();
+                float v[32];
                 if (srow) {
-                    const float keep = ex2(total);
-                    uint32_t u[2][16];
-                    tmem_ld16(h_at, u[0]);
-                    tmem_ld16(h_at + 16, u[1]);
+                    uint32_t u[32];
+                    tmem_ld32(h_at, u);
                     tmem_ld_wait();
 #pragma unroll
-                    for (int o = 0; o < 2; ++o) {
-                        float v[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[o][i]);
-                        put_state(v, 16 * o, keep);
-                    }
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
                 }
-                state_is_put();
+                put_state(v);
             }
             // (d) Y -> bf16 in X's place -> TMA store
             bar_wait(ms, bEvY1, par, p);
@@ -835,9 +834,10 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
                 tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t v = bf16_of(fma2(skip2, of_bf16(x[e]), pair(y[2 * e], y[2 * e + 1])));
-                    o[e] = in ? v : 0u;
+                for (int e = 0; e < 8; ++e) o[e] = bf16_of(fma2(skip2, of_bf16(x[e]), pair(y[2 * e], y[2 * e + 1])));
+                if (t0 + kTile > live && !in) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = 0u;
                 }
                 *at0 = make_uint4(o[0], o[1], o[2], o[3]);
                 *at1 = make_uint4(o[4], o[5], o[6], o[7]);
