@@ -18,7 +18,7 @@
 namespace hla {
 namespace {
 
-constexpr int kThreads = 256, kStrips = kThreads / 32;
+constexpr int kThreads = 128, kStrips = kThreads / 32;
 constexpr int kAhead = 8;  // rows a thread has in flight
 constexpr int kAheadBwd = 4;
 constexpr int kStrip = 4;  // strip lengths are multiples of this
@@ -220,6 +220,7 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
     };
     __shared__ Scratch sm;
     auto &red = sm.red;
+    let_next_begin();
     const Place at = place<V>(g);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kP = (V + 1) / 2;
@@ -331,25 +332,27 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
     }
 }
 
-// dw[c][j] and dbias[c] from `rows` partials [W + 1][C]: 32 entries a block, 8 groups of rows
+// dw[c][j] and dbias[c] from `rows` partials [W + 1][C]: 32 entries a block, a warp for every 16th row
+constexpr int kSumGroups = 16;
 template <int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kSumGroups * 32)
 conv_sum_kernel(const float *__restrict__ partial, int rows, int C, float *__restrict__ dw, float *__restrict__ dbias,
                 WsHeader *header) {
-    __shared__ float red[kStrips][32];
+    __shared__ float red[kSumGroups][32];
+    after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     const size_t width = (size_t)(W + 1) * C;
     float s = 0.f;
     if (i < (int)width)
 #pragma unroll 8
-        for (int r = group; r < rows; r += kStrips) s += partial[(size_t)r * width + i];
+        for (int r = group; r < rows; r += kSumGroups) s += partial[(size_t)r * width + i];
     red[group][lane] = s;
     __syncthreads();
     if (group || i >= (int)width) return;
     s = 0.f;
 #pragma unroll
-    for (int k = 0; k < kStrips; ++k) s += red[k][lane];
+    for (int k = 0; k < kSumGroups; ++k) s += red[k][lane];
     const int j = i / C, c = i % C;
     if (j < W)
         dw[(size_t)c * W + j] = s;
@@ -359,17 +362,19 @@ conv_sum_kernel(const float *__restrict__ partial, int rows, int C, float *__res
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-// Strip length: the one that ends first when kResident blocks an SM run at a time, each costing its
-// strip and about eight tokens more (the rows read twice, the taps, the first loads)
+// Strip length: the one that ends first, by the blocks of the fullest SM (at least kFull, below which
+// they gain nothing from one another's absence), each costing its strip and about eight tokens more
+// (the rows read twice, the taps, the first loads)
 Geom geometry(int B, int n, int C, int V) {
-    const int kResident = V == 1 ? 4 : 2;  // by their registers
+    constexpr long long kFull = 4;
     Geom g{B, n, C, kStrip, ceil_div(C, 32 * V), 1};
     long long best = 0;
     for (int L = kStrip; L <= 128; L += kStrip) {
         const long long tb = n > 0 ? ceil_div(n, (long long)L * kStrips) : 1;
-        const long long waves = ((long long)B * g.cblocks * tb + 152 * kResident - 1) / (152 * kResident);
-        if (L == kStrip || waves * (L + 8) <= best) {
-            best = waves * (L + 8);
+        long long blocks = ((long long)B * g.cblocks * tb + 151) / 152;
+        if (blocks < kFull) blocks = kFull;
+        if (L == kStrip || blocks * (L + 8) <= best) {
+            best = blocks * (L + 8);
             g.L = L;
             g.tblocks = (int)tb;
         }
@@ -419,9 +424,8 @@ cudaError_t backward_as(const ConvBwd &p, cudaStream_t s) {
             p.dout_stride, p.dx_stride, p.lengths, p.partial);
         cudaError_t e = cudaGetLastError();
         if (e) return e;
-        conv_sum_kernel<W()><<<ceil_div((long long)(W() + 1) * p.C, 32), kThreads, 0, s>>>(p.partial, rows, p.C, p.dw,
-                                                                                        p.dbias, p.header);
-        return cudaGetLastError();
+        return launch_after(conv_sum_kernel<W()>, ceil_div((long long)(W() + 1) * p.C, 32), kSumGroups * 32, 0, s,
+                            p.partial, rows, p.C, p.dw, p.dbias, p.header);
     });
 }
 

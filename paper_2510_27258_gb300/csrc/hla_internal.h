@@ -120,6 +120,30 @@ bool hla3_tc_applicable(const Fwd2 &p);
 int hla3_tc_launches(int BH, int n);
 cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 
+// ---------------------------------------------------------------------------
+// Dependent launches inside one entry point: a kernel launched by launch_after may begin while the one
+// before it in the stream ends (its launch and set-up overlap with it), and waits with after_previous()
+// before it reads or writes anything that kernel, or one before it, reads or writes.  The earlier kernel
+// says let_next_begin() once; without it the next one begins when it has ended.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // short causal convolution (hla_conv.cu); strides are row strides in elements
 struct Conv {
     const void *x, *w, *bias;

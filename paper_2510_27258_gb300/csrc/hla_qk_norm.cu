@@ -22,9 +22,9 @@
 namespace hla {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kAhead = 4, kAheadBwd = 2;  // heads whose rows a thread has in flight
-constexpr int kBlocksFwd = 4, kBlocksBwd = 2;  // blocks of an SM at a time
+constexpr int kThreads = 128;
+constexpr int kAhead = 4, kAheadBwd = 4;       // rows a thread has in flight
+constexpr int kBlocksFwd = 8, kBlocksBwd = 5;  // blocks of an SM at a time
 
 // four elements at p: one access, or element by element where rows are not aligned to it
 template <typename T, bool kVec>
@@ -72,6 +72,16 @@ __device__ __forceinline__ Runs runs_of(int sub, int rot) {
     return {{half + i, half + i + (D - rot) / 2}};
 }
 
+// the pairs of two runs
+template <typename T>
+__device__ __forceinline__ void pairs_of(const Raw<T, 4> (&r)[2], uint64_t (&v)[4]) {
+    uint64_t f[2];
+    to_pairs(r[0], f);
+    v[0] = f[0]; v[1] = f[1];
+    to_pairs(r[1], f);
+    v[2] = f[0]; v[3] = f[1];
+}
+
 template <typename T, bool kVec>
 struct Row {
     Raw<T, 4> r[2];
@@ -79,13 +89,7 @@ struct Row {
         r[0] = load4<T, kVec>(p + at.at[0]);
         r[1] = load4<T, kVec>(p + at.at[1]);
     }
-    __device__ __forceinline__ void pairs(uint64_t (&v)[4]) const {
-        uint64_t f[2];
-        to_pairs(r[0], f);
-        v[0] = f[0]; v[1] = f[1];
-        to_pairs(r[1], f);
-        v[2] = f[0]; v[3] = f[1];
-    }
+    __device__ __forceinline__ void pairs(uint64_t (&v)[4]) const { pairs_of<T>(r, v); }
 };
 
 // the other members of the pairs a lane holds
@@ -230,7 +234,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksFwd) qk_norm_forward_kernel(Q
 template <typename T, int D, bool kInter, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(QkNormBwd p, Split sp) {
     constexpr int kLanes = D / 8, kRows = kThreads / kLanes;
-    __shared__ float red[kRows][D];
+    union Scratch {
+        Raw<T, 4> ring[2][kAheadBwd][kThreads][2];  // rows of dout, rows of x
+        float red[kRows][D];
+    };
+    __shared__ Scratch sm;
+    let_next_begin();
+    auto &ring = sm.ring;
+    auto &red = sm.red;
     const QkNorm &f = p.f;
     const Runs at = runs_of<D, kInter>(threadIdx.x % kLanes, f.rot);
     const unsigned row = blockIdx.x * kRows + threadIdx.x / kLanes, rows = (unsigned)f.B * f.n;  // below 2^31
@@ -259,37 +270,57 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) w2[e] = pair(w[2 * e], w[2 * e + 1]);
         }
-        const size_t step = (size_t)f.n * D, jump = step * per;
+        const size_t step = (size_t)f.n * D;
         x += (size_t)lo * D;
         dx += (size_t)lo * D;
         const T *src = dout + (((size_t)b * f.H + (size_t)lo * per) * f.n + t) * D;
-        Row<T, kVec> xr[kAheadBwd];
-        Row<T, true> gr[kAheadBwd];
-#pragma unroll
-        for (int u = 0; u < kAheadBwd; ++u) {
-            const int k = lo + u < hi ? u : 0;
-            xr[u].load(x + k * D, at);
-            gr[u].load(src + k * jump, at);
-        }
-        int left = hi - lo;
-        while (left > 0) {
-#pragma unroll
-            for (int u = 0; u < kAheadBwd; ++u) {
-                if (left <= 0) break;
-                uint64_t v[4], g[4], m[4];
-                xr[u].pairs(v);
-                gr[u].pairs(g);
-                for (int k = 1; k < per; ++k) {
-                    Row<T, true> r;
-                    r.load(src + k * step, at);
-                    uint64_t more[4];
-                    r.pairs(more);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) g[e] = add2(g[e], more[e]);
+        // the rows of dout in their order (a head's `per` rows are neighbours), and a head's row of x with
+        // its first one
+        const int count = (hi - lo) * per;
+        int sent = 0, h_sent = 0, k_sent = 0;  // rows of dout sent for; the next one's head and place in it
+        const T *x_next = x, *g_next = src;
+        auto send = [&]() {
+            if (sent < count) {
+                Raw<T, 4> *slot = ring[0][sent % kAheadBwd][threadIdx.x];
+                ring_copy<T, 4>(slot, g_next + at.at[0], true);
+                ring_copy<T, 4>(slot + 1, g_next + at.at[1], true);
+                g_next += step;
+                if (k_sent == 0) {
+                    slot = ring[1][h_sent % kAheadBwd][threadIdx.x];
+                    if (kVec) {
+                        ring_copy<T, 4>(slot, x_next + at.at[0], true);
+                        ring_copy<T, 4>(slot + 1, x_next + at.at[1], true);
+                    } else {
+                        slot[0] = load4<T, false>(x_next + at.at[0]);
+                        slot[1] = load4<T, false>(x_next + at.at[1]);
+                    }
+                    x_next += D;
                 }
-                if (left > kAheadBwd) {
-                    xr[u].load(x + (size_t)kAheadBwd * D, at);
-                    gr[u].load(src + kAheadBwd * jump, at);
+                if (++k_sent == per) {
+                    k_sent = 0;
+                    ++h_sent;
+                }
+                ++sent;
+            }
+            ring_commit();
+        };
+#pragma unroll
+        for (int u = 0; u < kAheadBwd; ++u) send();
+        for (int h = 0, i = 0; h < hi - lo; ++h) {
+            {
+                uint64_t v[4], g[4], m[4];
+                for (int k = 0; k < per; ++k, ++i) {
+                    ring_wait<kAheadBwd - 1>();
+                    if (k == 0) pairs_of<T>(ring[1][h % kAheadBwd][threadIdx.x], v);
+                    if (k == 0) {
+                        pairs_of<T>(ring[0][i % kAheadBwd][threadIdx.x], g);
+                    } else {
+                        uint64_t more[4];
+                        pairs_of<T>(ring[0][i % kAheadBwd][threadIdx.x], more);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) g[e] = add2(g[e], more[e]);
+                    }
+                    send();
                 }
                 mates<kInter>(g, m);
                 uint64_t ss2 = pair(0.f, 0.f), dot2 = ss2;
@@ -319,10 +350,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
                     store4<T, kVec>(dx + at.at[0], d[0], d[1]);
                     store4<T, kVec>(dx + at.at[1], d[2], d[3]);
                 }
-                x += D;
                 dx += D;
-                src += jump;
-                --left;
             }
         }
     };
@@ -357,6 +385,7 @@ constexpr int kSumThreads = 1024;
 __global__ void __launch_bounds__(kSumThreads)
 qk_norm_sum_kernel(const float *__restrict__ partial, int rows, int d, float *dwq, float *dwk, WsHeader *header) {
     __shared__ float red[32][33];
+    after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;  // 2 d is a multiple of 32
     float s = 0.f;
@@ -375,17 +404,19 @@ struct Plan {
     Split sp;
 };
 
-// The split of the heads over blocks that ends first when `resident` blocks an SM run at a time, each
-// costing its heads and about four heads' time more (tables, weights, first loads)
+// The split of the heads over blocks that ends first: the blocks of the fullest SM (at least half of
+// what is resident, below which they gain nothing from one another's absence), each costing its heads
+// and about four heads' time more (tables, weights, first loads)
 Plan plan(long long rows, int heads, int per_block, int resident) {
     Plan best{};
     long long least = 0;
     const unsigned gx = (unsigned)((rows + per_block - 1) / per_block);
     for (int groups = 1; groups <= heads && groups <= 64; ++groups) {
         const int hpb = (heads + groups - 1) / groups, gy = (heads + hpb - 1) / hpb;
-        const long long slots = 152LL * resident, waves = ((long long)gx * gy + slots - 1) / slots;
-        if (groups == 1 || waves * (hpb + 4) < least) {
-            least = waves * (hpb + 4);
+        long long blocks = ((long long)gx * gy + 151) / 152;
+        if (blocks < resident / 2) blocks = resident / 2;
+        if (groups == 1 || blocks * (hpb + 4) < least) {
+            least = blocks * (hpb + 4);
             best = {gx, (unsigned)gy, {hpb}};
         }
     }
@@ -418,9 +449,8 @@ cudaError_t backward_as(const QkNormBwd &p, cudaStream_t s) {
         qk_norm_backward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
         cudaError_t e = cudaGetLastError();
         if (e) return e;
-        qk_norm_sum_kernel<<<2 * p.f.d / 32, kSumThreads, 0, s>>>(
-            p.partial, (int)(g.gx * g.gy), p.f.d, p.dwq, p.dwk, p.header);
-        return cudaGetLastError();
+        return launch_after(qk_norm_sum_kernel, 2 * p.f.d / 32, kSumThreads, 0, s, p.partial, (int)(g.gx * g.gy), p.f.d,
+                            p.dwq, p.dwk, p.header);
     });
 }
 

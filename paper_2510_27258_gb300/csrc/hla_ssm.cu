@@ -59,6 +59,8 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
     T *y = static_cast<T *>(p.y) + (size_t)b * p.n * p.y_stride + h * p.P + slice * kCols;
     const float a = p.a[h], bias = p.delta_bias ? p.delta_bias[h] : 0.f, skip = p.skip ? p.skip[h] : 0.f;
 
+    if (kStateOnly) let_next_begin();
+    if (!kStateOnly && segments > 1) after_previous();
     float st[NS];
     const float *from = kStateOnly ? nullptr
                         : segments > 1 ? seg_state + ((size_t)head * segments + seg) * N * p.P
@@ -178,6 +180,8 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
 // replaces each segment's own state (from zero) by the state before the segment
 __global__ void __launch_bounds__(256)
 chain_kernel(const float *state_in, float *seg_state, const float *seg_decay, long long units, int NP, int segments) {
+    let_next_begin();
+    after_previous();
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i >= units) return;
     const size_t head = i / NP, e = i % NP;
@@ -289,8 +293,10 @@ cudaError_t scan_as(const Ssm &p, cudaStream_t s) {
         if (e) return e;
         e = ssm_chain_launch(p.state_in, state, decay, BH, (int)NP, segments, s);
         if (e) return e;
+        return launch_after(scan_kernel<T, N, false>, per * segments, kScanThreads, 0, s, p, segments, seg_len, state,
+                            decay);
     }
-    scan_kernel<T, N, false><<<per * segments, kScanThreads, 0, s>>>(p, segments, seg_len, state, decay);
+    scan_kernel<T, N, false><<<per, kScanThreads, 0, s>>>(p, 1, seg_len, state, decay);
     return cudaGetLastError();
 }
 
@@ -320,8 +326,8 @@ cudaError_t step_of(const Ssm &p, cudaStream_t s) {
 cudaError_t ssm_chain_launch(const float *state_in, float *seg_state, const float *seg_decay, long long heads, int NP,
                              int segments, cudaStream_t s) {
     const long long units = heads * NP;
-    chain_kernel<<<(unsigned)((units + 255) / 256), 256, 0, s>>>(state_in, seg_state, seg_decay, units, NP, segments);
-    return cudaGetLastError();
+    return launch_after(chain_kernel, (unsigned)((units + 255) / 256), 256, 0, s, state_in, seg_state, seg_decay, units,
+                        NP, segments);
 }
 
 size_t ssm_scan_workspace_floats(const Ssm &p) {

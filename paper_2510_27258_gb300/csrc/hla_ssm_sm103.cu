@@ -279,6 +279,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kEpiWarps;
     const Unit u = unit_of(p);
+    let_next_begin();
 
     if (blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
     if (smem_u32(smem) & 1023u) {                          // the tile layout needs 1 KiB alignment
@@ -649,6 +650,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 tmem_st32(h_at, u);
             }
         };
+        if (p.segments > 1) after_previous();  // (nothing is written before this by any role)
         // state 0: from state_in or the segment's chained state
         const float *from = p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
                                            : state_at(const_cast<float *>(p.state_in), 1, 0);
@@ -982,6 +984,7 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     auto launch = [&](auto kern, int blocks, uint32_t smem) -> cudaError_t {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e) return e;
+        if (c.segments > 1) return launch_after(kern, blocks, kThreads, smem, stream, mx, mb, mc, my, q);
         kern<<<blocks, kThreads, smem, stream>>>(mx, mb, mc, my, q);
         return cudaGetLastError();
     };
