@@ -376,6 +376,25 @@ def test_another_stream(hla):
     assert torch.equal(got_c, want_c) and torch.equal(got_y, want_y) and torch.equal(got_q, want_q)
 
 
+def test_rows_beyond_32_bit_offsets(hla):
+    """Row offsets past 2^31 elements: the last rows equal those of a compact copy."""
+    n, C, stride, T = 33000, 64, 1 << 16, torch.bfloat16  # 2.16e9 elements, 4.3 GB
+    wide = torch.zeros(1, n, stride, dtype=T, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(1, n, 3 * C, generator=g, device=DEV).to(T)
+    wide[..., stride - 3 * C:] = x
+    far = wide[..., stride - 3 * C:]
+    w = torch.randn(C, 4, generator=g, device=DEV).to(T)
+    assert torch.equal(hla.hla_conv_forward(far[..., :C], w), hla.hla_conv_forward(x[..., :C].contiguous(), w))
+    for p, q in zip(hla.hla_qk_norm_forward(far[..., :C].unflatten(-1, (1, C)), far[..., C:2 * C].unflatten(-1, (1, C))),
+                    hla.hla_qk_norm_forward(x[..., :C].unflatten(-1, (1, C)), x[..., C:2 * C].unflatten(-1, (1, C)))):
+        assert torch.equal(p, q)
+    heads = lambda t, i: t[..., i * C:(i + 1) * C].unflatten(-1, (1, C))  # noqa: E731
+    a = -torch.ones(1, device=DEV)
+    run = lambda t: hla.hla_ssm_forward(heads(t, 0), t[..., :1], a, heads(t, 1), heads(t, 2))  # noqa: E731
+    assert torch.equal(run(far), run(x))
+
+
 def test_refusals_of_the_binding(hla):
     x = torch.zeros(2, 4, 16, device=DEV)
     w = torch.zeros(16, 4, device=DEV)
