@@ -448,8 +448,9 @@ def _gpu(t):
 
 
 def _on(stream, index):
+    """Handle of the stream to run on: the caller's, or GPU `index`'s current one."""
     if stream is None:
-        return torch.cuda.current_stream(index).cuda_stream
+        return torch._C._cuda_getCurrentRawStream(index)  # current_stream(index).cuda_stream without the object
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
