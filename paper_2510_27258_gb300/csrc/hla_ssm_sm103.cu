@@ -1,5 +1,5 @@
 // Selective state space scan over prompts on the tensor cores (sm_103a): tcgen05 MMAs with TMEM
-// accumulators, TMA tile loads.
+// accumulators, TMA tile loads and stores.
 //
 // With L_t = sum_{u <= t} a delta_u inside a 128-token tile and H the state before it, a tile is
 //   S = C B^T,   W_ts = S_ts exp(L_t - L_s) delta_s  (s <= t, else 0)
@@ -21,11 +21,12 @@
 // multiplied by the coming tile's decay, so that B^T w X accumulates onto it; Y is C H, whose rows the
 // epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
 // then hi), and lo, which takes C's place once S and C H are done (its own slot for N <= 64).  The
-// output goes straight from registers, a row's 64 bytes a thread.
+// output is staged in X's place.
 //
 // Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
-// state row) and columns 32 (w / 4) .. ; warp 16 issues loads and MMAs (one thread), warps 17 and 18
-// compute the next tile's decays, one half's each.  They meet at mbarriers only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
+// state row) and columns 32 (w / 4) .. ; warp 16 issues loads and MMAs, warp 17 stores the output (one
+// thread each), warps 18 and 19 compute the next tile's decays, one half's each.  They meet at mbarriers
+// only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
 // W while the tensor cores run B^T w X, puts the new H down while they run W X, and writes the output
 // while they run the next tile's C H.
 //
@@ -44,8 +45,8 @@ using namespace sm103;
 
 constexpr int kTile = 128;
 constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
-constexpr int kIssuerWarp = kEpiWarps, kStepWarp = kEpiWarps + 1;  // (two of the last)
-constexpr int kStateThreads = kEpiThreads + 32, kThreads = kEpiThreads + 3 * 32;
+constexpr int kIssuerWarp = kEpiWarps, kStoreWarp = kEpiWarps + 1, kStepWarp = kEpiWarps + 2;  // (two of the last)
+constexpr int kStateThreads = kEpiThreads + 32, kThreads = kEpiThreads + 4 * 32;
 // decay of a block (a power of two) down to which its diagonal part is factored, too
 constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -54,10 +55,11 @@ enum Bar {
     bLd0 = 0, bLd1 = 1,                      // C, B, X of a buffer have landed
     bEvS = 2, bEvY2 = 3, bEvY1 = 4, bEvU = 5,  // MMA commits
     bEpE = 6, bEpW = 7, bEpX = 8,            // epilogue hand-offs (16 warp arrivals)
-    bEpY0 = 9, bEpY1 = 10,                   // ... of an even, odd tile's X and Y, read for the output
-    bStep = 11,                              // a tile's decays are in shared memory (2 warp arrivals)
-    bTear = 12,
-    kNumBars = 13
+    bEpY0 = 9, bEpY1 = 10,                   // ... of the output, staged in X's slot of even, odd tiles
+    bXf = 11,                                // the output has left X's slot
+    bStep = 12,                              // a tile's decays are in shared memory (2 warp arrivals)
+    bTear = 13,
+    kNumBars = 14
 };
 
 struct Misc {
@@ -97,7 +99,6 @@ struct Params {
     const __nv_bfloat16 *delta;
     __nv_bfloat16 *y;
     long long y_stride;
-    int wide_y;            // rows of y are 32-byte aligned
     const float *a, *skip, *delta_bias;
     const int *lengths;
     const float *state_in;
@@ -192,18 +193,6 @@ __device__ __forceinline__ void sums_of(float &up, float &down) {
         const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
         if (lane >= o) up += x;
         if (lane + o < 32) down += z;
-    }
-}
-
-// 32 bytes of a row to global memory: whole 32-byte sectors where the rows are aligned to them
-__device__ __forceinline__ void store32(__nv_bfloat16 *p, const uint32_t (&v)[8], int wide) {
-    if (wide) {
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
-                     "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                     : "memory");
-    } else {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<uint4 *>(p + 8) = make_uint4(v[4], v[5], v[6], v[7]);
     }
 }
 
@@ -445,7 +434,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
 template <int kN>
 __global__ void __launch_bounds__(kThreads, 1)
 ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_b,
-              const __grid_constant__ CUtensorMap tm_c, Params p) {
+              const __grid_constant__ CUtensorMap tm_c, const __grid_constant__ CUtensorMap tm_y, Params p) {
     using Sm = Map<kN>;
     extern __shared__ __align__(1024) uint8_t smem[];
     Misc *ms = reinterpret_cast<Misc *>(smem + Sm::kEnd);
@@ -472,7 +461,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         tmem_relinquish();
         if (lane == 0) {
             prefetch_tmap(&tm_x); prefetch_tmap(&tm_b);
-            prefetch_tmap(&tm_c);
+            prefetch_tmap(&tm_c); prefetch_tmap(&tm_y);
         }
     }
     tc_fence_before();
@@ -515,8 +504,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 umma_commit(&ms->bar[bEvY2]);
                 mma_ss<false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);  // S = C B^T
                 umma_commit(&ms->bar[bEvS]);
-                if (loaded < tiles && j > 0) {  // the previous tile's products are done and its output is read out
-                    if (!(ok = bar_wait(ms, bEpY0 + ((j - 1) & 1), ((j - 1) >> 1) & 1, p))) break;
+                if (loaded < tiles && j > 0) {  // the previous tile's products are done and its output has left
+                    if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
                     load(loaded++);
                 }
                 if (!(ok = bar_wait(ms, bEpX, par, p))) break;
@@ -543,6 +532,21 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 umma_commit(&ms->bar[bTear]);
                 mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
             }
+        }
+        __syncwarp();
+    } else if (warp == kStoreWarp) {
+        if (lane == 0) {
+            for (int j = 0; j < tiles; ++j) {
+                const uint8_t *xs = smem + Sm::X(j & 1);
+                const int t0 = t_lo + j * kTile;
+                if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
+                tma_store_4d(&tm_y, xs, 0, h0, t0, b);
+                if (both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
+                tma_store_commit();
+                tma_store_wait_read();
+                mbar_arrive(&ms->bar[bXf]);
+            }
+            tma_store_wait_all();
         }
         __syncwarp();
     } else if (warp >= kStepWarp) {
@@ -771,6 +775,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         for (int j = 0; j < tiles; ++j) {
             const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
             uint8_t *xs = smem + Sm::X(buf);
+            const bool in = t0 + r < live;
             // (a) w X -> hi (EH), lo
             const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
             landed(j);
@@ -820,26 +825,26 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             // (d) Y -> bf16 in X's place -> TMA store
             bar_wait(ms, bEvY1, par, p);
             tc_fence_after();
-            // this thread's part of the row; tokens that do not count, and a half that is no head of the
-            // group, are not stored
-            const volatile Misc *m = ms;
-            const bool store = t0 + r < live && (!hs || m->both);
-            __nv_bfloat16 *out = p.y + ((long long)m->b * p.n + t0 + r) * p.y_stride +
-                                 (m->h0 + (one ? 0 : hs)) * p.P + (one ? c0 : (cq & 1) * 32);
             const uint64_t skip2 = pair(skip, skip);
 #pragma unroll
             for (int c = 0; c < 32; c += 16) {
                 uint32_t y[16], o[8];
                 tmem_ld16(y_at + c, y);
-                const uint4 u0 = *reinterpret_cast<const uint4 *>(xs + tile_off(r, c0 + c));
-                const uint4 u1 = *reinterpret_cast<const uint4 *>(xs + tile_off(r, c0 + c + 8));
+                uint4 *at0 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c));
+                uint4 *at1 = reinterpret_cast<uint4 *>(xs + tile_off(r, c0 + c + 8));
+                const uint4 u0 = *at0, u1 = *at1;
                 const uint32_t x[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
                 tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = bf16_of(fma2(skip2, of_bf16(x[e]), pair(y[2 * e], y[2 * e + 1])));
-                if (store && c < cols) store32(out + c, o, p.wide_y);
+                if (t0 + kTile > live && !in) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = 0u;
+                }
+                *at0 = make_uint4(o[0], o[1], o[2], o[3]);
+                *at1 = make_uint4(o[4], o[5], o[6], o[7]);
             }
-            tc_fence_before();
+            fence_async_smem();
             epi_arrive(ms, bEpY0 + buf);
         }
 
@@ -960,9 +965,9 @@ bool ssm_tc_applicable(const Ssm &p) {
 }
 
 cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
-    CUtensorMap mx, mb, mc;
+    CUtensorMap mx, mb, mc, my;
     if (!make_map(&mx, p.x, p.B, p.n, p.H, p.P, p.x_stride) || !make_map(&mb, p.b, p.B, p.n, p.G, p.N, p.b_stride) ||
-        !make_map(&mc, p.c, p.B, p.n, p.G, p.N, p.c_stride))
+        !make_map(&mc, p.c, p.B, p.n, p.G, p.N, p.c_stride) || !make_map(&my, p.y, p.B, p.n, p.H, p.P, p.y_stride))
         return cudaErrorInvalidValue;
     const Cut c = cut(p);
     Params q{};
@@ -970,7 +975,6 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     q.per_group = c.per_group; q.units = c.units; q.segments = c.segments; q.seg_tiles = c.seg_tiles;
     q.delta_stride = p.delta_stride; q.delta = static_cast<const __nv_bfloat16 *>(p.delta);
     q.y = static_cast<__nv_bfloat16 *>(p.y); q.y_stride = p.y_stride;
-    q.wide_y = rows_aligned(p.y, p.y_stride, 2, 32);
     q.a = p.a; q.skip = p.skip; q.delta_bias = p.delta_bias; q.lengths = p.lengths;
     q.state_in = p.state_in; q.state_out = p.state_out;
     q.seg_state = reinterpret_cast<float *>(p.ws + kWsHeaderBytes);
@@ -980,8 +984,8 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     auto launch = [&](auto kern, int blocks, uint32_t smem) -> cudaError_t {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e) return e;
-        if (c.segments > 1) return launch_after(kern, blocks, kThreads, smem, stream, mx, mb, mc, q);
-        kern<<<blocks, kThreads, smem, stream>>>(mx, mb, mc, q);
+        if (c.segments > 1) return launch_after(kern, blocks, kThreads, smem, stream, mx, mb, mc, my, q);
+        kern<<<blocks, kThreads, smem, stream>>>(mx, mb, mc, my, q);
         return cudaGetLastError();
     };
     const bool wide = p.N == 128;
