@@ -148,7 +148,7 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
                             y[v] = mul2(y[v], pair(s0, s1));
                         }
                     }
-                    store_pairs(dst, y);
+                    store_pairs<T, V>(dst, y);
                     dst += os;
                 }
             }
@@ -200,7 +200,7 @@ conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, co
             y[v] = mul2(y[v], pair(s0, s1));
         }
     }
-    store_pairs(out + b * os + c0, y);
+    store_pairs<T, V>(out + b * os + c0, y);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) *reinterpret_cast<Raw<T, V> *>(st + (size_t)j * C) = row[j + 1];
 }
@@ -300,7 +300,7 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
 #pragma unroll
                                 for (int j = 1; j < W; ++j) d[v] = fma2(wr[j][v], gw[(u + W - j) % W][v], d[v]);
                             }
-                            store_pairs(to, d);
+                            store_pairs<T, V>(to, d);
                             to += ds;
                         }
                     }
@@ -445,10 +445,10 @@ bool wide(const ConvBwd &p, size_t eb, int V) {
 
 }  // namespace
 
-// the larger of what the scalar and the wide variant write
+// the largest of what the variants write
 size_t conv_backward_partial_floats(int B, int n, int C, int width) {
     size_t rows = 0;
-    for (int V : {1, 4}) {
+    for (int V : {1, 2, 4}) {
         const Geom g = geometry(B, n, C, V);
         const size_t r = (size_t)g.tblocks * B;
         if (r > rows) rows = r;
@@ -456,14 +456,17 @@ size_t conv_backward_partial_floats(int B, int n, int C, int width) {
     return rows * (width + 1) * C;
 }
 
-#define HLA_CONV_DISPATCH(FN, P, V16)                                                      \
-    if ((P).dt == HLA_BF16) {                                                              \
-        if (wide(P, 2, V16))                                                               \
-            return (P).silu ? FN<__nv_bfloat16, V16, true>(P, s) : FN<__nv_bfloat16, V16, false>(P, s); \
-        return (P).silu ? FN<__nv_bfloat16, 1, true>(P, s) : FN<__nv_bfloat16, 1, false>(P, s); \
-    }                                                                                      \
-    if (wide(P, 4, 4)) return (P).silu ? FN<float, 4, true>(P, s) : FN<float, 4, false>(P, s); \
-    return (P).silu ? FN<float, 1, true>(P, s) : FN<float, 1, false>(P, s);
+// the widest access of V16 (bf16) or 4 (fp32) channels, 2 or 1
+#define HLA_CONV_WIDTH(FN, T, V, P) ((P).silu ? FN<T, V, true>(P, s) : FN<T, V, false>(P, s))
+#define HLA_CONV_DISPATCH(FN, P, V16)                                  \
+    if ((P).dt == HLA_BF16) {                                          \
+        if (wide(P, 2, V16)) return HLA_CONV_WIDTH(FN, __nv_bfloat16, V16, P); \
+        if (wide(P, 2, 2)) return HLA_CONV_WIDTH(FN, __nv_bfloat16, 2, P);     \
+        return HLA_CONV_WIDTH(FN, __nv_bfloat16, 1, P);                \
+    }                                                                  \
+    if (wide(P, 4, 4)) return HLA_CONV_WIDTH(FN, float, 4, P);         \
+    if (wide(P, 4, 2)) return HLA_CONV_WIDTH(FN, float, 2, P);         \
+    return HLA_CONV_WIDTH(FN, float, 1, P);
 
 cudaError_t conv_forward_launch(const Conv &p, cudaStream_t s) { HLA_CONV_DISPATCH(forward_as, p, 8) }
 cudaError_t conv_step_launch(const Conv &p, cudaStream_t s) { HLA_CONV_DISPATCH(step_as, p, 8) }

@@ -41,7 +41,7 @@ template <typename T, bool kVec>
 __device__ __forceinline__ void store4(T *p, uint64_t a, uint64_t b) {
     if (kVec) {
         const uint64_t f[2] = {a, b};
-        store_pairs(p, f);
+        store_pairs<T, 4>(p, f);
     } else {
         float v[4];
         unpair(a, v[0], v[1]);

@@ -18,6 +18,17 @@ struct VecIo<T, 1> {
 };
 
 template <>
+struct VecIo<float, 2> {
+    static __device__ __forceinline__ void load(const float *p, float (&v)[2]) {
+        const float2 u = *reinterpret_cast<const float2 *>(p);
+        v[0] = u.x; v[1] = u.y;
+    }
+    static __device__ __forceinline__ void store(float *p, const float (&v)[2]) {
+        *reinterpret_cast<float2 *>(p) = make_float2(v[0], v[1]);
+    }
+};
+
+template <>
 struct VecIo<float, 4> {
     static __device__ __forceinline__ void load(const float *p, float (&v)[4]) {
         const float4 u = *reinterpret_cast<const float4 *>(p);
@@ -35,6 +46,17 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
+
+template <>
+struct VecIo<__nv_bfloat16, 2> {
+    static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float (&v)[2]) {
+        const uint32_t u = *reinterpret_cast<const uint32_t *>(p);
+        v[0] = bf16_lo(u); v[1] = bf16_hi(u);
+    }
+    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float (&v)[2]) {
+        *reinterpret_cast<uint32_t *>(p) = bf16_pair(v[0], v[1]);
+    }
+};
 
 template <>
 struct VecIo<__nv_bfloat16, 4> {
@@ -64,6 +86,14 @@ struct VecIo<__nv_bfloat16, 8> {
 template <typename T, int V>
 struct Raw {
     T v[V];
+};
+template <>
+struct Raw<float, 2> {
+    float2 v;
+};
+template <>
+struct Raw<__nv_bfloat16, 2> {
+    uint32_t v;
 };
 template <>
 struct Raw<float, 4> {
@@ -145,6 +175,8 @@ __device__ __forceinline__ uint64_t of_bf16(uint32_t u) { return pair(bf16_lo(u)
 // a row's V elements as (V + 1) / 2 pairs (V = 1: the second half of the pair is zero), and back
 __device__ __forceinline__ void to_pairs(const Raw<float, 1> &r, uint64_t (&f)[1]) { f[0] = pair(r.v[0], 0.f); }
 __device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 1> &r, uint64_t (&f)[1]) { f[0] = pair(to_f32(r.v[0]), 0.f); }
+__device__ __forceinline__ void to_pairs(const Raw<float, 2> &r, uint64_t (&f)[1]) { f[0] = pair(r.v.x, r.v.y); }
+__device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 2> &r, uint64_t (&f)[1]) { f[0] = of_bf16(r.v); }
 __device__ __forceinline__ void to_pairs(const Raw<float, 4> &r, uint64_t (&f)[2]) {
     f[0] = pair(r.v.x, r.v.y);
     f[1] = pair(r.v.z, r.v.w);
@@ -159,23 +191,15 @@ __device__ __forceinline__ void to_pairs(const Raw<__nv_bfloat16, 8> &r, uint64_
     f[2] = of_bf16(r.v.z);
     f[3] = of_bf16(r.v.w);
 }
-__device__ __forceinline__ void store_pairs(float *p, const uint64_t (&f)[1]) {
-    float none;
-    unpair(f[0], *p, none);
-}
-__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[1]) {
-    float v, none;
-    unpair(f[0], v, none);
-    from_f32(p, v);
-}
-__device__ __forceinline__ void store_pairs(float *p, const uint64_t (&f)[2]) {
-    *reinterpret_cast<ulonglong2 *>(p) = make_ulonglong2(f[0], f[1]);
-}
-__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[2]) {
-    *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_of(f[0]), bf16_of(f[1]));
-}
-__device__ __forceinline__ void store_pairs(__nv_bfloat16 *p, const uint64_t (&f)[4]) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(bf16_of(f[0]), bf16_of(f[1]), bf16_of(f[2]), bf16_of(f[3]));
+template <typename T, int V>
+__device__ __forceinline__ void store_pairs(T *p, const uint64_t (&f)[(V + 1) / 2]) {
+    float v[V + 1];
+#pragma unroll
+    for (int i = 0; i < V; i += 2) unpair(f[i / 2], v[i], v[i + 1]);
+    float out[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = v[i];
+    VecIo<T, V>::store(p, out);
 }
 
 // whether a base pointer and a row stride (elements of `eb` bytes) keep every row aligned to `bytes`
