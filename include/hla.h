@@ -418,6 +418,15 @@ hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, con
                            hla_stream_t stream);
 
 /*
+ * hla_ssm_forward_path -- which CUDA path hla_ssm_forward takes for these arguments
+ * on the current device, without launching anything: 1 the tensor-core kernels
+ * (bf16 tokens, rows of x, b, c and y 16-byte aligned: aligned_rows = 1, an sm_103
+ * device), 0 the fp32 kernels, -1 the arguments are not supported.  *launches (if
+ * not NULL) receives the number of kernels the call launches (0 for an empty one).
+ */
+int hla_ssm_forward_path(int B, int n, int H, int P, int G, int N, hla_dtype dt, int aligned_rows, int *launches);
+
+/*
  * hla_ssm_step -- hla_ssm_forward of one token a sequence: x, y [B, H, P], delta
  * [B, H], b, c [B, G, N] with their row strides; state fp32 [B, H, N, P], updated
  * in place.  y may equal x.  No workspace.

@@ -185,6 +185,7 @@ struct Ssm {
     char *ws;          // workspace base (header included)
 };
 size_t ssm_scan_workspace_floats(const Ssm &p);
+int ssm_scan_launches(const Ssm &p);
 cudaError_t ssm_scan_launch(const Ssm &p, cudaStream_t stream);
 cudaError_t ssm_step_launch(const Ssm &p, cudaStream_t stream);
 // replaces each segment's own state by the state before it (`heads` x `segments` x NP floats)
@@ -192,6 +193,7 @@ cudaError_t ssm_chain_launch(const float *state_in, float *seg_state, const floa
                              int segments, cudaStream_t stream);
 // the scan on the tensor cores (hla_ssm_sm103.cu): bf16, 16-byte aligned rows
 size_t ssm_tc_workspace_floats(const Ssm &p);
+int ssm_tc_launches(const Ssm &p);
 bool ssm_tc_applicable(const Ssm &p);
 cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream);
 

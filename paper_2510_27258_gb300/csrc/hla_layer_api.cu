@@ -201,6 +201,19 @@ size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dty
     return scratch_bytes(scan > tc ? scan : tc);
 }
 
+int hla_ssm_forward_path(int B, int n, int H, int P, int G, int N, hla_dtype dt, int aligned_rows, int *launches) {
+    if (launches) *launches = 0;
+    if (hla_ssm_workspace_bytes(B, n, H, P, G, N, dt) == 0 || n > (1 << 30)) return -1;
+    Ssm p{};
+    p.dt = dt; p.B = B; p.n = n; p.H = H; p.P = P; p.G = G; p.N = N;
+    p.x = p.b = p.c = reinterpret_cast<const void *>(uintptr_t(aligned_rows ? 256 : 2));
+    p.y = reinterpret_cast<void *>(uintptr_t(256));
+    if (B == 0 || n == 0) return 0;
+    const bool tc = ssm_tc_applicable(p);
+    if (launches) *launches = tc ? ssm_tc_launches(p) : ssm_scan_launches(p);
+    return tc ? 1 : 0;
+}
+
 hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, const void *b, const void *c,
                            const float *skip, const float *delta_bias, void *y, hla_dtype dt, int B, int n, int H,
                            int P, int G, int N, long long x_stride, long long delta_stride, long long b_stride,

@@ -335,6 +335,8 @@ size_t ssm_scan_workspace_floats(const Ssm &p) {
     return s > 1 ? (size_t)(BH * s * ((long long)p.N * p.P + 1)) : 0;
 }
 
+int ssm_scan_launches(const Ssm &p) { return segments_of(p) > 1 ? 3 : 1; }
+
 cudaError_t ssm_scan_launch(const Ssm &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? scan_of<__nv_bfloat16>(p, s) : scan_of<float>(p, s);
 }

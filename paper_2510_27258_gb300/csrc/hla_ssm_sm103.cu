@@ -951,6 +951,8 @@ size_t ssm_tc_workspace_floats(const Ssm &p) {
     return c.segments > 1 ? (size_t)p.B * p.H * c.segments * ((size_t)p.N * p.P + 1) : 0;
 }
 
+int ssm_tc_launches(const Ssm &p) { return cut(p).segments > 1 ? 3 : 1; }
+
 bool ssm_tc_applicable(const Ssm &p) {
     if (getenv("HLA_DISABLE_FUSED")) return false;
     if (p.dt != HLA_BF16 || p.n <= 0 || p.B <= 0) return false;

@@ -27,7 +27,7 @@ EXPORTS = ("hla_status_string", "hla_last_error", "hla2_state_floats", "hla2_wor
            "hla2_state_to_sde", "hla2_step_sde", "ahla_state_floats", "ahla_workspace_bytes", "ahla_forward",
            "ahla_step", "hla2_backward_workspace_bytes", "hla2_backward", "ahla_forward_path",
            "hla_conv_forward", "hla_conv_step", "hla_conv_backward_workspace_bytes", "hla_conv_backward",
-           "hla_ssm_workspace_bytes", "hla_ssm_forward", "hla_ssm_step", "hla_qk_norm_forward",
+           "hla_ssm_workspace_bytes", "hla_ssm_forward", "hla_ssm_forward_path", "hla_ssm_step", "hla_qk_norm_forward",
            "hla_qk_norm_backward_workspace_bytes", "hla_qk_norm_backward")
 
 _lib = None
@@ -103,6 +103,8 @@ def lib():
         L.hla_qk_norm_forward.argtypes = [vp] * 9 + [i] * 8 + [ll, ll, i, i, f, vp]
         L.hla_qk_norm_backward_workspace_bytes.argtypes = [i] * 6
         L.hla_qk_norm_backward.argtypes = [vp] * 13 + [i] * 8 + [ll] * 4 + [i, i, f, vp, sz, vp]
+        L.hla_ssm_forward_path.argtypes = [i] * 8 + [ctypes.POINTER(i)]
+        L.hla_ssm_forward_path.restype = i
         for name in ("hla_conv_backward_workspace_bytes", "hla_ssm_workspace_bytes",
                      "hla_qk_norm_backward_workspace_bytes"):
             getattr(L, name).restype = sz
@@ -555,6 +557,13 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
         1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, f32, i),
         _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, _on(stream, i)), "hla_ssm_forward")
     return out
+
+
+def hla_ssm_forward_path(B, n, H, P, G, N, *, dtype=torch.bfloat16, aligned_rows=True):
+    """(path, launches) that hla_ssm_forward takes: path 1 = tensor-core kernels, 0 = fp32 kernels, -1 = unsupported."""
+    launches = ctypes.c_int(0)
+    path = lib().hla_ssm_forward_path(B, n, H, P, G, N, _type_code(dtype), int(aligned_rows), ctypes.byref(launches))
+    return int(path), int(launches.value)
 
 
 def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=None, softplus=True, stream=None):

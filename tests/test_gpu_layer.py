@@ -269,6 +269,13 @@ def test_ssm_prompt_in_two_parts(hla):
     near(st, h, 3 * bh)
 
 
+def test_ssm_path(hla):
+    assert hla.hla_ssm_forward_path(8, 2048, 32, 64, 1, 128) == (1, 1)
+    assert hla.hla_ssm_forward_path(1, 32768, 16, 64, 2, 64) == (1, 3)  # few heads: cut along the sequence
+    assert hla.hla_ssm_forward_path(8, 2048, 32, 64, 1, 128, dtype=torch.float32)[0] == 0
+    assert hla.hla_ssm_forward_path(8, 2048, 32, 64, 1, 128, aligned_rows=False)[0] == 0
+
+
 def test_ssm_empty_prompt(hla):
     B, H, P, G, N = 2, 2, 32, 1, 16
     z = lambda *s: torch.empty(*s, device=DEV)  # noqa: E731
@@ -374,6 +381,40 @@ def test_another_stream(hla):
     got_q = hla.hla_qk_norm_forward(late, late, stream=s)[0]
     s.synchronize()
     assert torch.equal(got_c, want_c) and torch.equal(got_y, want_y) and torch.equal(got_q, want_q)
+
+
+def test_in_a_cuda_graph(hla):
+    """Every operator captured once and replayed on new inputs equals direct calls."""
+    T, (B, n, H, P, N) = torch.bfloat16, (1, 700, 4, 64, 64)
+    x, delta, a, b, c, skip, bias, _, _ = (None if t is None else t.to(DEV) for t in
+                                           ssm_case(21, B, n, H, P, 1, N, T, False))
+    w = torch.randn(H * P, 4, device=DEV).to(T)
+    ws = [torch.empty(1 << 22, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    state = torch.empty(B, H, N, P, device=DEV)
+
+    def run():
+        y = hla.hla_conv_forward(x.flatten(2), w)
+        z = hla.hla_ssm_forward(y.unflatten(-1, (H, P)), delta, a, b, c, state_out=state, workspace=ws[0])
+        q, k = hla.hla_qk_norm_forward(z, z)
+        dq, dk, _, _ = hla.hla_qk_norm_backward(z, z, None, None, None, None, q, k, workspace=ws[1])
+        return (z, q, k, dq, dk, state) + hla.hla_conv_backward(x.flatten(2), w, dq.flatten(2), workspace=ws[2])[:2]
+
+    assert hla.hla_ssm_workspace_bytes(B, n, H, P, 1, N, T) <= ws[0].numel()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for seed in (1, 2):
+        x.copy_(torch.randn(x.shape, generator=gen(seed)).to(T))
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in got]
+        for p, q in zip(kept, run()):
+            assert torch.equal(p, q)
 
 
 def test_rows_beyond_32_bit_offsets(hla):

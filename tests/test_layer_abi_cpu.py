@@ -78,6 +78,13 @@ def test_ssm_forward_refuses(L, E):
     assert L.hla_ssm_workspace_bytes(1, 1 << 16, 4, 32, 2, 16, 0) > L.hla_ssm_workspace_bytes(1, 8, 4, 32, 2, 16, 0) > 0
 
 
+def test_ssm_path_without_a_device(L, E):
+    assert E.hla_ssm_forward_path(8, 2048, 32, 64, 1, 128) == (0, 1)  # no device here: the fp32 kernels
+    assert E.hla_ssm_forward_path(1, 2048, 4, 64, 1, 128, dtype=torch.float32) == (0, 3)  # few heads: segments
+    assert E.hla_ssm_forward_path(0, 2048, 4, 64, 1, 128) == (0, 0)
+    assert E.hla_ssm_forward_path(1, 2048, 4, 48, 1, 128) == (-1, 0)
+
+
 def test_ssm_step_refuses(L, E):
     def step(state=256, P=32, xs=128, delta=256):
         return L.hla_ssm_step(256, delta, 256, 256, 256, None, None, 256, 1, 2, 4, P, 2, 16, xs, 4, 32, 32, 128, 1, state,
