@@ -53,20 +53,14 @@ __device__ __forceinline__ float fast_exp2(float x) {
     return r;
 }
 
-// sigmoids of a pair.  exp(-v) is kept below 2^63 (v above -43.6, where v sigmoid(v) has come down to
-// 5e-18), so that two values can share one reciprocal: the multi-function unit takes 1.5 operations
-// a value instead of 2.  v itself is replaced by the kept value; NaN stays NaN.
-__device__ __forceinline__ void sigmoids(uint64_t &v, float &s0, float &s1) {
-    float v0, v1, e0, e1, r;
-    unpair(v, v0, v1);
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v0) : "f"(v0), "f"(-43.6f));
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(v1) : "f"(v1), "f"(-43.6f));
-    v = pair(v0, v1);
+// sigmoids of a pair, 1 / (1 + 2^(-v log2 e)).  (exp(-v) may overflow: the reciprocal is then 0.)
+__device__ __forceinline__ uint64_t sigmoids(uint64_t v) {
+    float e0, e1, s0, s1;
     unpair(mul2(v, pair(-1.4426950408889634f, -1.4426950408889634f)), e0, e1);
     unpair(add2(pair(fast_exp2(e0), fast_exp2(e1)), pair(1.f, 1.f)), e0, e1);
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e0 * e1));
-    s0 = r * e1;
-    s1 = r * e0;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s0) : "f"(e0));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s1) : "f"(e1));
+    return pair(s0, s1);
 }
 
 // w[c0 .. c0 + V - 1][W] and bias[c0 ..] as pairs of channels
@@ -142,11 +136,7 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
                         y[v] = br[v];
 #pragma unroll
                         for (int j = 0; j < W; ++j) y[v] = fma2(wr[j][v], win[(u + 1 + j) % W][v], y[v]);
-                        if (kSilu) {
-                            float s0, s1;
-                            sigmoids(y[v], s0, s1);
-                            y[v] = mul2(y[v], pair(s0, s1));
-                        }
+                        if (kSilu) y[v] = mul2(y[v], sigmoids(y[v]));
                     }
                     store_pairs<T, V>(dst, y);
                     dst += os;
@@ -194,11 +184,7 @@ conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, co
     }
     if (kSilu) {
 #pragma unroll
-        for (int v = 0; v < kP; ++v) {
-            float s0, s1;
-            sigmoids(y[v], s0, s1);
-            y[v] = mul2(y[v], pair(s0, s1));
-        }
+        for (int v = 0; v < kP; ++v) y[v] = mul2(y[v], sigmoids(y[v]));
     }
     store_pairs<T, V>(out + b * os + c0, y);
 #pragma unroll
@@ -274,9 +260,7 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
                                 uint64_t a = br[v];
 #pragma unroll
                                 for (int j = 0; j < W; ++j) a = fma2(wr[j][v], xw[(u + 1 + j) % W][v], a);
-                                float s0, s1;
-                                sigmoids(a, s0, s1);
-                                const uint64_t s = pair(s0, s1), one = pair(1.f, 1.f);
+                                const uint64_t s = sigmoids(a), one = pair(1.f, 1.f);
                                 gc[v] = mul2(mul2(gc[v], s), fma2(a, fma2(s, pair(-1.f, -1.f), one), one));
                             }
                         }

@@ -46,7 +46,7 @@ using namespace sm103;
 constexpr int kTile = 128;
 constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
 constexpr int kIssuerWarp = kEpiWarps, kStoreWarp = kEpiWarps + 1, kStepWarp = kEpiWarps + 2;  // (two of the last)
-constexpr int kStateThreads = kEpiThreads + 32, kThreads = kEpiThreads + 4 * 32;
+constexpr int kStateThreads = kEpiThreads + 3 * 32, kStateStepWarp = kEpiWarps + 1, kThreads = kEpiThreads + 4 * 32;
 // decay of a block (a power of two) down to which its diagonal part is factored, too
 constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -116,8 +116,6 @@ __device__ __forceinline__ void set_error(WsHeader *err, unsigned where, unsigne
     }
 }
 
-__device__ __forceinline__ void epi_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory"); }
-
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -185,17 +183,6 @@ __device__ __forceinline__ Unit unit_of(const Params &p) {
     return u;
 }
 
-// inclusive sums of a warp's values up to and down from each lane's
-__device__ __forceinline__ void sums_of(float &up, float &down) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const float x = __shfl_up_sync(0xffffffffu, up, o), z = __shfl_down_sync(0xffffffffu, down, o);
-        if (lane >= o) up += x;
-        if (lane + o < 32) down += z;
-    }
-}
-
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
@@ -249,9 +236,48 @@ struct StateMisc {
 static_assert(StateMap<64>::kEnd + sizeof(StateMisc) <= 232448 && StateMap<128>::kEnd + sizeof(StateMisc) <= 232448,
               "shared memory");
 
-// (the products of even and odd tiles commit to barriers of their own: a wait may come after the next
-// tile's commit, which would turn a shared barrier's parity)
-enum StateBar { sLd0 = 0, sEvU0 = 3, sEvU1 = 4, sEpX = 5, sTear = 6 };  // sLd0 + stage
+// Each of these may complete for the next tile before the last thread has waited for this one's, but not
+// for the one after it: even and odd tiles have barriers of their own.
+enum StateBar {
+    sLd0 = 0,               // + stage: B, X have landed
+    sEvU0 = 3, sEvU1 = 4,   // the products are done
+    sEpX0 = 5, sEpX1 = 6,   // hi, lo are there (16 warp arrivals)
+    sStep0 = 7, sStep1 = 8, // a tile's decays are (2 warp arrivals)
+    sTear = 9
+};
+
+// Steps and decays of a tile's tokens for one head: four consecutive tokens a lane, whose raw steps are
+// `raw`; eight lanes hold a 32-token block.  up: decay of the block up to each token; cf: step times the
+// decay from the token to the block's end.
+__device__ __forceinline__ void block_decays(const __nv_bfloat16 (&raw)[4], int count, float da, float bias, int softplus_on,
+                                             float4 &up4, float4 &cf4) {
+    const int lane8 = threadIdx.x & 7;
+    float d[4], up[4], down[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // the first `count` of the four tokens count
+        const float v = to_f32(raw[i]) + bias;
+        d[i] = i < count ? (softplus_on ? softplus(v) : v) : 0.f;
+        up[i] = i < count ? da * d[i] : 0.f;
+    }
+    down[3] = 0.f;
+#pragma unroll
+    for (int i = 2; i >= 0; --i) down[i] = down[i + 1] + up[i + 1];
+    float below = down[0] + up[0], above = below;  // of the lane's four; then inclusive over the block's lanes
+#pragma unroll
+    for (int i = 1; i < 4; ++i) up[i] += up[i - 1];
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+        const float x = __shfl_up_sync(0xffffffffu, below, o), z = __shfl_down_sync(0xffffffffu, above, o);
+        if (lane8 >= o) below += x;
+        if (lane8 + o < 8) above += z;
+    }
+    float first = __shfl_up_sync(0xffffffffu, below, 1), last = __shfl_down_sync(0xffffffffu, above, 1);
+    first = lane8 > 0 ? first : 0.f;  // what the lanes before and after it hold
+    last = lane8 < 7 ? last : 0.f;
+    up4 = make_float4(first + up[0], first + up[1], first + up[2], first + up[3]);
+    cf4 = make_float4(ex2(last + down[0]) * d[0], ex2(last + down[1]) * d[1], ex2(last + down[2]) * d[2],
+                      ex2(last + down[3]) * d[3]);
+}
 
 template <typename M>
 __device__ __forceinline__ bool bar_wait(M *ms, int b, uint32_t parity, const Params &p) {
@@ -287,7 +313,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], i == sEpX ? kEpiWarps : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], i == sEpX0 || i == sEpX1 ? kEpiWarps : i == sStep0 || i == sStep1 ? 2 : 1);
         ms->abort_flag = 0;
         fence_mbar_init();
     }
@@ -325,7 +351,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                 const int st = j % Sm::kStages;
                 if (!(ok = bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p))) break;
                 landed = j + 1;
-                if (!(ok = bar_wait(ms, sEpX, j & 1, p))) break;
+                if (!(ok = bar_wait(ms, sEpX0 + (j & 1), (j >> 1) & 1, p))) break;
                 tc_fence_after();
                 mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::X(st)), j > 0 ? 1u : 0u);
                 mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::Lo(j)), 1u);
@@ -345,33 +371,38 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             }
         }
         __syncwarp();
+    } else if (warp >= kStateStepWarp) {
+        // the decays of half e
+        const int e = warp - kStateStepWarp, head = u.one || !e || !u.both ? u.h0 : u.h0 + 1;
+        const float da = p.a[head] * kLog2e, bias = p.delta_bias ? p.delta_bias[head] : 0.f;
+        const __nv_bfloat16 *from = p.delta + (long long)u.b * p.n * p.delta_stride + head;
+        __nv_bfloat16 raw[4];
+        auto fetch = [&](int j) {
+            const int t = u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                raw[i] = t >= u.t_lo && t + i < u.live ? from[(long long)(t + i) * p.delta_stride] : __nv_bfloat16();
+        };
+        fetch(0);
+        for (int j = 0; j < u.tiles; ++j) {
+            float4 up, cf;
+            block_decays(raw, u.live - (u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane), da, bias, p.softplus, up, cf);
+            fetch(j + 1);
+            // every epilogue warp has done with the decays that were here
+            if (j >= 2 && !bar_wait(ms, sEpX0 + (j & 1), ((j - 2) >> 1) & 1, p)) break;
+            *reinterpret_cast<float4 *>(&ms->cf[j & 1][e][4 * lane]) = cf;
+            if ((lane & 7) == 7) ms->tot[j & 1][e][lane >> 3] = up.w;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ms->bar[sStep0 + (j & 1)]);
+        }
     } else {
         const int qd = warp & 3, cq = warp >> 2, r = 32 * qd + lane, c0 = 32 * cq, hs = cq >> 1;
         const int head = u.one || !hs || !u.both ? u.h0 : u.h0 + 1;  // a second head that is not there: the first
-        const float da = p.a[head] * kLog2e, dbias = p.delta_bias ? p.delta_bias[head] : 0.f;
-        const bool stepper = (cq & 1) == 0;
-        const __nv_bfloat16 *raw = p.delta + (long long)u.b * p.n * p.delta_stride + head;
-        auto fetch = [&](int j) {
-            const int t = u.t_lo + (u.tiles - 1 - j) * kTile + r;
-            return stepper && t >= u.t_lo && t < u.live ? raw[(long long)t * p.delta_stride] : __nv_bfloat16();
-        };
         float run = 0.f;  // decay of the tiles taken so far (a power of two)
-        __nv_bfloat16 now = fetch(0);
         for (int j = 0; j < u.tiles; ++j) {
             const int buf = j & 1, t0 = u.t_lo + (u.tiles - 1 - j) * kTile;
             const bool in = t0 + r < u.live;
-            const __nv_bfloat16 next = fetch(j + 1);
-            if (stepper) {
-                const float v = to_f32(now) + dbias;
-                const float d = in ? (p.softplus ? softplus(v) : v) : 0.f;
-                float up = in ? da * d : 0.f, down = up;
-                sums_of(up, down);
-                const float after = __shfl_down_sync(0xffffffffu, down, 1);  // decay of the block's later tokens
-                ms->cf[buf][hs][r] = ex2(lane < 31 ? after : 0.f) * d;
-                if (lane == 31) ms->tot[buf][hs][qd] = up;
-            }
-            now = next;
-            epi_sync();
+            bar_wait(ms, sStep0 + buf, (j >> 1) & 1, p);
             float later = run;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -397,7 +428,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             }
             split_row(xs, xs, smem + Sm::Lo(j), r, c0, wr);
             fence_async_smem();
-            epi_arrive(ms, sEpX);
+            epi_arrive(ms, sEpX0 + buf);
         }
         if (u.tiles > 0) {
             const int i = u.tiles - 1;
@@ -563,41 +594,14 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         };
         fetch(0);
         for (int j = 0; j < tiles; ++j) {
-            float d[4], up[4], down[4];  // step; decay of the block up to the token, and after it
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float v = to_f32(next[i]) + bias;
-                const bool in = t_lo + j * kTile + 4 * lane + i < live;
-                d[i] = in ? (p.softplus ? softplus(v) : v) : 0.f;
-                up[i] = in ? da * d[i] : 0.f;
-            }
+            float4 up, cf;
+            block_decays(next, live - (t_lo + j * kTile + 4 * lane), da, bias, p.softplus, up, cf);
             fetch(j + 1);
-            down[3] = 0.f;
-#pragma unroll
-            for (int i = 2; i >= 0; --i) down[i] = down[i + 1] + up[i + 1];
-            float own = down[0] + up[0];  // of the lane's four tokens
-#pragma unroll
-            for (int i = 1; i < 4; ++i) up[i] += up[i - 1];
-            float below = own, above = own;  // inclusive sums over the block's eight lanes
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) {
-                const float x = __shfl_up_sync(0xffffffffu, below, o), z = __shfl_down_sync(0xffffffffu, above, o);
-                if ((lane & 7) >= o) below += x;
-                if ((lane & 7) + o < 8) above += z;
-            }
-            // what the lanes before and after it hold, without this lane's own
-            float first = __shfl_up_sync(0xffffffffu, below, 1), last = __shfl_down_sync(0xffffffffu, above, 1);
-            first = (lane & 7) > 0 ? first : 0.f;
-            last = (lane & 7) < 7 ? last : 0.f;
             // every epilogue warp has done with the previous tile's decays
             if (j > 0 && !bar_wait(ms, bEpW, (j - 1) & 1, p)) break;
-            float4 cu, cf;
-            cu = make_float4(first + up[0], first + up[1], first + up[2], first + up[3]);
-            cf = make_float4(ex2(last + down[0]) * d[0], ex2(last + down[1]) * d[1], ex2(last + down[2]) * d[2],
-                             ex2(last + down[3]) * d[3]);
-            *reinterpret_cast<float4 *>(&ms->cum[e][4 * lane]) = cu;
+            *reinterpret_cast<float4 *>(&ms->cum[e][4 * lane]) = up;
             *reinterpret_cast<float4 *>(&ms->cf[e][4 * lane]) = cf;
-            if ((lane & 7) == 7) ms->tot[e][lane >> 3] = cu.w;
+            if ((lane & 7) == 7) ms->tot[e][lane >> 3] = up.w;
             __syncwarp();
             if (lane == 0) mbar_arrive(&ms->bar[bStep]);
         }
