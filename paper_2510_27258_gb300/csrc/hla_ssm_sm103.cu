@@ -46,7 +46,8 @@ using namespace sm103;
 constexpr int kTile = 128;
 constexpr int kEpiWarps = 16, kEpiThreads = kEpiWarps * 32;
 constexpr int kIssuerWarp = kEpiWarps, kStoreWarp = kEpiWarps + 1, kStepWarp = kEpiWarps + 2;  // (two of the last)
-constexpr int kStateThreads = kEpiThreads + 3 * 32, kStateStepWarp = kEpiWarps + 1, kThreads = kEpiThreads + 4 * 32;
+constexpr int kStateThreads = kEpiThreads + 4 * 32, kStateLoadWarp = kEpiWarps + 1, kStateStepWarp = kEpiWarps + 2;
+constexpr int kThreads = kEpiThreads + 4 * 32;
 // decay of a block (a power of two) down to which its diagonal part is factored, too
 constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -236,14 +237,14 @@ struct StateMisc {
 static_assert(StateMap<64>::kEnd + sizeof(StateMisc) <= 232448 && StateMap<128>::kEnd + sizeof(StateMisc) <= 232448,
               "shared memory");
 
-// Each of these may complete for the next tile before the last thread has waited for this one's, but not
-// for the one after it: even and odd tiles have barriers of their own.
+// Each of these may complete for later tiles before the last thread has waited for an earlier one's, so a
+// barrier serves every second or third tile only: its next completion needs that thread's own next step.
 enum StateBar {
-    sLd0 = 0,               // + stage: B, X have landed
-    sEvU0 = 3, sEvU1 = 4,   // the products are done
-    sEpX0 = 5, sEpX1 = 6,   // hi, lo are there (16 warp arrivals)
-    sStep0 = 7, sStep1 = 8, // a tile's decays are (2 warp arrivals)
-    sTear = 9
+    sLd0 = 0,                // + stage: B, X have landed
+    sEvU0 = 3,               // + stage: the products are done
+    sEpX0 = 6, sEpX1 = 7,    // hi, lo of even, odd tiles are there (16 warp arrivals)
+    sStep0 = 8, sStep1 = 9,  // their decays are (2 warp arrivals)
+    sTear = 10
 };
 
 // Steps and decays of a tile's tokens for one head: four consecutive tokens a lane, whose raw steps are
@@ -334,41 +335,40 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         if (lane == 0) {
             const uint32_t sb4 = smem_u32(smem) >> 4;
             auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
-            auto load = [&](int j) {  // the j-th tile from the end
-                const int buf = j % Sm::kStages, t = u.t_lo + (u.tiles - 1 - j) * kTile;
-                uint64_t *bar = &ms->bar[sLd0 + buf];
-                mbar_arrive_expect_tx(bar, kTileBytes + Sm::kOperand);
-                for (int i = 0; i < kN / 64; ++i)
-                    tma_load_4d(smem + Sm::B(buf) + i * kBlockBytes, &tm_b, bar, 64 * i, u.g, t, u.b);
-                tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, u.h0, t, u.b);
-                tma_load_4d(smem + Sm::X(buf) + kBlockBytes, &tm_x, bar, u.one ? 64 : 0,
-                            u.one || !u.both ? u.h0 : u.h0 + 1, t, u.b);
-            };
-            int loaded = 0, landed = 0;
-            while (loaded < Sm::kStages && loaded < u.tiles) load(loaded++);
             bool ok = true;
             for (int j = 0; j < u.tiles; ++j) {
                 const int st = j % Sm::kStages;
                 if (!(ok = bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p))) break;
-                landed = j + 1;
                 if (!(ok = bar_wait(ms, sEpX0 + (j & 1), (j >> 1) & 1, p))) break;
                 tc_fence_after();
                 mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::X(st)), j > 0 ? 1u : 0u);
                 mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::Lo(j)), 1u);
-                umma_commit(&ms->bar[sEvU0 + (j & 1)]);
-                if (j > 0 && loaded < u.tiles) {  // the previous tile's products are done: its stage is free
-                    if (!(ok = bar_wait(ms, sEvU0 + ((j - 1) & 1), ((j - 1) >> 1) & 1, p))) break;
-                    load(loaded++);
-                }
+                umma_commit(&ms->bar[sEvU0 + st]);
             }
-            if (!ok) {
-                // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
-                // TMEM are released
-                for (int j = landed; j < loaded; ++j)
-                    mbar_wait(&ms->bar[sLd0 + j % Sm::kStages], (j / Sm::kStages) & 1, kBarWaitNs);
+            if (!ok) {  // a wait gave up: MMAs in flight finish (bounded) before TMEM is released
                 umma_commit(&ms->bar[sTear]);
                 mbar_wait(&ms->bar[sTear], 0, kBarWaitNs);
             }
+        }
+        __syncwarp();
+    } else if (warp == kStateLoadWarp) {
+        if (lane == 0) {
+            int j = 0;
+            for (; j < u.tiles; ++j) {  // the j-th tile from the end
+                const int st = j % Sm::kStages, i = j - Sm::kStages, t = u.t_lo + (u.tiles - 1 - j) * kTile;
+                // the products of the tile that held the stage are done
+                if (i >= 0 && !bar_wait(ms, sEvU0 + st, (i / Sm::kStages) & 1, p)) break;
+                uint64_t *bar = &ms->bar[sLd0 + st];
+                mbar_arrive_expect_tx(bar, kTileBytes + Sm::kOperand);
+                for (int k = 0; k < kN / 64; ++k)
+                    tma_load_4d(smem + Sm::B(st) + k * kBlockBytes, &tm_b, bar, 64 * k, u.g, t, u.b);
+                tma_load_4d(smem + Sm::X(st), &tm_x, bar, 0, u.h0, t, u.b);
+                tma_load_4d(smem + Sm::X(st) + kBlockBytes, &tm_x, bar, u.one ? 64 : 0,
+                            u.one || !u.both ? u.h0 : u.h0 + 1, t, u.b);
+            }
+            // (where a wait gave up) copies in flight finish before shared memory is released
+            for (int i = max(j - Sm::kStages, 0); i < j; ++i)
+                mbar_wait(&ms->bar[sLd0 + i % Sm::kStages], (i / Sm::kStages) & 1, kBarWaitNs);
         }
         __syncwarp();
     } else if (warp >= kStateStepWarp) {
@@ -376,18 +376,21 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         const int e = warp - kStateStepWarp, head = u.one || !e || !u.both ? u.h0 : u.h0 + 1;
         const float da = p.a[head] * kLog2e, bias = p.delta_bias ? p.delta_bias[head] : 0.f;
         const __nv_bfloat16 *from = p.delta + (long long)u.b * p.n * p.delta_stride + head;
-        __nv_bfloat16 raw[4];
-        auto fetch = [&](int j) {
-            const int t = u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane;
+        __nv_bfloat16 raw[2][4];  // of two tiles
+        auto fetch = [&](int j, __nv_bfloat16 (&r)[4]) {  // rows that do not count: another one's, not used
+            const int t = u.t_lo + max(u.tiles - 1 - j, 0) * kTile + 4 * lane;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                raw[i] = t >= u.t_lo && t + i < u.live ? from[(long long)(t + i) * p.delta_stride] : __nv_bfloat16();
+            for (int i = 0; i < 4; ++i) r[i] = from[(long long)min(t + i, u.live - 1) * p.delta_stride];
         };
-        fetch(0);
+        if (u.tiles > 0) {
+            fetch(0, raw[0]);
+            fetch(1, raw[1]);
+        }
+#pragma unroll 2
         for (int j = 0; j < u.tiles; ++j) {
             float4 up, cf;
-            block_decays(raw, u.live - (u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane), da, bias, p.softplus, up, cf);
-            fetch(j + 1);
+            block_decays(raw[j & 1], u.live - (u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane), da, bias, p.softplus, up, cf);
+            fetch(j + 2, raw[j & 1]);
             // every epilogue warp has done with the decays that were here
             if (j >= 2 && !bar_wait(ms, sEpX0 + (j & 1), ((j - 2) >> 1) & 1, p)) break;
             *reinterpret_cast<float4 *>(&ms->cf[j & 1][e][4 * lane]) = cf;
@@ -423,7 +426,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                 }
             }
             if (j >= 2) {  // the products of two tiles ago have read this lo
-                bar_wait(ms, sEvU0 + (j & 1), ((j - 2) >> 1) & 1, p);
+                bar_wait(ms, sEvU0 + (j - 2) % Sm::kStages, ((j - 2) / Sm::kStages) & 1, p);
                 tc_fence_after();
             }
             split_row(xs, xs, smem + Sm::Lo(j), r, c0, wr);
@@ -432,7 +435,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         }
         if (u.tiles > 0) {
             const int i = u.tiles - 1;
-            bar_wait(ms, sEvU0 + (i & 1), (i >> 1) & 1, p);
+            bar_wait(ms, sEvU0 + i % Sm::kStages, (i / Sm::kStages) & 1, p);
             tc_fence_after();
         }
         const int col = u.one ? c0 : (cq & 1) * 32;  // of the head
@@ -584,15 +587,14 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         // steps and decays of a tile's tokens for half e, four consecutive tokens a lane
         const int e = warp - kStepWarp, head = one || !e || !both ? h0 : h0 + 1;
         const float da = p.a[head] * kLog2e, bias = p.delta_bias ? p.delta_bias[head] : 0.f;
-        const __nv_bfloat16 *raw = p.delta + ((long long)b * p.n + t_lo + 4 * lane) * p.delta_stride + head;
+        const __nv_bfloat16 *raw = p.delta + (long long)b * p.n * p.delta_stride + head;
         __nv_bfloat16 next[4];
-        auto fetch = [&](int j) {
+        auto fetch = [&](int j) {  // rows that do not count: the last one that does, not used
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                next[i] = t_lo + j * kTile + 4 * lane + i < live ? raw[((long long)j * kTile + i) * p.delta_stride]
-                                                                 : __nv_bfloat16();
+                next[i] = raw[(long long)min(t_lo + j * kTile + 4 * lane + i, live - 1) * p.delta_stride];
         };
-        fetch(0);
+        if (tiles > 0) fetch(0);
         for (int j = 0; j < tiles; ++j) {
             float4 up, cf;
             block_decays(next, live - (t_lo + j * kTile + 4 * lane), da, bias, p.softplus, up, cf);
