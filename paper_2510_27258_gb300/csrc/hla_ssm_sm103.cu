@@ -59,14 +59,15 @@ enum Bar {
     bEpY0 = 9, bEpY1 = 10,                   // ... of the output, staged in X's slot of even, odd tiles
     bXf = 11,                                // the output has left X's slot
     bStep = 12,                              // a tile's decays are in shared memory (2 warp arrivals)
-    bTear = 13,
-    kNumBars = 14
+    bTot0 = 13, bTot1 = 14,                  // ... an even, odd tile's block decays, ahead of the rest
+    bTear = 15,
+    kNumBars = 16
 };
 
 struct Misc {
     // of both halves' tokens: decay up to the token in its 32-token block, step times the decay from the
-    // token to its block's end; decay of each block
-    float cum[2][kTile], cf[2][kTile], tot[2][4];
+    // token to its block's end; decay of each block (of even and odd tiles)
+    float cum[2][kTile], cf[2][kTile], tot[2][2][4];
     uint64_t bar[kNumBars];
     uint32_t tmem_base;
     int abort_flag;
@@ -485,7 +486,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : i == bStep ? 2 : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : i >= bStep && i <= bTot1 ? 2 : 1);
         ms->abort_flag = 0;
         ms->b = b; ms->h0 = h0; ms->seg = seg; ms->both = both;
         fence_mbar_init();
@@ -599,11 +600,13 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             float4 up, cf;
             block_decays(next, live - (t_lo + j * kTile + 4 * lane), da, bias, p.softplus, up, cf);
             fetch(j + 1);
+            if ((lane & 7) == 7) ms->tot[j & 1][e][lane >> 3] = up.w;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ms->bar[bTot0 + (j & 1)]);
             // every epilogue warp has done with the previous tile's decays
             if (j > 0 && !bar_wait(ms, bEpW, (j - 1) & 1, p)) break;
             *reinterpret_cast<float4 *>(&ms->cum[e][4 * lane]) = up;
             *reinterpret_cast<float4 *>(&ms->cf[e][4 * lane]) = cf;
-            if ((lane & 7) == 7) ms->tot[e][lane >> 3] = up.w;
             __syncwarp();
             if (lane == 0) mbar_arrive(&ms->bar[bStep]);
         }
@@ -627,14 +630,16 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const uint32_t h_at = tb + lane_base + kTH + c0;
         // decay of the tile's blocks before / after this token's, and of the whole tile
         float before = 0.f, later = 0.f, total = 0.f;
-        auto decays = [&]() {
+        auto decays = [&](int j) {
+            bar_wait(ms, bTot0 + (j & 1), (j >> 1) & 1, p);
+            const float *tot = ms->tot[j & 1][hs];
             before = later = 0.f;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (q < qd) before += ms->tot[hs][q];
-                if (q > qd) later += ms->tot[hs][q];
+                if (q < qd) before += tot[q];
+                if (q > qd) later += tot[q];
             }
-            total = before + ms->tot[hs][qd] + later;
+            total = before + tot[qd] + later;
         };
         // the state before a tile: its bf16 copy to EH, handed over at once, and times the tile's decay to
         // TMEM, which is read only after the hand-over of w X
@@ -662,8 +667,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                                            : state_at(const_cast<float *>(p.state_in), 1, 0);
         const int cols = p.P - (one ? c0 : (cq & 1) * 32);  // columns of the head from this thread's first one on
         if (tiles > 0) {
-            bar_wait(ms, bStep, 0, p);
-            decays();
+            decays(0);
             float v[32];
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
@@ -703,10 +707,11 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if (cq <= qd) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float own = ms->tot[e][qd];
+                    const float *tot = ms->tot[j & 1][e];
+                    const float own = tot[qd];
                     float x = ms->cum[e][r] - (cq == qd ? own : 0.f);
-                    if (cq < 1 && qd > 1) x += ms->tot[e][1];
-                    if (cq < 2 && qd > 2) x += ms->tot[e][2];
+                    if (cq < 1 && qd > 1) x += tot[1];
+                    if (cq < 2 && qd > 2) x += tot[2];
                     rf[e] = ex2(x);
                     if (cq == qd && !(fabsf(own) <= kFactored)) factored = false;
                 }
@@ -783,6 +788,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             uint8_t *xs = smem + Sm::X(buf);
             const bool in = t0 + r < live;
             // (a) w X -> hi (EH), lo
+            bar_wait(ms, bStep, par, p);
             const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
             landed(j);
             bar_wait(ms, bEvY2, par, p);  // C H has read EH
@@ -816,8 +822,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             bar_wait(ms, bEvU, par, p);
             tc_fence_after();
             if (j + 1 < tiles) {
-                bar_wait(ms, bStep, (j + 1) & 1, p);
-                decays();
+                decays(j + 1);
                 float v[32];
                 if (srow) {
                     uint32_t u[32];
