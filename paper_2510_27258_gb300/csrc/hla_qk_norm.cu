@@ -379,24 +379,33 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
     }
 }
 
-// dwq and dwk from `rows` partials [2][d]: 32 entries a block, a warp for every 32nd row
-constexpr int kSumThreads = 1024;
+// dwq and dwk from `rows` partials [2][d]: 32 entries a block, four a thread, every 128th row
+constexpr int kSumThreads = 1024, kSumGroups = kSumThreads / 8;
 
 __global__ void __launch_bounds__(kSumThreads)
 qk_norm_sum_kernel(const float *__restrict__ partial, int rows, int d, float *dwq, float *dwk, WsHeader *header) {
-    __shared__ float red[32][33];
+    __shared__ float red[32][kSumGroups + 1];
     after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;  // 2 d is a multiple of 32
-    float s = 0.f;
+    const int quad = threadIdx.x & 7, group = threadIdx.x >> 3;  // (2 d is a multiple of 32)
+    const float *from = partial + blockIdx.x * 32 + quad * 4;
+    float s[4] = {};
 #pragma unroll 8
-    for (int r = group; r < rows; r += 32) s += partial[(size_t)r * 2 * d + i];
-    red[group][lane] = s;
+    for (int r = group; r < rows; r += kSumGroups) {
+        const float4 v = *reinterpret_cast<const float4 *>(from + (size_t)r * 2 * d);
+        s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[quad * 4 + i][group] = s[i];
     __syncthreads();
-    s = row_sum<32>(red[lane][group]);  // entry `group` of the block
-    const int e = blockIdx.x * 32 + group;
+    // warp w: entry w of the block
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, e = blockIdx.x * 32 + w;
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kSumGroups; k += 32) sum += red[w][k + lane];
+    sum = row_sum<32>(sum);
     float *to = e < d ? dwq : dwk;
-    if (lane == 0 && to) to[e < d ? e : e - d] = s;
+    if (lane == 0 && to) to[e < d ? e : e - d] = sum;
 }
 
 struct Plan {
