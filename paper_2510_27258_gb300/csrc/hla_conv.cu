@@ -10,7 +10,11 @@
 // About 2 W flops a value: bound by memory traffic.  A thread owns V neighbouring channels (one
 // 16-byte access a row, neighbouring lanes on neighbouring channels) and walks a strip of
 // consecutive tokens with the W - 1 previous rows in registers, so each x row is loaded once a strip
-// and W - 1 rows a strip are read twice (from L2).  A ring of kAhead rows is in flight.
+// and W - 1 rows a strip are read twice (from L2).  A ring of kAhead rows is in flight (asynchronous
+// copies: a ring in registers took 43 us where this takes 29).
+//
+// Measured on a GB300: forward, B2 n8192 C2304 bf16, 29.5 us a pass (5.1 TB/s), gradient, B8 n2048
+// C1280 bf16, 36.9 us (3.4 TB/s, bound by issue slots), step of 64 sequences 4 us.
 #include <type_traits>
 
 #include "hla_vec.cuh"

@@ -19,9 +19,9 @@
 //
 // TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H, and Y twice.  H is kept
 // multiplied by the coming tile's decay, so that B^T w X accumulates onto it; Y is C H, whose rows the
-// epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X double-buffered, the slot EH (H in bf16 for C H,
-// then hi), and lo, which takes C's place once S and C H are done (its own slot for N <= 64).  The
-// output is staged in X's place.
+// epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X
+// double-buffered, the slot EH (H in bf16 for C H, then hi), and lo, which takes C's place once S and
+// C H are done (its own slot for N <= 64).  The output is staged in X's place.
 //
 // Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
 // state row) and columns 32 (w / 4) .. ; warp 16 issues loads and MMAs, warp 17 stores the output (one
@@ -29,6 +29,11 @@
 // only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
 // W while the tensor cores run B^T w X, puts the new H down while they run W X, and writes the output
 // while they run the next tile's C H.
+//
+// What bounds it: the chain above, about 6,400 cycles a tile with every phase near what shared memory
+// gives it (580 KB a tile).  Measured on a GB300: B8 n2048 H32 P64 G1 N128 57.4 us (39 % of what its
+// bytes take), B1 n32768 H16 P64 G2 N64 76.9 us in three launches (the state sweep 25,
+// the chain 7, this kernel 50, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
 // each segment's own state, chain_kernel the state before each segment.
