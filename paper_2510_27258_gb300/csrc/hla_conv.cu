@@ -14,7 +14,7 @@
 // copies: a ring in registers took 43 us where this takes 29).
 //
 // Measured on a GB300: forward, B2 n8192 C2304 bf16, 29.5 us a pass (5.1 TB/s), gradient, B8 n2048
-// C1280 bf16, 36.9 us (3.4 TB/s, bound by issue slots), step of 64 sequences 4 us.
+// C1280 bf16, 34.4 us (3.7 TB/s, bound by issue slots), step of 64 sequences 4 us.
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -243,18 +243,19 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
             }
             constexpr int kTurn = W == 3 ? 3 * kAheadBwd : kAheadBwd;
             T *to = dx + (size_t)at.t0 * ds;  // of token t + u - (W - 1), once its g and the next W - 1 are there
-            for (int t = at.t0; t < live + W - 1; t += kTurn) {
+            auto turn = [&](int t, auto edge) {
+                constexpr bool kEdge = edge();
 #pragma unroll
                 for (int u = 0; u < kTurn; ++u) {
                     const int tt = t + u;
-                    if (tt < live + W - 1) {
+                    if (!kEdge || tt < live + W - 1) {
                         uint64_t(&gc)[kP] = gw[u % W];
                         ring_wait<kAheadBwd - 1>();
                         Raw<T, V> &xr = sm.ring[0][u % kAheadBwd][threadIdx.x], &gr = sm.ring[1][u % kAheadBwd][threadIdx.x];
-                        to_pairs(tt < last ? xr : raw_zero<T, V>(), xw[u % W]);
-                        to_pairs(tt < last ? gr : raw_zero<T, V>(), gc);
-                        ring_copy<T, V>(&xr, xp, tt + kAheadBwd < last);
-                        ring_copy<T, V>(&gr, gp, tt + kAheadBwd < last);
+                        to_pairs(!kEdge || tt < last ? xr : raw_zero<T, V>(), xw[u % W]);
+                        to_pairs(!kEdge || tt < last ? gr : raw_zero<T, V>(), gc);
+                        ring_copy<T, V>(&xr, xp, !kEdge || tt + kAheadBwd < last);
+                        ring_copy<T, V>(&gr, gp, !kEdge || tt + kAheadBwd < last);
                         ring_commit();
                         xp += xs;
                         gp += gs;
@@ -268,11 +269,11 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
                                 gc[v] = mul2(mul2(gc[v], s), fma2(a, fma2(s, pair(-1.f, -1.f), one), one));
                             }
                         }
-                        if (tt >= last) {  // (silu' of a row that was not read may be anything)
+                        if (kEdge && tt >= last) {  // (silu' of a row that was not read may be anything)
 #pragma unroll
                             for (int v = 0; v < kP; ++v) gc[v] = pair(0.f, 0.f);
                         }
-                        if (tt < live) {
+                        if (!kEdge || tt < live) {
 #pragma unroll
                             for (int v = 0; v < kP; ++v) {
 #pragma unroll
@@ -280,7 +281,7 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
                                 dw[W][v] = add2(dw[W][v], gc[v]);
                             }
                         }
-                        if (tt - (W - 1) >= at.t0) {
+                        if (!kEdge || tt - (W - 1) >= at.t0) {
                             uint64_t d[kP];
 #pragma unroll
                             for (int v = 0; v < kP; ++v) {
@@ -293,6 +294,13 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
                         }
                     }
                 }
+            };
+            // (a turn with neither end of the strip in it needs no conditions: 37 -> 34 us)
+            for (int t = at.t0; t < live + W - 1; t += kTurn) {
+                if (t > at.t0 && t + kTurn + kAheadBwd <= last && t + kTurn <= live)
+                    turn(t, std::false_type());
+                else
+                    turn(t, std::true_type());
             }
         }
         const float zero[V] = {};
