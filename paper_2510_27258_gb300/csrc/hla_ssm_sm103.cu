@@ -17,22 +17,24 @@
 // C H reads are rounded to bf16 once, they only reach the bf16 output.  w X, which reaches the fp32
 // state, is an exact-to-2^-16 pair hi + lo of bf16, two products.
 //
-// TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H, and Y twice.  H is kept
-// multiplied by the coming tile's decay, so that B^T w X accumulates onto it; Y is C H, whose rows the
-// epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X
+// TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H^T, and Y twice.  H is
+// transposed (a lane per column), so that its product's N is the number of states: half the time for
+// N <= 64, and neighbouring lanes write neighbouring elements of a state (long scan 77 -> 72 us).  It is
+// kept multiplied by the coming tile's decay, so that (w X)^T B accumulates onto it; Y is C H, whose rows
+// the epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X
 // double-buffered, the slot EH (H in bf16 for C H, then hi), and lo, which takes C's place once S and
 // C H are done (its own slot for N <= 64).  The output is staged in X's place.
 //
 // Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
-// state row) and columns 32 (w / 4) .. ; warp 16 issues loads and MMAs, warp 17 stores the output (one
+// column of H) and columns 32 (w / 4) .. (of H^T: its fourth of the states); warp 16 issues loads and MMAs, warp 17 stores the output (one
 // thread each), warps 18 and 19 compute the next tile's decays, one half's each.  They meet at mbarriers
 // only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
 // W while the tensor cores run B^T w X, puts the new H down while they run W X, and writes the output
 // while they run the next tile's C H.
 //
 // What bounds it: the chain above, about 6,400 cycles a tile with every phase near what shared memory
-// gives it (580 KB a tile).  Measured on a GB300: B8 n2048 H32 P64 G1 N128 57.4 us (39 % of what its
-// bytes take), B1 n32768 H16 P64 G2 N64 76.9 us in three launches (the state sweep 25,
+// gives it (580 KB a tile).  Measured on a GB300: B8 n2048 H32 P64 G1 N128 56.3 us (40 % of what its
+// bytes take), B1 n32768 H16 P64 G2 N64 72.4 us in three launches (the state sweep 25,
 // the chain 7, this kernel 50, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
@@ -146,9 +148,9 @@ constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
 constexpr uint32_t kLboK = 1u << 16, kLboMN = (kBlockBytes >> 4) << 16;
 
 // D (+)= A B, KS steps of 16 over K, N columns, both operands in shared memory (low descriptor words)
-template <bool A_MN, bool B_MN, int KS>
+template <int N, bool A_MN, bool B_MN, int KS>
 __device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t accumulate) {
-    constexpr uint32_t id = idesc_bf16(128, 128, A_MN, B_MN);
+    constexpr uint32_t id = idesc_bf16(128, N, A_MN, B_MN);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
         const uint32_t ka = A_MN ? kk * 128u : (kk >> 2) * (kBlockBytes >> 4) + (kk & 3) * 2u;
@@ -347,8 +349,8 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
                 if (!(ok = bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p))) break;
                 if (!(ok = bar_wait(ms, sEpX0 + (j & 1), (j >> 1) & 1, p))) break;
                 tc_fence_after();
-                mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::X(st)), j > 0 ? 1u : 0u);
-                mma_ss<true, true, 8>(tb, lm(Sm::B(st)), lm(Sm::Lo(j)), 1u);
+                mma_ss<kN, true, true, 8>(tb, lm(Sm::X(st)), lm(Sm::B(st)), j > 0 ? 1u : 0u);
+                mma_ss<kN, true, true, 8>(tb, lm(Sm::Lo(j)), lm(Sm::B(st)), 1u);
                 umma_commit(&ms->bar[sEvU0 + st]);
             }
             if (!ok) {  // a wait gave up: MMAs in flight finish (bounded) before TMEM is released
@@ -444,23 +446,23 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             bar_wait(ms, sEvU0 + i % Sm::kStages, (i / Sm::kStages) & 1, p);
             tc_fence_after();
         }
-        const int col = u.one ? c0 : (cq & 1) * 32;  // of the head
-        const bool mine = (!hs || u.both) && r < p.N;
-        const long long at = ((long long)u.b * p.H + head) * p.segments + u.seg;
-        if (mine && col == 0 && r == 0) p.seg_decay[at] = run * kLn2;
-        float *to = p.seg_state + (at * p.N + r) * p.P + col;
+        // TMEM lane r holds column r of the states: those of a head are written by neighbouring lanes
+        constexpr int kS = kN / 4;
+        const int half = qd >> 1, col = u.one ? r : r & 63, s0 = cq * kS;
+        const bool mine = (!half || u.both) && col < p.P;
+        const long long at = ((long long)u.b * p.H + (u.one || !half ? u.h0 : u.h0 + 1)) * p.segments + u.seg;
+        if (r == 0 && (cq == 0 || (cq == 2 && !u.one && u.both)))  // (of half cq / 2)
+            p.seg_decay[((long long)u.b * p.H + head) * p.segments + u.seg] = run * kLn2;
+        float *to = p.seg_state + (at * p.N + s0) * p.P + col;
 #pragma unroll
-        for (int o = 0; o < 32; o += 16) {
+        for (int o = 0; o < kS; o += 16) {
             uint32_t v[16];
-            tmem_ld16(tb + ((uint32_t)(32 * qd) << 16) + c0 + o, v);  // by whole warps, wherever the values go
+            tmem_ld16(tb + ((uint32_t)(32 * qd) << 16) + s0 + o, v);  // by whole warps, wherever the values go
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                if (mine && col + o + i < p.P)
-                    *reinterpret_cast<float4 *>(to + o + i) =
-                        u.tiles > 0 ? make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]),
-                                                  __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]))
-                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int i = 0; i < 16; ++i)
+                if (mine && s0 + o + i < p.N)
+                    to[(size_t)(o + i) * p.P] = u.tiles > 0 ? __uint_as_float(v[i]) : 0.f;
         }
     }
     tc_fence_before();
@@ -540,9 +542,9 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 // H before the tile is in EH and TMEM
                 if (!(ok = bar_wait(ms, bEpE, par, p))) break;
                 tc_fence_after();
-                mma_ss<false, true, kN / 16>(tb + kTY + 128 * buf, lk(Sm::C(buf)), lm(Sm::kEH), 0u);  // C H
+                mma_ss<128, false, false, kN / 16>(tb + kTY + 128 * buf, lk(Sm::C(buf)), lk(Sm::kEH), 0u);  // C H
                 umma_commit(&ms->bar[bEvY2]);
-                mma_ss<false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);  // S = C B^T
+                mma_ss<128, false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);  // S = C B^T
                 umma_commit(&ms->bar[bEvS]);
                 if (loaded < tiles && j > 0) {  // the previous tile's products are done and its output has left
                     if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
@@ -550,8 +552,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 }
                 if (!(ok = bar_wait(ms, bEpX, par, p))) break;
                 tc_fence_after();
-                mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::kEH), 1u);  // H += B^T (w X)
-                mma_ss<true, true, 8>(tb + kTH, lm(Sm::B(buf)), lm(Sm::lo(buf)), 1u);
+                mma_ss<kN, true, true, 8>(tb + kTH, lm(Sm::kEH), lm(Sm::B(buf)), 1u);  // H^T += (w X)^T B
+                mma_ss<kN, true, true, 8>(tb + kTH, lm(Sm::lo(buf)), lm(Sm::B(buf)), 1u);
                 umma_commit(&ms->bar[bEvU]);
                 if (!(ok = bar_wait(ms, bEpW, par, p))) break;
                 tc_fence_after();
@@ -621,19 +623,20 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const int r = 32 * qd + lane, c0 = 32 * cq;
         const uint32_t lane_base = (uint32_t)(32 * qd) << 16;
         const int hs = cq >> 1;                     // which half of the columns
-        const bool srow = kN == 128 || qd < 2;      // this thread's row is a state row
+        constexpr int kS = kN / 4;                  // as rows of H^T (its TMEM lanes): column r, states s0 ..
+        const int s0 = cq * kS;
         const int dhead = one || !hs || !both ? h0 : h0 + 1;  // a second head that is not there: the first
         const float skip = p.skip ? p.skip[dhead] : 0.f;
-        // the state rows and columns of this thread within [B, H, segs, N, P]; null where it has none
+        // this thread's first state within [B, H, segs, N, P], the others P apart; null where it has none
         auto state_at = [&](float *base, int segs, int seg_i) -> float * {
             const volatile Misc *m = ms;
-            const int col = p.P == 128 ? c0 : (cq & 1) * 32;
-            if (!base || r >= p.N || (hs && !m->both)) return nullptr;
-            const long long bh = (long long)m->b * p.H + m->h0 + (p.P != 128 && hs ? 1 : 0);
-            return base + ((bh * segs + seg_i) * p.N + r) * p.P + col;
+            const int half = p.P == 128 ? 0 : qd >> 1, col = r - 64 * half;
+            if (!base || col >= p.P || (half && !m->both)) return nullptr;
+            const long long bh = (long long)m->b * p.H + m->h0 + half;
+            return base + ((bh * segs + seg_i) * p.N + s0) * p.P + col;
         };
-        const uint32_t h_at = tb + lane_base + kTH + c0;
-        // decay of the tile's blocks before / after this token's, and of the whole tile
+        const uint32_t h_at = tb + lane_base + kTH + s0;
+        // decay of the tile's blocks before / after this token's, and (for H^T's row) of the whole tile
         float before = 0.f, later = 0.f, total = 0.f;
         auto decays = [&](int j) {
             bar_wait(ms, bTot0 + (j & 1), (j >> 1) & 1, p);
@@ -644,42 +647,34 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 if (q < qd) before += tot[q];
                 if (q > qd) later += tot[q];
             }
-            total = before + tot[qd] + later;
+            const float *all = ms->tot[j & 1][qd >> 1];
+            total = (all[0] + all[1]) + (all[2] + all[3]);
         };
         // the state before a tile: its bf16 copy to EH, handed over at once, and times the tile's decay to
         // TMEM, which is read only after the hand-over of w X
-        auto put_state = [&](float (&v)[32]) {
-            if (srow) {
+        auto put_state = [&](float (&v)[kS]) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 8)
-                    *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, c0 + i)) =
-                        make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
-                                   pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
-            }
+            for (int i = 0; i < kS; i += 8)
+                *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, s0 + i)) =
+                    make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                               pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
             fence_async_smem();
             epi_arrive(ms, bEpE);
-            if (srow) {
-                const float keep = ex2(total);
-                uint32_t u[32];
+            const float keep = ex2(total);
+            uint32_t u[kS];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i] * keep);
-                tmem_st32(h_at, u);
-            }
+            for (int i = 0; i < kS; ++i) u[i] = __float_as_uint(v[i] * keep);
+            if constexpr (kS == 32) tmem_st32(h_at, u); else tmem_st16(h_at, u);
         };
         if (p.segments > 1) after_previous();  // (nothing is written before this by any role)
         // state 0: from state_in or the segment's chained state
         const float *from = p.segments > 1 ? state_at(p.seg_state, p.segments, seg)
                                            : state_at(const_cast<float *>(p.state_in), 1, 0);
-        const int cols = p.P - (one ? c0 : (cq & 1) * 32);  // columns of the head from this thread's first one on
         if (tiles > 0) {
             decays(0);
-            float v[32];
+            float v[kS];
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (from && i < cols) f = *reinterpret_cast<const float4 *>(from + i);
-                v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
-            }
+            for (int i = 0; i < kS; ++i) v[i] = from && s0 + i < p.N ? from[(size_t)i * p.P] : 0.f;
             put_state(v);
         }
 
@@ -828,14 +823,12 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             tc_fence_after();
             if (j + 1 < tiles) {
                 decays(j + 1);
-                float v[32];
-                if (srow) {
-                    uint32_t u[32];
-                    tmem_ld32(h_at, u);
-                    tmem_ld_wait();
+                float v[kS];
+                uint32_t u[kS];
+                if constexpr (kS == 32) tmem_ld32(h_at, u); else tmem_ld16(h_at, u);
+                tmem_ld_wait();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
-                }
+                for (int i = 0; i < kS; ++i) v[i] = __uint_as_float(u[i]);
                 put_state(v);
             }
             // (d) Y -> bf16 in X's place -> TMA store
@@ -867,8 +860,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const volatile Misc *m = ms;
         const int hcol = one ? c0 : (cq & 1) * 32;
         const int head = m->h0 + (one ? 0 : hs);
-        const bool mine = !hs || m->both;
-        if (mine) {  // the rest of the segment does not count: zeros
+        const int cols = p.P - hcol;  // columns of the head from this thread's first one on
+        if (!hs || m->both) {  // the rest of the segment does not count: zeros
             const int end = min((m->seg + 1) * p.seg_tiles * kTile, p.n);
             for (int t = max(m->seg * p.seg_tiles * kTile, live) + r; t < end; t += kTile) {
                 __nv_bfloat16 *row = p.y + ((long long)m->b * p.n + t) * p.y_stride + (long long)head * p.P + hcol;
@@ -879,18 +872,15 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         }
         float *to = m->seg == p.segments - 1 ? state_at(p.state_out, 1, 0) : nullptr;
 #pragma unroll
-        for (int o = 0; o < 32; o += 16) {
+        for (int o = 0; o < kS; o += 16) {
             uint32_t u[16];
             tmem_ld16(h_at + o, u);  // by whole warps, wherever the values go
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                if (!to || o + i >= cols) continue;
-                float4 f = make_float4(__uint_as_float(u[i]), __uint_as_float(u[i + 1]), __uint_as_float(u[i + 2]),
-                                       __uint_as_float(u[i + 3]));
-                if (tiles == 0)  // nothing counts: the state as it was
-                    f = from ? *reinterpret_cast<const float4 *>(from + o + i) : make_float4(0.f, 0.f, 0.f, 0.f);
-                *reinterpret_cast<float4 *>(to + o + i) = f;
+            for (int i = 0; i < 16; ++i) {
+                if (!to || s0 + o + i >= p.N) continue;
+                const size_t e = (size_t)(o + i) * p.P;
+                to[e] = tiles > 0 ? __uint_as_float(u[i]) : from ? from[e] : 0.f;  // nothing counts: the state as it was
             }
         }
     }
