@@ -21,21 +21,24 @@
 // transposed (a lane per column), so that its product's N is the number of states: half the time for
 // N <= 64, and neighbouring lanes write neighbouring elements of a state (long scan 77 -> 72 us).  It is
 // kept multiplied by the coming tile's decay, so that (w X)^T B accumulates onto it; Y is C H, whose rows
-// the epilogue multiplies by exp(L_t) before W X accumulates onto it.  Shared memory: C, B and X
-// double-buffered, the slot EH (H in bf16 for C H, then hi), and lo, which takes C's place once S and
-// C H are done (its own slot for N <= 64).  The output is staged in X's place.
+// the epilogue multiplies by exp(L_t) before W X accumulates onto it.
+//
+// Shared memory, N = 128: C, B and X double-buffered, a slot for H in bf16 and then hi, and lo in C's place
+// once S and C H are done.  N <= 64: slots of their own for H, hi and lo, three for X and one for C, so that
+// the next tile's w X is split while the tensor cores run W X (long scan 72 -> 68 us).  The output is
+// staged in X's place.
 //
 // Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
-// column of H) and columns 32 (w / 4) .. (of H^T: its fourth of the states); warp 16 issues loads and MMAs, warp 17 stores the output (one
-// thread each), warps 18 and 19 compute the next tile's decays, one half's each.  They meet at mbarriers
-// only.  The chain from tile to tile is H -> C H -> hi, lo (in H's slot) -> H'; the epilogue turns S into
-// W while the tensor cores run B^T w X, puts the new H down while they run W X, and writes the output
-// while they run the next tile's C H.
+// column of H) and columns 32 (w / 4) .. (of H^T: its fourth of the states); warp 16 issues loads and
+// MMAs, warp 17 stores the output (one thread each), warps 18 and 19 compute the next tile's decays, one
+// half's each.  They meet at mbarriers only.  The chain from tile to tile is H -> C H -> hi, lo (for
+// N = 128 in H's slot) -> H'; the epilogue turns S into W while the tensor cores run (w X)^T B, puts the
+// new H down while they run W X, and writes the output while they run the next tile's C H.
 //
-// What bounds it: the chain above, about 6,400 cycles a tile with every phase near what shared memory
-// gives it (580 KB a tile).  Measured on a GB300: B8 n2048 H32 P64 G1 N128 56.3 us (40 % of what its
-// bytes take), B1 n32768 H16 P64 G2 N64 72.4 us in three launches (the state sweep 25,
-// the chain 7, this kernel 50, each alone).
+// What bounds it: about 5,600 cycles a tile of N = 128, of which the epilogue warps wait a fourth for the
+// chain above; 4,700 a tile of N <= 64, all of them the epilogue's.  Measured on a GB300: B8 n2048 H32 P64
+// G1 N128 56.6 us (40 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.3 us in three launches (the
+// state sweep 23, the chain 7, this kernel 42, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
 // each segment's own state, chain_kernel the state before each segment.
@@ -60,15 +63,15 @@ constexpr float kFactored = 100.f;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum Bar {
-    bLd0 = 0, bLd1 = 1,                      // C, B, X of a buffer have landed
-    bEvS = 2, bEvY2 = 3, bEvY1 = 4, bEvU = 5,  // MMA commits
-    bEpE = 6, bEpW = 7, bEpX = 8,            // epilogue hand-offs (16 warp arrivals)
-    bEpY0 = 9, bEpY1 = 10,                   // ... of the output, staged in X's slot of even, odd tiles
-    bXf = 11,                                // the output has left X's slot
-    bStep = 12,                              // a tile's decays are in shared memory (2 warp arrivals)
-    bTot0 = 13, bTot1 = 14,                  // ... an even, odd tile's block decays, ahead of the rest
-    bTear = 15,
-    kNumBars = 16
+    bLdX = 0, bLdB = 3, bLdC = 5,              // + stage: X, B, C have landed (N = 128: all three, bLdX)
+    bEvS = 7, bEvY2 = 8, bEvY1 = 9, bEvU = 10,  // MMA commits
+    bEpE = 11, bEpW = 12, bEpX = 13,           // epilogue hand-offs (16 warp arrivals)
+    bEpY0 = 14, bEpY1 = 15,                    // ... of the output, staged in X's slot of even, odd tiles
+    bXf = 16,                                  // the output has left X's slot
+    bStep = 17,                                // a tile's decays are in shared memory (2 warp arrivals)
+    bTot0 = 18, bTot1 = 19,                    // ... an even, odd tile's block decays, ahead of the rest
+    bTear = 20,
+    kNumBars = 21
 };
 
 struct Misc {
@@ -84,16 +87,18 @@ struct Misc {
 };
 static_assert(sizeof(Misc) <= 3072, "fits beside the tiles");
 
-// shared-memory map for N <= 64 (kN = 64) and N = 128
+// shared-memory map for N <= 64 (kN = 64) and N = 128.  N <= 64 has room for H's copy and hi, lo apart.
 template <int kN>
 struct Map {
-    static constexpr uint32_t kOperand = kN / 64 * kBlockBytes;  // a C or B tile
-    static constexpr uint32_t C(int buf) { return buf * kOperand; }
-    static constexpr uint32_t B(int buf) { return (2 + buf) * kOperand; }
-    static constexpr uint32_t X(int buf) { return 4 * kOperand + buf * kTileBytes; }
-    static constexpr uint32_t kEH = 4 * kOperand + 2 * kTileBytes;
-    static constexpr uint32_t kEnd = kEH + kTileBytes + (kN == 64 ? kTileBytes : 0);
-    static constexpr uint32_t lo(int buf) { return kN == 64 ? kEH + kTileBytes : C(buf); }
+    static constexpr bool kApart = kN == 64;
+    static constexpr int kXs = kApart ? 3 : 2, kCs = kApart ? 1 : 2;  // stages of X and C (B: two)
+    static constexpr uint32_t kOperand = kN / 64 * kBlockBytes;       // a C or B tile
+    static constexpr uint32_t C(int s) { return s * kOperand; }
+    static constexpr uint32_t B(int s) { return (kCs + s) * kOperand; }
+    static constexpr uint32_t X(int s) { return (kCs + 2) * kOperand + s * kTileBytes; }
+    static constexpr uint32_t kHi = X(kXs), kH = kApart ? kHi + 2 * kTileBytes : kHi;
+    static constexpr uint32_t kEnd = kHi + kTileBytes + (kApart ? kTileBytes + kOperand : 0);
+    static constexpr uint32_t lo(int j) { return kApart ? kHi + kTileBytes : C(j & 1); }
     static constexpr uint32_t kBytes = kEnd + sizeof(Misc);
 };
 static_assert(Map<128>::kBytes <= 232448 && Map<64>::kBytes <= 232448, "shared memory");
@@ -516,61 +521,105 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const uint32_t sb4 = smem_u32(smem) >> 4;
             auto lk = [&](uint32_t off) { return sb4 + (off >> 4) + kLboK; };
             auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
-            auto load = [&](int j) {
-                const int buf = j & 1, t = t_lo + j * kTile;
-                uint64_t *bar = &ms->bar[bLd0 + buf];
-                mbar_arrive_expect_tx(bar, kTileBytes + 2 * Sm::kOperand);
-                for (int i = 0; i < kN / 64; ++i) {
-                    tma_load_4d(smem + Sm::B(buf) + i * kBlockBytes, &tm_b, bar, 64 * i, g, t, b);
-                    tma_load_4d(smem + Sm::C(buf) + i * kBlockBytes, &tm_c, bar, 64 * i, g, t, b);
-                }
+            auto load_x = [&](int j, int st, uint64_t *bar) {
                 // a second head that the group does not have: the first one again, its result unused
-                tma_load_4d(smem + Sm::X(buf), &tm_x, bar, 0, h0, t, b);
-                tma_load_4d(smem + Sm::X(buf) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
+                const int t = t_lo + j * kTile;
+                tma_load_4d(smem + Sm::X(st), &tm_x, bar, 0, h0, t, b);
+                tma_load_4d(smem + Sm::X(st) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
             };
-            int loaded = 0, landed = 0;  // tiles whose copies were issued / have been waited for
-            auto wait_ld = [&](int j) {
-                if (!bar_wait(ms, bLd0 + (j & 1), (j >> 1) & 1, p)) return false;
-                landed = j + 1;
-                tc_fence_after();
-                return true;
+            auto load_bc = [&](const CUtensorMap *map, int j, uint32_t to, uint64_t *bar) {
+                for (int i = 0; i < kN / 64; ++i)
+                    tma_load_4d(smem + to + i * kBlockBytes, map, bar, 64 * i, g, t_lo + j * kTile, b);
             };
-            while (loaded < 2 && loaded < tiles) load(loaded++);
-            bool ok = tiles == 0 || wait_ld(0);
-            for (int j = 0; ok && j < tiles; ++j) {
-                const int buf = j & 1, par = j & 1;
-                // H before the tile is in EH and TMEM
-                if (!(ok = bar_wait(ms, bEpE, par, p))) break;
+            auto expect = [&](int bar, uint32_t bytes) {
+                mbar_arrive_expect_tx(&ms->bar[bar], bytes);
+                return &ms->bar[bar];
+            };
+            auto scores = [&](int buf, int cb) {  // with H before the tile in its slot and TMEM
                 tc_fence_after();
-                mma_ss<128, false, false, kN / 16>(tb + kTY + 128 * buf, lk(Sm::C(buf)), lk(Sm::kEH), 0u);  // C H
+                mma_ss<128, false, false, kN / 16>(tb + kTY + 128 * buf, lk(Sm::C(cb)), lk(Sm::kH), 0u);  // C H
                 umma_commit(&ms->bar[bEvY2]);
-                mma_ss<128, false, false, kN / 16>(tb + kTS, lk(Sm::C(buf)), lk(Sm::B(buf)), 0u);  // S = C B^T
+                mma_ss<128, false, false, kN / 16>(tb + kTS, lk(Sm::C(cb)), lk(Sm::B(buf)), 0u);  // S = C B^T
                 umma_commit(&ms->bar[bEvS]);
-                if (loaded < tiles && j > 0) {  // the previous tile's products are done and its output has left
-                    if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
-                    load(loaded++);
-                }
-                if (!(ok = bar_wait(ms, bEpX, par, p))) break;
+            };
+            auto update = [&](int buf) {
                 tc_fence_after();
-                mma_ss<kN, true, true, 8>(tb + kTH, lm(Sm::kEH), lm(Sm::B(buf)), 1u);  // H^T += (w X)^T B
+                mma_ss<kN, true, true, 8>(tb + kTH, lm(Sm::kHi), lm(Sm::B(buf)), 1u);  // H^T += (w X)^T B
                 mma_ss<kN, true, true, 8>(tb + kTH, lm(Sm::lo(buf)), lm(Sm::B(buf)), 1u);
                 umma_commit(&ms->bar[bEvU]);
-                if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+            };
+            auto output = [&](int buf, int xb) {  // Y += W X
                 tc_fence_after();
-                const uint32_t y = tb + kTY + 128 * buf;  // Y += W X
+                const uint32_t y = tb + kTY + 128 * buf;
                 if (one) {
-                    mma_ts<128>(y, tb + kTS, lm(Sm::X(buf)));
+                    mma_ts<128>(y, tb + kTS, lm(Sm::X(xb)));
                 } else {
-                    mma_ts<64>(y, tb + kTS, lm(Sm::X(buf)));
-                    mma_ts<64>(y + 64, tb + kTS + 8, lm(Sm::X(buf) + kBlockBytes));
+                    mma_ts<64>(y, tb + kTS, lm(Sm::X(xb)));
+                    mma_ts<64>(y + 64, tb + kTS + 8, lm(Sm::X(xb) + kBlockBytes));
                 }
                 umma_commit(&ms->bar[bEvY1]);
-                if (j + 1 < tiles && !(ok = wait_ld(j + 1))) break;
+            };
+            bool ok = true;
+            int xs = 0, bs = 0, cs = 0;  // tiles whose copies of X, B, C were issued (N = 128: all three, xs)
+            if constexpr (Sm::kApart) {
+                auto next_x = [&]() { load_x(xs, xs % Sm::kXs, expect(bLdX + xs % Sm::kXs, kTileBytes)); ++xs; };
+                auto next_b = [&]() { load_bc(&tm_b, bs, Sm::B(bs & 1), expect(bLdB + (bs & 1), Sm::kOperand)); ++bs; };
+                auto next_c = [&]() { load_bc(&tm_c, cs, Sm::C(0), expect(bLdC, Sm::kOperand)); ++cs; };
+                if (tiles > 0) { next_c(); next_b(); next_x(); }
+                if (tiles > 1) { next_b(); next_x(); }
+                if (tiles > 2) next_x();
+                for (int j = 0; j < tiles; ++j) {
+                    const int buf = j & 1, par = j & 1, xb = j % Sm::kXs;
+                    if (!(ok = bar_wait(ms, bLdC, par, p) && bar_wait(ms, bLdB + buf, (j >> 1) & 1, p))) break;
+                    if (!(ok = bar_wait(ms, bEpE, par, p))) break;
+                    scores(buf, 0);
+                    if (j > 0 && bs < tiles) next_b();  // the previous tile's (w X)^T B is done
+                    if (!(ok = bar_wait(ms, bLdX + xb, (j / Sm::kXs) & 1, p) && bar_wait(ms, bEpX, par, p))) break;
+                    update(buf);
+                    if (cs < tiles) {
+                        if (!(ok = bar_wait(ms, bEvS, par, p))) break;
+                        next_c();
+                    }
+                    if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+                    output(buf, xb);
+                    if (j > 0 && xs < tiles) {  // the previous tile's output has left
+                        if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
+                        next_x();
+                    }
+                }
+            } else {
+                auto next = [&]() {
+                    uint64_t *bar = expect(bLdX + (xs & 1), kTileBytes + 2 * Sm::kOperand);
+                    load_bc(&tm_b, xs, Sm::B(xs & 1), bar);
+                    load_bc(&tm_c, xs, Sm::C(xs & 1), bar);
+                    load_x(xs, xs & 1, bar);
+                    ++xs;
+                };
+                while (xs < 2 && xs < tiles) next();
+                ok = tiles == 0 || bar_wait(ms, bLdX, 0, p);
+                for (int j = 0; ok && j < tiles; ++j) {
+                    const int buf = j & 1, par = j & 1;
+                    if (!(ok = bar_wait(ms, bEpE, par, p))) break;
+                    scores(buf, buf);
+                    if (j > 0 && xs < tiles) {  // the previous tile's products are done and its output has left
+                        if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
+                        next();
+                    }
+                    if (!(ok = bar_wait(ms, bEpX, par, p))) break;
+                    update(buf);
+                    if (!(ok = bar_wait(ms, bEpW, par, p))) break;
+                    output(buf, buf);
+                    if (j + 1 < tiles) ok = bar_wait(ms, bLdX + (buf ^ 1), ((j + 1) >> 1) & 1, p);
+                }
             }
             if (!ok) {
                 // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
                 // TMEM are released
-                for (int j = landed; j < loaded; ++j) mbar_wait(&ms->bar[bLd0 + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                for (int j = max(xs - Sm::kXs, 0); j < xs; ++j) mbar_wait(&ms->bar[bLdX + j % Sm::kXs], (j / Sm::kXs) & 1, kBarWaitNs);
+                if (Sm::kApart) {
+                    for (int j = max(bs - 2, 0); j < bs; ++j) mbar_wait(&ms->bar[bLdB + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                    if (cs > 0) mbar_wait(&ms->bar[bLdC], (cs - 1) & 1, kBarWaitNs);
+                }
                 umma_commit(&ms->bar[bTear]);
                 mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
             }
@@ -579,7 +628,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     } else if (warp == kStoreWarp) {
         if (lane == 0) {
             for (int j = 0; j < tiles; ++j) {
-                const uint8_t *xs = smem + Sm::X(j & 1);
+                const uint8_t *xs = smem + Sm::X(j % Sm::kXs);
                 const int t0 = t_lo + j * kTile;
                 if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
                 tma_store_4d(&tm_y, xs, 0, h0, t0, b);
@@ -655,7 +704,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         auto put_state = [&](float (&v)[kS]) {
 #pragma unroll
             for (int i = 0; i < kS; i += 8)
-                *reinterpret_cast<uint4 *>(smem + Sm::kEH + tile_off(r, s0 + i)) =
+                *reinterpret_cast<uint4 *>(smem + Sm::kH + tile_off(r, s0 + i)) =
                     make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
                                pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
             fence_async_smem();
@@ -680,14 +729,15 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 
         // waits for tile j's copies; tokens that do not count: zero rows of X and B, whatever was read
         auto landed = [&](int j) {
-            const int buf = j & 1, t0 = t_lo + j * kTile;
-            bar_wait(ms, bLd0 + buf, (j >> 1) & 1, p);
+            const int xb = j % Sm::kXs, buf = j & 1, t0 = t_lo + j * kTile;
+            bar_wait(ms, bLdX + xb, (j / Sm::kXs) & 1, p);
             if (t0 + kTile > live) {
+                if (Sm::kApart) bar_wait(ms, bLdB + buf, (j >> 1) & 1, p);
                 if (t0 + r >= live) {
                     const uint4 z = make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
-                        *reinterpret_cast<uint4 *>(smem + Sm::X(buf) + tile_off(r, c0 + i)) = z;
+                        *reinterpret_cast<uint4 *>(smem + Sm::X(xb) + tile_off(r, c0 + i)) = z;
                         if (kN == 128 || cq < 2) *reinterpret_cast<uint4 *>(smem + Sm::B(buf) + tile_off(r, c0 + i)) = z;
                     }
                 }
@@ -783,23 +833,35 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             tmem_st_wait();
             epi_arrive(ms, bEpW);
         };
-        for (int j = 0; j < tiles; ++j) {
-            const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
-            uint8_t *xs = smem + Sm::X(buf);
-            const bool in = t0 + r < live;
-            // (a) w X -> hi (EH), lo
-            bar_wait(ms, bStep, par, p);
-            const float wr = ms->cf[hs][r] * ex2(later), yf = ex2(before + ms->cum[hs][r]);
+        // (a) w X of tile j -> hi, lo
+        float yf = 0.f;  // decay of the tile up to this token
+        auto split = [&](int j) {
+            bar_wait(ms, bStep, j & 1, p);
+            const float wr = ms->cf[hs][r] * ex2(later);
+            yf = ex2(before + ms->cum[hs][r]);
             landed(j);
-            bar_wait(ms, bEvY2, par, p);  // C H has read EH
-            if (kN == 128) bar_wait(ms, bEvS, par, p);  // (and C B^T has read C, where lo goes)
-            tc_fence_after();
-            split_row(xs, smem + Sm::kEH, smem + Sm::lo(buf), r, c0, wr);
+            if (!Sm::kApart) {
+                bar_wait(ms, bEvY2, j & 1, p);  // C H has read H, where hi goes,
+                bar_wait(ms, bEvS, j & 1, p);   // and C B^T has read C, where lo goes
+                tc_fence_after();
+            }
+            split_row(smem + Sm::X(j % Sm::kXs), smem + Sm::kHi, smem + Sm::lo(j), r, c0, wr);
             fence_async_smem();
             tmem_st_wait();  // (H times the tile's decay)
             epi_arrive(ms, bEpX);
+        };
+        if (Sm::kApart && tiles > 0) split(0);
+        for (int j = 0; j < tiles; ++j) {
+            const int buf = j & 1, par = j & 1, t0 = t_lo + j * kTile;
+            uint8_t *xs = smem + Sm::X(j % Sm::kXs);
+            const bool in = t0 + r < live;
+            if (!Sm::kApart) split(j);
             // (b) C H times the decay up to each token, and W, while the tensor cores run B^T (w X)
             const uint32_t y_at = tb + lane_base + kTY + 128 * buf + c0;
+            if (Sm::kApart) {
+                bar_wait(ms, bEvY2, par, p);
+                tc_fence_after();
+            }
             {
                 const uint64_t yf2 = pair(yf, yf);
 #pragma unroll
@@ -830,6 +892,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 #pragma unroll
                 for (int i = 0; i < kS; ++i) v[i] = __uint_as_float(u[i]);
                 put_state(v);
+                if (Sm::kApart) split(j + 1);
             }
             // (d) Y -> bf16 in X's place -> TMA store
             bar_wait(ms, bEvY1, par, p);
