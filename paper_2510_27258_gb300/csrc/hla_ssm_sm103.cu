@@ -35,9 +35,9 @@
 // N = 128 in H's slot) -> H'; the epilogue turns S into W while the tensor cores run (w X)^T B, puts the
 // new H down while they run W X, and writes the output while they run the next tile's C H.
 //
-// What bounds it: about 5,600 cycles a tile of N = 128, of which the epilogue warps wait a fourth for the
+// What bounds it: about 5,300 cycles a tile of N = 128, of which the epilogue warps wait a fourth for the
 // chain above; 4,700 a tile of N <= 64, all of them the epilogue's.  Measured on a GB300: B8 n2048 H32 P64
-// G1 N128 56.6 us (40 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.3 us in three launches (the
+// G1 N128 53.4 us (42 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.3 us in three launches (the
 // state sweep 23, the chain 7, this kernel 42, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
@@ -203,26 +203,39 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t 
     return r;
 }
 
-// 32 elements of a row of w X as the bf16 pairs hi + lo, rows and columns as in the X tile (hi may take
-// its place).  With w = wh + wl in bf16 (to 2^-17): hi = x wh rounded, x wh - hi is a bf16 exactly, and
-// lo = x wl + (x wh - hi) rounded, all by fused multiply-adds on the packed elements.
+// Elements c .. c + 7 of a row of w X as the bf16 pairs hi + lo.  With w = wh + wl in bf16 (to 2^-17): hi = x wh
+// rounded, x wh - hi is a bf16 exactly, and lo = x wl + (x wh - hi) rounded, all by fused multiply-adds on
+// the packed elements.
+struct Weight {
+    uint32_t wh, wl;
+    __device__ explicit Weight(float w) : wh(pack_bf16x2(w, w)) {
+        const float rest = w - bf16_lo(wh);
+        wl = pack_bf16x2(rest, rest);
+    }
+};
+
+__device__ __forceinline__ void split8(const uint8_t *xs, int r, int c, const Weight &w, uint4 &hi, uint4 &lo) {
+    const uint4 u = *reinterpret_cast<const uint4 *>(xs + tile_off(r, c));
+    const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        h[e] = fma_bf16x2(x[e], w.wh, 0x80008000u);  // (plus minus zero)
+        l[e] = fma_bf16x2(x[e], w.wl, fma_bf16x2(x[e], w.wh, h[e] ^ 0x80008000u));
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// 32 of them, rows and columns as in the X tile (hi may take its place)
 __device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
-    const uint32_t wh = pack_bf16x2(wr, wr);
-    const float rest = wr - bf16_lo(wh);
-    const uint32_t wl = pack_bf16x2(rest, rest);
+    const Weight w(wr);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t off = tile_off(r, c0 + 8 * i);
-        const uint4 u = *reinterpret_cast<const uint4 *>(xs + off);
-        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            hi[e] = fma_bf16x2(x[e], wh, 0x80008000u);                          // (plus minus zero)
-            lo[e] = fma_bf16x2(x[e], wl, fma_bf16x2(x[e], wh, hi[e] ^ 0x80008000u));
-        }
-        *reinterpret_cast<uint4 *>(hi_tile + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4 *>(lo_tile + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    for (int i = 0; i < 32; i += 8) {
+        uint4 hi, lo;
+        split8(xs, r, c0 + i, w, hi, lo);
+        *reinterpret_cast<uint4 *>(hi_tile + tile_off(r, c0 + i)) = hi;
+        *reinterpret_cast<uint4 *>(lo_tile + tile_off(r, c0 + i)) = lo;
     }
 }
 
@@ -840,12 +853,21 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const float wr = ms->cf[hs][r] * ex2(later);
             yf = ex2(before + ms->cum[hs][r]);
             landed(j);
-            if (!Sm::kApart) {
+            if constexpr (Sm::kApart) {
+                split_row(smem + Sm::X(j % Sm::kXs), smem + Sm::kHi, smem + Sm::lo(j), r, c0, wr);
+            } else {  // in registers until their slots are free
+                const Weight w(wr);
+                uint4 hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) split8(smem + Sm::X(j & 1), r, c0 + 8 * i, w, hi[i], lo[i]);
                 bar_wait(ms, bEvY2, j & 1, p);  // C H has read H, where hi goes,
-                bar_wait(ms, bEvS, j & 1, p);   // and C B^T has read C, where lo goes
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(smem + Sm::kHi + tile_off(r, c0 + 8 * i)) = hi[i];
+                bar_wait(ms, bEvS, j & 1, p);  // and C B^T has read C, where lo goes
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(smem + Sm::lo(j) + tile_off(r, c0 + 8 * i)) = lo[i];
                 tc_fence_after();
             }
-            split_row(smem + Sm::X(j % Sm::kXs), smem + Sm::kHi, smem + Sm::lo(j), r, c0, wr);
             fence_async_smem();
             tmem_st_wait();  // (H times the tile's decay)
             epi_arrive(ms, bEpX);
