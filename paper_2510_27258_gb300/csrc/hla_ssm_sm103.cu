@@ -29,15 +29,16 @@
 // staged in X's place.
 //
 // Roles: warps 0-15 are the epilogue, warp w on TMEM lanes 32 (w % 4) .. (one row each: a token, or a
-// column of H) and columns 32 (w / 4) .. (of H^T: its fourth of the states); warp 16 issues loads and
-// MMAs, warp 17 stores the output (one thread each), warps 18 and 19 compute the next tile's decays, one
-// half's each.  They meet at mbarriers only.  The chain from tile to tile is H -> C H -> hi, lo (for
+// column of H) and columns 32 (w / 4) .. (of H^T: its fourth of the states); warp 16 loads B and C and
+// issues MMAs, warp 17 stores the output and loads X (one thread each), warps 18 and 19 compute the next
+// tile's decays, one half's each.  They meet at mbarriers only.  The chain from tile to tile is H -> C H -> hi, lo (for
 // N = 128 in H's slot) -> H'; the epilogue turns S into W while the tensor cores run (w X)^T B, puts the
 // new H down while they run W X, and writes the output while they run the next tile's C H.
 //
-// What bounds it: about 5,300 cycles a tile of N = 128, of which the epilogue warps wait a fourth for the
-// chain above; 4,700 a tile of N <= 64, all of them the epilogue's.  Measured on a GB300: B8 n2048 H32 P64
-// G1 N128 53.4 us (42 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.3 us in three launches (the
+// What bounds it: shared memory.  A tile of N = 128 takes about 5,200 cycles and moves 620 KB (the products'
+// operands 290, hi, lo and H 128, x and the output 128, copies 128 and more), 4,900 cycles at 128 bytes; one
+// of N <= 64 takes 4,600 and moves 470 KB, its epilogue warps never waiting for long.  Measured on a GB300: B8 n2048 H32 P64
+// G1 N128 53.3 us (42 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.1 us in three launches (the
 // state sweep 23, the chain 7, this kernel 42, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
@@ -67,11 +68,10 @@ enum Bar {
     bEvS = 7, bEvY2 = 8, bEvY1 = 9, bEvU = 10,  // MMA commits
     bEpE = 11, bEpW = 12, bEpX = 13,           // epilogue hand-offs (16 warp arrivals)
     bEpY0 = 14, bEpY1 = 15,                    // ... of the output, staged in X's slot of even, odd tiles
-    bXf = 16,                                  // the output has left X's slot
-    bStep = 17,                                // a tile's decays are in shared memory (2 warp arrivals)
-    bTot0 = 18, bTot1 = 19,                    // ... an even, odd tile's block decays, ahead of the rest
-    bTear = 20,
-    kNumBars = 21
+    bStep = 16,                                // a tile's decays are in shared memory (2 warp arrivals)
+    bTot0 = 17, bTot1 = 18,                    // ... an even, odd tile's block decays, ahead of the rest
+    bTear = 19,
+    kNumBars = 20
 };
 
 struct Misc {
@@ -511,7 +511,10 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         return;
     }
     if (tid == 0) {
-        for (int i = 0; i < kNumBars; ++i) mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : i >= bStep && i <= bTot1 ? 2 : 1);
+        for (int i = 0; i < kNumBars; ++i) {
+            const bool two = (i >= bStep && i <= bTot1) || (!Sm::kApart && i < bLdB);
+            mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : two ? 2 : 1);
+        }
         ms->abort_flag = 0;
         ms->b = b; ms->h0 = h0; ms->seg = seg; ms->both = both;
         fence_mbar_init();
@@ -534,12 +537,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const uint32_t sb4 = smem_u32(smem) >> 4;
             auto lk = [&](uint32_t off) { return sb4 + (off >> 4) + kLboK; };
             auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
-            auto load_x = [&](int j, int st, uint64_t *bar) {
-                // a second head that the group does not have: the first one again, its result unused
-                const int t = t_lo + j * kTile;
-                tma_load_4d(smem + Sm::X(st), &tm_x, bar, 0, h0, t, b);
-                tma_load_4d(smem + Sm::X(st) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
-            };
             auto load_bc = [&](const CUtensorMap *map, int j, uint32_t to, uint64_t *bar) {
                 for (int i = 0; i < kN / 64; ++i)
                     tma_load_4d(smem + to + i * kBlockBytes, map, bar, 64 * i, g, t_lo + j * kTile, b);
@@ -573,14 +570,12 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 umma_commit(&ms->bar[bEvY1]);
             };
             bool ok = true;
-            int xs = 0, bs = 0, cs = 0;  // tiles whose copies of X, B, C were issued (N = 128: all three, xs)
+            int bs = 0, cs = 0;  // tiles whose copies of B, C were issued (N = 128: of both, bs)
             if constexpr (Sm::kApart) {
-                auto next_x = [&]() { load_x(xs, xs % Sm::kXs, expect(bLdX + xs % Sm::kXs, kTileBytes)); ++xs; };
                 auto next_b = [&]() { load_bc(&tm_b, bs, Sm::B(bs & 1), expect(bLdB + (bs & 1), Sm::kOperand)); ++bs; };
                 auto next_c = [&]() { load_bc(&tm_c, cs, Sm::C(0), expect(bLdC, Sm::kOperand)); ++cs; };
-                if (tiles > 0) { next_c(); next_b(); next_x(); }
-                if (tiles > 1) { next_b(); next_x(); }
-                if (tiles > 2) next_x();
+                if (tiles > 0) { next_c(); next_b(); }
+                if (tiles > 1) next_b();
                 for (int j = 0; j < tiles; ++j) {
                     const int buf = j & 1, par = j & 1, xb = j % Sm::kXs;
                     if (!(ok = bar_wait(ms, bLdC, par, p) && bar_wait(ms, bLdB + buf, (j >> 1) & 1, p))) break;
@@ -595,29 +590,21 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     }
                     if (!(ok = bar_wait(ms, bEpW, par, p))) break;
                     output(buf, xb);
-                    if (j > 0 && xs < tiles) {  // the previous tile's output has left
-                        if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
-                        next_x();
-                    }
                 }
             } else {
                 auto next = [&]() {
-                    uint64_t *bar = expect(bLdX + (xs & 1), kTileBytes + 2 * Sm::kOperand);
-                    load_bc(&tm_b, xs, Sm::B(xs & 1), bar);
-                    load_bc(&tm_c, xs, Sm::C(xs & 1), bar);
-                    load_x(xs, xs & 1, bar);
-                    ++xs;
+                    uint64_t *bar = expect(bLdX + (bs & 1), 2 * Sm::kOperand);  // (X is the storing warp's)
+                    load_bc(&tm_b, bs, Sm::B(bs & 1), bar);
+                    load_bc(&tm_c, bs, Sm::C(bs & 1), bar);
+                    ++bs;
                 };
-                while (xs < 2 && xs < tiles) next();
+                while (bs < 2 && bs < tiles) next();
                 ok = tiles == 0 || bar_wait(ms, bLdX, 0, p);
                 for (int j = 0; ok && j < tiles; ++j) {
                     const int buf = j & 1, par = j & 1;
                     if (!(ok = bar_wait(ms, bEpE, par, p))) break;
                     scores(buf, buf);
-                    if (j > 0 && xs < tiles) {  // the previous tile's products are done and its output has left
-                        if (!(ok = bar_wait(ms, bXf, (j - 1) & 1, p))) break;
-                        next();
-                    }
+                    if (j > 0 && bs < tiles) next();  // the previous tile's (w X)^T B is done
                     if (!(ok = bar_wait(ms, bEpX, par, p))) break;
                     update(buf);
                     if (!(ok = bar_wait(ms, bEpW, par, p))) break;
@@ -628,11 +615,9 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if (!ok) {
                 // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
                 // TMEM are released
-                for (int j = max(xs - Sm::kXs, 0); j < xs; ++j) mbar_wait(&ms->bar[bLdX + j % Sm::kXs], (j / Sm::kXs) & 1, kBarWaitNs);
-                if (Sm::kApart) {
-                    for (int j = max(bs - 2, 0); j < bs; ++j) mbar_wait(&ms->bar[bLdB + (j & 1)], (j >> 1) & 1, kBarWaitNs);
-                    if (cs > 0) mbar_wait(&ms->bar[bLdC], (cs - 1) & 1, kBarWaitNs);
-                }
+                for (int j = max(bs - 2, 0); j < bs; ++j)
+                    mbar_wait(&ms->bar[(Sm::kApart ? bLdB : bLdX) + (j & 1)], (j >> 1) & 1, kBarWaitNs);
+                if (cs > 0) mbar_wait(&ms->bar[bLdC], (cs - 1) & 1, kBarWaitNs);
                 umma_commit(&ms->bar[bTear]);
                 mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
             }
@@ -640,16 +625,31 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         __syncwarp();
     } else if (warp == kStoreWarp) {
         if (lane == 0) {
-            for (int j = 0; j < tiles; ++j) {
-                const uint8_t *xs = smem + Sm::X(j % Sm::kXs);
+            // X's slots are this warp's: a tile's output leaves from one, and then the next X that goes there
+            // is sent for
+            int xs = 0, j = 0;
+            auto next_x = [&]() {
+                const int st = xs % Sm::kXs, t = t_lo + xs * kTile;
+                uint64_t *bar = &ms->bar[bLdX + st];
+                mbar_arrive_expect_tx(bar, kTileBytes);
+                // a second head that the group does not have: the first one again, its result unused
+                tma_load_4d(smem + Sm::X(st), &tm_x, bar, 0, h0, t, b);
+                tma_load_4d(smem + Sm::X(st) + kBlockBytes, &tm_x, bar, one ? 64 : 0, one || !both ? h0 : h0 + 1, t, b);
+                ++xs;
+            };
+            while (xs < Sm::kXs && xs < tiles) next_x();
+            for (; j < tiles; ++j) {
+                const uint8_t *from = smem + Sm::X(j % Sm::kXs);
                 const int t0 = t_lo + j * kTile;
                 if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
-                tma_store_4d(&tm_y, xs, 0, h0, t0, b);
-                if (both) tma_store_4d(&tm_y, xs + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
+                tma_store_4d(&tm_y, from, 0, h0, t0, b);
+                if (both) tma_store_4d(&tm_y, from + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
                 tma_store_commit();
                 tma_store_wait_read();
-                mbar_arrive(&ms->bar[bXf]);
+                if (xs < tiles) next_x();
             }
+            // (where a wait gave up) copies in flight finish, or a time limit, before shared memory is released
+            for (; j < tiles && j < xs; ++j) mbar_wait(&ms->bar[bLdX + j % Sm::kXs], (j / Sm::kXs) & 1, kBarWaitNs);
             tma_store_wait_all();
         }
         __syncwarp();
