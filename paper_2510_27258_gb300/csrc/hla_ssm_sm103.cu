@@ -35,11 +35,13 @@
 // N = 128 in H's slot) -> H'; the epilogue turns S into W while the tensor cores run (w X)^T B, puts the
 // new H down while they run W X, and writes the output while they run the next tile's C H.
 //
-// What bounds it: shared memory.  A tile of N = 128 takes about 5,200 cycles and moves 620 KB (the products'
-// operands 290, hi, lo and H 128, x and the output 128, copies 128 and more), 4,900 cycles at 128 bytes; one
-// of N <= 64 takes 4,600 and moves 470 KB, its epilogue warps never waiting for long.  Measured on a GB300: B8 n2048 H32 P64
-// G1 N128 53.3 us (42 % of what its bytes take), B1 n32768 H16 P64 G2 N64 68.1 us in three launches (the
-// state sweep 23, the chain 7, this kernel 42, each alone).
+// What bounds it: a tile of N = 128 takes about 5,200 cycles, the chain C H and S (1,250) -> hi, lo to their
+// slots (800) -> (w X)^T B (1,200) -> H' and W X (1,000; an MMA of 64 columns takes as long as one of 128)
+// with hand-offs of some 200 each, beside 620 KB through shared memory (4,900 cycles of it).  One of
+// N <= 64 takes 4,600, all of it the epilogue's work: hi, lo 1,300, W 1,100, output 700, H' 450, C H 150, the
+// rest hand-offs.  Measured on a GB300: B8 n2048 H32 P64 G1 N128 53.3 us (42 % of what its bytes take),
+// B1 n32768 H16 P64 G2 N64 68.1 us in three launches (the state sweep 23, the chain 7, this kernel 42,
+// each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
 // each segment's own state, chain_kernel the state before each segment.
