@@ -87,7 +87,7 @@ struct Misc {
     // sequence, first head, segment, whether the second 64 columns are a head of this group
     int b, h0, seg, both;
 };
-static_assert(sizeof(Misc) <= 3072, "fits beside the tiles");
+static_assert(sizeof(Misc) <= 3 * 1024, "fits beside the tiles");
 
 // shared-memory map for N <= 64 (kN = 64) and N = 128.  N <= 64 has room for H's copy and hi, lo apart.
 template <int kN>
