@@ -96,10 +96,12 @@ __device__ __forceinline__ Raw<T, V> load_row(const T *x, size_t stride, const T
 
 template <typename T, int W, int V, bool kSilu>
 __global__ void __launch_bounds__(kThreads)
-conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ bias,
-                    T *__restrict__ out, size_t xs, size_t os, const int *__restrict__ lengths, const T *state_in,
+conv_forward_kernel(Geom g, const T *x, const T *w, const T *bias,
+                    T *out, size_t xs, size_t os, const int *lengths, const T *state_in,
                     T *state_out) {
     __shared__ Raw<T, V> ring[kAhead][kThreads];
+    let_next_begin();
+    after_previous();
     const Place at = place<V>(g);
     if (at.c0 >= g.C) return;
     const int len = length_of(lengths, at.b, g.n);
@@ -165,8 +167,10 @@ conv_forward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, co
 // one token a sequence: out = act(bias + taps . [state, x]), the state shifted by one row in place
 template <typename T, int W, int V, bool kSilu>
 __global__ void __launch_bounds__(kThreads)
-conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, const T *__restrict__ bias, T *out,
-                 size_t xs, size_t os, T *__restrict__ state) {
+conv_step_kernel(long long units, int C, const T *x, const T *w, const T *bias, T *out,
+                 size_t xs, size_t os, T *state) {
+    let_next_begin();
+    after_previous();
     const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
     if (i >= units) return;
     const int per = C / V, c0 = (int)(i % per) * V;
@@ -201,9 +205,9 @@ conv_step_kernel(long long units, int C, const T *x, const T *__restrict__ w, co
 // equal inputs give equal bits.
 template <typename T, int W, int V, bool kSilu>
 __global__ void __launch_bounds__(kThreads)
-conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, const T *__restrict__ bias,
-                     const T *__restrict__ dout, T *__restrict__ dx, size_t xs, size_t gs, size_t ds,
-                     const int *__restrict__ lengths, float *__restrict__ partial) {
+conv_backward_kernel(Geom g, const T *x, const T *w, const T *bias,
+                     const T *dout, T *dx, size_t xs, size_t gs, size_t ds,
+                     const int *lengths, float *partial) {
     union Scratch {
         Raw<T, V> ring[2][kAheadBwd][kThreads];
         float red[kStrips][W + 1][V][32];
@@ -211,6 +215,7 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
     __shared__ Scratch sm;
     auto &red = sm.red;
     let_next_begin();
+    after_previous();
     const Place at = place<V>(g);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kP = (V + 1) / 2;
@@ -332,9 +337,10 @@ conv_backward_kernel(Geom g, const T *__restrict__ x, const T *__restrict__ w, c
 constexpr int kSumGroups = 16;
 template <int W>
 __global__ void __launch_bounds__(kSumGroups * 32)
-conv_sum_kernel(const float *__restrict__ partial, int rows, int C, float *__restrict__ dw, float *__restrict__ dbias,
+conv_sum_kernel(const float *partial, int rows, int C, float *dw, float *dbias,
                 WsHeader *header) {
     __shared__ float red[kSumGroups][32];
+    let_next_begin();
     after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
@@ -392,10 +398,9 @@ cudaError_t forward_as(const Conv &p, cudaStream_t s) {
     return by_width(p.width, [&](auto W) -> cudaError_t {
         const Geom g = geometry(p.B, p.n, p.C, V);
         const unsigned blocks = (unsigned)g.cblocks * g.tblocks * p.B;
-        conv_forward_kernel<T, W(), V, kSilu><<<blocks, kThreads, 0, s>>>(
+        return launch_after(conv_forward_kernel<T, W(), V, kSilu>, blocks, kThreads, 0, s,
             g, (const T *)p.x, (const T *)p.w, (const T *)p.bias, (T *)p.out, p.x_stride, p.out_stride, p.lengths,
             (const T *)p.state_in, (T *)p.state_out);
-        return cudaGetLastError();
     });
 }
 
@@ -403,10 +408,9 @@ template <typename T, int V, bool kSilu>
 cudaError_t step_as(const Conv &p, cudaStream_t s) {
     return by_width(p.width, [&](auto W) -> cudaError_t {
         const long long units = (long long)p.B * (p.C / V);
-        conv_step_kernel<T, W(), V, kSilu><<<ceil_div(units, kThreads), kThreads, 0, s>>>(
+        return launch_after(conv_step_kernel<T, W(), V, kSilu>, ceil_div(units, kThreads), kThreads, 0, s,
             units, p.C, (const T *)p.x, (const T *)p.w, (const T *)p.bias, (T *)p.out, p.x_stride, p.out_stride,
             (T *)p.state_out);
-        return cudaGetLastError();
     });
 }
 
@@ -415,10 +419,9 @@ cudaError_t backward_as(const ConvBwd &p, cudaStream_t s) {
     return by_width(p.width, [&](auto W) -> cudaError_t {
         const Geom g = geometry(p.B, p.n, p.C, V);
         const int rows = g.tblocks * p.B;
-        conv_backward_kernel<T, W(), V, kSilu><<<(unsigned)g.cblocks * rows, kThreads, 0, s>>>(
+        cudaError_t e = launch_after(conv_backward_kernel<T, W(), V, kSilu>, (unsigned)g.cblocks * rows, kThreads, 0, s,
             g, (const T *)p.x, (const T *)p.w, (const T *)p.bias, (const T *)p.dout, (T *)p.dx, p.x_stride,
             p.dout_stride, p.dx_stride, p.lengths, p.partial);
-        cudaError_t e = cudaGetLastError();
         if (e) return e;
         return launch_after(conv_sum_kernel<W()>, ceil_div((long long)(W() + 1) * p.C, 32), kSumGroups * 32, 0, s,
                             p.partial, rows, p.C, p.dw, p.dbias, p.header);

@@ -121,21 +121,26 @@ int hla3_tc_launches(int BH, int n);
 cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 
 // ---------------------------------------------------------------------------
-// Dependent launches inside one entry point: a kernel launched by launch_after may begin while the one
-// before it in the stream ends (its launch and set-up overlap with it), and waits with after_previous()
-// before it reads or writes anything that kernel, or one before it, reads or writes.  The earlier kernel
-// says let_next_begin() once; without it the next one begins when it has ended.
+// Dependent launches: a kernel launched by launch_after may begin while the one before it in the stream
+// ends (its launch and set-up overlap with it), and waits with after_previous() before it reads or writes
+// anything that kernel, or one before it, reads or writes.  The earlier kernel says let_next_begin();
+// without it (other libraries' kernels) the next one begins when it has ended.
+// A kernel has ended only when it has waited for those before it: every thread calls after_previous(), at
+// the start wherever it is an entry point's first kernel.  A kernel that reads its inputs before it waits
+// (ssm_tc_kernel behind its segments' states) comes behind one that was launched without this.
+// What earlier kernels write is not read through const __restrict__ pointers, whose loads may be taken for
+// those of data that does not change while the kernel is there.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename... P, typename... A>
-cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream, A... args) {
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, A... args) {
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;

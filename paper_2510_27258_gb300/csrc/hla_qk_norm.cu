@@ -161,6 +161,8 @@ struct Split {
 template <typename T, int D, bool kInter, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBlocksFwd) qk_norm_forward_kernel(QkNorm p, Split sp) {
     constexpr int kLanes = D / 8, kRows = kThreads / kLanes;
+    let_next_begin();
+    after_previous();
     const Runs at = runs_of<D, kInter>(threadIdx.x % kLanes, p.rot);
     const unsigned row = blockIdx.x * kRows + threadIdx.x / kLanes, rows = (unsigned)p.B * p.n;  // below 2^31
     // rows past the end repeat the last one without storing: every lane joins the shuffles
@@ -243,6 +245,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
     };
     __shared__ Scratch sm;
     let_next_begin();
+    after_previous();
     auto &ring = sm.ring;
     auto &red = sm.red;
     const QkNorm &f = p.f;
@@ -386,8 +389,9 @@ __global__ void __launch_bounds__(kThreads, kBlocksBwd) qk_norm_backward_kernel(
 constexpr int kSumThreads = 1024, kSumGroups = kSumThreads / 8;
 
 __global__ void __launch_bounds__(kSumThreads)
-qk_norm_sum_kernel(const float *__restrict__ partial, int rows, int d, float *dwq, float *dwk, WsHeader *header) {
+qk_norm_sum_kernel(const float *partial, int rows, int d, float *dwq, float *dwk, WsHeader *header) {
     __shared__ float red[32][kSumGroups + 1];
+    let_next_begin();
     after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
     const int quad = threadIdx.x & 7, group = threadIdx.x >> 3;  // (2 d is a multiple of 32)
@@ -449,8 +453,7 @@ template <typename T, bool kInter, bool kVec>
 cudaError_t forward_as(const QkNorm &p, cudaStream_t s) {
     return by_size(p.d, [&](auto D) -> cudaError_t {
         const Plan g = plan((long long)p.B * p.n, p.H + p.Hk, kThreads / (D() / 8), kBlocksFwd);
-        qk_norm_forward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
-        return cudaGetLastError();
+        return launch_after(qk_norm_forward_kernel<T, D(), kInter, kVec>, dim3(g.gx, g.gy), kThreads, 0, s, p, g.sp);
     });
 }
 
@@ -458,8 +461,7 @@ template <typename T, bool kInter, bool kVec>
 cudaError_t backward_as(const QkNormBwd &p, cudaStream_t s) {
     return by_size(p.f.d, [&](auto D) -> cudaError_t {
         const Plan g = plan((long long)p.f.B * p.f.n, p.f.H + p.f.Hk, kThreads / (D() / 8), kBlocksBwd);
-        qk_norm_backward_kernel<T, D(), kInter, kVec><<<dim3(g.gx, g.gy), kThreads, 0, s>>>(p, g.sp);
-        cudaError_t e = cudaGetLastError();
+        cudaError_t e = launch_after(qk_norm_backward_kernel<T, D(), kInter, kVec>, dim3(g.gx, g.gy), kThreads, 0, s, p, g.sp);
         if (e) return e;
         return launch_after(qk_norm_sum_kernel, 2 * p.f.d / 32, kSumThreads, 0, s, p.partial, (int)(g.gx * g.gy), p.f.d,
                             p.dwq, p.dwk, p.header);

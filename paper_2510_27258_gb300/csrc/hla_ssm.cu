@@ -217,6 +217,8 @@ __global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(Ssm p) {
     constexpr int kQuads = kC / 4, kRows = kStepThreads / kQuads;
     __shared__ float4 red[kRows][kQuads];
     __shared__ float bs[128], cs[128];
+    let_next_begin();
+    after_previous();
     const int slices = p.P / kC, head = blockIdx.x / slices, c0 = (blockIdx.x % slices) * kC;
     const int b = head / p.H, h = head % p.H, g = h / (p.H / p.G), tid = threadIdx.x;
     const int quad = tid % kQuads, row = tid / kQuads;
@@ -318,10 +320,8 @@ cudaError_t step_of(const Ssm &p, cudaStream_t s) {
     // 16 columns a block (64-byte rows of the state) where whole heads would leave SMs without work
     const long long BH = (long long)p.B * p.H;
     if (p.P == 16 || p.P == 32 || BH < 152 * 2)
-        ssm_step_kernel<T, 16><<<(unsigned)(BH * (p.P / 16)), kStepThreads, 0, s>>>(p);
-    else
-        ssm_step_kernel<T, 64><<<(unsigned)(BH * (p.P / 64)), kStepThreads, 0, s>>>(p);
-    return cudaGetLastError();
+        return launch_after(ssm_step_kernel<T, 16>, (unsigned)(BH * (p.P / 16)), kStepThreads, 0, s, p);
+    return launch_after(ssm_step_kernel<T, 64>, (unsigned)(BH * (p.P / 64)), kStepThreads, 0, s, p);
 }
 
 }  // namespace

@@ -417,6 +417,77 @@ def test_in_a_cuda_graph(hla):
             assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("B,n,H,Hk,d", [(1, 8, 2, 1, 64), (2, 300, 8, 4, 64), (4, 1024, 16, 16, 128)])
+def test_calls_in_a_row(hla, captured, B, n, H, Hk, d):
+    """Calls begin while those before them end: chains of calls through the same few buffers, with other
+    kernels, a fill and another stream's work between them, give what they give with a wait after each."""
+    T, C = torch.bfloat16, (H + Hk) * d
+    g = torch.Generator(device=DEV).manual_seed(7)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    x0, w, token0 = rand(B, n, C).to(T), (rand(C, 4) / 2).to(T), rand(B, C).to(T)
+    delta, bm, a = rand(B, H).to(T), rand(B, 1, d).to(T), -rand(H).abs()
+    x, y, dx = (torch.empty(B, n, C, dtype=T, device=DEV) for _ in range(3))
+    token, conv_state, state = torch.empty_like(token0), torch.empty(B, 3, C, dtype=T, device=DEV), torch.empty(B, H, d, d, device=DEV)
+    qo, ko = (torch.empty(B, H, n, d, dtype=T, device=DEV) for _ in range(2))
+    tok_out = torch.empty(B, H, d, dtype=T, device=DEV)
+    ws = [torch.empty(max(hla.hla_conv_backward_workspace_bytes(B, n, C, 4, T),
+                          hla.hla_qk_norm_backward_workspace_bytes(B, n, H, Hk, d, T)), dtype=torch.uint8, device=DEV)]
+    heads = lambda t: (t[..., :H * d].unflatten(-1, (H, d)), t[..., H * d:].unflatten(-1, (Hk, d)))
+    side = torch.cuda.Stream()
+
+    def chain(wait):
+        kept = []
+
+        def did(*results):
+            wait()
+            kept.extend(results)
+
+        x.copy_(x0), token.copy_(token0), conv_state.zero_(), state.zero_()
+        did()
+        for _ in range(3):
+            hla.hla_conv_forward(x, w, out=y)
+            did()
+            hla.hla_qk_norm_forward(*heads(y), q_out=qo, k_out=ko)
+            did()
+            dq, dk, _, _ = hla.hla_qk_norm_backward(*heads(y), None, None, None, None, ko, qo, workspace=ws[0])
+            did()
+            dx.zero_()
+            hla.hla_conv_backward(x, w, y, dx=dx, workspace=ws[0])
+            did()
+            torch.add(x, dx, out=x)  # what the calls before it read
+            x.clamp_(-4, 4)
+            did(dq.clone(), dk.clone())
+            for _ in range(3):
+                hla.hla_conv_step(token, w, conv_state, out=token)
+                did()
+                hla.hla_ssm_step(token[:, :H * d].unflatten(-1, (H, d)), delta, a, bm, bm, state, tok_out)
+                did()
+                token[:, :H * d].copy_(tok_out.flatten(1))
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                token.clamp_(-2, 2)
+            torch.cuda.current_stream().wait_stream(side)
+            hla.hla_conv_step(token, w, conv_state, out=token)
+            did(qo.clone(), ko.clone(), token.clone())
+        return kept + [x, state, conv_state]
+
+    want = [t.clone() for t in chain(torch.cuda.synchronize)]
+    torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = chain(lambda: None)
+    for _ in range(5):
+        if captured:
+            graph.replay()
+        else:
+            got = chain(lambda: None)
+        torch.cuda.synchronize()
+        for p, r in zip(got, want):
+            assert torch.equal(p, r)
+
+
 def test_rows_beyond_32_bit_offsets(hla):
     """Row offsets past 2^31 elements: the last rows equal those of a compact copy."""
     n, C, stride, T = 33000, 64, 1 << 16, torch.bfloat16  # 2.16e9 elements, 4.3 GB
