@@ -45,6 +45,8 @@ template <typename T, int N, bool kStateOnly>
 __global__ void __launch_bounds__(kScanThreads)
 scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay) {
     constexpr int NS = N / kLanes;
+    if (kStateOnly || segments == 1) after_previous();
+    let_next_begin();
     __shared__ __align__(16) float bs[kTok][N], cs[kTok][N];
     __shared__ float xs[kTok][kCols], ys[kTok][kCols], decay[kTok], dl[kTok], la_sum;
     const int slices = p.P / kCols;
@@ -62,7 +64,6 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
     T *y = static_cast<T *>(p.y) + (size_t)b * p.n * p.y_stride + h * p.P + slice * kCols;
     const float a = p.a[h], bias = p.delta_bias ? p.delta_bias[h] : 0.f, skip = p.skip ? p.skip[h] : 0.f;
 
-    if (kStateOnly) let_next_begin();
     if (!kStateOnly && segments > 1) after_previous();
     float st[NS];
     const float *from = kStateOnly ? nullptr
@@ -293,16 +294,15 @@ cudaError_t scan_as(const Ssm &p, cudaStream_t s) {
     float *decay = state + BH * segments * NP;
     const unsigned per = (unsigned)(BH * (p.P / kCols));
     if (segments > 1) {
-        scan_kernel<T, N, true><<<per * (segments - 1), kScanThreads, 0, s>>>(p, segments, seg_len, state, decay);
-        cudaError_t e = cudaGetLastError();
+        cudaError_t e = launch_after(scan_kernel<T, N, true>, per * (segments - 1), kScanThreads, 0, s, p, segments,
+                                     seg_len, state, decay);
         if (e) return e;
         e = ssm_chain_launch(p.state_in, state, decay, BH, (int)NP, segments, s);
         if (e) return e;
         return launch_after(scan_kernel<T, N, false>, per * segments, kScanThreads, 0, s, p, segments, seg_len, state,
                             decay);
     }
-    scan_kernel<T, N, false><<<per, kScanThreads, 0, s>>>(p, 1, seg_len, state, decay);
-    return cudaGetLastError();
+    return launch_after(scan_kernel<T, N, false>, per, kScanThreads, 0, s, p, 1, seg_len, state, decay);
 }
 
 template <typename T>

@@ -333,8 +333,9 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
     StateMisc *ms = reinterpret_cast<StateMisc *>(smem + Sm::kEnd);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kEpiWarps;
-    const Unit u = unit_of(p);
+    after_previous();
     let_next_begin();
+    const Unit u = unit_of(p);
 
     if (blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
     if (smem_u32(smem) & 1023u) {                          // the tile layout needs 1 KiB alignment
@@ -503,6 +504,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kIssuerWarp;
 
+    if (p.segments == 1) after_previous();
+    let_next_begin();
     const Unit u = unit_of(p);
     const int b = u.b, g = u.g, h0 = u.h0, seg = u.seg, t_lo = u.t_lo, live = u.live, tiles = u.tiles;
     const bool one = u.one, both = u.both;
@@ -1079,9 +1082,7 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     auto launch = [&](auto kern, int blocks, uint32_t smem) -> cudaError_t {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e) return e;
-        if (c.segments > 1) return launch_after(kern, blocks, kThreads, smem, stream, mx, mb, mc, my, q);
-        kern<<<blocks, kThreads, smem, stream>>>(mx, mb, mc, my, q);
-        return cudaGetLastError();
+        return launch_after(kern, blocks, kThreads, smem, stream, mx, mb, mc, my, q);
     };
     const bool wide = p.N == 128;
     if (c.segments > 1) {
@@ -1089,8 +1090,7 @@ cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
         auto run = [&](auto kern, uint32_t smem) -> cudaError_t {
             cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e) return e;
-            kern<<<blocks, kStateThreads, smem, stream>>>(mx, mb, q);
-            return cudaGetLastError();
+            return launch_after(kern, blocks, kStateThreads, smem, stream, mx, mb, q);
         };
         constexpr uint32_t kMisc = sizeof(StateMisc);
         cudaError_t e = wide ? run(ssm_state_kernel<128>, StateMap<128>::kEnd + kMisc)

@@ -488,6 +488,52 @@ def test_calls_in_a_row(hla, captured, B, n, H, Hk, d):
             assert torch.equal(p, r)
 
 
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("B,n,H,P,N,T", [(1, 3000, 2, 64, 64, torch.bfloat16), (4, 300, 32, 64, 128, torch.bfloat16),
+                                         (1, 700, 2, 32, 16, torch.float32), (8, 40, 40, 16, 32, torch.float32)])
+def test_scans_in_a_row(hla, captured, B, n, H, P, N, T):
+    """The same for scans (one launch, or segments) whose inputs and states the calls before them write."""
+    x0, delta, a, b, c, skip, bias, _, _ = (None if t is None else t.to(DEV) for t in
+                                            ssm_case(33, B, n, H, P, 1, N, T, False))
+    w = torch.randn(H * P, 4, generator=gen(3)).to(DEV).to(T)
+    ws = torch.empty(hla.hla_ssm_workspace_bytes(B, n, H, P, 1, N, T), dtype=torch.uint8, device=DEV)
+    x, y, state = torch.empty_like(x0), torch.empty_like(x0), torch.empty(B, H, N, P, device=DEV)
+
+    def chain(wait):
+        kept = []
+        x.copy_(x0), state.zero_()
+        wait()
+        for _ in range(4):
+            hla.hla_conv_forward(x.flatten(2), w, out=y.flatten(2))
+            wait()
+            hla.hla_ssm_forward(y, delta, a, b, c, out=x, state_in=state, state_out=state, workspace=ws)
+            wait()
+            hla.hla_ssm_step(x[:, -1], delta[:, -1], a, b[:, -1], c[:, -1], state, y[:, 0].contiguous())
+            wait()
+            hla.hla_ssm_forward(x, delta, a, b, c, out=y, state_in=state, state_out=state, workspace=ws)
+            wait()
+            x.copy_(y).clamp_(-2, 2)
+            state.mul_(0.5)
+            kept += [y.clone(), state.clone()]
+            wait()
+        return kept
+
+    want = chain(torch.cuda.synchronize)
+    torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = chain(lambda: None)
+    for _ in range(5):
+        if captured:
+            graph.replay()
+        else:
+            got = chain(lambda: None)
+        torch.cuda.synchronize()
+        for p, r in zip(got, want):
+            assert torch.equal(p, r)
+
+
 def test_rows_beyond_32_bit_offsets(hla):
     """Row offsets past 2^31 elements: the last rows equal those of a compact copy."""
     n, C, stride, T = 33000, 64, 1 << 16, torch.bfloat16  # 2.16e9 elements, 4.3 GB
