@@ -16,8 +16,8 @@
 // walks through the heads of its token with the next heads' rows in flight.  Statistics and products
 // are fp32; each output is rounded once.
 //
-// Measured on a GB300: forward, B8 n2048 H16 Hk16 d64 bf16, 26.4 us a pass (5.1 TB/s), gradient with
-// Hk4, 35.7 us (4.2 TB/s).
+// Measured on a GB300: forward, B8 n2048 H16 Hk16 d64 bf16, 25.6 us a pass (5.3 TB/s), gradient with
+// Hk4, 33.5 us (4.5 TB/s).
 #include <type_traits>
 
 #include "hla_vec.cuh"

@@ -12,8 +12,8 @@
 // (state only), the segments' states are chained, and the scan proper starts each segment from its
 // state.  All of it is fp32, with no rounding between the tokens and the outputs.
 //
-// Measured on a GB300: step, B64 H32 P64 N128, 24.6 us a pass (5.5 TB/s); B3 n517 H6 P32 N16 fp32,
-// 16.9 us (three launches of 48 tokens' latency each).
+// Measured on a GB300: step, B64 H32 P64 N128, 21.7 us a pass (6.2 TB/s); B3 n517 H6 P32 N16 fp32,
+// 14.1 us on the device (three launches of 48 tokens' latency each).
 #include "hla_vec.cuh"
 
 namespace hla {
