@@ -16,7 +16,7 @@
 // walks through the heads of its token with the next heads' rows in flight.  Statistics and products
 // are fp32; each output is rounded once.
 //
-// Measured on a GB300: forward, B8 n2048 H16 Hk16 d64 bf16, 25.6 us a pass (5.3 TB/s), gradient with
+// Measured on a GB300: forward, B8 n2048 H16 Hk16 d64 bf16, 24.2 us a pass (5.6 TB/s), gradient with
 // Hk4, 33.5 us (4.5 TB/s).
 #include <type_traits>
 
@@ -27,7 +27,9 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kAhead = 4, kAheadBwd = 4;       // rows a thread has in flight
-constexpr int kBlocksFwd = 8, kBlocksBwd = 5;  // blocks of an SM at a time
+// blocks of an SM at a time (forward with 8, whose 64 registers spill more for fp32: 29.9 instead of 25.6 us for
+// B4 n2048 H16 d64 fp32; with 6 29.6 instead of 24.2 us for the bf16 case above)
+constexpr int kBlocksFwd = 7, kBlocksBwd = 5;
 
 // four elements at p: one access, or element by element where rows are not aligned to it
 template <typename T, bool kVec>
