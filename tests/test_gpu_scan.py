@@ -1,0 +1,84 @@
+"""The selective scan on the GPU where its tiles and segments depend on one another, against the 64-bit recurrence:
+slow decays and large states over many tiles.
+
+b, c, x, skip and the states are positive here, so that a sum's value is the magnitude its rounding errors scale
+with: a bound of a few 2^-8 resolves a carried part of one percent."""
+import pytest
+import torch
+
+import layer_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U16, U32 = 2.0 ** -8, 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+TILE = 128
+
+
+@pytest.fixture(scope="module")
+def hla():
+    from paper_2510_27258_gb300 import build
+    build.build()
+    from paper_2510_27258_gb300 import hla as binding
+    return binding
+
+
+def near(got, want, bound):
+    excess = (got.double() - want).abs() - bound
+    assert torch.isfinite(got).all()
+    assert float(excess.max()) <= 0, (float(excess.max()), float((got - want).abs().max()))
+
+
+def positive(g, *shape, T=torch.float32):
+    return torch.rand(*shape, generator=g, device=DEV).add_(0.1).to(T)
+
+
+def inputs(seed, B, n, H, P, G, N, T):
+    """x, delta, a, b, c, skip, state: steps of softplus(delta - 6), about 2.5e-3, and a in -2 .. -0.5, so that a
+    head forgets over hundreds of tokens."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x, b, c = positive(g, B, n, H, P, T=T), positive(g, B, n, G, N, T=T), positive(g, B, n, G, N, T=T)
+    delta = (torch.randn(B, n, H, generator=g, device=DEV) * 0.5).to(T)
+    a = -0.5 - 1.5 * torch.rand(H, generator=g, device=DEV)
+    return x, delta, a, b, c, positive(g, H), 4 * positive(g, B, H, N, P)
+
+
+def reference(*args, **kw):
+    with torch.device(DEV):
+        return R.ssm(*args, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,H,P,G,N,lens,cuts", [
+    (2, 890, 3, 64, 1, 128, [890, 700], (1, 7)),        # tiles of one CTA
+    (2, 1100, 152, 64, 1, 64, [900, 1100], (1, 9)),
+    (1, 3015, 76, 64, 2, 64, None, (4, 6)),             # segments of several tiles
+    (1, 3015, 76, 64, 1, 128, None, (4, 6)),
+    (1, 2048, 38, 128, 2, 32, None, (4, 4)),
+    (1, 2048, 38, 128, 1, 128, None, (4, 4)),
+    (2, 3000, 38, 64, 1, 128, [3000, 1037], (4, 6)),    # ... of which some count in part, or not at all
+    (2, 3000, 19, 128, 1, 16, [130, 2999], (4, 6))])
+def test_a_state_carried_over_tiles_and_segments(hla, dtype, B, n, H, P, G, N, lens, cuts):
+    """Rounding of the state of bf16 tokens: w X as bf16 pairs (2^-16); exponents of up to 16 (what lies further back
+    weighs nothing) whose steps and sums are good to 2^-21; and for each tile 32 accumulations of 2^-23 and the
+    tile's decay."""
+    T = TYPES[dtype]
+    if T == torch.bfloat16:
+        segments, tiles = cuts
+        assert segments * tiles * TILE >= n > (segments - 1) * tiles * TILE
+        assert hla.hla_ssm_forward_path(B, n, H, P, G, N) == (1, 1 if segments == 1 else 3)
+        if segments > 1:  # the workspace holds a state for each
+            assert hla.hla_ssm_workspace_bytes(B, n, H, P, G, N, T) // (4 * B * H * (N * P + 1)) == segments
+    x, delta, a, b, c, skip, state = inputs(n + N, B, n, H, P, G, N, T)
+    bias = torch.full((H,), -6.0, device=DEV)
+    lengths = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    y, h, ym, hm = reference(x, delta, a, b, c, skip, bias, True, lengths, state)
+    st = state.clone()
+    out = hla.hla_ssm_forward(x, delta, a, b, c, skip=skip, delta_bias=bias, lengths=lengths, state_in=st, state_out=st)
+    if T == torch.bfloat16:
+        rel = 2.0 ** -16 + 16 * 2.0 ** -21 + 64 * (n / TILE + 2) * U32
+        near(out, y, U16 * y.abs() + (2 * U16 + rel) * ym)
+    else:
+        rel = (6 * n + 2 * N + 64) * U32
+        near(out, y, rel * ym)
+    near(st, h, rel * hm)
