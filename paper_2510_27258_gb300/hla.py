@@ -165,6 +165,50 @@ def alloc_workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
+def _on(stream, index):
+    """(handle, side): the stream to run on, the caller's or GPU `index`'s current one; `side` is that stream as
+    an object where it is not the current one, else None."""
+    current = torch._C._cuda_getCurrentRawStream(index)  # current_stream(index).cuda_stream without the object
+    if stream is None:
+        return current, None
+    handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if getattr(stream, "device_index", index) != index:
+        raise ValueError("the stream is cuda:%d's, the tensors are on cuda:%d" % (stream.device_index, index))
+    if handle == current:
+        return handle, None
+    if not isinstance(stream, torch.cuda.Stream):
+        # (0 and 1 both name the default stream)
+        stream = torch.cuda.ExternalStream(handle, index) if handle > 1 else torch.cuda.default_stream(index)
+    return handle, stream
+
+
+def _on_gpu_of(t, stream):
+    """_on for the GPU a tensor is on."""
+    index = t.get_device()
+    return _on(stream, index if index >= 0 else torch.cuda.current_device())
+
+
+def _empty(shape, dtype, device, side):
+    """A new output tensor.  Where the call runs on another stream than the current one it is that stream's memory
+    (what is the current stream's may still be in use there), and is kept for the current one, where the caller may
+    read it, when it is released."""
+    if side is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(side):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(nbytes, device, side):
+    """alloc_workspace for the stream the call runs on: it is released when the call returns, and then goes to work
+    that comes later on that stream, not on the current one."""
+    if side is None:
+        return alloc_workspace(nbytes, device)
+    with torch.cuda.stream(side):
+        return alloc_workspace(nbytes, device)
+
+
 def _forward(fn_name, ws_fn, q, k, v, out, masked, normalized, eps, chunk, state_in, state_out, workspace, stream):
     if q.dim() != 4:
         raise ValueError("q, k, v must be [B, H, n, d]")
@@ -175,14 +219,15 @@ def _forward(fn_name, ws_fn, q, k, v, out, masked, normalized, eps, chunk, state
     for t in (q, k, v):
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, n, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, n, dv), q.dtype, q.device, side)
     dt = _dtype_code(q)
     if workspace is None:
-        workspace = alloc_workspace(ws_fn(B, H, n, d, dv, chunk, dt), q.device)
+        workspace = _workspace(ws_fn(B, H, n, d, dv, chunk, dt), q.device, side)
     code = getattr(lib(), fn_name)(_ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(masked),
                                    int(normalized), float(eps), int(chunk), _ptr(state_in), _ptr(state_out),
-                                   _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
+                                   _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
     _check(code, fn_name)
     return out
 
@@ -208,11 +253,11 @@ def hla2_forward_noalloc(q, k, v, out=None, *, masked=True, normalized=False, ep
     hla2_forward_noalloc).  Returns ``out``."""
     B, H, n, d = q.shape
     dv = v.shape[-1]
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, n, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, n, dv), q.dtype, q.device, side)
     code = lib().hla2_forward_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, n, d, dv,
-                                      int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in),
-                                      _stream(stream))
+                                      int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in), handle)
     _check(code, "hla2_forward_noalloc")
     return out
 
@@ -245,12 +290,13 @@ def hla2_step(q, k, v, state, out=None, *, masked=True, normalized=False, eps=1e
     """
     B, H, d = q.shape
     dv = v.shape[-1]
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
     code = lib().hla2_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(masked),
-                           int(normalized), float(eps), _ptr(state), _stream(stream))
+                           int(normalized), float(eps), _ptr(state), handle)
     _check(code, "hla2_step")
     return out
 
@@ -269,12 +315,13 @@ def hla2_backward(q, k, v, dout, *, normalized=False, eps=1e-6, chunk=64, worksp
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v, dout must be contiguous CUDA tensors of one dtype")
     dt = _dtype_code(q)
-    gq, gk, gv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    handle, side = _on_gpu_of(q, stream)
+    gq, gk, gv = (_empty(t.shape, t.dtype, t.device, side) for t in (q, k, v))
     if workspace is None:
-        workspace = alloc_workspace(hla2_backward_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device)
+        workspace = _workspace(hla2_backward_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
     code = lib().hla2_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(gq), _ptr(gk), _ptr(gv), dt, B, H, n, d,
                                dv, int(normalized), float(eps), int(chunk), _ptr(workspace),
-                               workspace.numel() * workspace.element_size(), _stream(stream))
+                               workspace.numel() * workspace.element_size(), handle)
     _check(code, "hla2_backward")
     return gq, gk, gv
 
@@ -298,14 +345,15 @@ def ahla_forward(q, k, v, out=None, *, normalized=False, eps=1e-6, chunk=64, sta
     for t in (q, k, v):
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, n, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, n, dv), q.dtype, q.device, side)
     dt = _dtype_code(q)
     if workspace is None:
-        workspace = alloc_workspace(ahla_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device)
+        workspace = _workspace(ahla_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
     code = lib().ahla_forward(_ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(normalized), float(eps),
                               int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace),
-                              workspace.numel() * workspace.element_size(), _stream(stream))
+                              workspace.numel() * workspace.element_size(), handle)
     _check(code, "ahla_forward")
     return out
 
@@ -328,12 +376,13 @@ def ahla_step(q, k, v, state, out=None, *, normalized=False, eps=1e-6, stream=No
     """One AHLA decode step for every head (include/hla.h: ahla_step); ``state`` is updated in place."""
     B, H, d = q.shape
     dv = v.shape[-1]
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
     code = lib().ahla_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-                           float(eps), _ptr(state), _stream(stream))
+                           float(eps), _ptr(state), handle)
     _check(code, "ahla_step")
     return out
 
@@ -346,9 +395,10 @@ def hla2_state_to_sde(state, d: int, dv: int, sde=None, *, stream=None):
     """(S, C, m, G, h) tuples [B, H, hla2_state_floats(d, dv)] -> (S, D, e) states
     [B, H, hla2_sde_state_floats(d, dv)] (include/hla.h: hla2_state_to_sde)."""
     B, H = state.shape[:2]
+    handle, side = _on_gpu_of(state, stream)
     if sde is None:
-        sde = torch.empty((B, H, hla2_sde_state_floats(d, dv)), dtype=torch.float32, device=state.device)
-    _check(lib().hla2_state_to_sde(_ptr(state), _ptr(sde), B, H, d, dv, _stream(stream)), "hla2_state_to_sde")
+        sde = _empty((B, H, hla2_sde_state_floats(d, dv)), torch.float32, state.device, side)
+    _check(lib().hla2_state_to_sde(_ptr(state), _ptr(sde), B, H, d, dv, handle), "hla2_state_to_sde")
     return sde
 
 
@@ -357,12 +407,13 @@ def hla2_step_sde(q, k, v, sde, out=None, *, normalized=False, eps=1e-6, stream=
     (include/hla.h: hla2_step_sde).  q, k: [B, H, d]; v: [B, H, dv]."""
     B, H, d = q.shape
     dv = v.shape[-1]
+    handle, side = _on_gpu_of(q, stream)
     if out is None:
-        out = torch.empty((B, H, dv), dtype=q.dtype, device=q.device)
+        out = _empty((B, H, dv), q.dtype, q.device, side)
     if sde.dtype != torch.float32 or not sde.is_contiguous():
         raise ValueError("state must be contiguous float32")
     code = lib().hla2_step_sde(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-                               float(eps), _ptr(sde), _stream(stream))
+                               float(eps), _ptr(sde), handle)
     _check(code, "hla2_step_sde")
     return out
 
@@ -449,17 +500,10 @@ def _gpu(t):
     return index
 
 
-def _on(stream, index):
-    """Handle of the stream to run on: the caller's, or GPU `index`'s current one."""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(index)  # current_stream(index).cuda_stream without the object
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-
-
-def _scratch(workspace, need, index, *sizes):
+def _scratch(workspace, need, index, side, *sizes):
     """(address, bytes, tensor) of the caller's workspace, or of a new one of need(*sizes) bytes."""
     if workspace is None:
-        workspace = alloc_workspace(need(*sizes), torch.device("cuda", index))
+        workspace = _workspace(need(*sizes), torch.device("cuda", index), side)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on cuda:%d" % index)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
@@ -480,15 +524,16 @@ def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None,
     states: [B, width - 1, C] (state_out may be state_in).
     """
     shape, W, dt, T, i = _conv_sizes(x, weight, 3)
+    handle, side = _on(stream, i)
     B, n, C = shape
     if out is None:
-        out = torch.empty(shape, dtype=T, device=x.device)
+        out = _empty(shape, T, x.device, side)
     kept = B * (W - 1) * C
     _check(lib().hla_conv_forward(
         x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, n, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
         _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, T, i),
-        _flat("state_out", state_out, kept, T, i), _on(stream, i)), "hla_conv_forward")
+        _flat("state_out", state_out, kept, T, i), handle), "hla_conv_forward")
     return out
 
 
@@ -496,13 +541,14 @@ def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=No
     """One token a sequence of hla_conv_forward (include/hla.h: hla_conv_step); ``state`` [B, width - 1, C] is
     updated in place.  x: [B, C]; ``out`` may be ``x``."""
     shape, W, dt, T, i = _conv_sizes(x, weight, 2)
+    handle, side = _on(stream, i)
     B, C = shape
     if out is None:
-        out = torch.empty(shape, dtype=T, device=x.device)
+        out = _empty(shape, T, x.device, side)
     _check(lib().hla_conv_step(
         x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("state", state, B * (W - 1) * C, T, i), _on(stream, i)), "hla_conv_step")
+        _flat("state", state, B * (W - 1) * C, T, i), handle), "hla_conv_step")
     return out
 
 
@@ -514,17 +560,18 @@ def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths
     """Gradients (dx, dweight, dbias) of sum(dout * out) for hla_conv_forward from a zero state
     (include/hla.h: hla_conv_backward); the weights' are fp32, dbias is None where bias is."""
     shape, W, dt, T, i = _conv_sizes(x, weight, 3)
+    handle, side = _on(stream, i)
     B, n, C = shape
     if dx is None:
-        dx = torch.empty(shape, dtype=T, device=x.device)
-    dw = torch.empty((C, W), dtype=torch.float32, device=x.device)
-    db = None if bias is None else torch.empty((C,), dtype=torch.float32, device=x.device)
-    ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, B, n, C, W, dt)
+        dx = _empty(shape, T, x.device, side)
+    dw = _empty((C, W), torch.float32, x.device, side)
+    db = None if bias is None else _empty((C,), torch.float32, x.device, side)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, side, B, n, C, W, dt)
     _check(lib().hla_conv_backward(
         x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), dout.data_ptr(), dx.data_ptr(),
         dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i),
         _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, _on(stream, i)), "hla_conv_backward")
+        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, handle), "hla_conv_backward")
     return dx, dw, db
 
 
@@ -542,20 +589,21 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
     if x.dim() != 4 or b.dim() != 4:
         raise ValueError("x must be [B, n, H, P] and b [B, n, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
     T, i, shape = x.dtype, _gpu(x), x.shape
+    handle, side = _on(stream, i)
     B, n, H, P = shape
     G, N = b.shape[2:]
     dt, f32 = _type_code(T), torch.float32
     if out is None:
-        out = torch.empty(shape, dtype=T, device=x.device)
+        out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), B * H * N * P
-    ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, B, n, H, P, G, N, dt)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, side, B, n, H, P, G, N, dt)
     _check(lib().hla_ssm_forward(
         x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
         _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, n, H, P, G, N,
         _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
         1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, f32, i),
-        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, _on(stream, i)), "hla_ssm_forward")
+        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle), "hla_ssm_forward")
     return out
 
 
@@ -572,18 +620,19 @@ def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=No
     if x.dim() != 3 or b.dim() != 3:
         raise ValueError("x must be [B, H, P] and b [B, G, N], got %s and %s" % (tuple(x.shape), tuple(b.shape)))
     T, i, shape, bc = x.dtype, _gpu(x), x.shape, b.shape
+    handle, side = _on(stream, i)
     B, H, P = shape
     G, N = bc[1], bc[2]
     dt, f32 = _type_code(T), torch.float32
     if out is None:
-        out = torch.empty(shape, dtype=T, device=x.device)
+        out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner = (B, G, N), (P, 1), (N, 1)
     _check(lib().hla_ssm_step(
         x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
         _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, H, P, G, N,
         _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i), _rows("b", b, bc, bc_inner, T, i),
         _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i), 1 if softplus else 0,
-        _flat("state", state, B * H * N * P, f32, i), _on(stream, i)), "hla_ssm_step")
+        _flat("state", state, B * H * N * P, f32, i), handle), "hla_ssm_step")
     return out
 
 
@@ -608,18 +657,19 @@ def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, 
     [rows, rot / 2]; positions: int32 [B, n], or None for pos0, pos0 + 1, ...
     """
     T, i, shape, Hk, rot, top = _qk_sizes(q, k, cos, sin)
+    handle, side = _on(stream, i)
     B, n, H, d = shape
     if q_out is None:
-        q_out = torch.empty((B, H, n, d), dtype=T, device=q.device)
+        q_out = _empty((B, H, n, d), T, q.device, side)
     if k_out is None:
-        k_out = torch.empty((B, H, n, d), dtype=T, device=q.device)
+        k_out = _empty((B, H, n, d), T, q.device, side)
     inner, table, count = (d, 1), top * rot // 2, B * H * n * d
     _check(lib().hla_qk_norm_forward(
         q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
         _flat("positions", positions, B * n, torch.int32, i), _flat("q_out", q_out, count, T, i),
         _flat("k_out", k_out, count, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
-        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, _on(stream, i)),
+        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, handle),
         "hla_qk_norm_forward")
     return q_out, k_out
 
@@ -633,16 +683,17 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
     """Gradients (dq, dk, dwq, dwk) of sum(dq_out * q_out) + sum(dk_out * k_out) for hla_qk_norm_forward
     (include/hla.h: hla_qk_norm_backward); dwq, dwk are fp32 [d], None where the weight is."""
     T, i, shape, Hk, rot, top = _qk_sizes(q, k, cos, sin)
+    handle, side = _on(stream, i)
     B, n, H, d = shape
     k_shape = (B, n, Hk, d)
     if dq is None:
-        dq = torch.empty(shape, dtype=T, device=q.device)
+        dq = _empty(shape, T, q.device, side)
     if dk is None:
-        dk = torch.empty(k_shape, dtype=T, device=q.device)
-    dwq = None if wq is None else torch.empty((d,), dtype=torch.float32, device=q.device)
-    dwk = None if wk is None else torch.empty((d,), dtype=torch.float32, device=q.device)
+        dk = _empty(k_shape, T, q.device, side)
+    dwq = None if wq is None else _empty((d,), torch.float32, q.device, side)
+    dwk = None if wk is None else _empty((d,), torch.float32, q.device, side)
     dt, inner, table, count = _type_code(T), (d, 1), top * rot // 2, B * H * n * d
-    ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, B, n, H, Hk, d, dt)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, side, B, n, H, Hk, d, dt)
     _check(lib().hla_qk_norm_backward(
         q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
@@ -650,5 +701,5 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
         _flat("dk_out", dk_out, count, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
         None if dwk is None else dwk.data_ptr(), dt, B, n, H, Hk, d, rot, 1 if interleaved else 0,
         _rows("q", q, shape, inner, T, i), _rows("k", k, k_shape, inner, T, i), _rows("dq", dq, shape, inner, T, i),
-        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, _on(stream, i)), "hla_qk_norm_backward")
+        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, handle), "hla_qk_norm_backward")
     return dq, dk, dwq, dwk
