@@ -182,10 +182,21 @@ def _on(stream, index):
     return handle, stream
 
 
-def _on_gpu_of(t, stream):
-    """_on for the GPU a tensor is on."""
+def _index(t):
+    """The GPU a tensor is on."""
     index = t.get_device()
-    return _on(stream, index if index >= 0 else torch.cuda.current_device())
+    return index if index >= 0 else torch.cuda.current_device()
+
+
+def _run(name, index, *args):
+    """Calls the entry point with GPU `index`, where its tensors and its stream are, as the current one."""
+    fn = getattr(lib(), name)
+    if torch.cuda.current_device() == index:
+        code = fn(*args)
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args)
+    _check(code, name)
 
 
 def _empty(shape, dtype, device, side):
@@ -219,16 +230,16 @@ def _forward(fn_name, ws_fn, q, k, v, out, masked, normalized, eps, chunk, state
     for t in (q, k, v):
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, n, dv), q.dtype, q.device, side)
     dt = _dtype_code(q)
     if workspace is None:
         workspace = _workspace(ws_fn(B, H, n, d, dv, chunk, dt), q.device, side)
-    code = getattr(lib(), fn_name)(_ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(masked),
-                                   int(normalized), float(eps), int(chunk), _ptr(state_in), _ptr(state_out),
-                                   _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
-    _check(code, fn_name)
+    _run(fn_name, index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(masked), int(normalized),
+         float(eps), int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace),
+         workspace.numel() * workspace.element_size(), handle)
     return out
 
 
@@ -253,12 +264,12 @@ def hla2_forward_noalloc(q, k, v, out=None, *, masked=True, normalized=False, ep
     hla2_forward_noalloc).  Returns ``out``."""
     B, H, n, d = q.shape
     dv = v.shape[-1]
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, n, dv), q.dtype, q.device, side)
-    code = lib().hla2_forward_noalloc(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, n, d, dv,
-                                      int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in), handle)
-    _check(code, "hla2_forward_noalloc")
+    _run("hla2_forward_noalloc", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, n, d, dv,
+         int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in), handle)
     return out
 
 
@@ -290,14 +301,14 @@ def hla2_step(q, k, v, state, out=None, *, masked=True, normalized=False, eps=1e
     """
     B, H, d = q.shape
     dv = v.shape[-1]
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    code = lib().hla2_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(masked),
-                           int(normalized), float(eps), _ptr(state), handle)
-    _check(code, "hla2_step")
+    _run("hla2_step", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(masked),
+         int(normalized), float(eps), _ptr(state), handle)
     return out
 
 
@@ -315,14 +326,14 @@ def hla2_backward(q, k, v, dout, *, normalized=False, eps=1e-6, chunk=64, worksp
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v, dout must be contiguous CUDA tensors of one dtype")
     dt = _dtype_code(q)
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     gq, gk, gv = (_empty(t.shape, t.dtype, t.device, side) for t in (q, k, v))
     if workspace is None:
         workspace = _workspace(hla2_backward_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
-    code = lib().hla2_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(gq), _ptr(gk), _ptr(gv), dt, B, H, n, d,
-                               dv, int(normalized), float(eps), int(chunk), _ptr(workspace),
-                               workspace.numel() * workspace.element_size(), handle)
-    _check(code, "hla2_backward")
+    _run("hla2_backward", index, _ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(gq), _ptr(gk), _ptr(gv), dt, B, H, n, d,
+         dv, int(normalized), float(eps), int(chunk), _ptr(workspace), workspace.numel() * workspace.element_size(),
+         handle)
     return gq, gk, gv
 
 
@@ -345,16 +356,16 @@ def ahla_forward(q, k, v, out=None, *, normalized=False, eps=1e-6, chunk=64, sta
     for t in (q, k, v):
         if not t.is_cuda or not t.is_contiguous() or t.dtype != q.dtype:
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, n, dv), q.dtype, q.device, side)
     dt = _dtype_code(q)
     if workspace is None:
         workspace = _workspace(ahla_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
-    code = lib().ahla_forward(_ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(normalized), float(eps),
-                              int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace),
-                              workspace.numel() * workspace.element_size(), handle)
-    _check(code, "ahla_forward")
+    _run("ahla_forward", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(normalized), float(eps),
+         int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+         handle)
     return out
 
 
@@ -376,14 +387,14 @@ def ahla_step(q, k, v, state, out=None, *, normalized=False, eps=1e-6, stream=No
     """One AHLA decode step for every head (include/hla.h: ahla_step); ``state`` is updated in place."""
     B, H, d = q.shape
     dv = v.shape[-1]
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    code = lib().ahla_step(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-                           float(eps), _ptr(state), handle)
-    _check(code, "ahla_step")
+    _run("ahla_step", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
+         float(eps), _ptr(state), handle)
     return out
 
 
@@ -395,10 +406,11 @@ def hla2_state_to_sde(state, d: int, dv: int, sde=None, *, stream=None):
     """(S, C, m, G, h) tuples [B, H, hla2_state_floats(d, dv)] -> (S, D, e) states
     [B, H, hla2_sde_state_floats(d, dv)] (include/hla.h: hla2_state_to_sde)."""
     B, H = state.shape[:2]
-    handle, side = _on_gpu_of(state, stream)
+    index = _index(state)
+    handle, side = _on(stream, index)
     if sde is None:
         sde = _empty((B, H, hla2_sde_state_floats(d, dv)), torch.float32, state.device, side)
-    _check(lib().hla2_state_to_sde(_ptr(state), _ptr(sde), B, H, d, dv, handle), "hla2_state_to_sde")
+    _run("hla2_state_to_sde", index, _ptr(state), _ptr(sde), B, H, d, dv, handle)
     return sde
 
 
@@ -407,14 +419,14 @@ def hla2_step_sde(q, k, v, sde, out=None, *, normalized=False, eps=1e-6, stream=
     (include/hla.h: hla2_step_sde).  q, k: [B, H, d]; v: [B, H, dv]."""
     B, H, d = q.shape
     dv = v.shape[-1]
-    handle, side = _on_gpu_of(q, stream)
+    index = _index(q)
+    handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if sde.dtype != torch.float32 or not sde.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    code = lib().hla2_step_sde(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-                               float(eps), _ptr(sde), handle)
-    _check(code, "hla2_step_sde")
+    _run("hla2_step_sde", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
+         float(eps), _ptr(sde), handle)
     return out
 
 
@@ -529,11 +541,12 @@ def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None,
     if out is None:
         out = _empty(shape, T, x.device, side)
     kept = B * (W - 1) * C
-    _check(lib().hla_conv_forward(
-        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, n, C, W,
+    _run(
+        "hla_conv_forward", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        out.data_ptr(), dt, B, n, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
         _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, T, i),
-        _flat("state_out", state_out, kept, T, i), handle), "hla_conv_forward")
+        _flat("state_out", state_out, kept, T, i), handle)
     return out
 
 
@@ -545,10 +558,11 @@ def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=No
     B, C = shape
     if out is None:
         out = _empty(shape, T, x.device, side)
-    _check(lib().hla_conv_step(
-        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), out.data_ptr(), dt, B, C, W,
+    _run(
+        "hla_conv_step", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        out.data_ptr(), dt, B, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("state", state, B * (W - 1) * C, T, i), handle), "hla_conv_step")
+        _flat("state", state, B * (W - 1) * C, T, i), handle)
     return out
 
 
@@ -567,11 +581,12 @@ def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths
     dw = _empty((C, W), torch.float32, x.device, side)
     db = None if bias is None else _empty((C,), torch.float32, x.device, side)
     ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, side, B, n, C, W, dt)
-    _check(lib().hla_conv_backward(
-        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i), dout.data_ptr(), dx.data_ptr(),
+    _run(
+        "hla_conv_backward", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        dout.data_ptr(), dx.data_ptr(),
         dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i),
         _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, handle), "hla_conv_backward")
+        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, handle)
     return dx, dw, db
 
 
@@ -597,13 +612,13 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
         out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), B * H * N * P
     ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, side, B, n, H, P, G, N, dt)
-    _check(lib().hla_ssm_forward(
-        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
-        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, n, H, P, G, N,
-        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
+    _run(
+        "hla_ssm_forward", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, n, H, P, G,
+        N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
         1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, f32, i),
-        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle), "hla_ssm_forward")
+        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle)
     return out
 
 
@@ -627,12 +642,12 @@ def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=No
     if out is None:
         out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner = (B, G, N), (P, 1), (N, 1)
-    _check(lib().hla_ssm_step(
-        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+    _run(
+        "hla_ssm_step", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
         _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, H, P, G, N,
-        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i), _rows("b", b, bc, bc_inner, T, i),
-        _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i), 1 if softplus else 0,
-        _flat("state", state, B * H * N * P, f32, i), handle), "hla_ssm_step")
+        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i),
+        _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
+        1 if softplus else 0, _flat("state", state, B * H * N * P, f32, i), handle)
     return out
 
 
@@ -664,13 +679,12 @@ def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, 
     if k_out is None:
         k_out = _empty((B, H, n, d), T, q.device, side)
     inner, table, count = (d, 1), top * rot // 2, B * H * n * d
-    _check(lib().hla_qk_norm_forward(
-        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+    _run(
+        "hla_qk_norm_forward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
         _flat("positions", positions, B * n, torch.int32, i), _flat("q_out", q_out, count, T, i),
         _flat("k_out", k_out, count, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
-        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, handle),
-        "hla_qk_norm_forward")
+        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, handle)
     return q_out, k_out
 
 
@@ -694,12 +708,12 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
     dwk = None if wk is None else _empty((d,), torch.float32, q.device, side)
     dt, inner, table, count = _type_code(T), (d, 1), top * rot // 2, B * H * n * d
     ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, side, B, n, H, Hk, d, dt)
-    _check(lib().hla_qk_norm_backward(
-        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+    _run(
+        "hla_qk_norm_backward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
         _flat("positions", positions, B * n, torch.int32, i), _flat("dq_out", dq_out, count, T, i),
         _flat("dk_out", dk_out, count, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
         None if dwk is None else dwk.data_ptr(), dt, B, n, H, Hk, d, rot, 1 if interleaved else 0,
         _rows("q", q, shape, inner, T, i), _rows("k", k, k_shape, inner, T, i), _rows("dq", dq, shape, inner, T, i),
-        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, handle), "hla_qk_norm_backward")
+        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, handle)
     return dq, dk, dwq, dwk

@@ -52,6 +52,17 @@ class World:
                 world.stream = self.kept
         return On()
 
+    def use(self, index):
+        world = self
+
+        class Use:
+            def __enter__(self):
+                self.kept, world.device = world.device, index
+
+            def __exit__(self, *_):
+                world.device = self.kept
+        return Use()
+
     def empty(self, *shape, dtype=None, device=None):
         t = Tensor(torch.zeros(*shape, dtype=dtype), torch.device(device).index)
         self.made.append((t, self.stream))
@@ -82,6 +93,7 @@ def world(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", w.on)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: Stream(w.stream))
     monkeypatch.setattr(torch.cuda, "current_device", lambda: w.device)
+    monkeypatch.setattr(torch.cuda, "device", w.use)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: w.stream, raising=False)
     return w
 
@@ -158,3 +170,13 @@ def test_a_stream_of_another_gpu(world):
     with pytest.raises(ValueError):
         calls(E)["hla_conv_forward"](Stream(32, device=1))
     assert not world.launched
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("index", [0, 1])
+def test_launched_on_the_gpu_of_the_tensors(world, name, index):
+    """Whichever GPU is the current one, a call is made with its tensors' one, and leaves the current one as it was."""
+    from paper_2510_27258_gb300 import hla as E
+    calls(E, index)[name](None)
+    assert [(n, device) for n, _, device in world.launched] == [(name, index)]
+    assert world.device == 0 and all(t.index == index for t, _ in world.made)
