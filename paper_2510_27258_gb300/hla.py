@@ -455,13 +455,28 @@ def _type_code(dtype) -> int:
     raise TypeError("tokens must be bfloat16 or float32, got %s" % dtype)
 
 
-def _flat(name, t, count, dtype, index):
-    """Address of a contiguous tensor of `count` elements on GPU `index` (None stays None)."""
+def _same_order(got, want):
+    """Whether contiguous tensors of two shapes hold the same elements in the same order as far as shapes can tell:
+    one of them is the other with neighbouring dimensions taken together."""
+    def steps(shape):  # elements from one index of a dimension to the next, and of all
+        seen, step = {1}, 1
+        for size in reversed(shape):
+            step *= size
+            seen.add(step)
+        return step, seen
+    (count, a), (other, b) = steps(got), steps(want)
+    return count == other and (count == 0 or a <= b or b <= a)
+
+
+def _flat(name, t, shape, dtype, index):
+    """Address of a contiguous tensor of a shape (or of one that holds it in the same order) on GPU `index` (None
+    stays None)."""
     if t is None:
         return None
-    if t.numel() != count or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of %d elements on cuda:%d, got %s %s on %s"
-                         % (name, dtype, count, index, t.dtype, tuple(t.shape), t.device))
+    if (t.dtype is not dtype or t.get_device() != index or not t.is_contiguous()
+            or not (t.shape == shape or _same_order(t.shape, shape))):
+        raise ValueError("%s must be a contiguous %s tensor %s on cuda:%d, got %s %s on %s"
+                         % (name, dtype, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
@@ -540,12 +555,12 @@ def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None,
     B, n, C = shape
     if out is None:
         out = _empty(shape, T, x.device, side)
-    kept = B * (W - 1) * C
+    kept = (B, W - 1, C)
     _run(
-        "hla_conv_forward", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        "hla_conv_forward", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
         out.data_ptr(), dt, B, n, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, T, i),
+        _flat("lengths", lengths, (B,), torch.int32, i), _flat("state_in", state_in, kept, T, i),
         _flat("state_out", state_out, kept, T, i), handle)
     return out
 
@@ -559,10 +574,10 @@ def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=No
     if out is None:
         out = _empty(shape, T, x.device, side)
     _run(
-        "hla_conv_step", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        "hla_conv_step", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
         out.data_ptr(), dt, B, C, W,
         _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("state", state, B * (W - 1) * C, T, i), handle)
+        _flat("state", state, (B, W - 1, C), T, i), handle)
     return out
 
 
@@ -582,11 +597,11 @@ def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths
     db = None if bias is None else _empty((C,), torch.float32, x.device, side)
     ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, side, B, n, C, W, dt)
     _run(
-        "hla_conv_backward", i, x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
+        "hla_conv_backward", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
         dout.data_ptr(), dx.data_ptr(),
         dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i),
         _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, handle)
+        _flat("lengths", lengths, (B,), torch.int32, i), ws, ws_bytes, handle)
     return dx, dw, db
 
 
@@ -610,15 +625,15 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
     dt, f32 = _type_code(T), torch.float32
     if out is None:
         out = _empty(shape, T, x.device, side)
-    bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), B * H * N * P
+    bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), (B, H, N, P)
     ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, side, B, n, H, P, G, N, dt)
     _run(
-        "hla_ssm_forward", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
-        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, n, H, P, G,
-        N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
+        "hla_ssm_forward", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, (H,), f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, (H,), f32, i), _flat("delta_bias", delta_bias, (H,), f32, i), out.data_ptr(),
+        dt, B, n, H, P, G, N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
-        1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i), _flat("state_in", state_in, kept, f32, i),
-        _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle)
+        1 if softplus else 0, _flat("lengths", lengths, (B,), torch.int32, i),
+        _flat("state_in", state_in, kept, f32, i), _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle)
     return out
 
 
@@ -643,11 +658,11 @@ def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=No
         out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner = (B, G, N), (P, 1), (N, 1)
     _run(
-        "hla_ssm_step", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
-        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(), dt, B, H, P, G, N,
-        _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i),
+        "hla_ssm_step", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, (H,), f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, (H,), f32, i), _flat("delta_bias", delta_bias, (H,), f32, i), out.data_ptr(),
+        dt, B, H, P, G, N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
-        1 if softplus else 0, _flat("state", state, B * H * N * P, f32, i), handle)
+        1 if softplus else 0, _flat("state", state, (B, H, N, P), f32, i), handle)
     return out
 
 
@@ -678,12 +693,12 @@ def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, 
         q_out = _empty((B, H, n, d), T, q.device, side)
     if k_out is None:
         k_out = _empty((B, H, n, d), T, q.device, side)
-    inner, table, count = (d, 1), top * rot // 2, B * H * n * d
+    inner, table, heads = (d, 1), (top, rot // 2), (B, H, n, d)
     _run(
-        "hla_qk_norm_forward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        "hla_qk_norm_forward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, (d,), T, i), _flat("wk", wk, (d,), T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
-        _flat("positions", positions, B * n, torch.int32, i), _flat("q_out", q_out, count, T, i),
-        _flat("k_out", k_out, count, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
+        _flat("positions", positions, (B, n), torch.int32, i), _flat("q_out", q_out, heads, T, i),
+        _flat("k_out", k_out, heads, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
         _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, handle)
     return q_out, k_out
 
@@ -706,13 +721,13 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
         dk = _empty(k_shape, T, q.device, side)
     dwq = None if wq is None else _empty((d,), torch.float32, q.device, side)
     dwk = None if wk is None else _empty((d,), torch.float32, q.device, side)
-    dt, inner, table, count = _type_code(T), (d, 1), top * rot // 2, B * H * n * d
+    dt, inner, table, heads = _type_code(T), (d, 1), (top, rot // 2), (B, H, n, d)
     ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, side, B, n, H, Hk, d, dt)
     _run(
-        "hla_qk_norm_backward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        "hla_qk_norm_backward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, (d,), T, i), _flat("wk", wk, (d,), T, i),
         _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
-        _flat("positions", positions, B * n, torch.int32, i), _flat("dq_out", dq_out, count, T, i),
-        _flat("dk_out", dk_out, count, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
+        _flat("positions", positions, (B, n), torch.int32, i), _flat("dq_out", dq_out, heads, T, i),
+        _flat("dk_out", dk_out, heads, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
         None if dwk is None else dwk.data_ptr(), dt, B, n, H, Hk, d, rot, 1 if interleaved else 0,
         _rows("q", q, shape, inner, T, i), _rows("k", k, k_shape, inner, T, i), _rows("dq", dq, shape, inner, T, i),
         _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, handle)
