@@ -333,7 +333,8 @@ conv_backward_kernel(Geom g, const T *x, const T *w, const T *bias,
     }
 }
 
-// dw[c][j] and dbias[c] from `rows` partials [W + 1][C]: 32 entries a block, a warp for every 16th row
+// dw[c][j] and dbias[c] from `rows` partials [W + 1][C]: 32 entries a block, a warp for every 16th row.  (The entries
+// of 430 million channels and more pass 32 bits.)
 constexpr int kSumGroups = 16;
 template <int W>
 __global__ void __launch_bounds__(kSumGroups * 32)
@@ -343,21 +344,23 @@ conv_sum_kernel(const float *partial, int rows, int C, float *dw, float *dbias,
     let_next_begin();
     after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // no device-side waits here: never an error
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
-    const size_t width = (size_t)(W + 1) * C;
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const size_t width = (size_t)(W + 1) * C, i = (size_t)blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (i < (int)width)
+    if (i < width)
 #pragma unroll 8
         for (int r = group; r < rows; r += kSumGroups) s += partial[(size_t)r * width + i];
     red[group][lane] = s;
     __syncthreads();
-    if (group || i >= (int)width) return;
+    if (group || i >= width) return;
     s = 0.f;
 #pragma unroll
     for (int k = 0; k < kSumGroups; ++k) s += red[k][lane];
-    const int j = i / C, c = i % C;
+    size_t c = i;
+    int j = 0;
+    for (; c >= (size_t)C; c -= C) ++j;  // (at most W)
     if (j < W)
-        dw[(size_t)c * W + j] = s;
+        dw[c * W + j] = s;
     else if (dbias)
         dbias[c] = s;
 }

@@ -13,6 +13,7 @@ bool size_ok(int v) { return v == 16 || v == 32 || v == 64 || v == 128; }
 
 constexpr long long kMaxRows = (1LL << 31) - 1;
 constexpr long long kMaxValues = 1LL << 40;
+constexpr int kMaxChannels = (int)kMaxRows - 256;  // a block has up to 256: its last one is within 32 bits
 
 #define HLA_TRY(expr)                       \
     do {                                    \
@@ -58,6 +59,7 @@ hla_status check_conv(const void *x, const void *w, const void *bias, hla_dtype 
     HLA_TRY(check_flag(silu, "silu"));
     if (C <= 0 || width <= 0) return fail(HLA_ERR_INVALID_ARGUMENT, "non-positive size C=%d width=%d", C, width);
     if (width < 2 || width > 4) return fail(HLA_ERR_UNSUPPORTED, "width=%d: supported widths are 2, 3, 4", width);
+    if (C > kMaxChannels) return fail(HLA_ERR_UNSUPPORTED, "problem too large");
     // one launch covers B x token blocks x channel blocks
     if (((long long)n / 32 + 1) * B > kMaxRows / (C / 32 + 1)) return fail(HLA_ERR_UNSUPPORTED, "problem too large");
     HLA_TRY(check_tensor(x, x_stride, C, dt, (long long)B * n, "x"));
@@ -164,7 +166,7 @@ hla_status hla_conv_step(const void *x, const void *w, const void *bias, void *o
 }
 
 size_t hla_conv_backward_workspace_bytes(int B, int n, int C, int width, hla_dtype dt) {
-    if (B < 0 || n < 0 || C <= 0 || width < 2 || width > 4 || (dt != HLA_F32 && dt != HLA_BF16)) return 0;
+    if (B < 0 || n < 0 || C <= 0 || C > kMaxChannels || width < 2 || width > 4 || (dt != HLA_F32 && dt != HLA_BF16)) return 0;
     if ((long long)B * n > kMaxRows) return 0;
     return scratch_bytes(conv_backward_partial_floats(B, n, C, width));
 }
