@@ -57,11 +57,12 @@ scan_kernel(Ssm p, int segments, int seg_len, float *seg_state, float *seg_decay
     const int len = length_of(p, b);
     const int t_lo = seg * seg_len, t_hi = min(t_lo + seg_len, p.n);
     const int live = min(t_hi, len);
-    const T *x = static_cast<const T *>(p.x) + (size_t)b * p.n * p.x_stride + h * p.P + slice * kCols;
+    // (a row may hold more than 2^31 elements)
+    const T *x = static_cast<const T *>(p.x) + (size_t)b * p.n * p.x_stride + (size_t)h * p.P + slice * kCols;
     const T *raw = static_cast<const T *>(p.delta) + (size_t)b * p.n * p.delta_stride + h;
-    const T *bm = static_cast<const T *>(p.b) + (size_t)b * p.n * p.b_stride + g * N;
-    const T *cm = static_cast<const T *>(p.c) + (size_t)b * p.n * p.c_stride + g * N;
-    T *y = static_cast<T *>(p.y) + (size_t)b * p.n * p.y_stride + h * p.P + slice * kCols;
+    const T *bm = static_cast<const T *>(p.b) + (size_t)b * p.n * p.b_stride + (size_t)g * N;
+    const T *cm = static_cast<const T *>(p.c) + (size_t)b * p.n * p.c_stride + (size_t)g * N;
+    T *y = static_cast<T *>(p.y) + (size_t)b * p.n * p.y_stride + (size_t)h * p.P + slice * kCols;
     const float a = p.a[h], bias = p.delta_bias ? p.delta_bias[h] : 0.f, skip = p.skip ? p.skip[h] : 0.f;
 
     if (!kStateOnly && segments > 1) after_previous();
@@ -230,13 +231,13 @@ __global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(Ssm p) {
     for (int i = 0; i < kMost; ++i)
         if (row + i * kRows < p.N) v[i] = *reinterpret_cast<const float4 *>(st + (size_t)(row + i * kRows) * p.P);
     if (tid < p.N) {
-        bs[tid] = to_f32(static_cast<const T *>(p.b)[(size_t)b * p.b_stride + g * p.N + tid]);
-        cs[tid] = to_f32(static_cast<const T *>(p.c)[(size_t)b * p.c_stride + g * p.N + tid]);
+        bs[tid] = to_f32(static_cast<const T *>(p.b)[(size_t)b * p.b_stride + (size_t)g * p.N + tid]);
+        cs[tid] = to_f32(static_cast<const T *>(p.c)[(size_t)b * p.c_stride + (size_t)g * p.N + tid]);
     }
     const float d = step_size(to_f32(static_cast<const T *>(p.delta)[(size_t)b * p.delta_stride + h]),
                               p.delta_bias ? p.delta_bias[h] : 0.f, p.softplus);
     const float e = expf(p.a[h] * d);
-    const T *xp = static_cast<const T *>(p.x) + (size_t)b * p.x_stride + h * p.P + c0 + quad * 4;
+    const T *xp = static_cast<const T *>(p.x) + (size_t)b * p.x_stride + (size_t)h * p.P + c0 + quad * 4;
     float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = to_f32(xp[i]);
@@ -264,8 +265,8 @@ __global__ void __launch_bounds__(kStepThreads) ssm_step_kernel(Ssm p) {
         const float *r = reinterpret_cast<const float *>(&red[0][0]);
         float s = 0.f;
         for (int k = 0; k < kRows && k < p.N; ++k) s += r[k * kC + tid];
-        const float xv = to_f32(static_cast<const T *>(p.x)[(size_t)b * p.x_stride + h * p.P + c0 + tid]);
-        from_f32(static_cast<T *>(p.y) + (size_t)b * p.y_stride + h * p.P + c0 + tid,
+        const float xv = to_f32(static_cast<const T *>(p.x)[(size_t)b * p.x_stride + (size_t)h * p.P + c0 + tid]);
+        from_f32(static_cast<T *>(p.y) + (size_t)b * p.y_stride + (size_t)h * p.P + c0 + tid,
                  fmaf(p.skip ? p.skip[h] : 0.f, xv, s));
     }
 }
