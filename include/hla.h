@@ -400,6 +400,7 @@ size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dty
  * delta : device [B, n, H], row stride delta_stride, of type dt (the raw step sizes)
  * b, c  : device [B, n, G, N], row strides b_stride, c_stride, of type dt
  * a     : device fp32 [H], not above 0 (with delta not below 0: the state does not grow)
+ *         (bf16 tokens: products c_t . b_u delta_u, taken before x_u, have to stay in range)
  * skip, delta_bias : device fp32 [H] or NULL (= 0)
  * state_in  : device fp32 [B, H, N, P] or NULL (= 0)
  * state_out : device fp32 [B, H, N, P] or NULL; the state after lengths[b] tokens.

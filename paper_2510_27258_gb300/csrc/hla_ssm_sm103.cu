@@ -818,10 +818,13 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     }
                 }
             } else {
+                // from the diagonal to the left: the exponents grow by one token's decay a column, so that what is
+                // near a token does not come from a difference of what a strong decay made large (or infinite)
                 const volatile Misc *m = ms;
                 const int tc = t_lo + j * kTile + c0 + lane;  // this lane's column
+                float x0 = 0.f, x1 = 0.f;
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
+                for (int o = 1; o >= 0; --o) {
                     uint32_t sv[16], w[8];
                     tmem_ld16(sw + 16 * o, sv);
                     tmem_ld_wait();
@@ -834,16 +837,20 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                                  (p.delta_bias ? p.delta_bias[he] : 0.f);
                             dc = p.softplus ? softplus(dc) : dc;
                         }
-                        const float lr = m->cum[e][r];
+                        const float da = p.a[he] * kLog2e;
+                        float x = e ? x1 : x0;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 7; i >= 0; --i) {
                             const int c = 16 * o + 2 * i;
                             const float d0 = __shfl_sync(0xffffffffu, dc, c), d1 = __shfl_sync(0xffffffffu, dc, c + 1);
-                            const float w0 = c <= lane ? ex2(lr - m->cum[e][c0 + c]) * d0 : 0.f;
-                            const float w1 = c + 1 <= lane ? ex2(lr - m->cum[e][c0 + c + 1]) * d1 : 0.f;
+                            const float w1 = c + 1 <= lane ? ex2(x) * d1 : 0.f;
+                            x += c + 1 <= lane ? da * d1 : 0.f;
+                            const float w0 = c <= lane ? ex2(x) * d0 : 0.f;
+                            x += c <= lane ? da * d0 : 0.f;
                             w[i] = pack_bf16x2(c <= lane ? __uint_as_float(sv[2 * i]) * w0 : 0.f,
                                                c + 1 <= lane ? __uint_as_float(sv[2 * i + 1]) * w1 : 0.f);
                         }
+                        (e ? x1 : x0) = x;
                         tmem_st8(sw + 16 * o + 8 * e, w);
                     }
                 }

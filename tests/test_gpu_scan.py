@@ -1,5 +1,5 @@
 """The selective scan on the GPU where its tiles and segments depend on one another, against the 64-bit recurrence:
-slow decays and large states over many tiles.
+slow decays and large states over many tiles, and decays so strong that sums of exponents lose their small terms.
 
 b, c, x, skip and the states are positive here, so that a sum's value is the magnitude its rounding errors scale
 with: a bound of a few 2^-8 resolves a carried part of one percent."""
@@ -82,3 +82,28 @@ def test_a_state_carried_over_tiles_and_segments(hla, dtype, B, n, H, P, G, N, l
         rel = (6 * n + 2 * N + 64) * U32
         near(out, y, rel * ym)
     near(st, h, rel * hm)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("P,N", [(64, 16), (16, 128), (128, 64)])
+def test_weights_behind_a_very_strong_decay(hla, dtype, P, N):
+    """Steps that wipe a state out leave the weights among the tokens after them as they are, in the same
+    32-token block too, up to steps whose exponent is beyond fp32's range."""
+    T, (B, n, H, G) = TYPES[dtype], (1, 300, 4, 2)
+    x, delta, a, b, c, skip, state = inputs(P + N, B, n, H, P, G, N, T)
+    a = a * 8
+    a[-1] = -1e6  # (times 1e34: beyond fp32's range)
+    delta = (delta.float().abs() * 0.05 + 0.01).to(T)
+    for t, big in ((3, 3e4), (36, 1e6), (37, 2e4), (63, 3e5), (130, 1e34), (200, 1e30), (259, 3e4)):
+        delta[:, t] = big
+    x[:, 130:] *= 1e-3
+    y, h, ym, hm = reference(x, delta, a, b, c, skip, softplus=False, state=state)
+    st = state.clone()
+    out = hla.hla_ssm_forward(x, delta, a, b, c, skip=skip, softplus=False, state_in=st, state_out=st)
+    serial = (6 * n + 2 * N + 64) * U32
+    if T == torch.bfloat16:
+        near(out, y, U16 * y.abs() + (2 * U16 + serial) * ym)
+        near(st, h, (2.0 ** -16 + serial) * hm)
+    else:
+        near(out, y, serial * ym)
+        near(st, h, serial * hm)
