@@ -408,8 +408,8 @@ size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dty
  * P, N in {16, 32, 64, 128}; H a multiple of G.
  * workspace : at least hla_ssm_workspace_bytes(...) bytes, 256-byte aligned; calls
  *             that share one are ordered on one stream; hla_poll_error reads its flag.
- * Finite inputs are assumed: a NaN or infinity in a token may also reach the
- * outputs of earlier tokens of its 128-token tile.
+ * A NaN or infinity in a token reaches the outputs of that token and later ones,
+ * where it enters them (there as NaN, or infinity), and the state.
  */
 hla_status hla_ssm_forward(const void *x, const void *delta, const float *a, const void *b, const void *c,
                            const float *skip, const float *delta_bias, void *y, hla_dtype dt, int B, int n, int H,

@@ -86,6 +86,10 @@ struct Misc {
     // what the epilogue needs now and then of its place in the problem (kept out of its registers):
     // sequence, first head, segment, whether the second 64 columns are a head of this group
     int b, h0, seg, both;
+    // of each slot of X: whether its tile holds a value that is not finite, and the first token with one in each
+    // column (a byte each, 255: none)
+    int odd[3];
+    uint32_t first[3][kTile / 4];
 };
 static_assert(sizeof(Misc) <= 3 * 1024, "fits beside the tiles");
 
@@ -207,7 +211,8 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t 
 
 // Elements c .. c + 7 of a row of w X as the bf16 pairs hi + lo.  With w = wh + wl in bf16 (to 2^-17): hi = x wh
 // rounded, x wh - hi is a bf16 exactly, and lo = x wl + (x wh - hi) rounded, all by fused multiply-adds on
-// the packed elements.
+// the packed elements.  odd collects products of neighbours: it becomes infinite or NaN where an element of X is
+// (or where products leave the range).
 struct Weight {
     uint32_t wh, wl;
     __device__ explicit Weight(float w) : wh(pack_bf16x2(w, w)) {
@@ -216,7 +221,8 @@ struct Weight {
     }
 };
 
-__device__ __forceinline__ void split8(const uint8_t *xs, int r, int c, const Weight &w, uint4 &hi, uint4 &lo) {
+__device__ __forceinline__ void split8(const uint8_t *xs, int r, int c, const Weight &w, uint4 &hi, uint4 &lo,
+                                       uint32_t &odd) {
     const uint4 u = *reinterpret_cast<const uint4 *>(xs + tile_off(r, c));
     const uint32_t x[4] = {u.x, u.y, u.z, u.w};
     uint32_t h[4], l[4];
@@ -225,19 +231,51 @@ __device__ __forceinline__ void split8(const uint8_t *xs, int r, int c, const We
         h[e] = fma_bf16x2(x[e], w.wh, 0x80008000u);  // (plus minus zero)
         l[e] = fma_bf16x2(x[e], w.wl, fma_bf16x2(x[e], w.wh, h[e] ^ 0x80008000u));
     }
+    odd = fma_bf16x2(x[2], x[3], fma_bf16x2(x[0], x[1], odd));
     hi = make_uint4(h[0], h[1], h[2], h[3]);
     lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-// 32 of them, rows and columns as in the X tile (hi may take its place)
-__device__ __forceinline__ void split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
+// 32 of them, rows and columns as in the X tile (hi may take its place); returns odd
+__device__ __forceinline__ uint32_t split_row(const uint8_t *xs, uint8_t *hi_tile, uint8_t *lo_tile, int r, int c0, float wr) {
     const Weight w(wr);
+    uint32_t odd = 0u;
 #pragma unroll
     for (int i = 0; i < 32; i += 8) {
         uint4 hi, lo;
-        split8(xs, r, c0 + i, w, hi, lo);
+        split8(xs, r, c0 + i, w, hi, lo, odd);
         *reinterpret_cast<uint4 *>(hi_tile + tile_off(r, c0 + i)) = hi;
         *reinterpret_cast<uint4 *>(lo_tile + tile_off(r, c0 + i)) = lo;
+    }
+    return odd;
+}
+
+// Values of X that are not finite, in a tile's row r and columns c0 .. c0 + 31: zero instead, and for each such
+// column the first token with one.  (This and put_nan are calls: inlined they cost 0.5 us of 51 where all is finite.)
+__device__ __noinline__ void take_out(uint8_t *xs, int r, int c0, uint32_t *first, volatile int *odd) {
+#pragma unroll 1
+    for (int c = c0; c < c0 + 32; ++c) {
+        uint16_t *at = reinterpret_cast<uint16_t *>(xs + tile_off(r, c & ~7)) + (c & 7);
+        if ((*at & 0x7f80) != 0x7f80) continue;
+        *at = 0;
+        uint32_t *word = first + c / 4, old = *(volatile uint32_t *)word;
+        const int sh = 8 * (c & 3);
+        while ((int)((old >> sh) & 255u) > r) {  // (a swap that fails: another thread's has lowered a byte)
+            const uint32_t was = old;
+            old = atomicCAS(word, was, (was & ~(255u << sh)) | (uint32_t)r << sh);
+            if (old == was) break;
+        }
+    }
+    *odd = 1;
+}
+
+// NaN in a tile's rows below `rows` from each column's first token with such a value on; none has one after that
+__device__ __noinline__ void put_nan(uint8_t *tile, uint8_t *first, int rows) {
+#pragma unroll 1
+    for (int c = 0; c < kTile; ++c) {
+#pragma unroll 1
+        for (int r = first[c]; r < rows; ++r) reinterpret_cast<uint16_t *>(tile + tile_off(r, c & ~7))[c & 7] = 0x7fff;
+        first[c] = 255;
     }
 }
 
@@ -521,9 +559,11 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             mbar_init(&ms->bar[i], (i >= bEpE && i <= bEpY1) ? kEpiWarps : two ? 2 : 1);
         }
         ms->abort_flag = 0;
+        ms->odd[0] = ms->odd[1] = ms->odd[2] = 0;
         ms->b = b; ms->h0 = h0; ms->seg = seg; ms->both = both;
         fence_mbar_init();
     }
+    if (tid < 3 * (kTile / 4)) ms->first[tid / (kTile / 4)][tid % (kTile / 4)] = ~0u;
     if (issuer) {
         tmem_alloc(&ms->tmem_base, 512);
         tmem_relinquish();
@@ -644,9 +684,14 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             };
             while (xs < Sm::kXs && xs < tiles) next_x();
             for (; j < tiles; ++j) {
-                const uint8_t *from = smem + Sm::X(j % Sm::kXs);
-                const int t0 = t_lo + j * kTile;
+                const int st = j % Sm::kXs, t0 = t_lo + j * kTile;
+                uint8_t *from = smem + Sm::X(st);
                 if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
+                if (*(volatile int *)&ms->odd[st]) {  // columns whose X was taken out, from its token on
+                    put_nan(from, reinterpret_cast<uint8_t *>(ms->first[st]), min(kTile, live - t0));
+                    ms->odd[st] = 0;
+                    fence_async_smem();
+                }
                 tma_store_4d(&tm_y, from, 0, h0, t0, b);
                 if (both) tma_store_4d(&tm_y, from + kBlockBytes, one ? 64 : 0, one ? h0 : h0 + 1, t0, b);
                 tma_store_commit();
@@ -858,6 +903,9 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             tmem_st_wait();
             epi_arrive(ms, bEpW);
         };
+        // W X multiplies a token's X by weights of zero for the tokens before it: a value that is not finite would
+        // make their outputs NaN.  It is taken out of X, once w X has it, and the storing warp makes the outputs from
+        // its token on NaN.
         // (a) w X of tile j -> hi, lo
         float yf = 0.f;  // decay of the tile up to this token
         auto split = [&](int j) {
@@ -865,13 +913,14 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const float wr = ms->cf[hs][r] * ex2(later);
             yf = ex2(before + ms->cum[hs][r]);
             landed(j);
+            uint32_t odd = 0u;
             if constexpr (Sm::kApart) {
-                split_row(smem + Sm::X(j % Sm::kXs), smem + Sm::kHi, smem + Sm::lo(j), r, c0, wr);
+                odd = split_row(smem + Sm::X(j % Sm::kXs), smem + Sm::kHi, smem + Sm::lo(j), r, c0, wr);
             } else {  // in registers until their slots are free
                 const Weight w(wr);
                 uint4 hi[4], lo[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) split8(smem + Sm::X(j & 1), r, c0 + 8 * i, w, hi[i], lo[i]);
+                for (int i = 0; i < 4; ++i) split8(smem + Sm::X(j & 1), r, c0 + 8 * i, w, hi[i], lo[i], odd);
                 bar_wait(ms, bEvY2, j & 1, p);  // C H has read H, where hi goes,
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(smem + Sm::kHi + tile_off(r, c0 + 8 * i)) = hi[i];
@@ -880,6 +929,9 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(smem + Sm::lo(j) + tile_off(r, c0 + 8 * i)) = lo[i];
                 tc_fence_after();
             }
+            if ((odd & 0x7f80u) == 0x7f80u || (odd & 0x7f800000u) == 0x7f800000u)
+                take_out(smem + Sm::X(j % Sm::kXs), r, c0, ms->first[j % Sm::kXs], &ms->odd[j % Sm::kXs]);
+            __syncwarp();
             fence_async_smem();
             tmem_st_wait();  // (H times the tile's decay)
             epi_arrive(ms, bEpX);

@@ -1,5 +1,6 @@
 """The selective scan on the GPU where its tiles and segments depend on one another, against the 64-bit recurrence:
-slow decays and large states over many tiles, and decays so strong that sums of exponents lose their small terms.
+slow decays and large states over many tiles, decays so strong that sums of exponents lose their small terms, and NaN and
+infinities in tokens.
 
 b, c, x, skip and the states are positive here, so that a sum's value is the magnitude its rounding errors scale
 with: a bound of a few 2^-8 resolves a carried part of one percent."""
@@ -107,3 +108,57 @@ def test_weights_behind_a_very_strong_decay(hla, dtype, P, N):
     else:
         near(out, y, serial * ym)
         near(st, h, serial * hm)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("B,n,H,P,G,N", [(2, 520, 3, 64, 1, 128), (2, 520, 3, 32, 3, 64), (1, 520, 2, 128, 1, 16),
+                                         (1, 520, 2, 128, 2, 128), (1, 2500, 38, 64, 1, 64)])
+def test_no_token_reaches_an_earlier_one(hla, dtype, bad, B, n, H, P, G, N):
+    """A token that is not finite leaves what comes before it, and the columns of a state that it does not
+    enter, as they are."""
+    T = TYPES[dtype]
+    x, delta, a, b, c, skip, state = inputs(7 * P + N, B, n, H, P, G, N, T)
+    bias = torch.full((H,), -6.0, device=DEV)
+    y, _, ym, _ = reference(x, delta, a, b, c, skip, bias, True, None, state)
+    rel = 2.0 ** -16 + 16 * 2.0 ** -21 + 64 * (n / TILE + 2) * U32
+    bound = U16 * y.abs() + (2 * U16 + rel) * ym if T == torch.bfloat16 else (6 * n + 2 * N + 64) * U32 * ym
+
+    def run(x, delta, b, c, state):
+        return hla.hla_ssm_forward(x, delta, a, b, c, skip=skip, delta_bias=bias, state_in=state)
+
+    def check(out, free):
+        """What is finite by the formula (`free`) is right, all else is not finite."""
+        assert torch.isfinite(out[free]).all() and not torch.isfinite(out[~free]).any()
+        assert bool(((out.double() - y).abs() <= bound)[free].all())
+
+    every = torch.ones(B, n, H, P, dtype=torch.bool, device=DEV)
+    # single elements of x, several in a tile, in neighbouring tiles, one column twice
+    places = [(0, 5, 0, 0), (0, 70, H - 1, P - 1), (B - 1, 127, 0, 1), (B - 1, 128, H - 1, 2), (0, 300, 1, P // 2),
+              (0, 310, 1, P // 2), (0, 290, 1, P // 2 + 1), (0, n - 2, 0, 3)]
+    x2, free = x.clone(), every.clone()
+    for s, t, h, p in places:
+        x2[s, t, h, p] = bad
+        free[s, t:, h, p] = False
+    check(run(x2, delta, b, c, state), free)
+    # c: its own token alone
+    c2, free = c.clone(), every.clone()
+    c2[0, 77, G - 1, 3] = bad
+    free[0, 77, (G - 1) * (H // G):] = False
+    check(run(x, delta, b, c2, state), free)
+    # b: every later token of its group's heads
+    b2, free = b.clone(), every.clone()
+    b2[0, 200, 0, 5] = bad
+    free[0, 200:, :H // G] = False
+    check(run(x, delta, b2, c, state), free)
+    # a step (minus infinity is one of zero)
+    if bad != float("-inf"):
+        d2, free = delta.clone(), every.clone()
+        d2[B - 1, 259, H - 1] = bad
+        free[B - 1, 259:, H - 1] = False
+        check(run(x, d2, b, c, state), free)
+    # a state
+    s2, free = state.clone(), every.clone()
+    s2[0, 0, 2, 1] = bad
+    free[0, :, 0, 1] = False
+    check(run(x, delta, b, c, s2), free)
