@@ -188,15 +188,16 @@ def _index(t):
     return index if index >= 0 else torch.cuda.current_device()
 
 
-def _run(name, index, *args):
-    """Calls the entry point with GPU `index`, where its tensors and its stream are, as the current one."""
+def _entry(name, index):
+    """The entry point, made with GPU `index`, where its tensors and its stream are, as the current one."""
     fn = getattr(lib(), name)
-    if torch.cuda.current_device() == index:
-        code = fn(*args)
-    else:
+    if torch._C._cuda_getDevice() == index:
+        return fn
+
+    def there(*args):
         with torch.cuda.device(index):
-            code = fn(*args)
-    _check(code, name)
+            return fn(*args)
+    return there
 
 
 def _empty(shape, dtype, device, side):
@@ -237,9 +238,10 @@ def _forward(fn_name, ws_fn, q, k, v, out, masked, normalized, eps, chunk, state
     dt = _dtype_code(q)
     if workspace is None:
         workspace = _workspace(ws_fn(B, H, n, d, dv, chunk, dt), q.device, side)
-    _run(fn_name, index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(masked), int(normalized),
-         float(eps), int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace),
-         workspace.numel() * workspace.element_size(), handle)
+    _check(_entry(fn_name, index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(masked), int(normalized),
+        float(eps), int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), handle), fn_name)
     return out
 
 
@@ -268,8 +270,9 @@ def hla2_forward_noalloc(q, k, v, out=None, *, masked=True, normalized=False, ep
     handle, side = _on(stream, index)
     if out is None:
         out = _empty((B, H, n, dv), q.dtype, q.device, side)
-    _run("hla2_forward_noalloc", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, n, d, dv,
-         int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in), handle)
+    _check(_entry("hla2_forward_noalloc", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, n, d, dv,
+        int(masked), int(normalized), float(eps), int(chunk), _ptr(state_in), handle), "hla2_forward_noalloc")
     return out
 
 
@@ -307,8 +310,9 @@ def hla2_step(q, k, v, state, out=None, *, masked=True, normalized=False, eps=1e
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    _run("hla2_step", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(masked),
-         int(normalized), float(eps), _ptr(state), handle)
+    _check(_entry("hla2_step", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(masked),
+        int(normalized), float(eps), _ptr(state), handle), "hla2_step")
     return out
 
 
@@ -331,9 +335,10 @@ def hla2_backward(q, k, v, dout, *, normalized=False, eps=1e-6, chunk=64, worksp
     gq, gk, gv = (_empty(t.shape, t.dtype, t.device, side) for t in (q, k, v))
     if workspace is None:
         workspace = _workspace(hla2_backward_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
-    _run("hla2_backward", index, _ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(gq), _ptr(gk), _ptr(gv), dt, B, H, n, d,
-         dv, int(normalized), float(eps), int(chunk), _ptr(workspace), workspace.numel() * workspace.element_size(),
-         handle)
+    _check(_entry("hla2_backward", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(dout), _ptr(gq), _ptr(gk), _ptr(gv), dt, B, H, n, d,
+        dv, int(normalized), float(eps), int(chunk), _ptr(workspace), workspace.numel() * workspace.element_size(),
+        handle), "hla2_backward")
     return gq, gk, gv
 
 
@@ -363,9 +368,10 @@ def ahla_forward(q, k, v, out=None, *, normalized=False, eps=1e-6, chunk=64, sta
     dt = _dtype_code(q)
     if workspace is None:
         workspace = _workspace(ahla_workspace_bytes(B, H, n, d, dv, chunk, dt), q.device, side)
-    _run("ahla_forward", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(normalized), float(eps),
-         int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace), workspace.numel() * workspace.element_size(),
-         handle)
+    _check(_entry("ahla_forward", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), dt, B, H, n, d, dv, int(normalized), float(eps),
+        int(chunk), _ptr(state_in), _ptr(state_out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+        handle), "ahla_forward")
     return out
 
 
@@ -393,8 +399,9 @@ def ahla_step(q, k, v, state, out=None, *, normalized=False, eps=1e-6, stream=No
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if state.dtype != torch.float32 or not state.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    _run("ahla_step", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-         float(eps), _ptr(state), handle)
+    _check(_entry("ahla_step", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
+        float(eps), _ptr(state), handle), "ahla_step")
     return out
 
 
@@ -410,7 +417,8 @@ def hla2_state_to_sde(state, d: int, dv: int, sde=None, *, stream=None):
     handle, side = _on(stream, index)
     if sde is None:
         sde = _empty((B, H, hla2_sde_state_floats(d, dv)), torch.float32, state.device, side)
-    _run("hla2_state_to_sde", index, _ptr(state), _ptr(sde), B, H, d, dv, handle)
+    _check(_entry("hla2_state_to_sde", index)(
+        _ptr(state), _ptr(sde), B, H, d, dv, handle), "hla2_state_to_sde")
     return sde
 
 
@@ -425,8 +433,9 @@ def hla2_step_sde(q, k, v, sde, out=None, *, normalized=False, eps=1e-6, stream=
         out = _empty((B, H, dv), q.dtype, q.device, side)
     if sde.dtype != torch.float32 or not sde.is_contiguous():
         raise ValueError("state must be contiguous float32")
-    _run("hla2_step_sde", index, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
-         float(eps), _ptr(sde), handle)
+    _check(_entry("hla2_step_sde", index)(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _dtype_code(q), B, H, d, dv, int(normalized),
+        float(eps), _ptr(sde), handle), "hla2_step_sde")
     return out
 
 
@@ -445,13 +454,15 @@ def hla_poll_error(workspace, stream=None) -> int:
 # the operators around the mixers: short convolution, selective scan, q/k norm with rotation
 # ------------------------------------------------------------------------------------------------
 
+_TYPE_CODES = {torch.bfloat16: HLA_BF16, torch.float32: HLA_F32}
+
+
 def _type_code(dtype) -> int:
+    code = _TYPE_CODES.get(dtype)
+    if code is not None:
+        return code
     if isinstance(dtype, int):
         return dtype
-    if dtype == torch.bfloat16:
-        return HLA_BF16
-    if dtype == torch.float32:
-        return HLA_F32
     raise TypeError("tokens must be bfloat16 or float32, got %s" % dtype)
 
 
@@ -468,21 +479,32 @@ def _same_order(got, want):
     return count == other and (count == 0 or a <= b or b <= a)
 
 
-def _flat(name, t, shape, dtype, index):
-    """Address of a contiguous tensor of a shape (or of one that holds it in the same order) on GPU `index` (None
+def _flat(name, t, count, dtype, index):
+    """Address of a contiguous tensor of one dimension and `count` elements on GPU `index` (None stays None)."""
+    if t is None:
+        return None
+    if t.numel() != count or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on cuda:%d, got %s %s on %s"
+                         % (name, dtype, count, index, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
+
+
+def _shaped(name, t, shape, dtype, index):
+    """Address of a contiguous tensor of a shape, or of one that holds it in the same order, on GPU `index` (None
     stays None)."""
     if t is None:
         return None
-    if (t.dtype is not dtype or t.get_device() != index or not t.is_contiguous()
-            or not (t.shape == shape or _same_order(t.shape, shape))):
+    if t.shape != shape and not _same_order(t.shape, shape) or (
+            t.dtype is not dtype or t.get_device() != index or not t.is_contiguous()):
         raise ValueError("%s must be a contiguous %s tensor %s on cuda:%d, got %s %s on %s"
                          % (name, dtype, tuple(shape), index, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
-def _rows(name, t, shape, inner, dtype, index):
-    """Row stride (elements) of a token tensor on GPU `index`: `shape` with rows of strides `inner`."""
-    if t.dtype is dtype and t.get_device() == index and t.shape == shape:
+def _rows(name, t, shape, inner, dtype, index, own=False):
+    """Row stride (elements) of a token tensor on GPU `index`: `shape` with rows of strides `inner`.  own: of the
+    tensor that shape, dtype and index were taken from."""
+    if own or (t.dtype is dtype and t.get_device() == index and t.shape == shape):
         st, lead = t.stride(), len(shape) - len(inner)
         if st[lead:] == inner:
             rows = shape[lead - 1]
@@ -556,12 +578,12 @@ def hla_conv_forward(x, weight, bias=None, out=None, *, silu=True, lengths=None,
     if out is None:
         out = _empty(shape, T, x.device, side)
     kept = (B, W - 1, C)
-    _run(
-        "hla_conv_forward", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
+    _check(_entry("hla_conv_forward", i)(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
         out.data_ptr(), dt, B, n, C, W,
-        _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, (B,), torch.int32, i), _flat("state_in", state_in, kept, T, i),
-        _flat("state_out", state_out, kept, T, i), handle)
+        _rows("x", x, shape, (1,), T, i, True), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
+        _flat("lengths", lengths, B, torch.int32, i), _shaped("state_in", state_in, kept, T, i),
+        _shaped("state_out", state_out, kept, T, i), handle), "hla_conv_forward")
     return out
 
 
@@ -573,11 +595,11 @@ def hla_conv_step(x, weight, state, bias=None, out=None, *, silu=True, stream=No
     B, C = shape
     if out is None:
         out = _empty(shape, T, x.device, side)
-    _run(
-        "hla_conv_step", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
+    _check(_entry("hla_conv_step", i)(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
         out.data_ptr(), dt, B, C, W,
-        _rows("x", x, shape, (1,), T, i), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
-        _flat("state", state, (B, W - 1, C), T, i), handle)
+        _rows("x", x, shape, (1,), T, i, True), _rows("out", out, shape, (1,), T, i), 1 if silu else 0,
+        _shaped("state", state, (B, W - 1, C), T, i), handle), "hla_conv_step")
     return out
 
 
@@ -596,12 +618,12 @@ def hla_conv_backward(x, weight, dout, bias=None, dx=None, *, silu=True, lengths
     dw = _empty((C, W), torch.float32, x.device, side)
     db = None if bias is None else _empty((C,), torch.float32, x.device, side)
     ws, ws_bytes, _keep = _scratch(workspace, hla_conv_backward_workspace_bytes, i, side, B, n, C, W, dt)
-    _run(
-        "hla_conv_backward", i, x.data_ptr(), _flat("weight", weight, (C, W), T, i), _flat("bias", bias, (C,), T, i),
+    _check(_entry("hla_conv_backward", i)(
+        x.data_ptr(), _flat("weight", weight, C * W, T, i), _flat("bias", bias, C, T, i),
         dout.data_ptr(), dx.data_ptr(),
-        dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i),
+        dw.data_ptr(), None if db is None else db.data_ptr(), dt, B, n, C, W, _rows("x", x, shape, (1,), T, i, True),
         _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), 1 if silu else 0,
-        _flat("lengths", lengths, (B,), torch.int32, i), ws, ws_bytes, handle)
+        _flat("lengths", lengths, B, torch.int32, i), ws, ws_bytes, handle), "hla_conv_backward")
     return dx, dw, db
 
 
@@ -627,13 +649,14 @@ def hla_ssm_forward(x, delta, a, b, c, out=None, *, skip=None, delta_bias=None, 
         out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner, kept = (B, n, G, N), (P, 1), (N, 1), (B, H, N, P)
     ws, ws_bytes, _keep = _scratch(workspace, hla_ssm_workspace_bytes, i, side, B, n, H, P, G, N, dt)
-    _run(
-        "hla_ssm_forward", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, (H,), f32, i), b.data_ptr(), c.data_ptr(),
-        _flat("skip", skip, (H,), f32, i), _flat("delta_bias", delta_bias, (H,), f32, i), out.data_ptr(),
-        dt, B, n, H, P, G, N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, n, H), (1,), T, i),
+    _check(_entry("hla_ssm_forward", i)(
+        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(),
+        dt, B, n, H, P, G, N, _rows("x", x, shape, inner, T, i, True), _rows("delta", delta, (B, n, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
-        1 if softplus else 0, _flat("lengths", lengths, (B,), torch.int32, i),
-        _flat("state_in", state_in, kept, f32, i), _flat("state_out", state_out, kept, f32, i), ws, ws_bytes, handle)
+        1 if softplus else 0, _flat("lengths", lengths, B, torch.int32, i),
+        _shaped("state_in", state_in, kept, f32, i), _shaped("state_out", state_out, kept, f32, i), ws, ws_bytes,
+        handle), "hla_ssm_forward")
     return out
 
 
@@ -657,12 +680,12 @@ def hla_ssm_step(x, delta, a, b, c, state, out=None, *, skip=None, delta_bias=No
     if out is None:
         out = _empty(shape, T, x.device, side)
     bc, inner, bc_inner = (B, G, N), (P, 1), (N, 1)
-    _run(
-        "hla_ssm_step", i, x.data_ptr(), delta.data_ptr(), _flat("a", a, (H,), f32, i), b.data_ptr(), c.data_ptr(),
-        _flat("skip", skip, (H,), f32, i), _flat("delta_bias", delta_bias, (H,), f32, i), out.data_ptr(),
-        dt, B, H, P, G, N, _rows("x", x, shape, inner, T, i), _rows("delta", delta, (B, H), (1,), T, i),
+    _check(_entry("hla_ssm_step", i)(
+        x.data_ptr(), delta.data_ptr(), _flat("a", a, H, f32, i), b.data_ptr(), c.data_ptr(),
+        _flat("skip", skip, H, f32, i), _flat("delta_bias", delta_bias, H, f32, i), out.data_ptr(),
+        dt, B, H, P, G, N, _rows("x", x, shape, inner, T, i, True), _rows("delta", delta, (B, H), (1,), T, i),
         _rows("b", b, bc, bc_inner, T, i), _rows("c", c, bc, bc_inner, T, i), _rows("out", out, shape, inner, T, i),
-        1 if softplus else 0, _flat("state", state, (B, H, N, P), f32, i), handle)
+        1 if softplus else 0, _shaped("state", state, (B, H, N, P), f32, i), handle), "hla_ssm_step")
     return out
 
 
@@ -694,12 +717,13 @@ def hla_qk_norm_forward(q, k, wq=None, wk=None, cos=None, sin=None, q_out=None, 
     if k_out is None:
         k_out = _empty((B, H, n, d), T, q.device, side)
     inner, table, heads = (d, 1), (top, rot // 2), (B, H, n, d)
-    _run(
-        "hla_qk_norm_forward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, (d,), T, i), _flat("wk", wk, (d,), T, i),
-        _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
-        _flat("positions", positions, (B, n), torch.int32, i), _flat("q_out", q_out, heads, T, i),
-        _flat("k_out", k_out, heads, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
-        _rows("q", q, shape, inner, T, i), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps, handle)
+    _check(_entry("hla_qk_norm_forward", i)(
+        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        _flat("cos", cos, top * rot // 2, torch.float32, i), _shaped("sin", sin, table, torch.float32, i),
+        _shaped("positions", positions, (B, n), torch.int32, i), _shaped("q_out", q_out, heads, T, i),
+        _shaped("k_out", k_out, heads, T, i), _type_code(T), B, n, H, Hk, d, rot, 1 if interleaved else 0,
+        _rows("q", q, shape, inner, T, i, True), _rows("k", k, (B, n, Hk, d), inner, T, i), pos0, top, eps,
+        handle), "hla_qk_norm_forward")
     return q_out, k_out
 
 
@@ -723,12 +747,13 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
     dwk = None if wk is None else _empty((d,), torch.float32, q.device, side)
     dt, inner, table, heads = _type_code(T), (d, 1), (top, rot // 2), (B, H, n, d)
     ws, ws_bytes, _keep = _scratch(workspace, hla_qk_norm_backward_workspace_bytes, i, side, B, n, H, Hk, d, dt)
-    _run(
-        "hla_qk_norm_backward", i, q.data_ptr(), k.data_ptr(), _flat("wq", wq, (d,), T, i), _flat("wk", wk, (d,), T, i),
-        _flat("cos", cos, table, torch.float32, i), _flat("sin", sin, table, torch.float32, i),
-        _flat("positions", positions, (B, n), torch.int32, i), _flat("dq_out", dq_out, heads, T, i),
-        _flat("dk_out", dk_out, heads, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
+    _check(_entry("hla_qk_norm_backward", i)(
+        q.data_ptr(), k.data_ptr(), _flat("wq", wq, d, T, i), _flat("wk", wk, d, T, i),
+        _flat("cos", cos, top * rot // 2, torch.float32, i), _shaped("sin", sin, table, torch.float32, i),
+        _shaped("positions", positions, (B, n), torch.int32, i), _shaped("dq_out", dq_out, heads, T, i),
+        _shaped("dk_out", dk_out, heads, T, i), dq.data_ptr(), dk.data_ptr(), None if dwq is None else dwq.data_ptr(),
         None if dwk is None else dwk.data_ptr(), dt, B, n, H, Hk, d, rot, 1 if interleaved else 0,
-        _rows("q", q, shape, inner, T, i), _rows("k", k, k_shape, inner, T, i), _rows("dq", dq, shape, inner, T, i),
-        _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes, handle)
+        _rows("q", q, shape, inner, T, i, True), _rows("k", k, k_shape, inner, T, i),
+        _rows("dq", dq, shape, inner, T, i), _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes,
+        handle), "hla_qk_norm_backward")
     return dq, dk, dwq, dwk

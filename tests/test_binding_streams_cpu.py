@@ -93,6 +93,7 @@ def world(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", w.on)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: Stream(w.stream))
     monkeypatch.setattr(torch.cuda, "current_device", lambda: w.device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: w.device, raising=False)
     monkeypatch.setattr(torch.cuda, "device", w.use)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: w.stream, raising=False)
     return w
