@@ -408,6 +408,9 @@ size_t hla_ssm_workspace_bytes(int B, int n, int H, int P, int G, int N, hla_dty
  * P, N in {16, 32, 64, 128}; H a multiple of G.
  * workspace : at least hla_ssm_workspace_bytes(...) bytes, 256-byte aligned; calls
  *             that share one are ordered on one stream; hla_poll_error reads its flag.
+ * fp32 tokens: fp32 throughout.  bf16 tokens with 16-byte aligned rows: sums and
+ * states are fp32 sums of products of bf16 pairs (16 bits: a state is about 4e-6
+ * from the exact one), and outputs, rounded to bf16, may differ by that rounding.
  * A NaN or infinity in a token reaches the outputs of that token and later ones,
  * where it enters them (there as NaN, or infinity), and the state.
  */

@@ -125,10 +125,10 @@ cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 // ends (its launch and set-up overlap with it), and waits with after_previous() before it reads or writes
 // anything that kernel, or one before it, reads or writes.  The earlier kernel says let_next_begin();
 // without it (other libraries' kernels) the next one begins when it has ended.
-// A kernel has ended only when it has waited for those before it: every thread calls after_previous(), at
-// the start wherever it is an entry point's first kernel.  The scans' kernels behind their segments' states
-// read the call's inputs before they wait: the kernel that sums those states waits before it lets the next
-// one begin.
+// A kernel has ended only when it has waited for those before it: every thread of an entry point's first kernel
+// calls after_previous() at the start, and in the others no thread writes to global memory before it has, or before
+// one that it waits for has.  The scans' kernels behind their segments' states read the call's inputs before they
+// wait: the kernel that sums those states waits before it lets the next one begin.
 // What earlier kernels write is not read through const __restrict__ pointers, whose loads may be taken for
 // those of data that does not change while the kernel is there.
 // ---------------------------------------------------------------------------

@@ -15,7 +15,9 @@
 //
 // Precision: products accumulate in fp32 and the state is fp32.  W and the copy of H that
 // C H reads are rounded to bf16 once, they only reach the bf16 output.  w X, which reaches the fp32
-// state, is an exact-to-2^-16 pair hi + lo of bf16, two products.
+// state, is a pair hi + lo of bf16 (16 bits), two products: a state is 4e-6 (2-norm) from a 64-bit one, where
+// fp32 products would leave 1e-7, and a four-hundredth of what the rounding of the bf16 inputs is.  Values of X
+// that are not finite are taken out of W X (take_out).
 //
 // TMEM (512 columns): S (then W of both heads as packed bf16 in its place), H^T, and Y twice.  H is
 // transposed (a lane per column), so that its product's N is the number of states: half the time for
@@ -37,11 +39,11 @@
 //
 // What bounds it: a tile of N = 128 takes about 5,200 cycles, the chain C H and S (1,250) -> hi, lo to their
 // slots (800) -> (w X)^T B (1,200) -> H' and W X (1,000; an MMA of 64 columns takes as long as one of 128)
-// with hand-offs of some 200 each, beside 620 KB through shared memory (4,900 cycles of it).  One of
+// with hand-offs of some 200 each, beside 610 KB through shared memory (4,900 cycles of it).  One of
 // N <= 64 takes 4,600, all of it the epilogue's work: hi, lo 1,300, W 1,100, output 700, H' 450, C H 150, the
-// rest hand-offs.  Measured on a GB300: B8 n2048 H32 P64 G1 N128 51.3 us (44 % of what its bytes take),
-// B1 n32768 H16 P64 G2 N64 67.9 us in three launches (the state sweep 23, the chain 7, this kernel 42,
-// each alone).
+// rest hand-offs.  Measured on a GB300: B8 n2048 H32 P64 G1 N128 51.6 us (44 % of what its bytes take; 9 of them
+// outside the loop over the tiles), B1 n32768 H16 P64 G2 N64 68.8 us in three launches (the state sweep 23, the
+// chain 7, this kernel 42, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
 // each segment's own state, chain_kernel the state before each segment.
