@@ -690,7 +690,11 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                 const int st = j % Sm::kXs, t0 = t_lo + j * kTile;
                 uint8_t *from = smem + Sm::X(st);
                 if (!bar_wait(ms, bEpY0 + (j & 1), (j >> 1) & 1, p)) break;
-                if (*(volatile int *)&ms->odd[st]) {  // columns whose X was taken out, from its token on
+                const int gave_up = *(volatile int *)&ms->abort_flag, odd = *(volatile int *)&ms->odd[st];
+                if (gave_up | odd) {
+                    // where a wait of any role gave up, the epilogue no longer waits for X: it may not have landed
+                    if (gave_up) break;
+                    // columns whose X was taken out, from its token on
                     put_nan(from, reinterpret_cast<uint8_t *>(ms->first[st]), min(kTile, live - t0));
                     ms->odd[st] = 0;
                     fence_async_smem();
