@@ -405,20 +405,19 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
         if (lane == 0) {
             const uint32_t sb4 = smem_u32(smem) >> 4;
             auto lm = [&](uint32_t off) { return sb4 + (off >> 4) + kLboMN; };
-            bool ok = true;
             for (int j = 0; j < u.tiles; ++j) {
                 const int st = j % Sm::kStages;
-                if (!(ok = bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p))) break;
-                if (!(ok = bar_wait(ms, sEpX0 + (j & 1), (j >> 1) & 1, p))) break;
+                if (!bar_wait(ms, sLd0 + st, (j / Sm::kStages) & 1, p)) break;
+                if (!bar_wait(ms, sEpX0 + (j & 1), (j >> 1) & 1, p)) break;
                 tc_fence_after();
                 mma_ss<kN, true, true, 8>(tb, lm(Sm::X(st)), lm(Sm::B(st)), j > 0 ? 1u : 0u);
                 mma_ss<kN, true, true, 8>(tb, lm(Sm::Lo(j)), lm(Sm::B(st)), 1u);
                 umma_commit(&ms->bar[sEvU0 + st]);
             }
-            if (!ok) {  // a wait gave up: MMAs in flight finish (bounded) before TMEM is released
-                umma_commit(&ms->bar[sTear]);
-                mbar_wait(&ms->bar[sTear], 0, kBarWaitNs);
-            }
+            // MMAs in flight finish (bounded) before TMEM is released: where a wait gave up, here or in the epilogue,
+            // nothing else has waited for them
+            umma_commit(&ms->bar[sTear]);
+            mbar_wait(&ms->bar[sTear], 0, kBarWaitNs);
         }
         __syncwarp();
     } else if (warp == kStateLoadWarp) {
@@ -660,15 +659,15 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     if (j + 1 < tiles) ok = bar_wait(ms, bLdX + (buf ^ 1), ((j + 1) >> 1) & 1, p);
                 }
             }
+            // copies and MMAs in flight finish (bounded) before shared memory and TMEM are released: where a wait gave
+            // up, here or in the epilogue, nothing else has waited for them
             if (!ok) {
-                // a wait gave up: copies and MMAs in flight finish (bounded) before shared memory and
-                // TMEM are released
                 for (int j = max(bs - 2, 0); j < bs; ++j)
                     mbar_wait(&ms->bar[(Sm::kApart ? bLdB : bLdX) + (j & 1)], (j >> 1) & 1, kBarWaitNs);
                 if (cs > 0) mbar_wait(&ms->bar[bLdC], (cs - 1) & 1, kBarWaitNs);
-                umma_commit(&ms->bar[bTear]);
-                mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
             }
+            umma_commit(&ms->bar[bTear]);
+            mbar_wait(&ms->bar[bTear], 0, kBarWaitNs);
         }
         __syncwarp();
     } else if (warp == kStoreWarp) {
