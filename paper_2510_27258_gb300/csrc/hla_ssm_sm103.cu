@@ -460,8 +460,8 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
             float4 up, cf;
             block_decays(raw[j & 1], u.live - (u.t_lo + (u.tiles - 1 - j) * kTile + 4 * lane), da, bias, p.softplus, up, cf);
             fetch(j + 2, raw[j & 1]);
-            // every epilogue warp has done with the decays that were here
-            if (j >= 2 && !bar_wait(ms, sEpX0 + (j & 1), ((j - 2) >> 1) & 1, p)) break;
+            // every epilogue warp has done with the decays that were here (the lanes leave together, if one gave up)
+            if (j >= 2 && !__all_sync(0xffffffffu, bar_wait(ms, sEpX0 + (j & 1), ((j - 2) >> 1) & 1, p))) break;
             *reinterpret_cast<float4 *>(&ms->cf[j & 1][e][4 * lane]) = cf;
             if ((lane & 7) == 7) ms->tot[j & 1][e][lane >> 3] = up.w;
             __syncwarp();
@@ -728,8 +728,8 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             if ((lane & 7) == 7) ms->tot[j & 1][e][lane >> 3] = up.w;
             __syncwarp();
             if (lane == 0) mbar_arrive(&ms->bar[bTot0 + (j & 1)]);
-            // every epilogue warp has done with the previous tile's decays
-            if (j > 0 && !bar_wait(ms, bEpW, (j - 1) & 1, p)) break;
+            // every epilogue warp has done with the previous tile's decays (the lanes leave together, if one gave up)
+            if (j > 0 && !__all_sync(0xffffffffu, bar_wait(ms, bEpW, (j - 1) & 1, p))) break;
             *reinterpret_cast<float4 *>(&ms->cum[e][4 * lane]) = up;
             *reinterpret_cast<float4 *>(&ms->cf[e][4 * lane]) = cf;
             __syncwarp();
