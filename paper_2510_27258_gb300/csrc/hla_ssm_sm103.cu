@@ -1048,13 +1048,13 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 }
 
 // rows [B, n] at a row stride, `heads` blocks of `inner` bf16 in each; boxes of 64 columns of one head x
-// 128 tokens, 128-byte swizzle, zero fill past a head's columns and past a sequence's n tokens
-bool make_map(CUtensorMap *m, const void *base, int B, int n, int heads, int inner, long long stride) {
+// `rows` tokens, 128-byte swizzle, zero fill past a head's columns and past a sequence's n tokens
+bool make_map(CUtensorMap *m, const void *base, int B, int n, int heads, int inner, long long stride, int rows = kTile) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[4] = {(cuuint64_t)inner, (cuuint64_t)heads, (cuuint64_t)n, (cuuint64_t)B};
     cuuint64_t strides[3] = {(cuuint64_t)inner * 2, (cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * (cuuint64_t)n};
-    cuuint32_t box[4] = {64, 1, (cuuint32_t)kTile, 1};
+    cuuint32_t box[4] = {64, 1, (cuuint32_t)rows, 1};
     cuuint32_t es[4] = {1, 1, 1, 1};
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -1112,8 +1112,10 @@ bool ssm_tc_applicable(const Ssm &p) {
 
 cudaError_t ssm_tc_launch(const Ssm &p, cudaStream_t stream) {
     CUtensorMap mx, mb, mc, my;
-    if (!make_map(&mx, p.x, p.B, p.n, p.H, p.P, p.x_stride) || !make_map(&mb, p.b, p.B, p.n, p.G, p.N, p.b_stride) ||
-        !make_map(&mc, p.c, p.B, p.n, p.G, p.N, p.c_stride) || !make_map(&my, p.y, p.B, p.n, p.H, p.P, p.y_stride))
+    const int x_rows = getenv("HLA_TEST_SHORT_COPY") ? kTile / 2 : kTile;  // testing: the waits for X run out
+    if (!make_map(&mx, p.x, p.B, p.n, p.H, p.P, p.x_stride, x_rows) ||
+        !make_map(&mb, p.b, p.B, p.n, p.G, p.N, p.b_stride) || !make_map(&mc, p.c, p.B, p.n, p.G, p.N, p.c_stride) ||
+        !make_map(&my, p.y, p.B, p.n, p.H, p.P, p.y_stride))
         return cudaErrorInvalidValue;
     const Cut c = cut(p);
     Params q{};

@@ -1,6 +1,6 @@
 """The selective scan on the GPU where its tiles and segments depend on one another, against the 64-bit recurrence:
-slow decays and large states over many tiles, decays so strong that sums of exponents lose their small terms, and NaN and
-infinities in tokens.
+slow decays and large states over many tiles, decays so strong that sums of exponents lose their small terms, NaN and
+infinities in tokens, and waits that run out.
 
 b, c, x, skip and the states are positive here, so that a sum's value is the magnitude its rounding errors scale
 with: a bound of a few 2^-8 resolves a carried part of one percent."""
@@ -162,3 +162,26 @@ def test_no_token_reaches_an_earlier_one(hla, dtype, bad, B, n, H, P, G, N):
     s2[0, 0, 2, 1] = bad
     free[0, :, 0, 1] = False
     check(run(x, delta, b, c, s2), free)
+
+
+@pytest.mark.parametrize("B,n,H,P,G,N,launches", [(2, 890, 3, 64, 1, 128, 1), (2, 890, 3, 64, 1, 64, 1),
+                                                  (1, 3015, 38, 128, 1, 32, 3)])
+def test_a_wait_that_runs_out_is_reported(hla, monkeypatch, B, n, H, P, G, N, launches):
+    """Copies of x that bring half of the bytes that are waited for (set up on the host): the waits run out (2 s each),
+    the kernels finish, hla_poll_error reports HLA_ERR_TIMEOUT, and the workspace works again."""
+    T = torch.bfloat16
+    assert hla.hla_ssm_forward_path(B, n, H, P, G, N) == (1, launches)
+    x, delta, a, b, c, skip, state = inputs(n + N, B, n, H, P, G, N, T)
+    bias = torch.full((H,), -6.0, device=DEV)
+    ws = hla.alloc_workspace(hla.hla_ssm_workspace_bytes(B, n, H, P, G, N, T), DEV)
+    so = torch.empty_like(state)
+    run = lambda: hla.hla_ssm_forward(x, delta, a, b, c, skip=skip, delta_bias=bias, state_in=state,  # noqa: E731
+                                      state_out=so, workspace=ws)
+    want, state_want = run(), so.clone()
+    assert hla.hla_poll_error(ws) == hla.HLA_OK
+    monkeypatch.setenv("HLA_TEST_SHORT_COPY", "1")
+    run()
+    assert hla.hla_poll_error(ws) == hla.HLA_ERR_TIMEOUT
+    monkeypatch.delenv("HLA_TEST_SHORT_COPY")
+    assert torch.equal(run(), want) and torch.equal(so, state_want)
+    assert hla.hla_poll_error(ws) == hla.HLA_OK
