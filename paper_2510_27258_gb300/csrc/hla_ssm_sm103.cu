@@ -41,8 +41,8 @@
 // slots (800) -> (w X)^T B (1,200) -> H' and W X (1,000; an MMA of 64 columns takes as long as one of 128)
 // with hand-offs of some 200 each, beside 610 KB through shared memory (4,900 cycles of it).  One of
 // N <= 64 takes 4,600, all of it the epilogue's work: hi, lo 1,300, W 1,100, output 700, H' 450, C H 150, the
-// rest hand-offs.  Measured on a GB300: B8 n2048 H32 P64 G1 N128 51.6 us (44 % of what its bytes take; 9 of them
-// outside the loop over the tiles), B1 n32768 H16 P64 G2 N64 68.8 us in three launches (the state sweep 23, the
+// rest hand-offs.  Measured on a GB300: B8 n2048 H32 P64 G1 N128 52.2 us (43 % of what its bytes take; 9 of them
+// outside the loop over the tiles), B1 n32768 H16 P64 G2 N64 68.2 us in three launches (the state sweep 23, the
 // chain 7, this kernel 42, each alone).
 //
 // Few heads: the sequence is cut into segments, one CTA each; a state-only pass (B and X alone) gives
