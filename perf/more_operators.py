@@ -66,14 +66,11 @@ def ffn(name, kind, dtype, rows, K, F, act=SILU):
 def draw(rng):
     """One more case: an operator, a direction, a type, and sizes spread over the listed range."""
     def log(lo, hi):
-        v = int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
-        return v + 1 if v == 3072 else v
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
 
     def width(lo, hi):  # three in four are multiples of 8, as projections are
         v = log(lo, hi)
-        if rng.random() < 0.75:
-            v = max(8, v // 8 * 8)
-        return v + 8 if v == 3072 else v
+        return max(8, v // 8 * 8) if rng.random() < 0.75 else v
 
     flag = lambda p=0.5: rng.random() < p  # noqa: E731
     op = rng.choice(["glr", "glr", "norm", "norm", "ffn"])
