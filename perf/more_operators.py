@@ -139,13 +139,11 @@ def prepare(case, seed):
             grads = empty(B, n, 3 * pad)  # written side by side, as the projection's gradient reads them
             s["dx"], s["dr"], s["dg"] = grads[..., :C], grads[..., pad:pad + C], grads[..., 2 * pad:2 * pad + C]
             s["dstate_in"] = empty(B, C, dtype=torch.float32)
-        if own:
-            s["ws"] = hla.alloc_workspace(hla.hla_glr_workspace_bytes(B, n, C, T), DEV)
-            if case["kind"] == "gradient":  # the states that a training step's forward leaves for its gradient
-                s["marks"] = empty(B, hla.hla_glr_marks(n), C, dtype=torch.float32)
-                hla.hla_glr_forward(s["x"], s["r"], s["g"], s["decay"], lengths=s["lengths"],
-                                    state_in=s["state"] if case["carried"] else None, marks=s["marks"])
-                s["ws"] = hla.alloc_workspace(hla.hla_glr_backward_workspace_bytes(B, n, C, T), DEV)
+        if own and case["kind"] == "gradient":  # the states that a training step's forward leaves for its gradient
+            s["marks"] = empty(B, hla.hla_glr_marks(n), C, dtype=torch.float32)
+            hla.hla_glr_forward(s["x"], s["r"], s["g"], s["decay"], lengths=s["lengths"],
+                                state_in=s["state"] if case["carried"] else None, marks=s["marks"])
+            s["ws"] = hla.alloc_workspace(hla.hla_glr_backward_workspace_bytes(B, n, C, T), DEV)
     elif case["op"] == "norm":
         B, n, C = case["B"], case["n"], case["C"]
         s["x"] = normal(B, n, C)
@@ -159,7 +157,7 @@ def prepare(case, seed):
         if case["kind"] == "gradient":
             s["dx_out"], s["dh"] = normal(B, n, C), normal(B, n, C) if case["pre"] else None
             if own:
-                s["ws"] = hla.alloc_workspace(hla.hla_block_norm_backward_workspace_bytes(B, n, C, T), DEV)
+                s["ws"] = hla.alloc_workspace(hla.hla_block_norm_backward_workspace_bytes(B * n, C, T), DEV)
     else:
         M, K, F = case["rows"], case["K"], case["F"]
         s["x"] = normal(M, K)
@@ -193,7 +191,7 @@ def _own_glr(hla, s, case):
                                      workspace=s["ws"])
         return grads + (s["dstate_in"],)
     hla.hla_glr_forward(s["x"], s["r"], s["g"], s["decay"], s["out"], lengths=s["lengths"],
-                        state_in=s["state"] if case["carried"] else None, state_out=s["state_out"], workspace=s["ws"])
+                        state_in=s["state"] if case["carried"] else None, state_out=s["state_out"])
     return s["out"], s["state_out"]
 
 
@@ -364,8 +362,8 @@ def work(case):
     if case["op"] == "glr":
         states = B * C * 4 * (1 + (case["carried"] or case["kind"] == "token"))
         if case["kind"] == "gradient":
-            # (with the state before every 64th token, without which the tokens are read a second time)
-            return {"bytes": 7 * v * e + B * -(-n // 64) * C * 4 + 2 * B * C * 4 + 2 * C * 4, "flops": 45 * v}
+            # (with the state before every 32nd token, without which the tokens are read a second time)
+            return {"bytes": 7 * v * e + B * -(-n // 32) * C * 4 + 2 * B * C * 4 + 2 * C * 4, "flops": 45 * v}
         return {"bytes": 4 * v * e + states + C * 4, "flops": 20 * v}
     tensors = 2 + case["gated"]
     if case["kind"] == "gradient":
