@@ -479,6 +479,138 @@ hla_status hla_qk_norm_backward(const void *q, const void *k, const void *wq, co
                                 void *workspace, size_t workspace_bytes, hla_stream_t stream);
 
 /*
+ * The rest of a block: a gated recurrence, norms around it, a gated feed-forward part
+ * ----------------------------------------------------------------------------------
+ * Operators that stand beside the mixers and after them (no counterpart in the paper).
+ * Rows, strides, lengths and overlap are as above: token t of sequence b is row
+ * b*n + t at a row stride in elements, and no alignment beyond the element's is
+ * asked of rows.  Sums over tokens are made in a fixed order: equal inputs give
+ * equal bits.
+ */
+
+/* Activations of a gate (also the slopes of the gradients). */
+typedef enum {
+    HLA_LINEAR = 0,  /* v */
+    HLA_SIGMOID = 1, /* 1 / (1 + e^-v) */
+    HLA_SILU = 2     /* v / (1 + e^-v) */
+} hla_act;
+
+/* Number of marks of n tokens: states that hla_glr_forward leaves for hla_glr_backward. */
+int hla_glr_marks(int n);
+
+/*
+ * hla_glr_forward -- gated linear recurrence over a prompt, for each channel:
+ *   s_t = sigmoid(r_t),  a_t = exp(decay s_t),  i_t = sigmoid(g_t),
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,   y_t = h_t
+ * x, r, g, y : device [B, n, C], row strides x_stride, r_stride, g_stride, y_stride, of type dt
+ * decay : device fp32 [C], below 0 (where it is 0, gradients of r and decay are unbounded)
+ * state_in  : device fp32 [B, C] or NULL (= 0)
+ * state_out : device fp32 [B, C] or NULL; the state after lengths[b] tokens.  May equal state_in.
+ * marks     : device fp32 [B, hla_glr_marks(n), C] or NULL; receives the state before
+ *             every 32nd token, which hla_glr_backward reads
+ * decay, states and marks are 16-byte aligned.
+ * No workspace.  fp32 throughout for both types; a NaN or infinity in a token reaches that token's
+ * output and, where it enters the state, later ones, and no earlier one.
+ */
+hla_status hla_glr_forward(const void *x, const void *r, const void *g, const float *decay, void *y, hla_dtype dt, int B,
+                           int n, int C, long long x_stride, long long r_stride, long long g_stride, long long y_stride,
+                           const int *lengths, const float *state_in, float *state_out, float *marks,
+                           hla_stream_t stream);
+
+/*
+ * hla_glr_step -- hla_glr_forward of one token a sequence: x, r, g, y [B, C] with their
+ * row strides; state fp32 [B, C], updated in place.  y may equal x, r or g.  No workspace.
+ */
+hla_status hla_glr_step(const void *x, const void *r, const void *g, const float *decay, void *y, hla_dtype dt, int B, int C,
+                        long long x_stride, long long r_stride, long long g_stride, long long y_stride, float *state,
+                        hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_glr_backward needs (0 if unsupported). */
+size_t hla_glr_backward_workspace_bytes(int B, int n, int C, hla_dtype dt);
+
+/*
+ * hla_glr_backward -- gradients of hla_glr_forward for L = sum dy . y + sum dstate_out . state_out:
+ * dx, dr, dg (rows like x, r, g, with their strides; zero at and after a length), ddecay
+ * (device fp32 [C]) and, if not NULL, dstate_in (device fp32 [B, C]).
+ * dy: device [B, n, C], row stride dy_stride; dstate_out: device fp32 [B, C] or NULL (= 0; may
+ * equal dstate_in); marks: those that the forward with the same x, r, g, decay, lengths and
+ * state_in left.  decay, states, marks and ddecay are 16-byte aligned.
+ */
+hla_status hla_glr_backward(const void *x, const void *r, const void *g, const float *decay, const void *dy,
+                            const float *marks, void *dx, void *dr, void *dg, float *ddecay, hla_dtype dt, int B, int n,
+                            int C, long long x_stride, long long r_stride, long long g_stride, long long dy_stride,
+                            long long dx_stride, long long dr_stride, long long dg_stride, const int *lengths,
+                            const float *dstate_out, float *dstate_in, void *workspace, size_t workspace_bytes,
+                            hla_stream_t stream);
+
+/*
+ * hla_block_norm_forward -- what stands between two blocks: the norm of a block's output y with
+ * its gate, residual scale and dropout, the residual sum, and the norm before the next block:
+ *   x' = alpha x + k scale act(gate) u w_post,   u = y / sqrt(mean(y^2) + eps), or y if post_norm == 0
+ *   h  = x' / sqrt(mean(x'^2) + eps) w_pre       if pre_norm   (of x' before it is rounded)
+ * means over a row's C columns; k = 1 without dropout, else 0 or 1 / (1 - dropout): value (row,
+ * column) is dropped where its 32 random bits are below floor(dropout 2^32), bits that
+ * Philox4x32-10 gives for the counter (column / 4, row, offset low, offset high) and the key (seed
+ * low, seed high), word column % 4.  The mask is not stored: the gradient makes it again.
+ * x, y, gate : device [rows, C], row strides x_stride, y_stride, gate_stride, of type dt; gate may be NULL (= 1)
+ * w_post, scale, w_pre : device [C] of type dt, or NULL (= 1; w_post and w_pre are not read without their norm)
+ * x_out : device [rows, C], row stride x_out_stride (written; may equal x, with its stride)
+ * h     : device [rows, C], row stride h_stride (written; not read or written without pre_norm)
+ * 0 <= dropout < 1; eps >= 0 finite; alpha finite; offset and seed: any 64 bits.
+ */
+hla_status hla_block_norm_forward(const void *x, const void *y, const void *gate, const void *w_post, const void *scale,
+                                  const void *w_pre, void *x_out, void *h, hla_dtype dt, int rows, int C,
+                                  long long x_stride, long long y_stride, long long gate_stride, long long x_out_stride,
+                                  long long h_stride, int post_norm, int pre_norm, int act, float alpha, float eps,
+                                  double dropout, unsigned long long seed, unsigned long long offset, hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_block_norm_backward needs (0 if unsupported). */
+size_t hla_block_norm_backward_workspace_bytes(int rows, int C, hla_dtype dt);
+
+/*
+ * hla_block_norm_backward -- gradients of hla_block_norm_forward for L = sum dx_out . x_out + sum dh . h:
+ * dx, dy, dgate (rows like x, y, gate, with their strides; dgate NULL without a gate) and, where not
+ * NULL, dw_post, dscale, dw_pre (device fp32 [C]; zeros where a norm is off).
+ * dx_out, dh: device [rows, C] with their row strides; dh is not read without pre_norm.
+ * dx may equal dx_out, with its stride.
+ */
+hla_status hla_block_norm_backward(const void *x, const void *y, const void *gate, const void *w_post, const void *scale,
+                                   const void *w_pre, const void *dx_out, const void *dh, void *dx, void *dy, void *dgate,
+                                   float *dw_post, float *dscale, float *dw_pre, hla_dtype dt, int rows, int C,
+                                   long long x_stride, long long y_stride, long long gate_stride, long long dx_out_stride,
+                                   long long dh_stride, long long dx_stride, long long dy_stride, long long dgate_stride,
+                                   int post_norm, int pre_norm, int act, float alpha, float eps, double dropout,
+                                   unsigned long long seed, unsigned long long offset, void *workspace,
+                                   size_t workspace_bytes, hla_stream_t stream);
+
+/* Bytes of scratch workspace hla_ffn_forward and hla_ffn_backward need (0 if unsupported). */
+size_t hla_ffn_workspace_bytes(int rows, int K, int F, hla_dtype dt);
+size_t hla_ffn_backward_workspace_bytes(int rows, int K, int F, hla_dtype dt);
+
+/*
+ * hla_ffn_forward -- gated feed-forward projections, activation and product:
+ *   out = act(x Wg^T) (x Wu^T)
+ * x   : device [rows, K], row stride x_stride, of type dt
+ * w   : device [2, F, K] of type dt: Wg, then Wu
+ * out : device [rows, F], row stride out_stride, of type dt (written)
+ * The products are rounded once, after the activation.  workspace: 256-byte aligned; hla_poll_error
+ * reads its flag.
+ */
+hla_status hla_ffn_forward(const void *x, const void *w, void *out, hla_dtype dt, int rows, int K, int F,
+                           long long x_stride, long long out_stride, int act, void *workspace, size_t workspace_bytes,
+                           hla_stream_t stream);
+
+/*
+ * hla_ffn_backward -- gradients of hla_ffn_forward for L = sum dout . out, which computes the
+ * projections again: dx (device [rows, K], row stride dx_stride) and dw (device [2, F, K]), of type dt.
+ * dout: device [rows, F], row stride dout_stride.  bf16: the projections' gradients are rounded to bf16
+ * once between the products.
+ */
+hla_status hla_ffn_backward(const void *x, const void *w, const void *dout, void *dx, void *dw, hla_dtype dt, int rows,
+                            int K, int F, long long x_stride, long long dout_stride, long long dx_stride, int act,
+                            void *workspace, size_t workspace_bytes, hla_stream_t stream);
+
+/*
  * hla_poll_error_noalloc -- hla_poll_error for hla2_forward_noalloc (no
  * counterpart in the paper): waits for `stream`, then reports and clears the
  * device-side error word of the library's scratch array on the current device:

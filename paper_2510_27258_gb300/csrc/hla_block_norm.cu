@@ -1,0 +1,576 @@
+// The norms after and before a block with its gate, residual scale and dropout, and their gradients.
+//
+//   u = y r1, r1 = 1 / sqrt(mean(y^2) + eps)   (u = y without the norm after the block)
+//   x' = alpha x + k scale act(gate) u w_post,   h = x' r2 w_pre,  r2 = 1 / sqrt(mean(x'^2) + eps)
+// k is 0 or 1 / (1 - p) by 32 bits for each value, Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3") of (column / 4, row, offset) under the seed: word column % 4; both directions make
+// the same bits, none are stored.  Backwards, with t the gradient of x':
+//   t = dx' + r2 (dh w_pre - x' r2 mean(dh w_pre x' r2)),  dx = alpha t,  q = t k act(gate),
+//   dy = r1 (q scale w_post - u mean(q scale w_post u)),  dgate = t k scale u w_post act'(gate),
+//   dw_post = sum q scale u,  dscale = sum q u w_post,  dw_pre = sum dh x' r2.
+//
+// Bound by memory traffic: every tensor is read and written once.  A row belongs to a block (up to 256 columns: to a
+// warp), eight columns a thread in registers, with the block's next row in flight; blocks stay for many rows, so
+// that the weights are loaded once and the gradient's sums over rows stay in registers.  Rows of more than
+// 8192 columns are walked several times by one block.  Statistics, products and sums are fp32; each output is
+// rounded once.
+#include <type_traits>
+
+#include "hla_vec.cuh"
+
+namespace hla {
+namespace {
+
+constexpr int kPer = 8;                        // columns of a thread
+constexpr int kNarrow = 32 * kPer, kWide = 1024 * kPer;
+constexpr int kMaxWarps = 32, kNarrowRows = 4;
+
+struct Words {
+    uint32_t w[4];
+};
+// Philox4x32-10
+__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint64_t offset, uint64_t seed) {
+    uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32), k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)p0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return {{c0, c1, c2, c3}};
+}
+
+// a bit for each of kV columns from `col` on: kept
+template <int kV>
+__device__ __forceinline__ uint32_t kept(const BlockNorm &p, long long row, int col) {
+    uint32_t bits = 0;
+    if (kV == 1) {
+        const Words r = philox((uint32_t)(col >> 2), (uint32_t)row, p.offset, p.seed);
+        const uint32_t w = (col & 2) ? ((col & 1) ? r.w[3] : r.w[2]) : ((col & 1) ? r.w[1] : r.w[0]);
+        return w >= p.drop_below;
+    }
+#pragma unroll
+    for (int j = 0; j < kV; j += 4) {
+        const Words r = philox((uint32_t)((col + j) >> 2), (uint32_t)row, p.offset, p.seed);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits |= (r.w[i] >= p.drop_below ? 1u : 0u) << (j + i);
+    }
+    return bits;
+}
+
+// act(v) and, if asked, its slope
+template <bool kSlope>
+__device__ __forceinline__ float activation(int act, float v, float &slope) {
+    if (act == HLA_LINEAR) {
+        slope = 1.f;
+        return v;
+    }
+    const float s = __fdividef(1.f, 1.f + __expf(-v));  // (v of -89 and below: 0, as the rounded sigmoid)
+    if (act == HLA_SIGMOID) {
+        if (kSlope) slope = s * (1.f - s);
+        return s;
+    }
+    if (kSlope) slope = s * (1.f + v * (1.f - s));
+    return v * s;
+}
+
+// A thread's eight columns: kE accesses of kV neighbours, `threads` apart
+template <typename T, int kV>
+struct Cols {
+    static constexpr int kE = kPer / kV;
+    Raw<T, kV> r[kE];
+    static __device__ __forceinline__ int at(int e, int t, int threads) { return (e * threads + t) * kV; }
+    __device__ __forceinline__ void load(const T *row, int t, int threads, int C) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const int c = at(e, t, threads);
+            r[e] = c < C ? raw_load<T, kV>(row + c) : raw_zero<T, kV>();
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[kPer]) const {
+        if constexpr (kV == 1) {
+#pragma unroll
+            for (int e = 0; e < kE; ++e) v[e] = to_f32(r[e].v[0]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kE; ++e) {
+                uint64_t f[kV / 2];
+                to_pairs(r[e], f);
+#pragma unroll
+                for (int i = 0; i < kV / 2; ++i) unpair(f[i], v[e * kV + 2 * i], v[e * kV + 2 * i + 1]);
+            }
+        }
+    }
+    static __device__ __forceinline__ void put(T *row, int t, int threads, int C, const float (&v)[kPer]) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const int c = at(e, t, threads);
+            float f[kV];
+#pragma unroll
+            for (int i = 0; i < kV; ++i) f[i] = v[e * kV + i];
+            if (c < C) VecIo<T, kV>::store(row + c, f);
+        }
+    }
+};
+
+// a weight's eight columns, or ones
+template <typename T, int kV>
+__device__ __forceinline__ void weight(const void *w, int t, int threads, int C, float (&v)[kPer]) {
+    if (!w) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[i] = 1.f;
+        return;
+    }
+    Cols<T, kV> c;
+    c.load(static_cast<const T *>(w), t, threads, C);
+    c.get(v);
+}
+
+// Sums of kN values over a warp, or over a block through `red` (two buffers in turn: one barrier a sum)
+template <int kN>
+struct Sum {
+    float v[kN];
+};
+template <int kN>
+__device__ __forceinline__ void warp_sum(Sum<kN> &s) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) s.v[i] += __shfl_xor_sync(0xffffffffu, s.v[i], o);
+}
+template <bool kBlock, int kN>
+__device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
+    warp_sum(s);
+    if (!kBlock) return;
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < kN; ++i) red[turn][i][warp] = s.v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+        float sum = 0.f;
+        for (int w = 0; w < warps; w += 4) {  // (what is behind the last warp was cleared)
+            const float4 f = *reinterpret_cast<const float4 *>(&red[turn][i][w]);
+            sum += (f.x + f.y) + (f.z + f.w);
+        }
+        s.v[i] = sum;
+    }
+    turn ^= 1;
+}
+
+__device__ __forceinline__ void clear(float (&red)[2][2][kMaxWarps]) {
+    float *f = &red[0][0][0];
+    for (int i = threadIdx.x; i < 4 * kMaxWarps; i += blockDim.x) f[i] = 0.f;
+    __syncthreads();
+}
+
+// ------------------------------------------------------------------------------------------------
+// forward
+// ------------------------------------------------------------------------------------------------
+
+// kMax: the block's threads at most (0: a warp for each row)
+template <typename T, int kV, int kMax>
+__global__ void __launch_bounds__(kMax ? kMax : 128) block_norm_forward_kernel(BlockNorm p) {
+    constexpr bool kBlock = kMax > 0;
+    __shared__ __align__(16) float red[2][2][kMaxWarps];
+    let_next_begin();
+    after_previous();
+    int turn = 0;
+    if (kBlock) clear(red);
+    const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
+    const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
+    const float inv = 1.f / C;
+    float w_post[kPer], scale[kPer], w_pre[kPer];
+    weight<T, kV>(p.scale, t, threads, C, scale);
+    weight<T, kV>(p.w_post, t, threads, C, w_post);
+    weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) scale[i] *= w_post[i] * p.keep_scale;
+    Cols<T, kV> cx, cy, cg;
+    auto load = [&](long long row) {
+        cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
+        cy.load(static_cast<const T *>(p.y) + row * p.y_stride, t, threads, C);
+        if (p.gate) cg.load(static_cast<const T *>(p.gate) + row * p.gate_stride, t, threads, C);
+    };
+    long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
+    if (row < p.rows) load(row);
+    for (; row < p.rows; row += step) {  // (all of a row's threads alike)
+        float x[kPer], y[kPer], g[kPer];
+        cx.get(x);
+        cy.get(y);
+        if (p.gate) cg.get(g);
+        if (row + step < p.rows) load(row + step);
+        float r1 = 1.f;
+        if (p.post) {
+            Sum<1> s{{0.f}};
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) s.v[0] += y[i] * y[i];
+            row_sum<kBlock>(s, red, turn);
+            r1 = rsqrtf(s.v[0] * inv + p.eps);
+        }
+        Sum<1> s2{{0.f}};
+#pragma unroll
+        for (int e = 0; e < kPer / kV; ++e) {
+            const uint32_t bits = p.drop ? kept<kV>(p, row, Cols<T, kV>::at(e, t, threads)) : ~0u;
+#pragma unroll
+            for (int j = 0; j < kV; ++j) {
+                const int i = e * kV + j;
+                float slope, f = y[i] * r1 * scale[i];
+                if (p.gate) f *= activation<false>(p.act, g[i], slope);
+                x[i] = p.alpha * x[i] + (bits >> j & 1 ? f : 0.f);
+                s2.v[0] += x[i] * x[i];
+            }
+        }
+        Cols<T, kV>::put(static_cast<T *>(p.x_out) + row * p.x_out_stride, t, threads, C, x);
+        if (p.pre) {
+            row_sum<kBlock>(s2, red, turn);
+            const float r2 = rsqrtf(s2.v[0] * inv + p.eps);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] *= r2 * w_pre[i];
+            Cols<T, kV>::put(static_cast<T *>(p.h) + row * p.h_stride, t, threads, C, x);
+        }
+    }
+}
+
+// One column of a wide row: what both passes over it need
+template <typename T>
+struct Wide {
+    const BlockNorm &p;
+    long long row;
+    __device__ __forceinline__ static float of(const void *w, int c) { return w ? to_f32(static_cast<const T *>(w)[c]) : 1.f; }
+    __device__ __forceinline__ float y(int c) const { return to_f32(static_cast<const T *>(p.y)[row * p.y_stride + c]); }
+    __device__ __forceinline__ float keep(int c) const { return !p.drop ? 1.f : kept<1>(p, row, c) ? p.keep_scale : 0.f; }
+    __device__ __forceinline__ float act(int c, float &slope) const {
+        return p.gate ? activation<true>(p.act, to_f32(static_cast<const T *>(p.gate)[row * p.gate_stride + c]), slope)
+                      : (slope = 0.f, 1.f);
+    }
+    // x' of one column (k, a and its slope too)
+    __device__ __forceinline__ float x_out(int c, float r1, float &k, float &a, float &slope) const {
+        k = keep(c);
+        a = act(c, slope);
+        const float f = k != 0.f ? y(c) * r1 * of(p.w_post, c) * of(p.scale, c) * k * a : 0.f;
+        return p.alpha * to_f32(static_cast<const T *>(p.x)[row * p.x_stride + c]) + f;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(1024) block_norm_wide_forward_kernel(BlockNorm p) {
+    __shared__ __align__(16) float red[2][2][kMaxWarps];
+    let_next_begin();
+    after_previous();
+    int turn = 0;
+    const float inv = 1.f / p.C;
+    float k, a, slope;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const Wide<T> in{p, row};
+        float r1 = 1.f, r2 = 1.f;
+        if (p.post) {
+            Sum<1> s{{0.f}};
+            for (int c = threadIdx.x; c < p.C; c += 1024) s.v[0] += in.y(c) * in.y(c);
+            row_sum<true>(s, red, turn);
+            r1 = rsqrtf(s.v[0] * inv + p.eps);
+        }
+        if (p.pre) {
+            Sum<1> s{{0.f}};
+            for (int c = threadIdx.x; c < p.C; c += 1024) {
+                const float x = in.x_out(c, r1, k, a, slope);
+                s.v[0] += x * x;
+            }
+            row_sum<true>(s, red, turn);
+            r2 = rsqrtf(s.v[0] * inv + p.eps);
+        }
+        for (int c = threadIdx.x; c < p.C; c += 1024) {  // (x_out may be x: a column is read and written by one thread)
+            const float x = in.x_out(c, r1, k, a, slope);
+            from_f32(static_cast<T *>(p.x_out) + row * p.x_out_stride + c, x);
+            if (p.pre) from_f32(static_cast<T *>(p.h) + row * p.h_stride + c, x * r2 * Wide<T>::of(p.w_pre, c));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// gradient
+// ------------------------------------------------------------------------------------------------
+
+// what is left of the gradient where the row's sums are known
+__device__ __forceinline__ float grad_x_out(float dx_out, float gw, float x_out, float r2, float m2) {
+    return dx_out + r2 * (gw - x_out * r2 * m2);
+}
+
+template <typename T, int kV, int kMax>
+__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 256 ? 2 : 1) block_norm_backward_kernel(BlockNormBwd q) {
+    constexpr bool kBlock = kMax > 0;
+    __shared__ __align__(16) float red[2][2][kMaxWarps];
+    __shared__ float sums[kBlock ? 1 : 3 * kNarrow];
+    let_next_begin();
+    after_previous();
+    const BlockNorm &p = q.f;
+    int turn = 0;
+    if (kBlock) clear(red);
+    const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
+    const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
+    const float inv = 1.f / C;
+    float w_post[kPer], scale[kPer], w_pre[kPer];
+    weight<T, kV>(p.scale, t, threads, C, scale);
+    weight<T, kV>(p.w_post, t, threads, C, w_post);
+    weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+    float dw_post[kPer] = {}, dscale[kPer] = {}, dw_pre[kPer] = {};
+    Cols<T, kV> cx, cy, cg, cd, ch;
+    auto load = [&](long long row) {
+        cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
+        cy.load(static_cast<const T *>(p.y) + row * p.y_stride, t, threads, C);
+        cd.load(static_cast<const T *>(q.dx_out) + row * q.dx_out_stride, t, threads, C);
+        if (p.gate) cg.load(static_cast<const T *>(p.gate) + row * p.gate_stride, t, threads, C);
+        if (p.pre) ch.load(static_cast<const T *>(q.dh) + row * q.dh_stride, t, threads, C);
+    };
+    long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
+    if (row < p.rows) load(row);
+    for (; row < p.rows; row += step) {
+        float x[kPer], y[kPer], a[kPer], slope[kPer], d[kPer], h[kPer];
+        cx.get(x);
+        cy.get(y);
+        cd.get(d);
+        if (p.gate) cg.get(a);
+        if (p.pre) ch.get(h);
+        if (row + step < p.rows) load(row + step);
+        float r1 = 1.f;
+        if (p.post) {
+            Sum<1> s{{0.f}};
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) s.v[0] += y[i] * y[i];
+            row_sum<kBlock>(s, red, turn);
+            r1 = rsqrtf(s.v[0] * inv + p.eps);
+        }
+        uint32_t bits = ~0u;
+        if (p.drop) {
+            bits = 0;
+#pragma unroll
+            for (int e = 0; e < kPer / kV; ++e) bits |= kept<kV>(p, row, Cols<T, kV>::at(e, t, threads)) << (e * kV);
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            y[i] *= r1;  // u
+            if (p.gate) {
+                a[i] = activation<true>(p.act, a[i], slope[i]);
+            } else {
+                a[i] = 1.f;
+            }
+        }
+        if (p.pre) {
+            Sum<2> s{{0.f, 0.f}};
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const float f = y[i] * w_post[i] * scale[i] * a[i] * p.keep_scale;
+                x[i] = p.alpha * x[i] + (bits >> i & 1 ? f : 0.f);  // x'
+                s.v[0] += x[i] * x[i];
+                s.v[1] += h[i] * w_pre[i] * x[i];
+            }
+            row_sum<kBlock>(s, red, turn);
+            const float r2 = rsqrtf(s.v[0] * inv + p.eps), m2 = s.v[1] * r2 * inv;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                d[i] = grad_x_out(d[i], h[i] * w_pre[i], x[i], r2, m2);  // t
+                dw_pre[i] += h[i] * x[i] * r2;
+            }
+        }
+        // (x is free now: the gradient of x, then q scale w_post)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = p.alpha * d[i];
+        Cols<T, kV>::put(static_cast<T *>(q.dx) + row * q.dx_stride, t, threads, C, x);
+        Sum<1> s3{{0.f}};
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const float tk = bits >> i & 1 ? d[i] * p.keep_scale : 0.f, through = tk * a[i], dn = through * scale[i];
+            const bool on = bits >> i & 1;
+            if (on) {
+                dscale[i] += through * y[i] * w_post[i];
+                dw_post[i] += dn * y[i];
+            }
+            x[i] = dn * w_post[i];
+            s3.v[0] += x[i] * y[i];
+            if (p.gate) a[i] = on ? tk * scale[i] * y[i] * w_post[i] * slope[i] : 0.f;  // dgate
+        }
+        if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, C, a);
+        if (p.post) {
+            row_sum<kBlock>(s3, red, turn);
+            const float m = s3.v[0] * inv;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) x[i] = r1 * (x[i] - y[i] * m);
+        }
+        Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, C, x);
+    }
+    // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
+    if (!kBlock) {
+        for (int w = 0; w < kNarrowRows; ++w) {
+            if ((threadIdx.x >> 5) == w) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const int c = Cols<T, kV>::at(i / kV, t, 32) + i % kV;
+                    sums[c] = w ? sums[c] + dw_post[i] : dw_post[i];
+                    sums[kNarrow + c] = w ? sums[kNarrow + c] + dscale[i] : dscale[i];
+                    sums[2 * kNarrow + c] = w ? sums[2 * kNarrow + c] + dw_pre[i] : dw_pre[i];
+                }
+            }
+            __syncthreads();
+        }
+    }
+    float *to = q.partial + (size_t)blockIdx.x * 3 * C;
+    if (kBlock || threadIdx.x < 32) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
+            if (c < C) {
+                to[c] = kBlock ? dw_post[i] : sums[c];
+                to[C + c] = kBlock ? dscale[i] : sums[kNarrow + c];
+                to[2 * (size_t)C + c] = kBlock ? dw_pre[i] : sums[2 * kNarrow + c];
+            }
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNormBwd q) {
+    __shared__ __align__(16) float red[2][2][kMaxWarps];
+    let_next_begin();
+    after_previous();
+    const BlockNorm &p = q.f;
+    int turn = 0;
+    const float inv = 1.f / p.C;
+    float *to = q.partial + (size_t)blockIdx.x * 3 * p.C;
+    float k, a, slope;
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const Wide<T> in{p, row};
+        float r1 = 1.f, r2 = 1.f, m2 = 0.f, m1 = 0.f;
+        if (p.post) {
+            Sum<1> s{{0.f}};
+            for (int c = threadIdx.x; c < p.C; c += 1024) s.v[0] += in.y(c) * in.y(c);
+            row_sum<true>(s, red, turn);
+            r1 = rsqrtf(s.v[0] * inv + p.eps);
+        }
+        auto dh = [&](int c) { return p.pre ? to_f32(static_cast<const T *>(q.dh)[row * q.dh_stride + c]) : 0.f; };
+        if (p.pre) {
+            Sum<2> s{{0.f, 0.f}};
+            for (int c = threadIdx.x; c < p.C; c += 1024) {
+                const float x = in.x_out(c, r1, k, a, slope);
+                s.v[0] += x * x;
+                s.v[1] += dh(c) * Wide<T>::of(p.w_pre, c) * x;
+            }
+            row_sum<true>(s, red, turn);
+            r2 = rsqrtf(s.v[0] * inv + p.eps);
+            m2 = s.v[1] * r2 * inv;
+        }
+        // the gradient of x' (and x' itself)
+        auto back = [&](int c, float &x) {
+            x = in.x_out(c, r1, k, a, slope);
+            const float d = to_f32(static_cast<const T *>(q.dx_out)[row * q.dx_out_stride + c]);
+            return p.pre ? grad_x_out(d, dh(c) * Wide<T>::of(p.w_pre, c), x, r2, m2) : d;
+        };
+        if (p.post) {
+            Sum<1> s{{0.f}};
+            for (int c = threadIdx.x; c < p.C; c += 1024) {
+                float x;
+                const float tk = back(c, x);
+                if (k != 0.f) s.v[0] += tk * k * a * Wide<T>::of(p.scale, c) * Wide<T>::of(p.w_post, c) * in.y(c) * r1;
+            }
+            row_sum<true>(s, red, turn);
+            m1 = s.v[0] * inv;
+        }
+        for (int c = threadIdx.x; c < p.C; c += 1024) {
+            float x;
+            const float tg = back(c, x), u = in.y(c) * r1, w = Wide<T>::of(p.w_post, c), sc = Wide<T>::of(p.scale, c);
+            const bool on = k != 0.f;
+            const float tk = on ? tg * k : 0.f, through = tk * a;
+            from_f32(static_cast<T *>(q.dx) + row * q.dx_stride + c, p.alpha * tg);
+            from_f32(static_cast<T *>(q.dy) + row * q.dy_stride + c,
+                     p.post ? r1 * (through * sc * w - u * m1) : through * sc * w);
+            if (p.gate) from_f32(static_cast<T *>(q.dgate) + row * q.dgate_stride + c, on ? tk * sc * u * w * slope : 0.f);
+            const float add[3] = {on ? through * sc * u : 0.f, on ? through * u * w : 0.f, p.pre ? dh(c) * x * r2 : 0.f};
+            const bool first = row == blockIdx.x;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+                float *at = to + (size_t)j * p.C + c;
+                *at = first ? add[j] : *at + add[j];
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------------------
+
+constexpr int kSMs = 152;
+
+struct Plan {
+    unsigned grid;
+    int threads;
+};
+// Blocks that the GPU holds at `per_sm` threads an SM, or fewer where there are not so many rows
+Plan plan(long long rows, int C, int per_sm) {
+    const int threads = C <= kNarrow ? 128 : C > kWide ? 1024 : (C + 32 * kPer - 1) / (32 * kPer) * 32;
+    const long long blocks = C <= kNarrow ? (rows + kNarrowRows - 1) / kNarrowRows : rows;
+    const long long most = (long long)kSMs * (per_sm / threads > 0 ? per_sm / threads : 1);
+    return {(unsigned)(blocks < most ? blocks : most), threads};
+}
+constexpr int kFwdThreads = 1024, kBwdThreads = 512;
+
+// the widest access that every row allows: 16 bytes, or one element
+template <typename T>
+bool wide_rows(const BlockNorm &p) {
+    const size_t by = 16;
+    auto ok = [&](const void *q, long long stride) { return !q || rows_aligned(q, stride, sizeof(T), by); };
+    return p.C % (by / sizeof(T)) == 0 && ok(p.x, p.x_stride) && ok(p.y, p.y_stride) && ok(p.gate, p.gate_stride) &&
+           ok(p.x_out, p.x_out_stride) && ok(p.h, p.h_stride) && ok(p.w_post, 0) && ok(p.scale, 0) && ok(p.w_pre, 0);
+}
+template <typename T>
+bool wide_rows(const BlockNormBwd &q) {
+    auto ok = [&](const void *p, long long stride) { return !p || rows_aligned(p, stride, sizeof(T), 16); };
+    return wide_rows<T>(q.f) && ok(q.dx_out, q.dx_out_stride) && ok(q.dh, q.dh_stride) && ok(q.dx, q.dx_stride) &&
+           ok(q.dy, q.dy_stride) && ok(q.dgate, q.dgate_stride);
+}
+
+template <typename T>
+cudaError_t forward_of(const BlockNorm &p, cudaStream_t s) {
+    const Plan g = plan(p.rows, p.C, kFwdThreads);
+    if (p.C > kWide) return launch_after(block_norm_wide_forward_kernel<T>, g.grid, 1024, 0, s, p);
+    auto as = [&](auto V) -> cudaError_t {
+        return p.C <= kNarrow      ? launch_after(block_norm_forward_kernel<T, V(), 0>, g.grid, g.threads, 0, s, p)
+               : g.threads <= 256 ? launch_after(block_norm_forward_kernel<T, V(), 256>, g.grid, g.threads, 0, s, p)
+               : g.threads <= 512 ? launch_after(block_norm_forward_kernel<T, V(), 512>, g.grid, g.threads, 0, s, p)
+                                  : launch_after(block_norm_forward_kernel<T, V(), 1024>, g.grid, g.threads, 0, s, p);
+    };
+    return wide_rows<T>(p) ? as(std::integral_constant<int, 16 / sizeof(T)>()) : as(std::integral_constant<int, 1>());
+}
+
+template <typename T>
+cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
+    const BlockNorm &p = q.f;
+    const Plan g = plan(p.rows, p.C, kBwdThreads);
+    auto as = [&](auto V) -> cudaError_t {
+        return p.C <= kNarrow      ? launch_after(block_norm_backward_kernel<T, V(), 0>, g.grid, g.threads, 0, s, q)
+               : g.threads <= 256 ? launch_after(block_norm_backward_kernel<T, V(), 256>, g.grid, g.threads, 0, s, q)
+               : g.threads <= 512 ? launch_after(block_norm_backward_kernel<T, V(), 512>, g.grid, g.threads, 0, s, q)
+                                  : launch_after(block_norm_backward_kernel<T, V(), 1024>, g.grid, g.threads, 0, s, q);
+    };
+    const cudaError_t e = p.C > kWide ? launch_after(block_norm_wide_backward_kernel<T>, g.grid, 1024, 0, s, q)
+                          : wide_rows<T>(q) ? as(std::integral_constant<int, 16 / sizeof(T)>())
+                                            : as(std::integral_constant<int, 1>());
+    if (e) return e;
+    return column_sum_launch({q.partial, g.grid, p.C, 3, {q.dw_post, q.dscale, q.dw_pre}, q.header}, s);
+}
+
+}  // namespace
+
+cudaError_t block_norm_forward_launch(const BlockNorm &p, cudaStream_t s) {
+    return p.dt == HLA_BF16 ? forward_of<__nv_bfloat16>(p, s) : forward_of<float>(p, s);
+}
+size_t block_norm_partial_floats(long long rows, int C) { return (size_t)plan(rows, C, kBwdThreads).grid * 3 * C; }
+cudaError_t block_norm_backward_launch(const BlockNormBwd &q, cudaStream_t s) {
+    return q.f.dt == HLA_BF16 ? backward_of<__nv_bfloat16>(q, s) : backward_of<float>(q, s);
+}
+
+}  // namespace hla

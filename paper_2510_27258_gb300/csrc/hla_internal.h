@@ -135,6 +135,26 @@ cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// (clusters of `cluster` blocks, which divides the grid)
+template <typename... P, typename... A>
+cudaError_t launch_cluster_after(void (*kernel)(P...), unsigned grid, unsigned block, unsigned cluster, size_t smem,
+                                 cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 template <typename... P, typename... A>
 cudaError_t launch_after(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, A... args) {
     cudaLaunchAttribute attr{};
@@ -226,5 +246,94 @@ struct QkNormBwd {
 cudaError_t qk_norm_forward_launch(const QkNorm &p, cudaStream_t stream);
 size_t qk_norm_partial_floats(int B, int n, int H, int Hk, int d);
 cudaError_t qk_norm_backward_launch(const QkNormBwd &p, cudaStream_t stream);
+
+// gated linear recurrence (hla_glr.cu)
+constexpr int kGlrTile = 32;  // tokens between marks
+__host__ __device__ constexpr int glr_marks(int n) { return n / kGlrTile + (n % kGlrTile ? 1 : 0); }
+struct Glr {
+    const void *x, *r, *g;
+    const float *decay;
+    void *y;
+    hla_dtype dt;
+    int B, n, C;
+    long long x_stride, r_stride, g_stride, y_stride;
+    const int *lengths;
+    const float *state_in;
+    float *state_out;  // the step's state, updated in place
+    float *marks;
+};
+struct GlrBwd {
+    Glr f;  // marks are read; y, state_in and state_out unused
+    const void *dy;
+    const float *dstate_out;
+    void *dx, *dr, *dg;
+    float *ddecay, *dstate_in;
+    long long dy_stride, dx_stride, dr_stride, dg_stride;
+    float *partial;
+    WsHeader *header;
+};
+bool glr_fits(int B, int C);  // whether the launches' grids have room
+cudaError_t glr_forward_launch(const Glr &p, cudaStream_t stream);
+cudaError_t glr_step_launch(const Glr &p, cudaStream_t stream);
+size_t glr_backward_partial_floats(int B, int n, int C);
+cudaError_t glr_backward_launch(const GlrBwd &p, cudaStream_t stream);
+
+// norms around a block with gate, residual scale and dropout (hla_block_norm.cu)
+struct BlockNorm {
+    const void *x, *y, *gate, *w_post, *scale, *w_pre;  // gate and weights: or null
+    void *x_out, *h;
+    hla_dtype dt;
+    long long rows;
+    int C, post, pre, act;
+    long long x_stride, y_stride, gate_stride, x_out_stride, h_stride;
+    float alpha, eps;
+    int drop;             // dropout: values whose 32 bits are below drop_below go, the others are multiplied by keep_scale
+    uint32_t drop_below;
+    float keep_scale;     // (1 without dropout)
+    uint64_t seed, offset;
+};
+struct BlockNormBwd {
+    BlockNorm f;  // x_out and h unused
+    const void *dx_out, *dh;
+    void *dx, *dy, *dgate;
+    float *dw_post, *dscale, *dw_pre;
+    long long dx_out_stride, dh_stride, dx_stride, dy_stride, dgate_stride;
+    float *partial;
+    WsHeader *header;
+};
+cudaError_t block_norm_forward_launch(const BlockNorm &p, cudaStream_t stream);
+size_t block_norm_partial_floats(long long rows, int C);
+cudaError_t block_norm_backward_launch(const BlockNormBwd &p, cudaStream_t stream);
+
+// sums over `rows` partial rows of `parts` runs of C floats, in a fixed order, into out[part] (or nowhere); clears
+// the workspace's header
+struct ColumnSum {
+    const float *partial;
+    long long rows;
+    int C, parts;
+    float *out[3];
+    WsHeader *header;
+};
+cudaError_t column_sum_launch(const ColumnSum &p, cudaStream_t stream);
+
+// gated feed-forward projections (hla_ffn.cu)
+struct Ffn {
+    const void *x, *w;
+    void *out;
+    hla_dtype dt;
+    int M, K, F, act;
+    long long x_stride, out_stride;
+    char *ws;  // workspace base (header included)
+};
+struct FfnBwd {
+    Ffn f;  // out unused
+    const void *dout;
+    void *dx, *dw;
+    long long dout_stride, dx_stride;
+};
+size_t ffn_forward_scratch_bytes(int M, int K, int F, hla_dtype dt);
+size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt);
+cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t stream);
+cudaError_t ffn_backward_launch(const FfnBwd &p, cudaStream_t stream);
 
 }  // namespace hla

@@ -2,55 +2,12 @@
 // argument checks, workspace sizing, dispatch.  See include/hla.h for the contracts.
 #include <cmath>
 
-#include "hla_internal.h"
+#include "hla_checks.h"
 
 namespace hla {
 namespace {
 
-bool aligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-size_t elem_bytes(hla_dtype dt) { return dt == HLA_BF16 ? 2 : 4; }
 bool size_ok(int v) { return v == 16 || v == 32 || v == 64 || v == 128; }
-
-constexpr long long kMaxRows = (1LL << 31) - 1;
-constexpr long long kMaxValues = 1LL << 40;
-constexpr int kMaxChannels = (int)kMaxRows - 256;  // a block has up to 256: its last one is within 32 bits
-
-#define HLA_TRY(expr)                       \
-    do {                                    \
-        const hla_status st_ = (expr);      \
-        if (st_ != HLA_OK) return st_;      \
-    } while (0)
-
-hla_status check_type(hla_dtype dt) {
-    return dt == HLA_F32 || dt == HLA_BF16 ? HLA_OK : fail(HLA_ERR_INVALID_ARGUMENT, "unknown dtype %d", (int)dt);
-}
-
-hla_status check_flag(int v, const char *name) {
-    return v == 0 || v == 1 ? HLA_OK : fail(HLA_ERR_INVALID_ARGUMENT, "%s must be 0 or 1, got %d", name, v);
-}
-
-hla_status check_rows(int B, int n) {
-    if (B < 0 || n < 0) return fail(HLA_ERR_INVALID_ARGUMENT, "negative size B=%d n=%d", B, n);
-    return n <= (1 << 30) && (long long)B * n <= kMaxRows ? HLA_OK : fail(HLA_ERR_UNSUPPORTED, "problem too large");
-}
-
-// a strided token tensor: pointer (where there are rows), element alignment, row stride
-hla_status check_tensor(const void *p, long long stride, long long width, hla_dtype dt, long long rows, const char *name) {
-    if (rows > 0 && !p) return fail(HLA_ERR_INVALID_ARGUMENT, "null %s pointer", name);
-    if (!aligned(p, elem_bytes(dt))) return fail(HLA_ERR_INVALID_ARGUMENT, "%s is not aligned to its elements", name);
-    if (stride < width)
-        return fail(HLA_ERR_INVALID_ARGUMENT, "%s: row stride %lld is below the row's %lld elements", name, stride, width);
-    if (stride > kMaxValues || (rows > 0 && stride > kMaxValues / rows))
-        return fail(HLA_ERR_UNSUPPORTED, "problem too large");
-    return HLA_OK;
-}
-
-hla_status check_workspace(const void *ws, size_t bytes, size_t need) {
-    if (!ws || bytes < need)
-        return fail(HLA_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, ws ? bytes : (size_t)0);
-    if (!aligned(ws, 256)) return fail(HLA_ERR_INVALID_ARGUMENT, "workspace must be 256-byte aligned");
-    return HLA_OK;
-}
 
 hla_status check_conv(const void *x, const void *w, const void *bias, hla_dtype dt, int B, int n, int C, int width,
                       long long x_stride, int silu, const int *lengths) {
@@ -121,15 +78,6 @@ hla_status check_qk(const QkNorm &p) {
                         (long long)p.pos0 + p.n - 1, p.table_rows);
     }
     return HLA_OK;
-}
-
-// one multiple of 16 bytes after the workspace header
-size_t scratch_bytes(size_t floats) { return align_up(kWsHeaderBytes + floats * sizeof(float), 256); }
-
-cudaStream_t as_stream(hla_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
-
-hla_status clear_header(void *ws, cudaStream_t s) {
-    return cuda_status(cudaMemsetAsync(ws, 0, kWsHeaderBytes, s), "clearing the workspace header");
 }
 
 }  // namespace

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libhla.so")
 
 HLA_OK, HLA_ERR_INVALID_ARGUMENT, HLA_ERR_UNSUPPORTED, HLA_ERR_CUDA, HLA_ERR_TIMEOUT, HLA_ERR_WORKSPACE = range(6)
 HLA_F32, HLA_BF16 = 0, 1
+HLA_LINEAR, HLA_SIGMOID, HLA_SILU = range(3)
 
 # every symbol include/hla.h declares
 EXPORTS = ("hla_status_string", "hla_last_error", "hla2_state_floats", "hla2_workspace_bytes", "hla2_forward",
@@ -28,7 +29,10 @@ EXPORTS = ("hla_status_string", "hla_last_error", "hla2_state_floats", "hla2_wor
            "ahla_step", "hla2_backward_workspace_bytes", "hla2_backward", "ahla_forward_path",
            "hla_conv_forward", "hla_conv_step", "hla_conv_backward_workspace_bytes", "hla_conv_backward",
            "hla_ssm_workspace_bytes", "hla_ssm_forward", "hla_ssm_forward_path", "hla_ssm_step", "hla_qk_norm_forward",
-           "hla_qk_norm_backward_workspace_bytes", "hla_qk_norm_backward")
+           "hla_qk_norm_backward_workspace_bytes", "hla_qk_norm_backward",
+           "hla_glr_marks", "hla_glr_forward", "hla_glr_step", "hla_glr_backward_workspace_bytes", "hla_glr_backward",
+           "hla_block_norm_forward", "hla_block_norm_backward_workspace_bytes", "hla_block_norm_backward",
+           "hla_ffn_workspace_bytes", "hla_ffn_backward_workspace_bytes", "hla_ffn_forward", "hla_ffn_backward")
 
 _lib = None
 
@@ -105,11 +109,27 @@ def lib():
         L.hla_qk_norm_backward.argtypes = [vp] * 13 + [i] * 8 + [ll] * 4 + [i, i, f, vp, sz, vp]
         L.hla_ssm_forward_path.argtypes = [i] * 8 + [ctypes.POINTER(i)]
         L.hla_ssm_forward_path.restype = i
+        f64, u64 = ctypes.c_double, ctypes.c_ulonglong
+        L.hla_glr_marks.argtypes = [i]
+        L.hla_glr_forward.argtypes = [vp] * 5 + [i] * 4 + [ll] * 4 + [vp] * 5
+        L.hla_glr_step.argtypes = [vp] * 5 + [i] * 3 + [ll] * 4 + [vp] * 2
+        L.hla_glr_backward_workspace_bytes.argtypes = [i] * 4
+        L.hla_glr_backward.argtypes = [vp] * 10 + [i] * 4 + [ll] * 7 + [vp] * 4 + [sz, vp]
+        L.hla_block_norm_forward.argtypes = [vp] * 8 + [i] * 3 + [ll] * 5 + [i] * 3 + [f, f, f64, u64, u64, vp]
+        L.hla_block_norm_backward_workspace_bytes.argtypes = [i] * 3
+        L.hla_block_norm_backward.argtypes = ([vp] * 14 + [i] * 3 + [ll] * 8 + [i] * 3 + [f, f, f64, u64, u64, vp, sz, vp])
+        L.hla_ffn_workspace_bytes.argtypes = L.hla_ffn_backward_workspace_bytes.argtypes = [i] * 4
+        L.hla_ffn_forward.argtypes = [vp] * 3 + [i] * 4 + [ll, ll, i, vp, sz, vp]
+        L.hla_ffn_backward.argtypes = [vp] * 5 + [i] * 4 + [ll] * 3 + [i, vp, sz, vp]
         for name in ("hla_conv_backward_workspace_bytes", "hla_ssm_workspace_bytes",
-                     "hla_qk_norm_backward_workspace_bytes"):
+                     "hla_qk_norm_backward_workspace_bytes", "hla_glr_backward_workspace_bytes",
+                     "hla_block_norm_backward_workspace_bytes", "hla_ffn_workspace_bytes",
+                     "hla_ffn_backward_workspace_bytes"):
             getattr(L, name).restype = sz
         for name in ("hla_conv_forward", "hla_conv_step", "hla_conv_backward", "hla_ssm_forward", "hla_ssm_step",
-                     "hla_qk_norm_forward", "hla_qk_norm_backward"):
+                     "hla_qk_norm_forward", "hla_qk_norm_backward", "hla_glr_marks", "hla_glr_forward", "hla_glr_step",
+                     "hla_glr_backward", "hla_block_norm_forward", "hla_block_norm_backward", "hla_ffn_forward",
+                     "hla_ffn_backward"):
             getattr(L, name).restype = i
         _lib = L
     return _lib
@@ -757,3 +777,203 @@ def hla_qk_norm_backward(q, k, wq, wk, cos, sin, dq_out, dk_out, dq=None, dk=Non
         _rows("dq", dq, shape, inner, T, i), _rows("dk", dk, k_shape, inner, T, i), pos0, top, eps, ws, ws_bytes,
         handle), "hla_qk_norm_backward")
     return dq, dk, dwq, dwk
+
+
+def hla_glr_marks(n) -> int:
+    return int(lib().hla_glr_marks(n))
+
+
+def _glr_sizes(x, dims):
+    if x.dim() != dims:
+        raise ValueError("x must be %s, got %s" % ("[B, n, C]" if dims == 3 else "[B, C]", tuple(x.shape)))
+    return x.shape, x.dtype, _type_code(x.dtype), _gpu(x)
+
+
+def hla_glr_forward(x, r, g, decay, out=None, *, lengths=None, state_in=None, state_out=None, marks=None, stream=None):
+    """Gated linear recurrence over a prompt (include/hla.h: hla_glr_forward).  Returns ``out``.
+
+    x, r, g: [B, n, C], rows may be slices of wider rows; decay: fp32 [C], below 0; lengths: int32 [B]; states: fp32
+    [B, C] (state_out may be state_in); marks: fp32 [B, hla_glr_marks(n), C], written for hla_glr_backward.
+    """
+    shape, T, dt, i = _glr_sizes(x, 3)
+    handle, side = _on(stream, i)
+    B, n, C = shape
+    if out is None:
+        out = _empty(shape, T, x.device, side)
+    f32, kept = torch.float32, (B, C)
+    _check(_entry("hla_glr_forward", i)(
+        x.data_ptr(), r.data_ptr(), g.data_ptr(), _flat("decay", decay, C, f32, i), out.data_ptr(), dt, B, n, C,
+        _rows("x", x, shape, (1,), T, i, True), _rows("r", r, shape, (1,), T, i), _rows("g", g, shape, (1,), T, i),
+        _rows("out", out, shape, (1,), T, i), _flat("lengths", lengths, B, torch.int32, i),
+        _shaped("state_in", state_in, kept, f32, i), _shaped("state_out", state_out, kept, f32, i),
+        None if marks is None else _shaped("marks", marks, (B, hla_glr_marks(n), C), f32, i), handle), "hla_glr_forward")
+    return out
+
+
+def hla_glr_step(x, r, g, decay, state, out=None, *, stream=None):
+    """One token a sequence of hla_glr_forward (include/hla.h: hla_glr_step); ``state`` fp32 [B, C] is updated in
+    place.  x, r, g: [B, C]; ``out`` may be ``x``, ``r`` or ``g``."""
+    shape, T, dt, i = _glr_sizes(x, 2)
+    handle, side = _on(stream, i)
+    B, C = shape
+    if out is None:
+        out = _empty(shape, T, x.device, side)
+    _check(_entry("hla_glr_step", i)(
+        x.data_ptr(), r.data_ptr(), g.data_ptr(), _flat("decay", decay, C, torch.float32, i), out.data_ptr(), dt, B, C,
+        _rows("x", x, shape, (1,), T, i, True), _rows("r", r, shape, (1,), T, i), _rows("g", g, shape, (1,), T, i),
+        _rows("out", out, shape, (1,), T, i), _shaped("state", state, shape, torch.float32, i), handle), "hla_glr_step")
+    return out
+
+
+def hla_glr_backward_workspace_bytes(B, n, C, dtype) -> int:
+    return int(lib().hla_glr_backward_workspace_bytes(B, n, C, _type_code(dtype)))
+
+
+def hla_glr_backward(x, r, g, decay, dout, marks, dx=None, dr=None, dg=None, *, dstate_out=None, dstate_in=None,
+                     lengths=None, workspace=None, stream=None):
+    """Gradients (dx, dr, dg, ddecay) of sum(dout * out) + sum(dstate_out * state_out) for hla_glr_forward
+    (include/hla.h: hla_glr_backward); ddecay is fp32 [C], and ``dstate_in`` (fp32 [B, C], may be dstate_out) receives
+    the state's.  marks: those of the forward with the same inputs."""
+    shape, T, dt, i = _glr_sizes(x, 3)
+    handle, side = _on(stream, i)
+    B, n, C = shape
+    dx, dr, dg = (_empty(shape, T, x.device, side) if t is None else t for t in (dx, dr, dg))
+    f32, kept = torch.float32, (B, C)
+    ddecay = _empty((C,), f32, x.device, side)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_glr_backward_workspace_bytes, i, side, B, n, C, dt)
+    _check(_entry("hla_glr_backward", i)(
+        x.data_ptr(), r.data_ptr(), g.data_ptr(), _flat("decay", decay, C, f32, i), dout.data_ptr(),
+        _shaped("marks", marks, (B, hla_glr_marks(n), C), f32, i), dx.data_ptr(), dr.data_ptr(), dg.data_ptr(),
+        ddecay.data_ptr(), dt, B, n, C, _rows("x", x, shape, (1,), T, i, True), _rows("r", r, shape, (1,), T, i),
+        _rows("g", g, shape, (1,), T, i), _rows("dout", dout, shape, (1,), T, i), _rows("dx", dx, shape, (1,), T, i),
+        _rows("dr", dr, shape, (1,), T, i), _rows("dg", dg, shape, (1,), T, i),
+        _flat("lengths", lengths, B, torch.int32, i), _shaped("dstate_out", dstate_out, kept, f32, i),
+        _shaped("dstate_in", dstate_in, kept, f32, i), ws, ws_bytes, handle), "hla_glr_backward")
+    return dx, dr, dg, ddecay
+
+
+def _lead(x, name):
+    """(shape, rows) of a token tensor [rows, C] or [B, n, C]."""
+    if x.dim() not in (2, 3):
+        raise ValueError("%s must be [rows, C] or [B, n, C], got %s" % (name, tuple(x.shape)))
+    shape = x.shape
+    return shape, shape[0] if len(shape) == 2 else shape[0] * shape[1]
+
+
+def _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm):
+    """What both directions of the block norm take of their inputs: strides, and addresses of weights."""
+    (shape, rows), T, i = _lead(x, "x"), x.dtype, _gpu(x)
+    C = shape[-1]
+    return shape, rows, C, T, _type_code(T), i, (
+        x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
+        _flat("w_post", w_post, C, T, i) if post_norm else None, _flat("scale", scale, C, T, i),
+        _flat("w_pre", w_pre, C, T, i) if pre_norm else None), (
+        _rows("x", x, shape, (1,), T, i, True), _rows("y", y, shape, (1,), T, i),
+        C if gate is None else _rows("gate", gate, shape, (1,), T, i))
+
+
+def hla_block_norm_forward(x, y, gate=None, x_out=None, h=None, *, w_post=None, scale=None, w_pre=None, post_norm=True,
+                           pre_norm=True, act=HLA_SILU, alpha=1.0, eps=1e-6, dropout=0.0, seed=0, offset=0, stream=None):
+    """Norm of a block's output with its gate, residual scale and dropout, the residual sum, and the norm before the
+    next block (include/hla.h: hla_block_norm_forward).  Returns (x_out, h); h is None without pre_norm.
+
+    x, y, gate: [rows, C] or [B, n, C], rows may be slices of wider rows; w_post, scale, w_pre: [C] or None (= 1);
+    x_out may be x; seed, offset: 64 bits, an offset for each use of a seed.
+    """
+    shape, rows, C, T, dt, i, given, strides = _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm)
+    handle, side = _on(stream, i)
+    if x_out is None:
+        x_out = _empty(shape, T, x.device, side)
+    if not pre_norm:
+        h = None
+    elif h is None:
+        h = _empty(shape, T, x.device, side)
+    _check(_entry("hla_block_norm_forward", i)(
+        *given, x_out.data_ptr(), None if h is None else h.data_ptr(), dt, rows, C, *strides,
+        _rows("x_out", x_out, shape, (1,), T, i), C if h is None else _rows("h", h, shape, (1,), T, i),
+        1 if post_norm else 0, 1 if pre_norm else 0, act, alpha, eps, dropout, seed, offset, handle),
+        "hla_block_norm_forward")
+    return x_out, h
+
+
+def hla_block_norm_backward_workspace_bytes(rows, C, dtype) -> int:
+    return int(lib().hla_block_norm_backward_workspace_bytes(rows, C, _type_code(dtype)))
+
+
+def hla_block_norm_backward(x, y, gate, dx_out, dh=None, dx=None, dy=None, dgate=None, *, w_post=None, scale=None,
+                            w_pre=None, post_norm=True, pre_norm=True, act=HLA_SILU, alpha=1.0, eps=1e-6, dropout=0.0,
+                            seed=0, offset=0, workspace=None, stream=None):
+    """Gradients (dx, dy, dgate, dw_post, dscale, dw_pre) of sum(dx_out * x_out) + sum(dh * h) for
+    hla_block_norm_forward with the same arguments (include/hla.h: hla_block_norm_backward); the weights' are fp32 [C],
+    None where the weight is not given; dgate is None without a gate.  dx may be dx_out."""
+    shape, rows, C, T, dt, i, given, strides = _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm)
+    handle, side = _on(stream, i)
+    dx = _empty(shape, T, x.device, side) if dx is None else dx
+    dy = _empty(shape, T, x.device, side) if dy is None else dy
+    if gate is None:
+        dgate = None
+    elif dgate is None:
+        dgate = _empty(shape, T, x.device, side)
+    if pre_norm and dh is None:
+        raise ValueError("dh is needed with pre_norm")
+    if not pre_norm:
+        dh = None
+    sums = [None if w is None else _empty((C,), torch.float32, x.device, side) for w in given[3:]]
+    ws, ws_bytes, _keep = _scratch(workspace, hla_block_norm_backward_workspace_bytes, i, side, rows, C, dt)
+    address = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    stride = lambda name, t: C if t is None else _rows(name, t, shape, (1,), T, i)  # noqa: E731
+    _check(_entry("hla_block_norm_backward", i)(
+        *given, dx_out.data_ptr(), address(dh), dx.data_ptr(), dy.data_ptr(), address(dgate), address(sums[0]),
+        address(sums[1]), address(sums[2]), dt, rows, C, *strides, stride("dx_out", dx_out), stride("dh", dh),
+        stride("dx", dx), stride("dy", dy), stride("dgate", dgate), 1 if post_norm else 0, 1 if pre_norm else 0, act, alpha,
+        eps, dropout, seed, offset, ws, ws_bytes, handle), "hla_block_norm_backward")
+    return (dx, dy, dgate) + tuple(sums)
+
+
+def hla_ffn_workspace_bytes(rows, K, F, dtype) -> int:
+    return int(lib().hla_ffn_workspace_bytes(rows, K, F, _type_code(dtype)))
+
+
+def hla_ffn_backward_workspace_bytes(rows, K, F, dtype) -> int:
+    return int(lib().hla_ffn_backward_workspace_bytes(rows, K, F, _type_code(dtype)))
+
+
+def _ffn_sizes(x, w):
+    (shape, rows), T, i = _lead(x, "x"), x.dtype, _gpu(x)
+    if w.dim() != 3 or w.shape[0] != 2 or w.shape[2] != shape[-1]:
+        raise ValueError("w must be [2, F, K] with the K of x %s, got %s" % (tuple(shape), tuple(w.shape)))
+    return shape, rows, shape[-1], w.shape[1], T, _type_code(T), i
+
+
+def hla_ffn_forward(x, w, out=None, *, act=HLA_SILU, workspace=None, stream=None):
+    """Gated feed-forward projections, act(x w[0]^T) * (x w[1]^T) (include/hla.h: hla_ffn_forward).  Returns ``out``.
+
+    x: [rows, K] or [B, n, K], rows may be slices of wider rows; w: [2, F, K], the gate's rows and then the others.
+    """
+    shape, rows, K, F, T, dt, i = _ffn_sizes(x, w)
+    handle, side = _on(stream, i)
+    wide = tuple(shape[:-1]) + (F,)
+    if out is None:
+        out = _empty(wide, T, x.device, side)
+    ws, ws_bytes, _keep = _scratch(workspace, hla_ffn_workspace_bytes, i, side, rows, K, F, dt)
+    _check(_entry("hla_ffn_forward", i)(
+        x.data_ptr(), _shaped("w", w, (2, F, K), T, i), out.data_ptr(), dt, rows, K, F,
+        _rows("x", x, shape, (1,), T, i, True), _rows("out", out, wide, (1,), T, i), act, ws, ws_bytes, handle),
+        "hla_ffn_forward")
+    return out
+
+
+def hla_ffn_backward(x, w, dout, dx=None, dw=None, *, act=HLA_SILU, workspace=None, stream=None):
+    """Gradients (dx, dw) of sum(dout * out) for hla_ffn_forward (include/hla.h: hla_ffn_backward), of the inputs' type."""
+    shape, rows, K, F, T, dt, i = _ffn_sizes(x, w)
+    handle, side = _on(stream, i)
+    wide = tuple(shape[:-1]) + (F,)
+    dx = _empty(shape, T, x.device, side) if dx is None else dx
+    dw = _empty((2, F, K), T, x.device, side) if dw is None else dw
+    ws, ws_bytes, _keep = _scratch(workspace, hla_ffn_backward_workspace_bytes, i, side, rows, K, F, dt)
+    _check(_entry("hla_ffn_backward", i)(
+        x.data_ptr(), _shaped("w", w, (2, F, K), T, i), dout.data_ptr(), dx.data_ptr(),
+        _shaped("dw", dw, (2, F, K), T, i), dt, rows, K, F, _rows("x", x, shape, (1,), T, i, True),
+        _rows("dout", dout, wide, (1,), T, i), _rows("dx", dx, shape, (1,), T, i), act, ws, ws_bytes, handle),
+        "hla_ffn_backward")
+    return dx, dw

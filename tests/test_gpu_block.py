@@ -1,0 +1,362 @@
+"""The block's operators (gated recurrence, norms around a block, gated feed-forward projections) on the GPU
+against their definitions in 64 bits, element by element within the bounds of block_ref.  A bf16 output
+adds its one rounding, 2^-9 of the next power of two: 2^-8 of the value."""
+import pytest
+import torch
+
+import block_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def hla():
+    from paper_2510_27258_gb300 import build
+    build.build()
+    from paper_2510_27258_gb300 import hla as binding
+    return binding
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def randn(g, *shape, T=torch.float32, scale=1.0):
+    return (torch.randn(*shape, generator=g) * scale).to(T)
+
+
+def near(name, got, want, bound):
+    """Every element within its bound and the rounding of its type."""
+    unit = 2.0 ** -8 if got.dtype == torch.bfloat16 else 2.0 ** -24
+    got = got.double().cpu()
+    assert got.shape == want.shape, name
+    assert torch.isfinite(got).all(), name
+    excess = (got - want).abs() - bound * (1 + unit) - unit * want.abs() - 1e-30
+    assert not excess.numel() or float(excess.max()) <= 0, (name, float(excess.max()), float((got - want).abs().max()))
+
+
+def sliced(t, extra=8, at=0, fill=float("nan")):
+    """`t` on the GPU as a slice of rows that are wider by `extra` elements, from element `at` on."""
+    wide = torch.full(t.shape[:-1] + (t.shape[-1] + extra,), fill, dtype=t.dtype, device=DEV)
+    wide[..., at:at + t.shape[-1]] = t.to(DEV)
+    return wide[..., at:at + t.shape[-1]]
+
+
+def ragged(g, B, n):
+    lens = [n, 0, 1] + [int(v) for v in torch.randint(0, n + 1, (max(B - 3, 0),), generator=g)]
+    return torch.tensor(lens[:B], dtype=torch.int32)
+
+
+def poison(t, lens):
+    """A copy with NaN and infinities at and after each length: nothing there may be read into a result."""
+    t = t.clone()
+    for i, m in enumerate(lens.tolist()):
+        t[i, m:] = float("nan")
+        t[i, m + 1:m + 2] = float("inf")
+    return t
+
+
+def on(t):
+    return None if t is None else t.to(DEV)
+
+
+# ---------------------------------------------------------------------------------- recurrence
+
+def glr_case(seed, B, n, C, T, ragged_lengths, slow=True):
+    g = gen(seed)
+    v = {k: randn(g, B, n, C, T=T, scale=1.5) for k in ("x", "r", "g")}
+    v["decay"] = 8 * torch.log(0.9 + 0.0999 * torch.rand(C, generator=g)) if slow else -20 * torch.rand(C, generator=g) - 1e-3
+    v["state"] = randn(g, B, C)
+    return g, v, ragged(g, B, n) if ragged_lengths else None
+
+
+GLR = [(1, 1, 8, False, 0, 0, True), (3, 2, 24, True, 8, 0, True), (4, 37, 264, True, 8, 8, True),
+       (2, 130, 203, False, 5, 3, False), (5, 64, 130, True, 0, 0, True), (1, 1000, 64, False, 8, 0, True),
+       (2, 600, 70, True, 1, 1, False), (1, 65, 1, False, 3, 2, True), (40, 33, 66, True, 0, 0, True),
+       (1, 2500, 100, False, 0, 0, True), (70, 5, 640, False, 0, 0, True)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,C,lens,extra,at,slow", GLR)
+def test_glr_forward(hla, dtype, B, n, C, lens, extra, at, slow):
+    T = TYPES[dtype]
+    _, v, lengths = glr_case(n + C, B, n, C, T, lens, slow)
+    want, last, bound, last_bound = R.glr(v["x"], v["r"], v["g"], v["decay"], v["state"], lengths)
+    x, r, g = ((v[k] if lengths is None else poison(v[k], lengths)) for k in ("x", "r", "g"))
+    st = on(v["state"])
+    out = hla.hla_glr_forward(sliced(x, extra, at), sliced(r, extra, at), sliced(g, extra, at), on(v["decay"]),
+                              lengths=on(lengths), state_in=st, state_out=st)  # the state in place
+    near("y", out, want, bound)
+    near("state", st, last, last_bound)
+    # from no state, into a strided output, with marks: the states before every 32nd token
+    want, last, bound, last_bound = R.glr(v["x"], v["r"], v["g"], v["decay"], None, lengths)
+    wide = torch.zeros(B, n, C + 7, dtype=T, device=DEV)
+    marks = torch.full((B, hla.hla_glr_marks(n), C), float("nan"), device=DEV)
+    so = torch.full_like(st, float("nan"))
+    hla.hla_glr_forward(on(x), on(r), on(g), on(v["decay"]), wide[..., 3:3 + C], lengths=on(lengths), state_out=so,
+                        marks=marks)
+    near("y", wide[..., 3:3 + C], want, bound)
+    near("state", so, last, last_bound)
+    assert not wide[..., :3].any() and not wide[..., 3 + C:].any()
+    for k in range(0, marks.shape[1], 3):
+        part = None if lengths is None else lengths.clamp(max=32 * k)
+        _, at_mark, _, mark_bound = R.glr(*(v[m][:, :32 * k] for m in ("x", "r", "g")), v["decay"], None, part)
+        near("marks", marks[:, k], at_mark, mark_bound)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,n,C,lens,extra,at,slow", GLR)
+def test_glr_backward(hla, dtype, B, n, C, lens, extra, at, slow):
+    T = TYPES[dtype]
+    gn, v, lengths = glr_case(n * C, B, n, C, T, lens, slow)
+    dy, dl = randn(gn, B, n, C, T=T), randn(gn, B, C)
+    want = R.glr_grad(v["x"], v["r"], v["g"], v["decay"], dy, v["state"], dl, lengths)
+    x, r, g, dy = ((t if lengths is None else poison(t, lengths)) for t in (v["x"], v["r"], v["g"], dy))
+    xs, rs, gs, ds = (sliced(t, extra, at) for t in (x, r, g, dy))
+    marks = torch.full((B, hla.hla_glr_marks(n), C), float("nan"), device=DEV)
+    hla.hla_glr_forward(xs, rs, gs, on(v["decay"]), lengths=on(lengths), state_in=on(v["state"]), marks=marks)
+    state = on(dl)
+
+    def run():
+        state.copy_(dl)
+        return hla.hla_glr_backward(xs, rs, gs, on(v["decay"]), ds, marks, dstate_out=state, dstate_in=state,
+                                    lengths=on(lengths))
+    got = run()
+    for name, t in zip(("dx", "dr", "dg", "ddecay"), got):
+        near(name, t, *want[name])
+    near("dstate", state, *want["dstate"])
+    again = run()
+    assert all(torch.equal(a, b) for a, b in zip(got, again))  # sums in a fixed order
+    # gradients side by side, no gradient of the state
+    want = R.glr_grad(v["x"], v["r"], v["g"], v["decay"], torch.where(R.live(lengths, B, n), dy, torch.zeros((), dtype=T)),
+                      v["state"], None, lengths)
+    rows = torch.zeros(B, n, 3 * C + 1, dtype=T, device=DEV)
+    got = hla.hla_glr_backward(on(x), on(r), on(g), on(v["decay"]), on(dy), marks, rows[..., :C], rows[..., C:2 * C],
+                               rows[..., 2 * C:3 * C], lengths=on(lengths))
+    for name, t in zip(("dx", "dr", "dg", "ddecay"), got):
+        near(name, t, *want[name])
+    assert not rows[..., 3 * C:].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,C,extra,at", [(1, 8, 8, 0), (7, 203, 3, 1), (64, 264, 8, 0), (33, 1, 0, 0)])
+def test_glr_step_continues_the_prompt(hla, dtype, B, C, extra, at):
+    """A prompt and then single tokens equal the whole sequence at once."""
+    T = TYPES[dtype]
+    _, v, _ = glr_case(B + C, B, 12, C, T, False)
+    want, last, bound, last_bound = R.glr(v["x"], v["r"], v["g"], v["decay"], v["state"])
+    st = on(v["state"])
+    hla.hla_glr_forward(*(v[k][:, :7].contiguous().to(DEV) for k in ("x", "r", "g")), on(v["decay"]), state_in=st, state_out=st)
+    for t in range(7, 12):
+        x, r, g = (sliced(v[k][:, t], extra, at) for k in ("x", "r", "g"))
+        out = hla.hla_glr_step(x, r, g, on(v["decay"]), st, (None, x, r, g, None)[t - 7])
+        near("y", out, want[:, t], bound[:, t])
+    near("state", st, last, last_bound)
+
+
+def test_glr_empty_prompt_keeps_the_state(hla):
+    st, decay, none = torch.randn(2, 16, device=DEV), -torch.ones(16, device=DEV), torch.empty(2, 0, 16, device=DEV)
+    keep = st.clone()
+    hla.hla_glr_forward(none, none, none, decay, state_in=st, state_out=st)
+    assert torch.equal(st, keep)
+    back = torch.empty_like(st)
+    grads = hla.hla_glr_backward(none, none, none, decay, none, torch.empty(2, 0, 16, device=DEV), dstate_out=st, dstate_in=back)
+    assert torch.equal(back, keep) and not grads[3].any()
+    hla.hla_glr_forward(none, none, none, decay, state_out=st)
+    assert not st.any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_glr_extreme_gates(hla, dtype):
+    """Gates that are shut or open as far as the type goes: no NaN, and what the limits say."""
+    T = TYPES[dtype]
+    for r, g, keeps, adds in ((-1e4, 0.0, True, False), (-200.0, 1e4, True, False), (0.0, -1e4, False, False),
+                              (1e4, 1e4, False, True), (-float("inf"), float("inf"), True, False)):
+        x = torch.full((1, 70, 64), 2.0, dtype=T, device=DEV)
+        st, decay = torch.ones(1, 64, device=DEV), torch.full((64,), -50.0, device=DEV)
+        y = hla.hla_glr_forward(x, torch.full_like(x, r), torch.full_like(x, g), decay, state_in=st)
+        want = 1.0 if keeps else 2.0 if adds else 0.0
+        # (shut at r = 0: the state decays by e^-25 a token, which is below 2^-24 after one)
+        assert torch.isfinite(y).all() and float((y[:, 1:] - want).abs().max()) <= 2.0 ** -23
+        marks = torch.empty(1, 3, 64, device=DEV)
+        hla.hla_glr_forward(x, torch.full_like(x, r), torch.full_like(x, g), decay, state_in=st, marks=marks)
+        grads = hla.hla_glr_backward(x, torch.full_like(x, r), torch.full_like(x, g), decay, x, marks)
+        assert all(torch.isfinite(t).all() for t in grads)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("which", ["x", "r", "g"])
+def test_glr_is_causal_for_tokens_that_are_not_finite(hla, which, bad):
+    _, v, _ = glr_case(9, 2, 300, 130, torch.float32, False)
+    clean = hla.hla_glr_forward(on(v["x"]), on(v["r"]), on(v["g"]), on(v["decay"]))
+    v[which][0, 150, 7] = bad
+    got = hla.hla_glr_forward(on(v["x"]), on(v["r"]), on(v["g"]), on(v["decay"]))
+    if bad != bad:
+        assert torch.isnan(got[0, 150:, 7]).all()
+    got[0, 150:, 7] = clean[0, 150:, 7]
+    assert torch.equal(got, clean)
+
+
+# ---------------------------------------------------------------------------------- norms
+
+NORM = [((1, 1), dict()), ((5, 8), dict(dropout=0.5)), ((37, 203), dict(dropout=0.1, gate=False)),
+        ((300, 256), dict(dropout=0.25, act=R.SIGMOID)), ((64, 260), dict(dropout=0.1)),
+        ((700, 2048), dict(dropout=0.1, alpha=0.75)), ((9, 2100), dict(act=R.LINEAR, post=False)),
+        ((11, 4104), dict(pre=False, dropout=0.1)), ((3, 8192), dict(dropout=0.1)), ((2, 1023), dict(weights=False)),
+        ((2, 8201), dict(dropout=0.1)), ((3, 20000), dict(post=False)), ((2, 8200), dict(pre=False, gate=False)),
+        ((400, 24), dict(post=False, pre=False))]
+
+
+def norm_case(seed, rows, C, T, gate=True, weights=True, **kw):
+    g = gen(seed)
+    v = {"x": randn(g, rows, C, T=T), "y": randn(g, rows, C, T=T, scale=0.5), "gate": randn(g, rows, C, T=T) if gate else None}
+    for k in ("w_post", "scale", "w_pre"):
+        v[k] = randn(g, C, T=T) if weights else None
+    kw = {"alpha": 1.0, "eps": 1e-6, "dropout": 0.0, "act": R.SILU, "post": True, "pre": True, **kw}
+    kw["seed"], kw["offset"] = 2 ** 63 + 12345 * seed, 2 ** 40 + seed
+    own = {("post_norm" if k == "post" else "pre_norm" if k == "pre" else k): x for k, x in kw.items()}
+    return g, v, kw, own
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size,opts", NORM)
+@pytest.mark.parametrize("extra,at", [(8, 0), (3, 1)])
+def test_block_norm(hla, dtype, size, opts, extra, at):
+    T = TYPES[dtype]
+    rows, C = size
+    g, v, kw, own = norm_case(rows + C, rows, C, T, **opts)
+    dx_out, dh = randn(g, rows, C, T=T), randn(g, rows, C, T=T) if kw["pre"] else None
+    want = R.norm(**v, dx_out=dx_out, dh=dh, **kw)
+    w = {k: on(v[k]) for k in ("w_post", "scale", "w_pre")}
+    cut = lambda t: None if t is None else sliced(t, extra, at)  # noqa: E731
+    x, y, gate = cut(v["x"]), cut(v["y"]), cut(v["gate"])
+    h = sliced(torch.zeros(rows, C, dtype=T), extra, at, 7.0)
+    x_out, h = hla.hla_block_norm_forward(x, y, gate, None, h, **w, **own)
+    near("x_out", x_out, *want["x_out"])
+    assert (h is None) == (not kw["pre"])
+    if h is not None:
+        near("h", h, *want["h"])
+        base = h._base
+        assert (base[:, :at] == 7).all() and (base[:, at + C:] == 7).all()
+    same = x.clone()
+    again, _ = hla.hla_block_norm_forward(same, y, gate, same, **w, **own)  # in place
+    assert again is same and torch.equal(same, x_out)
+
+    def run():
+        return hla.hla_block_norm_backward(x, y, gate, cut(dx_out), cut(dh), **w, **own)
+    got = run()
+    for name, t in zip(("dx", "dy", "dgate", "dw_post", "dscale", "dw_pre"), got):
+        if name == "dgate" and v["gate"] is None or name.startswith("d") and name[1:] in v and v[name[1:]] is None:
+            assert t is None
+        elif name[1:] in ("w_post", "w_pre") and not kw[name[3:]]:
+            assert t is None
+        else:
+            near(name, t, *want[name])
+    assert all(a is b is None or torch.equal(a, b) for a, b in zip(got, run()))
+    d = on(dx_out)
+    got2 = hla.hla_block_norm_backward(x, y, gate, d, cut(dh), d, **w, **own)  # dx over dx_out
+    assert got2[0] is d and torch.equal(d, got[0]) and torch.equal(got2[1], got[1])
+
+
+def test_block_norm_batches_and_masks(hla):
+    """[B, n, C] is the same rows, and a value's bits depend on row, column, seed and offset alone."""
+    _, v, _, own = norm_case(5, 24, 256, torch.float32, dropout=0.5)
+    args = [on(v[k]) for k in ("x", "y", "gate")]
+    a = hla.hla_block_norm_forward(*args, **own)
+    b = hla.hla_block_norm_forward(*(t.view(4, 6, 256) for t in args), **own)
+    assert all(torch.equal(s, t.view(24, 256)) for s, t in zip(a, b))
+    kept = (a[0] != args[0])
+    other = hla.hla_block_norm_forward(*args, **{**own, "offset": own["offset"] + 1})[0] != args[0]
+    # two masks of one half each: they agree on 0.5 +- 4.5 deviations of sqrt(1 / 4 / 6144) = 0.0064
+    assert abs(float(kept.float().mean()) - 0.5) < 0.03 and abs(float((kept == other).float().mean()) - 0.5) < 0.03
+    strided = hla.hla_block_norm_forward(*(sliced(v[k], 1, 1) for k in ("x", "y", "gate")), **own)[0]
+    assert torch.equal(strided != args[0], kept)
+
+
+def test_block_norm_rows_of_zeros(hla):
+    """eps keeps a row of zeros finite, forwards and backwards."""
+    z = torch.zeros(3, 512, device=DEV)
+    x, h = hla.hla_block_norm_forward(z, z, z)
+    assert not x.any() and not h.any()
+    grads = hla.hla_block_norm_backward(z, z, z, z + 1, z + 1)
+    assert all(t is None or torch.isfinite(t).all() for t in grads)
+    none = torch.empty(0, 512, device=DEV)
+    grads = hla.hla_block_norm_backward(none, none, None, none, none, w_post=z[0], scale=z[0], w_pre=z[0])
+    assert grads[0].shape == (0, 512) and not any(t.any() for t in grads[3:])
+
+
+# ---------------------------------------------------------------------------------- feed-forward
+
+FFN = [(1, 8, 8, R.SILU), (3, 1, 1, R.SILU), (16, 264, 520, R.SIGMOID), (129, 130, 67, R.SILU), (333, 260, 103, R.LINEAR),
+       (300, 512, 1032, R.SILU), (1, 2056, 384, R.SILU), (64, 33, 2050, R.SIGMOID), (520, 64, 328, R.SILU),
+       (17, 1000, 77, R.SILU)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,F,act", FFN)
+@pytest.mark.parametrize("extra,at", [(8, 0), (3, 1)])
+def test_ffn(hla, dtype, M, K, F, act, extra, at):
+    T = TYPES[dtype]
+    g = gen(M + K + F)
+    x, w, dout = randn(g, M, K, T=T), randn(g, 2, F, K, T=T, scale=K ** -0.5), randn(g, M, F, T=T)
+    # bf16 keeps the projections' gradients as bf16 between the products: half a step, 2^-8
+    want = R.ffn(x, w, dout, act, 2.0 ** -8 if dtype == "bf16" else 0.0)
+    cut = lambda t, fill=float("nan"): sliced(t, extra, at, fill)  # noqa: E731
+    out = cut(torch.zeros_like(dout), 7.0)
+    hla.hla_ffn_forward(cut(x), on(w), out, act=act)
+    near("out", out, *want["out"])
+    assert (out._base[:, :at] == 7).all() and (out._base[:, at + F:] == 7).all()
+    dx = cut(torch.zeros_like(x), 7.0)
+
+    def run():
+        return hla.hla_ffn_backward(cut(x), on(w), cut(dout), dx, act=act)
+    got = [t.clone() for t in run()]
+    near("dx", got[0], *want["dx"])
+    near("dw", got[1], *want["dw"])
+    assert (dx._base[:, :at] == 7).all() and (dx._base[:, at + K:] == 7).all()
+    assert all(torch.equal(a, b) for a, b in zip(got, run()))
+
+
+def test_ffn_batches_and_none(hla):
+    x, w = torch.randn(2, 5, 64, device=DEV), torch.randn(2, 96, 64, device=DEV)
+    out = hla.hla_ffn_forward(x, w)
+    assert out.shape == (2, 5, 96) and torch.equal(out.view(10, 96), hla.hla_ffn_forward(x.view(10, 64), w))
+    none = torch.empty(0, 64, device=DEV)
+    assert hla.hla_ffn_forward(none, w).shape == (0, 96)
+    dx, dw = hla.hla_ffn_backward(none, w, torch.empty(0, 96, device=DEV))
+    assert dx.shape == (0, 64) and not dw.any()
+
+
+# ---------------------------------------------------------------------------------- as they are used
+
+def chain(hla, v, ws):
+    """A block: norm, recurrence, norm with gate and residual, feed-forward."""
+    y = hla.hla_glr_forward(v["x"], v["r"], v["g"], v["decay"])
+    x1, h = hla.hla_block_norm_forward(v["x"], y, v["r"], scale=v["scale"], dropout=0.1, seed=3)
+    f = hla.hla_ffn_forward(h, v["w"], workspace=ws)
+    return hla.hla_block_norm_forward(x1, f, None, pre_norm=False)[0]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_chain_on_other_streams_and_in_graphs(hla, dtype):
+    T = TYPES[dtype]
+    g = gen(1)
+    C = 256
+    v = {k: randn(g, 2, 150, C, T=T).to(DEV) for k in ("x", "r", "g")}
+    v["decay"], v["scale"] = -torch.rand(C, generator=g).to(DEV) - 0.01, randn(g, C, T=T).to(DEV)
+    v["w"] = randn(g, 2, C, C, T=T, scale=C ** -0.5).to(DEV)
+    ws = hla.alloc_workspace(hla.hla_ffn_workspace_bytes(300, C, C, T), DEV)
+    want = chain(hla, v, ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [chain(hla, v, ws) for _ in range(3)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            captured = chain(hla, v, ws)
+        captured.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, want) for t in got) and torch.equal(captured, want)
