@@ -1,4 +1,4 @@
-// Gated feed-forward projections and their gradients on the CUDA cores, in fp32.
+// Gated feed-forward projections and their gradients in fp32, on the CUDA cores (bf16: hla_ffn_sm103.cu).
 //
 //   Z = x [Wg; Wu]^T (two products of one tile),  out = act(Zg) Zu
 //   dZg = dout Zu act'(Zg),  dZu = dout act(Zg),  dx = [dZg dZu] [Wg; Wu],  d[Wg; Wu] = [dZg dZu]^T x
@@ -8,6 +8,7 @@
 // sums and adds two neighbours an instruction.  The forward's tile is half gate and half up columns of the same
 // features, so that the activation and product happen in registers.  The gradient keeps [dZg dZu] in the workspace; its dx,
 // whose sum is over 2 F and whose tiles may be few, is cut along the sum, and the parts are added in their order.
+#include "hla_ffn.h"
 #include "hla_vec.cuh"
 
 namespace hla {
@@ -19,7 +20,7 @@ enum Mode { kProduct, kParts, kOut, kGrad };
 
 // a matrix by its rows' and columns' strides; a column is an index of the sum
 struct Mat {
-    const void *p;
+    const float *p;
     long long row, col;
 };
 
@@ -28,10 +29,11 @@ struct Product {
     int M, N, K, act;  // outputs M x N (kOut, kGrad: N features, whose up rows of b are N rows behind)
     int per;           // indices of the sum for each blockIdx.y
     int across;        // tiles along N (blockIdx.x counts all tiles)
-    void *out;         // kParts: fp32 [z][M][N]
+    float *out;        // kParts: [y][M][N]
     long long out_row;
-    const void *dout;  // kGrad: out is fp32 [M][2 N]
+    const float *dout;  // kGrad: out is fp32 [M][2 N]
     long long dout_row;
+    WsHeader *header;  // cleared (kOut, kGrad: the call's first product)
 };
 
 __device__ __forceinline__ float act_of(int act, float v, float &slope) {
@@ -45,7 +47,7 @@ __device__ __forceinline__ float act_of(int act, float v, float &slope) {
 }
 
 // A panel's elements of one thread: kRows x kDepth over 256 threads, neighbours along the contiguous direction
-template <typename T, int kRows, bool kAlong>
+template <int kRows, bool kAlong>
 struct Panel {
     static constexpr int kEach = kRows * kDepth / kThreads;
     float v[kEach];
@@ -64,7 +66,7 @@ struct Panel {
             const bool second = pair > 0 && r >= kRows / 2;
             if (second) r -= kRows / 2;
             const long long from = (long long)(at + r) + (second ? pair : 0);
-            v[i] = at + r < rows && k < k1 ? to_f32(static_cast<const T *>(m.p)[from * m.row + k * m.col]) : 0.f;
+            v[i] = at + r < rows && k < k1 ? m.p[from * m.row + k * m.col] : 0.f;
         }
     }
     __device__ __forceinline__ void store(float (&to)[kDepth][kRows + 4]) const {
@@ -74,7 +76,7 @@ struct Panel {
 };
 
 // kTile 128 or 64; kA, kB: whether the sum's index is the contiguous one
-template <typename TA, typename TB, typename TO, int kTile, bool kA, bool kB, Mode kMode>
+template <int kTile, bool kA, bool kB, Mode kMode>
 __global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
     constexpr int kE = kTile / 16, kH = kE / 2;  // a thread's rows and columns, in two runs of kH
     constexpr bool kPair = kMode == kOut || kMode == kGrad;
@@ -82,11 +84,12 @@ __global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
     __shared__ __align__(16) float as[2][kDepth][kTile + 4], bs[2][kDepth][kTile + 4];
     let_next_begin();
     after_previous();
+    if (kPair && blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // no device-side waits here: never an error
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const int down = blockIdx.x / p.across, m0 = down * kTile, n0 = (blockIdx.x - down * p.across) * kCols;
     const int k_lo = blockIdx.y * p.per, k_hi = (int)min((long long)p.K, (long long)k_lo + p.per), pair_rows = kPair ? p.N : 0;
-    Panel<TA, kTile, kA> pa;
-    Panel<TB, kTile, kB> pb;
+    Panel<kTile, kA> pa;
+    Panel<kTile, kB> pb;
     uint64_t acc[kE][kH];
 #pragma unroll
     for (int i = 0; i < kE; ++i)
@@ -140,10 +143,10 @@ __global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
                 float slope;
                 const float a = act_of(p.act, v[j], slope), up = v[kH + j];
                 if (kMode == kOut) {
-                    from_f32(static_cast<TO *>(p.out) + m * p.out_row + n, a * up);
+                    p.out[m * p.out_row + n] = a * up;
                 } else {
-                    const float d = to_f32(static_cast<const TA *>(p.dout)[m * p.dout_row + n]);
-                    float *to = static_cast<float *>(p.out) + m * p.out_row + n;
+                    const float d = p.dout[m * p.dout_row + n];
+                    float *to = p.out + m * p.out_row + n;
                     to[0] = d * up * slope;
                     to[p.N] = d * a;
                 }
@@ -152,17 +155,14 @@ __global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
 #pragma unroll
             for (int j = 0; j < kE; ++j) {
                 const int n = n0 + (j / kH) * kTile / 2 + tx * kH + j % kH;
-                if (n < p.N)
-                    from_f32(static_cast<TO *>(p.out) + ((kMode == kParts ? (long long)blockIdx.y * p.M : 0) + m) * p.out_row + n,
-                             v[j]);
+                if (n < p.N) p.out[((kMode == kParts ? (long long)blockIdx.y * p.M : 0) + m) * p.out_row + n] = v[j];
             }
         }
     }
 }
 
 // out = the sum of `parts` runs of M x N
-template <typename T>
-__global__ void __launch_bounds__(kThreads) ffn_parts_kernel(const float *from, int parts, int M, int N, T *out,
+__global__ void __launch_bounds__(kThreads) ffn_parts_kernel(const float *from, int parts, int M, int N, float *out,
                                                             long long out_row) {
     let_next_begin();
     after_previous();
@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kThreads) ffn_parts_kernel(const float *from, 
         float sum = 0.f;
         for (int z = 0; z < parts; ++z) sum += from[z * all + i];
         const long long m = i / N;
-        from_f32(out + m * out_row + (i - m * N), sum);
+        out[m * out_row + (i - m * N)] = sum;
     }
 }
 
@@ -190,64 +190,65 @@ int parts_of(int M, int K, int F) {
     return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
 }
 
-template <typename TA, typename TB, typename TO, bool kA, bool kB, Mode kMode>
+template <bool kA, bool kB, Mode kMode>
 cudaError_t product(Product p, int parts, cudaStream_t s) {
     constexpr bool paired = kMode == kOut || kMode == kGrad;
     const int tile = small_tiles(p.M, p.N, paired) ? 64 : 128, cols = paired ? tile / 2 : tile;
     p.across = (p.N + cols - 1) / cols;
     const dim3 grid((unsigned)p.across * ((p.M + tile - 1) / tile), parts);
-    return tile == 64 ? launch_after(ffn_product_kernel<TA, TB, TO, 64, kA, kB, kMode>, grid, kThreads, 0, s, p)
-                      : launch_after(ffn_product_kernel<TA, TB, TO, 128, kA, kB, kMode>, grid, kThreads, 0, s, p);
+    return tile == 64 ? launch_after(ffn_product_kernel<64, kA, kB, kMode>, grid, kThreads, 0, s, p)
+                      : launch_after(ffn_product_kernel<128, kA, kB, kMode>, grid, kThreads, 0, s, p);
 }
 
-cudaError_t clear(char *ws, cudaStream_t s) { return cudaMemsetAsync(ws, 0, kWsHeaderBytes, s); }
+const float *floats(const void *p) { return static_cast<const float *>(p); }
 
-template <typename T>
-cudaError_t forward_of(const Ffn &p, cudaStream_t s) {
-    const cudaError_t e = clear(p.ws, s);
-    if (e) return e;
-    const Product q{{p.x, p.x_stride, 1}, {p.w, p.K, 1}, p.M, p.F, p.K, p.act, p.K, 0, p.out, p.out_stride, nullptr, 0};
-    return product<T, T, T, true, true, kOut>(q, 1, s);
+cudaError_t forward_f32(const Ffn &p, cudaStream_t s) {
+    const Product q{{floats(p.x), p.x_stride, 1}, {floats(p.w), p.K, 1}, p.M, p.F, p.K, p.act, p.K, 0,
+                    static_cast<float *>(p.out), p.out_stride, nullptr, 0, reinterpret_cast<WsHeader *>(p.ws)};
+    return product<true, true, kOut>(q, 1, s);
 }
 
-template <typename T>
-cudaError_t backward_of(const FfnBwd &p, cudaStream_t s) {
+cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     const Ffn &f = p.f;
-    cudaError_t e = clear(f.ws, s);
-    if (e) return e;
     float *dz = reinterpret_cast<float *>(f.ws + kWsHeaderBytes);
     const int F2 = 2 * f.F, parts = parts_of(f.M, f.K, f.F);
-    const Product q{{f.x, f.x_stride, 1}, {f.w, f.K, 1}, f.M, f.F, f.K, f.act, f.K, 0, dz, F2, p.dout, p.dout_stride};
-    e = product<T, T, float, true, true, kGrad>(q, 1, s);
+    const Product q{{floats(f.x), f.x_stride, 1}, {floats(f.w), f.K, 1}, f.M, f.F, f.K, f.act, f.K, 0, dz, F2,
+                    floats(p.dout), p.dout_stride, reinterpret_cast<WsHeader *>(f.ws)};
+    cudaError_t e = product<true, true, kGrad>(q, 1, s);
     if (e) return e;
-    const Product dw{{dz, 1, F2}, {f.x, 1, f.x_stride}, F2, f.K, f.M, 0, f.M, 0, p.dw, f.K, nullptr, 0};
-    e = product<float, T, T, false, false, kProduct>(dw, 1, s);
+    const Product dw{{dz, 1, F2}, {floats(f.x), 1, f.x_stride}, F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
+                     nullptr, 0, nullptr};
+    e = product<false, false, kProduct>(dw, 1, s);
     if (e) return e;
-    Product dx{{dz, F2, 1}, {f.w, 1, f.K}, f.M, f.K, F2, 0, F2, 0, p.dx, p.dx_stride, nullptr, 0};
-    if (parts == 1) return product<float, T, T, true, false, kProduct>(dx, 1, s);
+    Product dx{{dz, F2, 1}, {floats(f.w), 1, f.K}, f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
+               nullptr, 0, nullptr};
+    if (parts == 1) return product<true, false, kProduct>(dx, 1, s);
     dx.per = ((F2 + parts - 1) / parts + kDepth - 1) / kDepth * kDepth;
     float *sums = dz + (size_t)f.M * F2;
     dx.out = sums;
     dx.out_row = f.K;
-    e = product<float, T, float, true, false, kParts>(dx, parts, s);
+    e = product<true, false, kParts>(dx, parts, s);
     if (e) return e;
     const long long all = (long long)f.M * f.K, blocks = (all + kThreads - 1) / kThreads;
-    return launch_after(ffn_parts_kernel<T>, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts,
-                        f.M, f.K, static_cast<T *>(p.dx), p.dx_stride);
+    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts, f.M,
+                        f.K, static_cast<float *>(p.dx), p.dx_stride);
 }
 
 }  // namespace
 
-size_t ffn_forward_scratch_bytes(int, int, int, hla_dtype) { return 0; }
-size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype) {
+size_t ffn_forward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
+    return dt == HLA_BF16 ? ffn_tc_forward_scratch_bytes(M, K, F) : 0;
+}
+size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
+    if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
     const int parts = M ? parts_of(M, K, F) : 1;
     return sizeof(float) * ((size_t)M * 2 * F + (parts > 1 ? (size_t)parts * M * K : 0));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
-    return p.dt == HLA_BF16 ? forward_of<__nv_bfloat16>(p, s) : forward_of<float>(p, s);
+    return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);
 }
 cudaError_t ffn_backward_launch(const FfnBwd &p, cudaStream_t s) {
-    return p.f.dt == HLA_BF16 ? backward_of<__nv_bfloat16>(p, s) : backward_of<float>(p, s);
+    return p.f.dt == HLA_BF16 ? ffn_tc_backward(p, s) : backward_f32(p, s);
 }
 
 }  // namespace hla

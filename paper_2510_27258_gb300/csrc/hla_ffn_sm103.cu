@@ -1,0 +1,698 @@
+// Gated feed-forward projections and their gradients on the tensor cores (bf16).
+//
+//   kOut   out = act(x Wg^T) (x Wu^T)
+//   kGrad  dZ = [dout Zu act'(Zg) | dout act(Zg)], Z computed again, to the workspace in bf16
+//   kDx    dx = dZg Wg + dZu Wu: one sum over both
+//   kDw    d[Wg; Wu] = dZ^T x
+//
+// Each is a product D = A B^T over tiles of 256 x 256, made by a pair of blocks (tcgen05.mma of both their SMs, M = N =
+// 256): a block loads 128 rows of A and 128 of B in steps of 64, so an SM reads 32 KB of shared memory's fill for 8.4
+// MFLOP.  Where the sum's index is not the contiguous one (B of kDx, both of kDw) the operand is read as it lies
+// (MN-major), so nothing is transposed in memory.  The forward's tile has 128 gate columns (the first block's half of B)
+// and the same 128 up columns (the second's), so that activation and product happen where the tile is read out.
+//
+// A block has a loading warp, a warp that issues the products (first block) or tells the first block that this one's
+// half of a step has landed (second), and four warps that read finished tiles out of tensor memory, whose 512 columns
+// hold two of them, so that reading out is hidden behind the next tile.  Blocks stay for many tiles, which are taken
+// in groups of eight columns so that a round of all blocks reads few distinct rows.  Where tiles are few and the
+// sum long, the sum is cut and the parts are added in their order by another kernel.
+//
+// Every wait has a limit: it sets the workspace's error word and the block's `stop`, after which all roles leave,
+// copies and products in flight are waited for (with a limit), and tensor memory is released.
+#include "hla_ffn.h"
+#include "hla_vec.cuh"
+#include "sm103_prims.cuh"
+#include "tensor_map.h"
+
+namespace hla {
+namespace {
+
+using namespace sm103;
+
+constexpr int kTile = 256, kHalf = 128, kStep = 64;
+constexpr int kThreads = 192;
+constexpr uint32_t kHalfBytes = kHalf * kStep * 2, kStageBytes = 2 * kHalfBytes;
+constexpr int kStages = 6;
+constexpr uint32_t kPitch = 144;                         // a staged row of 128 bytes and what keeps banks apart
+constexpr uint32_t kStagingBytes = 32 * kPitch;          // of a warp that reads out
+constexpr uint32_t kSmemBytes = 1024 + kStages * kStageBytes + 4 * kStagingBytes + 256;
+constexpr uint64_t kWaitNs = 2000000000ull;
+
+enum Mode { kOut, kGrad, kDx, kDw };
+
+struct Work {
+    int down, across, parts;   // tiles along A's and B's rows, cuts of the sum
+    int steps, per_part;       // steps of the sum, and of a part
+    int plane_steps;           // kDx: steps of one plane; kDw: tiles of one plane
+    int rows, cols;            // of the output (kOut, kGrad: cols = F; kDw: rows = F, of each plane)
+    int act;
+    void *out;                 // kOut, kDx, kDw: bf16, or fp32 parts [part][rows][cols] (kDw: [part][2][rows][cols]); kGrad: dZ
+    long long out_row;         // elements
+    long long out_plane;       // kGrad, kDw: elements from one plane to the other
+    int out_wide;              // whether rows of out allow 16-byte accesses
+    const __nv_bfloat16 *dout;  // kGrad
+    long long dout_row;
+    int dout_wide;
+    WsHeader *header;
+    int clear;                 // the call's first product clears the header
+};
+
+struct Bars {
+    uint64_t full[kStages], empty[kStages];
+    uint64_t done[2], taken[2];  // a tile's sums are there, have been read
+    uint64_t drain;
+    uint32_t tmem;
+    int stop;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// one arrival at the first block's barrier
+__device__ __forceinline__ void arrive_first(uint64_t *bar) {
+    asm volatile(
+        "{\n\t.reg .b32 at;\n\t"
+        "mapa.shared::cluster.u32 at, %0, 0;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [at];\n\t}" ::"r"(smem_u32(bar))
+        : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// false: another role gave up, or this wait did
+__device__ bool wait(uint64_t *bar, uint32_t parity, Bars *bars, WsHeader *header, unsigned where) {
+    if (try_wait_cluster(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    while (true) {
+        if (try_wait_cluster(bar, parity)) return true;
+        if (*reinterpret_cast<volatile int *>(&bars->stop)) return false;
+        if (globaltimer_ns() - t0 > kWaitNs) {
+            header->where = where;
+            header->detail = blockIdx.x;
+            header->error = kDevTimeout;
+            *reinterpret_cast<volatile int *>(&bars->stop) = 1;
+            return false;
+        }
+    }
+}
+// what is in flight when a role gives up; not longer than the limit
+__device__ void drain(uint64_t *bar, uint32_t parity, uint64_t t0) {
+    while (!try_wait_cluster(bar, parity) && globaltimer_ns() - t0 <= kWaitNs) {
+    }
+}
+
+__device__ __forceinline__ void umma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// an arrival at the same barrier of both blocks when the products issued so far are done
+__device__ __forceinline__ void commit_pair(uint64_t *bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+}
+
+__device__ __forceinline__ float act_of(int act, float v, float &slope) {
+    if (act == HLA_LINEAR) {
+        slope = 1.f;
+        return v;
+    }
+    const float s = __fdividef(1.f, 1.f + __expf(-v));
+    slope = act == HLA_SIGMOID ? s * (1.f - s) : s * (1.f + v * (1.f - s));
+    return act == HLA_SIGMOID ? s : v * s;
+}
+
+struct Tile {
+    int m, n, part;
+};
+// groups of eight columns; down within a group, a row's columns next to each other
+__device__ __forceinline__ Tile tile_of(const Work &w, int i) {
+    const int each = w.down * w.across, part = i / each;
+    i -= part * each;
+    const int group = i / (8 * w.down), first = group * 8, width = min(8, w.across - first);
+    i -= group * 8 * w.down;
+    const int m = i / width;
+    return {m, first + i - m * width, part};
+}
+
+// 32 staged rows of kBytes from or to global memory, row by row: 16 bytes a lane, or an element
+template <bool kLoad, int kBytes, typename E>
+__device__ __forceinline__ void copy_rows(char *staged, E *at, long long row, int rows, int cols, bool wide) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kLanes = kBytes / 16, kEach = 16 / sizeof(E);
+    if (wide) {
+        const int c = (lane % kLanes) * kEach;
+#pragma unroll
+        for (int r = lane / kLanes; r < 32; r += 32 / kLanes)
+            if (r < rows && c < cols) {
+                uint4 *s = reinterpret_cast<uint4 *>(staged + r * kPitch + c * sizeof(E));
+                if constexpr (kLoad) *s = *reinterpret_cast<const uint4 *>(at + r * row + c);
+                else *reinterpret_cast<uint4 *>(at + r * row + c) = *s;
+            }
+    } else {
+        for (int r = 0; r < 32 && r < rows; ++r)
+            for (int c = lane; c < kBytes / (int)sizeof(E) && c < cols; c += 32) {
+                char *s = staged + r * kPitch + c * sizeof(E);
+                if constexpr (kLoad) memcpy(s, at + r * row + c, sizeof(E));
+                else at[r * row + c] = *reinterpret_cast<const E *>(s);
+            }
+    }
+}
+
+template <Mode kMode>
+__global__ void __launch_bounds__(kThreads, 1)
+ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, Work w) {
+    extern __shared__ char raw[];
+    char *stages = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    char *staging = stages + kStages * kStageBytes;
+    Bars *bars = reinterpret_cast<Bars *>(staging + 4 * kStagingBytes);
+    static_assert(sizeof(Bars) <= 256, "the barriers' room");
+    constexpr bool kAcross = kMode == kDw, kBcross = kMode == kDx || kMode == kDw;  // read against the sum's direction
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int clusters = gridDim.x / 2, tiles = w.down * w.across * w.parts;
+    let_next_begin();
+    if (threadIdx.x == 0) {
+        prefetch_tmap(&map_a);
+        prefetch_tmap(&map_b);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&bars->full[s], rank == 0 ? 2 : 1);
+            mbar_init(&bars->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&bars->done[b], 1);
+            mbar_init(&bars->taken[b], 8);
+        }
+        mbar_init(&bars->drain, 1);
+        bars->stop = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&bars->tmem))
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_meet();
+    tc_fence_after();
+    after_previous();
+    if (w.clear && blockIdx.x == 0 && threadIdx.x == 0) *w.header = WsHeader{};  // (waits set it after seconds)
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&bars->tmem);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0, sent = 0;
+            bool ok = true;
+            for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
+                const Tile t = tile_of(w, i);
+                const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
+                for (int k = k_lo; k < k_hi; ++k) {
+                    if (!wait(&bars->empty[s], phase ^ 1, bars, w.header, 1)) {
+                        ok = false;
+                        break;
+                    }
+                    char *a = stages + s * kStageBytes, *b = a + kHalfBytes;
+                    uint64_t *bar = &bars->full[s];
+                    mbar_arrive_expect_tx(bar, kStageBytes);
+                    if (kMode == kOut || kMode == kGrad) {
+                        tma_load_3d(a, &map_a, bar, k * kStep, t.m * kTile + rank * kHalf, 0);
+                        tma_load_3d(b, &map_b, bar, k * kStep, t.n * kHalf, rank);
+                    } else if (kMode == kDx) {
+                        const int plane = k >= w.plane_steps, at = (k - plane * w.plane_steps) * kStep;
+                        tma_load_3d(a, &map_a, bar, at, t.m * kTile + rank * kHalf, plane);
+                        const int n = t.n * kTile + rank * kHalf;
+                        tma_load_3d(b, &map_b, bar, n, at, plane);
+                        tma_load_3d(b + kHalfBytes / 2, &map_b, bar, n + 64, at, plane);
+                    } else {
+                        const int plane = t.m >= w.plane_steps, m = (t.m - plane * w.plane_steps) * kTile + rank * kHalf;
+                        tma_load_3d(a, &map_a, bar, m, k * kStep, plane);
+                        tma_load_3d(a + kHalfBytes / 2, &map_a, bar, m + 64, k * kStep, plane);
+                        const int n = t.n * kTile + rank * kHalf;
+                        tma_load_3d(b, &map_b, bar, n, k * kStep, 0);
+                        tma_load_3d(b + kHalfBytes / 2, &map_b, bar, n + 64, k * kStep, 0);
+                    }
+                    ++sent;
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+            // shared memory goes when the last products have read each stage and said so here, or, where a role gave
+            // up, when the copies have landed
+            const uint64_t t0 = globaltimer_ns();
+            for (uint32_t d = 0; d < kStages && d < sent; ++d) {
+                if (s == 0) phase ^= 1;
+                s = s ? s - 1 : kStages - 1;
+                if (ok) ok = wait(&bars->empty[s], phase, bars, w.header, 6);
+                if (!ok) drain(&bars->full[s], phase, t0);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t idesc = idesc_bf16(256, 256, kAcross, kBcross);
+            int s = 0, b = 0;
+            uint32_t phase = 0, bphase = 0;
+            bool ok = true;
+            for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
+                const Tile t = tile_of(w, i);
+                const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
+                if (!wait(&bars->taken[b], bphase ^ 1, bars, w.header, 2)) break;
+                tc_fence_after();
+                for (int k = k_lo; k < k_hi; ++k) {
+                    if (!wait(&bars->full[s], phase, bars, w.header, 3)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t a = smem_u32(stages + s * kStageBytes), bb = a + kHalfBytes;
+#pragma unroll
+                    for (int kk = 0; kk < kStep / 16; ++kk) {
+                        const uint64_t da = kAcross ? desc_sw128(a + kk * 2048, kHalfBytes / 2, 1024) : desc_sw128(a + kk * 32, 16, 1024);
+                        const uint64_t db = kBcross ? desc_sw128(bb + kk * 2048, kHalfBytes / 2, 1024) : desc_sw128(bb + kk * 32, 16, 1024);
+                        umma_pair(tmem + b * 256, da, db, idesc, k > k_lo || kk > 0);
+                    }
+                    commit_pair(&bars->empty[s]);
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
+                    }
+                }
+                commit_pair(&bars->done[b]);
+                b ^= 1;
+                if (b == 0) bphase ^= 1;
+            }
+            // products in flight read both blocks' shared memory and write their tensor memory
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                             smem_u32(&bars->drain))
+                         : "memory");
+            drain(&bars->drain, 0, globaltimer_ns());
+        } else if (lane == 0) {
+            int s = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
+                const Tile t = tile_of(w, i);
+                const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
+                for (int k = k_lo; k < k_hi; ++k) {
+                    if (!wait(&bars->full[s], phase, bars, w.header, 4)) {
+                        ok = false;
+                        break;
+                    }
+                    arrive_first(&bars->full[s]);
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        char *mine = staging + (warp - 2) * kStagingBytes;
+        const int quarter = warp & 3;
+        int b = 0;
+        uint32_t bphase = 0;
+        for (int i = blockIdx.x / 2; i < tiles; i += clusters) {
+            const Tile t = tile_of(w, i);
+            if (!__all_sync(0xffffffffu, wait(&bars->done[b], bphase, bars, w.header, 5))) break;
+            tc_fence_after();
+            const uint32_t from = taddr(tmem + b * 256, quarter * 32, 0);
+            const int plane = kMode == kDw ? t.m >= w.plane_steps : 0;
+            const int m0 = (kMode == kDw ? t.m - plane * w.plane_steps : t.m) * kTile + rank * kHalf + quarter * 32;
+            const int rows = w.rows - m0;  // (may be below 1)
+            char *row = mine + lane * kPitch;
+            if (kMode == kOut) {
+#pragma unroll 1
+                for (int c = 0; c < kHalf; c += 64) {
+                    const int n0 = t.n * kHalf + c;
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        uint32_t g[32], u[32];
+                        tmem_ld32(from + c + h, g);
+                        tmem_ld32(from + kHalf + c + h, u);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t o[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float v[2], slope;
+#pragma unroll
+                                for (int q = 0; q < 2; ++q)
+                                    v[q] = act_of(w.act, __uint_as_float(g[j + 2 * e + q]), slope) *
+                                           __uint_as_float(u[j + 2 * e + q]);
+                                o[e] = pack_bf16x2(v[0], v[1]);
+                            }
+                            *reinterpret_cast<uint4 *>(row + (h + j) * 2) = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    }
+                    __syncwarp();
+                    copy_rows<false, 128>(mine, static_cast<__nv_bfloat16 *>(w.out) + m0 * w.out_row + n0,
+                                                         w.out_row, rows, w.cols - n0, w.out_wide);
+                    __syncwarp();
+                }
+            } else if (kMode == kGrad) {
+#pragma unroll 1
+                for (int c = 0; c < kHalf; c += 32) {
+                    const int n0 = t.n * kHalf + c;
+                    copy_rows<true, 64>(mine, w.dout + m0 * w.dout_row + n0, w.dout_row, rows,
+                                                             w.cols - n0, w.dout_wide);
+                    __syncwarp();
+                    uint32_t g[32], u[32];
+                    tmem_ld32(from + c, g);
+                    tmem_ld32(from + kHalf + c, u);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 8) {
+                        const uint4 d = *reinterpret_cast<const uint4 *>(row + j * 2);
+                        const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+                        uint32_t og[4], ou[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float d2[2] = {bf16_lo(dw[e]), bf16_hi(dw[e])};
+                            float vg[2], vu[2];
+#pragma unroll
+                            for (int q = 0; q < 2; ++q) {
+                                float slope;
+                                const float a = act_of(w.act, __uint_as_float(g[j + 2 * e + q]), slope);
+                                vg[q] = d2[q] * __uint_as_float(u[j + 2 * e + q]) * slope;
+                                vu[q] = d2[q] * a;
+                            }
+                            og[e] = pack_bf16x2(vg[0], vg[1]);
+                            ou[e] = pack_bf16x2(vu[0], vu[1]);
+                        }
+                        *reinterpret_cast<uint4 *>(row + j * 2) = make_uint4(og[0], og[1], og[2], og[3]);
+                        *reinterpret_cast<uint4 *>(row + 64 + j * 2) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                    }
+                    __syncwarp();
+                    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(w.out) + m0 * w.out_row + n0;
+                    // (dZ's rows are padded to 16 bytes: what is written behind the last column is not read)
+                    const int cols = (w.cols - n0 + 7) & ~7;
+                    copy_rows<false, 64>(mine, to, w.out_row, rows, cols, true);
+                    copy_rows<false, 64>(mine + 64, to + w.out_plane, w.out_row, rows, cols, true);
+                    __syncwarp();
+                }
+            } else if (w.parts == 1) {
+#pragma unroll 1
+                for (int c = 0; c < kTile; c += 64) {
+                    const int n0 = t.n * kTile + c;
+                    if (n0 >= w.cols) break;
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(from + c + h, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8)
+                            *reinterpret_cast<uint4 *>(row + (h + j) * 2) = make_uint4(
+                                pack_bf16x2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])),
+                                pack_bf16x2(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3])),
+                                pack_bf16x2(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5])),
+                                pack_bf16x2(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
+                    }
+                    __syncwarp();
+                    copy_rows<false, 128>(
+                        mine, static_cast<__nv_bfloat16 *>(w.out) + plane * w.out_plane + m0 * w.out_row + n0, w.out_row, rows,
+                        w.cols - n0, w.out_wide);
+                    __syncwarp();
+                }
+            } else {
+                float *out = static_cast<float *>(w.out) +
+                             ((long long)t.part * (kMode == kDw ? 2 : 1) + plane) * w.rows * w.cols + (long long)m0 * w.cols;
+#pragma unroll 1
+                for (int c = 0; c < kTile; c += 32) {
+                    const int n0 = t.n * kTile + c;
+                    if (n0 >= w.cols) break;
+                    uint32_t v[32];
+                    tmem_ld32(from + c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        *reinterpret_cast<uint4 *>(row + j * 4) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    __syncwarp();
+                    copy_rows<false, 128>(mine, out + n0, w.cols, rows, w.cols - n0, w.cols % 4 == 0);
+                    __syncwarp();
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_first(&bars->taken[b]);
+            b ^= 1;
+            if (b == 0) bphase ^= 1;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_meet();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// rows of K elements to rows of `stride` (a multiple of 8) elements
+__global__ void __launch_bounds__(256) ffn_align_kernel(const __nv_bfloat16 *from, long long from_row, __nv_bfloat16 *to,
+                                                       long long to_row, int rows, int K) {
+    let_next_begin();
+    after_previous();
+    for (int r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int k = threadIdx.x; k < K; k += 256) to[r * to_row + k] = from[r * from_row + k];
+}
+
+// out = the sum of `parts` runs of rows x cols
+__global__ void __launch_bounds__(256) ffn_parts_kernel(const float *from, int parts, long long rows, int cols,
+                                                       __nv_bfloat16 *out, long long out_row) {
+    let_next_begin();
+    after_previous();
+    const long long all = rows * cols;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+        float sum = 0.f;
+#pragma unroll 4
+        for (int z = 0; z < parts; ++z) sum += from[z * all + i];
+        const long long m = i / cols;
+        from_f32(out + m * out_row + (i - m * cols), sum);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// host side
+// ------------------------------------------------------------------------------------------------
+
+constexpr int kSMs = 152, kPairs = kSMs / 2;
+
+int up8(int v) { return (v + 7) & ~7; }
+int tiles_of(int v, int by) { return (v + by - 1) / by; }
+
+// [planes][rows][cols] of bf16 with rows `row` and planes `plane` elements apart; a box of 64 columns and box_rows rows
+cudaError_t map_of(CUtensorMap *map, const void *p, long long cols, long long rows, int planes, long long row, long long plane,
+                   int box_rows) {
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)row * 2, (cuuint64_t)plane * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, one[3] = {1, 1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <Mode kMode>
+cudaError_t run(const CUtensorMap &a, const CUtensorMap &b, const Work &w, cudaStream_t s) {
+    const cudaError_t e = cudaFuncSetAttribute(ffn_tile_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e) return e;
+    const long long tiles = (long long)w.down * w.across * w.parts;
+    return launch_cluster_after(ffn_tile_kernel<kMode>, 2u * (unsigned)(tiles < kPairs ? tiles : kPairs), kThreads, 2, kSmemBytes,
+                                s, a, b, w);
+}
+
+// Cuts of a sum of `steps`: as many as give every pair a tile, of eight steps or more
+int cuts(long long tiles, int steps) {
+    const long long by_pairs = kPairs / tiles, by_steps = steps / 8;
+    const long long n = by_pairs < by_steps ? by_pairs : by_steps;
+    return n < 1 ? 1 : (int)n;
+}
+struct Cut {
+    int parts, per;
+};
+Cut cut(long long tiles, int steps) {
+    const int per = tiles_of(steps, cuts(tiles, steps));
+    return {tiles_of(steps, per), per};
+}
+Cut cut_dx(int M, int K, int F) { return cut((long long)tiles_of(M, kTile) * tiles_of(K, kTile), 2 * tiles_of(F, kStep)); }
+Cut cut_dw(int M, int K, int F) { return cut(2LL * tiles_of(F, kTile) * tiles_of(K, kTile), tiles_of(M, kStep)); }
+
+size_t up256(size_t v) { return align_up(v, 256); }
+size_t aligned_bytes(int M, int K, int F) {  // x and w in aligned rows
+    return up256((size_t)M * up8(K) * 2) + up256((size_t)2 * F * up8(K) * 2);
+}
+
+struct Operands {
+    const __nv_bfloat16 *x, *w;
+    long long x_row, w_row;
+};
+// x and w as the copies need them: where rows do not begin at 16 bytes, in the workspace (at `at`, moved on)
+cudaError_t align_operands(const Ffn &p, char *&at, Operands &o, cudaStream_t s) {
+    const int K8 = up8(p.K);
+    o = {static_cast<const __nv_bfloat16 *>(p.x), static_cast<const __nv_bfloat16 *>(p.w), p.x_stride, p.K};
+    if (p.M == 1) o.x_row = K8;  // (the only row's stride is not used)
+    if (!rows_aligned(p.x, o.x_row, 2, 16)) {
+        __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(at);
+        const cudaError_t e = launch_after(ffn_align_kernel, p.M < 8 * kSMs ? p.M : 8 * kSMs, 256, 0, s, o.x, p.x_stride, to,
+                                           (long long)K8, p.M, p.K);
+        if (e) return e;
+        o.x = to;
+        o.x_row = K8;
+    }
+    at += up256((size_t)p.M * K8 * 2);
+    if (!rows_aligned(p.w, o.w_row, 2, 16)) {
+        __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(at);
+        const cudaError_t e = launch_after(ffn_align_kernel, 2 * p.F < 8 * kSMs ? 2 * p.F : 8 * kSMs, 256, 0, s, o.w,
+                                           (long long)p.K, to, (long long)K8, 2 * p.F, p.K);
+        if (e) return e;
+        o.w = to;
+        o.w_row = K8;
+    }
+    at += up256((size_t)2 * p.F * K8 * 2);
+    return cudaSuccess;
+}
+
+bool wide(const void *p, long long row, int cols) { return cols % 8 == 0 && rows_aligned(p, row, 2, 16); }
+
+// kOut and kGrad
+template <Mode kMode>
+cudaError_t forward_product(const Ffn &p, const Operands &o, Work w, cudaStream_t s) {
+    CUtensorMap a, b;
+    cudaError_t e = map_of(&a, o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kHalf);
+    if (!e) e = map_of(&b, o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kHalf);
+    if (e) return e;
+    w.down = tiles_of(p.M, kTile);
+    w.across = tiles_of(p.F, kHalf);
+    w.parts = 1;
+    w.steps = w.per_part = tiles_of(p.K, kStep);
+    w.rows = p.M;
+    w.cols = p.F;
+    w.act = p.act;
+    w.clear = 1;
+    return run<kMode>(a, b, w, s);
+}
+
+cudaError_t add_parts(const float *from, int parts, long long rows, int cols, void *out, long long out_row, cudaStream_t s) {
+    const long long blocks = (rows * cols + 255) / 256;
+    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 16 * kSMs ? blocks : 16 * kSMs), 256, 0, s, from, parts, rows, cols,
+                        static_cast<__nv_bfloat16 *>(out), out_row);
+}
+
+}  // namespace
+
+size_t ffn_tc_forward_scratch_bytes(int M, int K, int F) { return aligned_bytes(M, K, F); }
+
+size_t ffn_tc_backward_scratch_bytes(int M, int K, int F) {
+    if (M == 0) return 0;
+    const Cut dx = cut_dx(M, K, F), dw = cut_dw(M, K, F);
+    return aligned_bytes(M, K, F) + up256((size_t)2 * M * up8(F) * 2) + (dx.parts > 1 ? up256(sizeof(float) * dx.parts * M * K) : 0) +
+           (dw.parts > 1 ? up256(sizeof(float) * dw.parts * 2 * F * K) : 0);
+}
+
+cudaError_t ffn_tc_forward(const Ffn &p, cudaStream_t s) {
+    char *at = p.ws + kWsHeaderBytes;
+    Operands o;
+    cudaError_t e = align_operands(p, at, o, s);
+    if (e) return e;
+    Work w{};
+    w.out = p.out;
+    w.out_row = p.out_stride;
+    w.out_wide = wide(p.out, p.out_stride, p.F);
+    w.header = reinterpret_cast<WsHeader *>(p.ws);
+    return forward_product<kOut>(p, o, w, s);
+}
+
+cudaError_t ffn_tc_backward(const FfnBwd &q, cudaStream_t s) {
+    const Ffn &p = q.f;
+    char *at = p.ws + kWsHeaderBytes;
+    Operands o;
+    cudaError_t e = align_operands(p, at, o, s);
+    if (e) return e;
+    const int F8 = up8(p.F);
+    const long long dz_plane = (long long)p.M * F8;
+    __nv_bfloat16 *dz = reinterpret_cast<__nv_bfloat16 *>(at);
+    at += up256((size_t)2 * dz_plane * 2);
+    Work w{};
+    w.header = reinterpret_cast<WsHeader *>(p.ws);
+    w.out = dz;
+    w.out_row = F8;
+    w.out_plane = dz_plane;
+    w.out_wide = 1;
+    w.dout = static_cast<const __nv_bfloat16 *>(q.dout);
+    w.dout_row = q.dout_stride;
+    w.dout_wide = wide(q.dout, q.dout_stride, p.F);
+    e = forward_product<kGrad>(p, o, w, s);
+    if (e) return e;
+
+    CUtensorMap a, b;
+    // dx: the sum runs over both planes of dZ and w
+    e = map_of(&a, dz, p.F, p.M, 2, F8, dz_plane, kHalf);
+    if (!e) e = map_of(&b, o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kStep);
+    if (e) return e;
+    const Cut dx = cut_dx(p.M, p.K, p.F), dw = cut_dw(p.M, p.K, p.F);
+    w = Work{};
+    w.header = reinterpret_cast<WsHeader *>(p.ws);
+    w.down = tiles_of(p.M, kTile);
+    w.across = tiles_of(p.K, kTile);
+    w.plane_steps = tiles_of(p.F, kStep);
+    w.steps = 2 * w.plane_steps;
+    w.parts = dx.parts;
+    w.per_part = dx.per;
+    w.rows = p.M;
+    w.cols = p.K;
+    w.out = dx.parts > 1 ? at : q.dx;
+    w.out_row = q.dx_stride;
+    w.out_wide = wide(q.dx, q.dx_stride, p.K);
+    e = run<kDx>(a, b, w, s);
+    if (e) return e;
+    if (dx.parts > 1) {
+        e = add_parts(reinterpret_cast<const float *>(at), dx.parts, p.M, p.K, q.dx, q.dx_stride, s);
+        if (e) return e;
+        at += up256(sizeof(float) * dx.parts * p.M * p.K);
+    }
+
+    // dw: tiles of either plane, the sum over tokens
+    e = map_of(&a, dz, p.F, p.M, 2, F8, dz_plane, kStep);
+    if (!e) e = map_of(&b, o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kStep);
+    if (e) return e;
+    w.plane_steps = tiles_of(p.F, kTile);
+    w.down = 2 * w.plane_steps;
+    w.steps = tiles_of(p.M, kStep);
+    w.parts = dw.parts;
+    w.per_part = dw.per;
+    w.rows = p.F;
+    w.out = dw.parts > 1 ? at : q.dw;
+    w.out_row = p.K;
+    w.out_plane = (long long)p.F * p.K;
+    w.out_wide = wide(q.dw, p.K, p.K);
+    e = run<kDw>(a, b, w, s);
+    if (e || dw.parts == 1) return e;
+    return add_parts(reinterpret_cast<const float *>(at), dw.parts, 2LL * p.F, p.K, q.dw, p.K, s);
+}
+
+}  // namespace hla
