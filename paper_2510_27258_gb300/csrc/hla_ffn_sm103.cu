@@ -11,9 +11,9 @@
 // (MN-major), so nothing is transposed in memory.  The forward's tile has 128 gate columns (the first block's half of B)
 // and the same 128 up columns (the second's), so that activation and product happen where the tile is read out.
 //
-// A block has a loading warp, a warp that issues the products (first block) or tells the first block that this one's
-// half of a step has landed (second), and four warps that read finished tiles out of tensor memory, whose 512 columns
-// hold two of them, so that reading out is hidden behind the next tile.  Blocks stay for many tiles, which are taken
+// A block has a loading warp, whose copies count at the first block's barriers, a warp that issues the products (first
+// block) and four warps that read finished tiles out of tensor memory, whose 512 columns hold two of them, so that
+// reading out is hidden behind the next tile.  Blocks stay for many tiles, which are taken
 // in groups of eight columns so that a round of all blocks reads few distinct rows.  Where tiles are few and the
 // sum long, the sum is cut and the parts are added in their order by another kernel.
 //
@@ -36,7 +36,7 @@ constexpr int kStages = 6;
 constexpr uint32_t kPitch = 144;                         // a staged row of 128 bytes and what keeps banks apart
 constexpr uint32_t kStagingBytes = 32 * kPitch;          // of a warp that reads out
 constexpr uint32_t kSmemBytes = 1024 + kStages * kStageBytes + 4 * kStagingBytes + 256;
-constexpr uint64_t kWaitNs = 2000000000ull;
+constexpr uint64_t kWaitNs = 2000000000ull, kLandNs = 100000000ull;
 
 enum Mode { kOut, kGrad, kDx, kDw };
 
@@ -73,31 +73,28 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// one arrival at the first block's barrier
-__device__ __forceinline__ void arrive_first(uint64_t *bar) {
-    asm volatile(
-        "{\n\t.reg .b32 at;\n\t"
-        "mapa.shared::cluster.u32 at, %0, 0;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [at];\n\t}" ::"r"(smem_u32(bar))
-        : "memory");
+// the first block's barrier in the place of this one
+__device__ __forceinline__ uint32_t of_first(uint64_t *bar) {
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(bar)));
+    return at;
 }
-__device__ __forceinline__ bool try_wait_cluster(uint64_t *bar, uint32_t parity) {
-    uint32_t ok;
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// a copy into this block's shared memory whose bytes count at the first block's barrier
+__device__ __forceinline__ void load_pair(void *dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
         : "memory");
-    return ok != 0;
 }
 // false: another role gave up, or this wait did
 __device__ bool wait(uint64_t *bar, uint32_t parity, Bars *bars, WsHeader *header, unsigned where) {
-    if (try_wait_cluster(bar, parity)) return true;
+    if (mbar_try_wait(bar, parity)) return true;
     const uint64_t t0 = globaltimer_ns();
     while (true) {
-        if (try_wait_cluster(bar, parity)) return true;
+        if (mbar_try_wait(bar, parity)) return true;
         if (*reinterpret_cast<volatile int *>(&bars->stop)) return false;
         if (globaltimer_ns() - t0 > kWaitNs) {
             header->where = where;
@@ -108,9 +105,10 @@ __device__ bool wait(uint64_t *bar, uint32_t parity, Bars *bars, WsHeader *heade
         }
     }
 }
-// what is in flight when a role gives up; not longer than the limit
-__device__ void drain(uint64_t *bar, uint32_t parity, uint64_t t0) {
-    while (!try_wait_cluster(bar, parity) && globaltimer_ns() - t0 <= kWaitNs) {
+// products in flight when a role gives up; not longer than the limit
+__device__ void drain(uint64_t *bar, uint32_t parity) {
+    const uint64_t t0 = globaltimer_ns();
+    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 <= kWaitNs) {
     }
 }
 
@@ -195,7 +193,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         prefetch_tmap(&map_a);
         prefetch_tmap(&map_b);
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&bars->full[s], rank == 0 ? 2 : 1);
+            mbar_init(&bars->full[s], 1);
             mbar_init(&bars->empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -233,24 +231,24 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         break;
                     }
                     char *a = stages + s * kStageBytes, *b = a + kHalfBytes;
-                    uint64_t *bar = &bars->full[s];
-                    mbar_arrive_expect_tx(bar, kStageBytes);
+                    const uint32_t bar = of_first(&bars->full[s]);
+                    if (rank == 0) mbar_arrive_expect_tx(&bars->full[s], 2 * kStageBytes);
                     if (kMode == kOut || kMode == kGrad) {
-                        tma_load_3d(a, &map_a, bar, k * kStep, t.m * kTile + rank * kHalf, 0);
-                        tma_load_3d(b, &map_b, bar, k * kStep, t.n * kHalf, rank);
+                        load_pair(a, &map_a, bar, k * kStep, t.m * kTile + rank * kHalf, 0);
+                        load_pair(b, &map_b, bar, k * kStep, t.n * kHalf, rank);
                     } else if (kMode == kDx) {
                         const int plane = k >= w.plane_steps, at = (k - plane * w.plane_steps) * kStep;
-                        tma_load_3d(a, &map_a, bar, at, t.m * kTile + rank * kHalf, plane);
+                        load_pair(a, &map_a, bar, at, t.m * kTile + rank * kHalf, plane);
                         const int n = t.n * kTile + rank * kHalf;
-                        tma_load_3d(b, &map_b, bar, n, at, plane);
-                        tma_load_3d(b + kHalfBytes / 2, &map_b, bar, n + 64, at, plane);
+                        load_pair(b, &map_b, bar, n, at, plane);
+                        load_pair(b + kHalfBytes / 2, &map_b, bar, n + 64, at, plane);
                     } else {
                         const int plane = t.m >= w.plane_steps, m = (t.m - plane * w.plane_steps) * kTile + rank * kHalf;
-                        tma_load_3d(a, &map_a, bar, m, k * kStep, plane);
-                        tma_load_3d(a + kHalfBytes / 2, &map_a, bar, m + 64, k * kStep, plane);
+                        load_pair(a, &map_a, bar, m, k * kStep, plane);
+                        load_pair(a + kHalfBytes / 2, &map_a, bar, m + 64, k * kStep, plane);
                         const int n = t.n * kTile + rank * kHalf;
-                        tma_load_3d(b, &map_b, bar, n, k * kStep, 0);
-                        tma_load_3d(b + kHalfBytes / 2, &map_b, bar, n + 64, k * kStep, 0);
+                        load_pair(b, &map_b, bar, n, k * kStep, 0);
+                        load_pair(b + kHalfBytes / 2, &map_b, bar, n + 64, k * kStep, 0);
                     }
                     ++sent;
                     if (++s == kStages) {
@@ -259,14 +257,15 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     }
                 }
             }
-            // shared memory goes when the last products have read each stage and said so here, or, where a role gave
-            // up, when the copies have landed
+            // Shared memory goes when the last products have read each stage and said so here.  Where a role gave up
+            // there is no sign of a copy but its time: one that was sent lands within microseconds
             const uint64_t t0 = globaltimer_ns();
-            for (uint32_t d = 0; d < kStages && d < sent; ++d) {
+            for (uint32_t d = 0; ok && d < kStages && d < sent; ++d) {
                 if (s == 0) phase ^= 1;
                 s = s ? s - 1 : kStages - 1;
-                if (ok) ok = wait(&bars->empty[s], phase, bars, w.header, 6);
-                if (!ok) drain(&bars->full[s], phase, t0);
+                ok = wait(&bars->empty[s], phase, bars, w.header, 4);
+            }
+            while (!ok && globaltimer_ns() - t0 < kLandNs) {
             }
         }
         __syncwarp();
@@ -308,26 +307,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
                              smem_u32(&bars->drain))
                          : "memory");
-            drain(&bars->drain, 0, globaltimer_ns());
-        } else if (lane == 0) {
-            int s = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
-                const Tile t = tile_of(w, i);
-                const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
-                for (int k = k_lo; k < k_hi; ++k) {
-                    if (!wait(&bars->full[s], phase, bars, w.header, 4)) {
-                        ok = false;
-                        break;
-                    }
-                    arrive_first(&bars->full[s]);
-                    if (++s == kStages) {
-                        s = 0;
-                        phase ^= 1;
-                    }
-                }
-            }
+            drain(&bars->drain, 0);
         }
         __syncwarp();
     } else {
@@ -459,7 +439,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_first(&bars->taken[b]);
+            if (lane == 0) arrive_at(of_first(&bars->taken[b]));
             b ^= 1;
             if (b == 0) bphase ^= 1;
         }
