@@ -509,7 +509,8 @@ int hla_glr_marks(int n);
  * marks     : device fp32 [B, hla_glr_marks(n), C] or NULL; receives the state before
  *             every 32nd token, which hla_glr_backward reads
  * decay, states and marks are 16-byte aligned.
- * No workspace.  fp32 throughout for both types; a NaN or infinity in a token reaches that token's
+ * No workspace (should a wait between the blocks of one sequence run past its limit of 2 s, states and
+ * outputs are NaN from there on).  fp32 throughout for both types; a NaN or infinity in a token reaches that token's
  * output and, where it enters the state, later ones, and no earlier one.
  */
 hla_status hla_glr_forward(const void *x, const void *r, const void *g, const float *decay, void *y, hla_dtype dt, int B,

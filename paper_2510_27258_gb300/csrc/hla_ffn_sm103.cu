@@ -36,7 +36,7 @@ constexpr int kStages = 6;
 constexpr uint32_t kPitch = 144;                         // a staged row of 128 bytes and what keeps banks apart
 constexpr uint32_t kStagingBytes = 32 * kPitch;          // of a warp that reads out
 constexpr uint32_t kSmemBytes = 1024 + kStages * kStageBytes + 4 * kStagingBytes + 256;
-constexpr uint64_t kWaitNs = 2000000000ull, kLandNs = 100000000ull;
+constexpr long long kWaitCycles = 4000000000ll, kLandCycles = 200000000ll;  // about 2 and 0.1 s
 
 enum Mode { kOut, kGrad, kDx, kDw };
 
@@ -92,11 +92,11 @@ __device__ __forceinline__ void load_pair(void *dst, const CUtensorMap *map, uin
 // false: another role gave up, or this wait did
 __device__ bool wait(uint64_t *bar, uint32_t parity, Bars *bars, WsHeader *header, unsigned where) {
     if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = globaltimer_ns();
+    const long long t0 = clock64();
     while (true) {
         if (mbar_try_wait(bar, parity)) return true;
         if (*reinterpret_cast<volatile int *>(&bars->stop)) return false;
-        if (globaltimer_ns() - t0 > kWaitNs) {
+        if (clock64() - t0 > kWaitCycles) {
             header->where = where;
             header->detail = blockIdx.x;
             header->error = kDevTimeout;
@@ -107,8 +107,8 @@ __device__ bool wait(uint64_t *bar, uint32_t parity, Bars *bars, WsHeader *heade
 }
 // products in flight when a role gives up; not longer than the limit
 __device__ void drain(uint64_t *bar, uint32_t parity) {
-    const uint64_t t0 = globaltimer_ns();
-    while (!mbar_try_wait(bar, parity) && globaltimer_ns() - t0 <= kWaitNs) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity) && clock64() - t0 <= kWaitCycles) {
     }
 }
 
@@ -259,13 +259,13 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
             // Shared memory goes when the last products have read each stage and said so here.  Where a role gave up
             // there is no sign of a copy but its time: one that was sent lands within microseconds
-            const uint64_t t0 = globaltimer_ns();
+            const long long t0 = clock64();
             for (uint32_t d = 0; ok && d < kStages && d < sent; ++d) {
                 if (s == 0) phase ^= 1;
                 s = s ? s - 1 : kStages - 1;
                 ok = wait(&bars->empty[s], phase, bars, w.header, 4);
             }
-            while (!ok && globaltimer_ns() - t0 < kLandNs) {
+            while (!ok && clock64() - t0 < kLandCycles) {
             }
         }
         __syncwarp();

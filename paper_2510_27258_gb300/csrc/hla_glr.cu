@@ -2,27 +2,32 @@
 //
 //   s = sigmoid(r), i = sigmoid(g), a = e^(decay s), m = sqrt(1 - a^2), b = m i x,  h_t = a_t h_{t-1} + b_t
 // and backwards, with D_t = a_t (dy_t + D_{t+1}) the gradient of h_{t-1} and G_t = dy_t + D_{t+1} that of h_t,
-//   dx = G m i,  dg = dx x (1 - i),  e = G (a h_{t-1} - i x (1/m - m)),  dr = e decay s (1 - s),  ddecay = sum e s
-// (a^2 / m = 1/m - m).  1 - a^2 is u - u^2/2 + ... where u = -2 decay s is below 1/2: the difference would
-// lose what a slow decay is about.
+//   dx = G m i,  dg = G b (1 - i),  e = G (h_t - i x / m),  dr = e decay s (1 - s),  ddecay = sum e s
+// (the derivative of h_t by log a is a h_{t-1} - i x a^2 / m, and a h_{t-1} = h_t - m i x).  1 - a^2 is u - u^2/2 + ...
+// where u = -2 decay s is below 1/2: the difference would lose what a slow decay is about.
 //
 // The recurrence composes: a run of tokens takes h to P h + l, so the sequence is walked in tiles whose warps
 // scan their own tokens side by side and join by P and l in shared memory; one pass over the data.  A block holds 64
 // channels (two a lane, 128 bytes of bf16 a row).  Where there are few channels a cluster of blocks walks
-// one sequence together: every block hands its tile's P and l to the others' shared memory, one cluster barrier a
-// round, and all form the same state in the same order, so equal inputs give equal bits and no kernel waits on
-// another.  The gradient walks the tiles backwards and takes h before each tile from the marks that the forward
+// one sequence together: every block hands its tile's P and l to the others' shared memory, where their bytes
+// count at a barrier, and all form the same state in the same order, so equal inputs give equal bits.  The gradient walks the tiles backwards and takes h before each tile from the marks that the forward
 // leaves, so it reads every token once too.
 #include "hla_vec.cuh"
+#include "sm103_prims.cuh"
 
 namespace hla {
 namespace {
 
-constexpr int kChannels = 64;                 // channels of a block
-constexpr int kTile = kGlrTile;               // tokens of a block's tile, a mark each
-constexpr int kMaxCluster = 8;
+using namespace sm103;
+
+constexpr int kThreads = 256;
+constexpr int kMaxCluster = 16;
+constexpr int kSlotsFwd = 3, kSlotsBwd = 3;
+constexpr int kSMs = 152;
+constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
+constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN: a wait ran out
 constexpr float kLog2e = 1.44269504f;
-constexpr float kTiny = 1e-37f;               // below any 1 - a^2 of a decay that matters: keeps 1/m finite
+constexpr float kTiny = 1e-37f;               // beside 1 - a^2: keeps 1/m finite where a is 1
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -75,52 +80,156 @@ __device__ __forceinline__ void decay_of(const Decay &d, uint64_t s, uint64_t &a
     unpair(p, p0, p1);
     unpair(far, f0, f1);
     // (a NaN in r is in both)
-    w = pair(u0 < 0.5f ? fmaxf(p0, kTiny) : f0, u1 < 0.5f ? fmaxf(p1, kTiny) : f1);
+    w = pair(u0 < 0.5f ? p0 : f0, u1 < 0.5f ? p1 : f1);
 }
 
-// two channels of one lane: neighbours, or 32 apart where rows are not aligned to pairs
-template <bool kVec>
-struct Lane {
-    int c0, c1;
-    bool on0, on1;
-    __device__ __forceinline__ Lane(int slab, int C) {
-        const int lane = threadIdx.x & 31;
-        c0 = slab * kChannels + (kVec ? 2 * lane : lane);
-        c1 = kVec ? c0 + 1 : c0 + 32;
-        on0 = c0 < C;
-        on1 = c1 < C;
+// A block's shape: kLanes lanes walk a token's 2 kLanes channels, so a block of 256 threads has kGroups runs of kTok
+// tokens side by side
+template <int kLanes_, int kTok_>
+struct Shape {
+    static constexpr int kLanes = kLanes_, kTok = kTok_, kChannels = 2 * kLanes, kGroups = kThreads / kLanes;
+    static constexpr int kOfWarp = 32 / kLanes, kSpan = kGroups * kTok;
+    static_assert(kSpan % kGlrTile == 0, "a block's tile begins at a mark");
+    static __device__ __forceinline__ int lane() { return threadIdx.x % kLanes; }
+    static __device__ __forceinline__ int group() {
+        // (the same for a warp where a warp is a group: rows are uniform registers then)
+        return kLanes == 32 ? __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0) : threadIdx.x / kLanes;
     }
+};
+
+// Two neighbouring channels of one lane
+struct Lane {
+    uint32_t c0;
+    bool on0, on1;
+    __device__ __forceinline__ Lane(uint32_t first, int lane, int C) {
+        c0 = first + 2 * lane;  // (C is below 2^31 - 256: no wrap)
+        on0 = c0 < (uint32_t)C;
+        on1 = c0 + 1 < (uint32_t)C;
+    }
+    // pairs: rows are aligned to two elements, and C is even
     template <typename T>
-    __device__ __forceinline__ Raw<T, 2> load(const T *row, bool on) const {
+    __device__ __forceinline__ Raw<T, 2> load(const T *row, bool pairs) const {
         Raw<T, 2> r = raw_zero<T, 2>();
-        if (kVec) {
-            if (on && on0) r = raw_load<T, 2>(row + c0);
+        if (pairs) {
+            if (on0) r = raw_load<T, 2>(row + c0);
         } else {
             T *e = reinterpret_cast<T *>(&r);
-            if (on && on0) e[0] = row[c0];
-            if (on && on1) e[1] = row[c1];
+            if (on0) e[0] = row[c0];
+            if (on1) e[1] = row[c0 + 1];
         }
         return r;
     }
     template <typename T>
-    __device__ __forceinline__ uint64_t get(const T *row) const {
+    __device__ __forceinline__ uint64_t get(const T *row, bool pairs) const {
         uint64_t f[1];
-        to_pairs(load(row, true), f);
+        to_pairs(load(row, pairs), f);
         return f[0];
     }
     template <typename T>
-    __device__ __forceinline__ void put(T *row, uint64_t v) const {
+    __device__ __forceinline__ void put(T *row, uint64_t v, bool pairs) const {
         float x, y;
         unpair(v, x, y);
-        if (kVec) {
+        if (pairs) {
             const float f[2] = {x, y};
             if (on0) VecIo<T, 2>::store(row + c0, f);
         } else {
             if (on0) from_f32(row + c0, x);
-            if (on1) from_f32(row + c1, y);
+            if (on1) from_f32(row + c0 + 1, y);
         }
     }
 };
+
+// A lane's next tokens of kTensors tensors.  kRing: rows that begin at 16 bytes come through a ring of kSlots rounds in
+// shared memory by asynchronous copies of a warp for its own groups, all but the round in use in flight.  Else they are
+// loaded into registers a round ahead.
+template <typename T, typename S, int kTensors, int kSlots, bool kRing>
+struct Tokens {
+    static constexpr int kTok = S::kTok, kRow = S::kChannels * (int)sizeof(T), kChunks = kRow / 16;
+    static constexpr int kRows = kTok * S::kOfWarp, kSlotBytes = kTensors * kRows * kRow;
+    static constexpr int kSmem = kRing ? kThreads / 32 * kSlots * kSlotBytes : 0;
+    const T *from[kTensors];
+    long long stride[kTensors];
+    char *ring;      // this warp's
+    int len, bytes;  // of the sequence; of this lane's chunk
+    Raw<T, 2> ahead[kRing ? 1 : kTensors][kRing ? 1 : kTok];
+
+    __device__ __forceinline__ void set(int i, const void *p, long long row_stride, size_t row0, uint32_t channel) {
+        from[i] = static_cast<const T *>(p) + row0 * row_stride;
+        stride[i] = row_stride;
+        if constexpr (kRing) {
+            const int lane = threadIdx.x & 31;
+            from[i] += (lane / kChunks) * row_stride + (long long)channel + lane % kChunks * (16 / (int)sizeof(T));
+        }
+    }
+    __device__ __forceinline__ void open(char *smem, uint32_t channel, int C, int length) {
+        ring = smem + (threadIdx.x >> 5) * (kSlots * kSlotBytes);
+        len = length;
+        const int left = min((int)(C - channel), S::kChannels) * (int)sizeof(T) - (int)(threadIdx.x % kChunks) * 16;
+        bytes = min(max(left, 0), 16);
+    }
+    // t0: the group's first token
+    __device__ __forceinline__ void send(int slot, int t0, const Lane &at) {
+        if constexpr (kRing) {
+            const int lane = threadIdx.x & 31, first = t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0);  // the warp's
+            char *to = ring + slot * kSlotBytes + lane % kChunks * 16;
+            const bool all = first >= 0 && first + kRows <= len;
+#pragma unroll
+            for (int i = 0; i < kTensors; ++i) {
+                const T *p = from[i] + (long long)first * stride[i];
+#pragma unroll
+                for (int u = 0; u < kRows; u += 32 / kChunks, p += 32 / kChunks * stride[i]) {
+                    const int t = u + lane / kChunks, row = t % kTok * S::kOfWarp + t / kTok;  // (groups' rows by turns)
+                    const int n = all || (unsigned)(first + t) < (unsigned)len ? bytes : 0;  // (0 reads nothing)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to + (i * kRows + row) * kRow)),
+                                 "l"(p), "r"(n)
+                                 : "memory");
+                }
+            }
+            ring_commit();
+        } else {
+#pragma unroll
+            for (int u = 0; u < kTok; ++u)
+#pragma unroll
+                for (int i = 0; i < kTensors; ++i)
+                    ahead[i][u] = (unsigned)(t0 + u) < (unsigned)len
+                                      ? at.load(from[i] + (long long)(t0 + u) * stride[i], false)
+                                      : raw_zero<T, 2>();
+        }
+    }
+    // before the first round: the rounds behind it `step` tokens apart
+    __device__ __forceinline__ void begin(int t0, int step, const Lane &at) {
+        if constexpr (kRing) {
+#pragma unroll
+            for (int k = 0; k < kSlots - 1; ++k) send(k, t0 + k * step, at);
+        } else {
+            send(0, t0, at);
+        }
+    }
+    // at the start of a round: its tokens are there, and the slot of the last round is filled again
+    __device__ __forceinline__ void next(int slot, int t0, int step, const Lane &at) {
+        if constexpr (kRing) {
+            ring_wait<kSlots - 2>();
+            __syncwarp();
+            send(slot ? slot - 1 : kSlots - 1, t0 + (kSlots - 1) * step, at);
+        }
+    }
+    __device__ __forceinline__ Raw<T, 2> get(int slot, int i, int u) const {
+        if constexpr (kRing)
+            return raw_load<T, 2>(
+                reinterpret_cast<const T *>(ring + slot * kSlotBytes + (i * kRows + u * S::kOfWarp) * kRow) +
+                2 * (threadIdx.x & 31));
+        else
+            return ahead[i][u];
+    }
+    // when the round's tokens have been used
+    __device__ __forceinline__ void used(int t0, int step, const Lane &at) {
+        if constexpr (!kRing) send(0, t0 + step, at);
+    }
+};
+
+// r of tokens behind a length: minus infinity, whose decay is 1
+__device__ __forceinline__ void shut(Raw<__nv_bfloat16, 2> &r) { r.v = 0xff80ff80u; }
+__device__ __forceinline__ void shut(Raw<float, 2> &r) { r.v.x = r.v.y = __int_as_float(0xff800000); }
 
 template <typename T>
 __device__ __forceinline__ uint64_t as_pair(const Raw<T, 2> &r) {
@@ -137,14 +246,6 @@ __device__ __forceinline__ unsigned cluster_rank() {
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// a value into the same place of another block's shared memory
-__device__ __forceinline__ void put_remote(void *mine, unsigned rank, uint64_t a, uint64_t b) {
-    uint32_t to;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                 : "=r"(to)
-                 : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(mine))), "r"(rank));
-    asm volatile("st.shared::cluster.v2.b64 [%0], {%1, %2};" ::"r"(to), "l"(a), "l"(b) : "memory");
-}
 
 // what a run of tokens does to a state: h -> p h + l
 struct __align__(16) Run {
@@ -152,329 +253,399 @@ struct __align__(16) Run {
 };
 __device__ __forceinline__ uint64_t after(const Run &r, uint64_t h) { return fma2(r.p, h, r.l); }
 
-// The state before this warp's tokens and, in `state`, behind the cluster's round, from the runs of every
-// warp (in their order, `first` to `last` by `step`) and block.  kOrder 1: tokens forwards, -1: backwards.
-template <int kWarps, int kOrder>
-__device__ __forceinline__ uint64_t join(const Run (&runs)[kWarps][32], Run (&blocks)[kMaxCluster][32], int S,
-                                         unsigned rank, uint64_t &state, uint64_t &tile_in) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint64_t one = twice(1.f);
+// What the blocks of a cluster tell one another, in two buffers by turns: a block writes a round's run over the one
+// of two rounds before, which every warp of the receiver has read before it sent its run of the last round, which the
+// writer has waited for.
+template <int kLanes>
+struct Exchange {
+    Run runs[2][kMaxCluster][kLanes], mine[2][kLanes];
+    uint64_t bar[2];
+};
+__device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
+    uint32_t to;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(mine)), "r"(rank));
+    return to;
+}
+// every block is there, its barriers ready
+template <int kLanes>
+__device__ __forceinline__ void open_exchange(Exchange<kLanes> &x, int S) {
+    if (S == 1) return;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) mbar_init(&x.bar[i], 1);
+        fence_mbar_init();
+    }
+    __syncthreads();
+    cluster_meet();
+}
+
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, parity))
+        if (clock64() - t0 > kWaitCycles) return false;
+    return true;
+}
+
+// The state before this group's tokens and, in `state`, behind the cluster's round, from the runs of every group
+// (kOrder 1: in their order, -1: against it) and block.  The wait for the others' runs has a limit, after which the
+// states are NaN from there on, and so is what follows from them.
+template <typename Sh, int kOrder>
+__device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLanes], Exchange<Sh::kLanes> &x, int round, int S,
+                                         unsigned rank, int group, uint64_t &state) {
+    const int lane = Sh::lane();
     __syncthreads();
     if (S == 1) {
         uint64_t mine = 0, h = state;
-        tile_in = h;
 #pragma unroll
-        for (int k = 0; k < kWarps; ++k) {
-            const int w = kOrder > 0 ? k : kWarps - 1 - k;
-            if (w == warp) mine = h;
+        for (int k = 0; k < Sh::kGroups; ++k) {
+            const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
+            if (w == group) mine = h;
             h = after(runs[w][lane], h);
         }
         state = h;
         return mine;
     }
-    Run all{one, 0}, before{one, 0};
+    Run all{twice(1.f), 0}, before{twice(1.f), 0};
 #pragma unroll
-    for (int k = 0; k < kWarps; ++k) {
-        const int w = kOrder > 0 ? k : kWarps - 1 - k;
-        if (w == warp) before = all;
+    for (int k = 0; k < Sh::kGroups; ++k) {
+        const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
+        if (w == group) before = all;
         const Run r = runs[w][lane];
         all = {mul2(r.p, all.p), after(r, all.l)};
     }
-    for (int to = warp; to < S; to += kWarps) put_remote(&blocks[rank][lane], to, all.p, all.l);
-    cluster_meet();
-    uint64_t h = state;
-    for (int k = 0; k < S; ++k) {
-        const int b = kOrder > 0 ? k : S - 1 - k;
-        if (b == (int)rank) tile_in = h;
-        h = after(blocks[b][lane], h);
+    const int buf = round & 1;
+    if (threadIdx.x < 32) {
+        if (threadIdx.x < Sh::kLanes) x.mine[buf][lane] = all;
+        fence_async_smem();
+        if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
+        __syncwarp();
+        if (threadIdx.x < S)
+            asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                             in_block(x.runs[buf][rank], threadIdx.x)),
+                         "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])),
+                         "r"(in_block(&x.bar[buf], threadIdx.x))
+                         : "memory");
     }
+    if (state != kLost && !wait(&x.bar[buf], (round >> 1) & 1)) state = kLost;
+    uint64_t h = state, tile_in = 0;
+    for (int k0 = 0; k0 < S; k0 += 2) {  // (S is even)
+        Run r[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) r[k] = x.runs[buf][kOrder > 0 ? k0 + k : S - 1 - k0 - k][lane];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if ((kOrder > 0 ? k0 + k : S - 1 - k0 - k) == (int)rank) tile_in = h;
+            h = after(r[k], h);
+        }
+    }
+    if (state == kLost) return kLost;
     state = h;
     return after(before, tile_in);
 }
-
 // ------------------------------------------------------------------------------------------------
 // forward
 // ------------------------------------------------------------------------------------------------
 
-template <typename T>
-struct Fwd {
-    static constexpr int kTokens = sizeof(T) == 2 ? 8 : 4;  // of a warp: 24 registers of loads in flight
-    static constexpr int kWarps = 8, kSpan = kWarps * kTokens;
-    static_assert(kSpan % kTile == 0, "a mark is before a warp's tokens");
-};
+template <typename T, int kLanes>
+using FwdShape = Shape<kLanes, sizeof(T) == 2 ? 8 : 4>;
 
-template <typename T, bool kVec>
-__global__ void __launch_bounds__(256) glr_forward_kernel(Glr p, int slabs, int S) {
-    constexpr int kTok = Fwd<T>::kTokens, kWarps = Fwd<T>::kWarps, kSpan = Fwd<T>::kSpan;
-    __shared__ Run runs[2][kWarps][32];
-    __shared__ Run blocks[2][kMaxCluster][32];
+template <typename T, int kLanes, bool kRing>
+__global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int slabs, int S, bool y_pairs) {
+    using Sh = FwdShape<T, kLanes>;
+    constexpr int kTok = Sh::kTok;
+    extern __shared__ __align__(128) char ring[];
+    __shared__ Run runs[2][Sh::kGroups][kLanes];
+    __shared__ Exchange<kLanes> others;
     let_next_begin();
     after_previous();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = Sh::group(), lane = Sh::lane();
     const unsigned rank = S > 1 ? cluster_rank() : 0, unit = blockIdx.x / S;
-    const int b = unit / slabs, slab = unit - b * slabs;
-    const Lane<kVec> at(slab, p.C);
+    const int b = unit / slabs;
+    const uint32_t channel = (unit - b * slabs) * Sh::kChannels;
+    const Lane at(channel, lane, p.C);
+    const bool pairs = p.C % 2 == 0;
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.n) : p.n;
-    const Decay decay(at.get(p.decay));
-    uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C) : 0;
     const size_t row0 = (size_t)b * p.n;
-    const T *x = static_cast<const T *>(p.x) + row0 * p.x_stride, *r = static_cast<const T *>(p.r) + row0 * p.r_stride,
-            *g = static_cast<const T *>(p.g) + row0 * p.g_stride;
+    const int step = S * Sh::kSpan;
+    Tokens<T, Sh, 3, kSlotsFwd, kRing> in;
+    in.set(0, p.x, p.x_stride, row0, channel);
+    in.set(1, p.r, p.r_stride, row0, channel);
+    in.set(2, p.g, p.g_stride, row0, channel);
+    in.open(ring, channel, p.C, len);
+    int t0 = rank * Sh::kSpan + group * kTok;
+    in.begin(t0, step, at);
+    const Decay decay(at.get(p.decay, pairs));
+    uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C, pairs) : 0;
     T *y = static_cast<T *>(p.y) + row0 * p.y_stride;
-
-    Raw<T, 2> rx[kTok], rr[kTok], rg[kTok];
-    auto load = [&](int t0) {
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            const bool on = t0 + u < len;
-            rx[u] = at.load(x + (size_t)(t0 + u) * p.x_stride, on);
-            rr[u] = at.load(r + (size_t)(t0 + u) * p.r_stride, on);
-            rg[u] = at.load(g + (size_t)(t0 + u) * p.g_stride, on);
-        }
-    };
-    int t0 = rank * kSpan + warp * kTok;
-    load(t0);
-    if (S > 1) cluster_meet();  // every block is there before its shared memory is written
-    const int rounds = (int)(((long long)p.n + (long long)S * kSpan - 1) / ((long long)S * kSpan));
-    for (int round = 0; round < rounds; ++round, t0 += S * kSpan) {
+    open_exchange(others, S);
+    const int rounds = (int)(((long long)p.n + step - 1) / step);
+    for (int round = 0, slot = 0; round < rounds; ++round, t0 += step) {
         uint64_t h[kTok], pr[kTok];  // this warp's states from 0, and the products of decays
+        in.next(slot, t0, step, at);
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             uint64_t a, w;
-            const uint64_t s = each(one_plus_exp(as_pair(rr[u])), rcp);
-            decay_of(decay, s, a, w);
-            const uint64_t d = one_plus_exp(as_pair(rg[u]));
+            Raw<T, 2> rr = in.get(slot, 1, u);
+            if (t0 + u >= len) shut(rr);  // (x is 0 there)
+            decay_of(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
+            const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
             // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-            const uint64_t in = mul2(mul2(w, each(mul2(mul2(d, d), w), rsqrt_of)), as_pair(rx[u]));
-            const bool on = t0 + u < len;
-            if (!on) a = twice(1.f);
-            h[u] = u ? fma2(a, h[u - 1], on ? in : 0) : on ? in : 0;
+            const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
+            h[u] = u ? fma2(a, h[u - 1], add) : add;
             pr[u] = u ? mul2(a, pr[u - 1]) : a;
         }
-        if (round + 1 < rounds) load(t0 + S * kSpan);
+        in.used(t0, step, at);
+        if (++slot == kSlotsFwd) slot = 0;
         const int buf = round & 1;
-        runs[buf][warp][lane] = {pr[kTok - 1], h[kTok - 1]};
-        uint64_t tile_in;
-        const uint64_t before = join<kWarps, 1>(runs[buf], blocks[buf], S, rank, state, tile_in);
-        if (p.marks && t0 % kTile == 0 && t0 < p.n)
-            at.put(p.marks + ((size_t)b * glr_marks(p.n) + t0 / kTile) * p.C, before);
+        runs[buf][group][lane] = {pr[kTok - 1], h[kTok - 1]};
+        const uint64_t before = join<Sh, 1>(runs[buf], others, round, S, rank, group, state);
+        if (p.marks && t0 % kGlrTile == 0 && t0 < p.n)
+            at.put(p.marks + ((size_t)b * glr_marks(p.n) + t0 / kGlrTile) * p.C, before, pairs);
+        T *to = y + (size_t)t0 * p.y_stride;
+        if (t0 + kTok <= len && y_pairs) {
 #pragma unroll
-        for (int u = 0; u < kTok; ++u)
-            if (t0 + u < p.n)
-                at.put(y + (size_t)(t0 + u) * p.y_stride, t0 + u < len ? fma2(pr[u], before, h[u]) : 0);
+            for (int u = 0; u < kTok; ++u, to += p.y_stride) at.put(to, fma2(pr[u], before, h[u]), true);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kTok; ++u, to += p.y_stride)
+                if (t0 + u < p.n) at.put(to, t0 + u < len ? fma2(pr[u], before, h[u]) : 0, y_pairs);
+        }
     }
-    if (p.state_out && rank == 0 && warp == 0) at.put(p.state_out + (size_t)b * p.C, state);
+    if (p.state_out && rank == 0 && group == 0) at.put(p.state_out + (size_t)b * p.C, state, pairs);
+    ring_wait<0>();
+    if (S > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
 }
 
 // ------------------------------------------------------------------------------------------------
 // one token
 // ------------------------------------------------------------------------------------------------
 
-template <typename T, bool kVec>
-__global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs) {
+template <typename T>
+__global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool rows_pairs) {
     let_next_begin();
     after_previous();
     const long long unit = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (unit >= (long long)p.B * slabs) return;
     const int b = (int)(unit / slabs);
-    const Lane<kVec> at((int)(unit - (long long)b * slabs), p.C);
-    const uint64_t x = at.get(static_cast<const T *>(p.x) + (size_t)b * p.x_stride),
-                   r = at.get(static_cast<const T *>(p.r) + (size_t)b * p.r_stride),
-                   g = at.get(static_cast<const T *>(p.g) + (size_t)b * p.g_stride),
-                   h = at.get(p.state_in + (size_t)b * p.C);
-    const Decay decay(at.get(p.decay));
+    const Lane at((uint32_t)(unit - (long long)b * slabs) * 64, threadIdx.x & 31, p.C);
+    const bool pairs = p.C % 2 == 0;
+    const uint64_t x = at.get(static_cast<const T *>(p.x) + (size_t)b * p.x_stride, rows_pairs),
+                   r = at.get(static_cast<const T *>(p.r) + (size_t)b * p.r_stride, rows_pairs),
+                   g = at.get(static_cast<const T *>(p.g) + (size_t)b * p.g_stride, rows_pairs),
+                   h = at.get(p.state_in + (size_t)b * p.C, pairs);
+    const Decay decay(at.get(p.decay, pairs));
     uint64_t a, w;
     decay_of(decay, each(one_plus_exp(r), rcp), a, w);
     const uint64_t d = one_plus_exp(g);
-    const uint64_t in = mul2(mul2(w, each(mul2(mul2(d, d), w), rsqrt_of)), x), y = fma2(a, h, in);
-    at.put(p.state_out + (size_t)b * p.C, y);
-    at.put(static_cast<T *>(p.y) + (size_t)b * p.y_stride, y);
+    const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), x), y = fma2(a, h, add);
+    at.put(p.state_out + (size_t)b * p.C, y, pairs);
+    at.put(static_cast<T *>(p.y) + (size_t)b * p.y_stride, y, rows_pairs);
 }
 
 // ------------------------------------------------------------------------------------------------
 // gradient
 // ------------------------------------------------------------------------------------------------
 
-constexpr int kTokBwd = 4, kWarpsBwd = 8;
-static_assert(kTokBwd * kWarpsBwd == kTile, "a block's tile of the gradient begins at a mark");
-
-template <typename T, bool kVec>
-__global__ void __launch_bounds__(256) glr_backward_kernel(GlrBwd p, int slabs, int S) {
-    constexpr int kTok = kTokBwd, kWarps = kWarpsBwd;
-    __shared__ Run fwd[2][kWarps][32], bwd[2][kWarps][32];
-    __shared__ Run blocks[2][kMaxCluster][32];
+template <typename T, int kLanes, bool kRing>
+__global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int slabs, int S, bool out_pairs) {
+    using Sh = Shape<kLanes, 4>;
+    constexpr int kTok = Sh::kTok;
+    extern __shared__ __align__(128) char ring[];
+    __shared__ Run fwd[2][Sh::kGroups][kLanes], bwd[2][Sh::kGroups][kLanes];
+    __shared__ Exchange<kLanes> others;
     let_next_begin();
     after_previous();
     const Glr &f = p.f;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int group = Sh::group(), lane = Sh::lane();
     const unsigned rank = S > 1 ? cluster_rank() : 0, unit = blockIdx.x / S;
-    const int b = unit / slabs, slab = unit - b * slabs;
-    const Lane<kVec> at(slab, f.C);
+    const int b = unit / slabs;
+    const uint32_t channel = (unit - b * slabs) * Sh::kChannels;
+    const Lane at(channel, lane, f.C);
+    const bool pairs = f.C % 2 == 0;
     const int len = f.lengths ? min(max(f.lengths[b], 0), f.n) : f.n;
-    const uint64_t dec = at.get(f.decay);
-    const Decay decay(dec);
-    uint64_t D = p.dstate_out ? at.get(p.dstate_out + (size_t)b * f.C) : 0;  // the gradient of the state behind the round
     const size_t row0 = (size_t)b * f.n;
-    const T *x = static_cast<const T *>(f.x) + row0 * f.x_stride, *r = static_cast<const T *>(f.r) + row0 * f.r_stride,
-            *g = static_cast<const T *>(f.g) + row0 * f.g_stride,
-            *dy = static_cast<const T *>(p.dy) + row0 * p.dy_stride;
+    const int step = -S * Sh::kSpan, rounds = (int)(((long long)f.n - step - 1) / -step);
+    Tokens<T, Sh, 4, kSlotsBwd, kRing> in;
+    in.set(0, f.x, f.x_stride, row0, channel);
+    in.set(1, f.r, f.r_stride, row0, channel);
+    in.set(2, f.g, f.g_stride, row0, channel);
+    in.set(3, p.dy, p.dy_stride, row0, channel);
+    in.open(ring, channel, f.C, len);
+    int tile = ((rounds - 1) * S + rank) * Sh::kSpan, t0 = tile + group * kTok;
+    in.begin(t0, step, at);
+    const uint64_t dec = at.get(f.decay, pairs);
+    const Decay decay(dec);
+    uint64_t D = p.dstate_out ? at.get(p.dstate_out + (size_t)b * f.C, pairs) : 0;  // the gradient of the state behind the round
     T *dx = static_cast<T *>(p.dx) + row0 * p.dx_stride, *dr = static_cast<T *>(p.dr) + row0 * p.dr_stride,
       *dg = static_cast<T *>(p.dg) + row0 * p.dg_stride;
-    const int marks = glr_marks(f.n);
-    const float *mark = f.marks + (size_t)b * marks * f.C;
-
-    Raw<T, 2> rx[kTok], rr[kTok], rg[kTok], rd[kTok];
-    uint64_t first = 0;  // the state before the tile
-    auto load = [&](int t0) {
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            const bool on = t0 + u < len;
-            rx[u] = at.load(x + (size_t)(t0 + u) * f.x_stride, on);
-            rr[u] = at.load(r + (size_t)(t0 + u) * f.r_stride, on);
-            rg[u] = at.load(g + (size_t)(t0 + u) * f.g_stride, on);
-            rd[u] = at.load(dy + (size_t)(t0 + u) * p.dy_stride, on);
-        }
-        if (t0 / kTile < marks) first = at.get(mark + (size_t)(t0 / kTile) * f.C);
+    const float *mark = f.marks + (size_t)b * glr_marks(f.n) * f.C;
+    auto state_before = [&](int t) {
+        return (unsigned)t < (unsigned)f.n ? at.get(mark + (size_t)(t / kGlrTile) * f.C, pairs) : 0;
     };
-    const int rounds = (marks + S - 1) / S;
-    int t0 = ((rounds - 1) * S + rank) * kTile + warp * kTok;
-    load(t0);
-    if (S > 1) cluster_meet();  // every block is there before its shared memory is written
+    uint64_t first = state_before(tile);  // the state before the tile
+    open_exchange(others, S);
+    const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
-    for (int round = rounds - 1; round >= 0; --round, t0 -= S * kTile) {
-        uint64_t a[kTok], s[kTok], m[kTok], in[kTok], vx[kTok], vd[kTok];
-        Run forward{twice(1.f), 0};
+    for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
+        uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok], vd[kTok];  // 1 - i, b, i x / m
+        Run forward{0, 0};
+        in.next(slot, t0, step, at);
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             uint64_t w;
-            s[u] = each(one_plus_exp(as_pair(rr[u])), rcp);
+            Raw<T, 2> rr = in.get(slot, 1, u);
+            if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
+            s[u] = each(one_plus_exp(as_pair(rr)), rcp);
             decay_of(decay, s[u], a[u], w);
-            m[u] = mul2(w, each(w, rsqrt_of));
-            in[u] = each(one_plus_exp(as_pair(rg[u])), rcp);
-            vx[u] = as_pair(rx[u]);
-            vd[u] = as_pair(rd[u]);
-            if (t0 + u >= len) a[u] = twice(1.f);  // (x and dy are 0 there)
-            forward = {mul2(a[u], forward.p), fma2(a[u], forward.l, mul2(mul2(m[u], in[u]), vx[u]))};
+            const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, u))), rcp);
+            const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, u)));
+            mi[u] = mul2(m, i);
+            rest[u] = fma2(i, minus, twice(1.f));
+            add[u] = mul2(m, ix);
+            over[u] = mul2(rm, ix);
+            vd[u] = as_pair(in.get(slot, 3, u));
+            forward = u ? Run{mul2(a[u], forward.p), fma2(a[u], forward.l, add[u])} : Run{a[u], add[u]};
         }
-        Run backward{forward.p, 0};
+        in.used(t0, step, at);
+        if (++slot == kSlotsBwd) slot = 0;
+        uint64_t back = mul2(a[kTok - 1], vd[kTok - 1]);
 #pragma unroll
-        for (int u = kTok - 1; u >= 0; --u) backward.l = mul2(a[u], add2(vd[u], backward.l));
+        for (int u = kTok - 2; u >= 0; --u) back = mul2(a[u], add2(vd[u], back));
         const int buf = round & 1;
-        fwd[buf][warp][lane] = forward;
-        bwd[buf][warp][lane] = backward;
-        uint64_t h = first, tile_in;
-        if (round > 0) load(t0 - S * kTile);
-        uint64_t later = join<kWarps, -1>(bwd[buf], blocks[buf], S, rank, D, tile_in);
-#pragma unroll
-        for (int k = 0; k < kWarps - 1; ++k)
-            if (k < warp) h = after(fwd[buf][k][lane], h);
-        uint64_t hb[kTok];  // the states before each token
+        fwd[buf][group][lane] = forward;
+        bwd[buf][group][lane] = {forward.p, back};
+        uint64_t h = first;
+        first = state_before(tile + step);
+        uint64_t later = join<Sh, -1>(bwd[buf], others, round, S, rank, group, D);
+        for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);
+        uint64_t e[kTok];  // the derivative of the state by log a
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
-            hb[u] = h;
-            h = fma2(a[u], h, mul2(mul2(m[u], in[u]), vx[u]));
+            h = fma2(a[u], h, add[u]);
+            e[u] = fma2(over[u], minus, h);
         }
-#pragma unroll
-        for (int u = kTok - 1; u >= 0; --u) {
+        const size_t end = (size_t)(t0 + kTok - 1);
+        T *px = dx + end * p.dx_stride, *pr = dr + end * p.dr_stride, *pg = dg + end * p.dg_stride;
+        auto put = [&](int u, bool on, bool as_pairs) {
             const uint64_t G = add2(vd[u], later);
             later = mul2(a[u], G);
-            if (t0 + u < f.n) {
-                const bool on = t0 + u < len;
-                const uint64_t minus = twice(-1.f);
-                const uint64_t vdx = mul2(G, mul2(m[u], in[u]));
-                const uint64_t vdg = mul2(mul2(vdx, vx[u]), fma2(in[u], minus, twice(1.f)));
-                const uint64_t inv = fma2(m[u], minus, each(m[u], rcp));
-                const uint64_t e = mul2(G, fma2(mul2(mul2(in[u], vx[u]), minus), inv, mul2(a[u], hb[u])));
-                const uint64_t es = mul2(e, s[u]);
-                const uint64_t vdr = mul2(mul2(es, dec), fma2(s[u], minus, twice(1.f)));
-                if (on) dsum = add2(dsum, es);
-                at.put(dx + (size_t)(t0 + u) * p.dx_stride, on ? vdx : 0);
-                at.put(dr + (size_t)(t0 + u) * p.dr_stride, on ? vdr : 0);
-                at.put(dg + (size_t)(t0 + u) * p.dg_stride, on ? vdg : 0);
-            }
+            const uint64_t es = mul2(mul2(G, e[u]), s[u]);
+            if (on) dsum = add2(dsum, es);
+            at.put(px, on ? mul2(G, mi[u]) : 0, as_pairs);
+            at.put(pg, on ? mul2(mul2(G, add[u]), rest[u]) : 0, as_pairs);
+            at.put(pr, on ? mul2(es, fma2(mul2(s[u], dec), minus, dec)) : 0, as_pairs);
+        };
+        if (t0 + kTok <= len && out_pairs) {
+#pragma unroll
+            for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride) put(u, true, true);
+        } else {
+#pragma unroll
+            for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride)
+                if (t0 + u < f.n) put(u, t0 + u < len, out_pairs);
         }
     }
-    if (p.dstate_in && rank == 0 && warp == 0) at.put(p.dstate_in + (size_t)b * f.C, D);
-    // decay's gradient: the block's warps in order, then (another kernel) its blocks
+    if (p.dstate_in && rank == 0 && group == 0) at.put(p.dstate_in + (size_t)b * f.C, D, pairs);
+    // decay's gradient: the block's groups in order, then (another kernel) its blocks
     __syncthreads();
-    fwd[0][warp][lane].p = dsum;
+    fwd[0][group][lane].p = dsum;
     __syncthreads();
-    if (warp == 0) {
+    if (group == 0) {
 #pragma unroll
-        for (int k = 1; k < kWarps; ++k) dsum = add2(dsum, fwd[0][k][lane].p);
-        at.put(p.partial + ((size_t)b * S + rank) * f.C, dsum);
+        for (int k = 1; k < Sh::kGroups; ++k) dsum = add2(dsum, fwd[0][k][lane].p);
+        at.put(p.partial + ((size_t)b * S + rank) * f.C, dsum, pairs);
     }
+    ring_wait<0>();
+    if (S > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
 }
 
-// blocks of one sequence: as many as fill the GPU, each with a tile to work on
-int cluster_of(long long units, int n, int span, int want) {
-    int S = 1;
-    while (S < kMaxCluster && units * S * 2 <= want && (long long)S * span < n) S *= 2;
-    return S;
+// How a call is spread: lanes for a token's channels, and blocks of one sequence
+struct Spread {
+    int lanes, slabs, S;
+};
+// As many blocks as two an SM, up to eight for a sequence; where that leaves half of the SMs' room, blocks take half the
+// channels; where few clusters are left even so, they are of sixteen blocks (the GPU holds 36 clusters of
+// eight, 14 of sixteen, at two blocks an SM).  A sequence is not given more blocks than it has tiles.
+Spread spread(int B, int n, int C, int tok) {
+    auto units = [&](int lanes) { return (long long)B * ((C + 2 * lanes - 1) / (2 * lanes)); };
+    const int span = 8 * tok;
+    Spread r{32, 0, 1};
+    while (r.S < 8 && units(32) * r.S * 2 <= 2 * kSMs && (long long)r.S * span < n) r.S *= 2;
+    if ((r.S == 8 && units(16) <= 36) || C <= 32) r.lanes = 16;
+    if (r.S == 8 && units(16) <= 14 && 8LL * 2 * span < n) r.S = 16;
+    r.slabs = (C + 2 * r.lanes - 1) / (2 * r.lanes);
+    return r;
 }
-int bwd_cluster(int B, int n, int C) { return cluster_of((long long)B * ((C + kChannels - 1) / kChannels), n, kTile, 608); }
+Spread spread_bwd(int B, int n, int C) { return spread(B, n, C, 4); }
 
 template <typename T>
 bool pairs_ok(const void *p, long long stride, int C) {
     return C % 2 == 0 && rows_aligned(p, stride, sizeof(T), 2 * sizeof(T));
 }
+template <typename T>
+bool ring_ok(const void *p, long long stride) {
+    return rows_aligned(p, stride, sizeof(T), 16);
+}
 
-template <typename T, bool kVec>
-cudaError_t forward_as(const Glr &p, cudaStream_t s) {
-    const int slabs = (p.C + kChannels - 1) / kChannels;
-    const int S = cluster_of((long long)p.B * slabs, p.n, Fwd<T>::kSpan, 608);
-    return launch_cluster_after(glr_forward_kernel<T, kVec>, (unsigned)((long long)p.B * slabs * S), 256, S, 0, s, p, slabs, S);
+template <typename... P, typename... A>
+cudaError_t launch_clusters(void (*kernel)(P...), long long units, int S, int smem, cudaStream_t s, A... args) {
+    cudaError_t e = cudaSuccess;
+    if (smem > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (!e && S > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e ? e : launch_cluster_after(kernel, (unsigned)(units * S), kThreads, S, smem, s, args...);
+}
+
+template <typename T, int kLanes, bool kRing>
+cudaError_t forward_as(const Glr &p, const Spread &r, cudaStream_t s) {
+    return launch_clusters(glr_forward_kernel<T, kLanes, kRing>, (long long)p.B * r.slabs, r.S,
+                           Tokens<T, FwdShape<T, kLanes>, 3, kSlotsFwd, kRing>::kSmem, s, p, r.slabs, r.S,
+                           pairs_ok<T>(p.y, p.y_stride, p.C));
 }
 template <typename T>
 cudaError_t forward_of(const Glr &p, cudaStream_t s) {
-    return pairs_ok<T>(p.x, p.x_stride, p.C) && pairs_ok<T>(p.r, p.r_stride, p.C) && pairs_ok<T>(p.g, p.g_stride, p.C) &&
-                   pairs_ok<T>(p.y, p.y_stride, p.C)
-               ? forward_as<T, true>(p, s)
-               : forward_as<T, false>(p, s);
+    const Spread r = spread(p.B, p.n, p.C, FwdShape<T, 32>::kTok);
+    if (ring_ok<T>(p.x, p.x_stride) && ring_ok<T>(p.r, p.r_stride) && ring_ok<T>(p.g, p.g_stride))
+        return r.lanes == 32 ? forward_as<T, 32, true>(p, r, s) : forward_as<T, 16, true>(p, r, s);
+    return r.lanes == 32 ? forward_as<T, 32, false>(p, r, s) : forward_as<T, 16, false>(p, r, s);
 }
 
-template <typename T, bool kVec>
-cudaError_t step_as(const Glr &p, cudaStream_t s) {
-    const int slabs = (p.C + kChannels - 1) / kChannels;
-    return launch_after(glr_step_kernel<T, kVec>, (unsigned)(((long long)p.B * slabs + 3) / 4), 128, 0, s, p, slabs);
-}
 template <typename T>
 cudaError_t step_of(const Glr &p, cudaStream_t s) {
-    return pairs_ok<T>(p.x, p.x_stride, p.C) && pairs_ok<T>(p.r, p.r_stride, p.C) && pairs_ok<T>(p.g, p.g_stride, p.C) &&
-                   pairs_ok<T>(p.y, p.y_stride, p.C)
-               ? step_as<T, true>(p, s)
-               : step_as<T, false>(p, s);
+    const int slabs = (p.C + 63) / 64;
+    const bool pairs = pairs_ok<T>(p.x, p.x_stride, p.C) && pairs_ok<T>(p.r, p.r_stride, p.C) &&
+                       pairs_ok<T>(p.g, p.g_stride, p.C) && pairs_ok<T>(p.y, p.y_stride, p.C);
+    return launch_after(glr_step_kernel<T>, (unsigned)(((long long)p.B * slabs + 3) / 4), 128, 0, s, p, slabs, pairs);
 }
 
-template <typename T, bool kVec>
-cudaError_t backward_as(const GlrBwd &p, cudaStream_t s) {
+template <typename T, int kLanes, bool kRing>
+cudaError_t backward_as(const GlrBwd &p, const Spread &r, cudaStream_t s) {
     const Glr &f = p.f;
-    const int slabs = (f.C + kChannels - 1) / kChannels, S = bwd_cluster(f.B, f.n, f.C);
-    cudaError_t e = launch_cluster_after(glr_backward_kernel<T, kVec>, (unsigned)((long long)f.B * slabs * S), 256, S, 0, s, p,
-                                         slabs, S);
+    const bool pairs = pairs_ok<T>(p.dx, p.dx_stride, f.C) && pairs_ok<T>(p.dr, p.dr_stride, f.C) &&
+                       pairs_ok<T>(p.dg, p.dg_stride, f.C);
+    const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kRing>, (long long)f.B * r.slabs, r.S,
+                                          Tokens<T, Shape<kLanes, 4>, 4, kSlotsBwd, kRing>::kSmem, s, p, r.slabs, r.S, pairs);
     if (e) return e;
-    return column_sum_launch({p.partial, (long long)f.B * S, f.C, 1, {p.ddecay}, p.header}, s);
+    return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {p.ddecay}, p.header}, s);
 }
 template <typename T>
 cudaError_t backward_of(const GlrBwd &p, cudaStream_t s) {
     const Glr &f = p.f;
-    const bool vec = pairs_ok<T>(f.x, f.x_stride, f.C) && pairs_ok<T>(f.r, f.r_stride, f.C) &&
-                     pairs_ok<T>(f.g, f.g_stride, f.C) && pairs_ok<T>(p.dy, p.dy_stride, f.C) &&
-                     pairs_ok<T>(p.dx, p.dx_stride, f.C) && pairs_ok<T>(p.dr, p.dr_stride, f.C) &&
-                     pairs_ok<T>(p.dg, p.dg_stride, f.C);
-    return vec ? backward_as<T, true>(p, s) : backward_as<T, false>(p, s);
+    const Spread r = spread_bwd(f.B, f.n, f.C);
+    if (ring_ok<T>(f.x, f.x_stride) && ring_ok<T>(f.r, f.r_stride) && ring_ok<T>(f.g, f.g_stride) &&
+        ring_ok<T>(p.dy, p.dy_stride))
+        return r.lanes == 32 ? backward_as<T, 32, true>(p, r, s) : backward_as<T, 16, true>(p, r, s);
+    return r.lanes == 32 ? backward_as<T, 32, false>(p, r, s) : backward_as<T, 16, false>(p, r, s);
 }
 
 }  // namespace
 
-bool glr_fits(int B, int C) { return (long long)B * ((C + kChannels - 1) / kChannels) <= (1LL << 27); }
+bool glr_fits(int B, int C) { return (long long)B * ((C + 31) / 32) <= (1LL << 27); }
 cudaError_t glr_forward_launch(const Glr &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? forward_of<__nv_bfloat16>(p, s) : forward_of<float>(p, s);
 }
 cudaError_t glr_step_launch(const Glr &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? step_of<__nv_bfloat16>(p, s) : step_of<float>(p, s);
 }
-size_t glr_backward_partial_floats(int B, int n, int C) { return (size_t)B * bwd_cluster(B, n, C) * C; }
+size_t glr_backward_partial_floats(int B, int n, int C) { return (size_t)B * spread_bwd(B, n, C).S * C; }
 cudaError_t glr_backward_launch(const GlrBwd &p, cudaStream_t s) {
     return p.f.dt == HLA_BF16 ? backward_of<__nv_bfloat16>(p, s) : backward_of<float>(p, s);
 }
