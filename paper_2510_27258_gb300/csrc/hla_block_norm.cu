@@ -7,13 +7,13 @@
 // the same bits, none are stored.  Backwards, with t the gradient of x':
 //   t = dx' + r2 (dh w_pre - x' r2 mean(dh w_pre x' r2)),  dx = alpha t,  q = t k act(gate),
 //   dy = r1 (q scale w_post - u mean(q scale w_post u)),  dgate = t k scale u w_post act'(gate),
-//   dw_post = sum q scale u,  dscale = sum q u w_post,  dw_pre = sum dh x' r2.
+//   dw_post = scale sum q u,  dscale = w_post sum q u,  dw_pre = sum dh x' r2   (sums over rows).
 //
 // Bound by memory traffic: every tensor is read and written once.  A row belongs to a block (up to 256 columns: to a
 // warp), eight columns a thread in registers, with the block's next row in flight; blocks stay for many rows, so
-// that the weights are loaded once and the gradient's sums over rows stay in registers.  Rows of more than
-// 8192 columns are walked several times by one block.  Statistics, products and sums are fp32; each output is
-// rounded once.
+// that the weights are loaded once and the gradient's sums over rows stay in registers.  What does not depend on a
+// row's sum (gate, random bits) is done while the sum's barrier is waited for.  Rows of more than 8192 columns are
+// walked several times by one block.  Statistics, products and sums are fp32; each output is rounded once.
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -24,6 +24,7 @@ namespace {
 constexpr int kPer = 8;                        // columns of a thread
 constexpr int kNarrow = 32 * kPer, kWide = 1024 * kPer;
 constexpr int kMaxWarps = 32, kNarrowRows = 4;
+constexpr int kFwdThreads = 512, kBwdThreads = 512;  // threads of an SM at a time
 
 struct Words {
     uint32_t w[4];
@@ -44,22 +45,11 @@ __device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint64_t offse
     return {{c0, c1, c2, c3}};
 }
 
-// a bit for each of kV columns from `col` on: kept
-template <int kV>
-__device__ __forceinline__ uint32_t kept(const BlockNorm &p, long long row, int col) {
-    uint32_t bits = 0;
-    if (kV == 1) {
-        const Words r = philox((uint32_t)(col >> 2), (uint32_t)row, p.offset, p.seed);
-        const uint32_t w = (col & 2) ? ((col & 1) ? r.w[3] : r.w[2]) : ((col & 1) ? r.w[1] : r.w[0]);
-        return w >= p.drop_below;
-    }
-#pragma unroll
-    for (int j = 0; j < kV; j += 4) {
-        const Words r = philox((uint32_t)((col + j) >> 2), (uint32_t)row, p.offset, p.seed);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bits |= (r.w[i] >= p.drop_below ? 1u : 0u) << (j + i);
-    }
-    return bits;
+// whether one value is kept
+__device__ __forceinline__ bool kept(const BlockNorm &p, long long row, int col) {
+    const Words r = philox((uint32_t)(col >> 2), (uint32_t)row, p.offset, p.seed);
+    const uint32_t w = (col & 2) ? ((col & 1) ? r.w[3] : r.w[2]) : ((col & 1) ? r.w[1] : r.w[0]);
+    return w >= p.drop_below;
 }
 
 // act(v) and, if asked, its slope
@@ -78,6 +68,40 @@ __device__ __forceinline__ float activation(int act, float v, float &slope) {
     return v * s;
 }
 
+constexpr int kPairs = kPer / 2;
+using Pairs = uint64_t[kPairs];
+
+__device__ __forceinline__ uint64_t twice(float x) { return pair(x, x); }
+
+// the same of a thread's columns, two at a time
+template <bool kSlope>
+__device__ __forceinline__ void activate(int act, Pairs &v, Pairs &slope) {
+    if (act == HLA_LINEAR) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) slope[i] = twice(1.f);
+        return;
+    }
+    const uint64_t one = twice(1.f), minus = twice(-1.f);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        float a, b;
+        unpair(mul2(v[i], twice(-1.44269504f)), a, b);
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(a));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(b));
+        unpair(add2(pair(a, b), one), a, b);
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(a));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(b));
+        const uint64_t s = pair(a, b), r = fma2(s, minus, one);
+        if (act == HLA_SIGMOID) {
+            if (kSlope) slope[i] = mul2(s, r);
+            v[i] = s;
+        } else {
+            if (kSlope) slope[i] = mul2(s, fma2(v[i], r, one));
+            v[i] = mul2(v[i], s);
+        }
+    }
+}
+
 // A thread's eight columns: kE accesses of kV neighbours, `threads` apart
 template <typename T, int kV>
 struct Cols {
@@ -91,38 +115,65 @@ struct Cols {
             r[e] = c < C ? raw_load<T, kV>(row + c) : raw_zero<T, kV>();
         }
     }
-    __device__ __forceinline__ void get(float (&v)[kPer]) const {
+    __device__ __forceinline__ void get(Pairs &v) const {
         if constexpr (kV == 1) {
 #pragma unroll
-            for (int e = 0; e < kE; ++e) v[e] = to_f32(r[e].v[0]);
+            for (int i = 0; i < kPairs; ++i) v[i] = pair(to_f32(r[2 * i].v[0]), to_f32(r[2 * i + 1].v[0]));
         } else {
 #pragma unroll
             for (int e = 0; e < kE; ++e) {
                 uint64_t f[kV / 2];
                 to_pairs(r[e], f);
 #pragma unroll
-                for (int i = 0; i < kV / 2; ++i) unpair(f[i], v[e * kV + 2 * i], v[e * kV + 2 * i + 1]);
+                for (int i = 0; i < kV / 2; ++i) v[e * kV / 2 + i] = f[i];
             }
         }
     }
-    static __device__ __forceinline__ void put(T *row, int t, int threads, int C, const float (&v)[kPer]) {
+    static __device__ __forceinline__ void put(T *row, int t, int threads, int C, const Pairs &v) {
+        float f[kPer];
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) unpair(v[i], f[2 * i], f[2 * i + 1]);
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
             const int c = at(e, t, threads);
-            float f[kV];
+            float o[kV];
 #pragma unroll
-            for (int i = 0; i < kV; ++i) f[i] = v[e * kV + i];
-            if (c < C) VecIo<T, kV>::store(row + c, f);
+            for (int i = 0; i < kV; ++i) o[i] = f[e * kV + i];
+            if (c < C) VecIo<T, kV>::store(row + c, o);
         }
+    }
+    // zeros in the places of dropped values
+    template <int kN>
+    static __device__ __forceinline__ void drop(const BlockNorm &p, long long row, int t, int threads, Pairs (&v)[kN]) {
+        bool keep[kPer];
+        if constexpr (kV == 1) {
+#pragma unroll
+            for (int e = 0; e < kE; ++e) keep[e] = kept(p, row, at(e, t, threads));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; j += 4) {
+                const Words w = philox((uint32_t)(at(j / kV, t, threads) + j % kV) >> 2, (uint32_t)row, p.offset, p.seed);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) keep[j + i] = w.w[i] >= p.drop_below;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                float a, b;
+                unpair(v[n][i], a, b);
+                v[n][i] = pair(keep[2 * i] ? a : 0.f, keep[2 * i + 1] ? b : 0.f);
+            }
     }
 };
 
 // a weight's eight columns, or ones
 template <typename T, int kV>
-__device__ __forceinline__ void weight(const void *w, int t, int threads, int C, float (&v)[kPer]) {
+__device__ __forceinline__ void weight(const void *w, int t, int threads, int C, Pairs &v) {
     if (!w) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = 1.f;
+        for (int i = 0; i < kPairs; ++i) v[i] = twice(1.f);
         return;
     }
     Cols<T, kV> c;
@@ -142,14 +193,23 @@ __device__ __forceinline__ void warp_sum(Sum<kN> &s) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) s.v[i] += __shfl_xor_sync(0xffffffffu, s.v[i], o);
 }
+__device__ __forceinline__ void add_up(uint64_t v, float &sum) {
+    float a, b;
+    unpair(v, a, b);
+    sum = a + b;
+}
+// tell: this warp's part; read: the row's sum, behind a barrier
 template <bool kBlock, int kN>
-__device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
+__device__ __forceinline__ void tell(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int turn) {
     warp_sum(s);
-    if (!kBlock) return;
-    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) == 0)
+    if (kBlock && (threadIdx.x & 31) == 0)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) red[turn][i][warp] = s.v[i];
+        for (int i = 0; i < kN; ++i) red[turn][i][threadIdx.x >> 5] = s.v[i];
+}
+template <bool kBlock, int kN>
+__device__ __forceinline__ void read(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
+    if (!kBlock) return;
+    const int warps = blockDim.x >> 5;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -161,6 +221,11 @@ __device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps
         s.v[i] = sum;
     }
     turn ^= 1;
+}
+template <bool kBlock, int kN>
+__device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
+    tell<kBlock>(s, red, turn);
+    read<kBlock>(s, red, turn);
 }
 
 __device__ __forceinline__ void clear(float (&red)[2][2][kMaxWarps]) {
@@ -175,7 +240,7 @@ __device__ __forceinline__ void clear(float (&red)[2][2][kMaxWarps]) {
 
 // kMax: the block's threads at most (0: a warp for each row)
 template <typename T, int kV, int kMax>
-__global__ void __launch_bounds__(kMax ? kMax : 128) block_norm_forward_kernel(BlockNorm p) {
+__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThreads / (kMax ? kMax : 128)) block_norm_forward_kernel(BlockNorm p) {
     constexpr bool kBlock = kMax > 0;
     __shared__ __align__(16) float red[2][2][kMaxWarps];
     let_next_begin();
@@ -185,12 +250,15 @@ __global__ void __launch_bounds__(kMax ? kMax : 128) block_norm_forward_kernel(B
     const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
     const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
     const float inv = 1.f / C;
-    float w_post[kPer], scale[kPer], w_pre[kPer];
-    weight<T, kV>(p.scale, t, threads, C, scale);
-    weight<T, kV>(p.w_post, t, threads, C, w_post);
-    weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+    Pairs scale, w_pre;  // (the first times w_post)
+    {
+        Pairs w_post;
+        weight<T, kV>(p.scale, t, threads, C, scale);
+        weight<T, kV>(p.w_post, t, threads, C, w_post);
+        weight<T, kV>(p.w_pre, t, threads, C, w_pre);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) scale[i] *= w_post[i] * p.keep_scale;
+        for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
+    }
     Cols<T, kV> cx, cy, cg;
     auto load = [&](long long row) {
         cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
@@ -200,38 +268,49 @@ __global__ void __launch_bounds__(kMax ? kMax : 128) block_norm_forward_kernel(B
     long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
     if (row < p.rows) load(row);
     for (; row < p.rows; row += step) {  // (all of a row's threads alike)
-        float x[kPer], y[kPer], g[kPer];
+        Pairs x, y, f[1];
         cx.get(x);
         cy.get(y);
-        if (p.gate) cg.get(g);
+        if (p.gate) cg.get(f[0]);
         if (row + step < p.rows) load(row + step);
+        Sum<1> s1;
+        if (p.post) {
+            uint64_t sum = mul2(y[0], y[0]);
+#pragma unroll
+            for (int i = 1; i < kPairs; ++i) sum = fma2(y[i], y[i], sum);
+            add_up(sum, s1.v[0]);
+            tell<kBlock>(s1, red, turn);
+        }
+        if (p.gate) {
+            Pairs slope;
+            activate<false>(p.act, f[0], slope);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) f[0][i] = mul2(f[0][i], scale[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) f[0][i] = scale[i];
+        }
+        if (p.drop) Cols<T, kV>::drop(p, row, t, threads, f);
         float r1 = 1.f;
         if (p.post) {
-            Sum<1> s{{0.f}};
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) s.v[0] += y[i] * y[i];
-            row_sum<kBlock>(s, red, turn);
-            r1 = rsqrtf(s.v[0] * inv + p.eps);
+            read<kBlock>(s1, red, turn);
+            r1 = rsqrtf(s1.v[0] * inv + p.eps);
         }
-        Sum<1> s2{{0.f}};
+        uint64_t sum = 0;
 #pragma unroll
-        for (int e = 0; e < kPer / kV; ++e) {
-            const uint32_t bits = p.drop ? kept<kV>(p, row, Cols<T, kV>::at(e, t, threads)) : ~0u;
-#pragma unroll
-            for (int j = 0; j < kV; ++j) {
-                const int i = e * kV + j;
-                float slope, f = y[i] * r1 * scale[i];
-                if (p.gate) f *= activation<false>(p.act, g[i], slope);
-                x[i] = p.alpha * x[i] + (bits >> j & 1 ? f : 0.f);
-                s2.v[0] += x[i] * x[i];
-            }
+        for (int i = 0; i < kPairs; ++i) {
+            x[i] = fma2(mul2(y[i], twice(r1)), f[0][i], mul2(x[i], twice(p.alpha)));
+            sum = fma2(x[i], x[i], sum);
         }
+        Sum<1> s2;
+        add_up(sum, s2.v[0]);
+        if (p.pre) tell<kBlock>(s2, red, turn);
         Cols<T, kV>::put(static_cast<T *>(p.x_out) + row * p.x_out_stride, t, threads, C, x);
         if (p.pre) {
-            row_sum<kBlock>(s2, red, turn);
+            read<kBlock>(s2, red, turn);
             const float r2 = rsqrtf(s2.v[0] * inv + p.eps);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) x[i] *= r2 * w_pre[i];
+            for (int i = 0; i < kPairs; ++i) x[i] = mul2(mul2(x[i], twice(r2)), w_pre[i]);
             Cols<T, kV>::put(static_cast<T *>(p.h) + row * p.h_stride, t, threads, C, x);
         }
     }
@@ -244,7 +323,7 @@ struct Wide {
     long long row;
     __device__ __forceinline__ static float of(const void *w, int c) { return w ? to_f32(static_cast<const T *>(w)[c]) : 1.f; }
     __device__ __forceinline__ float y(int c) const { return to_f32(static_cast<const T *>(p.y)[row * p.y_stride + c]); }
-    __device__ __forceinline__ float keep(int c) const { return !p.drop ? 1.f : kept<1>(p, row, c) ? p.keep_scale : 0.f; }
+    __device__ __forceinline__ float keep(int c) const { return !p.drop ? 1.f : kept(p, row, c) ? p.keep_scale : 0.f; }
     __device__ __forceinline__ float act(int c, float &slope) const {
         return p.gate ? activation<true>(p.act, to_f32(static_cast<const T *>(p.gate)[row * p.gate_stride + c]), slope)
                       : (slope = 0.f, 1.f);
@@ -302,10 +381,10 @@ __device__ __forceinline__ float grad_x_out(float dx_out, float gw, float x_out,
 }
 
 template <typename T, int kV, int kMax>
-__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 256 ? 2 : 1) block_norm_backward_kernel(BlockNormBwd q) {
+__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThreads / (kMax ? kMax : 128)) block_norm_backward_kernel(BlockNormBwd q) {
     constexpr bool kBlock = kMax > 0;
     __shared__ __align__(16) float red[2][2][kMaxWarps];
-    __shared__ float sums[kBlock ? 1 : 3 * kNarrow];
+    __shared__ float sums[kBlock ? 1 : 2 * kNarrow];
     let_next_begin();
     after_previous();
     const BlockNorm &p = q.f;
@@ -314,11 +393,16 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 256 ? 2 : 1) block_
     const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
     const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
     const float inv = 1.f / C;
-    float w_post[kPer], scale[kPer], w_pre[kPer];
-    weight<T, kV>(p.scale, t, threads, C, scale);
-    weight<T, kV>(p.w_post, t, threads, C, w_post);
-    weight<T, kV>(p.w_pre, t, threads, C, w_pre);
-    float dw_post[kPer] = {}, dscale[kPer] = {}, dw_pre[kPer] = {};
+    Pairs scale, w_pre;  // (the first times w_post)
+    {
+        Pairs w_post;
+        weight<T, kV>(p.scale, t, threads, C, scale);
+        weight<T, kV>(p.w_post, t, threads, C, w_post);
+        weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) scale[i] = mul2(scale[i], w_post[i]);
+    }
+    Pairs qu = {}, dw_pre = {};  // sums over this thread's rows
     Cols<T, kV> cx, cy, cg, cd, ch;
     auto load = [&](long long row) {
         cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
@@ -330,103 +414,119 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 256 ? 2 : 1) block_
     long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
     if (row < p.rows) load(row);
     for (; row < p.rows; row += step) {
-        float x[kPer], y[kPer], a[kPer], slope[kPer], d[kPer], h[kPer];
+        Pairs x, y, d, h, f[2];  // f: k act(gate), k act'(gate)
         cx.get(x);
         cy.get(y);
         cd.get(d);
-        if (p.gate) cg.get(a);
+        if (p.gate) cg.get(f[0]);
         if (p.pre) ch.get(h);
         if (row + step < p.rows) load(row + step);
+        Sum<1> s1;
+        if (p.post) {
+            uint64_t sum = mul2(y[0], y[0]);
+#pragma unroll
+            for (int i = 1; i < kPairs; ++i) sum = fma2(y[i], y[i], sum);
+            add_up(sum, s1.v[0]);
+            tell<kBlock>(s1, red, turn);
+        }
+        if (p.gate) {
+            activate<true>(p.act, f[0], f[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) f[0][i] = f[1][i] = twice(1.f);
+        }
+        if (p.drop) {
+            Cols<T, kV>::drop(p, row, t, threads, f);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                f[0][i] = mul2(f[0][i], twice(p.keep_scale));
+                f[1][i] = mul2(f[1][i], twice(p.keep_scale));
+            }
+        }
         float r1 = 1.f;
         if (p.post) {
-            Sum<1> s{{0.f}};
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) s.v[0] += y[i] * y[i];
-            row_sum<kBlock>(s, red, turn);
-            r1 = rsqrtf(s.v[0] * inv + p.eps);
-        }
-        uint32_t bits = ~0u;
-        if (p.drop) {
-            bits = 0;
-#pragma unroll
-            for (int e = 0; e < kPer / kV; ++e) bits |= kept<kV>(p, row, Cols<T, kV>::at(e, t, threads)) << (e * kV);
+            read<kBlock>(s1, red, turn);
+            r1 = rsqrtf(s1.v[0] * inv + p.eps);
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            y[i] *= r1;  // u
-            if (p.gate) {
-                a[i] = activation<true>(p.act, a[i], slope[i]);
-            } else {
-                a[i] = 1.f;
-            }
-        }
+        for (int i = 0; i < kPairs; ++i) y[i] = mul2(y[i], twice(r1));  // u
         if (p.pre) {
-            Sum<2> s{{0.f, 0.f}};
+            uint64_t sum = 0, dot = 0;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const float f = y[i] * w_post[i] * scale[i] * a[i] * p.keep_scale;
-                x[i] = p.alpha * x[i] + (bits >> i & 1 ? f : 0.f);  // x'
-                s.v[0] += x[i] * x[i];
-                s.v[1] += h[i] * w_pre[i] * x[i];
+            for (int i = 0; i < kPairs; ++i) {
+                x[i] = fma2(mul2(y[i], scale[i]), f[0][i], mul2(x[i], twice(p.alpha)));  // x'
+                sum = fma2(x[i], x[i], sum);
+                dot = fma2(mul2(h[i], w_pre[i]), x[i], dot);
             }
-            row_sum<kBlock>(s, red, turn);
-            const float r2 = rsqrtf(s.v[0] * inv + p.eps), m2 = s.v[1] * r2 * inv;
+            Sum<2> s2;
+            add_up(sum, s2.v[0]);
+            add_up(dot, s2.v[1]);
+            row_sum<kBlock>(s2, red, turn);
+            const float r2 = rsqrtf(s2.v[0] * inv + p.eps), m2 = s2.v[1] * r2 * inv;
+            // t = dx' + r2 (dh w_pre - x' r2 m2)
+            const uint64_t by = twice(-r2 * r2 * m2);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                d[i] = grad_x_out(d[i], h[i] * w_pre[i], x[i], r2, m2);  // t
-                dw_pre[i] += h[i] * x[i] * r2;
+            for (int i = 0; i < kPairs; ++i) {
+                const uint64_t hr = mul2(h[i], twice(r2));
+                d[i] = fma2(x[i], by, fma2(hr, w_pre[i], d[i]));
+                dw_pre[i] = fma2(hr, x[i], dw_pre[i]);
             }
         }
-        // (x is free now: the gradient of x, then q scale w_post)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] = p.alpha * d[i];
+        for (int i = 0; i < kPairs; ++i) x[i] = mul2(d[i], twice(p.alpha));
         Cols<T, kV>::put(static_cast<T *>(q.dx) + row * q.dx_stride, t, threads, C, x);
-        Sum<1> s3{{0.f}};
+        uint64_t dot = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const float tk = bits >> i & 1 ? d[i] * p.keep_scale : 0.f, through = tk * a[i], dn = through * scale[i];
-            const bool on = bits >> i & 1;
-            if (on) {
-                dscale[i] += through * y[i] * w_post[i];
-                dw_post[i] += dn * y[i];
-            }
-            x[i] = dn * w_post[i];
-            s3.v[0] += x[i] * y[i];
-            if (p.gate) a[i] = on ? tk * scale[i] * y[i] * w_post[i] * slope[i] : 0.f;  // dgate
+        for (int i = 0; i < kPairs; ++i) {
+            const uint64_t du = mul2(d[i], y[i]);
+            qu[i] = fma2(du, f[0][i], qu[i]);
+            x[i] = mul2(mul2(d[i], f[0][i]), scale[i]);  // q scale w_post
+            dot = fma2(x[i], y[i], dot);
+            f[1][i] = mul2(mul2(du, f[1][i]), scale[i]);  // dgate
         }
-        if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, C, a);
+        Sum<1> s3;
+        add_up(dot, s3.v[0]);
+        if (p.post) tell<kBlock>(s3, red, turn);
+        if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, C, f[1]);
         if (p.post) {
-            row_sum<kBlock>(s3, red, turn);
-            const float m = s3.v[0] * inv;
+            read<kBlock>(s3, red, turn);
+            const uint64_t m = twice(-s3.v[0] * inv);
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) x[i] = r1 * (x[i] - y[i] * m);
+            for (int i = 0; i < kPairs; ++i) x[i] = mul2(fma2(y[i], m, x[i]), twice(r1));
         }
         Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, C, x);
     }
     // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
+    float sum[2][kPer];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+        unpair(qu[i], sum[0][2 * i], sum[0][2 * i + 1]);
+        unpair(dw_pre[i], sum[1][2 * i], sum[1][2 * i + 1]);
+    }
     if (!kBlock) {
         for (int w = 0; w < kNarrowRows; ++w) {
             if ((threadIdx.x >> 5) == w) {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
                     const int c = Cols<T, kV>::at(i / kV, t, 32) + i % kV;
-                    sums[c] = w ? sums[c] + dw_post[i] : dw_post[i];
-                    sums[kNarrow + c] = w ? sums[kNarrow + c] + dscale[i] : dscale[i];
-                    sums[2 * kNarrow + c] = w ? sums[2 * kNarrow + c] + dw_pre[i] : dw_pre[i];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        sum[n][i] += w ? sums[n * kNarrow + c] : 0.f;
+                        sums[n * kNarrow + c] = sum[n][i];
+                    }
                 }
             }
             __syncthreads();
         }
     }
-    float *to = q.partial + (size_t)blockIdx.x * 3 * C;
-    if (kBlock || threadIdx.x < 32) {
+    float *to = q.partial + (size_t)blockIdx.x * 2 * C;
+    if (kBlock || threadIdx.x / 32 == kNarrowRows - 1) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
             if (c < C) {
-                to[c] = kBlock ? dw_post[i] : sums[c];
-                to[C + c] = kBlock ? dscale[i] : sums[kNarrow + c];
-                to[2 * (size_t)C + c] = kBlock ? dw_pre[i] : sums[2 * kNarrow + c];
+                to[c] = sum[0][i];
+                to[(size_t)C + c] = sum[1][i];
             }
         }
     }
@@ -440,7 +540,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
     const BlockNorm &p = q.f;
     int turn = 0;
     const float inv = 1.f / p.C;
-    float *to = q.partial + (size_t)blockIdx.x * 3 * p.C;
+    float *to = q.partial + (size_t)blockIdx.x * 2 * p.C;
     float k, a, slope;
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const Wide<T> in{p, row};
@@ -488,10 +588,10 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
             from_f32(static_cast<T *>(q.dy) + row * q.dy_stride + c,
                      p.post ? r1 * (through * sc * w - u * m1) : through * sc * w);
             if (p.gate) from_f32(static_cast<T *>(q.dgate) + row * q.dgate_stride + c, on ? tk * sc * u * w * slope : 0.f);
-            const float add[3] = {on ? through * sc * u : 0.f, on ? through * u * w : 0.f, p.pre ? dh(c) * x * r2 : 0.f};
+            const float add[2] = {on ? through * u : 0.f, p.pre ? dh(c) * x * r2 : 0.f};
             const bool first = row == blockIdx.x;
 #pragma unroll
-            for (int j = 0; j < 3; ++j) {
+            for (int j = 0; j < 2; ++j) {
                 float *at = to + (size_t)j * p.C + c;
                 *at = first ? add[j] : *at + add[j];
             }
@@ -516,7 +616,6 @@ Plan plan(long long rows, int C, int per_sm) {
     const long long most = (long long)kSMs * (per_sm / threads > 0 ? per_sm / threads : 1);
     return {(unsigned)(blocks < most ? blocks : most), threads};
 }
-constexpr int kFwdThreads = 1024, kBwdThreads = 512;
 
 // the widest access that every row allows: 16 bytes, or one element
 template <typename T>
@@ -560,7 +659,8 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
                           : wide_rows<T>(q) ? as(std::integral_constant<int, 16 / sizeof(T)>())
                                             : as(std::integral_constant<int, 1>());
     if (e) return e;
-    return column_sum_launch({q.partial, g.grid, p.C, 3, {q.dw_post, q.dscale, q.dw_pre}, q.header}, s);
+    return column_sum_launch({q.partial, g.grid, p.C, 2,
+                              {{q.dw_post, 0, p.scale}, {q.dscale, 0, p.w_post}, {q.dw_pre, 1, nullptr}}, p.dt, q.header}, s);
 }
 
 }  // namespace
@@ -568,7 +668,7 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
 cudaError_t block_norm_forward_launch(const BlockNorm &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? forward_of<__nv_bfloat16>(p, s) : forward_of<float>(p, s);
 }
-size_t block_norm_partial_floats(long long rows, int C) { return (size_t)plan(rows, C, kBwdThreads).grid * 3 * C; }
+size_t block_norm_partial_floats(long long rows, int C) { return (size_t)plan(rows, C, kBwdThreads).grid * 2 * C; }
 cudaError_t block_norm_backward_launch(const BlockNormBwd &q, cudaStream_t s) {
     return q.f.dt == HLA_BF16 ? backward_of<__nv_bfloat16>(q, s) : backward_of<float>(q, s);
 }

@@ -29,9 +29,16 @@ __global__ void __launch_bounds__(kCols *kGroups) column_sum_kernel(ColumnSum p)
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const long long c = at + group;
     if (lane == 0 && c < cols) {
-        const int part = (int)(c / p.C);
-        float *out = part == 0 ? p.out[0] : part == 1 ? p.out[1] : p.out[2];
-        if (out) out[c - (long long)part * p.C] = sum;
+        const int part = (int)(c / p.C), i = (int)(c - (long long)part * p.C);
+#pragma unroll
+        for (int o = 0; o < 3; ++o) {
+            const ColumnSum::Out &out = p.out[o];
+            if (!out.to || out.part != part) continue;
+            const float by = !out.factor           ? 1.f
+                             : p.dt == HLA_BF16 ? to_f32(static_cast<const __nv_bfloat16 *>(out.factor)[i])
+                                                : static_cast<const float *>(out.factor)[i];
+            out.to[i] = sum * by;
+        }
     }
 }
 

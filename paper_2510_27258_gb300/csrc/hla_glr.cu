@@ -624,7 +624,7 @@ cudaError_t backward_as(const GlrBwd &p, const Spread &r, cudaStream_t s) {
     const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kRing>, (long long)f.B * r.slabs, r.S,
                                           Tokens<T, Shape<kLanes, 4>, 4, kSlotsBwd, kRing>::kSmem, s, p, r.slabs, r.S, pairs);
     if (e) return e;
-    return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {p.ddecay}, p.header}, s);
+    return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {{p.ddecay, 0, nullptr}}, f.dt, p.header}, s);
 }
 template <typename T>
 cudaError_t backward_of(const GlrBwd &p, cudaStream_t s) {

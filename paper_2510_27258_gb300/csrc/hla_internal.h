@@ -305,13 +305,18 @@ cudaError_t block_norm_forward_launch(const BlockNorm &p, cudaStream_t stream);
 size_t block_norm_partial_floats(long long rows, int C);
 cudaError_t block_norm_backward_launch(const BlockNormBwd &p, cudaStream_t stream);
 
-// sums over `rows` partial rows of `parts` runs of C floats, in a fixed order, into out[part] (or nowhere); clears
-// the workspace's header
+// sums over `rows` partial rows of `parts` runs of C floats, in a fixed order: out[i].to, unless null, receives those
+// of one run, times a factor of type dt for each column where that is given; clears the workspace's header
 struct ColumnSum {
     const float *partial;
     long long rows;
     int C, parts;
-    float *out[3];
+    struct Out {
+        float *to;
+        int part;
+        const void *factor;
+    } out[3];
+    hla_dtype dt;
     WsHeader *header;
 };
 cudaError_t column_sum_launch(const ColumnSum &p, cudaStream_t stream);
