@@ -67,6 +67,10 @@ hla_status check_norm(BlockNorm &p, int rows, double dropout) {
     p.drop_below = (uint32_t)(dropout * 4294967296.0);
     p.drop = p.drop_below != 0;
     p.keep_scale = p.drop ? (float)(1.0 / (1.0 - dropout)) : 1.f;
+    for (uint32_t i = 0; i < 10; ++i) {
+        p.key[i][0] = (uint32_t)p.seed + i * 0x9E3779B9u;
+        p.key[i][1] = (uint32_t)(p.seed >> 32) + i * 0xBB67AE85u;
+    }
     return HLA_OK;
 }
 
@@ -168,7 +172,7 @@ hla_status hla_block_norm_forward(const void *x, const void *y, const void *gate
                                   double dropout, unsigned long long seed, unsigned long long offset, hla_stream_t stream) {
     clear_last_error();
     BlockNorm p{x, y, gate, w_post, scale, w_pre, x_out, h, dt, rows, C, post_norm, pre_norm, act, x_stride, y_stride,
-                gate_stride, x_out_stride, h_stride, alpha, eps, 0, 0, 1.f, seed, offset};
+                gate_stride, x_out_stride, h_stride, alpha, eps, 0, 0, 1.f, seed, offset, {}};
     HLA_TRY(check_norm(p, rows, dropout));
     HLA_TRY(check_tensor(x_out, x_out_stride, C, dt, rows, "x_out"));
     if (pre_norm) {
@@ -195,7 +199,7 @@ hla_status hla_block_norm_backward(const void *x, const void *y, const void *gat
                                    size_t workspace_bytes, hla_stream_t stream) {
     clear_last_error();
     BlockNormBwd q{{x, y, gate, w_post, scale, w_pre, nullptr, nullptr, dt, rows, C, post_norm, pre_norm, act, x_stride,
-                    y_stride, gate_stride, C, C, alpha, eps, 0, 0, 1.f, seed, offset},
+                    y_stride, gate_stride, C, C, alpha, eps, 0, 0, 1.f, seed, offset, {}},
                    dx_out, dh, dx, dy, dgate, dw_post, dscale, dw_pre, dx_out_stride, dh_stride, dx_stride, dy_stride,
                    dgate_stride, nullptr, static_cast<WsHeader *>(workspace)};
     HLA_TRY(check_norm(q.f, rows, dropout));

@@ -26,28 +26,54 @@ constexpr int kNarrow = 32 * kPer, kWide = 1024 * kPer;
 constexpr int kMaxWarps = 32, kNarrowRows = 4;
 constexpr int kFwdThreads = 512, kBwdThreads = 512;  // threads of an SM at a time
 
+constexpr uint32_t kMul0 = 0xD2511F53u, kMul1 = 0xCD9E8D57u;
+constexpr int kRounds = 10;
+
 struct Words {
     uint32_t w[4];
 };
-// Philox4x32-10
-__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint64_t offset, uint64_t seed) {
-    uint32_t c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32), k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+// the last rounds of Philox4x32-10, from round kFrom on, with the keys of each round
+template <int kFrom>
+__device__ __forceinline__ Words philox(const BlockNorm &p, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) {
 #pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+    for (int i = kFrom; i < kRounds; ++i) {
+        const uint64_t p0 = (uint64_t)c0 * kMul0, p1 = (uint64_t)c2 * kMul1;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ p.key[i][0];
         c1 = (uint32_t)p1;
-        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ p.key[i][1];
         c3 = (uint32_t)p0;
-        k0 += 0x9E3779B9u;
-        k1 += 0xBB67AE85u;
     }
     return {{c0, c1, c2, c3}};
+}
+// What the first three rounds make of a column group is the same for every row, but for one product of the row:
+//   round 0: (r0, r1, r2, r3) = (hi(o0 M1) ^ row ^ k, lo(o0 M1), hi(g M0) ^ o1 ^ k', lo(g M0))
+//   round 1: (s0, s1, s2, s3) = (hi(r2 M1) ^ r1 ^ k, lo(r2 M1), hi(r0 M0) ^ r3 ^ k', lo(r0 M0))
+//   round 2: (hi(s2 M1) ^ s1 ^ k, lo(s2 M1), hi(s0 M0) ^ s3 ^ k', lo(s0 M0))
+// where only r0, s2 and s3 know the row.
+struct Group {
+    uint32_t a, b, c, d;  // r3 ^ k', s1 ^ k, hi(s0 M0) ^ k', lo(s0 M0)
+    __device__ __forceinline__ void set(const BlockNorm &p, uint32_t group) {
+        const uint64_t g = (uint64_t)group * kMul0;
+        const uint64_t r2 = (uint64_t)((uint32_t)(g >> 32) ^ (uint32_t)(p.offset >> 32) ^ p.key[0][1]) * kMul1;
+        const uint64_t s0 = (uint64_t)((uint32_t)(r2 >> 32) ^ (uint32_t)((p.offset & 0xffffffffu) * kMul1) ^ p.key[1][0]) * kMul0;
+        a = (uint32_t)g ^ p.key[1][1];
+        b = (uint32_t)r2 ^ p.key[2][0];
+        c = (uint32_t)(s0 >> 32) ^ p.key[2][1];
+        d = (uint32_t)s0;
+    }
+};
+// the row's product of round 1
+__device__ __forceinline__ uint64_t row_of(const BlockNorm &p, uint32_t row) {
+    return (uint64_t)((uint32_t)((p.offset & 0xffffffffu) * kMul1 >> 32) ^ row ^ p.key[0][0]) * kMul0;
+}
+__device__ __forceinline__ Words words_of(const BlockNorm &p, const Group &g, uint64_t row) {
+    const uint64_t p1 = (uint64_t)((uint32_t)(row >> 32) ^ g.a) * kMul1;
+    return philox<3>(p, (uint32_t)(p1 >> 32) ^ g.b, (uint32_t)p1, g.c ^ (uint32_t)row, g.d);
 }
 
 // whether one value is kept
 __device__ __forceinline__ bool kept(const BlockNorm &p, long long row, int col) {
-    const Words r = philox((uint32_t)(col >> 2), (uint32_t)row, p.offset, p.seed);
+    const Words r = philox<0>(p, (uint32_t)(col >> 2), (uint32_t)row, (uint32_t)p.offset, (uint32_t)(p.offset >> 32));
     const uint32_t w = (col & 2) ? ((col & 1) ? r.w[3] : r.w[2]) : ((col & 1) ? r.w[1] : r.w[0]);
     return w >= p.drop_below;
 }
@@ -142,19 +168,31 @@ struct Cols {
             if (c < C) VecIo<T, kV>::store(row + c, o);
         }
     }
-    // zeros in the places of dropped values
+};
+
+// zeros in the places of dropped values
+template <int kV>
+struct Drop {
+    Group group[kV == 1 ? 1 : 2];
+    __device__ __forceinline__ void open(const BlockNorm &p, int t, int threads) {
+        if (kV == 1 || !p.drop) return;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            group[j].set(p, (uint32_t)((4 * j / kV * threads + t) * kV + 4 * j % kV) >> 2);
+    }
     template <int kN>
-    static __device__ __forceinline__ void drop(const BlockNorm &p, long long row, int t, int threads, Pairs (&v)[kN]) {
+    __device__ __forceinline__ void apply(const BlockNorm &p, long long row, int t, int threads, Pairs (&v)[kN]) const {
         bool keep[kPer];
         if constexpr (kV == 1) {
 #pragma unroll
-            for (int e = 0; e < kE; ++e) keep[e] = kept(p, row, at(e, t, threads));
+            for (int e = 0; e < kPer; ++e) keep[e] = kept(p, row, e * threads + t);
         } else {
+            const uint64_t of_row = row_of(p, (uint32_t)row);
 #pragma unroll
-            for (int j = 0; j < kPer; j += 4) {
-                const Words w = philox((uint32_t)(at(j / kV, t, threads) + j % kV) >> 2, (uint32_t)row, p.offset, p.seed);
+            for (int j = 0; j < 2; ++j) {
+                const Words w = words_of(p, group[j], of_row);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) keep[j + i] = w.w[i] >= p.drop_below;
+                for (int i = 0; i < 4; ++i) keep[4 * j + i] = w.w[i] >= p.drop_below;
             }
         }
 #pragma unroll
@@ -167,6 +205,85 @@ struct Cols {
             }
     }
 };
+
+// A thread's columns of the rows that its block takes, one every `step`.  kSlots > 1: through a ring of shared memory,
+// all rows but the one in use in flight, written and read by the same thread.  1: in registers, a row ahead.  0: loaded
+// where they are used.
+template <typename T, int kV, int kTensors, int kSlots>
+struct Rows {
+    using C8 = Cols<T, kV>;
+    const T *from[kTensors];  // (null: not there)
+    long long stride[kTensors];
+    char *ring;
+    int t, threads, C;
+    long long rows, step;
+    C8 ahead[kSlots == 1 ? kTensors : 1];
+
+    __device__ __forceinline__ char *place(int slot, int i, int e) const {
+        return ring + ((slot * kTensors + i) * C8::kE + e) * (int)blockDim.x * 16;
+    }
+    __device__ __forceinline__ void send(int slot, long long row) const {
+        if constexpr (kSlots > 1) {
+#pragma unroll
+            for (int i = 0; i < kTensors; ++i)
+#pragma unroll
+                for (int e = 0; e < C8::kE; ++e) {
+                    const int c = C8::at(e, t, threads);
+                    if (from[i])
+                        ring_copy<T, kV>(reinterpret_cast<Raw<T, kV> *>(place(slot, i, e)), from[i] + row * stride[i] + c,
+                                         c < C && row < rows);
+                }
+            ring_commit();
+        }
+    }
+    __device__ __forceinline__ void begin(char *smem, long long row) {
+        if constexpr (kSlots > 1) {
+            ring = smem + threadIdx.x * 16;
+#pragma unroll
+            for (int k = 0; k < kSlots - 1; ++k) send(k, row + k * step);
+        } else {
+            used(row - step);
+        }
+    }
+    // when a row is in registers
+    __device__ __forceinline__ void used(long long row) {
+        if constexpr (kSlots == 1) {
+#pragma unroll
+            for (int i = 0; i < kTensors; ++i)
+                if (from[i] && row + step < rows) ahead[i].load(from[i] + (row + step) * stride[i], t, threads, C);
+        }
+    }
+    __device__ __forceinline__ void next(int slot, long long row) const {
+        if constexpr (kSlots > 1) {
+            ring_wait<kSlots - 2>();
+            send(slot ? slot - 1 : kSlots - 1, row + (kSlots - 1) * step);
+        }
+    }
+    __device__ __forceinline__ void get(int slot, int i, long long row, Pairs &v) const {
+        C8 c;
+        if constexpr (kSlots > 1) {
+#pragma unroll
+            for (int e = 0; e < C8::kE; ++e)
+                c.r[e] = C8::at(e, t, threads) < C ? *reinterpret_cast<const Raw<T, kV> *>(place(slot, i, e))
+                                                   : raw_zero<T, kV>();
+        } else if constexpr (kSlots == 1) {
+            c = ahead[i];
+        } else {
+            c.load(from[i] + row * stride[i], t, threads, C);
+        }
+        c.get(v);
+    }
+};
+// Slots of the gradient's ring: three, or two where that would take the room of another block (none where rows are
+// read an element at a time, or two do not fit).  The forward, with fewer rows to hold, keeps the next row in registers:
+// 68.6 us against 75.3 on B8 n2048 C2048 bf16 (the gradient, whose registers would spill: 159 against 124.6).
+template <typename T, int kV, int kMax>
+constexpr int slots() {
+    constexpr int bytes = 5 * (kMax ? kMax : 128) * kPer * (int)sizeof(T);
+    return kV == 1 ? 0 : 3 * bytes <= 64 * 1024 || (kMax == 512 && 3 * bytes <= 160 * 1024) ? 3 : 2 * bytes <= 200 * 1024 ? 2 : 0;
+}
+template <typename T>
+size_t ring_bytes(int threads, int slots) { return (size_t)slots * 5 * threads * kPer * sizeof(T); }
 
 // a weight's eight columns, or ones
 template <typename T, int kV>
@@ -206,15 +323,15 @@ __device__ __forceinline__ void tell(Sum<kN> &s, float (&red)[2][2][kMaxWarps], 
 #pragma unroll
         for (int i = 0; i < kN; ++i) red[turn][i][threadIdx.x >> 5] = s.v[i];
 }
-template <bool kBlock, int kN>
+template <int kMax, int kN>
 __device__ __forceinline__ void read(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
-    if (!kBlock) return;
-    const int warps = blockDim.x >> 5;
+    if (!kMax) return;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
         float sum = 0.f;
-        for (int w = 0; w < warps; w += 4) {  // (what is behind the last warp was cleared)
+#pragma unroll
+        for (int w = 0; w < kMax / 32; w += 4) {  // (what is behind the block's last warp was cleared)
             const float4 f = *reinterpret_cast<const float4 *>(&red[turn][i][w]);
             sum += (f.x + f.y) + (f.z + f.w);
         }
@@ -222,10 +339,10 @@ __device__ __forceinline__ void read(Sum<kN> &s, float (&red)[2][2][kMaxWarps], 
     }
     turn ^= 1;
 }
-template <bool kBlock, int kN>
+template <int kMax, int kN>
 __device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
-    tell<kBlock>(s, red, turn);
-    read<kBlock>(s, red, turn);
+    tell<(kMax > 0)>(s, red, turn);
+    read<kMax>(s, red, turn);
 }
 
 __device__ __forceinline__ void clear(float (&red)[2][2][kMaxWarps]) {
@@ -250,7 +367,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
     const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
     const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
     const float inv = 1.f / C;
-    Pairs scale, w_pre;  // (the first times w_post)
+    Pairs scale, w_pre;  // (the first times w_post and the kept values' factor)
     {
         Pairs w_post;
         weight<T, kV>(p.scale, t, threads, C, scale);
@@ -259,20 +376,18 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
     }
-    Cols<T, kV> cx, cy, cg;
-    auto load = [&](long long row) {
-        cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
-        cy.load(static_cast<const T *>(p.y) + row * p.y_stride, t, threads, C);
-        if (p.gate) cg.load(static_cast<const T *>(p.gate) + row * p.gate_stride, t, threads, C);
-    };
+    Drop<kV> drop;
+    drop.open(p, t, threads);
+    Rows<T, kV, 3, 1> in{{static_cast<const T *>(p.x), static_cast<const T *>(p.y), static_cast<const T *>(p.gate)},
+                              {p.x_stride, p.y_stride, p.gate_stride}, nullptr, t, threads, C, p.rows, step};
     long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
-    if (row < p.rows) load(row);
+    in.begin(nullptr, row);
     for (; row < p.rows; row += step) {  // (all of a row's threads alike)
         Pairs x, y, f[1];
-        cx.get(x);
-        cy.get(y);
-        if (p.gate) cg.get(f[0]);
-        if (row + step < p.rows) load(row + step);
+        in.get(0, 0, row, x);
+        in.get(0, 1, row, y);
+        if (p.gate) in.get(0, 2, row, f[0]);
+        in.used(row);
         Sum<1> s1;
         if (p.post) {
             uint64_t sum = mul2(y[0], y[0]);
@@ -290,10 +405,10 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = scale[i];
         }
-        if (p.drop) Cols<T, kV>::drop(p, row, t, threads, f);
+        if (p.drop) drop.apply(p, row, t, threads, f);
         float r1 = 1.f;
         if (p.post) {
-            read<kBlock>(s1, red, turn);
+            read<kMax>(s1, red, turn);
             r1 = rsqrtf(s1.v[0] * inv + p.eps);
         }
         uint64_t sum = 0;
@@ -307,7 +422,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
         if (p.pre) tell<kBlock>(s2, red, turn);
         Cols<T, kV>::put(static_cast<T *>(p.x_out) + row * p.x_out_stride, t, threads, C, x);
         if (p.pre) {
-            read<kBlock>(s2, red, turn);
+            read<kMax>(s2, red, turn);
             const float r2 = rsqrtf(s2.v[0] * inv + p.eps);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) x[i] = mul2(mul2(x[i], twice(r2)), w_pre[i]);
@@ -351,7 +466,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_forward_kernel(BlockNorm
         if (p.post) {
             Sum<1> s{{0.f}};
             for (int c = threadIdx.x; c < p.C; c += 1024) s.v[0] += in.y(c) * in.y(c);
-            row_sum<true>(s, red, turn);
+            row_sum<1024>(s, red, turn);
             r1 = rsqrtf(s.v[0] * inv + p.eps);
         }
         if (p.pre) {
@@ -360,7 +475,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_forward_kernel(BlockNorm
                 const float x = in.x_out(c, r1, k, a, slope);
                 s.v[0] += x * x;
             }
-            row_sum<true>(s, red, turn);
+            row_sum<1024>(s, red, turn);
             r2 = rsqrtf(s.v[0] * inv + p.eps);
         }
         for (int c = threadIdx.x; c < p.C; c += 1024) {  // (x_out may be x: a column is read and written by one thread)
@@ -393,34 +508,34 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
     const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
     const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
     const float inv = 1.f / C;
-    Pairs scale, w_pre;  // (the first times w_post)
+    Pairs scale, w_pre;  // (the first times w_post and the kept values' factor)
     {
         Pairs w_post;
         weight<T, kV>(p.scale, t, threads, C, scale);
         weight<T, kV>(p.w_post, t, threads, C, w_post);
         weight<T, kV>(p.w_pre, t, threads, C, w_pre);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) scale[i] = mul2(scale[i], w_post[i]);
+        for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
     }
+    Drop<kV> drop;
+    drop.open(p, t, threads);
     Pairs qu = {}, dw_pre = {};  // sums over this thread's rows
-    Cols<T, kV> cx, cy, cg, cd, ch;
-    auto load = [&](long long row) {
-        cx.load(static_cast<const T *>(p.x) + row * p.x_stride, t, threads, C);
-        cy.load(static_cast<const T *>(p.y) + row * p.y_stride, t, threads, C);
-        cd.load(static_cast<const T *>(q.dx_out) + row * q.dx_out_stride, t, threads, C);
-        if (p.gate) cg.load(static_cast<const T *>(p.gate) + row * p.gate_stride, t, threads, C);
-        if (p.pre) ch.load(static_cast<const T *>(q.dh) + row * q.dh_stride, t, threads, C);
-    };
+    constexpr int kSlots = slots<T, kV, kMax>();
+    extern __shared__ __align__(16) char ring[];
+    Rows<T, kV, 5, kSlots> in{{static_cast<const T *>(p.x), static_cast<const T *>(p.y), static_cast<const T *>(p.gate),
+                               static_cast<const T *>(q.dx_out), static_cast<const T *>(q.dh)},
+                              {p.x_stride, p.y_stride, p.gate_stride, q.dx_out_stride, q.dh_stride},
+                              nullptr, t, threads, C, p.rows, step};
     long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
-    if (row < p.rows) load(row);
-    for (; row < p.rows; row += step) {
-        Pairs x, y, d, h, f[2];  // f: k act(gate), k act'(gate)
-        cx.get(x);
-        cy.get(y);
-        cd.get(d);
-        if (p.gate) cg.get(f[0]);
-        if (p.pre) ch.get(h);
-        if (row + step < p.rows) load(row + step);
+    in.begin(ring, row);
+    for (int slot = 0; row < p.rows; row += step, slot = slot + 1 < kSlots ? slot + 1 : 0) {
+        Pairs x, y, d, h, f[2];  // f: act(gate), act'(gate), 0 where dropped
+        in.next(slot, row);
+        in.get(slot, 0, row, x);
+        in.get(slot, 1, row, y);
+        if (p.gate) in.get(slot, 2, row, f[0]);
+        in.get(slot, 3, row, d);
+        if (p.pre) in.get(slot, 4, row, h);
         Sum<1> s1;
         if (p.post) {
             uint64_t sum = mul2(y[0], y[0]);
@@ -435,17 +550,13 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = f[1][i] = twice(1.f);
         }
-        if (p.drop) {
-            Cols<T, kV>::drop(p, row, t, threads, f);
+        if (p.drop) drop.apply(p, row, t, threads, f);
+        Pairs fs;  // what multiplies u in x', and t in dn
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                f[0][i] = mul2(f[0][i], twice(p.keep_scale));
-                f[1][i] = mul2(f[1][i], twice(p.keep_scale));
-            }
-        }
+        for (int i = 0; i < kPairs; ++i) fs[i] = mul2(f[0][i], scale[i]);
         float r1 = 1.f;
         if (p.post) {
-            read<kBlock>(s1, red, turn);
+            read<kMax>(s1, red, turn);
             r1 = rsqrtf(s1.v[0] * inv + p.eps);
         }
 #pragma unroll
@@ -454,14 +565,14 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
             uint64_t sum = 0, dot = 0;
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
-                x[i] = fma2(mul2(y[i], scale[i]), f[0][i], mul2(x[i], twice(p.alpha)));  // x'
+                x[i] = fma2(y[i], fs[i], mul2(x[i], twice(p.alpha)));  // x'
                 sum = fma2(x[i], x[i], sum);
                 dot = fma2(mul2(h[i], w_pre[i]), x[i], dot);
             }
             Sum<2> s2;
             add_up(sum, s2.v[0]);
             add_up(dot, s2.v[1]);
-            row_sum<kBlock>(s2, red, turn);
+            row_sum<kMax>(s2, red, turn);
             const float r2 = rsqrtf(s2.v[0] * inv + p.eps), m2 = s2.v[1] * r2 * inv;
             // t = dx' + r2 (dh w_pre - x' r2 m2)
             const uint64_t by = twice(-r2 * r2 * m2);
@@ -480,7 +591,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
         for (int i = 0; i < kPairs; ++i) {
             const uint64_t du = mul2(d[i], y[i]);
             qu[i] = fma2(du, f[0][i], qu[i]);
-            x[i] = mul2(mul2(d[i], f[0][i]), scale[i]);  // q scale w_post
+            x[i] = mul2(d[i], fs[i]);  // q scale w_post
             dot = fma2(x[i], y[i], dot);
             f[1][i] = mul2(mul2(du, f[1][i]), scale[i]);  // dgate
         }
@@ -489,18 +600,19 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
         if (p.post) tell<kBlock>(s3, red, turn);
         if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, C, f[1]);
         if (p.post) {
-            read<kBlock>(s3, red, turn);
+            read<kMax>(s3, red, turn);
             const uint64_t m = twice(-s3.v[0] * inv);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) x[i] = mul2(fma2(y[i], m, x[i]), twice(r1));
         }
         Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, C, x);
     }
+    if (kSlots > 1) ring_wait<0>();
     // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
     float sum[2][kPer];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-        unpair(qu[i], sum[0][2 * i], sum[0][2 * i + 1]);
+        unpair(mul2(qu[i], twice(p.keep_scale)), sum[0][2 * i], sum[0][2 * i + 1]);
         unpair(dw_pre[i], sum[1][2 * i], sum[1][2 * i + 1]);
     }
     if (!kBlock) {
@@ -548,7 +660,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
         if (p.post) {
             Sum<1> s{{0.f}};
             for (int c = threadIdx.x; c < p.C; c += 1024) s.v[0] += in.y(c) * in.y(c);
-            row_sum<true>(s, red, turn);
+            row_sum<1024>(s, red, turn);
             r1 = rsqrtf(s.v[0] * inv + p.eps);
         }
         auto dh = [&](int c) { return p.pre ? to_f32(static_cast<const T *>(q.dh)[row * q.dh_stride + c]) : 0.f; };
@@ -559,7 +671,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
                 s.v[0] += x * x;
                 s.v[1] += dh(c) * Wide<T>::of(p.w_pre, c) * x;
             }
-            row_sum<true>(s, red, turn);
+            row_sum<1024>(s, red, turn);
             r2 = rsqrtf(s.v[0] * inv + p.eps);
             m2 = s.v[1] * r2 * inv;
         }
@@ -576,7 +688,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
                 const float tk = back(c, x);
                 if (k != 0.f) s.v[0] += tk * k * a * Wide<T>::of(p.scale, c) * Wide<T>::of(p.w_post, c) * in.y(c) * r1;
             }
-            row_sum<true>(s, red, turn);
+            row_sum<1024>(s, red, turn);
             m1 = s.v[0] * inv;
         }
         for (int c = threadIdx.x; c < p.C; c += 1024) {
@@ -632,15 +744,30 @@ bool wide_rows(const BlockNormBwd &q) {
            ok(q.dy, q.dy_stride) && ok(q.dgate, q.dgate_stride);
 }
 
+template <typename F>
+cudaError_t by_threads(int C, int threads, F f) {
+    return C <= kNarrow     ? f(std::integral_constant<int, 0>())
+           : threads <= 256 ? f(std::integral_constant<int, 256>())
+           : threads <= 512 ? f(std::integral_constant<int, 512>())
+                            : f(std::integral_constant<int, 1024>());
+}
+template <typename P>
+cudaError_t launch_ring(void (*kernel)(P), const Plan &g, size_t smem, cudaStream_t s, const P &p) {
+    if (smem > 32 * 1024) {  // (48 KB with what the kernel has besides)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e) return e;
+    }
+    return launch_after(kernel, g.grid, g.threads, smem, s, p);
+}
+
 template <typename T>
 cudaError_t forward_of(const BlockNorm &p, cudaStream_t s) {
     const Plan g = plan(p.rows, p.C, kFwdThreads);
     if (p.C > kWide) return launch_after(block_norm_wide_forward_kernel<T>, g.grid, 1024, 0, s, p);
     auto as = [&](auto V) -> cudaError_t {
-        return p.C <= kNarrow      ? launch_after(block_norm_forward_kernel<T, V(), 0>, g.grid, g.threads, 0, s, p)
-               : g.threads <= 256 ? launch_after(block_norm_forward_kernel<T, V(), 256>, g.grid, g.threads, 0, s, p)
-               : g.threads <= 512 ? launch_after(block_norm_forward_kernel<T, V(), 512>, g.grid, g.threads, 0, s, p)
-                                  : launch_after(block_norm_forward_kernel<T, V(), 1024>, g.grid, g.threads, 0, s, p);
+        return by_threads(p.C, g.threads, [&](auto M) {
+            return launch_after(block_norm_forward_kernel<T, V(), M()>, g.grid, g.threads, 0, s, p);
+        });
     };
     return wide_rows<T>(p) ? as(std::integral_constant<int, 16 / sizeof(T)>()) : as(std::integral_constant<int, 1>());
 }
@@ -650,10 +777,9 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
     const BlockNorm &p = q.f;
     const Plan g = plan(p.rows, p.C, kBwdThreads);
     auto as = [&](auto V) -> cudaError_t {
-        return p.C <= kNarrow      ? launch_after(block_norm_backward_kernel<T, V(), 0>, g.grid, g.threads, 0, s, q)
-               : g.threads <= 256 ? launch_after(block_norm_backward_kernel<T, V(), 256>, g.grid, g.threads, 0, s, q)
-               : g.threads <= 512 ? launch_after(block_norm_backward_kernel<T, V(), 512>, g.grid, g.threads, 0, s, q)
-                                  : launch_after(block_norm_backward_kernel<T, V(), 1024>, g.grid, g.threads, 0, s, q);
+        return by_threads(p.C, g.threads, [&](auto M) {
+            return launch_ring(block_norm_backward_kernel<T, V(), M()>, g, ring_bytes<T>(g.threads, slots<T, V(), M()>()), s, q);
+        });
     };
     const cudaError_t e = p.C > kWide ? launch_after(block_norm_wide_backward_kernel<T>, g.grid, 1024, 0, s, q)
                           : wide_rows<T>(q) ? as(std::integral_constant<int, 16 / sizeof(T)>())

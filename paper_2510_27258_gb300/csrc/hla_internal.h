@@ -291,6 +291,7 @@ struct BlockNorm {
     uint32_t drop_below;
     float keep_scale;     // (1 without dropout)
     uint64_t seed, offset;
+    uint32_t key[10][2];  // of each of the generator's rounds, from the seed
 };
 struct BlockNormBwd {
     BlockNorm f;  // x_out and h unused
