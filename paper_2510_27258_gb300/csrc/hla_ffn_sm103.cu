@@ -2,13 +2,13 @@
 //
 //   kOut   out = act(x Wg^T) (x Wu^T)
 //   kGrad  dZ = [dout Zu act'(Zg) | dout act(Zg)], Z computed again, to the workspace in bf16
-//   kDx    dx = dZg Wg + dZu Wu: one sum over both
-//   kDw    d[Wg; Wu] = dZ^T x
+//   kBack  dx = dZg Wg + dZu Wu (one sum over both), and d[Wg; Wu] = dZ^T x: the tiles of both in one list, which
+//          leaves fewer pairs without one at the end than two launches
 //
 // Each is a product D = A B^T over tiles of 256 x 256, made by a pair of blocks (tcgen05.mma of both their SMs, M = N =
-// 256): a block loads 128 rows of A and 128 of B in steps of 64, so an SM reads 32 KB of shared memory's fill for 8.4
-// MFLOP.  Where the sum's index is not the contiguous one (B of kDx, both of kDw) the operand is read as it lies
-// (MN-major), so nothing is transposed in memory.  The forward's tile has 128 gate columns (the first block's half of B)
+// 256): a block loads 128 rows of A and 128 of B in steps of 64, 32 KB for 8.4 MFLOP of its half.  Where the sum's index is
+// not the contiguous one (B of dx, both of dw) the operand is read as it lies (MN-major), so nothing is transposed in
+// memory.  The forward's tile has 128 gate columns (the first block's half of B)
 // and the same 128 up columns (the second's), so that activation and product happen where the tile is read out.
 //
 // A block has a loading warp, whose copies count at the first block's barriers, a warp that issues the products (first
@@ -19,6 +19,8 @@
 //
 // Every wait has a limit: it sets the workspace's error word and the block's `stop`, after which all roles leave,
 // copies and products in flight are waited for (with a limit), and tensor memory is released.
+#include <climits>
+
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
 #include "sm103_prims.cuh"
@@ -38,23 +40,28 @@ constexpr uint32_t kStagingBytes = 32 * kPitch;          // of a warp that reads
 constexpr uint32_t kSmemBytes = 1024 + kStages * kStageBytes + 4 * kStagingBytes + 256;
 constexpr long long kWaitCycles = 4000000000ll, kLandCycles = 200000000ll;  // about 2 and 0.1 s
 
-enum Mode { kOut, kGrad, kDx, kDw };
+enum Mode { kOut, kGrad, kBack };
 
 struct Work {
     int down, across, parts;   // tiles along A's and B's rows, cuts of the sum
     int steps, per_part;       // steps of the sum, and of a part
-    int plane_steps;           // kDx: steps of one plane; kDw: tiles of one plane
-    int rows, cols;            // of the output (kOut, kGrad: cols = F; kDw: rows = F, of each plane)
+    int dw;                    // kBack: of dw, else of dx
+    int plane_steps;           // dx: steps of one plane; dw: tiles of one plane
+    int rows, cols;            // of the output (kOut, kGrad: cols = F; dw: rows = F, of each plane)
     int act;
-    void *out;                 // kOut, kDx, kDw: bf16, or fp32 parts [part][rows][cols] (kDw: [part][2][rows][cols]); kGrad: dZ
+    void *out;                 // bf16, or fp32 parts [part][rows][cols] (dw: [part][2][rows][cols]); kGrad: dZ
     long long out_row;         // elements
-    long long out_plane;       // kGrad, kDw: elements from one plane to the other
+    long long out_plane;       // kGrad, dw: elements from one plane to the other
     int out_wide;              // whether rows of out allow 16-byte accesses
     const __nv_bfloat16 *dout;  // kGrad
     long long dout_row;
     int dout_wide;
+};
+struct Call {
+    Work w[2];       // kBack: two lists of tiles, one behind the other
+    int first, all;  // tiles of the first, of both
     WsHeader *header;
-    int clear;                 // the call's first product clears the header
+    int clear;       // the call's first product clears the header
 };
 
 struct Bars {
@@ -178,16 +185,20 @@ __device__ __forceinline__ void copy_rows(char *staged, E *at, long long row, in
 
 template <Mode kMode>
 __global__ void __launch_bounds__(kThreads, 1)
-ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, Work w) {
+ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_b1,
+                const __grid_constant__ Call call) {
     extern __shared__ char raw[];
     char *stages = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
     char *staging = stages + kStages * kStageBytes;
     Bars *bars = reinterpret_cast<Bars *>(staging + 4 * kStagingBytes);
     static_assert(sizeof(Bars) <= 256, "the barriers' room");
-    constexpr bool kAcross = kMode == kDw, kBcross = kMode == kDx || kMode == kDw;  // read against the sum's direction
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
-    const int clusters = gridDim.x / 2, tiles = w.down * w.across * w.parts;
+    const int clusters = gridDim.x / 2, tiles = call.all;
+    WsHeader *header = call.header;
+    auto work_of = [&](int i) -> const Work & { return call.w[kMode == kBack && i >= call.first]; };
+    auto place_of = [&](int i) { return tile_of(work_of(i), kMode == kBack && i >= call.first ? i - call.first : i); };
     let_next_begin();
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_a);
@@ -214,7 +225,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     cluster_meet();
     tc_fence_after();
     after_previous();
-    if (w.clear && blockIdx.x == 0 && threadIdx.x == 0) *w.header = WsHeader{};  // (waits set it after seconds)
+    if (call.clear && blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // (waits set it after seconds)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&bars->tmem);
 
     if (warp == 0) {
@@ -223,10 +234,11 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             uint32_t phase = 0, sent = 0;
             bool ok = true;
             for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
-                const Tile t = tile_of(w, i);
+                const Work &w = work_of(i);
+                const Tile t = place_of(i);
                 const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
                 for (int k = k_lo; k < k_hi; ++k) {
-                    if (!wait(&bars->empty[s], phase ^ 1, bars, w.header, 1)) {
+                    if (!wait(&bars->empty[s], phase ^ 1, bars, header, 1)) {
                         ok = false;
                         break;
                     }
@@ -236,19 +248,21 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     if (kMode == kOut || kMode == kGrad) {
                         load_pair(a, &map_a, bar, k * kStep, t.m * kTile + rank * kHalf, 0);
                         load_pair(b, &map_b, bar, k * kStep, t.n * kHalf, rank);
-                    } else if (kMode == kDx) {
+                    } else if (!w.dw) {
+                        const CUtensorMap *ma = i < call.first ? &map_a : &map_a1, *mb = i < call.first ? &map_b : &map_b1;
                         const int plane = k >= w.plane_steps, at = (k - plane * w.plane_steps) * kStep;
-                        load_pair(a, &map_a, bar, at, t.m * kTile + rank * kHalf, plane);
+                        load_pair(a, ma, bar, at, t.m * kTile + rank * kHalf, plane);
                         const int n = t.n * kTile + rank * kHalf;
-                        load_pair(b, &map_b, bar, n, at, plane);
-                        load_pair(b + kHalfBytes / 2, &map_b, bar, n + 64, at, plane);
+                        load_pair(b, mb, bar, n, at, plane);
+                        load_pair(b + kHalfBytes / 2, mb, bar, n + 64, at, plane);
                     } else {
+                        const CUtensorMap *ma = i < call.first ? &map_a : &map_a1, *mb = i < call.first ? &map_b : &map_b1;
                         const int plane = t.m >= w.plane_steps, m = (t.m - plane * w.plane_steps) * kTile + rank * kHalf;
-                        load_pair(a, &map_a, bar, m, k * kStep, plane);
-                        load_pair(a + kHalfBytes / 2, &map_a, bar, m + 64, k * kStep, plane);
+                        load_pair(a, ma, bar, m, k * kStep, plane);
+                        load_pair(a + kHalfBytes / 2, ma, bar, m + 64, k * kStep, plane);
                         const int n = t.n * kTile + rank * kHalf;
-                        load_pair(b, &map_b, bar, n, k * kStep, 0);
-                        load_pair(b + kHalfBytes / 2, &map_b, bar, n + 64, k * kStep, 0);
+                        load_pair(b, mb, bar, n, k * kStep, 0);
+                        load_pair(b + kHalfBytes / 2, mb, bar, n + 64, k * kStep, 0);
                     }
                     ++sent;
                     if (++s == kStages) {
@@ -263,7 +277,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             for (uint32_t d = 0; ok && d < kStages && d < sent; ++d) {
                 if (s == 0) phase ^= 1;
                 s = s ? s - 1 : kStages - 1;
-                ok = wait(&bars->empty[s], phase, bars, w.header, 4);
+                ok = wait(&bars->empty[s], phase, bars, header, 4);
             }
             while (!ok && clock64() - t0 < kLandCycles) {
             }
@@ -271,17 +285,23 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t idesc = idesc_bf16(256, 256, kAcross, kBcross);
             int s = 0, b = 0;
             uint32_t phase = 0, bphase = 0;
             bool ok = true;
             for (int i = blockIdx.x / 2; i < tiles && ok; i += clusters) {
-                const Tile t = tile_of(w, i);
+                const Work &w = work_of(i);
+                const Tile t = place_of(i);
                 const int k_lo = t.part * w.per_part, k_hi = min(w.steps, k_lo + w.per_part);
-                if (!wait(&bars->taken[b], bphase ^ 1, bars, w.header, 2)) break;
+                if (!wait(&bars->taken[b], bphase ^ 1, bars, header, 2)) break;
                 tc_fence_after();
+                // operands that are read against the sum's direction: 16 of its indices are 2048 bytes on, else 32
+                const bool a_cross = kMode == kBack && w.dw;
+                constexpr bool b_cross = kMode == kBack;
+                const uint32_t idesc = idesc_bf16(256, 256, a_cross, b_cross), a_step = a_cross ? 2048 : 32,
+                               a_lbo = a_cross ? kHalfBytes / 2 : 16;
+                constexpr uint32_t b_step = b_cross ? 2048 : 32, b_lbo = b_cross ? kHalfBytes / 2 : 16;
                 for (int k = k_lo; k < k_hi; ++k) {
-                    if (!wait(&bars->full[s], phase, bars, w.header, 3)) {
+                    if (!wait(&bars->full[s], phase, bars, header, 3)) {
                         ok = false;
                         break;
                     }
@@ -289,8 +309,8 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     const uint32_t a = smem_u32(stages + s * kStageBytes), bb = a + kHalfBytes;
 #pragma unroll
                     for (int kk = 0; kk < kStep / 16; ++kk) {
-                        const uint64_t da = kAcross ? desc_sw128(a + kk * 2048, kHalfBytes / 2, 1024) : desc_sw128(a + kk * 32, 16, 1024);
-                        const uint64_t db = kBcross ? desc_sw128(bb + kk * 2048, kHalfBytes / 2, 1024) : desc_sw128(bb + kk * 32, 16, 1024);
+                        const uint64_t da = desc_sw128(a + kk * a_step, a_lbo, 1024);
+                        const uint64_t db = desc_sw128(bb + kk * b_step, b_lbo, 1024);
                         umma_pair(tmem + b * 256, da, db, idesc, k > k_lo || kk > 0);
                     }
                     commit_pair(&bars->empty[s]);
@@ -316,12 +336,14 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         int b = 0;
         uint32_t bphase = 0;
         for (int i = blockIdx.x / 2; i < tiles; i += clusters) {
-            const Tile t = tile_of(w, i);
-            if (!__all_sync(0xffffffffu, wait(&bars->done[b], bphase, bars, w.header, 5))) break;
+            const Work &w = work_of(i);
+            const Tile t = place_of(i);
+            if (!__all_sync(0xffffffffu, wait(&bars->done[b], bphase, bars, header, 5))) break;
             tc_fence_after();
             const uint32_t from = taddr(tmem + b * 256, quarter * 32, 0);
-            const int plane = kMode == kDw ? t.m >= w.plane_steps : 0;
-            const int m0 = (kMode == kDw ? t.m - plane * w.plane_steps : t.m) * kTile + rank * kHalf + quarter * 32;
+            const bool dw = kMode == kBack && w.dw;
+            const int plane = dw && t.m >= w.plane_steps;
+            const int m0 = (t.m - plane * w.plane_steps) * kTile + rank * kHalf + quarter * 32;
             const int rows = w.rows - m0;  // (may be below 1)
             char *row = mine + lane * kPitch;
             if (kMode == kOut) {
@@ -421,7 +443,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
             } else {
                 float *out = static_cast<float *>(w.out) +
-                             ((long long)t.part * (kMode == kDw ? 2 : 1) + plane) * w.rows * w.cols + (long long)m0 * w.cols;
+                             ((long long)t.part * (dw ? 2 : 1) + plane) * w.rows * w.cols + (long long)m0 * w.cols;
 #pragma unroll 1
                 for (int c = 0; c < kTile; c += 32) {
                     const int n0 = t.n * kTile + c;
@@ -498,12 +520,16 @@ cudaError_t map_of(CUtensorMap *map, const void *p, long long cols, long long ro
 }
 
 template <Mode kMode>
-cudaError_t run(const CUtensorMap &a, const CUtensorMap &b, const Work &w, cudaStream_t s) {
+cudaError_t run(const CUtensorMap (&m)[4], Call &c, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(ffn_tile_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e) return e;
-    const long long tiles = (long long)w.down * w.across * w.parts;
-    return launch_cluster_after(ffn_tile_kernel<kMode>, 2u * (unsigned)(tiles < kPairs ? tiles : kPairs), kThreads, 2, kSmemBytes,
-                                s, a, b, w);
+    auto tiles = [](const Work &w) { return (long long)w.down * w.across * w.parts; };
+    const long long all = tiles(c.w[0]) + (kMode == kBack ? tiles(c.w[1]) : 0);
+    if (all > INT_MAX) return cudaErrorInvalidValue;
+    c.first = (int)tiles(c.w[0]);
+    c.all = (int)all;
+    return launch_cluster_after(ffn_tile_kernel<kMode>, 2u * (unsigned)(all < kPairs ? all : kPairs), kThreads, 2, kSmemBytes, s, m[0],
+                                m[1], m[2], m[3], c);
 }
 
 // Cuts of a sum of `steps`: as many as give every pair a tile, of eight steps or more
@@ -562,10 +588,12 @@ bool wide(const void *p, long long row, int cols) { return cols % 8 == 0 && rows
 // kOut and kGrad
 template <Mode kMode>
 cudaError_t forward_product(const Ffn &p, const Operands &o, Work w, cudaStream_t s) {
-    CUtensorMap a, b;
-    cudaError_t e = map_of(&a, o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kHalf);
-    if (!e) e = map_of(&b, o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kHalf);
+    CUtensorMap m[4];
+    cudaError_t e = map_of(&m[0], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kHalf);
+    if (!e) e = map_of(&m[1], o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kHalf);
     if (e) return e;
+    m[2] = m[0];
+    m[3] = m[1];
     w.down = tiles_of(p.M, kTile);
     w.across = tiles_of(p.F, kHalf);
     w.parts = 1;
@@ -573,8 +601,8 @@ cudaError_t forward_product(const Ffn &p, const Operands &o, Work w, cudaStream_
     w.rows = p.M;
     w.cols = p.F;
     w.act = p.act;
-    w.clear = 1;
-    return run<kMode>(a, b, w, s);
+    Call c{{w, w}, 0, 0, reinterpret_cast<WsHeader *>(p.ws), 1};
+    return run<kMode>(m, c, s);
 }
 
 cudaError_t add_parts(const float *from, int parts, long long rows, int cols, void *out, long long out_row, cudaStream_t s) {
@@ -597,13 +625,12 @@ size_t ffn_tc_backward_scratch_bytes(int M, int K, int F) {
 cudaError_t ffn_tc_forward(const Ffn &p, cudaStream_t s) {
     char *at = p.ws + kWsHeaderBytes;
     Operands o;
-    cudaError_t e = align_operands(p, at, o, s);
+    const cudaError_t e = align_operands(p, at, o, s);
     if (e) return e;
     Work w{};
     w.out = p.out;
     w.out_row = p.out_stride;
     w.out_wide = wide(p.out, p.out_stride, p.F);
-    w.header = reinterpret_cast<WsHeader *>(p.ws);
     return forward_product<kOut>(p, o, w, s);
 }
 
@@ -617,62 +644,62 @@ cudaError_t ffn_tc_backward(const FfnBwd &q, cudaStream_t s) {
     const long long dz_plane = (long long)p.M * F8;
     __nv_bfloat16 *dz = reinterpret_cast<__nv_bfloat16 *>(at);
     at += up256((size_t)2 * dz_plane * 2);
-    Work w{};
-    w.header = reinterpret_cast<WsHeader *>(p.ws);
-    w.out = dz;
-    w.out_row = F8;
-    w.out_plane = dz_plane;
-    w.out_wide = 1;
-    w.dout = static_cast<const __nv_bfloat16 *>(q.dout);
-    w.dout_row = q.dout_stride;
-    w.dout_wide = wide(q.dout, q.dout_stride, p.F);
-    e = forward_product<kGrad>(p, o, w, s);
-    if (e) return e;
-
-    CUtensorMap a, b;
-    // dx: the sum runs over both planes of dZ and w
-    e = map_of(&a, dz, p.F, p.M, 2, F8, dz_plane, kHalf);
-    if (!e) e = map_of(&b, o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kStep);
-    if (e) return e;
-    const Cut dx = cut_dx(p.M, p.K, p.F), dw = cut_dw(p.M, p.K, p.F);
-    w = Work{};
-    w.header = reinterpret_cast<WsHeader *>(p.ws);
-    w.down = tiles_of(p.M, kTile);
-    w.across = tiles_of(p.K, kTile);
-    w.plane_steps = tiles_of(p.F, kStep);
-    w.steps = 2 * w.plane_steps;
-    w.parts = dx.parts;
-    w.per_part = dx.per;
-    w.rows = p.M;
-    w.cols = p.K;
-    w.out = dx.parts > 1 ? at : q.dx;
-    w.out_row = q.dx_stride;
-    w.out_wide = wide(q.dx, q.dx_stride, p.K);
-    e = run<kDx>(a, b, w, s);
-    if (e) return e;
-    if (dx.parts > 1) {
-        e = add_parts(reinterpret_cast<const float *>(at), dx.parts, p.M, p.K, q.dx, q.dx_stride, s);
+    {
+        Work w{};
+        w.out = dz;
+        w.out_row = F8;
+        w.out_plane = dz_plane;
+        w.out_wide = 1;
+        w.dout = static_cast<const __nv_bfloat16 *>(q.dout);
+        w.dout_row = q.dout_stride;
+        w.dout_wide = wide(q.dout, q.dout_stride, p.F);
+        e = forward_product<kGrad>(p, o, w, s);
         if (e) return e;
-        at += up256(sizeof(float) * dx.parts * p.M * p.K);
     }
-
+    const Cut dx_cut = cut_dx(p.M, p.K, p.F), dw_cut = cut_dw(p.M, p.K, p.F);
+    float *dx_parts = reinterpret_cast<float *>(at);
+    at += dx_cut.parts > 1 ? up256(sizeof(float) * dx_cut.parts * p.M * p.K) : 0;
+    float *dw_parts = reinterpret_cast<float *>(at);
+    Work dx{}, dw{};
+    // dx: the sum runs over both planes of dZ and w
+    dx.down = tiles_of(p.M, kTile);
+    dx.across = tiles_of(p.K, kTile);
+    dx.plane_steps = tiles_of(p.F, kStep);
+    dx.steps = 2 * dx.plane_steps;
+    dx.parts = dx_cut.parts;
+    dx.per_part = dx_cut.per;
+    dx.rows = p.M;
+    dx.cols = p.K;
+    dx.out = dx.parts > 1 ? dx_parts : q.dx;
+    dx.out_row = q.dx_stride;
+    dx.out_wide = wide(q.dx, q.dx_stride, p.K);
     // dw: tiles of either plane, the sum over tokens
-    e = map_of(&a, dz, p.F, p.M, 2, F8, dz_plane, kStep);
-    if (!e) e = map_of(&b, o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kStep);
+    dw.dw = 1;
+    dw.plane_steps = tiles_of(p.F, kTile);
+    dw.down = 2 * dw.plane_steps;
+    dw.across = dx.across;
+    dw.steps = tiles_of(p.M, kStep);
+    dw.parts = dw_cut.parts;
+    dw.per_part = dw_cut.per;
+    dw.rows = p.F;
+    dw.cols = p.K;
+    dw.out = dw.parts > 1 ? dw_parts : q.dw;
+    dw.out_row = p.K;
+    dw.out_plane = (long long)p.F * p.K;
+    dw.out_wide = wide(q.dw, p.K, p.K);
+    // the list with the longer sums first
+    const int at_dx = dw.per_part > dx.per_part, at_dw = 1 - at_dx;
+    CUtensorMap m[4];
+    e = map_of(&m[2 * at_dx], dz, p.F, p.M, 2, F8, dz_plane, kHalf);
+    if (!e) e = map_of(&m[2 * at_dx + 1], o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kStep);
+    if (!e) e = map_of(&m[2 * at_dw], dz, p.F, p.M, 2, F8, dz_plane, kStep);
+    if (!e) e = map_of(&m[2 * at_dw + 1], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kStep);
     if (e) return e;
-    w.plane_steps = tiles_of(p.F, kTile);
-    w.down = 2 * w.plane_steps;
-    w.steps = tiles_of(p.M, kStep);
-    w.parts = dw.parts;
-    w.per_part = dw.per;
-    w.rows = p.F;
-    w.out = dw.parts > 1 ? at : q.dw;
-    w.out_row = p.K;
-    w.out_plane = (long long)p.F * p.K;
-    w.out_wide = wide(q.dw, p.K, p.K);
-    e = run<kDw>(a, b, w, s);
-    if (e || dw.parts == 1) return e;
-    return add_parts(reinterpret_cast<const float *>(at), dw.parts, 2LL * p.F, p.K, q.dw, p.K, s);
+    Call c{{at_dx ? dw : dx, at_dx ? dx : dw}, 0, 0, reinterpret_cast<WsHeader *>(p.ws), 0};
+    e = run<kBack>(m, c, s);
+    if (!e && dx.parts > 1) e = add_parts(dx_parts, dx.parts, p.M, p.K, q.dx, q.dx_stride, s);
+    if (!e && dw.parts > 1) e = add_parts(dw_parts, dw.parts, 2LL * p.F, p.K, q.dw, p.K, s);
+    return e;
 }
 
 }  // namespace hla
