@@ -472,6 +472,207 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
+// ------------------------------------------------------------------------------------------------
+// few rows: the weights are the rows of the product, the tokens its columns
+//
+// With up to 256 tokens the weights' bytes are what counts.  A block reads 128 of their rows (64 gate and 64 up rows of
+// the same features; for dx 128 columns, against the sum's direction) for all tokens, 16 to 256 columns of one
+// product, so the products cost what the tokens need, and every SM streams weights: the sum is cut over the blocks of a
+// cluster, whose parts meet in shared memory and are added in the blocks' order, each block finishing some of the tokens.
+// ------------------------------------------------------------------------------------------------
+
+constexpr int kFewMost = 256, kFewThreads = 192, kFewStages = 8;
+constexpr uint32_t kFewABytes = 128 * kStep * 2;
+
+struct Few {
+    int cols, stages;   // tokens' columns in the product (a multiple of 16), stages of the ring
+    int steps, per;     // steps of the sum, of a block
+    int plane_steps;    // kBack: steps of one plane
+    int tokens, width;  // rows of the output, and its columns (kOut, kGrad: F; kBack: K)
+    int act;
+    __nv_bfloat16 *out;
+    long long out_row, out_plane;
+    const __nv_bfloat16 *dout;
+    long long dout_row;
+    WsHeader *header;
+    int clear;
+};
+
+struct FewBars {
+    uint64_t full[kFewStages], empty[kFewStages], done;
+    uint32_t tmem;
+    int stop;
+};
+
+__device__ bool wait_few(uint64_t *bar, uint32_t parity, FewBars *bars, WsHeader *header, unsigned where) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*reinterpret_cast<volatile int *>(&bars->stop)) return false;
+        if (clock64() - t0 > kWaitCycles) {
+            header->where = where;
+            header->detail = blockIdx.x;
+            header->error = kDevTimeout;
+            *reinterpret_cast<volatile int *>(&bars->stop) = 1;
+            return false;
+        }
+    }
+}
+
+// the first block of the cluster's partial sums and so on, in their order
+__device__ __forceinline__ float add_blocks(const float *mine, int S) {
+    if (S == 1) return *mine;
+    float sum = 0.f;
+    for (int b = 0; b < S; ++b) {
+        uint32_t at;
+        float v;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(b));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+        sum += v;
+    }
+    return sum;
+}
+
+// grid: tiles of weights' rows x blocks of a cluster
+template <Mode kMode>
+__global__ void __launch_bounds__(kFewThreads)
+ffn_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_t, Few f, int S) {
+    extern __shared__ char raw[];
+    __shared__ FewBars bars_;
+    FewBars *bars = &bars_;
+    char *stages = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = S > 1 ? (int)cluster_rank() : 0, tile = blockIdx.x / S;
+    const uint32_t stage_bytes = kFewABytes + f.cols * kStep * 2;
+    const uint32_t tmem_cols = f.cols <= 32 ? 32 : f.cols <= 64 ? 64 : f.cols <= 128 ? 128 : 256;
+    const int k_lo = min(rank * f.per, f.steps), k_hi = min(k_lo + f.per, f.steps);
+    let_next_begin();
+    if (threadIdx.x == 0) {
+        prefetch_tmap(&map_w);
+        prefetch_tmap(&map_t);
+        for (int s = 0; s < f.stages; ++s) {
+            mbar_init(&bars->full[s], 1);
+            mbar_init(&bars->empty[s], 1);
+        }
+        mbar_init(&bars->done, 1);
+        bars->stop = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(&bars->tmem, tmem_cols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    after_previous();
+    if (f.clear && blockIdx.x == 0 && threadIdx.x == 0) *f.header = WsHeader{};  // (waits set it after seconds)
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&bars->tmem);
+
+    if (warp == 0 && lane == 0) {
+        int s = 0;
+        uint32_t phase = 0, sent = 0;
+        bool ok = true;
+        for (int k = k_lo; k < k_hi; ++k) {
+            if (!wait_few(&bars->empty[s], phase ^ 1, bars, f.header, 11)) {
+                ok = false;
+                break;
+            }
+            char *a = stages + s * stage_bytes, *b = a + kFewABytes;
+            uint64_t *bar = &bars->full[s];
+            mbar_arrive_expect_tx(bar, stage_bytes);
+            if (kMode == kBack) {
+                const int plane = k >= f.plane_steps, at = (k - plane * f.plane_steps) * kStep;
+                tma_load_3d(a, &map_w, bar, tile * 128, at, plane);
+                tma_load_3d(a + kFewABytes / 2, &map_w, bar, tile * 128 + 64, at, plane);
+                tma_load_3d(b, &map_t, bar, at, 0, plane);
+            } else {
+                tma_load_3d(a, &map_w, bar, k * kStep, tile * 64, 0);
+                tma_load_3d(a + kFewABytes / 2, &map_w, bar, k * kStep, tile * 64, 1);
+                tma_load_3d(b, &map_t, bar, k * kStep, 0, 0);
+            }
+            ++sent;
+            if (++s == f.stages) {
+                s = 0;
+                phase ^= 1;
+            }
+        }
+        // (where a role gave up: the copies in flight land before shared memory goes)
+        const long long t0 = clock64();
+        for (uint32_t d = 0; !ok && d < (uint32_t)f.stages && d < sent; ++d) {
+            if (s == 0) phase ^= 1;
+            s = s ? s - 1 : f.stages - 1;
+            while (!mbar_try_wait(&bars->full[s], phase) && clock64() - t0 < kLandCycles) {
+            }
+        }
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t idesc = idesc_bf16(128, f.cols, kMode == kBack, 0);
+        int s = 0;
+        uint32_t phase = 0;
+        for (int k = k_lo; k < k_hi; ++k) {
+            if (!wait_few(&bars->full[s], phase, bars, f.header, 12)) break;
+            tc_fence_after();
+            const uint32_t a = smem_u32(stages + s * stage_bytes), b = a + kFewABytes;
+#pragma unroll
+            for (int kk = 0; kk < kStep / 16; ++kk) {
+                const uint64_t da = kMode == kBack ? desc_sw128(a + kk * 2048, kFewABytes / 2, 1024) : desc_sw128(a + kk * 32, 16, 1024);
+                umma_bf16(tmem, da, desc_sw128(b + kk * 32, 16, 1024), idesc, k > k_lo || kk > 0);
+            }
+            umma_commit(&bars->empty[s]);
+            if (++s == f.stages) {
+                s = 0;
+                phase ^= 1;
+            }
+        }
+        umma_commit(&bars->done);
+    }
+    __syncwarp();
+    // every block's sums to its shared memory, [token][row]: the stages are free when the last product is done
+    float *sums = reinterpret_cast<float *>(stages);
+    const bool some = k_lo < k_hi;
+    if (warp >= 2) {
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        if (__all_sync(0xffffffffu, wait_few(&bars->done, 0, bars, f.header, 13))) {
+            tc_fence_after();
+            for (int c = 0; c < f.cols; c += 16) {
+                uint32_t v[16];
+                tmem_ld16(taddr(tmem, quarter * 32, c), v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sums[(c + j) * 128 + row] = some ? __uint_as_float(v[j]) : 0.f;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (S > 1) cluster_meet();
+    // the block's tokens, a warp a row of 64 (kBack: 128) neighbours by turns
+    const int each = (f.tokens + S - 1) / S, lo = rank * each, hi = min(lo + each, f.tokens);
+    const int n0 = tile * (kMode == kBack ? 128 : 64), per_token = kMode == kBack ? 128 : 64;
+    for (int i = threadIdx.x; i < (hi - lo) * per_token; i += kFewThreads) {
+        const int token = lo + i / per_token, r = i % per_token, n = n0 + r;
+        if (n >= f.width) continue;
+        const float v = add_blocks(sums + token * 128 + r, S);
+        if (kMode == kBack) {
+            from_f32(f.out + token * f.out_row + n, v);
+        } else {
+            const float up = add_blocks(sums + token * 128 + 64 + r, S);
+            float slope;
+            const float a = act_of(f.act, v, slope);
+            if (kMode == kOut) {
+                from_f32(f.out + token * f.out_row + n, a * up);
+            } else {
+                const float d = to_f32(f.dout[token * f.dout_row + n]);
+                from_f32(f.out + token * f.out_row + n, d * up * slope);
+                from_f32(f.out + f.out_plane + token * f.out_row + n, d * a);
+            }
+        }
+    }
+    if (S > 1) cluster_meet();  // the others have read this block's sums
+    if (warp == 1) tmem_dealloc(tmem, tmem_cols);
+}
+
 // rows of K elements to rows of `stride` (a multiple of 8) elements
 __global__ void __launch_bounds__(256) ffn_align_kernel(const __nv_bfloat16 *from, long long from_row, __nv_bfloat16 *to,
                                                        long long to_row, int rows, int K) {
@@ -585,11 +786,51 @@ cudaError_t align_operands(const Ffn &p, char *&at, Operands &o, cudaStream_t s)
 
 bool wide(const void *p, long long row, int cols) { return cols % 8 == 0 && rows_aligned(p, row, 2, 16); }
 
+// Few rows: blocks of a cluster as many as fill two blocks an SM (one where the ring takes more than half of an SM's
+// shared memory), each with four steps or more
+template <Mode kMode>
+cudaError_t run_few(const CUtensorMap &weights, const CUtensorMap &tokens, Few f, int tiles, cudaStream_t s) {
+    const int bytes = (int)kFewABytes + f.cols * kStep * 2, sums = f.cols * 128 * 4;
+    const int room = f.cols <= 64 ? 100 * 1024 : 200 * 1024;
+    f.stages = room / bytes < kFewStages ? room / bytes : kFewStages;
+    const int blocks = f.cols <= 64 ? 2 * kSMs : kSMs;
+    int S = 1;
+    while (S < 8 && (long long)tiles * S * 2 <= blocks && f.steps >= S * 2 * 4) S *= 2;
+    f.per = tiles_of(f.steps, S);
+    const int smem = 1024 + (f.stages * bytes > sums ? f.stages * bytes : sums);
+    const cudaError_t e = cudaFuncSetAttribute(ffn_few_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e) return e;
+    return launch_cluster_after(ffn_few_kernel<kMode>, (unsigned)((long long)tiles * S), kFewThreads, S, smem, s, weights, tokens, f, S);
+}
+
+// Up to 256 tokens, where the tiles of 256 x 256 would leave pairs without one
+bool few(int M, int F) { return M <= kFewMost && tiles_of(F, kHalf) < kPairs; }
+int few_cols(int M) { return (M + 15) / 16 * 16; }
+
 // kOut and kGrad
 template <Mode kMode>
 cudaError_t forward_product(const Ffn &p, const Operands &o, Work w, cudaStream_t s) {
     CUtensorMap m[4];
-    cudaError_t e = map_of(&m[0], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kHalf);
+    cudaError_t e;
+    if (few(p.M, p.F)) {
+        Few f{};
+        f.cols = few_cols(p.M);
+        f.steps = tiles_of(p.K, kStep);
+        f.tokens = p.M;
+        f.width = p.F;
+        f.act = p.act;
+        f.out = static_cast<__nv_bfloat16 *>(w.out);
+        f.out_row = w.out_row;
+        f.out_plane = w.out_plane;
+        f.dout = w.dout;
+        f.dout_row = w.dout_row;
+        f.header = reinterpret_cast<WsHeader *>(p.ws);
+        f.clear = 1;
+        e = map_of(&m[0], o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kStep);
+        if (!e) e = map_of(&m[1], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, f.cols);
+        return e ? e : run_few<kMode>(m[0], m[1], f, tiles_of(p.F, 64), s);
+    }
+    e = map_of(&m[0], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kHalf);
     if (!e) e = map_of(&m[1], o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kHalf);
     if (e) return e;
     m[2] = m[0];
@@ -687,6 +928,30 @@ cudaError_t ffn_tc_backward(const FfnBwd &q, cudaStream_t s) {
     dw.out_row = p.K;
     dw.out_plane = (long long)p.F * p.K;
     dw.out_wide = wide(q.dw, p.K, p.K);
+    if (few(p.M, p.F)) {
+        Few f{};
+        f.cols = few_cols(p.M);
+        f.plane_steps = dx.plane_steps;
+        f.steps = dx.steps;
+        f.tokens = p.M;
+        f.width = p.K;
+        f.out = static_cast<__nv_bfloat16 *>(q.dx);
+        f.out_row = q.dx_stride;
+        f.header = reinterpret_cast<WsHeader *>(p.ws);
+        CUtensorMap m[4];
+        e = map_of(&m[0], o.w, p.K, p.F, 2, o.w_row, o.w_row * p.F, kStep);
+        if (!e) e = map_of(&m[1], dz, p.F, p.M, 2, F8, dz_plane, f.cols);
+        if (!e) e = run_few<kBack>(m[0], m[1], f, tiles_of(p.K, 128), s);
+        if (!e) e = map_of(&m[0], dz, p.F, p.M, 2, F8, dz_plane, kStep);
+        if (!e) e = map_of(&m[1], o.x, p.K, p.M, 1, o.x_row, o.x_row * p.M, kStep);
+        if (e) return e;
+        m[2] = m[0];
+        m[3] = m[1];
+        dx.down = 0;
+        Call c{{dw, dx}, 0, 0, f.header, 0};
+        e = run<kBack>(m, c, s);
+        return e || dw.parts == 1 ? e : add_parts(dw_parts, dw.parts, 2LL * p.F, p.K, q.dw, p.K, s);
+    }
     // the list with the longer sums first
     const int at_dx = dw.per_part > dx.per_part, at_dw = 1 - at_dx;
     CUtensorMap m[4];
