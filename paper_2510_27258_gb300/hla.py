@@ -852,24 +852,37 @@ def hla_glr_backward(x, r, g, decay, dout, marks, dx=None, dr=None, dg=None, *, 
     return dx, dr, dg, ddecay
 
 
+def _like(x, side):
+    """A new tensor of x's shape and type."""
+    if side is None and x.is_contiguous():
+        return torch.empty_like(x)
+    return _empty(x.shape, x.dtype, x.device, side)
+
+
 def _lead(x, name):
     """(shape, rows) of a token tensor [rows, C] or [B, n, C]."""
-    if x.dim() not in (2, 3):
-        raise ValueError("%s must be [rows, C] or [B, n, C], got %s" % (name, tuple(x.shape)))
     shape = x.shape
-    return shape, shape[0] if len(shape) == 2 else shape[0] * shape[1]
+    if len(shape) == 3:
+        return shape, shape[0] * shape[1]
+    if len(shape) == 2:
+        return shape, shape[0]
+    raise ValueError("%s must be [rows, C] or [B, n, C], got %s" % (name, tuple(shape)))
 
 
 def _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm):
-    """What both directions of the block norm take of their inputs: strides, and addresses of weights."""
-    (shape, rows), T, i = _lead(x, "x"), x.dtype, _gpu(x)
-    C = shape[-1]
+    """What both directions of the block norm take of their inputs: addresses, and strides."""
+    shape, rows = _lead(x, "x")
+    T, i, C, one = x.dtype, _gpu(x), shape[-1], (1,)
+    if gate is None:
+        at_gate, gate_stride = None, C
+    else:
+        at_gate, gate_stride = gate.data_ptr(), _rows("gate", gate, shape, one, T, i)
     return shape, rows, C, T, _type_code(T), i, (
-        x.data_ptr(), y.data_ptr(), None if gate is None else gate.data_ptr(),
-        _flat("w_post", w_post, C, T, i) if post_norm else None, _flat("scale", scale, C, T, i),
-        _flat("w_pre", w_pre, C, T, i) if pre_norm else None), (
-        _rows("x", x, shape, (1,), T, i, True), _rows("y", y, shape, (1,), T, i),
-        C if gate is None else _rows("gate", gate, shape, (1,), T, i))
+        x.data_ptr(), y.data_ptr(), at_gate,
+        None if w_post is None or not post_norm else _flat("w_post", w_post, C, T, i),
+        None if scale is None else _flat("scale", scale, C, T, i),
+        None if w_pre is None or not pre_norm else _flat("w_pre", w_pre, C, T, i)), (
+        _rows("x", x, shape, one, T, i, True), _rows("y", y, shape, one, T, i), gate_stride)
 
 
 def hla_block_norm_forward(x, y, gate=None, x_out=None, h=None, *, w_post=None, scale=None, w_pre=None, post_norm=True,
@@ -882,17 +895,25 @@ def hla_block_norm_forward(x, y, gate=None, x_out=None, h=None, *, w_post=None, 
     """
     shape, rows, C, T, dt, i, given, strides = _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm)
     handle, side = _on(stream, i)
+    x_stride = h_stride = C
     if x_out is None:
-        x_out = _empty(shape, T, x.device, side)
+        x_out = _like(x, side)
+    else:
+        x_stride = _rows("x_out", x_out, shape, (1,), T, i)
+    at_h = None
     if not pre_norm:
         h = None
-    elif h is None:
-        h = _empty(shape, T, x.device, side)
-    _check(_entry("hla_block_norm_forward", i)(
-        *given, x_out.data_ptr(), None if h is None else h.data_ptr(), dt, rows, C, *strides,
-        _rows("x_out", x_out, shape, (1,), T, i), C if h is None else _rows("h", h, shape, (1,), T, i),
-        1 if post_norm else 0, 1 if pre_norm else 0, act, alpha, eps, dropout, seed, offset, handle),
-        "hla_block_norm_forward")
+    else:
+        if h is None:
+            h = _like(x, side)
+        else:
+            h_stride = _rows("h", h, shape, (1,), T, i)
+        at_h = h.data_ptr()
+    code = _entry("hla_block_norm_forward", i)(
+        *given, x_out.data_ptr(), at_h, dt, rows, C, *strides, x_stride, h_stride, 1 if post_norm else 0,
+        1 if pre_norm else 0, act, alpha, eps, dropout, seed, offset, handle)
+    if code:
+        _check(code, "hla_block_norm_forward")
     return x_out, h
 
 
@@ -908,12 +929,12 @@ def hla_block_norm_backward(x, y, gate, dx_out, dh=None, dx=None, dy=None, dgate
     None where the weight is not given; dgate is None without a gate.  dx may be dx_out."""
     shape, rows, C, T, dt, i, given, strides = _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm)
     handle, side = _on(stream, i)
-    dx = _empty(shape, T, x.device, side) if dx is None else dx
-    dy = _empty(shape, T, x.device, side) if dy is None else dy
+    dx = _like(x, side) if dx is None else dx
+    dy = _like(x, side) if dy is None else dy
     if gate is None:
         dgate = None
     elif dgate is None:
-        dgate = _empty(shape, T, x.device, side)
+        dgate = _like(x, side)
     if pre_norm and dh is None:
         raise ValueError("dh is needed with pre_norm")
     if not pre_norm:
@@ -952,14 +973,18 @@ def hla_ffn_forward(x, w, out=None, *, act=HLA_SILU, workspace=None, stream=None
     """
     shape, rows, K, F, T, dt, i = _ffn_sizes(x, w)
     handle, side = _on(stream, i)
-    wide = tuple(shape[:-1]) + (F,)
+    wide = (rows, F) if len(shape) == 2 else (shape[0], shape[1], F)
+    out_stride = F
     if out is None:
-        out = _empty(wide, T, x.device, side)
+        out = x.new_empty(wide) if side is None else _empty(wide, T, x.device, side)
+    else:
+        out_stride = _rows("out", out, wide, (1,), T, i)
     ws, ws_bytes, _keep = _scratch(workspace, hla_ffn_workspace_bytes, i, side, rows, K, F, dt)
-    _check(_entry("hla_ffn_forward", i)(
+    code = _entry("hla_ffn_forward", i)(
         x.data_ptr(), _shaped("w", w, (2, F, K), T, i), out.data_ptr(), dt, rows, K, F,
-        _rows("x", x, shape, (1,), T, i, True), _rows("out", out, wide, (1,), T, i), act, ws, ws_bytes, handle),
-        "hla_ffn_forward")
+        _rows("x", x, shape, (1,), T, i, True), out_stride, act, ws, ws_bytes, handle)
+    if code:
+        _check(code, "hla_ffn_forward")
     return out
 
 
