@@ -4,25 +4,31 @@
 //   dZg = dout Zu act'(Zg),  dZu = dout act(Zg),  dx = [dZg dZu] [Wg; Wu],  d[Wg; Wu] = [dZg dZu]^T x
 //
 // One tiled product serves all four: a block of 256 threads forms 128 x 128 outputs (64 x 64 where those would leave
-// SMs without a tile) from panels of 16 in shared memory, the next panel in registers meanwhile; a thread holds 8 x 8 (4 x 4)
-// sums and adds two neighbours an instruction.  The forward's tile is half gate and half up columns of the same
-// features, so that the activation and product happen in registers.  The gradient keeps [dZg dZu] in the workspace; its dx,
-// whose sum is over 2 F and whose tiles may be few, is cut along the sum, and the parts are added in their order.
+// SMs without a tile: there two groups of threads share each panel's indices, so that SMs have twice the warps), a thread
+// 8 x 8 (4 x 4) of them, from panels of 16 in a ring of shared memory, all but the one in
+// use in flight.  A panel lies as its matrix does: where the sum's index is the contiguous one a thread reads four
+// (two) of its indices of a row at a time, else four rows of an index, so that either way a wide access feeds many products.
+// The forward's tile is half gate and half up columns of the same features, so that the activation and product happen in
+// registers.  The gradient keeps [dZg dZu] in the workspace; its dx, whose sum is over 2 F and whose tiles may be few, is
+// cut along the sum, and the parts are added in their order.
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
 
 namespace hla {
 namespace {
 
-constexpr int kThreads = 256, kDepth = 16;
+constexpr int kThreads = 256, kDepth = 16, kStages = 4, kGroups = 2;
 
 enum Mode { kProduct, kParts, kOut, kGrad };
 
-// a matrix by its rows' and columns' strides; a column is an index of the sum
+// A matrix of the product, its rows those of A or B and its columns the sum's indices: `step` elements from one row to
+// the next where columns are neighbours (kAlong), else from one column to the next.  wide: such runs begin at 16 bytes.
 struct Mat {
     const float *p;
-    long long row, col;
+    long long step;
+    int wide;
 };
+Mat mat(const float *p, long long step) { return {p, step, rows_aligned(p, step, 4, 16)}; }
 
 struct Product {
     Mat a, b;
@@ -46,102 +52,144 @@ __device__ __forceinline__ float act_of(int act, float v, float &slope) {
     return act == HLA_SIGMOID ? s : v * s;
 }
 
-// A panel's elements of one thread: kRows x kDepth over 256 threads, neighbours along the contiguous direction
+// A panel of kRows rows and kDepth indices of the sum: rows from `at` on (of `rows`), the second half of them `pair` rows
+// behind the first's where pair > 0
 template <int kRows, bool kAlong>
 struct Panel {
-    static constexpr int kEach = kRows * kDepth / kThreads;
-    float v[kEach];
-    static __device__ __forceinline__ int row(int i) {
-        return kAlong ? (threadIdx.x >> 4) + 16 * i : threadIdx.x % kRows;
-    }
-    static __device__ __forceinline__ int depth(int i) {
-        return kAlong ? threadIdx.x & 15 : threadIdx.x / kRows + kThreads / kRows * i;
-    }
-    // rows from `at` on (of `rows`), the second half of the panel `pair` rows on where pair > 0
-    __device__ __forceinline__ void load(const Mat &m, int at, int rows, int k0, int k1, int pair) {
+    static constexpr int kPitch = (kAlong ? kDepth : kRows) + 4, kFloats = (kAlong ? kRows : kDepth) * kPitch;
+    static constexpr int kRun = (kAlong ? kDepth : kRows) / 4, kChunks = kRows * kDepth / 4;
+    // (by a block of kBlock threads)
+    template <int kBlock>
+    static __device__ __forceinline__ void send(const Mat &m, float *to, int at, int rows, int pair, int k0, int k1) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            int r = row(i);
-            const int k = k0 + depth(i);
+        for (int i = 0; i < (kChunks + kBlock - 1) / kBlock; ++i) {
+            const int c = threadIdx.x + i * kBlock;
+            if (kChunks % kBlock && c >= kChunks) break;
+            const int line = c / kRun, four = c % kRun * 4;
+            int r = kAlong ? line : four;
+            const int k = k0 + (kAlong ? four : line);
             const bool second = pair > 0 && r >= kRows / 2;
             if (second) r -= kRows / 2;
-            const long long from = (long long)(at + r) + (second ? pair : 0);
-            v[i] = at + r < rows && k < k1 ? m.p[from * m.row + k * m.col] : 0.f;
+            const long long row = (long long)(at + r) + (second ? pair : 0);
+            const int left = kAlong ? (at + r < rows ? k1 - k : 0) : (k < k1 ? rows - at - r : 0);  // of the four
+            const float *from = m.p + (kAlong ? row * m.step + k : k * m.step + row);
+            const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(to + line * kPitch + four));
+            if (m.wide) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(min(max(left, 0), 4) * 4)
+                             : "memory");
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 4 * j), "l"(from + j),
+                                 "r"(j < left ? 4 : 0)
+                                 : "memory");
+            }
         }
     }
-    __device__ __forceinline__ void store(float (&to)[kDepth][kRows + 4]) const {
+    // row i of thread t (of 16 along this side)
+    static __device__ __forceinline__ int row(int t, int i) { return kAlong ? t + 16 * i : i / 4 * 64 + t * 4 + i % 4; }
+    // kK indices from k on of its kE rows
+    template <int kE, int kK>
+    static __device__ __forceinline__ void get(const float *from, int t, int k, float (&v)[kK][kE]) {
+        if constexpr (kAlong) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) to[depth(i)][row(i)] = v[i];
+            for (int i = 0; i < kE; ++i) {
+                float f[kK];
+                VecIo<float, kK>::load(from + row(t, i) * kPitch + k, f);
+#pragma unroll
+                for (int q = 0; q < kK; ++q) v[q][i] = f[q];
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < kK; ++q)
+#pragma unroll
+                for (int i = 0; i < kE; i += 4) {
+                    float f[4];
+                    VecIo<float, 4>::load(from + (k + q) * kPitch + row(t, i), f);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[q][i + j] = f[j];
+                }
+        }
     }
 };
 
 // kTile 128 or 64; kA, kB: whether the sum's index is the contiguous one
+constexpr int groups_of(int tile) { return tile == 64 ? kGroups : 1; }
+
 template <int kTile, bool kA, bool kB, Mode kMode>
-__global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
-    constexpr int kE = kTile / 16, kH = kE / 2;  // a thread's rows and columns, in two runs of kH
+__global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel(Product p) {
+    constexpr int kG = groups_of(kTile);
+    constexpr int kE = kTile / 16, kK = kTile == 64 ? 4 : 2;  // a thread's rows and columns; indices read at a time
     constexpr bool kPair = kMode == kOut || kMode == kGrad;
     constexpr int kCols = kPair ? kTile / 2 : kTile;
-    __shared__ __align__(16) float as[2][kDepth][kTile + 4], bs[2][kDepth][kTile + 4];
+    static_assert(!kPair || kB, "a thread's gate and up columns are of the same features");
+    using A = Panel<kTile, kA>;
+    using B = Panel<kTile, kB>;
+    constexpr int kFloats = A::kFloats + B::kFloats;
+    extern __shared__ __align__(16) float ring[];  // [stage][a, b]
     let_next_begin();
     after_previous();
     if (kPair && blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // no device-side waits here: never an error
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4 & 15, group = threadIdx.x / kThreads;
     const int down = blockIdx.x / p.across, m0 = down * kTile, n0 = (blockIdx.x - down * p.across) * kCols;
-    const int k_lo = blockIdx.y * p.per, k_hi = (int)min((long long)p.K, (long long)k_lo + p.per), pair_rows = kPair ? p.N : 0;
-    Panel<kTile, kA> pa;
-    Panel<kTile, kB> pb;
-    uint64_t acc[kE][kH];
+    const int k_lo = blockIdx.y * p.per, k_hi = (int)min((long long)p.K, (long long)k_lo + p.per);
+    auto send = [&](int stage, int k0) {
+        A::template send<kThreads * kG>(p.a, ring + stage * kFloats, m0, p.M, 0, k0, k_hi);
+        B::template send<kThreads * kG>(p.b, ring + stage * kFloats + A::kFloats, n0, p.N, kPair ? p.N : 0, k0, k_hi);
+        ring_commit();
+    };
 #pragma unroll
-    for (int i = 0; i < kE; ++i)
+    for (int i = 0; i < kStages - 1; ++i) send(i, k_lo + i * kDepth);
+    float acc[kE][kE] = {};
+    int stage = 0;
+    for (int k0 = k_lo; k0 < k_hi; k0 += kDepth, stage = stage + 1 < kStages ? stage + 1 : 0) {
+        ring_wait<kStages - 2>();
+        __syncthreads();  // (and the stage of the last step has been read)
+        send(stage ? stage - 1 : kStages - 1, k0 + (kStages - 1) * kDepth);
+        const float *as = ring + stage * kFloats, *bs = as + A::kFloats;
 #pragma unroll
-        for (int j = 0; j < kH; ++j) acc[i][j] = 0;
-    pa.load(p.a, m0, p.M, k_lo, k_hi, 0);
-    pb.load(p.b, n0, p.N, k_lo, k_hi, pair_rows);
-    int buf = 0;
-    for (int k0 = k_lo; k0 < k_hi; k0 += kDepth, buf ^= 1) {
-        pa.store(as[buf]);
-        pb.store(bs[buf]);
-        __syncthreads();  // (the other buffer was read before it)
-        if (k0 + kDepth < k_hi) {
-            pa.load(p.a, m0, p.M, k0 + kDepth, k_hi, 0);
-            pb.load(p.b, n0, p.N, k0 + kDepth, k_hi, pair_rows);
+        for (int step = 0; step < kDepth / kG; step += kK) {
+            const int k = group * (kDepth / kG) + step;
+            float a[kK][kE], b[kK][kE];
+            A::template get<kE, kK>(as, ty, k, a);
+            B::template get<kE, kK>(bs, tx, k, b);
+#pragma unroll
+            for (int q = 0; q < kK; ++q)
+#pragma unroll
+                for (int i = 0; i < kE; ++i)
+#pragma unroll
+                    for (int j = 0; j < kE; ++j) acc[i][j] = fmaf(a[q][i], b[q][j], acc[i][j]);
         }
+    }
+    ring_wait<0>();
+    if constexpr (kG > 1) {  // the groups' sums, in their order
+        __syncthreads();
+#pragma unroll 1
+        for (int g = 1; g < kG; ++g) {
 #pragma unroll
-        for (int k = 0; k < kDepth; ++k) {
-            float a[kE];
-            uint64_t b[kH];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float f[kH];
-                VecIo<float, kH>::load(&as[buf][k][h * kTile / 2 + ty * kH], f);
-#pragma unroll
-                for (int i = 0; i < kH; ++i) a[h * kH + i] = f[i];
-                VecIo<float, kH>::load(&bs[buf][k][h * kTile / 2 + tx * kH], f);
-#pragma unroll
-                for (int i = 0; i < kH; i += 2) b[(h * kH + i) / 2] = pair(f[i], f[i + 1]);
+            for (int i = 0; i < kE * kE; ++i) {
+                float *at = ring + i * kThreads + threadIdx.x % kThreads;
+                if (group == g) *at = acc[i / kE][i % kE];
             }
+            __syncthreads();
+            if (group == 0)
 #pragma unroll
-            for (int i = 0; i < kE; ++i) {
-                const uint64_t a2 = pair(a[i], a[i]);
-#pragma unroll
-                for (int j = 0; j < kH; ++j) acc[i][j] = fma2(a2, b[j], acc[i][j]);
-            }
+                for (int i = 0; i < kE * kE; ++i) acc[i / kE][i % kE] += ring[i * kThreads + threadIdx.x];
+            __syncthreads();
         }
+        if (group > 0) return;
     }
 #pragma unroll
     for (int i = 0; i < kE; ++i) {
-        const int m = m0 + (i / kH) * kTile / 2 + ty * kH + i % kH;
+        const int m = m0 + A::row(ty, i);
         if (m >= p.M) continue;
-        float v[kE];
+        if constexpr (kPair) {
 #pragma unroll
-        for (int j = 0; j < kH; ++j) unpair(acc[i][j], v[2 * j], v[2 * j + 1]);
-        if (kPair) {
-#pragma unroll
-            for (int j = 0; j < kH; ++j) {
-                const int n = n0 + tx * kH + j;
+            for (int j = 0; j < kE / 2; ++j) {
+                const int n = n0 + B::row(tx, j);
                 if (n >= p.N) continue;
                 float slope;
-                const float a = act_of(p.act, v[j], slope), up = v[kH + j];
+                const float a = act_of(p.act, acc[i][j], slope), up = acc[i][j + kE / 2];
                 if (kMode == kOut) {
                     p.out[m * p.out_row + n] = a * up;
                 } else {
@@ -154,8 +202,8 @@ __global__ void __launch_bounds__(kThreads) ffn_product_kernel(Product p) {
         } else {
 #pragma unroll
             for (int j = 0; j < kE; ++j) {
-                const int n = n0 + (j / kH) * kTile / 2 + tx * kH + j % kH;
-                if (n < p.N) p.out[((kMode == kParts ? (long long)blockIdx.y * p.M : 0) + m) * p.out_row + n] = v[j];
+                const int n = n0 + B::row(tx, j);
+                if (n < p.N) p.out[((kMode == kParts ? (long long)blockIdx.y * p.M : 0) + m) * p.out_row + n] = acc[i][j];
             }
         }
     }
@@ -169,6 +217,7 @@ __global__ void __launch_bounds__(kThreads) ffn_parts_kernel(const float *from, 
     const long long all = (long long)M * N;
     for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < all; i += (long long)gridDim.x * kThreads) {
         float sum = 0.f;
+#pragma unroll 8
         for (int z = 0; z < parts; ++z) sum += from[z * all + i];
         const long long m = i / N;
         out[m * out_row + (i - m * N)] = sum;
@@ -196,14 +245,22 @@ cudaError_t product(Product p, int parts, cudaStream_t s) {
     const int tile = small_tiles(p.M, p.N, paired) ? 64 : 128, cols = paired ? tile / 2 : tile;
     p.across = (p.N + cols - 1) / cols;
     const dim3 grid((unsigned)p.across * ((p.M + tile - 1) / tile), parts);
-    return tile == 64 ? launch_after(ffn_product_kernel<64, kA, kB, kMode>, grid, kThreads, 0, s, p)
-                      : launch_after(ffn_product_kernel<128, kA, kB, kMode>, grid, kThreads, 0, s, p);
+    auto as = [&](auto kernel, int floats) -> cudaError_t {
+        const int smem = kStages * floats * (int)sizeof(float);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        return e ? e : launch_after(kernel, grid, kThreads * groups_of(tile), smem, s, p);
+    };
+    return tile == 64 ? as(ffn_product_kernel<64, kA, kB, kMode>, Panel<64, kA>::kFloats + Panel<64, kB>::kFloats)
+                      : as(ffn_product_kernel<128, kA, kB, kMode>, Panel<128, kA>::kFloats + Panel<128, kB>::kFloats);
 }
 
 const float *floats(const void *p) { return static_cast<const float *>(p); }
 
+// [dZg dZu] in rows of whole 16 bytes
+long long dz_row(int F) { return (2LL * F + 3) / 4 * 4; }
+
 cudaError_t forward_f32(const Ffn &p, cudaStream_t s) {
-    const Product q{{floats(p.x), p.x_stride, 1}, {floats(p.w), p.K, 1}, p.M, p.F, p.K, p.act, p.K, 0,
+    const Product q{mat(floats(p.x), p.x_stride), mat(floats(p.w), p.K), p.M, p.F, p.K, p.act, p.K, 0,
                     static_cast<float *>(p.out), p.out_stride, nullptr, 0, reinterpret_cast<WsHeader *>(p.ws)};
     return product<true, true, kOut>(q, 1, s);
 }
@@ -212,19 +269,20 @@ cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     const Ffn &f = p.f;
     float *dz = reinterpret_cast<float *>(f.ws + kWsHeaderBytes);
     const int F2 = 2 * f.F, parts = parts_of(f.M, f.K, f.F);
-    const Product q{{floats(f.x), f.x_stride, 1}, {floats(f.w), f.K, 1}, f.M, f.F, f.K, f.act, f.K, 0, dz, F2,
+    const long long row = dz_row(f.F);
+    const Product q{mat(floats(f.x), f.x_stride), mat(floats(f.w), f.K), f.M, f.F, f.K, f.act, f.K, 0, dz, row,
                     floats(p.dout), p.dout_stride, reinterpret_cast<WsHeader *>(f.ws)};
     cudaError_t e = product<true, true, kGrad>(q, 1, s);
     if (e) return e;
-    const Product dw{{dz, 1, F2}, {floats(f.x), 1, f.x_stride}, F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
+    const Product dw{mat(dz, row), mat(floats(f.x), f.x_stride), F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
                      nullptr, 0, nullptr};
     e = product<false, false, kProduct>(dw, 1, s);
     if (e) return e;
-    Product dx{{dz, F2, 1}, {floats(f.w), 1, f.K}, f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
+    Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
                nullptr, 0, nullptr};
     if (parts == 1) return product<true, false, kProduct>(dx, 1, s);
     dx.per = ((F2 + parts - 1) / parts + kDepth - 1) / kDepth * kDepth;
-    float *sums = dz + (size_t)f.M * F2;
+    float *sums = dz + (size_t)f.M * row;
     dx.out = sums;
     dx.out_row = f.K;
     e = product<true, false, kParts>(dx, parts, s);
@@ -242,7 +300,7 @@ size_t ffn_forward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
 size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
     if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
     const int parts = M ? parts_of(M, K, F) : 1;
-    return sizeof(float) * ((size_t)M * 2 * F + (parts > 1 ? (size_t)parts * M * K : 0));
+    return sizeof(float) * ((size_t)M * dz_row(F) + (parts > 1 ? (size_t)parts * M * K : 0));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);
