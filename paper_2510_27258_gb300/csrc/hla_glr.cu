@@ -3,8 +3,9 @@
 //   s = sigmoid(r), i = sigmoid(g), a = e^(decay s), m = sqrt(1 - a^2), b = m i x,  h_t = a_t h_{t-1} + b_t
 // and backwards, with D_t = a_t (dy_t + D_{t+1}) the gradient of h_{t-1} and G_t = dy_t + D_{t+1} that of h_t,
 //   dx = G m i,  dg = G b (1 - i),  e = G (h_t - i x / m),  dr = e decay s (1 - s),  ddecay = sum e s
-// (the derivative of h_t by log a is a h_{t-1} - i x a^2 / m, and a h_{t-1} = h_t - m i x).  1 - a^2 is u - u^2/2 + ...
-// where u = -2 decay s is below 1/2: the difference would lose what a slow decay is about.
+// (the derivative of h_t by log a is a h_{t-1} - i x a^2 / m, and a h_{t-1} = h_t - m i x).  Where v = -decay s is at most 1,
+// q = 1 - e^-v is a polynomial, and a = 1 - q, m^2 = 1 - a^2 = q (2 - q): a slow decay, which a long memory multiplies up, is
+// off by no more than its rounding, and m keeps what 1 - a^2 would lose.  Slabs whose decays are all -1 or above take that alone.
 //
 // The recurrence composes: a run of tokens takes h to P h + l, so the sequence is walked in tiles whose warps
 // scan their own tokens side by side and join by P and l in shared memory; one pass over the data.  A block holds 64
@@ -12,6 +13,8 @@
 // one sequence together: every block hands its tile's P and l to the others' shared memory, where their bytes
 // count at a barrier, and all form the same state in the same order, so equal inputs give equal bits.  The gradient walks the tiles backwards and takes h before each tile from the marks that the forward
 // leaves, so it reads every token once too.
+#include <type_traits>
+
 #include "hla_vec.cuh"
 #include "sm103_prims.cuh"
 
@@ -57,30 +60,39 @@ __device__ __forceinline__ uint64_t one_plus_exp(uint64_t v) {
     return add2(each(mul2(v, twice(-kLog2e)), ex2), twice(1.f));
 }
 
-// a lane's decays: log2 and, doubled and negated, natural
+// a lane's decays, negated
 struct Decay {
-    uint64_t log2a, u;
-    __device__ __forceinline__ explicit Decay(uint64_t d) : log2a(mul2(d, twice(kLog2e))), u(mul2(d, twice(-2.f))) {}
+    uint64_t d;
+    bool near;  // all of the warp's at most 1
+    __device__ __forceinline__ explicit Decay(uint64_t decay) : d(mul2(decay, twice(-1.f))) {
+        float x, y;
+        unpair(d, x, y);
+        near = __all_sync(0xffffffffu, x <= 1.f && y <= 1.f);
+    }
 };
 
 // a and w = 1 - a^2 from s
+template <bool kNear>
 __device__ __forceinline__ void decay_of(const Decay &d, uint64_t s, uint64_t &a, uint64_t &w) {
-    a = each(mul2(d.log2a, s), ex2);
-    const uint64_t u = mul2(d.u, s);
-    uint64_t p = fma2(u, twice(1.f / 5040.f), twice(-1.f / 720.f));
-    p = fma2(p, u, twice(1.f / 120.f));
-    p = fma2(p, u, twice(-1.f / 24.f));
-    p = fma2(p, u, twice(1.f / 6.f));
-    p = fma2(p, u, twice(-0.5f));
-    p = fma2(p, u, twice(1.f));
-    p = mul2(p, u);
-    const uint64_t far = fma2(mul2(a, twice(-1.f)), a, twice(1.f));
-    float u0, u1, p0, p1, f0, f1;
-    unpair(u, u0, u1);
-    unpair(p, p0, p1);
-    unpair(far, f0, f1);
-    // (a NaN in r is in both)
-    w = pair(u0 < 0.5f ? p0 : f0, u1 < 0.5f ? p1 : f1);
+    // (1 - e^-v) / v on 0..1 to 1.3e-8: interpolated at the Chebyshev nodes with the value 1 at 0
+    constexpr float kPoly[7] = {1.f, -0.5f, 0.166666031f, -0.0416592546f, 0.00830117054f, -0.001324818f, 0.000137424184f};
+    const uint64_t v = mul2(d.d, s), minus = twice(-1.f);
+    uint64_t q = fma2(v, twice(kPoly[6]), twice(kPoly[5]));
+#pragma unroll
+    for (int i = 4; i >= 0; --i) q = fma2(q, v, twice(kPoly[i]));
+    q = mul2(q, v);
+    a = fma2(q, minus, twice(1.f));
+    w = mul2(q, fma2(q, minus, twice(2.f)));
+    if (kNear) return;
+    const uint64_t far_a = each(mul2(v, twice(-kLog2e)), ex2), far_w = fma2(mul2(far_a, minus), far_a, twice(1.f));
+    float v0, v1, a0, a1, w0, w1, f0, f1, g0, g1;
+    unpair(v, v0, v1);
+    unpair(a, a0, a1);
+    unpair(w, w0, w1);
+    unpair(far_a, f0, f1);
+    unpair(far_w, g0, g1);
+    a = pair(v0 <= 1.f ? a0 : f0, v1 <= 1.f ? a1 : f1);  // (a NaN in r is in both)
+    w = pair(v0 <= 1.f ? w0 : g0, v1 <= 1.f ? w1 : g1);
 }
 
 // A block's shape: kLanes lanes walk a token's 2 kLanes channels, so a block of 256 threads has kGroups runs of kTok
@@ -379,15 +391,16 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     T *y = static_cast<T *>(p.y) + row0 * p.y_stride;
     open_exchange(others, S);
     const int rounds = (int)(((long long)p.n + step - 1) / step);
+    auto walk = [&](auto near) {
     for (int round = 0, slot = 0; round < rounds; ++round, t0 += step) {
-        uint64_t h[kTok], pr[kTok];  // this warp's states from 0, and the products of decays
+        uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
         in.next(slot, t0, step, at);
 #pragma unroll
         for (int u = 0; u < kTok; ++u) {
             uint64_t a, w;
             Raw<T, 2> rr = in.get(slot, 1, u);
             if (t0 + u >= len) shut(rr);  // (x is 0 there)
-            decay_of(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
+            decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
             const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
             // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
             const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
@@ -411,6 +424,9 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
                 if (t0 + u < p.n) at.put(to, t0 + u < len ? fma2(pr[u], before, h[u]) : 0, y_pairs);
         }
     }
+    };
+    if (decay.near) walk(std::true_type());
+    else walk(std::false_type());
     if (p.state_out && rank == 0 && group == 0) at.put(p.state_out + (size_t)b * p.C, state, pairs);
     ring_wait<0>();
     if (S > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
@@ -435,7 +451,7 @@ __global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool ro
                    h = at.get(p.state_in + (size_t)b * p.C, pairs);
     const Decay decay(at.get(p.decay, pairs));
     uint64_t a, w;
-    decay_of(decay, each(one_plus_exp(r), rcp), a, w);
+    decay_of<false>(decay, each(one_plus_exp(r), rcp), a, w);
     const uint64_t d = one_plus_exp(g);
     const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), x), y = fma2(a, h, add);
     at.put(p.state_out + (size_t)b * p.C, y, pairs);
@@ -486,6 +502,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     open_exchange(others, S);
     const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
+    auto walk = [&](auto near) {
     for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
         uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok], vd[kTok];  // 1 - i, b, i x / m
         Run forward{0, 0};
@@ -496,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
             Raw<T, 2> rr = in.get(slot, 1, u);
             if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
             s[u] = each(one_plus_exp(as_pair(rr)), rcp);
-            decay_of(decay, s[u], a[u], w);
+            decay_of<near()>(decay, s[u], a[u], w);
             const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, u))), rcp);
             const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, u)));
             mi[u] = mul2(m, i);
@@ -544,6 +561,9 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
                 if (t0 + u < f.n) put(u, t0 + u < len, out_pairs);
         }
     }
+    };
+    if (decay.near) walk(std::true_type());
+    else walk(std::false_type());
     if (p.dstate_in && rank == 0 && group == 0) at.put(p.dstate_in + (size_t)b * f.C, D, pairs);
     // decay's gradient: the block's groups in order, then (another kernel) its blocks
     __syncthreads();
