@@ -25,7 +25,7 @@ using namespace sm103;
 
 constexpr int kThreads = 256;
 constexpr int kMaxCluster = 16;
-constexpr int kSlotsFwd = 3, kSlotsBwd = 3;
+constexpr int kSlots = 2;  // a round in use, the next in flight (3: 57.3 and 124.9 us on B8 n2048 C2048 bf16 instead of 56.3 and 124.5)
 constexpr int kSMs = 152;
 constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
 constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN: a wait ran out
@@ -154,23 +154,27 @@ struct Lane {
 // A lane's next tokens of kTensors tensors.  kRing: rows that begin at 16 bytes come through a ring of kSlots rounds in
 // shared memory by asynchronous copies of a warp for its own groups, all but the round in use in flight.  Else they are
 // loaded into registers a round ahead.
-template <typename T, typename S, int kTensors, int kSlots, bool kRing>
+template <typename T, typename S, int kTensors, bool kRing>
 struct Tokens {
     static constexpr int kTok = S::kTok, kRow = S::kChannels * (int)sizeof(T), kChunks = kRow / 16;
     static constexpr int kRows = kTok * S::kOfWarp, kSlotBytes = kTensors * kRows * kRow;
     static constexpr int kSmem = kRing ? kThreads / 32 * kSlots * kSlotBytes : 0;
     const T *from[kTensors];
-    long long stride[kTensors];
+    long long stride[kTensors], ahead_by[kRing ? kTensors : 1];
     char *ring;      // this warp's
     int len, bytes;  // of the sequence; of this lane's chunk
     Raw<T, 2> ahead[kRing ? 1 : kTensors][kRing ? 1 : kTok];
 
-    __device__ __forceinline__ void set(int i, const void *p, long long row_stride, size_t row0, uint32_t channel) {
+    // t0: the group's first token, step: from a round's to the next one's
+    __device__ __forceinline__ void set(int i, const void *p, long long row_stride, size_t row0, uint32_t channel, int t0,
+                                        int step) {
         from[i] = static_cast<const T *>(p) + row0 * row_stride;
         stride[i] = row_stride;
-        if constexpr (kRing) {
+        if constexpr (kRing) {  // (the lane's first element of the next round to be sent for)
             const int lane = threadIdx.x & 31;
-            from[i] += (lane / kChunks) * row_stride + (long long)channel + lane % kChunks * (16 / (int)sizeof(T));
+            from[i] += (t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0) + lane / kChunks) * row_stride +
+                       (long long)channel + lane % kChunks * (16 / (int)sizeof(T));
+            ahead_by[i] = step * row_stride;
         }
     }
     __device__ __forceinline__ void open(char *smem, uint32_t channel, int C, int length) {
@@ -179,7 +183,6 @@ struct Tokens {
         const int left = min((int)(C - channel), S::kChannels) * (int)sizeof(T) - (int)(threadIdx.x % kChunks) * 16;
         bytes = min(max(left, 0), 16);
     }
-    // t0: the group's first token
     __device__ __forceinline__ void send(int slot, int t0, const Lane &at) {
         if constexpr (kRing) {
             const int lane = threadIdx.x & 31, first = t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0);  // the warp's
@@ -187,7 +190,8 @@ struct Tokens {
             const bool all = first >= 0 && first + kRows <= len;
 #pragma unroll
             for (int i = 0; i < kTensors; ++i) {
-                const T *p = from[i] + (long long)first * stride[i];
+                const T *p = from[i];
+                from[i] += ahead_by[i];
 #pragma unroll
                 for (int u = 0; u < kRows; u += 32 / kChunks, p += 32 / kChunks * stride[i]) {
                     const int t = u + lane / kChunks, row = t % kTok * S::kOfWarp + t / kTok;  // (groups' rows by turns)
@@ -379,51 +383,53 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.n) : p.n;
     const size_t row0 = (size_t)b * p.n;
     const int step = S * Sh::kSpan;
-    Tokens<T, Sh, 3, kSlotsFwd, kRing> in;
-    in.set(0, p.x, p.x_stride, row0, channel);
-    in.set(1, p.r, p.r_stride, row0, channel);
-    in.set(2, p.g, p.g_stride, row0, channel);
-    in.open(ring, channel, p.C, len);
+    Tokens<T, Sh, 3, kRing> in;
     int t0 = rank * Sh::kSpan + group * kTok;
+    in.set(0, p.x, p.x_stride, row0, channel, t0, step);
+    in.set(1, p.r, p.r_stride, row0, channel, t0, step);
+    in.set(2, p.g, p.g_stride, row0, channel, t0, step);
+    in.open(ring, channel, p.C, len);
     in.begin(t0, step, at);
     const Decay decay(at.get(p.decay, pairs));
     uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C, pairs) : 0;
-    T *y = static_cast<T *>(p.y) + row0 * p.y_stride;
+    T *y = static_cast<T *>(p.y) + (row0 + t0) * p.y_stride;
+    const long long y_step = step * p.y_stride;
     open_exchange(others, S);
     const int rounds = (int)(((long long)p.n + step - 1) / step);
     auto walk = [&](auto near) {
-    for (int round = 0, slot = 0; round < rounds; ++round, t0 += step) {
-        uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
-        in.next(slot, t0, step, at);
+        for (int round = 0, slot = 0; round < rounds; ++round, t0 += step) {
+            uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
+            in.next(slot, t0, step, at);
 #pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            uint64_t a, w;
-            Raw<T, 2> rr = in.get(slot, 1, u);
-            if (t0 + u >= len) shut(rr);  // (x is 0 there)
-            decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
-            const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
-            // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-            const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
-            h[u] = u ? fma2(a, h[u - 1], add) : add;
-            pr[u] = u ? mul2(a, pr[u - 1]) : a;
+            for (int u = 0; u < kTok; ++u) {
+                uint64_t a, w;
+                Raw<T, 2> rr = in.get(slot, 1, u);
+                if (t0 + u >= len) shut(rr);  // (x is 0 there)
+                decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
+                const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
+                // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
+                const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
+                h[u] = u ? fma2(a, h[u - 1], add) : add;
+                pr[u] = u ? mul2(a, pr[u - 1]) : a;
+            }
+            in.used(t0, step, at);
+            if (++slot == kSlots) slot = 0;
+            const int buf = round & 1;
+            runs[buf][group][lane] = {pr[kTok - 1], h[kTok - 1]};
+            const uint64_t before = join<Sh, 1>(runs[buf], others, round, S, rank, group, state);
+            if (p.marks && t0 % kGlrTile == 0 && t0 < p.n)
+                at.put(p.marks + ((size_t)b * glr_marks(p.n) + t0 / kGlrTile) * p.C, before, pairs);
+            T *to = y;
+            y += y_step;
+            if (t0 + kTok <= len && y_pairs) {
+#pragma unroll
+                for (int u = 0; u < kTok; ++u, to += p.y_stride) at.put(to, fma2(pr[u], before, h[u]), true);
+            } else {
+#pragma unroll
+                for (int u = 0; u < kTok; ++u, to += p.y_stride)
+                    if (t0 + u < p.n) at.put(to, t0 + u < len ? fma2(pr[u], before, h[u]) : 0, y_pairs);
+            }
         }
-        in.used(t0, step, at);
-        if (++slot == kSlotsFwd) slot = 0;
-        const int buf = round & 1;
-        runs[buf][group][lane] = {pr[kTok - 1], h[kTok - 1]};
-        const uint64_t before = join<Sh, 1>(runs[buf], others, round, S, rank, group, state);
-        if (p.marks && t0 % kGlrTile == 0 && t0 < p.n)
-            at.put(p.marks + ((size_t)b * glr_marks(p.n) + t0 / kGlrTile) * p.C, before, pairs);
-        T *to = y + (size_t)t0 * p.y_stride;
-        if (t0 + kTok <= len && y_pairs) {
-#pragma unroll
-            for (int u = 0; u < kTok; ++u, to += p.y_stride) at.put(to, fma2(pr[u], before, h[u]), true);
-        } else {
-#pragma unroll
-            for (int u = 0; u < kTok; ++u, to += p.y_stride)
-                if (t0 + u < p.n) at.put(to, t0 + u < len ? fma2(pr[u], before, h[u]) : 0, y_pairs);
-        }
-    }
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
@@ -481,19 +487,22 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     const int len = f.lengths ? min(max(f.lengths[b], 0), f.n) : f.n;
     const size_t row0 = (size_t)b * f.n;
     const int step = -S * Sh::kSpan, rounds = (int)(((long long)f.n - step - 1) / -step);
-    Tokens<T, Sh, 4, kSlotsBwd, kRing> in;
-    in.set(0, f.x, f.x_stride, row0, channel);
-    in.set(1, f.r, f.r_stride, row0, channel);
-    in.set(2, f.g, f.g_stride, row0, channel);
-    in.set(3, p.dy, p.dy_stride, row0, channel);
-    in.open(ring, channel, f.C, len);
+    Tokens<T, Sh, 4, kRing> in;
     int tile = ((rounds - 1) * S + rank) * Sh::kSpan, t0 = tile + group * kTok;
+    in.set(0, f.x, f.x_stride, row0, channel, t0, step);
+    in.set(1, f.r, f.r_stride, row0, channel, t0, step);
+    in.set(2, f.g, f.g_stride, row0, channel, t0, step);
+    in.set(3, p.dy, p.dy_stride, row0, channel, t0, step);
+    in.open(ring, channel, f.C, len);
     in.begin(t0, step, at);
     const uint64_t dec = at.get(f.decay, pairs);
     const Decay decay(dec);
     uint64_t D = p.dstate_out ? at.get(p.dstate_out + (size_t)b * f.C, pairs) : 0;  // the gradient of the state behind the round
-    T *dx = static_cast<T *>(p.dx) + row0 * p.dx_stride, *dr = static_cast<T *>(p.dr) + row0 * p.dr_stride,
-      *dg = static_cast<T *>(p.dg) + row0 * p.dg_stride;
+    // a group's last token of the round
+    T *dx = static_cast<T *>(p.dx) + (long long)(row0 + t0 + kTok - 1) * p.dx_stride,
+      *dr = static_cast<T *>(p.dr) + (long long)(row0 + t0 + kTok - 1) * p.dr_stride,
+      *dg = static_cast<T *>(p.dg) + (long long)(row0 + t0 + kTok - 1) * p.dg_stride;
+    const long long dx_step = step * p.dx_stride, dr_step = step * p.dr_stride, dg_step = step * p.dg_stride;
     const float *mark = f.marks + (size_t)b * glr_marks(f.n) * f.C;
     auto state_before = [&](int t) {
         return (unsigned)t < (unsigned)f.n ? at.get(mark + (size_t)(t / kGlrTile) * f.C, pairs) : 0;
@@ -503,64 +512,69 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
     auto walk = [&](auto near) {
-    for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
-        uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok], vd[kTok];  // 1 - i, b, i x / m
-        Run forward{0, 0};
-        in.next(slot, t0, step, at);
+        for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
+            uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok];  // .., m i, 1 - i, b, i x / m
+            uint64_t kept[kRing ? 1 : kTok] = {};
+            // dy, from the ring again where there is one: registers are what this kernel is short of
+            auto vd = [&](int u) { return kRing ? as_pair(in.get(slot, 3, u)) : kept[kRing ? 0 : u]; };
+            Run forward{0, 0};
+            in.next(slot, t0, step, at);
 #pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            uint64_t w;
-            Raw<T, 2> rr = in.get(slot, 1, u);
-            if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
-            s[u] = each(one_plus_exp(as_pair(rr)), rcp);
-            decay_of<near()>(decay, s[u], a[u], w);
-            const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, u))), rcp);
-            const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, u)));
-            mi[u] = mul2(m, i);
-            rest[u] = fma2(i, minus, twice(1.f));
-            add[u] = mul2(m, ix);
-            over[u] = mul2(rm, ix);
-            vd[u] = as_pair(in.get(slot, 3, u));
-            forward = u ? Run{mul2(a[u], forward.p), fma2(a[u], forward.l, add[u])} : Run{a[u], add[u]};
+            for (int u = 0; u < kTok; ++u) {
+                uint64_t w;
+                Raw<T, 2> rr = in.get(slot, 1, u);
+                if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
+                s[u] = each(one_plus_exp(as_pair(rr)), rcp);
+                decay_of<near()>(decay, s[u], a[u], w);
+                const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, u))), rcp);
+                const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, u)));
+                mi[u] = mul2(m, i);
+                rest[u] = fma2(i, minus, twice(1.f));
+                add[u] = mul2(m, ix);
+                over[u] = mul2(rm, ix);
+                if (!kRing) kept[kRing ? 0 : u] = as_pair(in.get(slot, 3, u));
+                forward = u ? Run{mul2(a[u], forward.p), fma2(a[u], forward.l, add[u])} : Run{a[u], add[u]};
+            }
+            in.used(t0, step, at);
+            uint64_t back = mul2(a[kTok - 1], vd(kTok - 1));
+#pragma unroll
+            for (int u = kTok - 2; u >= 0; --u) back = mul2(a[u], add2(vd(u), back));
+            const int buf = round & 1;
+            fwd[buf][group][lane] = forward;
+            bwd[buf][group][lane] = {forward.p, back};
+            uint64_t h = first;
+            first = state_before(tile + step);
+            uint64_t later = join<Sh, -1>(bwd[buf], others, round, S, rank, group, D);
+            for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);
+            uint64_t e[kTok];  // the derivative of the state by log a
+#pragma unroll
+            for (int u = 0; u < kTok; ++u) {
+                h = fma2(a[u], h, add[u]);
+                e[u] = fma2(over[u], minus, h);
+            }
+            T *px = dx, *pr = dr, *pg = dg;
+            dx += dx_step;
+            dr += dr_step;
+            dg += dg_step;
+            auto put = [&](int u, bool on, bool as_pairs) {
+                const uint64_t G = add2(vd(u), later);
+                later = mul2(a[u], G);
+                const uint64_t es = mul2(mul2(G, e[u]), s[u]);
+                if (on) dsum = add2(dsum, es);
+                at.put(px, on ? mul2(G, mi[u]) : 0, as_pairs);
+                at.put(pg, on ? mul2(mul2(G, add[u]), rest[u]) : 0, as_pairs);
+                at.put(pr, on ? mul2(es, fma2(mul2(s[u], dec), minus, dec)) : 0, as_pairs);
+            };
+            if (t0 + kTok <= len && out_pairs) {
+#pragma unroll
+                for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride) put(u, true, true);
+            } else {
+#pragma unroll
+                for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride)
+                    if (t0 + u < f.n) put(u, t0 + u < len, out_pairs);
+            }
+            if (++slot == kSlots) slot = 0;
         }
-        in.used(t0, step, at);
-        if (++slot == kSlotsBwd) slot = 0;
-        uint64_t back = mul2(a[kTok - 1], vd[kTok - 1]);
-#pragma unroll
-        for (int u = kTok - 2; u >= 0; --u) back = mul2(a[u], add2(vd[u], back));
-        const int buf = round & 1;
-        fwd[buf][group][lane] = forward;
-        bwd[buf][group][lane] = {forward.p, back};
-        uint64_t h = first;
-        first = state_before(tile + step);
-        uint64_t later = join<Sh, -1>(bwd[buf], others, round, S, rank, group, D);
-        for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);
-        uint64_t e[kTok];  // the derivative of the state by log a
-#pragma unroll
-        for (int u = 0; u < kTok; ++u) {
-            h = fma2(a[u], h, add[u]);
-            e[u] = fma2(over[u], minus, h);
-        }
-        const size_t end = (size_t)(t0 + kTok - 1);
-        T *px = dx + end * p.dx_stride, *pr = dr + end * p.dr_stride, *pg = dg + end * p.dg_stride;
-        auto put = [&](int u, bool on, bool as_pairs) {
-            const uint64_t G = add2(vd[u], later);
-            later = mul2(a[u], G);
-            const uint64_t es = mul2(mul2(G, e[u]), s[u]);
-            if (on) dsum = add2(dsum, es);
-            at.put(px, on ? mul2(G, mi[u]) : 0, as_pairs);
-            at.put(pg, on ? mul2(mul2(G, add[u]), rest[u]) : 0, as_pairs);
-            at.put(pr, on ? mul2(es, fma2(mul2(s[u], dec), minus, dec)) : 0, as_pairs);
-        };
-        if (t0 + kTok <= len && out_pairs) {
-#pragma unroll
-            for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride) put(u, true, true);
-        } else {
-#pragma unroll
-            for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride)
-                if (t0 + u < f.n) put(u, t0 + u < len, out_pairs);
-        }
-    }
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
@@ -617,7 +631,7 @@ cudaError_t launch_clusters(void (*kernel)(P...), long long units, int S, int sm
 template <typename T, int kLanes, bool kRing>
 cudaError_t forward_as(const Glr &p, const Spread &r, cudaStream_t s) {
     return launch_clusters(glr_forward_kernel<T, kLanes, kRing>, (long long)p.B * r.slabs, r.S,
-                           Tokens<T, FwdShape<T, kLanes>, 3, kSlotsFwd, kRing>::kSmem, s, p, r.slabs, r.S,
+                           Tokens<T, FwdShape<T, kLanes>, 3, kRing>::kSmem, s, p, r.slabs, r.S,
                            pairs_ok<T>(p.y, p.y_stride, p.C));
 }
 template <typename T>
@@ -642,7 +656,7 @@ cudaError_t backward_as(const GlrBwd &p, const Spread &r, cudaStream_t s) {
     const bool pairs = pairs_ok<T>(p.dx, p.dx_stride, f.C) && pairs_ok<T>(p.dr, p.dr_stride, f.C) &&
                        pairs_ok<T>(p.dg, p.dg_stride, f.C);
     const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kRing>, (long long)f.B * r.slabs, r.S,
-                                          Tokens<T, Shape<kLanes, 4>, 4, kSlotsBwd, kRing>::kSmem, s, p, r.slabs, r.S, pairs);
+                                          Tokens<T, Shape<kLanes, 4>, 4, kRing>::kSmem, s, p, r.slabs, r.S, pairs);
     if (e) return e;
     return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {{p.ddecay, 0, nullptr}}, f.dt, p.header}, s);
 }

@@ -361,3 +361,148 @@ def test_chain_on_other_streams_and_in_graphs(hla, dtype):
         graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(t, want) for t in got) and torch.equal(captured, want)
+
+
+def test_long_sequences_of_few_channels(hla):
+    """Blocks of a cluster that hand their runs on many times, with both shapes of a block."""
+    for B, n, C in ((1, 9000, 24), (1, 5000, 600), (2, 3001, 40), (3, 1500, 1100)):
+        g, v, lengths = glr_case(n, B, n, C, torch.bfloat16, B > 2)
+        want, last, bound, last_bound = R.glr(v["x"], v["r"], v["g"], v["decay"], v["state"], lengths)
+        so = torch.empty(B, C, device=DEV)
+        marks = torch.empty(B, hla.hla_glr_marks(n), C, device=DEV)
+        y = hla.hla_glr_forward(on(v["x"]), on(v["r"]), on(v["g"]), on(v["decay"]), lengths=on(lengths),
+                                state_in=on(v["state"]), state_out=so, marks=marks)
+        near("y", y, want, bound)
+        near("state", so, last, last_bound)
+        dy, dl = randn(g, B, n, C, T=torch.bfloat16), randn(g, B, C)
+        want = R.glr_grad(v["x"], v["r"], v["g"], v["decay"], dy, v["state"], dl, lengths)
+        di = torch.empty(B, C, device=DEV)
+        got = hla.hla_glr_backward(on(v["x"]), on(v["r"]), on(v["g"]), on(v["decay"]), on(dy), marks, dstate_out=on(dl),
+                                   dstate_in=di, lengths=on(lengths))
+        for name, t in zip(("dx", "dr", "dg", "ddecay", "dstate"), got + (di,)):
+            near(name, t, *want[name])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_more_than_2_31_elements_apart(hla, dtype):
+    """Offsets inside the tensors pass 32 bits: the same values in rows that are 2^29 and a bit elements apart."""
+    T, step, n, C = TYPES[dtype], (1 << 29) + 64, 6, 40
+    if torch.cuda.mem_get_info()[0] < 40e9:
+        pytest.skip("the device's memory is in use")
+    buf = torch.empty(n * step, dtype=T, device=DEV)
+    places = iter(range(0, 1 << 28, 1 << 20))
+
+    def far(values=None):
+        t = buf.as_strided((1, n, C), (n * step, step, 1), next(places))
+        return t if values is None else t.copy_(values)
+    g = gen(4)
+    x, r, gt, dy = (randn(g, 1, n, C, T=T).to(DEV) for _ in range(4))
+    decay = -torch.rand(C, generator=g).to(DEV) - 0.1
+    marks = torch.empty(1, 1, C, device=DEV)
+    fx, fr, fg, fdy = (far(t) for t in (x, r, gt, dy))
+    assert torch.equal(hla.hla_glr_forward(fx, fr, fg, decay, far(), marks=marks), hla.hla_glr_forward(x, r, gt, decay))
+    want = hla.hla_glr_backward(x, r, gt, decay, dy, marks)
+    got = hla.hla_glr_backward(fx, fr, fg, decay, fdy, marks, far(), far(), far())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    w = randn(g, C, T=T).to(DEV)
+    kw = dict(w_post=w, scale=w, w_pre=w, dropout=0.25, seed=5)
+    want = hla.hla_block_norm_forward(x, r, gt, **kw)
+    got = hla.hla_block_norm_forward(fx, fr, fg, far(), far(), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    want = hla.hla_block_norm_backward(x, r, gt, dy, x, **kw)
+    got = hla.hla_block_norm_backward(fx, fr, fg, fdy, fx, far(), far(), far(), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    wf = randn(g, 2, C, C, T=T).to(DEV)
+    assert torch.equal(hla.hla_ffn_forward(fx, wf, far()), hla.hla_ffn_forward(x, wf))
+    want, got = hla.hla_ffn_backward(x, wf, dy), hla.hla_ffn_backward(fx, wf, fdy, far())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_used_workspaces(hla, dtype):
+    """What a workspace held before does not matter, and a call leaves no error in it."""
+    T = TYPES[dtype]
+    for M, K, F in ((40, 72, 136), (300, 130, 260)):
+        g = gen(M)
+        x, w, d = randn(g, M, K, T=T).to(DEV), randn(g, 2, F, K, T=T).to(DEV), randn(g, M, F, T=T).to(DEV)
+        y, gate = randn(g, M, K, T=T).to(DEV), randn(g, M, K, T=T).to(DEV)
+        decay, marks = -torch.ones(K, device=DEV), torch.empty(1, hla.hla_glr_marks(M), K, device=DEV)
+        seq = [t[None] for t in (x, y, gate)]
+        hla.hla_glr_forward(*seq, decay, marks=marks)
+        for size, call in (
+                (hla.hla_ffn_workspace_bytes(M, K, F, T), lambda ws: [hla.hla_ffn_forward(x, w, workspace=ws)]),
+                (hla.hla_ffn_backward_workspace_bytes(M, K, F, T), lambda ws: hla.hla_ffn_backward(x, w, d, workspace=ws)),
+                (hla.hla_block_norm_backward_workspace_bytes(M, K, T),
+                 lambda ws: hla.hla_block_norm_backward(x, y, gate, y, x, w_pre=x[0], workspace=ws)),
+                (hla.hla_glr_backward_workspace_bytes(1, M, K, T),
+                 lambda ws: hla.hla_glr_backward(*seq, decay, seq[0], marks, workspace=ws))):
+            ws = hla.alloc_workspace(size, DEV)
+            want = [t.clone() for t in call(ws) if t is not None]
+            ws.fill_(255)
+            got = [t for t in call(ws) if t is not None]
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            hla.hla_poll_error(ws)
+
+
+def test_calls_on_another_stream_without_a_workspace(hla):
+    """Scratch and outputs of a call on another stream, while the current one goes on allocating and writing."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    x, r, gt, dy, w = rand(1, 700, 264), rand(1, 700, 264), rand(1, 700, 264), rand(1, 700, 264), rand(2, 520, 264)
+    decay, few = -torch.rand(264, generator=g, device=DEV) - 0.01, x[0, :20]
+    w_pre = decay.to(x.dtype)  # (an input lives as long as the kernels that read it)
+    marks = torch.empty(1, hla.hla_glr_marks(700), 264, device=DEV)
+    hla.hla_glr_forward(x, r, gt, decay, marks=marks)
+    calls = [lambda s: hla.hla_glr_forward(x, r, gt, decay, stream=s),
+             lambda s: hla.hla_glr_backward(x, r, gt, decay, dy, marks, stream=s),
+             lambda s: hla.hla_block_norm_forward(x, r, gt, dropout=0.5, seed=1, stream=s),
+             lambda s: hla.hla_block_norm_backward(x, r, gt, dy, x, w_pre=w_pre, stream=s),
+             lambda s: hla.hla_ffn_forward(x, w, stream=s), lambda s: hla.hla_ffn_backward(x, w, rand_out, stream=s),
+             lambda s: hla.hla_ffn_forward(few, w, stream=s), lambda s: hla.hla_ffn_backward(few, w, rand_out[0, :20], stream=s)]
+    rand_out = rand(1, 700, 520)
+    tensors = lambda out: [t for t in (out if isinstance(out, tuple) else (out,)) if t is not None]  # noqa: E731
+    want = [[t.clone() for t in tensors(call(None))] for call in calls]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(40_000_000)  # the calls' kernels run well after the calls return
+    got = []
+    for call in calls:
+        got.append(tensors(call(side)))
+        for size in (1 << 12, 1 << 18, 1 << 20, 1 << 22):
+            for _ in range(4):
+                torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255)
+    torch.cuda.current_stream().wait_stream(side)
+    assert [all(torch.equal(a, b) for a, b in zip(p, q)) for p, q in zip(got, want)] == [True] * len(calls)
+
+
+def test_gradients_in_graphs(hla):
+    """A training step captured twice, each graph with workspaces of its own, replayed by turns on new inputs."""
+    g = gen(8)
+    B, n, C, F, T = 2, 100, 136, 264, torch.bfloat16
+    v = {k: randn(g, B, n, C, T=T).to(DEV) for k in ("x", "r", "g", "dy")}
+    w, decay, wr = randn(g, 2, F, C, T=T).to(DEV), -torch.rand(C, generator=g).to(DEV) - 0.01, randn(g, C, T=T).to(DEV)
+    dout = randn(g, B, n, F, T=T).to(DEV)
+
+    def step():
+        marks = torch.empty(B, hla.hla_glr_marks(n), C, device=DEV)
+        y = hla.hla_glr_forward(v["x"], v["r"], v["g"], decay, marks=marks)
+        kw = dict(w_pre=wr, scale=wr, dropout=0.1, seed=2, offset=3)
+        x1, h = hla.hla_block_norm_forward(v["x"], y, v["g"], **kw)
+        dh, dw = hla.hla_ffn_backward(h, w, dout)
+        dn = hla.hla_block_norm_backward(v["x"], y, v["g"], v["dy"], dh, **kw)
+        return [hla.hla_ffn_forward(h, w), x1, dw] + [t for t in dn if t is not None] + list(
+            hla.hla_glr_backward(v["x"], v["r"], v["g"], decay, dn[1], marks))
+    step()
+    graphs, outs = [], []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(step())
+        graphs.append(graph)
+    for turn in range(4):
+        v["x"].normal_(), dout.normal_()
+        want = step()
+        graphs[turn % 2].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[turn % 2], want))
