@@ -272,9 +272,9 @@ __device__ __forceinline__ uint64_t after(const Run &r, uint64_t h) { return fma
 // What the blocks of a cluster tell one another, in two buffers by turns: a block writes a round's run over the one
 // of two rounds before, which every warp of the receiver has read before it sent its run of the last round, which the
 // writer has waited for.
-template <int kLanes>
+template <int kLanes, int kTiles>
 struct Exchange {
-    Run runs[2][kMaxCluster][kLanes], mine[2][kLanes];
+    Run runs[2][kMaxCluster][kTiles][kLanes], mine[2][kTiles][kLanes];
     uint64_t bar[2];
 };
 __device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
@@ -283,8 +283,8 @@ __device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
     return to;
 }
 // every block is there, its barriers ready
-template <int kLanes>
-__device__ __forceinline__ void open_exchange(Exchange<kLanes> &x, int S) {
+template <int kLanes, int kTiles>
+__device__ __forceinline__ void open_exchange(Exchange<kLanes, kTiles> &x, int S) {
     if (S == 1) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) mbar_init(&x.bar[i], 1);
@@ -302,36 +302,46 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
     return true;
 }
 
-// The state before this group's tokens and, in `state`, behind the cluster's round, from the runs of every group
-// (kOrder 1: in their order, -1: against it) and block.  The wait for the others' runs has a limit, after which the
-// states are NaN from there on, and so is what follows from them.
+// The state before this group's tokens and, in `state`, behind the block's tile, from the runs of every group
+// (kOrder 1: in their order, -1: against it)
 template <typename Sh, int kOrder>
-__device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLanes], Exchange<Sh::kLanes> &x, int round, int S,
-                                         unsigned rank, int group, uint64_t &state) {
+__device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLanes], int group, uint64_t &state) {
     const int lane = Sh::lane();
     __syncthreads();
-    if (S == 1) {
-        uint64_t mine = 0, h = state;
-#pragma unroll
-        for (int k = 0; k < Sh::kGroups; ++k) {
-            const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
-            if (w == group) mine = h;
-            h = after(runs[w][lane], h);
-        }
-        state = h;
-        return mine;
-    }
-    Run all{twice(1.f), 0}, before{twice(1.f), 0};
+    uint64_t mine = 0, h = state;
 #pragma unroll
     for (int k = 0; k < Sh::kGroups; ++k) {
         const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
-        if (w == group) before = all;
-        const Run r = runs[w][lane];
-        all = {mul2(r.p, all.p), after(r, all.l)};
+        if (w == group) mine = h;
+        h = after(runs[w][lane], h);
     }
-    const int buf = round & 1;
+    state = h;
+    return mine;
+}
+
+// The same for a cluster's S blocks, each with kTiles tiles of its own between two exchanges: the cluster's first tiles
+// (one a block) come before its second ones.  The wait for the others' runs has a limit, after which the states are NaN
+// from there on, and so is what follows from them.
+template <typename Sh, int kOrder, int kTiles>
+__device__ __forceinline__ void join_cluster(const Run (&runs)[kTiles][Sh::kGroups][Sh::kLanes],
+                                             Exchange<Sh::kLanes, kTiles> &x, int turn, int S, unsigned rank, int group,
+                                             uint64_t &state, uint64_t (&mine)[kTiles]) {
+    const int lane = Sh::lane(), buf = turn & 1;
+    Run before[kTiles];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        Run all{twice(1.f), 0};
+#pragma unroll
+        for (int k = 0; k < Sh::kGroups; ++k) {
+            const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
+            if (w == group) before[i] = all;
+            const Run r = runs[i][w][lane];
+            all = {mul2(r.p, all.p), after(r, all.l)};
+        }
+        if (threadIdx.x < Sh::kLanes) x.mine[buf][i][lane] = all;
+    }
     if (threadIdx.x < 32) {
-        if (threadIdx.x < Sh::kLanes) x.mine[buf][lane] = all;
         fence_async_smem();
         if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
         __syncwarp();
@@ -342,22 +352,26 @@ __device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLan
                          "r"(in_block(&x.bar[buf], threadIdx.x))
                          : "memory");
     }
-    if (state != kLost && !wait(&x.bar[buf], (round >> 1) & 1)) state = kLost;
-    uint64_t h = state, tile_in = 0;
-    for (int k0 = 0; k0 < S; k0 += 2) {  // (S is even)
-        Run r[2];
+    if (state != kLost && !wait(&x.bar[buf], (turn >> 1) & 1)) state = kLost;
+    uint64_t h = state;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) r[k] = x.runs[buf][kOrder > 0 ? k0 + k : S - 1 - k0 - k][lane];
+    for (int i = 0; i < kTiles; ++i) {
+        uint64_t tile_in = 0;
+        for (int k0 = 0; k0 < S; k0 += 2) {  // (S is even)
+            Run r[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if ((kOrder > 0 ? k0 + k : S - 1 - k0 - k) == (int)rank) tile_in = h;
-            h = after(r[k], h);
+            for (int k = 0; k < 2; ++k) r[k] = x.runs[buf][kOrder > 0 ? k0 + k : S - 1 - k0 - k][i][lane];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if ((kOrder > 0 ? k0 + k : S - 1 - k0 - k) == (int)rank) tile_in = h;
+                h = after(r[k], h);
+            }
         }
+        mine[i] = state == kLost ? kLost : after(before[i], tile_in);
     }
-    if (state == kLost) return kLost;
-    state = h;
-    return after(before, tile_in);
+    if (state != kLost) state = h;
 }
+
 // ------------------------------------------------------------------------------------------------
 // forward
 // ------------------------------------------------------------------------------------------------
@@ -365,13 +379,22 @@ __device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLan
 template <typename T, int kLanes>
 using FwdShape = Shape<kLanes, sizeof(T) == 2 ? 8 : 4>;
 
-template <typename T, int kLanes, bool kRing>
+// kTiles: tiles of a block between two exchanges with its cluster's others (1: a block alone).  The states of all but the
+// last one wait in shared memory.
+template <typename T, int kLanes, bool kRing, int kTiles>
+struct FwdSmem {
+    using In = Tokens<T, FwdShape<T, kLanes>, 3, kRing>;
+    static constexpr int kKept = (kTiles - 1) * FwdShape<T, kLanes>::kTok * kThreads * (int)sizeof(Run);
+    static constexpr int kBytes = In::kSmem + kKept;
+};
+
+template <typename T, int kLanes, bool kRing, int kTiles>
 __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int slabs, int S, bool y_pairs) {
     using Sh = FwdShape<T, kLanes>;
     constexpr int kTok = Sh::kTok;
-    extern __shared__ __align__(128) char ring[];
-    __shared__ Run runs[2][Sh::kGroups][kLanes];
-    __shared__ Exchange<kLanes> others;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ Run runs[kTiles == 1 ? 2 : 1][kTiles][Sh::kGroups][kLanes];
+    __shared__ Exchange<kLanes, kTiles> others;  // (kTiles > 1)
     let_next_begin();
     after_previous();
     const int group = Sh::group(), lane = Sh::lane();
@@ -388,46 +411,62 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     in.set(0, p.x, p.x_stride, row0, channel, t0, step);
     in.set(1, p.r, p.r_stride, row0, channel, t0, step);
     in.set(2, p.g, p.g_stride, row0, channel, t0, step);
-    in.open(ring, channel, p.C, len);
+    in.open(smem, channel, p.C, len);
     in.begin(t0, step, at);
+    Run *kept = reinterpret_cast<Run *>(smem + FwdSmem<T, kLanes, kRing, kTiles>::In::kSmem) + threadIdx.x;
     const Decay decay(at.get(p.decay, pairs));
     uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C, pairs) : 0;
     T *y = static_cast<T *>(p.y) + (row0 + t0) * p.y_stride;
     const long long y_step = step * p.y_stride;
-    open_exchange(others, S);
-    const int rounds = (int)(((long long)p.n + step - 1) / step);
+    if (kTiles > 1) open_exchange(others, S);
+    const int turns = (int)(((long long)p.n + kTiles * step - 1) / (kTiles * step));
     auto walk = [&](auto near) {
-        for (int round = 0, slot = 0; round < rounds; ++round, t0 += step) {
+        int slot = 0;
+        for (int turn = 0; turn < turns; ++turn) {
             uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
-            in.next(slot, t0, step, at);
+            const int buf = kTiles == 1 ? turn & 1 : 0;
 #pragma unroll
-            for (int u = 0; u < kTok; ++u) {
-                uint64_t a, w;
-                Raw<T, 2> rr = in.get(slot, 1, u);
-                if (t0 + u >= len) shut(rr);  // (x is 0 there)
-                decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
-                const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
-                // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-                const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
-                h[u] = u ? fma2(a, h[u - 1], add) : add;
-                pr[u] = u ? mul2(a, pr[u - 1]) : a;
+            for (int i = 0; i < kTiles; ++i, t0 += step) {
+                in.next(slot, t0, step, at);
+#pragma unroll
+                for (int u = 0; u < kTok; ++u) {
+                    uint64_t a, w;
+                    Raw<T, 2> rr = in.get(slot, 1, u);
+                    if (t0 + u >= len) shut(rr);  // (x is 0 there)
+                    decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
+                    const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
+                    // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
+                    const uint64_t add =
+                        mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
+                    h[u] = u ? fma2(a, h[u - 1], add) : add;
+                    pr[u] = u ? mul2(a, pr[u - 1]) : a;
+                    if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
+                }
+                in.used(t0, step, at);
+                if (++slot == kSlots) slot = 0;
+                runs[buf][i][group][lane] = {pr[kTok - 1], h[kTok - 1]};
             }
-            in.used(t0, step, at);
-            if (++slot == kSlots) slot = 0;
-            const int buf = round & 1;
-            runs[buf][group][lane] = {pr[kTok - 1], h[kTok - 1]};
-            const uint64_t before = join<Sh, 1>(runs[buf], others, round, S, rank, group, state);
-            if (p.marks && t0 % kGlrTile == 0 && t0 < p.n)
-                at.put(p.marks + ((size_t)b * glr_marks(p.n) + t0 / kGlrTile) * p.C, before, pairs);
-            T *to = y;
-            y += y_step;
-            if (t0 + kTok <= len && y_pairs) {
+            uint64_t before[kTiles];
+            if constexpr (kTiles == 1) before[0] = join<Sh, 1>(runs[buf][0], group, state);
+            else join_cluster<Sh, 1>(runs[0], others, turn, S, rank, group, state, before);
+            int t = t0 - kTiles * step;
 #pragma unroll
-                for (int u = 0; u < kTok; ++u, to += p.y_stride) at.put(to, fma2(pr[u], before, h[u]), true);
-            } else {
+            for (int i = 0; i < kTiles; ++i, t += step, y += y_step) {
+                if (p.marks && t % kGlrTile == 0 && t < p.n)
+                    at.put(p.marks + ((size_t)b * glr_marks(p.n) + t / kGlrTile) * p.C, before[i], pairs);
+                auto put = [&](T *to, int u, bool on, bool as_pairs) {
+                    const Run r = i + 1 < kTiles ? kept[(i * kTok + u) * kThreads] : Run{pr[u], h[u]};
+                    at.put(to, on ? after(r, before[i]) : 0, as_pairs);
+                };
+                T *to = y;
+                if (t + kTok <= len && y_pairs) {
 #pragma unroll
-                for (int u = 0; u < kTok; ++u, to += p.y_stride)
-                    if (t0 + u < p.n) at.put(to, t0 + u < len ? fma2(pr[u], before, h[u]) : 0, y_pairs);
+                    for (int u = 0; u < kTok; ++u, to += p.y_stride) put(to, u, true, true);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kTok; ++u, to += p.y_stride)
+                        if (t + u < p.n) put(to, u, t + u < len, y_pairs);
+                }
             }
         }
     };
@@ -435,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     else walk(std::false_type());
     if (p.state_out && rank == 0 && group == 0) at.put(p.state_out + (size_t)b * p.C, state, pairs);
     ring_wait<0>();
-    if (S > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
+    if (kTiles > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -473,8 +512,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     using Sh = Shape<kLanes, 4>;
     constexpr int kTok = Sh::kTok;
     extern __shared__ __align__(128) char ring[];
-    __shared__ Run fwd[2][Sh::kGroups][kLanes], bwd[2][Sh::kGroups][kLanes];
-    __shared__ Exchange<kLanes> others;
+    __shared__ Run fwd[2][Sh::kGroups][kLanes], bwd[2][1][Sh::kGroups][kLanes];
+    __shared__ Exchange<kLanes, 1> others;
     let_next_begin();
     after_previous();
     const Glr &f = p.f;
@@ -541,10 +580,17 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
             for (int u = kTok - 2; u >= 0; --u) back = mul2(a[u], add2(vd(u), back));
             const int buf = round & 1;
             fwd[buf][group][lane] = forward;
-            bwd[buf][group][lane] = {forward.p, back};
+            bwd[buf][0][group][lane] = {forward.p, back};
             uint64_t h = first;
             first = state_before(tile + step);
-            uint64_t later = join<Sh, -1>(bwd[buf], others, round, S, rank, group, D);
+            uint64_t later;
+            if (S == 1) {
+                later = join<Sh, -1>(bwd[buf][0], group, D);
+            } else {
+                uint64_t mine[1];
+                join_cluster<Sh, -1>(bwd[buf], others, round, S, rank, group, D, mine);
+                later = mine[0];
+            }
             for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);
             uint64_t e[kTok];  // the derivative of the state by log a
 #pragma unroll
@@ -630,9 +676,12 @@ cudaError_t launch_clusters(void (*kernel)(P...), long long units, int S, int sm
 
 template <typename T, int kLanes, bool kRing>
 cudaError_t forward_as(const Glr &p, const Spread &r, cudaStream_t s) {
-    return launch_clusters(glr_forward_kernel<T, kLanes, kRing>, (long long)p.B * r.slabs, r.S,
-                           Tokens<T, FwdShape<T, kLanes>, 3, kRing>::kSmem, s, p, r.slabs, r.S,
-                           pairs_ok<T>(p.y, p.y_stride, p.C));
+    const bool pairs = pairs_ok<T>(p.y, p.y_stride, p.C);
+    const long long units = (long long)p.B * r.slabs;
+    return r.S == 1 ? launch_clusters(glr_forward_kernel<T, kLanes, kRing, 1>, units, 1, FwdSmem<T, kLanes, kRing, 1>::kBytes, s, p,
+                                      r.slabs, 1, pairs)
+                    : launch_clusters(glr_forward_kernel<T, kLanes, kRing, 2>, units, r.S,
+                                      FwdSmem<T, kLanes, kRing, 2>::kBytes, s, p, r.slabs, r.S, pairs);
 }
 template <typename T>
 cudaError_t forward_of(const Glr &p, cudaStream_t s) {
