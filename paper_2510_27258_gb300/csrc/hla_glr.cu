@@ -28,7 +28,7 @@ constexpr int kMaxCluster = 16;
 constexpr int kSlots = 2;  // a round in use, the next in flight (3: 57.3 and 124.9 us on B8 n2048 C2048 bf16 instead of 56.3 and 124.5)
 constexpr int kSMs = 152;
 constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
-constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN: a wait ran out
+constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN, for states behind a wait that ran out
 constexpr float kLog2e = 1.44269504f;
 constexpr float kTiny = 1e-37f;               // beside 1 - a^2: keeps 1/m finite where a is 1
 
@@ -320,12 +320,12 @@ __device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLan
 }
 
 // The same for a cluster's S blocks, each with kTiles tiles of its own between two exchanges: the cluster's first tiles
-// (one a block) come before its second ones.  The wait for the others' runs has a limit, after which the states are NaN
-// from there on, and so is what follows from them.
+// (one a block) come before its second ones.  The wait for the others' runs has a limit, after which (`lost`) the states
+// are NaN from there on, and so is what follows from them.
 template <typename Sh, int kOrder, int kTiles>
 __device__ __forceinline__ void join_cluster(const Run (&runs)[kTiles][Sh::kGroups][Sh::kLanes],
                                              Exchange<Sh::kLanes, kTiles> &x, int turn, int S, unsigned rank, int group,
-                                             uint64_t &state, uint64_t (&mine)[kTiles]) {
+                                             bool &lost, uint64_t &state, uint64_t (&mine)[kTiles]) {
     const int lane = Sh::lane(), buf = turn & 1;
     Run before[kTiles];
     __syncthreads();
@@ -352,8 +352,8 @@ __device__ __forceinline__ void join_cluster(const Run (&runs)[kTiles][Sh::kGrou
                          "r"(in_block(&x.bar[buf], threadIdx.x))
                          : "memory");
     }
-    if (state != kLost && !wait(&x.bar[buf], (turn >> 1) & 1)) state = kLost;
-    uint64_t h = state;
+    if (!lost) lost = !wait(&x.bar[buf], (turn >> 1) & 1);
+    uint64_t h = lost ? kLost : state;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         uint64_t tile_in = 0;
@@ -367,9 +367,9 @@ __device__ __forceinline__ void join_cluster(const Run (&runs)[kTiles][Sh::kGrou
                 h = after(r[k], h);
             }
         }
-        mine[i] = state == kLost ? kLost : after(before[i], tile_in);
+        mine[i] = lost ? kLost : after(before[i], tile_in);
     }
-    if (state != kLost) state = h;
+    state = h;
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -420,6 +420,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     const long long y_step = step * p.y_stride;
     if (kTiles > 1) open_exchange(others, S);
     const int turns = (int)(((long long)p.n + kTiles * step - 1) / (kTiles * step));
+    bool lost = false;
     auto walk = [&](auto near) {
         int slot = 0;
         for (int turn = 0; turn < turns; ++turn) {
@@ -448,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
             }
             uint64_t before[kTiles];
             if constexpr (kTiles == 1) before[0] = join<Sh, 1>(runs[buf][0], group, state);
-            else join_cluster<Sh, 1>(runs[0], others, turn, S, rank, group, state, before);
+            else join_cluster<Sh, 1>(runs[0], others, turn, S, rank, group, lost, state, before);
             int t = t0 - kTiles * step;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t += step, y += y_step) {
@@ -550,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     open_exchange(others, S);
     const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
+    bool lost = false;
     auto walk = [&](auto near) {
         for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
             uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok];  // .., m i, 1 - i, b, i x / m
@@ -588,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
                 later = join<Sh, -1>(bwd[buf][0], group, D);
             } else {
                 uint64_t mine[1];
-                join_cluster<Sh, -1>(bwd[buf], others, round, S, rank, group, D, mine);
+                join_cluster<Sh, -1>(bwd[buf], others, round, S, rank, group, lost, D, mine);
                 later = mine[0];
             }
             for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);

@@ -199,6 +199,27 @@ def test_glr_is_causal_for_tokens_that_are_not_finite(hla, which, bad):
     assert torch.equal(got, clean)
 
 
+@pytest.mark.parametrize("B,n,C", [(1, 3000, 66), (2, 700, 130), (40, 70, 66)])
+def test_glr_states_that_are_nan(hla, B, n, C):
+    """NaN in every channel: the states of a whole sequence turn to NaN, and blocks of one sequence still meet."""
+    _, v, _ = glr_case(n, B, n, C, torch.float32, False)
+    x, r, g, decay = (on(v[k]) for k in ("x", "r", "g", "decay"))
+    marks = torch.empty(B, hla.hla_glr_marks(n), C, device=DEV)
+    clean = hla.hla_glr_forward(x, r, g, decay, marks=marks)
+    grads = hla.hla_glr_backward(x, r, g, decay, x, marks)
+    bad, at = x.clone(), n // 3
+    bad[0, at] = float("nan")
+    state = torch.empty(B, C, device=DEV)
+    y = hla.hla_glr_forward(bad, r, g, decay, state_out=state)
+    assert torch.isnan(y[0, at:]).all() and torch.isnan(state[0]).all()
+    assert torch.equal(y[0, :at], clean[0, :at]) and torch.equal(y[1:], clean[1:])
+    got = hla.hla_glr_backward(x, r, g, decay, bad, marks)  # a gradient that is NaN there, in tokens before it
+    for a, b in zip(got[:3], grads):
+        assert torch.isnan(a[0, :at + 1]).all()
+        assert torch.equal(a[0, at + 1:], b[0, at + 1:]) and torch.equal(a[1:], b[1:])
+    assert torch.isnan(got[3]).all()
+
+
 # ---------------------------------------------------------------------------------- norms
 
 NORM = [((1, 1), dict()), ((5, 8), dict(dropout=0.5)), ((37, 203), dict(dropout=0.1, gate=False)),
