@@ -24,7 +24,8 @@ namespace {
 using namespace sm103;
 
 constexpr int kThreads = 256;
-constexpr int kMaxCluster = 16;
+template <int kLanes>
+constexpr int kMostBlocks = kLanes == 32 ? 8 : 16;  // of a cluster
 constexpr int kSlots = 2;  // a round in use, the next in flight (3: 57.3 and 124.9 us on B8 n2048 C2048 bf16 instead of 56.3 and 124.5)
 constexpr int kSMs = 152;
 constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
@@ -274,7 +275,7 @@ __device__ __forceinline__ uint64_t after(const Run &r, uint64_t h) { return fma
 // writer has waited for.
 template <int kLanes, int kTiles>
 struct Exchange {
-    Run runs[2][kMaxCluster][kTiles][kLanes], mine[2][kTiles][kLanes];
+    Run runs[2][kMostBlocks<kLanes>][kTiles][kLanes], mine[2][kTiles][kLanes];
     uint64_t bar[2];
 };
 __device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
@@ -302,75 +303,103 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
     return true;
 }
 
-// The state before this group's tokens and, in `state`, behind the block's tile, from the runs of every group
-// (kOrder 1: in their order, -1: against it)
+// A warp's groups as one run: returns it, and in `before` what comes before the lane's group within the warp
 template <typename Sh, int kOrder>
-__device__ __forceinline__ uint64_t join(const Run (&runs)[Sh::kGroups][Sh::kLanes], int group, uint64_t &state) {
-    const int lane = Sh::lane();
-    __syncthreads();
-    uint64_t mine = 0, h = state;
-#pragma unroll
-    for (int k = 0; k < Sh::kGroups; ++k) {
-        const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
-        if (w == group) mine = h;
-        h = after(runs[w][lane], h);
-    }
-    state = h;
-    return mine;
+__device__ __forceinline__ Run of_warp(const Run &mine, Run &before) {
+    before = {twice(1.f), 0};
+    if constexpr (Sh::kOfWarp == 1) return mine;
+    const Run other{__shfl_xor_sync(0xffffffffu, mine.p, 16), __shfl_xor_sync(0xffffffffu, mine.l, 16)};
+    const bool second = ((threadIdx.x & 16) != 0) == (kOrder > 0);
+    if (second) before = other;
+    const Run &first = second ? other : mine, &then = second ? mine : other;
+    return {mul2(then.p, first.p), after(then, first.l)};
 }
 
-// The same for a cluster's S blocks, each with kTiles tiles of its own between two exchanges: the cluster's first tiles
-// (one a block) come before its second ones.  The wait for the others' runs has a limit, after which (`lost`) the states
-// are NaN from there on, and so is what follows from them.
-template <typename Sh, int kOrder, int kTiles>
-__device__ __forceinline__ void join_cluster(const Run (&runs)[kTiles][Sh::kGroups][Sh::kLanes],
-                                             Exchange<Sh::kLanes, kTiles> &x, int turn, int S, unsigned rank, int group,
-                                             bool &lost, uint64_t &state, uint64_t (&mine)[kTiles]) {
-    const int lane = Sh::lane(), buf = turn & 1;
-    Run before[kTiles];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        Run all{twice(1.f), 0};
-#pragma unroll
-        for (int k = 0; k < Sh::kGroups; ++k) {
-            const int w = kOrder > 0 ? k : Sh::kGroups - 1 - k;
-            if (w == group) before[i] = all;
-            const Run r = runs[i][w][lane];
-            all = {mul2(r.p, all.p), after(r, all.l)};
+constexpr int kWarps = kThreads / 32;
+template <int kLanes>
+using Runs = Run[kWarps][kLanes];
+
+// Joining a tile's runs (kOrder 1: in the warps' order, -1: against it).  Every warp takes those before its own; the last
+// one has the tile's, and hands the state behind it to the next tile's warps (`carry`, two places by turns).
+template <typename Sh, int kOrder>
+struct Joint {
+    int warp, place, lane;  // place: in the joining order
+    __device__ __forceinline__ Joint() : lane(Sh::lane()) {
+        warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+        place = kOrder > 0 ? warp : kWarps - 1 - warp;
+    }
+    __device__ __forceinline__ bool last() const { return place == kWarps - 1; }
+    __device__ __forceinline__ bool speaks() const { return (threadIdx.x & 31) < Sh::kLanes; }
+    __device__ __forceinline__ const Run &run(const Runs<Sh::kLanes> &runs, int k) const {
+        return runs[kOrder > 0 ? k : kWarps - 1 - k][lane];
+    }
+    __device__ __forceinline__ void tell(Runs<Sh::kLanes> &runs, const Run &mine) const {
+        if (speaks()) runs[warp][lane] = mine;
+    }
+    // The state before the lane's group; in the last warp `end` is the one behind the tile
+    __device__ __forceinline__ uint64_t alone(const Runs<Sh::kLanes> &runs, uint64_t (&carry)[2][Sh::kLanes], int turn,
+                                              const Run &mine, const Run &before, uint64_t &end) const {
+        __syncthreads();
+        uint64_t h = carry[(turn + 1) & 1][lane];
+        for (int k = 0; k < place; ++k) h = after(run(runs, k), h);
+        if (last()) {
+            end = after(mine, h);
+            if (speaks()) carry[turn & 1][lane] = end;
         }
-        if (threadIdx.x < Sh::kLanes) x.mine[buf][i][lane] = all;
+        return Sh::kOfWarp == 1 ? h : after(before, h);
     }
-    if (threadIdx.x < 32) {
-        fence_async_smem();
-        if (threadIdx.x == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
-        __syncwarp();
-        if (threadIdx.x < S)
-            asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                             in_block(x.runs[buf][rank], threadIdx.x)),
-                         "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])),
-                         "r"(in_block(&x.bar[buf], threadIdx.x))
-                         : "memory");
-    }
-    if (!lost) lost = !wait(&x.bar[buf], (turn >> 1) & 1);
-    uint64_t h = lost ? kLost : state;
+    // The same for a cluster's S blocks, each with kTiles tiles of its own between two exchanges: the cluster's first
+    // tiles (one a block) come before its second ones.  `state`: behind the round, in every warp.  The wait for the
+    // others' runs has a limit, after which (`lost`) the states are NaN from there on, and so is what follows from them.
+    template <int kTiles>
+    __device__ __forceinline__ void among(const Runs<Sh::kLanes> (&runs)[kTiles], Exchange<Sh::kLanes, kTiles> &x, int turn, int S,
+                                          unsigned rank, const Run (&mine)[kTiles], const Run (&before)[kTiles], bool &lost,
+                                          uint64_t &state, uint64_t (&got)[kTiles]) const {
+        const int buf = turn & 1;
+        Run ahead[kTiles];
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        uint64_t tile_in = 0;
-        for (int k0 = 0; k0 < S; k0 += 2) {  // (S is even)
-            Run r[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) r[k] = x.runs[buf][kOrder > 0 ? k0 + k : S - 1 - k0 - k][i][lane];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if ((kOrder > 0 ? k0 + k : S - 1 - k0 - k) == (int)rank) tile_in = h;
-                h = after(r[k], h);
+        for (int i = 0; i < kTiles; ++i) {
+            ahead[i] = {twice(1.f), 0};
+            for (int k = 0; k < place; ++k) {
+                const Run r = run(runs[i], k);
+                ahead[i] = {mul2(r.p, ahead[i].p), after(r, ahead[i].l)};
             }
+            if (last() && speaks()) x.mine[buf][i][lane] = {mul2(mine[i].p, ahead[i].p), after(mine[i], ahead[i].l)};
         }
-        mine[i] = lost ? kLost : after(before[i], tile_in);
+        if (last()) {
+            fence_async_smem();
+            const int to = threadIdx.x & 31;
+            if (to == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
+            __syncwarp();
+            if (to < S)
+                asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 in_block(x.runs[buf][rank], to)),
+                             "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])), "r"(in_block(&x.bar[buf], to))
+                             : "memory");
+        }
+        if (!lost) lost = !wait(&x.bar[buf], (turn >> 1) & 1);
+        uint64_t h = lost ? kLost : state;
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            uint64_t tile_in = 0;
+            for (int k0 = 0; k0 < S; k0 += 2) {  // (S is even)
+                Run r[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) r[k] = x.runs[buf][kOrder > 0 ? k0 + k : S - 1 - k0 - k][i][lane];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if ((kOrder > 0 ? k0 + k : S - 1 - k0 - k) == (int)rank) tile_in = h;
+                    h = after(r[k], h);
+                }
+            }
+            got[i] = after(ahead[i], tile_in);
+            if (Sh::kOfWarp > 1) got[i] = after(before[i], got[i]);
+            if (lost) got[i] = kLost;
+        }
+        state = h;
     }
-    state = h;
-}
+};
 
 // ------------------------------------------------------------------------------------------------
 // forward
@@ -393,7 +422,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     using Sh = FwdShape<T, kLanes>;
     constexpr int kTok = Sh::kTok;
     extern __shared__ __align__(128) char smem[];
-    __shared__ Run runs[kTiles == 1 ? 2 : 1][kTiles][Sh::kGroups][kLanes];
+    __shared__ Runs<kLanes> runs[2][kTiles];
+    __shared__ uint64_t carry[2][kLanes];        // (kTiles 1)
     __shared__ Exchange<kLanes, kTiles> others;  // (kTiles > 1)
     let_next_begin();
     after_previous();
@@ -418,14 +448,17 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C, pairs) : 0;
     T *y = static_cast<T *>(p.y) + (row0 + t0) * p.y_stride;
     const long long y_step = step * p.y_stride;
+    const Joint<Sh, 1> joint;
     if (kTiles > 1) open_exchange(others, S);
+    else if (joint.last() && joint.speaks()) carry[1][lane] = state;
     const int turns = (int)(((long long)p.n + kTiles * step - 1) / (kTiles * step));
     bool lost = false;
     auto walk = [&](auto near) {
         int slot = 0;
         for (int turn = 0; turn < turns; ++turn) {
             uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
-            const int buf = kTiles == 1 ? turn & 1 : 0;
+            Run mine[kTiles], ahead[kTiles];
+            const int buf = turn & 1;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t0 += step) {
                 in.next(slot, t0, step, at);
@@ -445,11 +478,12 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
                 }
                 in.used(t0, step, at);
                 if (++slot == kSlots) slot = 0;
-                runs[buf][i][group][lane] = {pr[kTok - 1], h[kTok - 1]};
+                mine[i] = of_warp<Sh, 1>({pr[kTok - 1], h[kTok - 1]}, ahead[i]);
+                joint.tell(runs[buf][i], mine[i]);
             }
             uint64_t before[kTiles];
-            if constexpr (kTiles == 1) before[0] = join<Sh, 1>(runs[buf][0], group, state);
-            else join_cluster<Sh, 1>(runs[0], others, turn, S, rank, group, lost, state, before);
+            if constexpr (kTiles == 1) before[0] = joint.alone(runs[buf][0], carry, turn, mine[0], ahead[0], state);
+            else joint.among(runs[buf], others, turn, S, rank, mine, ahead, lost, state, before);
             int t = t0 - kTiles * step;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t += step, y += y_step) {
@@ -473,7 +507,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
-    if (p.state_out && rank == 0 && group == 0) at.put(p.state_out + (size_t)b * p.C, state, pairs);
+    // (a block alone: the last warp has it)
+    if (p.state_out && rank == 0 && joint.last() && joint.speaks()) at.put(p.state_out + (size_t)b * p.C, state, pairs);
     ring_wait<0>();
     if (kTiles > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
 }
@@ -513,8 +548,9 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     using Sh = Shape<kLanes, 4>;
     constexpr int kTok = Sh::kTok;
     extern __shared__ __align__(128) char ring[];
-    __shared__ Run fwd[2][Sh::kGroups][kLanes], bwd[2][1][Sh::kGroups][kLanes];
-    __shared__ Exchange<kLanes, 1> others;
+    __shared__ Runs<kLanes> fwd[2], bwd[2][1];
+    __shared__ uint64_t carry[2][kLanes];   // (S 1)
+    __shared__ Exchange<kLanes, 1> others;  // (S > 1)
     let_next_begin();
     after_previous();
     const Glr &f = p.f;
@@ -548,7 +584,9 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
         return (unsigned)t < (unsigned)f.n ? at.get(mark + (size_t)(t / kGlrTile) * f.C, pairs) : 0;
     };
     uint64_t first = state_before(tile);  // the state before the tile
-    open_exchange(others, S);
+    const Joint<Sh, -1> joint;
+    if (S > 1) open_exchange(others, S);
+    else if (joint.last() && joint.speaks()) carry[1][lane] = D;
     const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
     bool lost = false;
@@ -577,23 +615,28 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
                 forward = u ? Run{mul2(a[u], forward.p), fma2(a[u], forward.l, add[u])} : Run{a[u], add[u]};
             }
             in.used(t0, step, at);
+            const uint64_t own = forward.p;
             uint64_t back = mul2(a[kTok - 1], vd(kTok - 1));
 #pragma unroll
             for (int u = kTok - 2; u >= 0; --u) back = mul2(a[u], add2(vd(u), back));
             const int buf = round & 1;
-            fwd[buf][group][lane] = forward;
-            bwd[buf][0][group][lane] = {forward.p, back};
+            Run in_warp, mine[1], ahead[1];
+            forward = of_warp<Sh, 1>(forward, in_warp);
+            if (joint.speaks()) fwd[buf][joint.warp][lane] = forward;
+            mine[0] = of_warp<Sh, -1>({own, back}, ahead[0]);
+            joint.tell(bwd[buf][0], mine[0]);
             uint64_t h = first;
             first = state_before(tile + step);
             uint64_t later;
             if (S == 1) {
-                later = join<Sh, -1>(bwd[buf][0], group, D);
+                later = joint.alone(bwd[buf][0], carry, round, mine[0], ahead[0], D);
             } else {
-                uint64_t mine[1];
-                join_cluster<Sh, -1>(bwd[buf], others, round, S, rank, group, lost, D, mine);
-                later = mine[0];
+                uint64_t got[1];
+                joint.among(bwd[buf], others, round, S, rank, mine, ahead, lost, D, got);
+                later = got[0];
             }
-            for (int k = 0; k < group; ++k) h = after(fwd[buf][k][lane], h);
+            for (int k = 0; k < joint.warp; ++k) h = after(fwd[buf][k][lane], h);
+            if (Sh::kOfWarp > 1) h = after(in_warp, h);
             uint64_t e[kTok];  // the derivative of the state by log a
 #pragma unroll
             for (int u = 0; u < kTok; ++u) {
@@ -626,14 +669,15 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
-    if (p.dstate_in && rank == 0 && group == 0) at.put(p.dstate_in + (size_t)b * f.C, D, pairs);
-    // decay's gradient: the block's groups in order, then (another kernel) its blocks
+    if (p.dstate_in && rank == 0 && joint.last() && joint.speaks()) at.put(p.dstate_in + (size_t)b * f.C, D, pairs);
+    // decay's gradient: the block's warps in order, then (another kernel) its blocks
+    if (Sh::kOfWarp > 1) dsum = add2(dsum, __shfl_xor_sync(0xffffffffu, dsum, 16));
     __syncthreads();
-    fwd[0][group][lane].p = dsum;
+    if (joint.speaks()) fwd[0][joint.warp][lane].p = dsum;
     __syncthreads();
-    if (group == 0) {
+    if (threadIdx.x < kLanes) {
 #pragma unroll
-        for (int k = 1; k < Sh::kGroups; ++k) dsum = add2(dsum, fwd[0][k][lane].p);
+        for (int k = 1; k < kWarps; ++k) dsum = add2(dsum, fwd[0][k][lane].p);
         at.put(p.partial + ((size_t)b * S + rank) * f.C, dsum, pairs);
     }
     ring_wait<0>();
