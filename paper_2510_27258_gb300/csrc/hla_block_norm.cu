@@ -9,8 +9,8 @@
 //   dy = r1 (q scale w_post - u mean(q scale w_post u)),  dgate = t k scale u w_post act'(gate),
 //   dw_post = scale sum q u,  dscale = w_post sum q u,  dw_pre = sum dh x' r2   (sums over rows).
 //
-// Bound by memory traffic: every tensor is read and written once.  A row belongs to a block (up to 256 columns: to a
-// warp), eight columns a thread in registers, with the block's next row in flight; blocks stay for many rows, so
+// Bound by memory traffic: every tensor is read and written once.  A row belongs to a block (up to 256 columns: to 4 to 32
+// lanes), eight columns a thread in registers, with the block's next row in flight; blocks stay for many rows, so
 // that the weights are loaded once and the gradient's sums over rows stay in registers.  What does not depend on a
 // row's sum (gate, random bits) is done while the sum's barrier is waited for.  Rows of more than 8192 columns are
 // walked several times by one block.  Statistics, products and sums are fp32; each output is rounded once.
@@ -23,8 +23,9 @@ namespace {
 
 constexpr int kPer = 8;                        // columns of a thread
 constexpr int kNarrow = 32 * kPer, kWide = 1024 * kPer;
-constexpr int kMaxWarps = 32, kNarrowRows = 4;
+constexpr int kMaxWarps = 32, kNarrowThreads = 128;
 constexpr int kFwdThreads = 512, kBwdThreads = 512;  // threads of an SM at a time
+constexpr int block_of(int kMax) { return kMax > 32 ? kMax : kNarrowThreads; }
 
 constexpr uint32_t kMul0 = 0xD2511F53u, kMul1 = 0xCD9E8D57u;
 constexpr int kRounds = 10;
@@ -170,30 +171,50 @@ struct Cols {
     }
 };
 
-// zeros in the places of dropped values
+// Zeros in the places of dropped values.  Where a thread's accesses are narrower than the generator's four words, the
+// lanes that share a group of four columns each make the words of two of their eight groups and exchange them.
 template <int kV>
 struct Drop {
-    Group group[kV == 1 ? 1 : 2];
+    static constexpr int kShare = kV >= 4 ? 1 : 4 / kV;  // lanes to a group
+    Group group[2];
     __device__ __forceinline__ void open(const BlockNorm &p, int t, int threads) {
-        if (kV == 1 || !p.drop) return;
+        if (!p.drop) return;
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-            group[j].set(p, (uint32_t)((4 * j / kV * threads + t) * kV + 4 * j % kV) >> 2);
+        for (int j = 0; j < 2; ++j) {
+            const int e = kV >= 4 ? 4 * j / kV : t % kShare + j * kShare;
+            group[j].set(p, (uint32_t)((e * threads + t) * kV + (kV >= 4 ? 4 * j % kV : 0)) >> 2);
+        }
+    }
+    // lanes o = 0, 1 or 0 .. 3 that share groups, each with the words of group o, come to have their own words of all
+    static __device__ __forceinline__ void exchange(Words &w, int t) {
+        if constexpr (kV == 2) {
+            const bool odd = t & 1;
+            const uint32_t a = __shfl_xor_sync(0xffffffffu, odd ? w.w[0] : w.w[2], 1),
+                           b = __shfl_xor_sync(0xffffffffu, odd ? w.w[1] : w.w[3], 1);
+            w = odd ? Words{{a, b, w.w[2], w.w[3]}} : Words{{w.w[0], w.w[1], a, b}};
+        } else if constexpr (kV == 1) {
+#pragma unroll
+            for (int o = 1; o < 4; o *= 2) {
+                const bool high = t & o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i & o) continue;
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, high ? w.w[i] : w.w[i | o], o);
+                    if (high) w.w[i] = got; else w.w[i | o] = got;
+                }
+            }
+        }
     }
     template <int kN>
-    __device__ __forceinline__ void apply(const BlockNorm &p, long long row, int t, int threads, Pairs (&v)[kN]) const {
+    __device__ __forceinline__ void apply(const BlockNorm &p, long long row, int t, Pairs (&v)[kN]) const {
         bool keep[kPer];
-        if constexpr (kV == 1) {
+        const uint64_t of_row = row_of(p, (uint32_t)row);
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) keep[e] = kept(p, row, e * threads + t);
-        } else {
-            const uint64_t of_row = row_of(p, (uint32_t)row);
+        for (int j = 0; j < 2; ++j) {
+            Words w = words_of(p, group[j], of_row);
+            exchange(w, t);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const Words w = words_of(p, group[j], of_row);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) keep[4 * j + i] = w.w[i] >= p.drop_below;
-            }
+            for (int i = 0; i < 4; ++i) keep[4 * j + i] = w.w[i] >= p.drop_below;
         }
 #pragma unroll
         for (int n = 0; n < kN; ++n)
@@ -220,7 +241,7 @@ struct Rows {
     C8 ahead[kSlots == 1 ? kTensors : 1];
 
     __device__ __forceinline__ char *place(int slot, int i, int e) const {
-        return ring + ((slot * kTensors + i) * C8::kE + e) * (int)blockDim.x * 16;
+        return ring + ((slot * kTensors + i) * C8::kE + e) * (int)(blockDim.x * sizeof(Raw<T, kV>));
     }
     __device__ __forceinline__ void send(int slot, long long row) const {
         if constexpr (kSlots > 1) {
@@ -238,7 +259,7 @@ struct Rows {
     }
     __device__ __forceinline__ void begin(char *smem, long long row) {
         if constexpr (kSlots > 1) {
-            ring = smem + threadIdx.x * 16;
+            ring = smem + threadIdx.x * sizeof(Raw<T, kV>);
 #pragma unroll
             for (int k = 0; k < kSlots - 1; ++k) send(k, row + k * step);
         } else {
@@ -269,7 +290,7 @@ struct Rows {
         } else if constexpr (kSlots == 1) {
             c = ahead[i];
         } else {
-            c.load(from[i] + row * stride[i], t, threads, C);
+            c.load(from[i] + row * stride[i], t, threads, row < rows ? C : 0);
         }
         c.get(v);
     }
@@ -279,8 +300,8 @@ struct Rows {
 // 68.6 us against 75.3 on B8 n2048 C2048 bf16 (the gradient, whose registers would spill: 159 against 124.6).
 template <typename T, int kV, int kMax>
 constexpr int slots() {
-    constexpr int bytes = 5 * (kMax ? kMax : 128) * kPer * (int)sizeof(T);
-    return kV == 1 ? 0 : 3 * bytes <= 64 * 1024 || (kMax == 512 && 3 * bytes <= 160 * 1024) ? 3 : 2 * bytes <= 200 * 1024 ? 2 : 0;
+    constexpr int bytes = 5 * (kMax > 32 ? kMax : kNarrowThreads) * kPer * (int)sizeof(T);
+    return sizeof(Raw<T, kV>) < 4 ? 0 : 3 * bytes <= 64 * 1024 || (kMax == 512 && 3 * bytes <= 160 * 1024) ? 3 : 2 * bytes <= 200 * 1024 ? 2 : 0;
 }
 template <typename T>
 size_t ring_bytes(int threads, int slots) { return (size_t)slots * 5 * threads * kPer * sizeof(T); }
@@ -298,15 +319,15 @@ __device__ __forceinline__ void weight(const void *w, int t, int threads, int C,
     c.get(v);
 }
 
-// Sums of kN values over a warp, or over a block through `red` (two buffers in turn: one barrier a sum)
+// Sums of kN values over a row's lanes, or over a block through `red` (two buffers in turn: one barrier a sum)
 template <int kN>
 struct Sum {
     float v[kN];
 };
-template <int kN>
-__device__ __forceinline__ void warp_sum(Sum<kN> &s) {
+template <int kLanes, int kN>
+__device__ __forceinline__ void lane_sum(Sum<kN> &s) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = kLanes / 2; o > 0; o >>= 1)
 #pragma unroll
         for (int i = 0; i < kN; ++i) s.v[i] += __shfl_xor_sync(0xffffffffu, s.v[i], o);
 }
@@ -316,16 +337,16 @@ __device__ __forceinline__ void add_up(uint64_t v, float &sum) {
     sum = a + b;
 }
 // tell: this warp's part; read: the row's sum, behind a barrier
-template <bool kBlock, int kN>
+template <int kMax, int kN>
 __device__ __forceinline__ void tell(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int turn) {
-    warp_sum(s);
-    if (kBlock && (threadIdx.x & 31) == 0)
+    lane_sum<(kMax > 32 ? 32 : kMax)>(s);
+    if (kMax > 32 && (threadIdx.x & 31) == 0)
 #pragma unroll
         for (int i = 0; i < kN; ++i) red[turn][i][threadIdx.x >> 5] = s.v[i];
 }
 template <int kMax, int kN>
 __device__ __forceinline__ void read(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
-    if (!kMax) return;
+    if (kMax <= 32) return;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -341,7 +362,7 @@ __device__ __forceinline__ void read(Sum<kN> &s, float (&red)[2][2][kMaxWarps], 
 }
 template <int kMax, int kN>
 __device__ __forceinline__ void row_sum(Sum<kN> &s, float (&red)[2][2][kMaxWarps], int &turn) {
-    tell<(kMax > 0)>(s, red, turn);
+    tell<kMax>(s, red, turn);
     read<kMax>(s, red, turn);
 }
 
@@ -355,17 +376,18 @@ __device__ __forceinline__ void clear(float (&red)[2][2][kMaxWarps]) {
 // forward
 // ------------------------------------------------------------------------------------------------
 
-// kMax: the block's threads at most (0: a warp for each row)
+// kMax: the block's threads at most, or (up to 32) the lanes of a row, of which a block of 128 threads has several
 template <typename T, int kV, int kMax>
-__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThreads / (kMax ? kMax : 128)) block_norm_forward_kernel(BlockNorm p) {
-    constexpr bool kBlock = kMax > 0;
+__global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kFwdThreads / block_of(kMax)) block_norm_forward_kernel(BlockNorm p) {
+    constexpr bool kBlock = kMax > 32;
+    constexpr int kAtOnce = kBlock ? 1 : kNarrowThreads / kMax, kOfWarp = kBlock ? 1 : 32 / kMax;  // rows of a block, of a warp
     __shared__ __align__(16) float red[2][2][kMaxWarps];
     let_next_begin();
     after_previous();
     int turn = 0;
     if (kBlock) clear(red);
-    const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
-    const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
+    const int threads = kBlock ? blockDim.x : kMax, t = kBlock ? threadIdx.x : threadIdx.x % kMax, C = p.C;
+    const long long step = (long long)gridDim.x * kAtOnce;
     const float inv = 1.f / C;
     Pairs scale, w_pre;  // (the first times w_post and the kept values' factor)
     {
@@ -380,9 +402,12 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
     drop.open(p, t, threads);
     Rows<T, kV, 3, 1> in{{static_cast<const T *>(p.x), static_cast<const T *>(p.y), static_cast<const T *>(p.gate)},
                               {p.x_stride, p.y_stride, p.gate_stride}, nullptr, t, threads, C, p.rows, step};
-    long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
+    long long row = (long long)blockIdx.x * kAtOnce + (kBlock ? 0 : threadIdx.x / kMax);
+    // a warp's rows together: those behind the last one take part in sums and exchanges alone
+    const int in_warp = kBlock ? 0 : (threadIdx.x & 31) / kMax;
     in.begin(nullptr, row);
-    for (; row < p.rows; row += step) {  // (all of a row's threads alike)
+    for (; row - in_warp < p.rows; row += step) {
+        const bool live = kOfWarp == 1 || row < p.rows;
         Pairs x, y, f[1];
         in.get(0, 0, row, x);
         in.get(0, 1, row, y);
@@ -394,7 +419,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
 #pragma unroll
             for (int i = 1; i < kPairs; ++i) sum = fma2(y[i], y[i], sum);
             add_up(sum, s1.v[0]);
-            tell<kBlock>(s1, red, turn);
+            tell<kMax>(s1, red, turn);
         }
         if (p.gate) {
             Pairs slope;
@@ -405,7 +430,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = scale[i];
         }
-        if (p.drop) drop.apply(p, row, t, threads, f);
+        if (p.drop) drop.apply(p, row, t, f);
         float r1 = 1.f;
         if (p.post) {
             read<kMax>(s1, red, turn);
@@ -419,14 +444,14 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kFwdThre
         }
         Sum<1> s2;
         add_up(sum, s2.v[0]);
-        if (p.pre) tell<kBlock>(s2, red, turn);
-        Cols<T, kV>::put(static_cast<T *>(p.x_out) + row * p.x_out_stride, t, threads, C, x);
+        if (p.pre) tell<kMax>(s2, red, turn);
+        Cols<T, kV>::put(static_cast<T *>(p.x_out) + row * p.x_out_stride, t, threads, live ? C : 0, x);
         if (p.pre) {
             read<kMax>(s2, red, turn);
             const float r2 = rsqrtf(s2.v[0] * inv + p.eps);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) x[i] = mul2(mul2(x[i], twice(r2)), w_pre[i]);
-            Cols<T, kV>::put(static_cast<T *>(p.h) + row * p.h_stride, t, threads, C, x);
+            Cols<T, kV>::put(static_cast<T *>(p.h) + row * p.h_stride, t, threads, live ? C : 0, x);
         }
     }
 }
@@ -496,8 +521,9 @@ __device__ __forceinline__ float grad_x_out(float dx_out, float gw, float x_out,
 }
 
 template <typename T, int kV, int kMax>
-__global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThreads / (kMax ? kMax : 128)) block_norm_backward_kernel(BlockNormBwd q) {
-    constexpr bool kBlock = kMax > 0;
+__global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kBwdThreads / block_of(kMax)) block_norm_backward_kernel(BlockNormBwd q) {
+    constexpr bool kBlock = kMax > 32;
+    constexpr int kAtOnce = kBlock ? 1 : kNarrowThreads / kMax, kOfWarp = kBlock ? 1 : 32 / kMax;  // rows of a block, of a warp
     __shared__ __align__(16) float red[2][2][kMaxWarps];
     __shared__ float sums[kBlock ? 1 : 2 * kNarrow];
     let_next_begin();
@@ -505,8 +531,8 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
     const BlockNorm &p = q.f;
     int turn = 0;
     if (kBlock) clear(red);
-    const int threads = kBlock ? blockDim.x : 32, t = kBlock ? threadIdx.x : threadIdx.x & 31, C = p.C;
-    const long long rows_at_once = kBlock ? 1 : kNarrowRows, step = gridDim.x * rows_at_once;
+    const int threads = kBlock ? blockDim.x : kMax, t = kBlock ? threadIdx.x : threadIdx.x % kMax, C = p.C;
+    const long long step = (long long)gridDim.x * kAtOnce;
     const float inv = 1.f / C;
     Pairs scale, w_pre;  // (the first times w_post and the kept values' factor)
     {
@@ -526,9 +552,12 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
                                static_cast<const T *>(q.dx_out), static_cast<const T *>(q.dh)},
                               {p.x_stride, p.y_stride, p.gate_stride, q.dx_out_stride, q.dh_stride},
                               nullptr, t, threads, C, p.rows, step};
-    long long row = blockIdx.x * rows_at_once + (kBlock ? 0 : threadIdx.x >> 5);
+    long long row = (long long)blockIdx.x * kAtOnce + (kBlock ? 0 : threadIdx.x / kMax);
+    // a warp's rows together: those behind the last one take part in sums and exchanges alone
+    const int in_warp = kBlock ? 0 : (threadIdx.x & 31) / kMax;
     in.begin(ring, row);
-    for (int slot = 0; row < p.rows; row += step, slot = slot + 1 < kSlots ? slot + 1 : 0) {
+    for (int slot = 0; row - in_warp < p.rows; row += step, slot = slot + 1 < kSlots ? slot + 1 : 0) {
+        const bool live = kOfWarp == 1 || row < p.rows;
         Pairs x, y, d, h, f[2];  // f: act(gate), act'(gate), 0 where dropped
         in.next(slot, row);
         in.get(slot, 0, row, x);
@@ -542,7 +571,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
 #pragma unroll
             for (int i = 1; i < kPairs; ++i) sum = fma2(y[i], y[i], sum);
             add_up(sum, s1.v[0]);
-            tell<kBlock>(s1, red, turn);
+            tell<kMax>(s1, red, turn);
         }
         if (p.gate) {
             activate<true>(p.act, f[0], f[1]);
@@ -550,7 +579,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = f[1][i] = twice(1.f);
         }
-        if (p.drop) drop.apply(p, row, t, threads, f);
+        if (p.drop) drop.apply(p, row, t, f);
         Pairs fs;  // what multiplies u in x', and t in dn
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) fs[i] = mul2(f[0][i], scale[i]);
@@ -580,32 +609,32 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
             for (int i = 0; i < kPairs; ++i) {
                 const uint64_t hr = mul2(h[i], twice(r2));
                 d[i] = fma2(x[i], by, fma2(hr, w_pre[i], d[i]));
-                dw_pre[i] = fma2(hr, x[i], dw_pre[i]);
+                if (live) dw_pre[i] = fma2(hr, x[i], dw_pre[i]);
             }
         }
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) x[i] = mul2(d[i], twice(p.alpha));
-        Cols<T, kV>::put(static_cast<T *>(q.dx) + row * q.dx_stride, t, threads, C, x);
+        Cols<T, kV>::put(static_cast<T *>(q.dx) + row * q.dx_stride, t, threads, live ? C : 0, x);
         uint64_t dot = 0;
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             const uint64_t du = mul2(d[i], y[i]);
-            qu[i] = fma2(du, f[0][i], qu[i]);
+            if (live) qu[i] = fma2(du, f[0][i], qu[i]);
             x[i] = mul2(d[i], fs[i]);  // q scale w_post
             dot = fma2(x[i], y[i], dot);
             f[1][i] = mul2(mul2(du, f[1][i]), scale[i]);  // dgate
         }
         Sum<1> s3;
         add_up(dot, s3.v[0]);
-        if (p.post) tell<kBlock>(s3, red, turn);
-        if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, C, f[1]);
+        if (p.post) tell<kMax>(s3, red, turn);
+        if (p.gate) Cols<T, kV>::put(static_cast<T *>(q.dgate) + row * q.dgate_stride, t, threads, live ? C : 0, f[1]);
         if (p.post) {
             read<kMax>(s3, red, turn);
             const uint64_t m = twice(-s3.v[0] * inv);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) x[i] = mul2(fma2(y[i], m, x[i]), twice(r1));
         }
-        Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, C, x);
+        Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, live ? C : 0, x);
     }
     if (kSlots > 1) ring_wait<0>();
     // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
@@ -616,11 +645,17 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
         unpair(dw_pre[i], sum[1][2 * i], sum[1][2 * i + 1]);
     }
     if (!kBlock) {
-        for (int w = 0; w < kNarrowRows; ++w) {
-            if ((threadIdx.x >> 5) == w) {
+#pragma unroll
+        for (int o = kMax; o < 32; o *= 2)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) sum[n][i] += __shfl_xor_sync(0xffffffffu, sum[n][i], o);
+        for (int w = 0; w < kNarrowThreads / 32; ++w) {
+            if ((threadIdx.x >> 5) == w && in_warp == 0) {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
-                    const int c = Cols<T, kV>::at(i / kV, t, 32) + i % kV;
+                    const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         sum[n][i] += w ? sums[n * kNarrow + c] : 0.f;
@@ -632,7 +667,7 @@ __global__ void __launch_bounds__(kMax ? kMax : 128, kMax == 1024 ? 1 : kBwdThre
         }
     }
     float *to = q.partial + (size_t)blockIdx.x * 2 * C;
-    if (kBlock || threadIdx.x / 32 == kNarrowRows - 1) {
+    if (kBlock || (threadIdx.x >= kNarrowThreads - 32 && in_warp == 0)) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
@@ -721,32 +756,42 @@ struct Plan {
     unsigned grid;
     int threads;
 };
+// lanes of a narrow row: eight columns each
+int lanes_of(int C) { return C <= 32 ? 4 : C <= 64 ? 8 : C <= 128 ? 16 : 32; }
 // Blocks that the GPU holds at `per_sm` threads an SM, or fewer where there are not so many rows
 Plan plan(long long rows, int C, int per_sm) {
-    const int threads = C <= kNarrow ? 128 : C > kWide ? 1024 : (C + 32 * kPer - 1) / (32 * kPer) * 32;
-    const long long blocks = C <= kNarrow ? (rows + kNarrowRows - 1) / kNarrowRows : rows;
+    const int threads = C <= kNarrow ? kNarrowThreads : C > kWide ? 1024 : (C + 32 * kPer - 1) / (32 * kPer) * 32;
+    const long long at_once = C <= kNarrow ? kNarrowThreads / lanes_of(C) : 1, blocks = (rows + at_once - 1) / at_once;
     const long long most = (long long)kSMs * (per_sm / threads > 0 ? per_sm / threads : 1);
     return {(unsigned)(blocks < most ? blocks : most), threads};
 }
 
-// the widest access that every row allows: 16 bytes, or one element
+// whether every row begins at `by` bytes and has whole accesses of so many
 template <typename T>
-bool wide_rows(const BlockNorm &p) {
-    const size_t by = 16;
+bool rows_of(const BlockNorm &p, size_t by) {
     auto ok = [&](const void *q, long long stride) { return !q || rows_aligned(q, stride, sizeof(T), by); };
     return p.C % (by / sizeof(T)) == 0 && ok(p.x, p.x_stride) && ok(p.y, p.y_stride) && ok(p.gate, p.gate_stride) &&
            ok(p.x_out, p.x_out_stride) && ok(p.h, p.h_stride) && ok(p.w_post, 0) && ok(p.scale, 0) && ok(p.w_pre, 0);
 }
 template <typename T>
-bool wide_rows(const BlockNormBwd &q) {
-    auto ok = [&](const void *p, long long stride) { return !p || rows_aligned(p, stride, sizeof(T), 16); };
-    return wide_rows<T>(q.f) && ok(q.dx_out, q.dx_out_stride) && ok(q.dh, q.dh_stride) && ok(q.dx, q.dx_stride) &&
+bool rows_of(const BlockNormBwd &q, size_t by) {
+    auto ok = [&](const void *p, long long stride) { return !p || rows_aligned(p, stride, sizeof(T), by); };
+    return rows_of<T>(q.f, by) && ok(q.dx_out, q.dx_out_stride) && ok(q.dh, q.dh_stride) && ok(q.dx, q.dx_stride) &&
            ok(q.dy, q.dy_stride) && ok(q.dgate, q.dgate_stride);
+}
+// the widest access that every row allows: 16 bytes, two elements, or one
+template <typename T, typename P, typename F>
+cudaError_t by_access(const P &p, F f) {
+    if (rows_of<T>(p, 16)) return f(std::integral_constant<int, 16 / sizeof(T)>());
+    return rows_of<T>(p, 2 * sizeof(T)) ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
 template <typename F>
 cudaError_t by_threads(int C, int threads, F f) {
-    return C <= kNarrow     ? f(std::integral_constant<int, 0>())
+    return C <= 32          ? f(std::integral_constant<int, 4>())
+           : C <= 64        ? f(std::integral_constant<int, 8>())
+           : C <= 128       ? f(std::integral_constant<int, 16>())
+           : C <= kNarrow   ? f(std::integral_constant<int, 32>())
            : threads <= 256 ? f(std::integral_constant<int, 256>())
            : threads <= 512 ? f(std::integral_constant<int, 512>())
                             : f(std::integral_constant<int, 1024>());
@@ -769,7 +814,7 @@ cudaError_t forward_of(const BlockNorm &p, cudaStream_t s) {
             return launch_after(block_norm_forward_kernel<T, V(), M()>, g.grid, g.threads, 0, s, p);
         });
     };
-    return wide_rows<T>(p) ? as(std::integral_constant<int, 16 / sizeof(T)>()) : as(std::integral_constant<int, 1>());
+    return by_access<T>(p, as);
 }
 
 template <typename T>
@@ -781,9 +826,8 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
             return launch_ring(block_norm_backward_kernel<T, V(), M()>, g, ring_bytes<T>(g.threads, slots<T, V(), M()>()), s, q);
         });
     };
-    const cudaError_t e = p.C > kWide ? launch_after(block_norm_wide_backward_kernel<T>, g.grid, 1024, 0, s, q)
-                          : wide_rows<T>(q) ? as(std::integral_constant<int, 16 / sizeof(T)>())
-                                            : as(std::integral_constant<int, 1>());
+    const cudaError_t e =
+        p.C > kWide ? launch_after(block_norm_wide_backward_kernel<T>, g.grid, 1024, 0, s, q) : by_access<T>(q, as);
     if (e) return e;
     return column_sum_launch({q.partial, g.grid, p.C, 2,
                               {{q.dw_post, 0, p.scale}, {q.dscale, 0, p.w_post}, {q.dw_pre, 1, nullptr}}, p.dt, q.header}, s);

@@ -9,8 +9,8 @@
 // use in flight.  A panel lies as its matrix does: where the sum's index is the contiguous one a thread reads four
 // (two) of its indices of a row at a time, else four rows of an index, so that either way a wide access feeds many products.
 // The forward's tile is half gate and half up columns of the same features, so that the activation and product happen in
-// registers.  The gradient keeps [dZg dZu] in the workspace; its dx, whose sum is over 2 F and whose tiles may be few, is
-// cut along the sum, and the parts are added in their order.
+// registers.  The gradient keeps [dZg dZu] in the workspace; its last two products, whose sums are over 2 F and over tokens and
+// whose tiles may be few, are cut along the sum, and the parts are added in their order.
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
 
@@ -231,13 +231,15 @@ long long tiles(long long M, long long N, int tile, bool paired) {
 }
 bool small_tiles(long long M, long long N, bool paired) { return tiles(M, N, 128, paired) < kSMs; }
 
-// how many parts the sum of dx is cut into: as many as bring two blocks an SM, each of 128 indices or more
-int parts_of(int M, int K, int F) {
-    const long long t = tiles(M, K, small_tiles(M, K, false) ? 64 : 128, false);
-    const long long by_blocks = 2 * kSMs / t, by_sum = 2LL * F / 128;
+// how many parts a sum is cut into: as many as bring two blocks an SM, each of 128 indices or more
+int parts_of(long long M, long long N, long long sum) {
+    const long long t = tiles(M, N, small_tiles(M, N, false) ? 64 : 128, false);
+    const long long by_blocks = 2 * kSMs / t, by_sum = sum / 128;
     const long long parts = by_blocks < by_sum ? by_blocks : by_sum;
     return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
 }
+int parts_dx(int M, int K, int F) { return parts_of(M, K, 2LL * F); }
+int parts_dw(int M, int K, int F) { return parts_of(2LL * F, K, M); }
 
 template <bool kA, bool kB, Mode kMode>
 cudaError_t product(Product p, int parts, cudaStream_t s) {
@@ -256,6 +258,23 @@ cudaError_t product(Product p, int parts, cudaStream_t s) {
 
 const float *floats(const void *p) { return static_cast<const float *>(p); }
 
+size_t parts_floats(int parts, long long M, long long N) { return parts > 1 ? (size_t)parts * M * N : 0; }
+
+// a product whose sum is cut into parts, which lie in `sums` until they are added
+template <bool kA>
+cudaError_t cut_product(Product p, int parts, float *sums, cudaStream_t s) {
+    if (parts == 1) return product<kA, false, kProduct>(p, 1, s);
+    float *out = p.out;
+    const long long out_row = p.out_row, all = (long long)p.M * p.N, blocks = (all + kThreads - 1) / kThreads;
+    p.per = ((p.K + parts - 1) / parts + kDepth - 1) / kDepth * kDepth;
+    p.out = sums;
+    p.out_row = p.N;
+    const cudaError_t e = product<kA, false, kParts>(p, parts, s);
+    if (e) return e;
+    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts, p.M, p.N,
+                        out, out_row);
+}
+
 // [dZg dZu] in rows of whole 16 bytes
 long long dz_row(int F) { return (2LL * F + 3) / 4 * 4; }
 
@@ -268,28 +287,21 @@ cudaError_t forward_f32(const Ffn &p, cudaStream_t s) {
 cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     const Ffn &f = p.f;
     float *dz = reinterpret_cast<float *>(f.ws + kWsHeaderBytes);
-    const int F2 = 2 * f.F, parts = parts_of(f.M, f.K, f.F);
+    const int F2 = 2 * f.F;
     const long long row = dz_row(f.F);
     const Product q{mat(floats(f.x), f.x_stride), mat(floats(f.w), f.K), f.M, f.F, f.K, f.act, f.K, 0, dz, row,
                     floats(p.dout), p.dout_stride, reinterpret_cast<WsHeader *>(f.ws)};
     cudaError_t e = product<true, true, kGrad>(q, 1, s);
     if (e) return e;
+    float *sums = dz + (size_t)f.M * row;
     const Product dw{mat(dz, row), mat(floats(f.x), f.x_stride), F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
                      nullptr, 0, nullptr};
-    e = product<false, false, kProduct>(dw, 1, s);
+    e = cut_product<false>(dw, parts_dw(f.M, f.K, f.F), sums, s);
     if (e) return e;
-    Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
-               nullptr, 0, nullptr};
-    if (parts == 1) return product<true, false, kProduct>(dx, 1, s);
-    dx.per = ((F2 + parts - 1) / parts + kDepth - 1) / kDepth * kDepth;
-    float *sums = dz + (size_t)f.M * row;
-    dx.out = sums;
-    dx.out_row = f.K;
-    e = product<true, false, kParts>(dx, parts, s);
-    if (e) return e;
-    const long long all = (long long)f.M * f.K, blocks = (all + kThreads - 1) / kThreads;
-    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts, f.M,
-                        f.K, static_cast<float *>(p.dx), p.dx_stride);
+    sums += parts_floats(parts_dw(f.M, f.K, f.F), F2, f.K);
+    const Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
+                     nullptr, 0, nullptr};
+    return cut_product<true>(dx, parts_dx(f.M, f.K, f.F), sums, s);
 }
 
 }  // namespace
@@ -299,8 +311,9 @@ size_t ffn_forward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
 }
 size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
     if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
-    const int parts = M ? parts_of(M, K, F) : 1;
-    return sizeof(float) * ((size_t)M * dz_row(F) + (parts > 1 ? (size_t)parts * M * K : 0));
+    if (M == 0) return 0;
+    return sizeof(float) *
+           ((size_t)M * dz_row(F) + parts_floats(parts_dx(M, K, F), M, K) + parts_floats(parts_dw(M, K, F), 2LL * F, K));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);

@@ -20,6 +20,7 @@
 // Every wait has a limit: it sets the workspace's error word and the block's `stop`, after which all roles leave,
 // copies and products in flight are waited for (with a limit), and tensor memory is released.
 #include <climits>
+#include <type_traits>
 
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
@@ -174,12 +175,25 @@ __device__ __forceinline__ void copy_rows(char *staged, E *at, long long row, in
                 else *reinterpret_cast<uint4 *>(at + r * row + c) = *s;
             }
     } else {
-        for (int r = 0; r < 32 && r < rows; ++r)
-            for (int c = lane; c < kBytes / (int)sizeof(E) && c < cols; c += 32) {
+        // (eight in flight)
+        constexpr int kCols = kBytes / (int)sizeof(E);
+#pragma unroll 1
+        for (int i0 = lane; i0 < 32 * kCols; i0 += 256) {
+            std::remove_const_t<E> v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j, r = i / kCols, c = i % kCols;
                 char *s = staged + r * kPitch + c * sizeof(E);
-                if constexpr (kLoad) memcpy(s, at + r * row + c, sizeof(E));
-                else at[r * row + c] = *reinterpret_cast<const E *>(s);
+                if constexpr (!kLoad) v[j] = *reinterpret_cast<const E *>(s);
+                else if (r < rows && c < cols) memcpy(&v[j], at + r * row + c, sizeof(E));
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j, r = i / kCols, c = i % kCols;
+                if constexpr (kLoad) memcpy(staged + r * kPitch + c * sizeof(E), &v[j], sizeof(E));
+                else if (r < rows && c < cols) at[r * row + c] = v[j];
+            }
+        }
     }
 }
 

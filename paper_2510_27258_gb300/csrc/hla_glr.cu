@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     using Sh = FwdShape<T, kLanes>;
     constexpr int kTok = Sh::kTok;
     extern __shared__ __align__(128) char smem[];
-    __shared__ Runs<kLanes> runs[2][kTiles];
+    // (a cluster's turns take one place, behind a barrier more: two blocks an SM have to fit)
+    __shared__ Runs<kLanes> runs[kTiles == 1 ? 2 : 1][kTiles];
     __shared__ uint64_t carry[2][kLanes];        // (kTiles 1)
     __shared__ Exchange<kLanes, kTiles> others;  // (kTiles > 1)
     let_next_begin();
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
         for (int turn = 0; turn < turns; ++turn) {
             uint64_t h[kTok], pr[kTok];  // this group's states from 0, and the products of decays
             Run mine[kTiles], ahead[kTiles];
-            const int buf = turn & 1;
+            const int buf = kTiles == 1 ? turn & 1 : 0;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t0 += step) {
                 in.next(slot, t0, step, at);
@@ -484,6 +485,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
             uint64_t before[kTiles];
             if constexpr (kTiles == 1) before[0] = joint.alone(runs[buf][0], carry, turn, mine[0], ahead[0], state);
             else joint.among(runs[buf], others, turn, S, rank, mine, ahead, lost, state, before);
+            if (kTiles > 1) __syncthreads();  // every warp has read this turn's runs
             int t = t0 - kTiles * step;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t += step, y += y_step) {

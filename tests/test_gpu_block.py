@@ -227,7 +227,9 @@ NORM = [((1, 1), dict()), ((5, 8), dict(dropout=0.5)), ((37, 203), dict(dropout=
         ((700, 2048), dict(dropout=0.1, alpha=0.75)), ((9, 2100), dict(act=R.LINEAR, post=False)),
         ((11, 4104), dict(pre=False, dropout=0.1)), ((3, 8192), dict(dropout=0.1)), ((2, 1023), dict(weights=False)),
         ((2, 8201), dict(dropout=0.1)), ((3, 20000), dict(post=False)), ((2, 8200), dict(pre=False, gate=False)),
-        ((400, 24), dict(post=False, pre=False))]
+        ((400, 24), dict(post=False, pre=False)), ((33, 1022), dict(dropout=0.1)), ((77, 30), dict(dropout=0.25)),
+        ((2000, 32), dict(dropout=0.1)), ((51, 60), dict(dropout=0.5)), ((131, 100), dict(dropout=0.1)),
+        ((41, 250), dict(dropout=0.1, gate=False)), ((3000, 49), dict(dropout=0.1)), ((9, 8190), dict(dropout=0.1))]
 
 
 def norm_case(seed, rows, C, T, gate=True, weights=True, **kw):
