@@ -489,13 +489,13 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // ------------------------------------------------------------------------------------------------
 // few rows: the weights are the rows of the product, the tokens its columns
 //
-// With up to 256 tokens the weights' bytes are what counts.  A block reads 128 of their rows (64 gate and 64 up rows of
-// the same features; for dx 128 columns, against the sum's direction) for all tokens, 16 to 256 columns of one
+// With up to 128 tokens the weights' bytes are what counts.  A block reads 128 of their rows (64 gate and 64 up rows of
+// the same features; for dx 128 columns, against the sum's direction) for all tokens, 16 to 128 columns of one
 // product, so the products cost what the tokens need, and every SM streams weights: the sum is cut over the blocks of a
 // cluster, whose parts meet in shared memory and are added in the blocks' order, each block finishing some of the tokens.
 // ------------------------------------------------------------------------------------------------
 
-constexpr int kFewMost = 256, kFewThreads = 192, kFewStages = 8;
+constexpr int kFewMost = 128, kFewThreads = 192, kFewStages = 8;
 constexpr uint32_t kFewABytes = 128 * kStep * 2;
 
 struct Few {
@@ -534,18 +534,31 @@ __device__ bool wait_few(uint64_t *bar, uint32_t parity, FewBars *bars, WsHeader
     }
 }
 
-// the first block of the cluster's partial sums and so on, in their order
-__device__ __forceinline__ float add_blocks(const float *mine, int S) {
-    if (S == 1) return *mine;
-    float sum = 0.f;
-    for (int b = 0; b < S; ++b) {
-        uint32_t at;
-        float v;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(b));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-        sum += v;
+// kN values of the cluster's blocks' partial sums, added in the blocks' order
+template <int kN>
+__device__ __forceinline__ void add_blocks(const float *const (&mine)[kN], int S, float (&sum)[kN]) {
+    if (S == 1) {
+#pragma unroll
+        for (int j = 0; j < kN; ++j) sum[j] = *mine[j];
+        return;
     }
-    return sum;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) sum[j] = 0.f;
+    for (int b = 0; b < S; b += 2) {  // (S is even)
+        float v[2][kN];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                uint32_t at;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine[j])), "r"(b + q));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[q][j]) : "r"(at) : "memory");
+            }
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < kN; ++j) sum[j] += v[q][j];
+    }
 }
 
 // grid: tiles of weights' rows x blocks of a cluster
@@ -559,7 +572,7 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = S > 1 ? (int)cluster_rank() : 0, tile = blockIdx.x / S;
     const uint32_t stage_bytes = kFewABytes + f.cols * kStep * 2;
-    const uint32_t tmem_cols = f.cols <= 32 ? 32 : f.cols <= 64 ? 64 : f.cols <= 128 ? 128 : 256;
+    const uint32_t tmem_cols = f.cols <= 32 ? 32 : f.cols <= 64 ? 64 : 128;
     const int k_lo = min(rank * f.per, f.steps), k_hi = min(k_lo + f.per, f.steps);
     let_next_begin();
     if (threadIdx.x == 0) {
@@ -661,25 +674,40 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     if (S > 1) cluster_meet();
-    // the block's tokens, a warp a row of 64 (kBack: 128) neighbours by turns
+    // the block's tokens, neighbouring threads a row's neighbours, four values of a thread in flight
     const int each = (f.tokens + S - 1) / S, lo = rank * each, hi = min(lo + each, f.tokens);
-    const int n0 = tile * (kMode == kBack ? 128 : 64), per_token = kMode == kBack ? 128 : 64;
-    for (int i = threadIdx.x; i < (hi - lo) * per_token; i += kFewThreads) {
-        const int token = lo + i / per_token, r = i % per_token, n = n0 + r;
-        if (n >= f.width) continue;
-        const float v = add_blocks(sums + token * 128 + r, S);
-        if (kMode == kBack) {
-            from_f32(f.out + token * f.out_row + n, v);
-        } else {
-            const float up = add_blocks(sums + token * 128 + 64 + r, S);
+    constexpr int kPerToken = kMode == kBack ? 128 : 64, kFour = 4;
+    const int n0 = tile * kPerToken, all = (hi - lo) * kPerToken;
+    for (int i0 = threadIdx.x; i0 < all; i0 += kFewThreads * kFour) {
+        const float *at[kFour], *at_up[kFour];
+        float v[kFour], up[kFour], d[kFour];
+        long long to[kFour];
+        bool on[kFour];
+#pragma unroll
+        for (int j = 0; j < kFour; ++j) {
+            const int i = min(i0 + j * kFewThreads, all - 1), token = lo + i / kPerToken, r = i % kPerToken;
+            on[j] = i0 + j * kFewThreads < all && n0 + r < f.width;
+            at[j] = sums + token * 128 + r;
+            at_up[j] = at[j] + 64;
+            to[j] = token * f.out_row + n0 + r;
+            if (kMode == kGrad) d[j] = on[j] ? to_f32(f.dout[token * f.dout_row + n0 + r]) : 0.f;
+        }
+        add_blocks(at, S, v);
+        if (kMode != kBack) add_blocks(at_up, S, up);
+#pragma unroll
+        for (int j = 0; j < kFour; ++j) {
+            if (!on[j]) continue;
+            if (kMode == kBack) {
+                from_f32(f.out + to[j], v[j]);
+                continue;
+            }
             float slope;
-            const float a = act_of(f.act, v, slope);
+            const float a = act_of(f.act, v[j], slope);
             if (kMode == kOut) {
-                from_f32(f.out + token * f.out_row + n, a * up);
+                from_f32(f.out + to[j], a * up[j]);
             } else {
-                const float d = to_f32(f.dout[token * f.dout_row + n]);
-                from_f32(f.out + token * f.out_row + n, d * up * slope);
-                from_f32(f.out + f.out_plane + token * f.out_row + n, d * a);
+                from_f32(f.out + to[j], d[j] * up[j] * slope);
+                from_f32(f.out + f.out_plane + to[j], d[j] * a);
             }
         }
     }
@@ -800,16 +828,14 @@ cudaError_t align_operands(const Ffn &p, char *&at, Operands &o, cudaStream_t s)
 
 bool wide(const void *p, long long row, int cols) { return cols % 8 == 0 && rows_aligned(p, row, 2, 16); }
 
-// Few rows: blocks of a cluster as many as fill two blocks an SM (one where the ring takes more than half of an SM's
-// shared memory), each with four steps or more
+// Few rows: blocks of a cluster as many as fill two blocks an SM, each with four steps or more
 template <Mode kMode>
 cudaError_t run_few(const CUtensorMap &weights, const CUtensorMap &tokens, Few f, int tiles, cudaStream_t s) {
     const int bytes = (int)kFewABytes + f.cols * kStep * 2, sums = f.cols * 128 * 4;
-    const int room = f.cols <= 64 ? 100 * 1024 : 200 * 1024;
-    f.stages = room / bytes < kFewStages ? room / bytes : kFewStages;
-    const int blocks = f.cols <= 64 ? 2 * kSMs : kSMs;
+    constexpr int kRoom = 100 * 1024;
+    f.stages = kRoom / bytes < kFewStages ? kRoom / bytes : kFewStages;
     int S = 1;
-    while (S < 8 && (long long)tiles * S * 2 <= blocks && f.steps >= S * 2 * 4) S *= 2;
+    while (S < 8 && (long long)tiles * S * 2 <= 2 * kSMs && f.steps >= S * 2 * 4) S *= 2;
     f.per = tiles_of(f.steps, S);
     const int smem = 1024 + (f.stages * bytes > sums ? f.stages * bytes : sums);
     const cudaError_t e = cudaFuncSetAttribute(ffn_few_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -817,7 +843,8 @@ cudaError_t run_few(const CUtensorMap &weights, const CUtensorMap &tokens, Few f
     return launch_cluster_after(ffn_few_kernel<kMode>, (unsigned)((long long)tiles * S), kFewThreads, S, smem, s, weights, tokens, f, S);
 }
 
-// Up to 256 tokens, where the tiles of 256 x 256 would leave pairs without one
+// Up to 128 tokens, where the tiles of 256 x 256 would leave pairs without one (16 x 2048 x 5632: 9 us on the device
+// instead of 18; above, the tiles cost no more than the tokens' own products)
 bool few(int M, int F) { return M <= kFewMost && tiles_of(F, kHalf) < kPairs; }
 int few_cols(int M) { return (M + 15) / 16 * 16; }
 
