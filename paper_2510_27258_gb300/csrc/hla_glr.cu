@@ -152,31 +152,36 @@ struct Lane {
     }
 };
 
-// A lane's next tokens of kTensors tensors.  kRing: rows that begin at 16 bytes come through a ring of kSlots rounds in
-// shared memory by asynchronous copies of a warp for its own groups, all but the round in use in flight.  Else they are
-// loaded into registers a round ahead.
-template <typename T, typename S, int kTensors, bool kRing>
+// A lane's next tokens of kTensors tensors, through a ring of kSlots rounds in shared memory by asynchronous copies of a
+// warp for itself, all but the round in use in flight.  kWide: rows begin at 16 bytes and are copied in chunks of that.
+// Else a lane copies the one or two 4-byte words that hold its two channels, wherever they begin.
+template <typename T, typename S, int kTensors, bool kWide>
 struct Tokens {
-    static constexpr int kTok = S::kTok, kRow = S::kChannels * (int)sizeof(T), kChunks = kRow / 16;
+    static constexpr int kTok = S::kTok, kRow = kWide ? S::kChannels * (int)sizeof(T) : S::kLanes * 8, kChunks = kRow / 16;
     static constexpr int kRows = kTok * S::kOfWarp, kSlotBytes = kTensors * kRows * kRow;
-    static constexpr int kSmem = kRing ? kThreads / 32 * kSlots * kSlotBytes : 0;
-    const T *from[kTensors];
-    long long stride[kTensors], ahead_by[kRing ? kTensors : 1];
+    static constexpr int kSmem = kThreads / 32 * kSlots * kSlotBytes;
+    const T *from[kTensors];  // the lane's first element of the next round to be sent for
+    long long stride[kTensors], ahead_by[kTensors];
     char *ring;      // this warp's
     int len, bytes;  // of the sequence; of this lane's chunk
-    Raw<T, 2> ahead[kRing ? 1 : kTensors][kRing ? 1 : kTok];
+    unsigned odd;    // a bit for each tensor: this lane's channels of token 0 begin in the middle of a word
 
     // t0: the group's first token, step: from a round's to the next one's
     __device__ __forceinline__ void set(int i, const void *p, long long row_stride, size_t row0, uint32_t channel, int t0,
                                         int step) {
-        from[i] = static_cast<const T *>(p) + row0 * row_stride;
+        const int lane = threadIdx.x & 31;
+        const T *at = static_cast<const T *>(p) + row0 * row_stride + channel;
         stride[i] = row_stride;
-        if constexpr (kRing) {  // (the lane's first element of the next round to be sent for)
-            const int lane = threadIdx.x & 31;
-            from[i] += (t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0) + lane / kChunks) * row_stride +
-                       (long long)channel + lane % kChunks * (16 / (int)sizeof(T));
-            ahead_by[i] = step * row_stride;
+        ahead_by[i] = step * row_stride;
+        if constexpr (kWide) {
+            at += (t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0) + lane / kChunks) * row_stride +
+                  lane % kChunks * (16 / (int)sizeof(T));
+        } else {
+            if (i == 0) odd = 0;
+            odd |= (unsigned)(reinterpret_cast<uintptr_t>(at) >> 1 & 1) << i;
+            at += t0 * row_stride + 2 * S::lane();
         }
+        from[i] = at;
     }
     __device__ __forceinline__ void open(char *smem, uint32_t channel, int C, int length) {
         ring = smem + (threadIdx.x >> 5) * (kSlots * kSlotBytes);
@@ -184,9 +189,12 @@ struct Tokens {
         const int left = min((int)(C - channel), S::kChannels) * (int)sizeof(T) - (int)(threadIdx.x % kChunks) * 16;
         bytes = min(max(left, 0), 16);
     }
+    // whether a lane's channels of token t begin in the middle of a word
+    __device__ __forceinline__ bool split(int i, int t) const { return (odd >> i ^ (unsigned)(t & stride[i])) & 1; }
     __device__ __forceinline__ void send(int slot, int t0, const Lane &at) {
-        if constexpr (kRing) {
-            const int lane = threadIdx.x & 31, first = t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0);  // the warp's
+        const int lane = threadIdx.x & 31;
+        if constexpr (kWide) {
+            const int first = t0 - (S::kOfWarp > 1 ? lane / S::kLanes * kTok : 0);  // the warp's
             char *to = ring + slot * kSlotBytes + lane % kChunks * 16;
             const bool all = first >= 0 && first + kRows <= len;
 #pragma unroll
@@ -202,45 +210,52 @@ struct Tokens {
                                  : "memory");
                 }
             }
-            ring_commit();
         } else {
 #pragma unroll
-            for (int u = 0; u < kTok; ++u)
+            for (int i = 0; i < kTensors; ++i) {
+                const T *p = from[i];
+                from[i] += ahead_by[i];
 #pragma unroll
-                for (int i = 0; i < kTensors; ++i)
-                    ahead[i][u] = (unsigned)(t0 + u) < (unsigned)len
-                                      ? at.load(from[i] + (long long)(t0 + u) * stride[i], false)
-                                      : raw_zero<T, 2>();
+                for (int u = 0; u < kTok; ++u, p += stride[i]) {
+                    const bool live = (unsigned)(t0 + u) < (unsigned)len;
+                    const uint32_t to = smem_u32(ring + slot * kSlotBytes + (i * kTok + u) * 256 + lane * 8);
+                    const char *word = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
+                    // (a word that holds one element of the row is memory of the tensor)
+                    const bool second = sizeof(T) == 4 || split(i, t0 + u);
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(word), "r"(live && at.on0 ? 4 : 0)
+                                 : "memory");
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4), "l"(word + 4),
+                                 "r"(live && second && at.on1 ? 4 : 0)
+                                 : "memory");
+                }
+            }
         }
+        ring_commit();
     }
     // before the first round: the rounds behind it `step` tokens apart
     __device__ __forceinline__ void begin(int t0, int step, const Lane &at) {
-        if constexpr (kRing) {
 #pragma unroll
-            for (int k = 0; k < kSlots - 1; ++k) send(k, t0 + k * step, at);
-        } else {
-            send(0, t0, at);
-        }
+        for (int k = 0; k < kSlots - 1; ++k) send(k, t0 + k * step, at);
     }
     // at the start of a round: its tokens are there, and the slot of the last round is filled again
     __device__ __forceinline__ void next(int slot, int t0, int step, const Lane &at) {
-        if constexpr (kRing) {
-            ring_wait<kSlots - 2>();
-            __syncwarp();
-            send(slot ? slot - 1 : kSlots - 1, t0 + (kSlots - 1) * step, at);
-        }
+        ring_wait<kSlots - 2>();
+        __syncwarp();
+        send(slot ? slot - 1 : kSlots - 1, t0 + (kSlots - 1) * step, at);
     }
-    __device__ __forceinline__ Raw<T, 2> get(int slot, int i, int u) const {
-        if constexpr (kRing)
+    // token t0 + u of the slot
+    __device__ __forceinline__ Raw<T, 2> get(int slot, int i, int t0, int u) const {
+        if constexpr (kWide) {
             return raw_load<T, 2>(
                 reinterpret_cast<const T *>(ring + slot * kSlotBytes + (i * kRows + u * S::kOfWarp) * kRow) +
                 2 * (threadIdx.x & 31));
-        else
-            return ahead[i][u];
-    }
-    // when the round's tokens have been used
-    __device__ __forceinline__ void used(int t0, int step, const Lane &at) {
-        if constexpr (!kRing) send(0, t0 + step, at);
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(ring + slot * kSlotBytes + (i * kTok + u) * 256 + (threadIdx.x & 31) * 8);
+            Raw<T, 2> r;
+            if constexpr (sizeof(T) == 4) r.v = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+            else r.v = split(i, t0 + u) ? __byte_perm(w.x, w.y, 0x5432) : w.x;
+            return r;
+        }
     }
 };
 
@@ -410,14 +425,14 @@ using FwdShape = Shape<kLanes, sizeof(T) == 2 ? 8 : 4>;
 
 // kTiles: tiles of a block between two exchanges with its cluster's others (1: a block alone).  The states of all but the
 // last one wait in shared memory.
-template <typename T, int kLanes, bool kRing, int kTiles>
+template <typename T, int kLanes, bool kWide, int kTiles>
 struct FwdSmem {
-    using In = Tokens<T, FwdShape<T, kLanes>, 3, kRing>;
+    using In = Tokens<T, FwdShape<T, kLanes>, 3, kWide>;
     static constexpr int kKept = (kTiles - 1) * FwdShape<T, kLanes>::kTok * kThreads * (int)sizeof(Run);
     static constexpr int kBytes = In::kSmem + kKept;
 };
 
-template <typename T, int kLanes, bool kRing, int kTiles>
+template <typename T, int kLanes, bool kWide, int kTiles>
 __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int slabs, int S, bool y_pairs) {
     using Sh = FwdShape<T, kLanes>;
     constexpr int kTok = Sh::kTok;
@@ -437,14 +452,14 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     const int len = p.lengths ? min(max(p.lengths[b], 0), p.n) : p.n;
     const size_t row0 = (size_t)b * p.n;
     const int step = S * Sh::kSpan;
-    Tokens<T, Sh, 3, kRing> in;
+    Tokens<T, Sh, 3, kWide> in;
     int t0 = rank * Sh::kSpan + group * kTok;
     in.set(0, p.x, p.x_stride, row0, channel, t0, step);
     in.set(1, p.r, p.r_stride, row0, channel, t0, step);
     in.set(2, p.g, p.g_stride, row0, channel, t0, step);
     in.open(smem, channel, p.C, len);
     in.begin(t0, step, at);
-    Run *kept = reinterpret_cast<Run *>(smem + FwdSmem<T, kLanes, kRing, kTiles>::In::kSmem) + threadIdx.x;
+    Run *kept = reinterpret_cast<Run *>(smem + FwdSmem<T, kLanes, kWide, kTiles>::In::kSmem) + threadIdx.x;
     const Decay decay(at.get(p.decay, pairs));
     uint64_t state = p.state_in ? at.get(p.state_in + (size_t)b * p.C, pairs) : 0;
     T *y = static_cast<T *>(p.y) + (row0 + t0) * p.y_stride;
@@ -466,18 +481,17 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
 #pragma unroll
                 for (int u = 0; u < kTok; ++u) {
                     uint64_t a, w;
-                    Raw<T, 2> rr = in.get(slot, 1, u);
+                    Raw<T, 2> rr = in.get(slot, 1, t0, u);
                     if (t0 + u >= len) shut(rr);  // (x is 0 there)
                     decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
-                    const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, u)));
+                    const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
                     // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
                     const uint64_t add =
-                        mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, u)));
+                        mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, t0, u)));
                     h[u] = u ? fma2(a, h[u - 1], add) : add;
                     pr[u] = u ? mul2(a, pr[u - 1]) : a;
                     if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
                 }
-                in.used(t0, step, at);
                 if (++slot == kSlots) slot = 0;
                 mine[i] = of_warp<Sh, 1>({pr[kTok - 1], h[kTok - 1]}, ahead[i]);
                 joint.tell(runs[buf][i], mine[i]);
@@ -545,7 +559,7 @@ __global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool ro
 // gradient
 // ------------------------------------------------------------------------------------------------
 
-template <typename T, int kLanes, bool kRing>
+template <typename T, int kLanes, bool kWide>
 __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int slabs, int S, bool out_pairs) {
     using Sh = Shape<kLanes, 4>;
     constexpr int kTok = Sh::kTok;
@@ -565,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     const int len = f.lengths ? min(max(f.lengths[b], 0), f.n) : f.n;
     const size_t row0 = (size_t)b * f.n;
     const int step = -S * Sh::kSpan, rounds = (int)(((long long)f.n - step - 1) / -step);
-    Tokens<T, Sh, 4, kRing> in;
+    Tokens<T, Sh, 4, kWide> in;
     int tile = ((rounds - 1) * S + rank) * Sh::kSpan, t0 = tile + group * kTok;
     in.set(0, f.x, f.x_stride, row0, channel, t0, step);
     in.set(1, f.r, f.r_stride, row0, channel, t0, step);
@@ -595,28 +609,25 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     auto walk = [&](auto near) {
         for (int round = 0, slot = 0; round < rounds; ++round, t0 += step, tile += step) {
             uint64_t a[kTok], s[kTok], mi[kTok], rest[kTok], add[kTok], over[kTok];  // .., m i, 1 - i, b, i x / m
-            uint64_t kept[kRing ? 1 : kTok] = {};
-            // dy, from the ring again where there is one: registers are what this kernel is short of
-            auto vd = [&](int u) { return kRing ? as_pair(in.get(slot, 3, u)) : kept[kRing ? 0 : u]; };
+            // dy, from the ring each time: registers are what this kernel is short of
+            auto vd = [&](int u) { return as_pair(in.get(slot, 3, t0, u)); };
             Run forward{0, 0};
             in.next(slot, t0, step, at);
 #pragma unroll
             for (int u = 0; u < kTok; ++u) {
                 uint64_t w;
-                Raw<T, 2> rr = in.get(slot, 1, u);
+                Raw<T, 2> rr = in.get(slot, 1, t0, u);
                 if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
                 s[u] = each(one_plus_exp(as_pair(rr)), rcp);
                 decay_of<near()>(decay, s[u], a[u], w);
-                const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, u))), rcp);
-                const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, u)));
+                const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, t0, u))), rcp);
+                const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, t0, u)));
                 mi[u] = mul2(m, i);
                 rest[u] = fma2(i, minus, twice(1.f));
                 add[u] = mul2(m, ix);
                 over[u] = mul2(rm, ix);
-                if (!kRing) kept[kRing ? 0 : u] = as_pair(in.get(slot, 3, u));
                 forward = u ? Run{mul2(a[u], forward.p), fma2(a[u], forward.l, add[u])} : Run{a[u], add[u]};
             }
-            in.used(t0, step, at);
             const uint64_t own = forward.p;
             uint64_t back = mul2(a[kTok - 1], vd(kTok - 1));
 #pragma unroll
@@ -722,14 +733,14 @@ cudaError_t launch_clusters(void (*kernel)(P...), long long units, int S, int sm
     return e ? e : launch_cluster_after(kernel, (unsigned)(units * S), kThreads, S, smem, s, args...);
 }
 
-template <typename T, int kLanes, bool kRing>
+template <typename T, int kLanes, bool kWide>
 cudaError_t forward_as(const Glr &p, const Spread &r, cudaStream_t s) {
     const bool pairs = pairs_ok<T>(p.y, p.y_stride, p.C);
     const long long units = (long long)p.B * r.slabs;
-    return r.S == 1 ? launch_clusters(glr_forward_kernel<T, kLanes, kRing, 1>, units, 1, FwdSmem<T, kLanes, kRing, 1>::kBytes, s, p,
+    return r.S == 1 ? launch_clusters(glr_forward_kernel<T, kLanes, kWide, 1>, units, 1, FwdSmem<T, kLanes, kWide, 1>::kBytes, s, p,
                                       r.slabs, 1, pairs)
-                    : launch_clusters(glr_forward_kernel<T, kLanes, kRing, 2>, units, r.S,
-                                      FwdSmem<T, kLanes, kRing, 2>::kBytes, s, p, r.slabs, r.S, pairs);
+                    : launch_clusters(glr_forward_kernel<T, kLanes, kWide, 2>, units, r.S,
+                                      FwdSmem<T, kLanes, kWide, 2>::kBytes, s, p, r.slabs, r.S, pairs);
 }
 template <typename T>
 cudaError_t forward_of(const Glr &p, cudaStream_t s) {
@@ -747,13 +758,13 @@ cudaError_t step_of(const Glr &p, cudaStream_t s) {
     return launch_after(glr_step_kernel<T>, (unsigned)(((long long)p.B * slabs + 3) / 4), 128, 0, s, p, slabs, pairs);
 }
 
-template <typename T, int kLanes, bool kRing>
+template <typename T, int kLanes, bool kWide>
 cudaError_t backward_as(const GlrBwd &p, const Spread &r, cudaStream_t s) {
     const Glr &f = p.f;
     const bool pairs = pairs_ok<T>(p.dx, p.dx_stride, f.C) && pairs_ok<T>(p.dr, p.dr_stride, f.C) &&
                        pairs_ok<T>(p.dg, p.dg_stride, f.C);
-    const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kRing>, (long long)f.B * r.slabs, r.S,
-                                          Tokens<T, Shape<kLanes, 4>, 4, kRing>::kSmem, s, p, r.slabs, r.S, pairs);
+    const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kWide>, (long long)f.B * r.slabs, r.S,
+                                          Tokens<T, Shape<kLanes, 4>, 4, kWide>::kSmem, s, p, r.slabs, r.S, pairs);
     if (e) return e;
     return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {{p.ddecay, 0, nullptr}}, f.dt, p.header}, s);
 }
