@@ -75,7 +75,8 @@ def glr_case(seed, B, n, C, T, ragged_lengths, slow=True):
 GLR = [(1, 1, 8, False, 0, 0, True), (3, 2, 24, True, 8, 0, True), (4, 37, 264, True, 8, 8, True),
        (2, 130, 203, False, 5, 3, False), (5, 64, 130, True, 0, 0, True), (1, 1000, 64, False, 8, 0, True),
        (2, 600, 70, True, 1, 1, False), (1, 65, 1, False, 3, 2, True), (40, 33, 66, True, 0, 0, True),
-       (1, 2500, 100, False, 0, 0, True), (70, 5, 640, False, 0, 0, True)]
+       (1, 2500, 100, False, 0, 0, True), (70, 5, 640, False, 0, 0, True), (40, 32, 520, True, 8, 0, False),
+       (120, 9, 203, True, 3, 1, True), (304, 1, 30, True, 0, 0, True)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
