@@ -1,33 +1,43 @@
 // Sums of partial rows, in a fixed order: the last step of gradients that are sums over tokens.
-#include "hla_internal.h"
+#include "hla_vec.cuh"
 
 namespace hla {
 namespace {
 
-constexpr int kCols = 32, kGroups = 32;  // columns of a block, and the rows it reads side by side
+constexpr int kCols = 32, kThreads = 1024;  // columns of a block
 
-// (bound by latency: each thread's loads are independent, a few dozen at most; 304 rows of 6144 columns take
-// 3 us)
-__global__ void __launch_bounds__(kCols *kGroups) column_sum_kernel(ColumnSum p) {
-    __shared__ float red[kGroups][kCols + 1];
+// Bound by latency: with four columns a thread (kV 4) all the rows of a block are on their way at once
+template <int kV>
+__global__ void __launch_bounds__(kThreads) column_sum_kernel(ColumnSum p) {
+    constexpr int kLanes = kCols / kV, kGroups = kThreads / kLanes;  // lanes of a row, rows side by side
+    __shared__ float red[kCols][kGroups + 1];
     let_next_begin();
     after_previous();
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // no device-side waits before: never an error
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const int place = threadIdx.x % kLanes * kV, group = threadIdx.x / kLanes;
     const long long cols = (long long)p.C * p.parts, at = (long long)blockIdx.x * kCols;
-    float sum = 0.f;
-    if (at + lane < cols) {
-        const float *from = p.partial + at + lane;
+    float sum[kV] = {};
+    if (at + place < cols) {
+        const float *from = p.partial + at + place;
 #pragma unroll 8
-        for (long long r = group; r < p.rows; r += kGroups) sum += from[r * cols];
+        for (long long r = group; r < p.rows; r += kGroups) {
+            float v[kV];
+            VecIo<float, kV>::load(from + r * cols, v);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) sum[i] += v[i];
+        }
     }
-    red[group][lane] = sum;
+#pragma unroll
+    for (int i = 0; i < kV; ++i) red[place + i][group] = sum[i];
     __syncthreads();
     // warp w: column w
-    sum = red[lane][group];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    float all = 0.f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const long long c = at + group;
+    for (int k = 0; k < kGroups; k += 32) all += red[w][k + lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    const long long c = at + w;
     if (lane == 0 && c < cols) {
         const int part = (int)(c / p.C), i = (int)(c - (long long)part * p.C);
 #pragma unroll
@@ -37,7 +47,7 @@ __global__ void __launch_bounds__(kCols *kGroups) column_sum_kernel(ColumnSum p)
             const float by = !out.factor           ? 1.f
                              : p.dt == HLA_BF16 ? to_f32(static_cast<const __nv_bfloat16 *>(out.factor)[i])
                                                 : static_cast<const float *>(out.factor)[i];
-            out.to[i] = sum * by;
+            out.to[i] = all * by;
         }
     }
 }
@@ -46,7 +56,9 @@ __global__ void __launch_bounds__(kCols *kGroups) column_sum_kernel(ColumnSum p)
 
 cudaError_t column_sum_launch(const ColumnSum &p, cudaStream_t s) {
     const long long cols = (long long)p.C * p.parts;
-    return launch_after(column_sum_kernel, (unsigned)((cols + kCols - 1) / kCols), kCols * kGroups, 0, s, p);
+    const unsigned blocks = (unsigned)((cols + kCols - 1) / kCols);
+    return cols % 4 == 0 ? launch_after(column_sum_kernel<4>, blocks, kThreads, 0, s, p)
+                         : launch_after(column_sum_kernel<1>, blocks, kThreads, 0, s, p);
 }
 
 }  // namespace hla

@@ -20,7 +20,6 @@
 // Every wait has a limit: it sets the workspace's error word and the block's `stop`, after which all roles leave,
 // copies and products in flight are waited for (with a limit), and tensor memory is released.
 #include <climits>
-#include <type_traits>
 
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
@@ -160,40 +159,43 @@ __device__ __forceinline__ Tile tile_of(const Work &w, int i) {
     return {m, first + i - m * width, part};
 }
 
-// 32 staged rows of kBytes from or to global memory, row by row: 16 bytes a lane, or an element
-template <bool kLoad, int kBytes, typename E>
-__device__ __forceinline__ void copy_rows(char *staged, E *at, long long row, int rows, int cols, bool wide) {
+// 32 staged rows of kBytes to global memory, row by row: 16 bytes a lane, or an element, eight in flight
+template <int kBytes, typename E>
+__device__ __forceinline__ void store_rows(const char *staged, E *at, long long row, int rows, int cols, bool wide) {
     const int lane = threadIdx.x & 31;
-    constexpr int kLanes = kBytes / 16, kEach = 16 / sizeof(E);
+    constexpr int kLanes = kBytes / 16, kEach = 16 / sizeof(E), kCols = kBytes / (int)sizeof(E);
     if (wide) {
         const int c = (lane % kLanes) * kEach;
 #pragma unroll
         for (int r = lane / kLanes; r < 32; r += 32 / kLanes)
-            if (r < rows && c < cols) {
-                uint4 *s = reinterpret_cast<uint4 *>(staged + r * kPitch + c * sizeof(E));
-                if constexpr (kLoad) *s = *reinterpret_cast<const uint4 *>(at + r * row + c);
-                else *reinterpret_cast<uint4 *>(at + r * row + c) = *s;
-            }
+            if (r < rows && c < cols)
+                *reinterpret_cast<uint4 *>(at + r * row + c) = *reinterpret_cast<const uint4 *>(staged + r * kPitch + c * sizeof(E));
     } else {
-        // (eight in flight)
-        constexpr int kCols = kBytes / (int)sizeof(E);
 #pragma unroll 1
         for (int i0 = lane; i0 < 32 * kCols; i0 += 256) {
-            std::remove_const_t<E> v[8];
+            E v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = *reinterpret_cast<const E *>(staged + (i0 + 32 * j) / kCols * kPitch + (i0 + 32 * j) % kCols * sizeof(E));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = i0 + 32 * j, r = i / kCols, c = i % kCols;
-                char *s = staged + r * kPitch + c * sizeof(E);
-                if constexpr (!kLoad) v[j] = *reinterpret_cast<const E *>(s);
-                else if (r < rows && c < cols) memcpy(&v[j], at + r * row + c, sizeof(E));
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int i = i0 + 32 * j, r = i / kCols, c = i % kCols;
-                if constexpr (kLoad) memcpy(staged + r * kPitch + c * sizeof(E), &v[j], sizeof(E));
-                else if (r < rows && c < cols) at[r * row + c] = v[j];
+                const int r = (i0 + 32 * j) / kCols, c = (i0 + 32 * j) % kCols;
+                if (r < rows && c < cols) at[r * row + c] = v[j];
             }
         }
+    }
+}
+// 32 rows of 32 elements from global memory, eight in flight (behind the last row or column: 0)
+__device__ __forceinline__ void load_rows(char *staged, const __nv_bfloat16 *at, long long row, int rows, int cols) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+        __nv_bfloat16 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = r0 + j < rows && lane < cols ? at[(r0 + j) * row + lane] : __float2bfloat16(0.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<__nv_bfloat16 *>(staged + (r0 + j) * kPitch + lane * 2) = v[j];
     }
 }
 
@@ -352,6 +354,17 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         for (int i = blockIdx.x / 2; i < tiles; i += clusters) {
             const Work &w = work_of(i);
             const Tile t = place_of(i);
+            // kGrad: a lane's part of dout's next 32 columns (four rows' 16 bytes, eight rows apart), the first before the
+            // tile is there
+            uint4 next[4] = {};
+            auto fetch = [&](int c) {
+                const int n0 = t.n * kHalf + c + lane % 4 * 8, m0 = t.m * kTile + rank * kHalf + quarter * 32 + lane / 4;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (m0 + 8 * j < w.rows && n0 < w.cols)
+                        next[j] = *reinterpret_cast<const uint4 *>(w.dout + (m0 + 8 * j) * w.dout_row + n0);
+            };
+            if (kMode == kGrad && w.dout_wide) fetch(0);
             if (!__all_sync(0xffffffffu, wait(&bars->done[b], bphase, bars, header, 5))) break;
             tc_fence_after();
             const uint32_t from = taddr(tmem + b * 256, quarter * 32, 0);
@@ -386,7 +399,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         }
                     }
                     __syncwarp();
-                    copy_rows<false, 128>(mine, static_cast<__nv_bfloat16 *>(w.out) + m0 * w.out_row + n0,
+                    store_rows<128>(mine, static_cast<__nv_bfloat16 *>(w.out) + m0 * w.out_row + n0,
                                                          w.out_row, rows, w.cols - n0, w.out_wide);
                     __syncwarp();
                 }
@@ -394,8 +407,14 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 #pragma unroll 1
                 for (int c = 0; c < kHalf; c += 32) {
                     const int n0 = t.n * kHalf + c;
-                    copy_rows<true, 64>(mine, w.dout + m0 * w.dout_row + n0, w.dout_row, rows,
-                                                             w.cols - n0, w.dout_wide);
+                    if (w.dout_wide) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<uint4 *>(mine + (lane / 4 + 8 * j) * kPitch + lane % 4 * 16) = next[j];
+                        if (c + 32 < kHalf) fetch(c + 32);
+                    } else {
+                        load_rows(mine, w.dout + m0 * w.dout_row + n0, w.dout_row, rows, w.cols - n0);
+                    }
                     __syncwarp();
                     uint32_t g[32], u[32];
                     tmem_ld32(from + c, g);
@@ -427,8 +446,8 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(w.out) + m0 * w.out_row + n0;
                     // (dZ's rows are padded to 16 bytes: what is written behind the last column is not read)
                     const int cols = (w.cols - n0 + 7) & ~7;
-                    copy_rows<false, 64>(mine, to, w.out_row, rows, cols, true);
-                    copy_rows<false, 64>(mine + 64, to + w.out_plane, w.out_row, rows, cols, true);
+                    store_rows<64>(mine, to, w.out_row, rows, cols, true);
+                    store_rows<64>(mine + 64, to + w.out_plane, w.out_row, rows, cols, true);
                     __syncwarp();
                 }
             } else if (w.parts == 1) {
@@ -450,7 +469,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                                 pack_bf16x2(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7])));
                     }
                     __syncwarp();
-                    copy_rows<false, 128>(
+                    store_rows<128>(
                         mine, static_cast<__nv_bfloat16 *>(w.out) + plane * w.out_plane + m0 * w.out_row + n0, w.out_row, rows,
                         w.cols - n0, w.out_wide);
                     __syncwarp();
@@ -469,7 +488,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     for (int j = 0; j < 32; j += 4)
                         *reinterpret_cast<uint4 *>(row + j * 4) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                     __syncwarp();
-                    copy_rows<false, 128>(mine, out + n0, w.cols, rows, w.cols - n0, w.cols % 4 == 0);
+                    store_rows<128>(mine, out + n0, w.cols, rows, w.cols - n0, w.cols % 4 == 0);
                     __syncwarp();
                 }
             }

@@ -478,19 +478,30 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
 #pragma unroll
             for (int i = 0; i < kTiles; ++i, t0 += step) {
                 in.next(slot, t0, step, at);
+                // (a block's second tile may lie behind the sequence as a whole)
+                const bool some = kTiles == 1 || i == 0 || t0 - group * kTok < len;
+                if (some) {
 #pragma unroll
-                for (int u = 0; u < kTok; ++u) {
-                    uint64_t a, w;
-                    Raw<T, 2> rr = in.get(slot, 1, t0, u);
-                    if (t0 + u >= len) shut(rr);  // (x is 0 there)
-                    decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
-                    const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
-                    // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-                    const uint64_t add =
-                        mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, t0, u)));
-                    h[u] = u ? fma2(a, h[u - 1], add) : add;
-                    pr[u] = u ? mul2(a, pr[u - 1]) : a;
-                    if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
+                    for (int u = 0; u < kTok; ++u) {
+                        uint64_t a, w;
+                        Raw<T, 2> rr = in.get(slot, 1, t0, u);
+                        if (t0 + u >= len) shut(rr);  // (x is 0 there)
+                        decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
+                        const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
+                        // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
+                        const uint64_t add =
+                            mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, t0, u)));
+                        h[u] = u ? fma2(a, h[u - 1], add) : add;
+                        pr[u] = u ? mul2(a, pr[u - 1]) : a;
+                        if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
+                    }
+                } else {
+#pragma unroll
+                    for (int u = 0; u < kTok; ++u) {
+                        h[u] = 0;
+                        pr[u] = twice(1.f);
+                        if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], 0};
+                    }
                 }
                 if (++slot == kSlots) slot = 0;
                 mine[i] = of_warp<Sh, 1>({pr[kTok - 1], h[kTok - 1]}, ahead[i]);
