@@ -552,7 +552,8 @@ hla_status hla_glr_backward(const void *x, const void *r, const void *g, const f
  * means over a row's C columns; k = 1 without dropout, else 0 or 1 / (1 - dropout): value (row,
  * column) is dropped where its 32 random bits are below floor(dropout 2^32), bits that
  * Philox4x32-10 gives for the counter (column / 4, row, offset low, offset high) and the key (seed
- * low, seed high), word column % 4.  The mask is not stored: the gradient makes it again.
+ * low, seed high), word column % 4.  The mask is not stored: the gradient makes it again.  Where a value
+ * is dropped, y and gate may hold anything, NaN and infinities too (y without post_norm, whose mean has it).
  * x, y, gate : device [rows, C], row strides x_stride, y_stride, gate_stride, of type dt; gate may be NULL (= 1)
  * w_post, scale, w_pre : device [C] of type dt, or NULL (= 1; w_post and w_pre are not read without their norm)
  * x_out : device [rows, C], row stride x_out_stride (written; may equal x, with its stride)

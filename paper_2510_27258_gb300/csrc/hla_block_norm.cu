@@ -205,25 +205,29 @@ struct Drop {
             }
         }
     }
-    template <int kN>
-    __device__ __forceinline__ void apply(const BlockNorm &p, long long row, int t, Pairs (&v)[kN]) const {
-        bool keep[kPer];
+    struct Kept {
+        bool on[kPer];
+        // selected, not multiplied: what y and gate hold where a value is dropped, NaN and infinities too, reaches nothing
+        __device__ __forceinline__ void apply(Pairs &v) const {
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                float a, b;
+                unpair(v[i], a, b);
+                v[i] = pair(on[2 * i] ? a : 0.f, on[2 * i + 1] ? b : 0.f);
+            }
+        }
+    };
+    __device__ __forceinline__ Kept of(const BlockNorm &p, long long row, int t) const {
+        Kept keep;
         const uint64_t of_row = row_of(p, (uint32_t)row);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             Words w = words_of(p, group[j], of_row);
             exchange(w, t);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) keep[4 * j + i] = w.w[i] >= p.drop_below;
+            for (int i = 0; i < 4; ++i) keep.on[4 * j + i] = w.w[i] >= p.drop_below;
         }
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                float a, b;
-                unpair(v[n][i], a, b);
-                v[n][i] = pair(keep[2 * i] ? a : 0.f, keep[2 * i + 1] ? b : 0.f);
-            }
+        return keep;
     }
 };
 
@@ -408,10 +412,10 @@ __global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kFwdThreads
     in.begin(nullptr, row);
     for (; row - in_warp < p.rows; row += step) {
         const bool live = kOfWarp == 1 || row < p.rows;
-        Pairs x, y, f[1];
+        Pairs x, y, f;
         in.get(0, 0, row, x);
         in.get(0, 1, row, y);
-        if (p.gate) in.get(0, 2, row, f[0]);
+        if (p.gate) in.get(0, 2, row, f);
         in.used(row);
         Sum<1> s1;
         if (p.post) {
@@ -423,14 +427,14 @@ __global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kFwdThreads
         }
         if (p.gate) {
             Pairs slope;
-            activate<false>(p.act, f[0], slope);
+            activate<false>(p.act, f, slope);
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) f[0][i] = mul2(f[0][i], scale[i]);
+            for (int i = 0; i < kPairs; ++i) f[i] = mul2(mul2(f[i], scale[i]), y[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPairs; ++i) f[0][i] = scale[i];
+            for (int i = 0; i < kPairs; ++i) f[i] = mul2(scale[i], y[i]);
         }
-        if (p.drop) drop.apply(p, row, t, f);
+        if (p.drop) drop.of(p, row, t).apply(f);
         float r1 = 1.f;
         if (p.post) {
             read<kMax>(s1, red, turn);
@@ -439,7 +443,7 @@ __global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kFwdThreads
         uint64_t sum = 0;
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            x[i] = fma2(mul2(y[i], twice(r1)), f[0][i], mul2(x[i], twice(p.alpha)));
+            x[i] = fma2(f[i], twice(r1), mul2(x[i], twice(p.alpha)));
             sum = fma2(x[i], x[i], sum);
         }
         Sum<1> s2;
@@ -579,7 +583,12 @@ __global__ void __launch_bounds__(block_of(kMax), kMax == 1024 ? 1 : kBwdThreads
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = f[1][i] = twice(1.f);
         }
-        if (p.drop) drop.apply(p, row, t, f);
+        if (p.drop) {
+            const auto keep = drop.of(p, row, t);
+            keep.apply(f[0]);
+            keep.apply(f[1]);
+            if (!p.post) keep.apply(y);  // (with the norm, u of dropped values is part of dy)
+        }
         Pairs fs;  // what multiplies u in x', and t in dn
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) fs[i] = mul2(f[0][i], scale[i]);
@@ -730,7 +739,7 @@ __global__ void __launch_bounds__(1024) block_norm_wide_backward_kernel(BlockNor
             float x;
             const float tg = back(c, x), u = in.y(c) * r1, w = Wide<T>::of(p.w_post, c), sc = Wide<T>::of(p.scale, c);
             const bool on = k != 0.f;
-            const float tk = on ? tg * k : 0.f, through = tk * a;
+            const float tk = on ? tg * k : 0.f, through = on ? tk * a : 0.f;
             from_f32(static_cast<T *>(q.dx) + row * q.dx_stride + c, p.alpha * tg);
             from_f32(static_cast<T *>(q.dy) + row * q.dy_stride + c,
                      p.post ? r1 * (through * sc * w - u * m1) : through * sc * w);

@@ -1,6 +1,7 @@
 """The block's operators (gated recurrence, norms around a block, gated feed-forward projections) on the GPU
 against their definitions in 64 bits, element by element within the bounds of block_ref.  A bf16 output
 adds its one rounding, 2^-9 of the next power of two: 2^-8 of the value."""
+import numpy as np
 import pytest
 import torch
 
@@ -297,6 +298,24 @@ def test_block_norm_batches_and_masks(hla):
     assert abs(float(kept.float().mean()) - 0.5) < 0.03 and abs(float((kept == other).float().mean()) - 0.5) < 0.03
     strided = hla.hla_block_norm_forward(*(sliced(v[k], 1, 1) for k in ("x", "y", "gate")), **own)[0]
     assert torch.equal(strided != args[0], kept)
+
+
+@pytest.mark.parametrize("C", [24, 203, 256, 2048, 2047, 8200])
+def test_block_norm_dropped_values_that_are_not_finite(hla, C):
+    """What y and gate hold where a value is dropped reaches nothing, in either direction."""
+    g, v, kw, own = norm_case(11, 40, C, torch.bfloat16, dropout=0.5, post=False)
+    x, y, gate, dx_out, dh = (on(t) for t in (v["x"], v["y"], v["gate"], randn(g, 40, C, T=torch.bfloat16),
+                                              randn(g, 40, C, T=torch.bfloat16)))
+    dropped = on(torch.from_numpy(R.words(40, C, kw["seed"], kw["offset"]) < np.uint64(2 ** 31)))
+    odd = torch.arange(C, device=DEV) % 2 == 1
+    bad_y = torch.where(dropped, torch.where(odd, float("nan"), float("inf")).to(y.dtype), y)
+    bad_gate = torch.where(dropped, torch.where(odd, -float("inf"), float("nan")).to(y.dtype), gate)
+    w = {k: on(v[k]) for k in ("w_post", "scale", "w_pre")}
+    assert all(torch.equal(a, b) for a, b in zip(hla.hla_block_norm_forward(x, y, gate, **w, **own),
+                                                 hla.hla_block_norm_forward(x, bad_y, bad_gate, **w, **own)))
+    for a, b in zip(hla.hla_block_norm_backward(x, y, gate, dx_out, dh, **w, **own),
+                    hla.hla_block_norm_backward(x, bad_y, bad_gate, dx_out, dh, **w, **own)):
+        assert a is b is None or torch.equal(a, b)
 
 
 def test_block_norm_rows_of_zeros(hla):
