@@ -485,7 +485,9 @@ hla_status hla_qk_norm_backward(const void *q, const void *k, const void *wq, co
  * Rows, strides, lengths and overlap are as above: token t of sequence b is row
  * b*n + t at a row stride in elements, and no alignment beyond the element's is
  * asked of rows.  Sums over tokens are made in a fixed order: equal inputs give
- * equal bits.
+ * equal bits.  Calls that share a workspace run one after another, on one stream or ordered by
+ * events; a captured graph's workspace stays its own while the graph may run.  No call's workspace
+ * keeps anything from one call for the next.
  */
 
 /* Activations of a gate (also the slopes of the gradients). */
@@ -503,15 +505,16 @@ int hla_glr_marks(int n);
  *   s_t = sigmoid(r_t),  a_t = exp(decay s_t),  i_t = sigmoid(g_t),
  *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) i_t x_t,   y_t = h_t
  * x, r, g, y : device [B, n, C], row strides x_stride, r_stride, g_stride, y_stride, of type dt
- * decay : device fp32 [C], below 0 (where it is 0, gradients of r and decay are unbounded)
+ * decay : device fp32 [C], finite and below 0 (where it is 0, gradients of r and decay are unbounded)
  * state_in  : device fp32 [B, C] or NULL (= 0)
  * state_out : device fp32 [B, C] or NULL; the state after lengths[b] tokens.  May equal state_in.
  * marks     : device fp32 [B, hla_glr_marks(n), C] or NULL; receives the state before
  *             every 32nd token, which hla_glr_backward reads
  * decay, states and marks are 16-byte aligned.
  * No workspace (should a wait between the blocks of one sequence run past its limit of 2 s, states and
- * outputs are NaN from there on).  fp32 throughout for both types; a NaN or infinity in a token reaches that token's
- * output and, where it enters the state, later ones, and no earlier one.
+ * outputs are NaN from there on).  fp32 throughout for both types; i_t below 1e-19 counts as 0.  A NaN
+ * or infinity in a token reaches that token's output and, where it enters the state, later ones, and no
+ * earlier one.
  */
 hla_status hla_glr_forward(const void *x, const void *r, const void *g, const float *decay, void *y, hla_dtype dt, int B,
                            int n, int C, long long x_stride, long long r_stride, long long g_stride, long long y_stride,

@@ -222,8 +222,10 @@ hla_status hla_block_norm_backward(const void *x, const void *y, const void *gat
     cudaStream_t s = as_stream(stream);
     if (rows == 0) {
         HLA_TRY(clear_header(workspace, s));
-        for (float *out : {dw_post, dscale, dw_pre})
-            if (out) HLA_TRY(cuda_status(cudaMemsetAsync(out, 0, sizeof(float) * (size_t)C, s), "clearing weight gradients"));
+        for (float *out : {dw_post, dscale, dw_pre}) {
+            if (!out) continue;
+            HLA_TRY(cuda_status(cudaMemsetAsync(out, 0, sizeof(float) * (size_t)C, s), "clearing weight gradients"));
+        }
         return HLA_OK;
     }
     q.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + kWsHeaderBytes);

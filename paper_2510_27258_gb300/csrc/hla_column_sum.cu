@@ -6,7 +6,8 @@ namespace {
 
 constexpr int kCols = 32, kThreads = 1024;  // columns of a block
 
-// Bound by latency: with four columns a thread (kV 4) all the rows of a block are on their way at once
+// Bound by latency: with four columns a thread (kV 4) all the rows of a block are on their way at once (304 rows of 4096
+// columns, not in cache: 9 us with one column a thread)
 template <int kV>
 __global__ void __launch_bounds__(kThreads) column_sum_kernel(ColumnSum p) {
     constexpr int kLanes = kCols / kV, kGroups = kThreads / kLanes;  // lanes of a row, rows side by side

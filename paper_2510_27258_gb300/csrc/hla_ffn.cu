@@ -5,19 +5,26 @@
 //
 // One tiled product serves all four: a block of 256 threads forms 128 x 128 outputs (64 x 64 where those would leave
 // SMs without a tile: there two groups of threads share each panel's indices, so that SMs have twice the warps), a thread
-// 8 x 8 (4 x 4) of them, from panels of 16 in a ring of shared memory, all but the one in
-// use in flight.  A panel lies as its matrix does: where the sum's index is the contiguous one a thread reads four
-// (two) of its indices of a row at a time, else four rows of an index, so that either way a wide access feeds many products.
-// The forward's tile is half gate and half up columns of the same features, so that the activation and product happen in
-// registers.  The gradient keeps [dZg dZu] in the workspace; its last two products, whose sums are over 2 F and over tokens and
-// whose tiles may be few, are cut along the sum, and the parts are added in their order.
+// 8 x 8 (4 x 4) of them, from panels of 16 in a ring of shared memory, all but the one in use in flight.  A panel lies
+// as its matrix does: where the sum's index is the contiguous one a thread reads four (two) of its indices of a row at a
+// time, else four rows of an index, so that either way a wide access feeds many products.  The forward's tile is half
+// gate and half up columns of the same features, so that the activation and product happen in registers.  The gradient
+// keeps [dZg dZu] in the workspace; its last two products, whose sums are over 2 F and over tokens and whose tiles may
+// be few, are cut along the sum, and the parts are added in their order.
+//
+// Bound by the CUDA cores' 80 TFLOP/s, from which shared memory's bandwidth and few warps keep it: gradient of 333 x 260 x
+// 1031 72 us (one group of threads 85, four 106), where 1.3 blocks an SM are all there is; large products 35 TFLOP/s.
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
 
 namespace hla {
 namespace {
 
-constexpr int kThreads = 256, kDepth = 16, kStages = 4, kGroups = 2;
+constexpr int kThreads = 256;
+// of a tile of 128 or 64: indices of a panel, panels of the ring, groups of threads that share a panel's indices
+constexpr int depth_of(int tile) { return tile == 128 ? 32 : 16; }
+constexpr int stages_of(int tile) { return tile == 128 ? 3 : 4; }
+constexpr int groups_of(int tile) { return tile == 128 ? 1 : 2; }
 
 enum Mode { kProduct, kParts, kOut, kGrad };
 
@@ -56,6 +63,7 @@ __device__ __forceinline__ float act_of(int act, float v, float &slope) {
 // behind the first's where pair > 0
 template <int kRows, bool kAlong>
 struct Panel {
+    static constexpr int kDepth = depth_of(kRows);
     static constexpr int kPitch = (kAlong ? kDepth : kRows) + 4, kFloats = (kAlong ? kRows : kDepth) * kPitch;
     static constexpr int kRun = (kAlong ? kDepth : kRows) / 4, kChunks = kRows * kDepth / 4;
     // (by a block of kBlock threads)
@@ -75,7 +83,8 @@ struct Panel {
             const float *from = m.p + (kAlong ? row * m.step + k : k * m.step + row);
             const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(to + line * kPitch + four));
             if (m.wide) {
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(min(max(left, 0), 4) * 4)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from),
+                             "r"(min(max(left, 0), 4) * 4)
                              : "memory");
             } else {
 #pragma unroll
@@ -114,11 +123,9 @@ struct Panel {
 };
 
 // kTile 128 or 64; kA, kB: whether the sum's index is the contiguous one
-constexpr int groups_of(int tile) { return tile == 64 ? kGroups : 1; }
-
 template <int kTile, bool kA, bool kB, Mode kMode>
 __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel(Product p) {
-    constexpr int kG = groups_of(kTile);
+    constexpr int kG = groups_of(kTile), kDepth = depth_of(kTile), kStages = stages_of(kTile);
     constexpr int kE = kTile / 16, kK = kTile == 64 ? 4 : 2;  // a thread's rows and columns; indices read at a time
     constexpr bool kPair = kMode == kOut || kMode == kGrad;
     constexpr int kCols = kPair ? kTile / 2 : kTile;
@@ -140,7 +147,12 @@ __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) send(i, k_lo + i * kDepth);
+    // pairs of products at a time (tiles of 128): of neighbouring indices of the sum where both panels have them side by
+    // side, else of neighbouring columns
+    constexpr bool kTwo = kTile == 128, kAlong = kA && kB;
+    constexpr int kPairs = kAlong ? kE : kE / 2;
     float acc[kE][kE] = {};
+    uint64_t pairs[kTwo ? kE : 1][kPairs] = {};
     int stage = 0;
     for (int k0 = k_lo; k0 < k_hi; k0 += kDepth, stage = stage + 1 < kStages ? stage + 1 : 0) {
         ring_wait<kStages - 2>();
@@ -153,15 +165,48 @@ __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel
             float a[kK][kE], b[kK][kE];
             A::template get<kE, kK>(as, ty, k, a);
             B::template get<kE, kK>(bs, tx, k, b);
+            if constexpr (kTwo) {
 #pragma unroll
-            for (int q = 0; q < kK; ++q)
+                for (int q = 0; q < kK; q += kAlong ? 2 : 1) {
+                    uint64_t ap[kE], bp[kPairs];
 #pragma unroll
-                for (int i = 0; i < kE; ++i)
+                    for (int i = 0; i < kE; ++i) ap[i] = pair(a[q][i], a[kAlong ? q + 1 : q][i]);
 #pragma unroll
-                    for (int j = 0; j < kE; ++j) acc[i][j] = fmaf(a[q][i], b[q][j], acc[i][j]);
+                    for (int j = 0; j < kPairs; ++j) {
+                        if constexpr (kAlong) bp[j] = pair(b[q][j], b[q + 1][j]);
+                        else bp[j] = pair(b[q][2 * j], b[q][2 * j + 1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kE; ++i)
+#pragma unroll
+                        for (int j = 0; j < kPairs; ++j) pairs[i][j] = fma2(ap[i], bp[j], pairs[i][j]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kK; ++q)
+#pragma unroll
+                    for (int i = 0; i < kE; ++i)
+#pragma unroll
+                        for (int j = 0; j < kE; ++j) acc[i][j] = fmaf(a[q][i], b[q][j], acc[i][j]);
+            }
         }
     }
     ring_wait<0>();
+    if constexpr (kTwo) {
+#pragma unroll
+        for (int i = 0; i < kE; ++i)
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                float x, y;
+                unpair(pairs[i][j], x, y);
+                if constexpr (kAlong) {
+                    acc[i][j] = x + y;
+                } else {
+                    acc[i][2 * j] = x;
+                    acc[i][2 * j + 1] = y;
+                }
+            }
+    }
     if constexpr (kG > 1) {  // the groups' sums, in their order
         __syncthreads();
 #pragma unroll 1
@@ -229,26 +274,44 @@ constexpr int kSMs = 152;
 long long tiles(long long M, long long N, int tile, bool paired) {
     return ((M + tile - 1) / tile) * ((N + (paired ? tile / 2 : tile) - 1) / (paired ? tile / 2 : tile));
 }
-bool small_tiles(long long M, long long N, bool paired) { return tiles(M, N, 128, paired) < kSMs; }
 
-// how many parts a sum is cut into: as many as bring two blocks an SM, each of 128 indices or more
-int parts_of(long long M, long long N, long long sum) {
-    const long long t = tiles(M, N, small_tiles(M, N, false) ? 64 : 128, false);
-    const long long by_blocks = 2 * kSMs / t, by_sum = sum / 128;
-    const long long parts = by_blocks < by_sum ? by_blocks : by_sum;
-    return parts < 1 ? 1 : parts > 64 ? 64 : (int)parts;
+// Tiles of 128 or 64, and how many parts the sum is cut into
+struct Plan {
+    int tile, parts;
+};
+// What takes least by this count, in us: the blocks that an SM works through, each with its share of the sum, at the rates
+// that full SMs reach (48 and 36 TFLOP/s over all of them; blocks of 64 that have an SM each take 1.7 times as long),
+// and the parts' way through memory.  A part has 128 indices or more.  Against tiles of 128 wherever there are 152 and
+// as many parts as bring two blocks an SM: gradient of 2048 x 1024 x 2816 1522 us instead of 1849, of 1000 x 512 x 1500 268
+// instead of 343.
+Plan plan(long long M, long long N, long long sum, bool paired, int most) {
+    Plan best{128, 1};
+    double least = 0;
+    for (int tile = 128; tile >= 64; tile /= 2)
+        for (int parts = 1; parts == 1 || (parts <= most && sum / parts >= 128); ++parts) {
+            const long long rounds = (tiles(M, N, tile, paired) * parts + kSMs - 1) / kSMs;
+            const double each = 2. * tile * tile * (double)((sum + parts - 1) / parts) / ((tile == 128 ? 48e6 : 36e6) / kSMs);
+            const double start = tile == 128 ? 2 : rounds == 1 ? 0.7 * each : 0;
+            const double us = rounds * each + start + (parts > 1 ? 5 + parts * 8e-6 * (double)(M * N) / 6 : 0);
+            if ((tile == 128 && parts == 1) || us < least) {
+                least = us;
+                best = {tile, parts};
+            }
+        }
+    return best;
 }
-int parts_dx(int M, int K, int F) { return parts_of(M, K, 2LL * F); }
-int parts_dw(int M, int K, int F) { return parts_of(2LL * F, K, M); }
+constexpr int kMostParts = 64;
+Plan plan_dx(int M, int K, int F) { return plan(M, K, 2LL * F, false, kMostParts); }
+Plan plan_dw(int M, int K, int F) { return plan(2LL * F, K, M, false, kMostParts); }
 
 template <bool kA, bool kB, Mode kMode>
-cudaError_t product(Product p, int parts, cudaStream_t s) {
+cudaError_t product(Product p, const Plan &by, cudaStream_t s) {
     constexpr bool paired = kMode == kOut || kMode == kGrad;
-    const int tile = small_tiles(p.M, p.N, paired) ? 64 : 128, cols = paired ? tile / 2 : tile;
+    const int tile = by.tile, cols = paired ? tile / 2 : tile;
     p.across = (p.N + cols - 1) / cols;
-    const dim3 grid((unsigned)p.across * ((p.M + tile - 1) / tile), parts);
+    const dim3 grid((unsigned)p.across * ((p.M + tile - 1) / tile), by.parts);
     auto as = [&](auto kernel, int floats) -> cudaError_t {
-        const int smem = kStages * floats * (int)sizeof(float);
+        const int smem = stages_of(tile) * floats * (int)sizeof(float);
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         return e ? e : launch_after(kernel, grid, kThreads * groups_of(tile), smem, s, p);
     };
@@ -262,17 +325,18 @@ size_t parts_floats(int parts, long long M, long long N) { return parts > 1 ? (s
 
 // a product whose sum is cut into parts, which lie in `sums` until they are added
 template <bool kA>
-cudaError_t cut_product(Product p, int parts, float *sums, cudaStream_t s) {
-    if (parts == 1) return product<kA, false, kProduct>(p, 1, s);
+cudaError_t cut_product(Product p, const Plan &by, float *sums, cudaStream_t s) {
+    const int parts = by.parts, depth = depth_of(by.tile);
+    if (parts == 1) return product<kA, false, kProduct>(p, by, s);
     float *out = p.out;
     const long long out_row = p.out_row, all = (long long)p.M * p.N, blocks = (all + kThreads - 1) / kThreads;
-    p.per = ((p.K + parts - 1) / parts + kDepth - 1) / kDepth * kDepth;
+    p.per = ((p.K + parts - 1) / parts + depth - 1) / depth * depth;
     p.out = sums;
     p.out_row = p.N;
-    const cudaError_t e = product<kA, false, kParts>(p, parts, s);
+    const cudaError_t e = product<kA, false, kParts>(p, by, s);
     if (e) return e;
-    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts, p.M, p.N,
-                        out, out_row);
+    return launch_after(ffn_parts_kernel, (unsigned)(blocks < 8 * kSMs ? blocks : 8 * kSMs), kThreads, 0, s, sums, parts,
+                        p.M, p.N, out, out_row);
 }
 
 // [dZg dZu] in rows of whole 16 bytes
@@ -281,7 +345,7 @@ long long dz_row(int F) { return (2LL * F + 3) / 4 * 4; }
 cudaError_t forward_f32(const Ffn &p, cudaStream_t s) {
     const Product q{mat(floats(p.x), p.x_stride), mat(floats(p.w), p.K), p.M, p.F, p.K, p.act, p.K, 0,
                     static_cast<float *>(p.out), p.out_stride, nullptr, 0, reinterpret_cast<WsHeader *>(p.ws)};
-    return product<true, true, kOut>(q, 1, s);
+    return product<true, true, kOut>(q, plan(p.M, p.F, p.K, true, 1), s);
 }
 
 cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
@@ -291,17 +355,18 @@ cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     const long long row = dz_row(f.F);
     const Product q{mat(floats(f.x), f.x_stride), mat(floats(f.w), f.K), f.M, f.F, f.K, f.act, f.K, 0, dz, row,
                     floats(p.dout), p.dout_stride, reinterpret_cast<WsHeader *>(f.ws)};
-    cudaError_t e = product<true, true, kGrad>(q, 1, s);
+    cudaError_t e = product<true, true, kGrad>(q, plan(f.M, f.F, f.K, true, 1), s);
     if (e) return e;
     float *sums = dz + (size_t)f.M * row;
     const Product dw{mat(dz, row), mat(floats(f.x), f.x_stride), F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
                      nullptr, 0, nullptr};
-    e = cut_product<false>(dw, parts_dw(f.M, f.K, f.F), sums, s);
+    const Plan by_dw = plan_dw(f.M, f.K, f.F);
+    e = cut_product<false>(dw, by_dw, sums, s);
     if (e) return e;
-    sums += parts_floats(parts_dw(f.M, f.K, f.F), F2, f.K);
+    sums += parts_floats(by_dw.parts, F2, f.K);
     const Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
                      nullptr, 0, nullptr};
-    return cut_product<true>(dx, parts_dx(f.M, f.K, f.F), sums, s);
+    return cut_product<true>(dx, plan_dx(f.M, f.K, f.F), sums, s);
 }
 
 }  // namespace
@@ -313,7 +378,7 @@ size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
     if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
     if (M == 0) return 0;
     return sizeof(float) *
-           ((size_t)M * dz_row(F) + parts_floats(parts_dx(M, K, F), M, K) + parts_floats(parts_dw(M, K, F), 2LL * F, K));
+           ((size_t)M * dz_row(F) + parts_floats(plan_dx(M, K, F).parts, M, K) + parts_floats(plan_dw(M, K, F).parts, 2LL * F, K));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);

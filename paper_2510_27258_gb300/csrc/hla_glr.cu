@@ -3,16 +3,23 @@
 //   s = sigmoid(r), i = sigmoid(g), a = e^(decay s), m = sqrt(1 - a^2), b = m i x,  h_t = a_t h_{t-1} + b_t
 // and backwards, with D_t = a_t (dy_t + D_{t+1}) the gradient of h_{t-1} and G_t = dy_t + D_{t+1} that of h_t,
 //   dx = G m i,  dg = G b (1 - i),  e = G (h_t - i x / m),  dr = e decay s (1 - s),  ddecay = sum e s
-// (the derivative of h_t by log a is a h_{t-1} - i x a^2 / m, and a h_{t-1} = h_t - m i x).  Where v = -decay s is at most 1,
-// q = 1 - e^-v is a polynomial, and a = 1 - q, m^2 = 1 - a^2 = q (2 - q): a slow decay, which a long memory multiplies up, is
-// off by no more than its rounding, and m keeps what 1 - a^2 would lose.  Slabs whose decays are all -1 or above take that alone.
+// (the derivative of h_t by log a is a h_{t-1} - i x a^2 / m, and a h_{t-1} = h_t - m i x).  Where v = -decay s is at
+// most 1, q = 1 - e^-v is a polynomial, and a = 1 - q, m^2 = 1 - a^2 = q (2 - q): a slow decay, which a long memory
+// multiplies up, is off by no more than its rounding, and m keeps what 1 - a^2 would lose.  Slabs whose decays are all
+// -1 or above take that alone.
 //
-// The recurrence composes: a run of tokens takes h to P h + l, so the sequence is walked in tiles whose warps
-// scan their own tokens side by side and join by P and l in shared memory; one pass over the data.  A block holds 64
-// channels (two a lane, 128 bytes of bf16 a row).  Where there are few channels a cluster of blocks walks
-// one sequence together: every block hands its tile's P and l to the others' shared memory, where their bytes
-// count at a barrier, and all form the same state in the same order, so equal inputs give equal bits.  The gradient walks the tiles backwards and takes h before each tile from the marks that the forward
-// leaves, so it reads every token once too.
+// The recurrence composes: a run of tokens takes h to P h + l, so the sequence is walked in tiles whose warps scan
+// their own tokens side by side and join by P and l in shared memory; one pass over the data.  A block holds 64
+// channels (two a lane, 128 bytes of bf16 a row).  Where there are few channels a cluster of blocks walks one sequence
+// together: every block hands its tiles' P and l to the others' shared memory, where their bytes count at a barrier, and
+// all form the same state in the same order, so equal inputs give equal bits.  The gradient walks the tiles backwards
+// and takes h before each tile from the marks that the forward leaves, so it reads every token once too.
+//
+// Least traffic: four (gradient: seven) values a token and channel.  bf16, B8 n2048 C2048: 52 us, 5.1 TB/s, 77 % of what
+// a copy reaches; the gradient 120 us, 4.0 TB/s, 60 %.  Both are bound by issue slots (60 % of them in use, 256 blocks
+// of 304 places, 16 warps an SM, which their 128 registers a thread allow), not by DRAM.  B1 n32768 C1024, clusters of
+// eight: 85 us, 47 %, of which the exchanges take 10 us and the joins of the tiles 12.  One token of 64 x 2048: 2.5 us on
+// the device.
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -26,7 +33,9 @@ using namespace sm103;
 constexpr int kThreads = 256;
 template <int kLanes>
 constexpr int kMostBlocks = kLanes == 32 ? 8 : 16;  // of a cluster
-constexpr int kSlots = 2;  // a round in use, the next in flight (3: 57.3 and 124.9 us on B8 n2048 C2048 bf16 instead of 56.3 and 124.5)
+// a round in use, the next in flight (with three, on B8 n2048 C2048 bf16: forward 57.3 us instead of 56.3, gradient 124.9
+// instead of 124.5)
+constexpr int kSlots = 2;
 constexpr int kSMs = 152;
 constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
 constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN, for states behind a wait that ran out
@@ -205,9 +214,8 @@ struct Tokens {
                 for (int u = 0; u < kRows; u += 32 / kChunks, p += 32 / kChunks * stride[i]) {
                     const int t = u + lane / kChunks, row = t % kTok * S::kOfWarp + t / kTok;  // (groups' rows by turns)
                     const int n = all || (unsigned)(first + t) < (unsigned)len ? bytes : 0;  // (0 reads nothing)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to + (i * kRows + row) * kRow)),
-                                 "l"(p), "r"(n)
-                                 : "memory");
+                    const uint32_t dst = smem_u32(to + (i * kRows + row) * kRow);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(p), "r"(n) : "memory");
                 }
             }
         } else {
@@ -222,7 +230,8 @@ struct Tokens {
                     const char *word = reinterpret_cast<const char *>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
                     // (a word that holds one element of the row is memory of the tensor)
                     const bool second = sizeof(T) == 4 || split(i, t0 + u);
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(word), "r"(live && at.on0 ? 4 : 0)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(word),
+                                 "r"(live && at.on0 ? 4 : 0)
                                  : "memory");
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4), "l"(word + 4),
                                  "r"(live && second && at.on1 ? 4 : 0)
@@ -250,7 +259,8 @@ struct Tokens {
                 reinterpret_cast<const T *>(ring + slot * kSlotBytes + (i * kRows + u * S::kOfWarp) * kRow) +
                 2 * (threadIdx.x & 31));
         } else {
-            const uint2 w = *reinterpret_cast<const uint2 *>(ring + slot * kSlotBytes + (i * kTok + u) * 256 + (threadIdx.x & 31) * 8);
+            const char *at = ring + slot * kSlotBytes + (i * kTok + u) * 256 + (threadIdx.x & 31) * 8;
+            const uint2 w = *reinterpret_cast<const uint2 *>(at);
             Raw<T, 2> r;
             if constexpr (sizeof(T) == 4) r.v = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
             else r.v = split(i, t0 + u) ? __byte_perm(w.x, w.y, 0x5432) : w.x;
@@ -367,9 +377,10 @@ struct Joint {
     // tiles (one a block) come before its second ones.  `state`: behind the round, in every warp.  The wait for the
     // others' runs has a limit, after which (`lost`) the states are NaN from there on, and so is what follows from them.
     template <int kTiles>
-    __device__ __forceinline__ void among(const Runs<Sh::kLanes> (&runs)[kTiles], Exchange<Sh::kLanes, kTiles> &x, int turn, int S,
-                                          unsigned rank, const Run (&mine)[kTiles], const Run (&before)[kTiles], bool &lost,
-                                          uint64_t &state, uint64_t (&got)[kTiles]) const {
+    __device__ __forceinline__ void among(const Runs<Sh::kLanes> (&runs)[kTiles], Exchange<Sh::kLanes, kTiles> &x,
+                                          int turn, int S, unsigned rank, const Run (&mine)[kTiles],
+                                          const Run (&before)[kTiles], bool &lost, uint64_t &state,
+                                          uint64_t (&got)[kTiles]) const {
         const int buf = turn & 1;
         Run ahead[kTiles];
         __syncthreads();
@@ -388,10 +399,11 @@ struct Joint {
             if (to == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
             __syncwarp();
             if (to < S)
-                asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                                 in_block(x.runs[buf][rank], to)),
-                             "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])), "r"(in_block(&x.bar[buf], to))
-                             : "memory");
+                asm volatile(
+                    "cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                        in_block(x.runs[buf][rank], to)),
+                    "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])), "r"(in_block(&x.bar[buf], to))
+                    : "memory");
         }
         if (!lost) lost = !wait(&x.bar[buf], (turn >> 1) & 1);
         uint64_t h = lost ? kLost : state;
@@ -424,7 +436,8 @@ template <typename T, int kLanes>
 using FwdShape = Shape<kLanes, sizeof(T) == 2 ? 8 : 4>;
 
 // kTiles: tiles of a block between two exchanges with its cluster's others (1: a block alone).  The states of all but the
-// last one wait in shared memory.
+// last one wait in shared memory.  Two: half as many exchanges (B1 n32768 C1024 with three tiles, which leave room for one
+// block an SM: 177 us instead of 85).
 template <typename T, int kLanes, bool kWide, int kTiles>
 struct FwdSmem {
     using In = Tokens<T, FwdShape<T, kLanes>, 3, kWide>;
@@ -489,8 +502,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
                         decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
                         const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
                         // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-                        const uint64_t add =
-                            mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), as_pair(in.get(slot, 0, t0, u)));
+                        const uint64_t x = as_pair(in.get(slot, 0, t0, u)),
+                                       add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), x);
                         h[u] = u ? fma2(a, h[u - 1], add) : add;
                         pr[u] = u ? mul2(a, pr[u - 1]) : a;
                         if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
@@ -600,7 +613,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     in.begin(t0, step, at);
     const uint64_t dec = at.get(f.decay, pairs);
     const Decay decay(dec);
-    uint64_t D = p.dstate_out ? at.get(p.dstate_out + (size_t)b * f.C, pairs) : 0;  // the gradient of the state behind the round
+    // the gradient of the state behind the round
+    uint64_t D = p.dstate_out ? at.get(p.dstate_out + (size_t)b * f.C, pairs) : 0;
     // a group's last token of the round
     T *dx = static_cast<T *>(p.dx) + (long long)(row0 + t0 + kTok - 1) * p.dx_stride,
       *dr = static_cast<T *>(p.dr) + (long long)(row0 + t0 + kTok - 1) * p.dr_stride,
@@ -631,7 +645,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
                 if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
                 s[u] = each(one_plus_exp(as_pair(rr)), rcp);
                 decay_of<near()>(decay, s[u], a[u], w);
-                const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm), i = each(one_plus_exp(as_pair(in.get(slot, 2, t0, u))), rcp);
+                const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm);
+                const uint64_t i = each(one_plus_exp(as_pair(in.get(slot, 2, t0, u))), rcp);
                 const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, t0, u)));
                 mi[u] = mul2(m, i);
                 rest[u] = fma2(i, minus, twice(1.f));
@@ -682,7 +697,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
             };
             if (t0 + kTok <= len && out_pairs) {
 #pragma unroll
-                for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride) put(u, true, true);
+                for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride)
+                    put(u, true, true);
             } else {
 #pragma unroll
                 for (int u = kTok - 1; u >= 0; --u, px -= p.dx_stride, pr -= p.dr_stride, pg -= p.dg_stride)
@@ -713,8 +729,9 @@ struct Spread {
     int lanes, slabs, S;
 };
 // As many blocks as two an SM, up to eight for a sequence; where that leaves half of the SMs' room, blocks take half the
-// channels; where few clusters are left even so, they are of sixteen blocks (the GPU holds 36 clusters of
-// eight, 14 of sixteen, at two blocks an SM).  A sequence is not given more blocks than it has tiles.
+// channels; where few clusters are left even so, they are of sixteen blocks (the GPU holds 36 clusters of eight, 14 of
+// sixteen, at two blocks an SM; more would be a second wave: B1 n32768 C1024 in clusters of eight of blocks that fill an
+// SM, of which it holds 15, 186 us instead of 85).  A sequence is not given more blocks than it has tiles.
 Spread spread(int B, int n, int C, int tok) {
     auto units = [&](int lanes) { return (long long)B * ((C + 2 * lanes - 1) / (2 * lanes)); };
     const int span = 8 * tok;
@@ -748,8 +765,8 @@ template <typename T, int kLanes, bool kWide>
 cudaError_t forward_as(const Glr &p, const Spread &r, cudaStream_t s) {
     const bool pairs = pairs_ok<T>(p.y, p.y_stride, p.C);
     const long long units = (long long)p.B * r.slabs;
-    return r.S == 1 ? launch_clusters(glr_forward_kernel<T, kLanes, kWide, 1>, units, 1, FwdSmem<T, kLanes, kWide, 1>::kBytes, s, p,
-                                      r.slabs, 1, pairs)
+    return r.S == 1 ? launch_clusters(glr_forward_kernel<T, kLanes, kWide, 1>, units, 1,
+                                      FwdSmem<T, kLanes, kWide, 1>::kBytes, s, p, r.slabs, 1, pairs)
                     : launch_clusters(glr_forward_kernel<T, kLanes, kWide, 2>, units, r.S,
                                       FwdSmem<T, kLanes, kWide, 2>::kBytes, s, p, r.slabs, r.S, pairs);
 }
