@@ -14,6 +14,8 @@
 //
 // Bound by the CUDA cores' 80 TFLOP/s, from which shared memory's bandwidth and few warps keep it: gradient of 333 x 260 x
 // 1031 72 us (one group of threads 85, four 106), where 1.3 blocks an SM are all there is; large products 35 TFLOP/s.
+#include <type_traits>
+
 #include "hla_ffn.h"
 #include "hla_vec.cuh"
 
@@ -254,6 +256,192 @@ __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel
     }
 }
 
+// ------------------------------------------------------------------------------------------------
+// few rows: up to 32 tokens, whose tiles of 64 would be half empty while the weights' bytes are what counts.  The sum is
+// cut over a block's eight warps and over the blocks of a cluster, whose parts meet in shared memory and are added in
+// order; each block finishes some of the tokens.
+// ------------------------------------------------------------------------------------------------
+
+constexpr int kFewMost = 32, kWarps = kThreads / 32, kFewDepth = 4 * kWarps, kFewPitch = kFewDepth + 4, kFewStages = 6;
+
+__device__ __forceinline__ unsigned cluster_rank() {
+    unsigned r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// one value of every block's, added in the blocks' order
+__device__ __forceinline__ float of_blocks(const float *mine, int S) {
+    if (S == 1) return *mine;
+    float sum = 0.f;
+#pragma unroll 2
+    for (int b = 0; b < S; ++b) {
+        uint32_t at;
+        float v;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;"
+            : "=r"(at)
+            : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(mine))), "r"(b));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+        sum += v;
+    }
+    return sum;
+}
+// the warps' values ([warp][kValues] in shared memory), added in the warps' order in place of the first's; the cluster's
+// blocks have done so when this returns
+template <int kValues>
+__device__ __forceinline__ void add_warps(float *values, int S) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kValues; i += kThreads) {
+        float sum = values[i];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) sum += values[w * kValues + i];
+        values[i] = sum;
+    }
+    __syncthreads();
+    if (S > 1) cluster_meet();
+}
+
+// kOut and kGrad.  A lane has one feature's gate and up row for all tokens, a warp four of a panel's 32 indices.
+template <int kTok>
+constexpr int kFewFloats = (64 + kTok) * kFewPitch;  // of a panel
+template <int kTok, Mode kMode>
+__global__ void __launch_bounds__(kThreads) ffn_few_kernel(Product p, int S) {
+    extern __shared__ __align__(16) float ring[];  // [stage][32 gate rows, 32 up rows, tokens]
+    let_next_begin();
+    after_previous();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // no device-side waits here: never an error
+    const int rank = S > 1 ? (int)cluster_rank() : 0, f0 = blockIdx.x / S * 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int k_lo = (int)min((long long)p.K, (long long)rank * p.per), k_hi = (int)min((long long)p.K, (long long)k_lo + p.per);
+    auto send = [&](int stage, int k0) {
+#pragma unroll
+        for (int c = threadIdx.x; c < (64 + kTok) * 8; c += kThreads) {
+            const int line = c / 8, four = c % 8 * 4;
+            const bool weight = line < 64;
+            const Mat &m = weight ? p.b : p.a;
+            const int row = weight ? f0 + line % 32 : line - 64, left = row < (weight ? p.N : p.M) ? k_hi - k0 - four : 0;
+            const float *from = m.p + ((long long)row + (weight && line >= 32 ? p.N : 0)) * m.step + k0 + four;
+            const uint32_t dst =
+                static_cast<uint32_t>(__cvta_generic_to_shared(ring + stage * kFewFloats<kTok> + line * kFewPitch + four));
+            if (m.wide) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from),
+                             "r"(min(max(left, 0), 4) * 4)
+                             : "memory");
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + 4 * j), "l"(from + j),
+                                 "r"(j < left ? 4 : 0)
+                                 : "memory");
+            }
+        }
+        ring_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kFewStages - 1; ++i) send(i, k_lo + i * kFewDepth);
+    float acc[2][kTok] = {};
+    int stage = 0;
+    for (int k0 = k_lo; k0 < k_hi; k0 += kFewDepth, stage = stage + 1 < kFewStages ? stage + 1 : 0) {
+        ring_wait<kFewStages - 2>();
+        __syncthreads();  // (and the stage of the last step has been read)
+        send(stage ? stage - 1 : kFewStages - 1, k0 + (kFewStages - 1) * kFewDepth);
+        const float *at = ring + stage * kFewFloats<kTok> + warp * 4;
+        float g[4], u[4];
+        VecIo<float, 4>::load(at + lane * kFewPitch, g);
+        VecIo<float, 4>::load(at + (32 + lane) * kFewPitch, u);
+#pragma unroll
+        for (int t = 0; t < kTok; ++t) {
+            float x[4];
+            VecIo<float, 4>::load(at + (64 + t) * kFewPitch, x);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                acc[0][t] = fmaf(g[q], x[q], acc[0][t]);
+                acc[1][t] = fmaf(u[q], x[q], acc[1][t]);
+            }
+        }
+    }
+    ring_wait<0>();
+    __syncthreads();
+    constexpr int kValues = 2 * kTok * 32;
+#pragma unroll
+    for (int t = 0; t < 2 * kTok; ++t) ring[warp * kValues + t * 32 + lane] = acc[t / kTok][t % kTok];
+    add_warps<kValues>(ring, S);
+    const int each = (p.M + S - 1) / S, lo = rank * each, hi = min(lo + each, p.M);
+    for (int t = lo + warp; t < hi; t += kWarps) {
+        const int n = f0 + lane;
+        const float g = of_blocks(ring + t * 32 + lane, S), up = of_blocks(ring + (kTok + t) * 32 + lane, S);
+        if (n >= p.N) continue;
+        float slope;
+        const float a = act_of(p.act, g, slope);
+        float *to = p.out + t * p.out_row + n;
+        if (kMode == kOut) {
+            *to = a * up;
+        } else {
+            const float d = p.dout[t * p.dout_row + n];
+            to[0] = d * up * slope;
+            to[p.N] = d * a;
+        }
+    }
+    if (S > 1) cluster_meet();  // the others have read this block's sums
+}
+
+// dx.  A lane has two of 64 columns for all tokens, a warp every eighth row of the weights.
+constexpr int kBackRows = 128, kBackCols = 64;
+template <int kTok>
+constexpr int kBackFloats = kWarps * kTok * kBackCols;  // the warps' sums (and room for a panel of dZ)
+template <int kTok>
+__global__ void __launch_bounds__(kThreads) ffn_few_back_kernel(Product p, int S) {
+    extern __shared__ __align__(16) float panel[];  // [row][token]
+    constexpr int kPitch = kTok + 4, kOfWarp = kBackRows / kWarps;
+    static_assert(kBackRows * kPitch <= kBackFloats<kTok>, "a panel's room");
+    let_next_begin();
+    after_previous();
+    const int rank = S > 1 ? (int)cluster_rank() : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c0 = blockIdx.x / S * kBackCols + lane;
+    const int r_lo = (int)min((long long)p.K, (long long)rank * p.per), r_hi = (int)min((long long)p.K, (long long)r_lo + p.per);
+    float acc[2][kTok] = {};
+    for (int r0 = r_lo; r0 < r_hi; r0 += kBackRows) {
+        float w[kOfWarp][2];
+#pragma unroll
+        for (int i = 0; i < kOfWarp; ++i) {
+            const int r = r0 + warp + kWarps * i;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) w[i][j] = r < r_hi && c0 + 32 * j < p.N ? p.b.p[r * p.b.step + c0 + 32 * j] : 0.f;
+        }
+        __syncthreads();  // the last panel has been read
+        const int row = threadIdx.x % kBackRows;
+#pragma unroll
+        for (int t = threadIdx.x / kBackRows; t < kTok; t += kThreads / kBackRows)
+            panel[row * kPitch + t] = t < p.M && r0 + row < r_hi ? p.a.p[t * p.a.step + r0 + row] : 0.f;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kOfWarp; ++i)
+#pragma unroll
+            for (int t = 0; t < kTok; t += 4) {
+                float d[4];
+                VecIo<float, 4>::load(panel + (warp + kWarps * i) * kPitch + t, d);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[j][t + q] = fmaf(w[i][j], d[q], acc[j][t + q]);
+            }
+    }
+    __syncthreads();
+    constexpr int kValues = kTok * kBackCols;
+#pragma unroll
+    for (int t = 0; t < 2 * kTok; ++t) panel[warp * kValues + t / 2 * kBackCols + t % 2 * 32 + lane] = acc[t % 2][t / 2];
+    add_warps<kValues>(panel, S);
+    const int each = (p.M + S - 1) / S, lo = rank * each, hi = min(lo + each, p.M);
+    for (int i = threadIdx.x; i < (hi - lo) * kBackCols; i += kThreads) {
+        const int t = lo + i / kBackCols, c = i % kBackCols, n = blockIdx.x / S * kBackCols + c;
+        const float sum = of_blocks(panel + t * kBackCols + c, S);
+        if (n < p.N) p.out[t * p.out_row + n] = sum;
+    }
+    if (S > 1) cluster_meet();  // the others have read this block's sums
+}
+
 // out = the sum of `parts` runs of M x N
 __global__ void __launch_bounds__(kThreads) ffn_parts_kernel(const float *from, int parts, int M, int N, float *out,
                                                             long long out_row) {
@@ -319,6 +507,36 @@ cudaError_t product(Product p, const Plan &by, cudaStream_t s) {
                       : as(ffn_product_kernel<128, kA, kB, kMode>, Panel<128, kA>::kFloats + Panel<128, kB>::kFloats);
 }
 
+// Few rows: blocks of a cluster as many as fill three blocks an SM, each with `least` indices of the sum or more
+template <typename K>
+cudaError_t few(K kernel, Product p, long long tiles, int least, int step, int floats, cudaStream_t s) {
+    int S = 1;
+    while (S < 8 && tiles * S * 2 <= 3 * kSMs && p.K >= S * 2 * least) S *= 2;
+    p.per = ((p.K + S - 1) / S + step - 1) / step * step;
+    const int smem = floats * (int)sizeof(float);
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return e ? e : launch_cluster_after(kernel, (unsigned)(tiles * S), kThreads, S, smem, s, p, S);
+}
+template <Mode kMode>
+cudaError_t few_forward(const Product &p, cudaStream_t s) {
+    auto as = [&](auto Tok) {
+        constexpr int kTok = Tok(), kSums = kWarps * 2 * kTok * 32, kRing = kFewStages * kFewFloats<kTok>;
+        return few(ffn_few_kernel<kTok, kMode>, p, (p.N + 31) / 32, 4 * kFewDepth, kFewDepth, kRing > kSums ? kRing : kSums, s);
+    };
+    return p.M <= 8    ? as(std::integral_constant<int, 8>())
+           : p.M <= 16 ? as(std::integral_constant<int, 16>())
+                       : as(std::integral_constant<int, 32>());
+}
+cudaError_t few_back(const Product &p, cudaStream_t s) {
+    auto as = [&](auto Tok) {
+        constexpr int kTok = Tok();
+        return few(ffn_few_back_kernel<kTok>, p, (p.N + kBackCols - 1) / kBackCols, kBackRows, kBackRows, kBackFloats<kTok>, s);
+    };
+    return p.M <= 8    ? as(std::integral_constant<int, 8>())
+           : p.M <= 16 ? as(std::integral_constant<int, 16>())
+                       : as(std::integral_constant<int, 32>());
+}
+
 const float *floats(const void *p) { return static_cast<const float *>(p); }
 
 size_t parts_floats(int parts, long long M, long long N) { return parts > 1 ? (size_t)parts * M * N : 0; }
@@ -345,7 +563,7 @@ long long dz_row(int F) { return (2LL * F + 3) / 4 * 4; }
 cudaError_t forward_f32(const Ffn &p, cudaStream_t s) {
     const Product q{mat(floats(p.x), p.x_stride), mat(floats(p.w), p.K), p.M, p.F, p.K, p.act, p.K, 0,
                     static_cast<float *>(p.out), p.out_stride, nullptr, 0, reinterpret_cast<WsHeader *>(p.ws)};
-    return product<true, true, kOut>(q, plan(p.M, p.F, p.K, true, 1), s);
+    return p.M <= kFewMost ? few_forward<kOut>(q, s) : product<true, true, kOut>(q, plan(p.M, p.F, p.K, true, 1), s);
 }
 
 cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
@@ -355,7 +573,7 @@ cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     const long long row = dz_row(f.F);
     const Product q{mat(floats(f.x), f.x_stride), mat(floats(f.w), f.K), f.M, f.F, f.K, f.act, f.K, 0, dz, row,
                     floats(p.dout), p.dout_stride, reinterpret_cast<WsHeader *>(f.ws)};
-    cudaError_t e = product<true, true, kGrad>(q, plan(f.M, f.F, f.K, true, 1), s);
+    cudaError_t e = f.M <= kFewMost ? few_forward<kGrad>(q, s) : product<true, true, kGrad>(q, plan(f.M, f.F, f.K, true, 1), s);
     if (e) return e;
     float *sums = dz + (size_t)f.M * row;
     const Product dw{mat(dz, row), mat(floats(f.x), f.x_stride), F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
@@ -366,7 +584,7 @@ cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     sums += parts_floats(by_dw.parts, F2, f.K);
     const Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
                      nullptr, 0, nullptr};
-    return cut_product<true>(dx, plan_dx(f.M, f.K, f.F), sums, s);
+    return f.M <= kFewMost ? few_back(dx, s) : cut_product<true>(dx, plan_dx(f.M, f.K, f.F), sums, s);
 }
 
 }  // namespace
@@ -378,7 +596,7 @@ size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
     if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
     if (M == 0) return 0;
     return sizeof(float) *
-           ((size_t)M * dz_row(F) + parts_floats(plan_dx(M, K, F).parts, M, K) + parts_floats(plan_dw(M, K, F).parts, 2LL * F, K));
+           ((size_t)M * dz_row(F) + parts_floats(M <= kFewMost ? 1 : plan_dx(M, K, F).parts, M, K) + parts_floats(plan_dw(M, K, F).parts, 2LL * F, K));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);

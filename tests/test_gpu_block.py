@@ -335,7 +335,8 @@ def test_block_norm_rows_of_zeros(hla):
 FFN = [(1, 8, 8, R.SILU), (3, 1, 1, R.SILU), (16, 264, 520, R.SIGMOID), (129, 130, 67, R.SILU), (333, 260, 103, R.LINEAR),
        (300, 512, 1032, R.SILU), (1, 2056, 384, R.SILU), (64, 33, 2050, R.SIGMOID), (520, 64, 328, R.SILU),
        (17, 1000, 77, R.SILU), (256, 320, 136, R.SILU), (257, 72, 200, R.SILU), (100, 1600, 72, R.SIGMOID),
-       (5, 2048, 1288, R.SILU)]
+       (5, 2048, 1288, R.SILU), (9, 700, 1100, R.SILU), (32, 1030, 600, R.SIGMOID), (31, 64, 50, R.SILU),
+       (8, 4100, 70, R.LINEAR), (1030, 520, 2600, R.SILU)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
