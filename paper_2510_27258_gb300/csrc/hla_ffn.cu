@@ -3,17 +3,18 @@
 //   Z = x [Wg; Wu]^T (two products of one tile),  out = act(Zg) Zu
 //   dZg = dout Zu act'(Zg),  dZu = dout act(Zg),  dx = [dZg dZu] [Wg; Wu],  d[Wg; Wu] = [dZg dZu]^T x
 //
-// One tiled product serves all four: a block of 256 threads forms 128 x 128 outputs (64 x 64 where those would leave
-// SMs without a tile: there two groups of threads share each panel's indices, so that SMs have twice the warps), a thread
-// 8 x 8 (4 x 4) of them, from panels of 16 in a ring of shared memory, all but the one in use in flight.  A panel lies
-// as its matrix does: where the sum's index is the contiguous one a thread reads four (two) of its indices of a row at a
-// time, else four rows of an index, so that either way a wide access feeds many products.  The forward's tile is half
+// One tiled product serves all four: a block of 256 threads forms 128 x 128 outputs (or 64 x 64, with two groups of
+// threads that share each panel's indices, so that SMs have twice the warps), a thread 8 x 8 (4 x 4) of them, from panels
+// of 32 (16) in a ring of shared memory, all but the one in use in flight.  A panel lies as its matrix does: where the
+// sum's index is the contiguous one a thread reads two (four) of its indices of a row at a time, else four rows of an
+// index, so that either way a wide access feeds many products.  The forward's tile is half
 // gate and half up columns of the same features, so that the activation and product happen in registers.  The gradient
-// keeps [dZg dZu] in the workspace; its last two products, whose sums are over 2 F and over tokens and whose tiles may
-// be few, are cut along the sum, and the parts are added in their order.
+// keeps [dZg dZu] in the workspace; its last two products, whose sums are over 2 F and over tokens, are cut along the sum
+// where that fills the SMs better, and the parts are added in their order.  Few tokens have kernels of their own, below.
 //
-// Bound by the CUDA cores' 80 TFLOP/s, from which shared memory's bandwidth and few warps keep it: gradient of 333 x 260 x
-// 1031 72 us (one group of threads 85, four 106), where 1.3 blocks an SM are all there is; large products 35 TFLOP/s.
+// Bound by the CUDA cores (80 TFLOP/s at the highest clock): 4096 x 2048 x 1408 44.8 TFLOP/s, its gradient 49; tiles of
+// 128 with panels of 32 and products in pairs instead of 16 and single ones: 43.1 and 42.3.  Gradient of 333 x 260 x 1031
+// 72 us (one group of threads a small tile 85, four 106), where 1.3 blocks an SM are all there is.
 #include <type_traits>
 
 #include "hla_ffn.h"
@@ -259,7 +260,9 @@ __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel
 // ------------------------------------------------------------------------------------------------
 // few rows: up to 32 tokens, whose tiles of 64 would be half empty while the weights' bytes are what counts.  The sum is
 // cut over a block's eight warps and over the blocks of a cluster, whose parts meet in shared memory and are added in
-// order; each block finishes some of the tokens.
+// order; each block finishes some of the tokens.  2048 x 5632: one token 31 us, 16 46, 32 74 (by tiles 140; 33 tokens
+// 139), gradient of 16 160 instead of 293; the weights' bytes take 14 us, the rest goes with the tokens.  Not kept: panels
+// of 64 indices (45 us), four or eight rows by eight tokens a lane (46, gradient 202), two blocks an SM (53).
 // ------------------------------------------------------------------------------------------------
 
 constexpr int kFewMost = 32, kWarps = kThreads / 32, kFewDepth = 4 * kWarps, kFewPitch = kFewDepth + 4, kFewStages = 6;
