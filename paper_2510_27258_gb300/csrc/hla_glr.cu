@@ -37,7 +37,7 @@ constexpr int kMostBlocks = kLanes == 32 ? 8 : 16;  // of a cluster
 // instead of 124.5)
 constexpr int kSlots = 2;
 constexpr int kSMs = 152;
-constexpr long long kWaitCycles = 4000000000ll;  // about 2 s
+constexpr long long kWaitCycles = 4000000000ll, kLandCycles = 200000000ll;  // about 2 and 0.1 s
 constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN, for states behind a wait that ran out
 constexpr float kLog2e = 1.44269504f;
 constexpr float kTiny = 1e-37f;               // beside 1 - a^2: keeps 1/m finite where a is 1
@@ -328,6 +328,15 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
     return true;
 }
 
+// At the end: what was sent to a block has arrived before its shared memory goes.  Where a wait ran out there is no sign
+// of a copy but its time: one that was sent lands within microseconds.
+__device__ __forceinline__ void close_exchange(bool lost) {
+    cluster_meet();
+    const long long t0 = clock64();
+    while (lost && clock64() - t0 < kLandCycles) {
+    }
+}
+
 // A warp's groups as one run: returns it, and in `before` what comes before the lane's group within the warp
 template <typename Sh, int kOrder>
 __device__ __forceinline__ Run of_warp(const Run &mine, Run &before) {
@@ -393,7 +402,7 @@ struct Joint {
             }
             if (last() && speaks()) x.mine[buf][i][lane] = {mul2(mine[i].p, ahead[i].p), after(mine[i], ahead[i].l)};
         }
-        if (last()) {
+        if (last() && !lost) {  // (else the others' waits run out, too)
             fence_async_smem();
             const int to = threadIdx.x & 31;
             if (to == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
@@ -550,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     // (a block alone: the last warp has it)
     if (p.state_out && rank == 0 && joint.last() && joint.speaks()) at.put(p.state_out + (size_t)b * p.C, state, pairs);
     ring_wait<0>();
-    if (kTiles > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
+    if (kTiles > 1) close_exchange(lost);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -721,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
         at.put(p.partial + ((size_t)b * S + rank) * f.C, dsum, pairs);
     }
     ring_wait<0>();
-    if (S > 1) cluster_meet();  // what was sent to a block has arrived before its shared memory goes
+    if (S > 1) close_exchange(lost);
 }
 
 // How a call is spread: lanes for a token's channels, and blocks of one sequence
