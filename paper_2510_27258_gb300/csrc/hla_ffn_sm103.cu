@@ -18,7 +18,7 @@
 // parts are added in their order by another kernel.
 //
 // Bound by the tensor cores.  8192 x 2048 x 5632: forward 204 us in a capture of its own, 1.85 PFLOP/s, 97 % of what a
-// library product reaches in a burst (226 us one after another, at the clocks that leaves); gradient 717 us, of
+// library product reaches in a burst (224 us one after another, at the clocks that leaves); gradient 700 us, of
 // which kBack 406 (97 %) and kGrad about 230, whose read-out of a tile (dout, two planes of dZ) takes as long as the
 // products of the next.  Up to 128 tokens, where the weights' bytes count, ffn_few_kernel: 16 tokens 8.8 us on the device,
 // 5.3 TB/s, against 18 by the tiles.
