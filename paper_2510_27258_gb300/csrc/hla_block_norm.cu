@@ -314,10 +314,10 @@ constexpr int slots() {
     constexpr int bytes = 5 * block_of(kMax) * kPer * (int)sizeof(T);
     if (sizeof(Raw<T, kV>) < 4) return 0;
     if (3 * bytes <= 64 * 1024 || (kMax == 512 && 3 * bytes <= 160 * 1024)) return 3;
-    return 2 * bytes <= 200 * 1024 ? 2 : 0;
+    return 2 * bytes <= 160 * 1024 ? 2 : 0;
 }
 template <typename T>
-size_t ring_bytes(int threads, int slots) { return (size_t)slots * 5 * threads * kPer * sizeof(T); }
+__host__ __device__ constexpr size_t ring_bytes(int threads, int slots) { return (size_t)slots * 5 * threads * kPer * sizeof(T); }
 
 // a weight's eight columns, or ones
 template <typename T, int kV>
@@ -558,19 +558,40 @@ block_norm_backward_kernel(BlockNormBwd q) {
         Pairs w_post;
         weight<T, kV>(p.scale, t, threads, C, scale);
         weight<T, kV>(p.w_post, t, threads, C, w_post);
-        weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+        if (kMax < 1024) weight<T, kV>(p.w_pre, t, threads, C, w_pre);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
     }
     Drop<kV> drop;
     drop.open(p, t, threads);
     Pairs qu = {}, dw_pre = {};  // sums over this thread's rows
+    // With 64 registers a thread the sums wait in shared memory and w_pre is read where it is used (gradient of C 8190
+    // 285 us instead of 354, of C 6144 248 instead of 278, of C 8192 in fp32 148 instead of 170)
+    constexpr bool kApart = kMax == 1024;
     constexpr int kSlots = slots<T, kV, kMax>();
     extern __shared__ __align__(16) char ring[];
     Rows<T, kV, 5, kSlots> in{{static_cast<const T *>(p.x), static_cast<const T *>(p.y), static_cast<const T *>(p.gate),
                                static_cast<const T *>(q.dx_out), static_cast<const T *>(q.dh)},
                               {p.x_stride, p.y_stride, p.gate_stride, q.dx_out_stride, q.dh_stride},
                               nullptr, t, threads, C, p.rows, step};
+    // (kApart) this thread's sums in shared memory
+    ulonglong2 *apart = reinterpret_cast<ulonglong2 *>(ring + ring_bytes<T>(blockDim.x, kSlots)) + threadIdx.x;
+    auto keep_sums = [&](int k, const Pairs &v) {
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) apart[(k * 2 + i / 2) * blockDim.x] = make_ulonglong2(v[i], v[i + 1]);
+    };
+    auto get_sums = [&](int k, Pairs &v) {
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) {
+            const ulonglong2 w = apart[(k * 2 + i / 2) * blockDim.x];
+            v[i] = w.x;
+            v[i + 1] = w.y;
+        }
+    };
+    if (kApart) {
+        keep_sums(0, qu);
+        keep_sums(1, dw_pre);
+    }
     long long row = (long long)blockIdx.x * kAtOnce + (kBlock ? 0 : threadIdx.x / kMax);
     // a warp's rows together: those behind the last one take part in sums and exchanges alone
     const int in_warp = kBlock ? 0 : (threadIdx.x & 31) / kMax;
@@ -604,9 +625,10 @@ block_norm_backward_kernel(BlockNormBwd q) {
             keep.apply(f[1]);
             if (!p.post) keep.apply(y);  // (with the norm, u of dropped values is part of dy)
         }
-        Pairs fs;  // what multiplies u in x', and t in dn
+        Pairs fs;  // what multiplies u in x', and t in dn (kApart: made where it is used)
+        if (!kApart)
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) fs[i] = mul2(f[0][i], scale[i]);
+            for (int i = 0; i < kPairs; ++i) fs[i] = mul2(f[0][i], scale[i]);
         float r1 = 1.f;
         if (p.post) {
             read<kMax>(s1, red, turn);
@@ -616,9 +638,11 @@ block_norm_backward_kernel(BlockNormBwd q) {
         for (int i = 0; i < kPairs; ++i) y[i] = mul2(y[i], twice(r1));  // u
         if (p.pre) {
             uint64_t sum = 0, dot = 0;
+            if (kApart) weight<T, kV>(p.w_pre, t, threads, C, w_pre);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
-                x[i] = fma2(y[i], fs[i], mul2(x[i], twice(p.alpha)));  // x'
+                const uint64_t ax = mul2(x[i], twice(p.alpha));
+                x[i] = kApart ? fma2(mul2(y[i], f[0][i]), scale[i], ax) : fma2(y[i], fs[i], ax);  // x'
                 sum = fma2(x[i], x[i], sum);
                 dot = fma2(mul2(h[i], w_pre[i]), x[i], dot);
             }
@@ -629,25 +653,32 @@ block_norm_backward_kernel(BlockNormBwd q) {
             const float r2 = rsqrtf(s2.v[0] * inv + p.eps), m2 = s2.v[1] * r2 * inv;
             // t = dx' + r2 (dh w_pre - x' r2 m2)
             const uint64_t by = twice(-r2 * r2 * m2);
+            if (kApart) {
+                get_sums(1, dw_pre);
+                weight<T, kV>(p.w_pre, t, threads, C, w_pre);
+            }
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
                 const uint64_t hr = mul2(h[i], twice(r2));
                 d[i] = fma2(x[i], by, fma2(hr, w_pre[i], d[i]));
                 if (live) dw_pre[i] = fma2(hr, x[i], dw_pre[i]);
             }
+            if (kApart) keep_sums(1, dw_pre);
         }
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) x[i] = mul2(d[i], twice(p.alpha));
         Cols<T, kV>::put(static_cast<T *>(q.dx) + row * q.dx_stride, t, threads, live ? C : 0, x);
         uint64_t dot = 0;
+        if (kApart) get_sums(0, qu);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
             const uint64_t du = mul2(d[i], y[i]);
             if (live) qu[i] = fma2(du, f[0][i], qu[i]);
-            x[i] = mul2(d[i], fs[i]);  // q scale w_post
+            x[i] = kApart ? mul2(mul2(d[i], f[0][i]), scale[i]) : mul2(d[i], fs[i]);  // q scale w_post
             dot = fma2(x[i], y[i], dot);
             f[1][i] = mul2(mul2(du, f[1][i]), scale[i]);  // dgate
         }
+        if (kApart) keep_sums(0, qu);
         Sum<1> s3;
         add_up(dot, s3.v[0]);
         if (p.post) tell<kMax>(s3, red, turn);
@@ -661,6 +692,10 @@ block_norm_backward_kernel(BlockNormBwd q) {
         Cols<T, kV>::put(static_cast<T *>(q.dy) + row * q.dy_stride, t, threads, live ? C : 0, x);
     }
     if (kSlots > 1) ring_wait<0>();
+    if (kApart) {
+        get_sums(0, qu);
+        get_sums(1, dw_pre);
+    }
     // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
     float sum[2][kPer];
 #pragma unroll
@@ -847,7 +882,7 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
     const Plan g = plan(p.rows, p.C);
     auto as = [&](auto V) -> cudaError_t {
         return by_threads(p.C, g.threads, [&](auto M) {
-            const size_t smem = ring_bytes<T>(g.threads, slots<T, V(), M()>());
+            const size_t smem = ring_bytes<T>(g.threads, slots<T, V(), M()>()) + (M() == 1024 ? 64 * g.threads : 0);
             return launch_ring(block_norm_backward_kernel<T, V(), M()>, g, smem, s, q);
         });
     };
