@@ -260,12 +260,14 @@ __global__ void __launch_bounds__(kThreads *groups_of(kTile)) ffn_product_kernel
 // ------------------------------------------------------------------------------------------------
 // few rows: up to 32 tokens, whose tiles of 64 would be half empty while the weights' bytes are what counts.  The sum is
 // cut over a block's eight warps and over the blocks of a cluster, whose parts meet in shared memory and are added in
-// order; each block finishes some of the tokens.  2048 x 5632: one token 31 us, 16 46, 32 74 (by tiles 140; 33 tokens
-// 139), gradient of 16 160 instead of 293; the weights' bytes take 14 us, the rest goes with the tokens.  Not kept: panels
-// of 64 indices (45 us), four or eight rows by eight tokens a lane (46, gradient 202), two blocks an SM (53).
+// order; each block finishes some of the tokens.  2048 x 5632: one token 29 us, 16 40, 32 65 (by tiles 140; 33 tokens
+// 139), gradient of one 80, of 16 125 instead of 293, of 32 193; the weights' bytes take 14 us (42 in the gradient), the
+// rest goes with the tokens (issue slots 63 % in use).  Not kept: panels of 64 indices (no change), four or eight rows
+// by eight tokens a lane (gradient of 16 202), two blocks an SM (forward of 16 53).
 // ------------------------------------------------------------------------------------------------
 
-constexpr int kFewMost = 32, kWarps = kThreads / 32, kFewDepth = 4 * kWarps, kFewPitch = kFewDepth + 4, kFewStages = 6;
+constexpr int kFewMost = 32, kWarps = kThreads / 32, kFewDepth = 4 * kWarps, kFewPitch = kFewDepth + 4, kFewStages = 4;
+constexpr int few_blocks(int tok) { return tok == 32 ? 2 : 3; }  // of an SM, at 128 or 80 registers a thread
 
 __device__ __forceinline__ unsigned cluster_rank() {
     unsigned r;
@@ -310,7 +312,7 @@ __device__ __forceinline__ void add_warps(float *values, int S) {
 template <int kTok>
 constexpr int kFewFloats = (64 + kTok) * kFewPitch;  // of a panel
 template <int kTok, Mode kMode>
-__global__ void __launch_bounds__(kThreads) ffn_few_kernel(Product p, int S) {
+__global__ void __launch_bounds__(kThreads, few_blocks(kTok)) ffn_few_kernel(Product p, int S) {
     extern __shared__ __align__(16) float ring[];  // [stage][32 gate rows, 32 up rows, tokens]
     let_next_begin();
     after_previous();
@@ -391,13 +393,14 @@ __global__ void __launch_bounds__(kThreads) ffn_few_kernel(Product p, int S) {
 }
 
 // dx.  A lane has two of 64 columns for all tokens, a warp every eighth row of the weights.
-constexpr int kBackRows = 128, kBackCols = 64;
+constexpr int kBackCols = 64;
+constexpr int back_rows(int tok) { return tok == 32 ? 64 : 128; }  // of a panel
 template <int kTok>
 constexpr int kBackFloats = kWarps * kTok * kBackCols;  // the warps' sums (and room for a panel of dZ)
 template <int kTok>
-__global__ void __launch_bounds__(kThreads) ffn_few_back_kernel(Product p, int S) {
+__global__ void __launch_bounds__(kThreads, 2) ffn_few_back_kernel(Product p, int S) {
     extern __shared__ __align__(16) float panel[];  // [row][token]
-    constexpr int kPitch = kTok + 4, kOfWarp = kBackRows / kWarps;
+    constexpr int kBackRows = back_rows(kTok), kPitch = kTok + 4, kOfWarp = kBackRows / kWarps;
     static_assert(kBackRows * kPitch <= kBackFloats<kTok>, "a panel's room");
     let_next_begin();
     after_previous();
@@ -405,19 +408,29 @@ __global__ void __launch_bounds__(kThreads) ffn_few_back_kernel(Product p, int S
     const int c0 = blockIdx.x / S * kBackCols + lane;
     const int r_lo = (int)min((long long)p.K, (long long)rank * p.per), r_hi = (int)min((long long)p.K, (long long)r_lo + p.per);
     float acc[2][kTok] = {};
-    for (int r0 = r_lo; r0 < r_hi; r0 += kBackRows) {
-        float w[kOfWarp][2];
+    float next[kOfWarp][2];  // of the weights' next panel
+    auto fetch = [&](int r0) {
 #pragma unroll
         for (int i = 0; i < kOfWarp; ++i) {
             const int r = r0 + warp + kWarps * i;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) w[i][j] = r < r_hi && c0 + 32 * j < p.N ? p.b.p[r * p.b.step + c0 + 32 * j] : 0.f;
+            for (int j = 0; j < 2; ++j)
+                next[i][j] = r < r_hi && c0 + 32 * j < p.N ? p.b.p[r * p.b.step + c0 + 32 * j] : 0.f;
         }
+    };
+    fetch(r_lo);
+    for (int r0 = r_lo; r0 < r_hi; r0 += kBackRows) {
         __syncthreads();  // the last panel has been read
         const int row = threadIdx.x % kBackRows;
 #pragma unroll
         for (int t = threadIdx.x / kBackRows; t < kTok; t += kThreads / kBackRows)
             panel[row * kPitch + t] = t < p.M && r0 + row < r_hi ? p.a.p[t * p.a.step + r0 + row] : 0.f;
+        float w[kOfWarp][2];
+#pragma unroll
+        for (int i = 0; i < kOfWarp; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) w[i][j] = next[i][j];
+        fetch(r0 + kBackRows);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kOfWarp; ++i)
@@ -443,6 +456,47 @@ __global__ void __launch_bounds__(kThreads) ffn_few_back_kernel(Product p, int S
         if (n < p.N) p.out[t * p.out_row + n] = sum;
     }
     if (S > 1) cluster_meet();  // the others have read this block's sums
+}
+
+// dw of up to 16 tokens (above, a tile's panel is full enough: 32 of them 196 us instead of 212 in all).  A lane has four of
+// 128 columns of x for all tokens, a warp every eighth of a panel's rows of dZ.
+constexpr int kFewWeights = 16;
+template <int kTok>
+__global__ void __launch_bounds__(kThreads) ffn_few_weights_kernel(Product p) {
+    constexpr int kCols = 4, kRows = 128, kPitch = kTok + 4;
+    __shared__ __align__(16) float panel[kRows * kPitch];  // [row][token]
+    let_next_begin();
+    after_previous();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int down = blockIdx.x / p.across, r0 = down * kRows, c0 = (blockIdx.x - down * p.across) * 32 * kCols + lane;
+    float x[kCols][kTok];
+#pragma unroll
+    for (int t = 0; t < kTok; ++t)
+#pragma unroll
+        for (int j = 0; j < kCols; ++j) x[j][t] = t < p.K && c0 + 32 * j < p.N ? p.b.p[t * p.b.step + c0 + 32 * j] : 0.f;
+    const int row = threadIdx.x % kRows;
+#pragma unroll
+    for (int t = threadIdx.x / kRows; t < kTok; t += kThreads / kRows)
+        panel[row * kPitch + t] = t < p.K && r0 + row < p.M ? p.a.p[t * p.a.step + r0 + row] : 0.f;
+    __syncthreads();
+#pragma unroll 2
+    for (int i = warp; i < kRows; i += kWarps) {
+        if (r0 + i >= p.M) break;
+        float sum[kCols] = {};
+#pragma unroll
+        for (int t = 0; t < kTok; t += 4) {
+            float d[4];
+            VecIo<float, 4>::load(panel + i * kPitch + t, d);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) sum[j] = fmaf(x[j][t + q], d[q], sum[j]);
+        }
+        float *to = p.out + (r0 + i) * p.out_row + c0;
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+            if (c0 + 32 * j < p.N) to[32 * j] = sum[j];
+    }
 }
 
 // out = the sum of `parts` runs of M x N
@@ -510,11 +564,11 @@ cudaError_t product(Product p, const Plan &by, cudaStream_t s) {
                       : as(ffn_product_kernel<128, kA, kB, kMode>, Panel<128, kA>::kFloats + Panel<128, kB>::kFloats);
 }
 
-// Few rows: blocks of a cluster as many as fill three blocks an SM, each with `least` indices of the sum or more
+// Few rows: blocks of a cluster as many as fill `blocks` an SM, each with `least` indices of the sum or more
 template <typename K>
-cudaError_t few(K kernel, Product p, long long tiles, int least, int step, int floats, cudaStream_t s) {
+cudaError_t few(K kernel, Product p, long long tiles, int blocks, int least, int step, int floats, cudaStream_t s) {
     int S = 1;
-    while (S < 8 && tiles * S * 2 <= 3 * kSMs && p.K >= S * 2 * least) S *= 2;
+    while (S < 8 && tiles * S * 2 <= blocks * kSMs && p.K >= S * 2 * least) S *= 2;
     p.per = ((p.K + S - 1) / S + step - 1) / step * step;
     const int smem = floats * (int)sizeof(float);
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -524,7 +578,8 @@ template <Mode kMode>
 cudaError_t few_forward(const Product &p, cudaStream_t s) {
     auto as = [&](auto Tok) {
         constexpr int kTok = Tok(), kSums = kWarps * 2 * kTok * 32, kRing = kFewStages * kFewFloats<kTok>;
-        return few(ffn_few_kernel<kTok, kMode>, p, (p.N + 31) / 32, 4 * kFewDepth, kFewDepth, kRing > kSums ? kRing : kSums, s);
+        return few(ffn_few_kernel<kTok, kMode>, p, (p.N + 31) / 32, 3, 4 * kFewDepth, kFewDepth,
+                   kRing > kSums ? kRing : kSums, s);
     };
     return p.M <= 8    ? as(std::integral_constant<int, 8>())
            : p.M <= 16 ? as(std::integral_constant<int, 16>())
@@ -533,11 +588,19 @@ cudaError_t few_forward(const Product &p, cudaStream_t s) {
 cudaError_t few_back(const Product &p, cudaStream_t s) {
     auto as = [&](auto Tok) {
         constexpr int kTok = Tok();
-        return few(ffn_few_back_kernel<kTok>, p, (p.N + kBackCols - 1) / kBackCols, kBackRows, kBackRows, kBackFloats<kTok>, s);
+        return few(ffn_few_back_kernel<kTok>, p, (p.N + kBackCols - 1) / kBackCols, 2, 128, back_rows(kTok),
+                   kBackFloats<kTok>, s);
     };
     return p.M <= 8    ? as(std::integral_constant<int, 8>())
            : p.M <= 16 ? as(std::integral_constant<int, 16>())
                        : as(std::integral_constant<int, 32>());
+}
+
+cudaError_t few_weights(Product p, cudaStream_t s) {
+    p.across = (p.N + 127) / 128;
+    const unsigned blocks = (unsigned)p.across * ((p.M + 127) / 128);
+    return p.K <= 8 ? launch_after(ffn_few_weights_kernel<8>, blocks, kThreads, 0, s, p)
+                    : launch_after(ffn_few_weights_kernel<16>, blocks, kThreads, 0, s, p);
 }
 
 const float *floats(const void *p) { return static_cast<const float *>(p); }
@@ -581,10 +644,15 @@ cudaError_t backward_f32(const FfnBwd &p, cudaStream_t s) {
     float *sums = dz + (size_t)f.M * row;
     const Product dw{mat(dz, row), mat(floats(f.x), f.x_stride), F2, f.K, f.M, 0, f.M, 0, static_cast<float *>(p.dw), f.K,
                      nullptr, 0, nullptr};
-    const Plan by_dw = plan_dw(f.M, f.K, f.F);
-    e = cut_product<false>(dw, by_dw, sums, s);
-    if (e) return e;
-    sums += parts_floats(by_dw.parts, F2, f.K);
+    if (f.M <= kFewWeights) {
+        e = few_weights(dw, s);
+        if (e) return e;
+    } else {
+        const Plan by_dw = plan_dw(f.M, f.K, f.F);
+        e = cut_product<false>(dw, by_dw, sums, s);
+        if (e) return e;
+        sums += parts_floats(by_dw.parts, F2, f.K);
+    }
     const Product dx{mat(dz, row), mat(floats(f.w), f.K), f.M, f.K, F2, 0, F2, 0, static_cast<float *>(p.dx), p.dx_stride,
                      nullptr, 0, nullptr};
     return f.M <= kFewMost ? few_back(dx, s) : cut_product<true>(dx, plan_dx(f.M, f.K, f.F), sums, s);
@@ -598,8 +666,9 @@ size_t ffn_forward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
 size_t ffn_backward_scratch_bytes(int M, int K, int F, hla_dtype dt) {
     if (dt == HLA_BF16) return ffn_tc_backward_scratch_bytes(M, K, F);
     if (M == 0) return 0;
-    return sizeof(float) *
-           ((size_t)M * dz_row(F) + parts_floats(M <= kFewMost ? 1 : plan_dx(M, K, F).parts, M, K) + parts_floats(plan_dw(M, K, F).parts, 2LL * F, K));
+    if (M <= kFewMost) return sizeof(float) * (size_t)M * dz_row(F);  // (a sum of so few is not cut)
+    const Plan dx = plan_dx(M, K, F), dw = plan_dw(M, K, F);
+    return sizeof(float) * ((size_t)M * dz_row(F) + parts_floats(dx.parts, M, K) + parts_floats(dw.parts, 2LL * F, K));
 }
 cudaError_t ffn_forward_launch(const Ffn &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? ffn_tc_forward(p, s) : forward_f32(p, s);
