@@ -136,10 +136,10 @@ __device__ __forceinline__ void activate(int act, Pairs &v, Pairs &slope) {
     }
 }
 
-// A thread's eight columns: kE accesses of kV neighbours, `threads` apart
+// A thread's eight columns: kE accesses of kV neighbours (kNear of them lie side by side), `threads` apart
 template <typename T, int kV>
 struct Cols {
-    static constexpr int kE = kPer / kV;
+    static constexpr int kE = kPer / kV, kNear = kV;
     Raw<T, kV> r[kE];
     static __device__ __forceinline__ int at(int e, int t, int threads) { return (e * threads + t) * kV; }
     __device__ __forceinline__ void load(const T *row, int t, int threads, int C) {
@@ -174,6 +174,67 @@ struct Cols {
 #pragma unroll
             for (int i = 0; i < kV; ++i) o[i] = f[e * kV + i];
             if (c < C) VecIo<T, kV>::store(row + c, o);
+        }
+    }
+};
+
+// bf16 rows of blocks that begin anywhere, in the forward (kWords): pairs of neighbours out of the one or two 4-byte words
+// that hold them (a word that holds one element of a row is memory of its tensor).  C 2047: 119 us against 191 by the
+// element, C 519 175 against 291; not for rows of lanes (C 255: 110 against 81), nor in the gradient, which has no
+// registers for the words of its next row (C 2047: 349 against 250).
+constexpr int kWords = 0;
+template <>
+struct Cols<__nv_bfloat16, kWords> {
+    using T = __nv_bfloat16;
+    static constexpr int kE = kPer / 2, kNear = 2;
+    uint32_t a[kE], b[kE], half;  // words; a bit for each pair of which one element is the row's last
+    bool odd;                     // the row begins in the middle of a word
+    static __device__ __forceinline__ int at(int e, int t, int threads) { return (e * threads + t) * 2; }
+    __device__ __forceinline__ void load(const T *row, int t, int threads, int C) {
+        odd = reinterpret_cast<uintptr_t>(row) & 2;
+        half = 0;
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(row) & ~uintptr_t(3));
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const int c = at(e, t, threads);
+            a[e] = c < C ? words[c / 2] : 0u;
+            b[e] = odd && c + 1 < C ? words[c / 2 + 1] : 0u;
+            if (c + 1 == C) half |= 1u << e;
+        }
+    }
+    __device__ __forceinline__ void get(Pairs &v) const {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            Raw<T, 2> r;
+            r.v = odd ? __byte_perm(a[e], b[e], 0x5432) : a[e];
+            if (half >> e & 1) r.v &= 0xffffu;
+            uint64_t f[1];
+            to_pairs(r, f);
+            v[e] = f[0];
+        }
+    }
+    // (every lane takes part) where a row begins in the middle of a word, a lane's words are its first element and the
+    // lane's before it: whole words, because halves of them by turns cost twice the way to L2
+    static __device__ __forceinline__ void put(T *row, int t, int threads, int C, const Pairs &v) {
+        const bool odd = reinterpret_cast<uintptr_t>(row) & 2, first = (t & 31) == 0, last = (t & 31) == 31 || t == threads - 1;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const int c = at(e, t, threads);
+            float f[2];
+            unpair(v[e], f[0], f[1]);
+            const float before = __shfl_up_sync(0xffffffffu, f[1], 1);
+            if (!odd) {
+                if (c + 1 < C) VecIo<T, 2>::store(row + c, f);
+                else if (c < C) from_f32(row + c, f[0]);
+            } else {
+                const float pair[2] = {before, f[0]};
+                if (c < C) {
+                    if (first) from_f32(row + c, f[0]);
+                    else VecIo<T, 2>::store(row + c - 1, pair);
+                }
+                // (where the next lane has nothing of the row, the second is this lane's to write, too)
+                if (c + 1 < C && (last || c + 2 >= C)) from_f32(row + c + 1, f[1]);
+            }
         }
     }
 };
@@ -413,7 +474,7 @@ block_norm_forward_kernel(BlockNorm p) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
     }
-    Drop<kV> drop;
+    Drop<Cols<T, kV>::kNear> drop;
     drop.open(p, t, threads);
     Rows<T, kV, 3, 1> in{{static_cast<const T *>(p.x), static_cast<const T *>(p.y), static_cast<const T *>(p.gate)},
                               {p.x_stride, p.y_stride, p.gate_stride}, nullptr, t, threads, C, p.rows, step};
@@ -562,7 +623,7 @@ block_norm_backward_kernel(BlockNormBwd q) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) scale[i] = mul2(mul2(scale[i], w_post[i]), twice(p.keep_scale));
     }
-    Drop<kV> drop;
+    Drop<Cols<T, kV>::kNear> drop;
     drop.open(p, t, threads);
     Pairs qu = {}, dw_pre = {};  // sums over this thread's rows
     // With 64 registers a thread the sums wait in shared memory and w_pre is read where it is used (gradient of C 8190
@@ -697,6 +758,7 @@ block_norm_backward_kernel(BlockNormBwd q) {
         get_sums(1, dw_pre);
     }
     // this block's sums, in the order of its warps (the blocks' by column_sum_launch)
+    constexpr int kNear = Cols<T, kV>::kNear;
     float sum[2][kPer];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
@@ -714,7 +776,7 @@ block_norm_backward_kernel(BlockNormBwd q) {
             if ((threadIdx.x >> 5) == w && in_warp == 0) {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
-                    const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
+                    const int c = Cols<T, kV>::at(i / kNear, t, threads) + i % kNear;
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         sum[n][i] += w ? sums[n * kNarrow + c] : 0.f;
@@ -729,7 +791,7 @@ block_norm_backward_kernel(BlockNormBwd q) {
     if (kBlock || (threadIdx.x >= kNarrowThreads - 32 && in_warp == 0)) {
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const int c = Cols<T, kV>::at(i / kV, t, threads) + i % kV;
+            const int c = Cols<T, kV>::at(i / kNear, t, threads) + i % kNear;
             if (c < C) {
                 to[c] = sum[0][i];
                 to[(size_t)C + c] = sum[1][i];
@@ -870,7 +932,8 @@ cudaError_t forward_of(const BlockNorm &p, cudaStream_t s) {
     if (p.C > kWide) return launch_after(block_norm_wide_forward_kernel<T>, g.grid, 1024, 0, s, p);
     auto as = [&](auto V) -> cudaError_t {
         return by_threads(p.C, g.threads, [&](auto M) {
-            return launch_after(block_norm_forward_kernel<T, V(), M()>, g.grid, g.threads, 0, s, p);
+            constexpr int kV = V() == 1 && sizeof(T) == 2 && M() > 32 ? kWords : V();
+            return launch_after(block_norm_forward_kernel<T, kV, M()>, g.grid, g.threads, 0, s, p);
         });
     };
     return by_access<T>(p, as);
