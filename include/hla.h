@@ -512,7 +512,8 @@ int hla_glr_marks(int n);
  *             every 32nd token, which hla_glr_backward reads
  * decay, states and marks are 16-byte aligned.
  * No workspace (should a wait between the blocks of one sequence run past its limit of 2 s, states and
- * outputs are NaN from there on).  fp32 throughout for both types; i_t below 1e-19 counts as 0.  A NaN
+ * outputs are NaN from there on).  fp32 throughout for both types; i_t below 1e-19 counts as 0, and a token
+ * whose gates are both shut (r and g far below 0, minus infinity too) leaves the state as it is.  A NaN
  * or infinity in a token reaches that token's output and, where it enters the state, later ones, and no
  * earlier one.
  */

@@ -15,7 +15,7 @@
 // all form the same state in the same order, so equal inputs give equal bits.  The gradient walks the tiles backwards
 // and takes h before each tile from the marks that the forward leaves, so it reads every token once too.
 //
-// Least traffic: four (gradient: seven) values a token and channel.  bf16, B8 n2048 C2048: 52 us, 5.1 TB/s, 77 % of what
+// Least traffic: four (gradient: seven) values a token and channel.  bf16, B8 n2048 C2048: 53 us, 5.0 TB/s, 76 % of what
 // a copy reaches; the gradient 120 us, 4.0 TB/s, 60 %.  Both are bound by issue slots (60 % of them in use, 256 blocks
 // of 304 places, 16 warps an SM, which their 128 registers a thread allow), not by DRAM.  B1 n32768 C1024, clusters of
 // eight: 85 us, 47 %, of which the exchanges take 10 us and the joins of the tiles 12.  One token of 64 x 2048: 2.5 us on
@@ -103,6 +103,14 @@ __device__ __forceinline__ void decay_of(const Decay &d, uint64_t s, uint64_t &a
     unpair(far_w, g0, g1);
     a = pair(v0 <= 1.f ? a0 : f0, v1 <= 1.f ? a1 : f1);  // (a NaN in r is in both)
     w = pair(v0 <= 1.f ? w0 : g0, v1 <= 1.f ? w1 : g1);
+}
+
+// sqrt(w) / d, d = 1 + e^-g being 1 / i: w rsqrt((w + tiny) d^2), whose argument is above 0 whatever w is.  0 where w is 0
+// (a shut r) or d^2 leaves the range (i below 1e-19), and where both are so, as where both gates mask a token.  B8 n2048
+// C2048 bf16: 53.4 us; with the tiny value behind the product with d^2, which is infinity times 0 there, 52.4; as the
+// root of w times the reciprocal of d 55.0.
+__device__ __forceinline__ uint64_t input_of(uint64_t w, uint64_t d) {
+    return mul2(w, each(mul2(mul2(d, d), add2(w, twice(kTiny))), rsqrt_of));
 }
 
 // A block's shape: kLanes lanes walk a token's 2 kLanes channels, so a block of 256 threads has kGroups runs of kTok
@@ -510,9 +518,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
                         if (t0 + u >= len) shut(rr);  // (x is 0 there)
                         decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
                         const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
-                        // sqrt(w) / d = w rsqrt(w d^2)  (0 where d^2 leaves the range: i is below 1e-19 there)
-                        const uint64_t x = as_pair(in.get(slot, 0, t0, u)),
-                                       add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), x);
+                        const uint64_t x = as_pair(in.get(slot, 0, t0, u)), add = mul2(input_of(w, d), x);
                         h[u] = u ? fma2(a, h[u - 1], add) : add;
                         pr[u] = u ? mul2(a, pr[u - 1]) : a;
                         if (i + 1 < kTiles) kept[(i * kTok + u) * kThreads] = {pr[u], h[u]};
@@ -583,7 +589,7 @@ __global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool ro
     uint64_t a, w;
     decay_of<false>(decay, each(one_plus_exp(r), rcp), a, w);
     const uint64_t d = one_plus_exp(g);
-    const uint64_t add = mul2(mul2(w, each(fma2(mul2(d, d), w, twice(kTiny)), rsqrt_of)), x), y = fma2(a, h, add);
+    const uint64_t add = mul2(input_of(w, d), x), y = fma2(a, h, add);
     at.put(p.state_out + (size_t)b * p.C, y, pairs);
     at.put(static_cast<T *>(p.y) + (size_t)b * p.y_stride, y, rows_pairs);
 }
