@@ -952,8 +952,10 @@ cudaError_t backward_of(const BlockNormBwd &q, cudaStream_t s) {
     const cudaError_t e =
         p.C > kWide ? launch_after(block_norm_wide_backward_kernel<T>, g.grid, 1024, 0, s, q) : by_access<T>(q, as);
     if (e) return e;
+    // (what the sum for dscale is of y is none of a weight that is not there)
+    const int post = p.post ? 0 : ColumnSum::kNoSum, pre = p.pre ? 1 : ColumnSum::kNoSum;
     const ColumnSum sums{q.partial, g.grid, p.C, 2,
-                         {{q.dw_post, 0, p.scale}, {q.dscale, 0, p.w_post}, {q.dw_pre, 1, nullptr}}, p.dt, q.header};
+                         {{q.dw_post, post, p.scale}, {q.dscale, 0, p.w_post}, {q.dw_pre, pre, nullptr}}, p.dt, q.header};
     return column_sum_launch(sums, s);
 }
 

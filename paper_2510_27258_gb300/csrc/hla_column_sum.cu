@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(kThreads) column_sum_kernel(ColumnSum p) {
 #pragma unroll
         for (int o = 0; o < 3; ++o) {
             const ColumnSum::Out &out = p.out[o];
+            if (out.to && out.part == ColumnSum::kNoSum && part == 0) out.to[i] = 0.f;
             if (!out.to || out.part != part) continue;
             const float by = !out.factor           ? 1.f
                              : p.dt == HLA_BF16 ? to_f32(static_cast<const __nv_bfloat16 *>(out.factor)[i])

@@ -307,8 +307,9 @@ size_t block_norm_partial_floats(long long rows, int C);
 cudaError_t block_norm_backward_launch(const BlockNormBwd &p, cudaStream_t stream);
 
 // sums over `rows` partial rows of `parts` runs of C floats, in a fixed order: out[i].to, unless null, receives those
-// of one run, times a factor of type dt for each column where that is given; clears the workspace's header
+// of one run, times a factor of type dt for each column where that is given, or (kNoSum) zeros; clears the workspace's header
 struct ColumnSum {
+    static constexpr int kNoSum = -1;
     const float *partial;
     long long rows;
     int C, parts;
