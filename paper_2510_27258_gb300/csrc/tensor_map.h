@@ -29,4 +29,18 @@ inline EncodeTiledFn encode_fn() {
     return fn;
 }
 
+// cuTensorMapEncodeTiled.  A driver's call, which wants a context: a host thread whose first CUDA call this is has none
+// (the runtime's calls give it one where they need it), so it is given its GPU's here.
+template <typename... Args>
+CUresult encode_tiled(Args... args) {
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return CUDA_ERROR_NOT_SUPPORTED;
+    CUresult r = fn(args...);
+    int gpu;
+    if ((r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) && cudaGetDevice(&gpu) == cudaSuccess &&
+        cudaSetDevice(gpu) == cudaSuccess)
+        r = fn(args...);
+    return r;
+}
+
 }  // namespace hla
