@@ -592,13 +592,9 @@ cudaError_t launch_all(const Fwd2 &p, const C3Layout &L, float *ws, cudaStream_t
     T *out = static_cast<T *>(p.out);
     cudaError_t e;
     const dim3 grid(L.nc, L.BH);
-    if ((e = cudaFuncSetAttribute(c3_local_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_local(L))))
-        return e;
-    if ((e = cudaFuncSetAttribute(c3_bracket_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                  (int)smem_bracket(L))))
-        return e;
-    if ((e = cudaFuncSetAttribute(c3_out_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_out(L))))
-        return e;
+    if ((e = allow_smem(c3_local_kernel<T>, smem_local(L)))) return e;
+    if ((e = allow_smem(c3_bracket_kernel<T>, smem_bracket(L)))) return e;
+    if ((e = allow_smem(c3_out_kernel<T>, smem_out(L)))) return e;
     cudaFuncSetAttribute(c3_out_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
     cudaFuncSetAttribute(c3_local_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);
     cudaFuncSetAttribute(c3_bracket_kernel<T>, cudaFuncAttributePreferredSharedMemoryCarveout, 100);

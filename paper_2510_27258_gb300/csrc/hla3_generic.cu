@@ -192,17 +192,13 @@ cudaError_t generic3_forward(const Fwd2 &p, cudaStream_t stream) {
     float *ws_state = reinterpret_cast<float *>(p.ws + kWsHeaderBytes);
     cudaError_t e;
     if (p.dt == HLA_BF16) {
-        if ((e = cudaFuncSetAttribute(hla3_serial_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      (int)smem)))
-            return e;
+        if ((e = allow_smem(hla3_serial_kernel<__nv_bfloat16>, smem))) return e;
         hla3_serial_kernel<__nv_bfloat16><<<p.BH, kT3, smem, stream>>>(
             static_cast<const __nv_bfloat16 *>(p.q), static_cast<const __nv_bfloat16 *>(p.k),
             static_cast<const __nv_bfloat16 *>(p.v), static_cast<__nv_bfloat16 *>(p.out), p.n, p.d, p.dv, p.masked,
             p.normalized, p.eps, p.state_in, p.state_out, ws_state, in_smem);
     } else {
-        if ((e = cudaFuncSetAttribute(hla3_serial_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      (int)smem)))
-            return e;
+        if ((e = allow_smem(hla3_serial_kernel<float>, smem))) return e;
         hla3_serial_kernel<float><<<p.BH, kT3, smem, stream>>>(
             static_cast<const float *>(p.q), static_cast<const float *>(p.k), static_cast<const float *>(p.v),
             static_cast<float *>(p.out), p.n, p.d, p.dv, p.masked, p.normalized, p.eps, p.state_in, p.state_out,

@@ -389,21 +389,19 @@ cudaError_t forward_t(const Fwd2 &p, cudaStream_t stream) {
     cudaError_t e;
     if (L.nch > 0) {
         const size_t sm1 = sizeof(float) * ((size_t)L.C * (2 * L.d + 1 + 2 * (L.dv + 1)) + (size_t)L.C * L.C);
-        if ((e = cudaFuncSetAttribute(ahla_local_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm1)))
-            return e;
+        if ((e = allow_smem(ahla_local_kernel<T>, sm1))) return e;
         ahla_local_kernel<T><<<dim3(L.nch, p.BH), kThreads, sm1, stream>>>(q, k, v, ws, L);
         if ((e = cudaGetLastError())) return e;
     }
     const size_t sm2 = sizeof(float) * ((size_t)2 * p.d * kCols + (size_t)p.d * p.d);
-    if ((e = cudaFuncSetAttribute(ahla_scan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm2))) return e;
+    if ((e = allow_smem(ahla_scan_kernel, sm2))) return e;
     ahla_scan_kernel<<<dim3((p.dv + 1 + kCols - 1) / kCols, p.BH), kThreads, sm2, stream>>>(ws, L, p.state_in,
                                                                                             p.state_out);
     if ((e = cudaGetLastError())) return e;
     if (L.nch > 0) {
         const size_t sm3 = sizeof(float) * ((size_t)L.C * (L.d + std::max(L.d + 1, L.dv + 1) + L.dv + 1) +
                                             (size_t)L.C * L.C + 2 * (size_t)L.d * (L.dv + 1));
-        if ((e = cudaFuncSetAttribute(ahla_out_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm3)))
-            return e;
+        if ((e = allow_smem(ahla_out_kernel<T>, sm3))) return e;
         ahla_out_kernel<T><<<dim3(L.nch, p.BH), kThreads, sm3, stream>>>(q, k, static_cast<T *>(p.out), ws, L,
                                                                          p.normalized, p.eps);
         if ((e = cudaGetLastError())) return e;
@@ -439,16 +437,12 @@ cudaError_t ahla_step_launch(const void *q, const void *k, const void *v, void *
     const size_t smem = 2 * 16 * (size_t)((d * dv + d) / 4) + tsz * (2 * (size_t)d + dv);
     cudaError_t e;
     if (dt == HLA_BF16) {
-        if ((e = cudaFuncSetAttribute(ahla_step_staged_kernel<__nv_bfloat16>,
-                                      cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)))
-            return e;
+        if ((e = allow_smem(ahla_step_staged_kernel<__nv_bfloat16>, smem))) return e;
         ahla_step_staged_kernel<__nv_bfloat16><<<grid, kStepPThreads, smem, stream>>>(
             static_cast<const __nv_bfloat16 *>(q), static_cast<const __nv_bfloat16 *>(k),
             static_cast<const __nv_bfloat16 *>(v), static_cast<__nv_bfloat16 *>(out), state, BH, d, dv, normalized, eps);
     } else {
-        if ((e = cudaFuncSetAttribute(ahla_step_staged_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      (int)smem)))
-            return e;
+        if ((e = allow_smem(ahla_step_staged_kernel<float>, smem))) return e;
         ahla_step_staged_kernel<float><<<grid, kStepPThreads, smem, stream>>>(
             static_cast<const float *>(q), static_cast<const float *>(k), static_cast<const float *>(v),
             static_cast<float *>(out), state, BH, d, dv, normalized, eps);

@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 
 #include "hla_internal.h"
 
@@ -32,6 +33,15 @@ hla_status poll_header(void *header, cudaStream_t s) {
     st = cuda_status(cudaMemsetAsync(header, 0, sizeof(h), s), "clearing flag");
     if (st != HLA_OK) return st;
     return fail(HLA_ERR_TIMEOUT, "device-side wait gave up (where=%u detail=%u)", h.where, h.detail);
+}
+
+cudaError_t allow_smem(const void *kernel, size_t bytes) {
+    static std::mutex raising;
+    const std::lock_guard<std::mutex> lock(raising);
+    cudaFuncAttributes a;
+    const cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+    if (e || (size_t)a.maxDynamicSharedSizeBytes >= bytes) return e;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
 hla_status cuda_status(cudaError_t err, const char *what) {

@@ -339,25 +339,25 @@ cudaError_t backward_t(const Bwd2 &p, cudaStream_t s) {
     cudaError_t e;
     auto smem = [](size_t floats) { return (int)(floats * sizeof(float)); };
     const int sm1 = smem((size_t)C * d + (size_t)C * kd + (size_t)C * W + (size_t)C * C + (size_t)C * d);
-    if ((e = cudaFuncSetAttribute(bwd_fwd_local<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, sm1))) return e;
+    if ((e = allow_smem(bwd_fwd_local<T>, sm1))) return e;
     bwd_fwd_local<T><<<grid, kThreads, sm1, s>>>(q, k, v, ws, L);
     if ((e = cudaGetLastError())) return e;
     const int sm2 = smem((size_t)d * d + 3 * (size_t)d * kCols);
-    if ((e = cudaFuncSetAttribute(bwd_fwd_scan, cudaFuncAttributeMaxDynamicSharedMemorySize, sm2))) return e;
+    if ((e = allow_smem(bwd_fwd_scan, sm2))) return e;
     bwd_fwd_scan<<<dim3((W + kCols - 1) / kCols, p.BH), kThreads, sm2, s>>>(ws, L);
     if ((e = cudaGetLastError())) return e;
     const int sm3 = smem((size_t)C * d + (size_t)C * kd + 2 * (size_t)C * W + 2 * (size_t)C * C + (size_t)C * d +
                          (size_t)C * std::max(W, d));
-    if ((e = cudaFuncSetAttribute(bwd_local1<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, sm3))) return e;
+    if ((e = allow_smem(bwd_local1<T>, sm3))) return e;
     bwd_local1<T><<<grid, kThreads, sm3, s>>>(q, k, v, g, ws, L, p.normalized, p.eps);
     if ((e = cudaGetLastError())) return e;
     const int sm4 = smem(2 * (size_t)W * d + (size_t)d * kCols);
-    if ((e = cudaFuncSetAttribute(bwd_scan, cudaFuncAttributeMaxDynamicSharedMemorySize, sm4))) return e;
+    if ((e = allow_smem(bwd_scan, sm4))) return e;
     bwd_scan<<<dim3((d + kCols - 1) / kCols, p.BH), kThreads, sm4, s>>>(ws, L);
     if ((e = cudaGetLastError())) return e;
     const int sm5 = smem((size_t)C * d + (size_t)C * kd + 2 * (size_t)C * W + 4 * (size_t)C * C + 2 * (size_t)C * d +
                          (size_t)C * std::max(W, d));
-    if ((e = cudaFuncSetAttribute(bwd_local2<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, sm5))) return e;
+    if ((e = allow_smem(bwd_local2<T>, sm5))) return e;
     bwd_local2<T><<<grid, kThreads, sm5, s>>>(q, k, v, static_cast<T *>(p.dq), static_cast<T *>(p.dk),
                                                static_cast<T *>(p.dval), ws, L);
     return cudaGetLastError();

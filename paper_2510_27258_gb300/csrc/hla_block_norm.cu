@@ -920,7 +920,7 @@ cudaError_t by_threads(int C, int threads, F f) {
 template <typename P>
 cudaError_t launch_ring(void (*kernel)(P), const Plan &g, size_t smem, cudaStream_t s, const P &p) {
     if (smem > 32 * 1024) {  // (48 KB with what the kernel has besides)
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = allow_smem(kernel, smem);
         if (e) return e;
     }
     return launch_after(kernel, g.grid, g.threads, smem, s, p);

@@ -865,7 +865,7 @@ cudaError_t run_few(const CUtensorMap &weights, const CUtensorMap &tokens, Few f
     while (S < 8 && (long long)tiles * S * 2 <= 2 * kSMs && f.steps >= S * 2 * 4) S *= 2;
     f.per = tiles_of(f.steps, S);
     const int smem = 1024 + (f.stages * bytes > sums ? f.stages * bytes : sums);
-    const cudaError_t e = cudaFuncSetAttribute(ffn_few_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t e = allow_smem(ffn_few_kernel<kMode>, smem);
     if (e) return e;
     return launch_cluster_after(ffn_few_kernel<kMode>, (unsigned)((long long)tiles * S), kFewThreads, S, smem, s, weights,
                                 tokens, f, S);

@@ -327,12 +327,9 @@ cudaError_t launch_all(const Fwd2 &p, const GLayout &L, float *scratch, cudaStre
     const size_t sm_scan = sizeof(float) * (size_t)(L.d * L.d + L.d);
     const size_t sm_out = sizeof(float) * (size_t)L.C * (L.d + L.dv + 1);
     cudaError_t e;
-    if ((e = cudaFuncSetAttribute(g2_local_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm_local)))
-        return e;
-    if ((e = cudaFuncSetAttribute(g2_scan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm_scan)))
-        return e;
-    if ((e = cudaFuncSetAttribute(g2_out_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm_out)))
-        return e;
+    if ((e = allow_smem(g2_local_kernel<T>, sm_local))) return e;
+    if ((e = allow_smem(g2_scan_kernel, sm_scan))) return e;
+    if ((e = allow_smem(g2_out_kernel<T>, sm_out))) return e;
     if (L.nch > 0) {
         g2_local_kernel<T><<<dim3(L.nch, L.BH), kThreads, sm_local, stream>>>(q, k, v, scratch, L);
         if ((e = cudaGetLastError())) return e;

@@ -36,6 +36,14 @@ hla_status poll_header(void *header, cudaStream_t stream);
 // Maps a CUDA error to HLA_ERR_CUDA (recording the CUDA message), or HLA_OK.
 hla_status cuda_status(cudaError_t err, const char *what);
 
+// Lets `kernel` be launched with `bytes` of dynamic shared memory on the current GPU.  The setting is the kernel's, not the
+// call's: it is only ever raised, since another thread may be between its own call of this and its launch.
+cudaError_t allow_smem(const void *kernel, size_t bytes);
+template <typename... P>
+cudaError_t allow_smem(void (*kernel)(P...), size_t bytes) {
+    return allow_smem(reinterpret_cast<const void *>(kernel), bytes);
+}
+
 // ---------------------------------------------------------------------------
 // token element access
 // ---------------------------------------------------------------------------

@@ -353,7 +353,7 @@ cudaError_t step2_launch_t(const void *q, const void *k, const void *v, void *ou
     if (dt == HLA_BF16) {
         auto kern = step2_kernel<__nv_bfloat16, kSDE>;
         const size_t sm = step2_smem(d, dv, masked, sizeof(__nv_bfloat16));
-        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm))) return e;
+        if ((e = allow_smem(kern, sm))) return e;
         kern<<<grid, kStepThreads, sm, stream>>>(static_cast<const __nv_bfloat16 *>(q),
                                                 static_cast<const __nv_bfloat16 *>(k),
                                                 static_cast<const __nv_bfloat16 *>(v),
@@ -362,7 +362,7 @@ cudaError_t step2_launch_t(const void *q, const void *k, const void *v, void *ou
     } else {
         auto kern = step2_kernel<float, kSDE>;
         const size_t sm = step2_smem(d, dv, masked, sizeof(float));
-        if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sm))) return e;
+        if ((e = allow_smem(kern, sm))) return e;
         kern<<<grid, kStepThreads, sm, stream>>>(static_cast<const float *>(q), static_cast<const float *>(k),
                                                 static_cast<const float *>(v), static_cast<float *>(out), state,
                                                 BH, d, dv, masked, normalized, eps);
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(256) state_to_sde_kernel(const float *src, flo
 cudaError_t state_to_sde_launch(const float *src, float *dst, int BH, int d, int dv, cudaStream_t stream) {
     if (BH == 0) return cudaSuccess;
     const size_t smem = sizeof(float) * ((size_t)d * d + 2 * (size_t)d * dv + 2 * (size_t)d);
-    cudaError_t e = cudaFuncSetAttribute(state_to_sde_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = allow_smem(state_to_sde_kernel, smem);
     if (e) return e;
     state_to_sde_kernel<<<BH, 256, smem, stream>>>(src, dst, d, dv);
     return cudaGetLastError();
