@@ -511,8 +511,8 @@ int hla_glr_marks(int n);
  * marks     : device fp32 [B, hla_glr_marks(n), C] or NULL; receives the state before
  *             every 32nd token, which hla_glr_backward reads
  * decay, states and marks are 16-byte aligned.
- * No workspace (should a wait between the blocks of one sequence run past its limit of 2 s, states and
- * outputs are NaN from there on).  fp32 throughout for both types; i_t below 1e-19 counts as 0, and a token
+ * No workspace (should a wait between the blocks of one sequence run past its limit of 2 s, the state behind
+ * the sequence is NaN, and so are the outputs and marks that are not known without it).  fp32 throughout for both types; i_t below 1e-19 counts as 0, and a token
  * whose gates are both shut (r and g far below 0, minus infinity too) leaves the state as it is.  A NaN
  * or infinity in a token reaches that token's output and, where it enters the state, later ones, and no
  * earlier one.
@@ -539,7 +539,8 @@ size_t hla_glr_backward_workspace_bytes(int B, int n, int C, hla_dtype dt);
  * (device fp32 [C]) and, if not NULL, dstate_in (device fp32 [B, C]).
  * dy: device [B, n, C], row stride dy_stride; dstate_out: device fp32 [B, C] or NULL (= 0; may
  * equal dstate_in); marks: those that the forward with the same x, r, g, decay, lengths and
- * state_in left.  decay, states, marks and ddecay are 16-byte aligned.
+ * state_in left.  decay, states, marks and ddecay are 16-byte aligned.  workspace: 256-byte aligned;
+ * hla_poll_error reads its flag (a wait that ran out; what is not known without it, dstate_in and ddecay among it, is NaN).
  */
 hla_status hla_glr_backward(const void *x, const void *r, const void *g, const float *decay, const void *dy,
                             const float *marks, void *dx, void *dr, void *dg, float *ddecay, hla_dtype dt, int B, int n,

@@ -14,7 +14,8 @@ __global__ void __launch_bounds__(kThreads) column_sum_kernel(ColumnSum p) {
     __shared__ float red[kCols][kGroups + 1];
     let_next_begin();
     after_previous();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // no device-side waits before: never an error
+    // (of calls without device-side waits: never an error)
+    if (p.header && blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};
     const int place = threadIdx.x % kLanes * kV, group = threadIdx.x / kLanes;
     const long long cols = (long long)p.C * p.parts, at = (long long)blockIdx.x * kCols;
     float sum[kV] = {};

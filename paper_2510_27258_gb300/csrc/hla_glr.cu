@@ -16,10 +16,11 @@
 // and takes h before each tile from the marks that the forward leaves, so it reads every token once too.
 //
 // Least traffic: four (gradient: seven) values a token and channel.  bf16, B8 n2048 C2048: 53 us, 5.0 TB/s, 76 % of what
-// a copy reaches; the gradient 120 us, 4.0 TB/s, 60 %.  Both are bound by issue slots (60 % of them in use, 256 blocks
+// a copy reaches; the gradient 113 us, 4.2 TB/s, 63 %.  Both are bound by issue slots (60 % of them in use, 256 blocks
 // of 304 places, 16 warps an SM, which their 128 registers a thread allow), not by DRAM.  B1 n32768 C1024, clusters of
-// eight: 85 us, 47 %, of which the exchanges take 10 us and the joins of the tiles 12.  One token of 64 x 2048: 2.5 us on
+// eight: 86 us, 47 %, of which the exchanges take 10 us and the joins of the tiles 12.  One token of 64 x 2048: 2.5 us on
 // the device.
+#include <cstdlib>
 #include <type_traits>
 
 #include "hla_vec.cuh"
@@ -310,6 +311,8 @@ template <int kLanes, int kTiles>
 struct Exchange {
     Run runs[2][kMostBlocks<kLanes>][kTiles][kLanes], mine[2][kTiles][kLanes];
     uint64_t bar[2];
+    int lost;          // a wait of this block's ran out (at the end, in the first block: one of the cluster's did)
+    uint32_t missing;  // bytes to wait for that do not come (a test's, in the second block)
 };
 __device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
     uint32_t to;
@@ -318,27 +321,48 @@ __device__ __forceinline__ uint32_t in_block(const void *mine, unsigned rank) {
 }
 // every block is there, its barriers ready
 template <int kLanes, int kTiles>
-__device__ __forceinline__ void open_exchange(Exchange<kLanes, kTiles> &x, int S) {
+__device__ __forceinline__ void open_exchange(Exchange<kLanes, kTiles> &x, int S, uint32_t missing) {
     if (S == 1) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) mbar_init(&x.bar[i], 1);
+        x.lost = 0;
+        x.missing = cluster_rank() == 1 ? missing : 0;
         fence_mbar_init();
     }
     __syncthreads();
     cluster_meet();
 }
 
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity) {
-    if (mbar_try_wait(bar, parity)) return true;
+template <int kLanes, int kTiles>
+__device__ __forceinline__ bool is_lost(const Exchange<kLanes, kTiles> &x) {
+    return *reinterpret_cast<const volatile int *>(&x.lost);
+}
+// Whether the runs of one of the buffers came in time (where a wait of the block's has run out, no other takes longer).
+// A lane's own verdict, which decides no more than what the lane's channels are; what a warp or the block does goes by
+// x.lost behind a barrier.  (A vote of the warp here took the registers that the gradient's next mark is loaded into: B4
+// n2048 C2048 in fp32 97 us instead of 81.)
+template <int kLanes, int kTiles>
+__device__ __forceinline__ bool wait(Exchange<kLanes, kTiles> &x, int buf, uint32_t parity) {
+    if (mbar_try_wait(&x.bar[buf], parity)) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity))
-        if (clock64() - t0 > kWaitCycles) return false;
+    while (!mbar_try_wait(&x.bar[buf], parity))
+        if (is_lost(x) || clock64() - t0 > kWaitCycles) {
+            *reinterpret_cast<volatile int *>(&x.lost) = 1;
+            return false;
+        }
     return true;
 }
 
 // At the end: what was sent to a block has arrived before its shared memory goes.  Where a wait ran out there is no sign
-// of a copy but its time: one that was sent lands within microseconds.
-__device__ __forceinline__ void close_exchange(bool lost) {
+// of a copy but its time: one that was sent lands within microseconds.  The first block, which hands the state on, learns
+// whether a wait of any block ran out.
+template <int kLanes, int kTiles>
+__device__ __forceinline__ void close_exchange(Exchange<kLanes, kTiles> &x) {
+    __syncthreads();
+    const bool lost = is_lost(x);
+    if (lost && threadIdx.x == 0)
+        asm volatile("st.shared::cluster.u32 [%0], 1;" ::"r"(in_block(&x.lost, 0)) : "memory");
+    __syncwarp();
     cluster_meet();
     const long long t0 = clock64();
     while (lost && clock64() - t0 < kLandCycles) {
@@ -393,6 +417,7 @@ struct Joint {
     // The same for a cluster's S blocks, each with kTiles tiles of its own between two exchanges: the cluster's first
     // tiles (one a block) come before its second ones.  `state`: behind the round, in every warp.  The wait for the
     // others' runs has a limit, after which (`lost`) the states are NaN from there on, and so is what follows from them.
+    // From the next turn on the block sends no more, so no block has all runs of that turn, and every wait for them runs out.
     template <int kTiles>
     __device__ __forceinline__ void among(const Runs<Sh::kLanes> (&runs)[kTiles], Exchange<Sh::kLanes, kTiles> &x,
                                           int turn, int S, unsigned rank, const Run (&mine)[kTiles],
@@ -410,10 +435,10 @@ struct Joint {
             }
             if (last() && speaks()) x.mine[buf][i][lane] = {mul2(mine[i].p, ahead[i].p), after(mine[i], ahead[i].l)};
         }
-        if (last() && !lost) {  // (else the others' waits run out, too)
+        if (last() && __all_sync(0xffffffffu, !is_lost(x))) {
             fence_async_smem();
             const int to = threadIdx.x & 31;
-            if (to == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]));
+            if (to == 0) mbar_arrive_expect_tx(&x.bar[buf], S * (uint32_t)sizeof(x.mine[buf]) + x.missing);
             __syncwarp();
             if (to < S)
                 asm volatile(
@@ -422,7 +447,7 @@ struct Joint {
                     "r"(smem_u32(x.mine[buf])), "r"((uint32_t)sizeof(x.mine[buf])), "r"(in_block(&x.bar[buf], to))
                     : "memory");
         }
-        if (!lost) lost = !wait(&x.bar[buf], (turn >> 1) & 1);
+        if (!lost) lost = !wait(x, buf, (turn >> 1) & 1);
         uint64_t h = lost ? kLost : state;
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
@@ -495,7 +520,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     T *y = static_cast<T *>(p.y) + (row0 + t0) * p.y_stride;
     const long long y_step = step * p.y_stride;
     const Joint<Sh, 1> joint;
-    if (kTiles > 1) open_exchange(others, S);
+    if (kTiles > 1) open_exchange(others, S, p.missing);
     else if (joint.last() && joint.speaks()) carry[1][lane] = state;
     const int turns = (int)(((long long)p.n + kTiles * step - 1) / (kTiles * step));
     bool lost = false;
@@ -562,10 +587,15 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
-    // (a block alone: the last warp has it)
-    if (p.state_out && rank == 0 && joint.last() && joint.speaks()) at.put(p.state_out + (size_t)b * p.C, state, pairs);
+    auto put_state = [&](uint64_t v) {  // (a block alone: the last warp has it)
+        if (p.state_out && rank == 0 && joint.last() && joint.speaks()) at.put(p.state_out + (size_t)b * p.C, v, pairs);
+    };
+    put_state(state);
     ring_wait<0>();
-    if (kTiles > 1) close_exchange(lost);
+    if (kTiles > 1) {
+        close_exchange(others);
+        if (is_lost(others)) put_state(kLost);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -598,19 +628,21 @@ __global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool ro
 // gradient
 // ------------------------------------------------------------------------------------------------
 
-template <typename T, int kLanes, bool kWide>
-__global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int slabs, int S, bool out_pairs) {
+// kAlone: a sequence is one block's (S is 1).  With both in one kernel B8 n2048 C2048 in bf16 takes 117 us instead of 113.
+template <typename T, int kLanes, bool kWide, bool kAlone>
+__global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int slabs, int blocks, bool out_pairs) {
     using Sh = Shape<kLanes, 4>;
     constexpr int kTok = Sh::kTok;
     extern __shared__ __align__(128) char ring[];
     __shared__ Runs<kLanes> fwd[2], bwd[2][1];
-    __shared__ uint64_t carry[2][kLanes];   // (S 1)
-    __shared__ Exchange<kLanes, 1> others;  // (S > 1)
+    __shared__ uint64_t carry[2][kLanes];   // (kAlone)
+    __shared__ Exchange<kLanes, 1> others;  // (else)
     let_next_begin();
     after_previous();
     const Glr &f = p.f;
     const int group = Sh::group(), lane = Sh::lane();
-    const unsigned rank = S > 1 ? cluster_rank() : 0, unit = blockIdx.x / S;
+    const int S = kAlone ? 1 : blocks;
+    const unsigned rank = kAlone ? 0 : cluster_rank(), unit = blockIdx.x / S;
     const int b = unit / slabs;
     const uint32_t channel = (unit - b * slabs) * Sh::kChannels;
     const Lane at(channel, lane, f.C);
@@ -641,8 +673,12 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     };
     uint64_t first = state_before(tile);  // the state before the tile
     const Joint<Sh, -1> joint;
-    if (S > 1) open_exchange(others, S);
-    else if (joint.last() && joint.speaks()) carry[1][lane] = D;
+    if constexpr (!kAlone) {
+        open_exchange(others, S, f.missing);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *p.header = WsHeader{};  // (waits set it after seconds)
+    } else if (joint.last() && joint.speaks()) {
+        carry[1][lane] = D;
+    }
     const uint64_t minus = twice(-1.f);
     uint64_t dsum = 0;
     bool lost = false;
@@ -682,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
             uint64_t h = first;
             first = state_before(tile + step);
             uint64_t later;
-            if (S == 1) {
+            if constexpr (kAlone) {
                 later = joint.alone(bwd[buf][0], carry, round, mine[0], ahead[0], D);
             } else {
                 uint64_t got[1];
@@ -724,7 +760,10 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
     };
     if (decay.near) walk(std::true_type());
     else walk(std::false_type());
-    if (p.dstate_in && rank == 0 && joint.last() && joint.speaks()) at.put(p.dstate_in + (size_t)b * f.C, D, pairs);
+    auto put_state = [&](uint64_t v) {
+        if (p.dstate_in && rank == 0 && joint.last() && joint.speaks()) at.put(p.dstate_in + (size_t)b * f.C, v, pairs);
+    };
+    put_state(D);
     // decay's gradient: the block's warps in order, then (another kernel) its blocks
     if (Sh::kOfWarp > 1) dsum = add2(dsum, __shfl_xor_sync(0xffffffffu, dsum, 16));
     __syncthreads();
@@ -736,7 +775,17 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
         at.put(p.partial + ((size_t)b * S + rank) * f.C, dsum, pairs);
     }
     ring_wait<0>();
-    if (S > 1) close_exchange(lost);
+    if constexpr (!kAlone) {
+        close_exchange(others);
+        if (is_lost(others)) {
+            put_state(kLost);
+            if (threadIdx.x == 0) {
+                p.header->where = 1;
+                p.header->detail = blockIdx.x;
+                p.header->error = kDevTimeout;
+            }
+        }
+    }
 }
 
 // How a call is spread: lanes for a token's channels, and blocks of one sequence
@@ -806,10 +855,14 @@ cudaError_t backward_as(const GlrBwd &p, const Spread &r, cudaStream_t s) {
     const Glr &f = p.f;
     const bool pairs = pairs_ok<T>(p.dx, p.dx_stride, f.C) && pairs_ok<T>(p.dr, p.dr_stride, f.C) &&
                        pairs_ok<T>(p.dg, p.dg_stride, f.C);
-    const cudaError_t e = launch_clusters(glr_backward_kernel<T, kLanes, kWide>, (long long)f.B * r.slabs, r.S,
-                                          Tokens<T, Shape<kLanes, 4>, 4, kWide>::kSmem, s, p, r.slabs, r.S, pairs);
+    const cudaError_t e = launch_clusters(r.S == 1 ? glr_backward_kernel<T, kLanes, kWide, true>
+                                                   : glr_backward_kernel<T, kLanes, kWide, false>,
+                                          (long long)f.B * r.slabs, r.S, Tokens<T, Shape<kLanes, 4>, 4, kWide>::kSmem, s, p,
+                                          r.slabs, r.S, pairs);
     if (e) return e;
-    return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {{p.ddecay, 0, nullptr}}, f.dt, p.header}, s);
+    // (blocks that wait for one another have cleared the header before)
+    return column_sum_launch({p.partial, (long long)f.B * r.S, f.C, 1, {{p.ddecay, 0, nullptr}}, f.dt, r.S > 1 ? nullptr : p.header},
+                             s);
 }
 template <typename T>
 cudaError_t backward_of(const GlrBwd &p, cudaStream_t s) {
@@ -821,17 +874,24 @@ cudaError_t backward_of(const GlrBwd &p, cudaStream_t s) {
     return r.lanes == 32 ? backward_as<T, 32, false>(p, r, s) : backward_as<T, 16, false>(p, r, s);
 }
 
+// testing: the waits of a sequence's second block run out
+uint32_t missing_bytes() { return getenv("HLA_TEST_SHORT_COPY") ? 16 : 0; }
+
 }  // namespace
 
 bool glr_fits(int B, int C) { return (long long)B * ((C + 31) / 32) <= (1LL << 27); }
-cudaError_t glr_forward_launch(const Glr &p, cudaStream_t s) {
+cudaError_t glr_forward_launch(const Glr &q, cudaStream_t s) {
+    Glr p = q;
+    p.missing = missing_bytes();
     return p.dt == HLA_BF16 ? forward_of<__nv_bfloat16>(p, s) : forward_of<float>(p, s);
 }
 cudaError_t glr_step_launch(const Glr &p, cudaStream_t s) {
     return p.dt == HLA_BF16 ? step_of<__nv_bfloat16>(p, s) : step_of<float>(p, s);
 }
 size_t glr_backward_partial_floats(int B, int n, int C) { return (size_t)B * spread_bwd(B, n, C).S * C; }
-cudaError_t glr_backward_launch(const GlrBwd &p, cudaStream_t s) {
+cudaError_t glr_backward_launch(const GlrBwd &q, cudaStream_t s) {
+    GlrBwd p = q;
+    p.f.missing = missing_bytes();
     return p.f.dt == HLA_BF16 ? backward_of<__nv_bfloat16>(p, s) : backward_of<float>(p, s);
 }
 

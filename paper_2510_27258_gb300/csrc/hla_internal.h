@@ -269,6 +269,7 @@ struct Glr {
     const float *state_in;
     float *state_out;  // the step's state, updated in place
     float *marks;
+    uint32_t missing = 0;  // testing: bytes that a wait is for and that do not come
 };
 struct GlrBwd {
     Glr f;  // marks are read; y, state_in and state_out unused
@@ -315,7 +316,8 @@ size_t block_norm_partial_floats(long long rows, int C);
 cudaError_t block_norm_backward_launch(const BlockNormBwd &p, cudaStream_t stream);
 
 // sums over `rows` partial rows of `parts` runs of C floats, in a fixed order: out[i].to, unless null, receives those
-// of one run, times a factor of type dt for each column where that is given, or (kNoSum) zeros; clears the workspace's header
+// of one run, times a factor of type dt for each column where that is given, or (kNoSum) zeros; clears the
+// workspace's header, unless null
 struct ColumnSum {
     static constexpr int kNoSum = -1;
     const float *partial;
