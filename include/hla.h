@@ -485,7 +485,8 @@ hla_status hla_qk_norm_backward(const void *q, const void *k, const void *wq, co
  * Rows, strides, lengths and overlap are as above: token t of sequence b is row
  * b*n + t at a row stride in elements, and no alignment beyond the element's is
  * asked of rows.  Sums over tokens are made in a fixed order: equal inputs give
- * equal bits.  Calls that share a workspace run one after another, on one stream or ordered by
+ * equal bits.  Exponentials (of gates, of decays) are made in fp32, for fp32 tokens to the last bits, for bf16
+ * tokens to 2^-23 |v| of e^v.  Calls that share a workspace run one after another, on one stream or ordered by
  * events; a captured graph's workspace stays its own while the graph may run.  No call's workspace
  * keeps anything from one call for the next.
  */

@@ -86,14 +86,14 @@ __device__ __forceinline__ bool kept(const BlockNorm &p, long long row, int col)
     return w >= p.drop_below;
 }
 
-// act(v) and, if asked, its slope
-template <bool kSlope>
+// act(v) and, if asked, its slope, for values of type T
+template <typename T, bool kSlope>
 __device__ __forceinline__ float activation(int act, float v, float &slope) {
     if (act == HLA_LINEAR) {
         slope = 1.f;
         return v;
     }
-    const float s = __fdividef(1.f, 1.f + __expf(-v));  // (v of -89 and below: 0, as the rounded sigmoid)
+    const float s = __fdividef(1.f, 1.f + exp_minus<T>(v));  // (v of -89 and below: 0, as the rounded sigmoid)
     if (act == HLA_SIGMOID) {
         if (kSlope) slope = s * (1.f - s);
         return s;
@@ -108,7 +108,7 @@ using Pairs = uint64_t[kPairs];
 __device__ __forceinline__ uint64_t twice(float x) { return pair(x, x); }
 
 // the same of a thread's columns, two at a time
-template <bool kSlope>
+template <typename T, bool kSlope>
 __device__ __forceinline__ void activate(int act, Pairs &v, Pairs &slope) {
     if (act == HLA_LINEAR) {
 #pragma unroll
@@ -119,10 +119,7 @@ __device__ __forceinline__ void activate(int act, Pairs &v, Pairs &slope) {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
         float a, b;
-        unpair(mul2(v[i], twice(-1.44269504f)), a, b);
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(a));
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(b));
-        unpair(add2(pair(a, b), one), a, b);
+        unpair(add2(exp_minus2<T>(v[i]), one), a, b);
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(a));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(b));
         const uint64_t s = pair(a, b), r = fma2(s, minus, one);
@@ -499,7 +496,7 @@ block_norm_forward_kernel(BlockNorm p) {
         }
         if (p.gate) {
             Pairs slope;
-            activate<false>(p.act, f, slope);
+            activate<T, false>(p.act, f, slope);
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[i] = mul2(mul2(f[i], scale[i]), y[i]);
         } else {
@@ -543,7 +540,7 @@ struct Wide {
     __device__ __forceinline__ float y(int c) const { return to_f32(static_cast<const T *>(p.y)[row * p.y_stride + c]); }
     __device__ __forceinline__ float keep(int c) const { return !p.drop ? 1.f : kept(p, row, c) ? p.keep_scale : 0.f; }
     __device__ __forceinline__ float act(int c, float &slope) const {
-        return p.gate ? activation<true>(p.act, to_f32(static_cast<const T *>(p.gate)[row * p.gate_stride + c]), slope)
+        return p.gate ? activation<T, true>(p.act, to_f32(static_cast<const T *>(p.gate)[row * p.gate_stride + c]), slope)
                       : (slope = 0.f, 1.f);
     }
     // x' of one column (k, a and its slope too)
@@ -675,7 +672,7 @@ block_norm_backward_kernel(BlockNormBwd q) {
             tell<kMax>(s1, red, turn);
         }
         if (p.gate) {
-            activate<true>(p.act, f[0], f[1]);
+            activate<T, true>(p.act, f[0], f[1]);
         } else {
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) f[0][i] = f[1][i] = twice(1.f);

@@ -57,7 +57,7 @@ __device__ __forceinline__ float act_of(int act, float v, float &slope) {
         slope = 1.f;
         return v;
     }
-    const float s = __fdividef(1.f, 1.f + __expf(-v));
+    const float s = __fdividef(1.f, 1.f + exp_minus<float>(v));
     slope = act == HLA_SIGMOID ? s * (1.f - s) : s * (1.f + v * (1.f - s));
     return act == HLA_SIGMOID ? s : v * s;
 }

@@ -40,14 +40,8 @@ constexpr int kSlots = 2;
 constexpr int kSMs = 152;
 constexpr long long kWaitCycles = 4000000000ll, kLandCycles = 200000000ll;  // about 2 and 0.1 s
 constexpr uint64_t kLost = 0x7fffffff7fffffffull;  // two NaN, for states behind a wait that ran out
-constexpr float kLog2e = 1.44269504f;
 constexpr float kTiny = 1e-37f;               // beside 1 - a^2: keeps 1/m finite where a is 1
 
-__device__ __forceinline__ float ex2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 __device__ __forceinline__ float rcp(float x) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -67,8 +61,9 @@ __device__ __forceinline__ uint64_t each(uint64_t v, F f) {
 __device__ __forceinline__ uint64_t twice(float x) { return pair(x, x); }
 
 // 1 + e^-v, whose reciprocal is the sigmoid
+template <typename T>
 __device__ __forceinline__ uint64_t one_plus_exp(uint64_t v) {
-    return add2(each(mul2(v, twice(-kLog2e)), ex2), twice(1.f));
+    return add2(exp_minus2<T>(v), twice(1.f));
 }
 
 // a lane's decays, negated
@@ -83,7 +78,7 @@ struct Decay {
 };
 
 // a and w = 1 - a^2 from s
-template <bool kNear>
+template <typename T, bool kNear>
 __device__ __forceinline__ void decay_of(const Decay &d, uint64_t s, uint64_t &a, uint64_t &w) {
     // (1 - e^-v) / v on 0..1 to 1.3e-8: interpolated at the Chebyshev nodes with the value 1 at 0
     constexpr float kPoly[7] = {1.f, -0.5f, 0.166666031f, -0.0416592546f, 0.00830117054f, -0.001324818f, 0.000137424184f};
@@ -95,7 +90,7 @@ __device__ __forceinline__ void decay_of(const Decay &d, uint64_t s, uint64_t &a
     a = fma2(q, minus, twice(1.f));
     w = mul2(q, fma2(q, minus, twice(2.f)));
     if (kNear) return;
-    const uint64_t far_a = each(mul2(v, twice(-kLog2e)), ex2), far_w = fma2(mul2(far_a, minus), far_a, twice(1.f));
+    const uint64_t far_a = exp_minus2<T>(v), far_w = fma2(mul2(far_a, minus), far_a, twice(1.f));
     float v0, v1, a0, a1, w0, w1, f0, f1, g0, g1;
     unpair(v, v0, v1);
     unpair(a, a0, a1);
@@ -541,8 +536,8 @@ __global__ void __launch_bounds__(kThreads, 2) glr_forward_kernel(Glr p, int sla
                         uint64_t a, w;
                         Raw<T, 2> rr = in.get(slot, 1, t0, u);
                         if (t0 + u >= len) shut(rr);  // (x is 0 there)
-                        decay_of<near()>(decay, each(one_plus_exp(as_pair(rr)), rcp), a, w);
-                        const uint64_t d = one_plus_exp(as_pair(in.get(slot, 2, t0, u)));
+                        decay_of<T, near()>(decay, each(one_plus_exp<T>(as_pair(rr)), rcp), a, w);
+                        const uint64_t d = one_plus_exp<T>(as_pair(in.get(slot, 2, t0, u)));
                         const uint64_t x = as_pair(in.get(slot, 0, t0, u)), add = mul2(input_of(w, d), x);
                         h[u] = u ? fma2(a, h[u - 1], add) : add;
                         pr[u] = u ? mul2(a, pr[u - 1]) : a;
@@ -617,8 +612,8 @@ __global__ void __launch_bounds__(128) glr_step_kernel(Glr p, int slabs, bool ro
                    h = at.get(p.state_in + (size_t)b * p.C, pairs);
     const Decay decay(at.get(p.decay, pairs));
     uint64_t a, w;
-    decay_of<false>(decay, each(one_plus_exp(r), rcp), a, w);
-    const uint64_t d = one_plus_exp(g);
+    decay_of<T, false>(decay, each(one_plus_exp<T>(r), rcp), a, w);
+    const uint64_t d = one_plus_exp<T>(g);
     const uint64_t add = mul2(input_of(w, d), x), y = fma2(a, h, add);
     at.put(p.state_out + (size_t)b * p.C, y, pairs);
     at.put(static_cast<T *>(p.y) + (size_t)b * p.y_stride, y, rows_pairs);
@@ -694,10 +689,10 @@ __global__ void __launch_bounds__(kThreads, 2) glr_backward_kernel(GlrBwd p, int
                 uint64_t w;
                 Raw<T, 2> rr = in.get(slot, 1, t0, u);
                 if (t0 + u >= len) shut(rr);  // (x and dy are 0 there)
-                s[u] = each(one_plus_exp(as_pair(rr)), rcp);
-                decay_of<near()>(decay, s[u], a[u], w);
+                s[u] = each(one_plus_exp<T>(as_pair(rr)), rcp);
+                decay_of<T, near()>(decay, s[u], a[u], w);
                 const uint64_t rm = each(add2(w, twice(kTiny)), rsqrt_of), m = mul2(w, rm);
-                const uint64_t i = each(one_plus_exp(as_pair(in.get(slot, 2, t0, u))), rcp);
+                const uint64_t i = each(one_plus_exp<T>(as_pair(in.get(slot, 2, t0, u))), rcp);
                 const uint64_t ix = mul2(i, as_pair(in.get(slot, 0, t0, u)));
                 mi[u] = mul2(m, i);
                 rest[u] = fma2(i, minus, twice(1.f));
