@@ -224,7 +224,6 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     WsHeader *header = call.header;
     auto work_of = [&](int i) -> const Work & { return call.w[kMode == kBack && i >= call.first]; };
     auto place_of = [&](int i) { return tile_of(work_of(i), kMode == kBack && i >= call.first ? i - call.first : i); };
-    let_next_begin();
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_a);
         prefetch_tmap(&map_b);
@@ -249,6 +248,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     __syncthreads();
     cluster_meet();
     tc_fence_after();
+    let_next_begin();
     after_previous();
     if (call.clear && blockIdx.x == 0 && threadIdx.x == 0) *header = WsHeader{};  // (waits set it after seconds)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&bars->tmem);
@@ -601,7 +601,6 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     const uint32_t stage_bytes = kFewABytes + f.cols * kStep * 2;
     const uint32_t tmem_cols = f.cols <= 32 ? 32 : f.cols <= 64 ? 64 : 128;
     const int k_lo = min(rank * f.per, f.steps), k_hi = min(k_lo + f.per, f.steps);
-    let_next_begin();
     if (threadIdx.x == 0) {
         prefetch_tmap(&map_w);
         prefetch_tmap(&map_t);
@@ -620,6 +619,7 @@ ffn_few_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    let_next_begin();
     after_previous();
     if (f.clear && blockIdx.x == 0 && threadIdx.x == 0) *f.header = WsHeader{};  // (waits set it after seconds)
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&bars->tmem);

@@ -137,6 +137,8 @@ cudaError_t hla3_tc_forward(const Fwd2 &p, cudaStream_t stream);
 // calls after_previous() at the start, and in the others no thread writes to global memory before it has, or before
 // one that it waits for has.  The scans' kernels behind their segments' states read the call's inputs before they
 // wait: the kernel that sums those states waits before it lets the next one begin.
+// A block that takes tensor memory has it before it lets the next kernel begin: else a block of that one, which waits for
+// this kernel's end, may hold what this one waits for without a limit.
 // What earlier kernels write is not read through const __restrict__ pointers, whose loads may be taken for
 // those of data that does not change while the kernel is there.
 // ---------------------------------------------------------------------------

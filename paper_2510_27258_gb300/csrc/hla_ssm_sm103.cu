@@ -375,7 +375,6 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool issuer = warp == kEpiWarps;
     after_previous();
-    let_next_begin();
     const Unit u = unit_of(p);
 
     if (blockIdx.x == 0 && tid == 0) *p.err = WsHeader{};  // a wait takes seconds to give up
@@ -399,6 +398,7 @@ ssm_state_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    let_next_begin();
     const uint32_t tb = ms->tmem_base;
 
     if (issuer) {
@@ -545,7 +545,6 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     const bool issuer = warp == kIssuerWarp;
 
     if (p.segments == 1) after_previous();
-    let_next_begin();
     const Unit u = unit_of(p);
     const int b = u.b, g = u.g, h0 = u.h0, seg = u.seg, t_lo = u.t_lo, live = u.live, tiles = u.tiles;
     const bool one = u.one, both = u.both;
@@ -577,6 +576,7 @@ ssm_tc_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    let_next_begin();
     const uint32_t tb = ms->tmem_base;
 
     if (issuer) {
