@@ -18,10 +18,12 @@
 // parts are added in their order by another kernel.
 //
 // Bound by the tensor cores.  8192 x 2048 x 5632: forward 204 us in a capture of its own, 1.85 PFLOP/s, 97 % of what a
-// library product reaches in a burst (224 us one after another, at the clocks that leaves); gradient 700 us, of
-// which kBack 406 (97 %) and kGrad about 230, whose read-out of a tile (dout, two planes of dZ) takes as long as the
-// products of the next.  Up to 128 tokens, where the weights' bytes count, ffn_few_kernel: 16 tokens 8.8 us on the device,
-// 5.3 TB/s, against 18 by the tiles.
+// library product reaches in a burst (225 to 233 us one after another, at the clocks that leaves); gradient 709 to 727 us,
+// of which kBack 404 (97 %) and kGrad 223 (89 %), whose read-out of a tile (dout, two planes of dZ) takes as long as the
+// products of the next.  dZ lies in bf16 between the products: the error of dx and dw against 64 bits is 0.0023 of their norm
+// instead of the 0.0017 that their own rounding makes; fp32 would double its bytes, and the products read it twice.
+// Up to 128 tokens, where the weights' bytes count, ffn_few_kernel: 16 tokens 8.6 us on the device where the weights' 46 MB are
+// in L2, 11.3 us from memory (4.1 TB/s, 62 % of what a copy reaches).
 //
 // Every wait has a limit: it sets the workspace's error word and the block's `stop`, after which all roles leave,
 // copies and products in flight are waited for (with a limit), and tensor memory is released.
@@ -520,6 +522,7 @@ ffn_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // the same features; for dx 128 columns, against the sum's direction) for all tokens, 16 to 128 columns of one
 // product, so the products cost what the tokens need, and every SM streams weights: the sum is cut over the blocks of a
 // cluster, whose parts meet in shared memory and are added in the blocks' order, each block finishing some of the tokens.
+// The cuts are powers of two, so the SMs' shares are uneven: with F 5632 176 blocks, of which 24 SMs have two.
 // ------------------------------------------------------------------------------------------------
 
 constexpr int kFewMost = 128, kFewThreads = 192, kFewStages = 8;
@@ -872,7 +875,8 @@ cudaError_t run_few(const CUtensorMap &weights, const CUtensorMap &tokens, Few f
 }
 
 // Up to 128 tokens, where the tiles of 256 x 256 would leave pairs without one (16 x 2048 x 5632: 9 us on the device
-// instead of 18; above, the tiles cost no more than the tokens' own products)
+// instead of 18, weights in L2; above, the tiles cost no more than the tokens' own products.  1 x 4096 x 14336 by the tiles:
+// 74 us, where the weights' bytes take 35)
 bool few(int M, int F) { return M <= kFewMost && tiles_of(F, kHalf) < kPairs; }
 int few_cols(int M) { return (M + 15) / 16 * 16; }
 

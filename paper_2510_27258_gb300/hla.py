@@ -926,7 +926,7 @@ def hla_block_norm_backward(x, y, gate, dx_out, dh=None, dx=None, dy=None, dgate
                             seed=0, offset=0, workspace=None, stream=None):
     """Gradients (dx, dy, dgate, dw_post, dscale, dw_pre) of sum(dx_out * x_out) + sum(dh * h) for
     hla_block_norm_forward with the same arguments (include/hla.h: hla_block_norm_backward); the weights' are fp32 [C],
-    None where the weight is not given; dgate is None without a gate.  dx may be dx_out."""
+    None where the weight is not given or its norm is off; dgate is None without a gate.  dx may be dx_out."""
     shape, rows, C, T, dt, i, given, strides = _norm_args(x, y, gate, w_post, scale, w_pre, post_norm, pre_norm)
     handle, side = _on(stream, i)
     dx = _like(x, side) if dx is None else dx
