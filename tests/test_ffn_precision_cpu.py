@@ -7,6 +7,15 @@ import block_ref as R
 import ffn_precision as P
 
 
+@pytest.fixture(autouse=True, scope="module")
+def one_thread():
+    """(tests of several processes fork this one, which is safe while no pool of threads has been started)"""
+    threads = torch.get_num_threads()
+    torch.set_num_threads(1)
+    yield
+    torch.set_num_threads(threads)
+
+
 def cut(t, bits):
     """Rounded to `bits` bits of mantissa."""
     m, e = torch.frexp(t.double())
