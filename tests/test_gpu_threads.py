@@ -40,13 +40,15 @@ def both(calls, times):
 
 def feed_forward(hla, M):
     x, w = (torch.randn(*s, device=DEV).to(torch.bfloat16) for s in ((M, 256), (2, 512, 256)))
-    out, ws = torch.empty(M, 512, dtype=x.dtype, device=DEV), hla.alloc_workspace(hla.hla_ffn_workspace_bytes(M, 256, 512, x.dtype), DEV)
+    out = torch.empty(M, 512, dtype=x.dtype, device=DEV)
+    ws = hla.alloc_workspace(hla.hla_ffn_workspace_bytes(M, 256, 512, x.dtype), DEV)
     return lambda: hla.hla_ffn_forward(x, w, out, workspace=ws)
 
 
 def norm_gradient(hla, C, T):
     x = torch.randn(8, C, device=DEV).to(T)
-    ws, dx, dy = hla.alloc_workspace(hla.hla_block_norm_backward_workspace_bytes(8, C, T), DEV), torch.empty_like(x), torch.empty_like(x)
+    ws = hla.alloc_workspace(hla.hla_block_norm_backward_workspace_bytes(8, C, T), DEV)
+    dx, dy = torch.empty_like(x), torch.empty_like(x)
     return lambda: hla.hla_block_norm_backward(x, x, None, x, x, dx, dy, workspace=ws)
 
 
